@@ -31,11 +31,10 @@ def listed():
         _attention("attention packed documents", S=64, n=384, H=12, HK=12, causal=False, docs=4),
         # prompts of 1,024 tokens whose first 512 (a shared document) are seen in both directions
         _attention("attention prefix of 512", S=32, n=1024, H=12, HK=12, causal=True, prefix=512),
-        # two long prompts with grouped heads, capped scores and a linear bias, in [sequence, head, token] layout
+        # two long rows of packed documents with grouped heads, capped scores and a linear bias, in [sequence, head, token]
+        # layout
         _attention("attention capped, long, grouped heads", S=2, n=4001, H=16, HK=4, causal=True, cap=30.0, bias="slopes",
-                   layout="heads_first"),
-        # packed documents of a causal model with a linear bias, odd row length
-        _attention("attention causal documents, slopes", S=8, n=2047, H=16, HK=16, causal=True, bias="slopes", docs=5),
+                   docs=2, layout="heads_first"),
         # the next token of one sequence: latency
         _chunk("chunk one token", B=1, lo=517, hi=517, rows=1, H=12, HK=12, page=16),
         # the next token of 64 sequences of uneven lengths, with the received attention recorded
@@ -45,6 +44,9 @@ def listed():
         # the last tokens of two long prompts: their attention decides what the cache keeps
         _chunk("chunk over long caches, capped, weights", B=2, lo=17003, hi=30001, rows=250, H=16, HK=4, page=32, cap=30.0,
                bias="slopes", weights=True),
+        # a batch goes on after an eviction: the entries of every head have positions of their own
+        _chunk("chunk after an eviction, table", B=16, lo=513, hi=640, rows=33, H=12, HK=12, page=16, bias="table", evicted=True,
+               weights=True),
         # one sequence goes back from 640 entries to 512: latency
         _evict("evict one sequence", B=1, lo=640, hi=640, HK=12, page=16, budget=512, recent=64, sinks=4),
         # a batch of uneven lengths is cut to 512 entries
@@ -59,8 +61,9 @@ def _attention(name, S, n, H, HK, causal, cap=0.0, bias="none", docs=0, prefix=0
                 layout=layout)
 
 
-def _chunk(name, B, lo, hi, rows, H, HK, page, cap=0.0, bias="none", weights=False):
-    return dict(name=name, op="chunk", B=B, lo=lo, hi=hi, rows=rows, H=H, HK=HK, page=page, cap=cap, bias=bias, weights=weights)
+def _chunk(name, B, lo, hi, rows, H, HK, page, cap=0.0, bias="none", weights=False, evicted=False):
+    return dict(name=name, op="chunk", B=B, lo=lo, hi=hi, rows=rows, H=H, HK=HK, page=page, cap=cap, bias=bias, weights=weights,
+                evicted=evicted)
 
 
 def _evict(name, B, lo, hi, HK, page, budget, recent, sinks):
@@ -89,7 +92,8 @@ def draw(rng):
         hi = max(rows, _spread(rng, 1, 30000))
         most = max(1, min(64, int(32 * 512 * 1024 * 12 / (rows * hi * H)), int(64 * 4100 * 4 * 2 / (hi * HK))))
         c = _chunk("", B=_spread(rng, 1, most), lo=max(rows, int(hi * rng.uniform(0.1, 1.0))), hi=hi, rows=rows, H=H, HK=HK,
-                   page=rng.choice([16, 32, 64, 128]), cap=cap, bias=bias, weights=rng.random() < 0.5)
+                   page=rng.choice([16, 32, 64, 128]), cap=cap, bias=bias, weights=rng.random() < 0.5,
+                   evicted=rng.random() < 0.25)
     else:
         hi = _spread(rng, 1, 32000)
         budget = _spread(rng, 1, min(8192, hi))
@@ -143,7 +147,7 @@ def work(case):
         pairs = sum(r * (n - r) + r * (r + 1) // 2 for r, n in zip(rows, lens))
         T, keys = sum(rows), sum(lens)
         # cached keys and values read, new ones read and written, queries read, outputs written, a weight per key written
-        bytes_ = (keys - T) * HK * DH * 4 + 2 * T * HK * DH * 4 + T * H * (DH * 4 + 4) + (keys * HK * 4 if case["weights"] else 0)
+        bytes_ = (keys - T) * HK * DH * 4 + 2 * T * HK * DH * 4 + T * H * (DH * 4 + 4) + keys * HK * (4 * case["weights"] + 4 * case["evicted"])
         return {"bytes": bytes_, "flops": (6 if case["weights"] else 4) * DH * H * pairs}
     kept = sum(min(n, case["budget"]) for n in lens)
     # every entry's weight and position is read; kept rows are read and written, their weights and positions written
@@ -224,10 +228,7 @@ def prepare(case, seed):
         used[0] = False
     for t in (st["k"], st["v"]):
         t.masked_fill_(~used.view(pages, 1, ps, 1), float("nan"))
-    place = torch.zeros((pages, ps), dtype=torch.int32, device=DEV)
-    place[st["pages"].long().view(-1)[(st["pages"] >= 0).view(-1)]] = slot.expand(B, -1, ps).reshape(-1, ps)[
-        (st["pages"] >= 0).view(-1)].int()
-    st["positions"] = place.view(pages, 1, ps).expand(pages, HK, ps).contiguous()
+    width = max(need) * ps
 
     if case["op"] == "chunk":
         H = case["H"]
@@ -239,26 +240,32 @@ def prepare(case, seed):
         st["q"], st["k_new"], st["v_new"] = qkv[:, :H], qkv[:, H:H + HK], qkv[:, H + HK:]
         st["q"].mul_(2.0)
         st["slopes"], st["bias"] = _bias(case, g)
-        st["weights"] = torch.zeros((pages, HK, ps), dtype=torch.float32, device=DEV) if case["weights"] else None
+        st["weights"] = torch.zeros((B, HK, width), dtype=torch.float32, device=DEV) if case["weights"] else None
+        st["positions"] = st["first"] = None
+        if case["evicted"]:                              # entries of positions with gaps, the new rows behind them
+            gaps = torch.randint(1, 4, (B, HK, width), generator=g, device=DEV)
+            st["positions"] = (gaps.cumsum(-1) - 1).int()
+            st["first"] = torch.tensor([3 * n for n in lens], dtype=torch.int32, device=DEV)
         st["out"] = torch.empty((T, H, DH), dtype=torch.bfloat16, device=DEV)
         st["lse"] = torch.empty((T, H), dtype=torch.float32, device=DEV)
         if own:
             from paper_2512_16843_b200 import binding as L
             st["mods"] = L.make_score_mods(causal=True, cap=case["cap"], slopes=st["slopes"], table=st["bias"])
-            st["cache"] = L.KVCache(st["k"], st["v"], heads=H, max_seqs=B, max_rows=T, max_len=max(need) * ps,
-                                    weights=st["weights"])
+            st["cache"] = L.KVCache(st["k"], st["v"], heads=H, max_seqs=B, max_rows=T, max_len=width)
         return st
 
     # weights as attention leaves them: most entries got little, some a lot
-    st["weights"] = torch.exp(1.5 * torch.randn((pages, HK, ps), generator=g, device=DEV) - 2.0)
+    st["weights"] = torch.exp(1.5 * torch.randn((B, HK, width), generator=g, device=DEV) - 2.0)
+    st["positions"] = torch.arange(width, dtype=torch.int32, device=DEV).expand(B, HK, width).contiguous()
+    st["new_weights"] = torch.zeros((B, HK, case["budget"]), device=DEV)
+    st["new_positions"] = torch.zeros((B, HK, case["budget"]), dtype=torch.int32, device=DEV)
     new = ids[at:at + B * fresh].reshape(B, fresh)
     st["new_pages"] = torch.from_numpy(np.ascontiguousarray(new)).to(DEV)
     st["new_lens"] = torch.zeros(B, dtype=torch.int32, device=DEV)
     st["kept"] = torch.empty((B, HK, case["budget"]), dtype=torch.int32, device=DEV)
     if own:
         from paper_2512_16843_b200 import binding as L
-        st["cache"] = L.KVCache(st["k"], st["v"], heads=HK, max_seqs=B, max_rows=B, max_len=max(need) * ps,
-                                weights=st["weights"], positions=st["positions"])
+        st["cache"] = L.KVCache(st["k"], st["v"], heads=HK, max_seqs=B, max_rows=B, max_len=width)
     return st
 
 
@@ -274,11 +281,13 @@ def run(st):
             # the weights of this chunk's queries alone (decay 0): what earlier chunks gave is forgotten
             st["cache"].attention(st["q"], st["out"], cu_rows=st["cu"], lens=st["lens"], pages=st["pages"],
                                   longest=st["most_rows"], k_new=st["k_new"], v_new=st["v_new"], lse=st["lse"],
-                                  mods=st["mods"], decay=0.0 if case["weights"] else None)
+                                  mods=st["mods"], weights=st["weights"], decay=0.0, positions=st["positions"], first=st["first"])
             return _chunk_answer(st, st["out"], st["lse"])
-        st["cache"].evict(lens=st["lens"], pages=st["pages"], new_pages=st["new_pages"], new_lens=st["new_lens"],
-                          budget=case["budget"], recent=case["recent"], sinks=case["sinks"], kept=st["kept"])
-        return _evict_answer(st, st["new_lens"], st["kept"])
+        st["cache"].evict(lens=st["lens"], pages=st["pages"], weights=st["weights"], positions=st["positions"],
+                          new_pages=st["new_pages"], new_lens=st["new_lens"], new_weights=st["new_weights"],
+                          new_positions=st["new_positions"], kept=st["kept"], budget=case["budget"], recent=case["recent"],
+                          sinks=case["sinks"])
+        return _evict_answer(st, st["new_weights"], st["new_positions"], st["new_lens"], st["kept"])
     return {"attention": _plain_attention, "chunk": _plain_chunk, "evict": _plain_evict}[case["op"]](st)
 
 
@@ -286,11 +295,13 @@ def _chunk_answer(st, out, lse):
     answer = {"out": out, "lse": lse, "k": st["k"], "v": st["v"]}
     if st["weights"] is not None:
         answer["weights"] = st["weights"]
+    if st["positions"] is not None:
+        answer["positions"] = st["positions"]
     return answer
 
 
-def _evict_answer(st, new_lens, kept):
-    return {"k": st["k"], "v": st["v"], "weights": st["weights"], "positions": st["positions"], "new_lens": new_lens, "kept": kept}
+def _evict_answer(st, weights, positions, new_lens, kept):
+    return {"k": st["k"], "v": st["v"], "weights": weights, "positions": positions, "new_lens": new_lens, "kept": kept}
 
 
 def _softmax(s, seen):
@@ -304,17 +315,17 @@ def _softmax(s, seen):
 
 
 def _modified(s, case, slopes, table, apart):
-    """The scaled products s [.., HK, G, rows, keys], capped and biased; apart: key position - query position."""
-    G = case["H"] // case["HK"]
+    """The scaled products s [.., HK, G, rows, keys], capped and biased; apart [.., 1 or HK, 1, rows, keys]: key position -
+    query position."""
+    HK, G = case["HK"], case["H"] // case["HK"]
     if case["cap"]:
         s = case["cap"] * torch.tanh(s / case["cap"])
     if slopes is not None:
-        s = s - slopes.view(-1, G, 1, 1) * apart.abs().float()
+        s = s - slopes.view(HK, G, 1, 1) * apart.abs().float()
     if table is not None:
         reach = table.shape[1] // 2
-        per_head = table.view(-1, G, table.shape[1])
-        value = per_head[:, :, (apart.reshape(-1, *apart.shape[-2:]).clamp(-reach, reach) + reach).long()]     # [HK, G, *, rows, keys]
-        s = s + value.movedim(2, 0)
+        hk, g = torch.arange(HK, device=DEV).view(HK, 1, 1, 1), torch.arange(G, device=DEV).view(G, 1, 1)
+        s = s + table.view(HK, G, 2 * reach + 1)[hk, g, (apart.clamp(-reach, reach) + reach).long()]
     return s
 
 
@@ -325,7 +336,7 @@ def _plain_attention(st):
     k, v = (st[x].float().permute(0, 2, 1, 3).unsqueeze(2) for x in ("k", "v"))
     at = torch.arange(n, device=DEV)
     apart = at.view(1, n) - at.view(n, 1)
-    s = _modified(torch.matmul(q, k.transpose(-1, -2)) * DH ** -0.5, case, st["slopes"], st["table"], apart)
+    s = _modified(torch.matmul(q, k.transpose(-1, -2)) * DH ** -0.5, case, st["slopes"], st["table"], apart.view(1, 1, n, n))
     seen = torch.ones((1, n, n), dtype=torch.bool, device=DEV)
     if case["causal"]:
         seen = (apart <= 0).view(1, n, n)
@@ -365,19 +376,17 @@ def _plain_chunk(st):
     real = i.view(1, most) < count.view(B, 1)
     q = st["q"].float()[(cu[:-1].view(B, 1) + i.view(1, most)).clamp(max=T - 1)]
     q = q.view(B, most, HK, H // HK, DH).permute(0, 2, 3, 1, 4)
-    mine = (lens - count).view(B, 1) + i.view(1, most)                       # position of every query
-    apart = torch.arange(width, device=DEV).view(1, 1, 1, 1, width) - mine.view(B, 1, 1, most, 1)
+    behind = torch.arange(width, device=DEV).view(1, 1, 1, 1, width) - ((lens - count).view(B, 1) + i.view(1, most)).view(B, 1, 1, most, 1)
+    apart = behind
+    if st["positions"] is not None:
+        st["positions"].transpose(1, 2)[seq, slot] = (st["first"][seq] + (row - cu[seq]).int()).view(T, 1)
+        apart = st["positions"].view(B, HK, 1, 1, width) - (st["first"].view(B, 1) + i.view(1, most)).view(B, 1, 1, most, 1)
     s = _modified(torch.matmul(q, k.transpose(-1, -2)) * DH ** -0.5, case, st["slopes"], st["bias"], apart)
-    seen = (apart <= 0) & there.view(B, 1, 1, 1, width) & real.view(B, 1, 1, most, 1)
+    seen = (behind <= 0) & there.view(B, 1, 1, 1, width) & real.view(B, 1, 1, most, 1)
     p, lse = _softmax(s, seen)
     out = torch.matmul(p, v).permute(0, 3, 1, 2, 4).reshape(B, most, H, DH)
     if st["weights"] is not None:
-        got = p.sum((2, 3)).transpose(1, 2)                                  # [B, width, HK]
-        # (slots that are not there point at page 0: they add nothing to what its owner has)
-        new, written = torch.zeros_like(st["weights"]), torch.zeros_like(st["weights"][:, 0])
-        new.permute(0, 2, 1).index_put_((page, place), torch.where(there.unsqueeze(-1), got, 0.0), accumulate=True)
-        written.index_put_((page, place), there.float(), accumulate=True)
-        st["weights"].copy_(torch.where(written.unsqueeze(1) > 0, new, st["weights"]))
+        st["weights"].copy_(torch.where(there.view(B, 1, width), p.sum((2, 3)), st["weights"]))
     pick = (seq, row - cu[seq])
     return _chunk_answer(st, out[pick].to(torch.bfloat16), lse.permute(0, 3, 1, 2).reshape(B, most, H)[pick])
 
@@ -387,8 +396,7 @@ def _plain_evict(st):
     B, HK, budget, ps = case["B"], case["HK"], case["budget"], case["page"]
     width = st["pages"].shape[1] * ps
     page, place, there = _slots(st, width)
-    w = st["weights"][page, :, place].transpose(1, 2)                        # [B, HK, width]
-    pos = st["positions"][page, :, place].transpose(1, 2)
+    w, pos = st["weights"], st["positions"]                                  # [B, HK, width]
     there = there.unsqueeze(1).expand_as(w)
     last = torch.where(there, pos, -1).amax(-1, keepdim=True)
     safe = (pos < case["sinks"]) | (pos > last - case["recent"])
@@ -405,11 +413,11 @@ def _plain_evict(st):
     to = torch.arange(budget, device=DEV)
     to_page = st["new_pages"].long()[:, to // ps].unsqueeze(1).expand_as(src)
     to_place = (to % ps).view(1, 1, -1).expand_as(src)
-    for x in ("k", "v", "weights", "positions"):
-        t = st[x]
+    for t in (st["k"], st["v"]):
         moved, before = t[from_page, head, from_place], t[to_page, head, to_place]
-        t[to_page, head, to_place] = torch.where(real.unsqueeze(-1) if t.dim() == 4 else real, moved, before)
-    return _evict_answer(st, new_lens, torch.where(real, kept, -1).to(torch.int32))
+        t[to_page, head, to_place] = torch.where(real.unsqueeze(-1), moved, before)
+    new_weights, new_positions = torch.where(real, w.gather(2, src), 0.0), torch.where(real, pos.gather(2, src), 0)
+    return _evict_answer(st, new_weights, new_positions, new_lens, torch.where(real, kept, -1).to(torch.int32))
 
 
 # ------------------------------------------------------------------------------------------- the definition, exactly
@@ -454,20 +462,24 @@ def exact(case, seed):
 
     T, H, ps = st["q"].shape[0], case["H"], case["page"]
     out, lse = torch.empty((T, H, DH), dtype=f8, device=DEV), torch.empty((T, H), dtype=f8, device=DEV)
-    weights = torch.zeros(st["k"].shape[:3], dtype=f8, device=DEV)
+    weights = torch.zeros((case["B"], case["HK"], st["pages"].shape[1] * ps), dtype=f8, device=DEV)
     t0 = 0
     for b, (n, r) in enumerate(zip(st["host_lens"], st["rows"])):
-        kpos = torch.arange(n, device=DEV)
-        qpos = kpos[n - r:]
-        page, place = st["pages"][b].long()[kpos // ps], kpos % ps
+        slot = torch.arange(n, device=DEV)
+        vis = slot[None, :] <= slot[n - r:, None]
+        kpos, qpos = slot, slot[n - r:]
+        page, place = st["pages"][b].long()[slot // ps], slot % ps
         for hk in range(case["HK"]):
             k = torch.cat([st["k"][page, hk, place][:n - r], st["k_new"][t0:t0 + r, hk]])
             v = torch.cat([st["v"][page, hk, place][:n - r], st["v_new"][t0:t0 + r, hk]])
+            if case["evicted"]:
+                qpos = int(st["first"][b]) + slot[:r]
+                kpos = torch.cat([st["positions"][b, hk, :n - r].long(), qpos])
             for h in range(hk * G, hk * G + G):
-                out[t0:t0 + r, h], lse[t0:t0 + r, h], p = head(st["q"][t0:t0 + r, h], k, v, h, qpos, kpos, kpos[None, :] <= qpos[:, None])
-                weights[page, hk, place] += p.sum(0)
+                out[t0:t0 + r, h], lse[t0:t0 + r, h], p = head(st["q"][t0:t0 + r, h], k, v, h, qpos, kpos, vis)
+                weights[b, hk, :n] += p.sum(0)
         t0 += r
-    answer = {"out": out, "lse": lse, "k": None, "v": None}
+    answer = {"out": out, "lse": lse, "k": None, "v": None, "positions": None}
     if case["weights"]:
         answer["weights"] = weights
     return answer
