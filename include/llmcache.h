@@ -438,6 +438,152 @@ int llmcache_divergence_check(llmcache_bank_t* bank, llmcache_layer_t* layer, co
                               const llmcache_probe_io* io, uint32_t stride, float bound, void* h_sample,
                               void* out_sample, float* rel_out, uint32_t* counters_dev, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Attention as operators of their own: over whole sequences with score modifiers (llmcache_attention, and
+ * inside llmcache_layer_forward), over a paged key/value cache for a chunk of new tokens or a single one
+ * (llmcache_kv_attention, and inside llmcache_layer_extend), and the eviction of cached tokens by the
+ * attention they received (llmcache_kv_evict).  Heads have 64 columns and are bf16, as in the layers; scores,
+ * softmax statistics and recorded weights are f32, products of two bf16 matrices accumulate in f32.
+ * ------------------------------------------------------------------------------------------------ */
+
+/* What happens to the score of query i and key j (positions within the sequence) of head h before the softmax:
+ *     z = scale * <q_i, k_j>;   cap > 0: z = cap * tanh(z / cap);
+ *     slopes: z -= slopes[h] * |i - j|;   table: z += table[h][clamp(j - i, -reach, reach) + reach]
+ * and which keys a query sees:
+ *     (not causal, or j <= i, or j < prefix[s])  and  (no doc, or doc[s][i] == doc[s][j] >= 0).
+ * A key that a query does not see takes no part in that query's output, whatever the key's row holds (infinities
+ * and NaN included).  A query that sees no key, or only keys of score -inf, gets a row of zeros and lse = -inf.
+ * Zero-initialise, set struct_size = sizeof, fill in; all pointers are DEVICE memory. */
+typedef struct llmcache_score_mods {
+  uint32_t struct_size;
+  uint32_t causal;
+  float    scale;            /* 0 => 1/8 = 1/sqrt(64); must not be negative */
+  float    cap;              /* 0 => scores are not capped; at least 1e-3 otherwise */
+  uint32_t reach;            /* table: largest distance with an entry of its own, <= 1,024 */
+  const float*   slopes;     /* f32 [heads], or NULL */
+  const float*   table;      /* f32 [heads, 2 * reach + 1], or NULL; entries may be -inf */
+  const int32_t* doc;        /* i32 [n_seqs, seq_len] document of every token, < 0: padding; or NULL */
+  const int32_t* prefix;     /* i32 [n_seqs], keys below it are seen by every query (causal only); or NULL */
+} llmcache_score_mods;
+
+/* A bf16 array of rows of 64 columns: element c of head h of token t of sequence s is
+ * ptr[s * seq_stride + t * tok_stride + h * head_stride + c].  Strides are counted in elements, multiples of 8;
+ * ptr is 16-byte aligned. */
+typedef struct llmcache_rows {
+  void*   ptr;
+  int64_t seq_stride, tok_stride, head_stride;
+} llmcache_rows;
+
+/* out = softmax(z) v over whole sequences of seq_len tokens.  q, out: heads heads; k, v: kv_heads heads, a divisor of
+ * heads (query head h reads key/value head h / (heads / kv_heads)); lse: optional f32 [n_seqs, seq_len, heads], natural
+ * logarithm of the sum of exp(z).  mods: NULL = plain attention.  n_seqs_dev: optional DEVICE u32, only
+ * min(n_seqs, *n_seqs_dev) sequences are processed and the rows of the others stay as they were.  Takes no object:
+ * runs on the CURRENT device, allocates nothing, does not synchronise.  out must not overlap an input.  A stride
+ * must be positive where its dimension is larger than one.  The first call on a device looks up an address and sets
+ * kernel attributes: make it outside any stream capture. */
+int llmcache_attention(const llmcache_rows* q, const llmcache_rows* k, const llmcache_rows* v, const llmcache_rows* out,
+                       uint32_t n_seqs, uint32_t seq_len, uint32_t heads, uint32_t kv_heads, const uint32_t* n_seqs_dev,
+                       const llmcache_score_mods* mods, float* lse, void* stream);
+/* LLMCACHE_OK, or LLMCACHE_ERR_TIMEOUT once a bounded device-side wait of llmcache_attention has expired on the current
+ * device (sticky).  Synchronises the device. */
+int llmcache_attention_status(void);
+/* As llmcache_bank_debug_knobs, for llmcache_attention on the current device (which it must have run on before). */
+int llmcache_attention_debug_knobs(uint64_t wait_limit_ns, uint32_t flags);
+
+/* A paged key/value cache.  The caller owns the pages and hands them out; the object holds what describes them and
+ * scratch for one call.  Slot j of a sequence lies in page pages[j / page_size] at place j % page_size; the page
+ * arrays are bf16 [num_pages][kv_heads][page_size][64], page_stride elements from page to page.  Sequences may share
+ * pages.  An object must be driven from one stream at a time (graphs captured from it included). */
+typedef struct llmcache_kv llmcache_kv_t;
+
+typedef struct llmcache_kv_desc {
+  uint32_t struct_size;
+  int32_t  device;
+  uint32_t heads, kv_heads;  /* heads: a multiple of kv_heads */
+  uint32_t num_pages;
+  uint32_t page_size;        /* 16, 32, 64, 128 or 256 */
+  uint32_t max_seqs;         /* most sequences of one call */
+  uint32_t max_rows;         /* most new tokens of one call, all sequences together */
+  uint32_t max_len;          /* most slots of one sequence */
+  void*    k_pages;          /* DEVICE, 16-byte aligned, borrowed: they must outlive the object */
+  void*    v_pages;
+  uint64_t page_stride;      /* elements, a multiple of 64; 0 => kv_heads * page_size * 64 */
+  void*    workspace;        /* device scratch (256-byte aligned) or NULL => the library cudaMallocs it */
+  size_t   workspace_bytes;  /* llmcache_kv_bytes tells how much is needed */
+} llmcache_kv_desc;
+
+/* New tokens of a batch: sequence s brings the rows cu_rows[s] .. cu_rows[s+1]-1 of q (and k_new, v_new).  lens[s] counts
+ * its slots with these tokens included: row r takes slot lens[s] - (cu_rows[s+1] - r).  Rows behind
+ * cu_rows[n_seqs] are left as they were.  Zero-initialise, set struct_size = sizeof, fill in. */
+typedef struct llmcache_kv_chunk {
+  uint32_t struct_size;
+  uint32_t n_seqs;
+  uint32_t n_rows;           /* rows of q, out, lse */
+  uint32_t longest;          /* most rows of one sequence (rows beyond it are not computed); 0 => n_rows */
+  const int32_t* cu_rows;    /* i32 [n_seqs + 1], ascending from 0 to at most n_rows */
+  const int32_t* lens;       /* i32 [n_seqs], at most max_len and pages_ld * page_size (more is taken as that) */
+  const int32_t* pages;      /* i32 [n_seqs, pages_ld]; an id outside [0, num_pages): its slots are seen by nobody
+                                and rows that belong there are not stored */
+  uint32_t pages_ld;
+  float    decay;            /* weights: factor of what is there, 0 <= decay <= 1; 0 does not read it */
+  llmcache_rows q, out;      /* heads heads; seq_stride is not used */
+  llmcache_rows k_new, v_new;/* kv_heads heads, stored in the pages before the attention; ptr NULL (both): they are there */
+  float*   lse;              /* optional f32 [n_rows, heads] */
+  float*   weights;          /* optional f32 [n_seqs, kv_heads, side_ld]: slots below lens[s] become decay * weight + the
+                                sum of the softmax over this call's rows and the heads that share the key */
+  int32_t* positions;        /* optional i32 [n_seqs, kv_heads, side_ld]: position of every slot for the distance bias
+                                (NULL: the slot); written for new rows: first[s] + row of the sequence */
+  const int32_t* first;      /* i32 [n_seqs], position of a sequence's first new row; NULL: its slot */
+  uint64_t side_ld;          /* at least min(max_len, pages_ld * page_size) where weights or positions are given */
+  const llmcache_score_mods* mods;   /* NULL: plain causal; doc and prefix are refused (LLMCACHE_ERR_UNSUPPORTED) */
+} llmcache_kv_chunk;
+
+/* Keeps, per sequence and key/value head, at most `budget` of the lens[s] slots: first those with a position below
+ * `sinks` or among the last `recent` positions (above the head's largest position - recent), then those of the largest
+ * weight (not a number and below zero count as zero), the lower slot on equal weights.  They are copied in slot order
+ * to the slots 0 .. new_lens[s]-1 of new_pages, new_lens[s] = min(lens[s], budget); the old pages stay as they are. */
+typedef struct llmcache_kv_eviction {
+  uint32_t struct_size;
+  uint32_t n_seqs;
+  uint32_t budget;           /* >= 1, <= max_len */
+  uint32_t recent, sinks;    /* recent + sinks <= budget */
+  uint32_t pages_ld, new_pages_ld;   /* new_pages_ld * page_size >= budget */
+  const int32_t* lens;       /* i32 [n_seqs] */
+  const int32_t* pages;      /* i32 [n_seqs, pages_ld] */
+  const int32_t* new_pages;  /* i32 [n_seqs, new_pages_ld]; pages that no sequence of the call reads or gets twice */
+  int32_t* new_lens;         /* i32 [n_seqs]; may be lens */
+  const float*   weights;    /* f32 [n_seqs, kv_heads, side_ld] */
+  const int32_t* positions;  /* i32 [n_seqs, kv_heads, side_ld], or NULL: the slot */
+  uint64_t side_ld;          /* >= min(max_len, pages_ld * page_size) */
+  float*   new_weights;      /* optional f32 [n_seqs, kv_heads, new_side_ld]; entries new_lens[s] .. budget-1: 0 */
+  int32_t* new_positions;    /* optional i32 [n_seqs, kv_heads, new_side_ld]; likewise */
+  uint64_t new_side_ld;      /* >= budget */
+  int32_t* kept;             /* optional i32 [n_seqs, kv_heads, budget]: the slots kept, ascending, then -1 */
+} llmcache_kv_eviction;
+
+int llmcache_kv_bytes(const llmcache_kv_desc* desc, size_t* bytes_out);
+int llmcache_kv_create(const llmcache_kv_desc* desc, llmcache_kv_t** kv_out);    /* synchronous */
+int llmcache_kv_destroy(llmcache_kv_t* kv);                                      /* synchronises the device */
+int llmcache_kv_attention(llmcache_kv_t* kv, const llmcache_kv_chunk* chunk, void* stream);
+int llmcache_kv_evict(llmcache_kv_t* kv, const llmcache_kv_eviction* eviction, void* stream);
+/* LLMCACHE_OK or LLMCACHE_ERR_TIMEOUT (a bounded device-side wait expired).  Synchronises the device. */
+int llmcache_kv_status(llmcache_kv_t* kv);
+/* As llmcache_bank_debug_knobs, for the cache's kernels. */
+int llmcache_kv_debug_knobs(llmcache_kv_t* kv, uint64_t wait_limit_ns, uint32_t flags);
+
+/* Score modifiers of the layer's attention in the forward calls that follow; NULL switches them off.  The struct is
+ * copied, the arrays it points at are borrowed.  causal must equal the layer's.  doc and prefix are indexed by the
+ * sequence's place in the forward call; a layer that has them is refused (LLMCACHE_ERR_UNSUPPORTED) by llmcache_infer
+ * with banks and by llmcache_divergence_check, where sequences change their places and a match does not look at masks. */
+int llmcache_layer_score_mods(llmcache_layer_t* layer, const llmcache_score_mods* mods);
+
+/* The layer on new tokens only: out[r] = f_l(x[r]) for the rows of `chunk` (x, out: bf16 [n_rows, d], not overlapping),
+ * whose keys and values are stored in kv and which attend to everything their sequences have there.  For causal layers;
+ * kv must have the layer's heads as heads and kv_heads.  chunk->q, k_new, v_new, out and mods are not looked at (the
+ * layer's own take their place; doc and prefix are refused); n_rows <= max_seqs * seq_len of the layer. */
+int llmcache_layer_extend(llmcache_layer_t* layer, llmcache_kv_t* kv, const void* x, const llmcache_kv_chunk* chunk,
+                          void* out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -39,6 +39,9 @@ EXPORTS = [
     "llmcache_infer_pooled", "llmcache_fingerprint_static_status", "llmcache_bank_debug_knobs",
     "llmcache_layer_debug_knobs", "llmcache_debug_bounds_build", "llmcache_bank_input_stable",
     "llmcache_shard_scan", "llmcache_shard_decide", "llmcache_embed",
+    "llmcache_attention", "llmcache_attention_status", "llmcache_attention_debug_knobs", "llmcache_kv_bytes",
+    "llmcache_kv_create", "llmcache_kv_destroy", "llmcache_kv_attention", "llmcache_kv_evict", "llmcache_kv_status",
+    "llmcache_kv_debug_knobs", "llmcache_layer_score_mods", "llmcache_layer_extend",
 ]
 KNOB_PRODUCER_IDLE = 1
 FINGERPRINT_STATIC_MAX_FLOATS = 2 * 1024 * 1024
@@ -76,6 +79,46 @@ class LayerDesc(C.Structure):
         ("ln1_g", C.c_void_p), ("ln1_b", C.c_void_p), ("w_1", C.c_void_p), ("b_1", C.c_void_p),
         ("w_2", C.c_void_p), ("b_2", C.c_void_p), ("ln2_g", C.c_void_p), ("ln2_b", C.c_void_p),
         ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class ScoreMods(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("causal", C.c_uint32), ("scale", C.c_float), ("cap", C.c_float),
+        ("reach", C.c_uint32), ("slopes", C.c_void_p), ("table", C.c_void_p), ("doc", C.c_void_p), ("prefix", C.c_void_p),
+    ]
+
+
+class Rows(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("seq_stride", C.c_int64), ("tok_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class KVDesc(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("device", C.c_int32), ("heads", C.c_uint32), ("kv_heads", C.c_uint32),
+        ("num_pages", C.c_uint32), ("page_size", C.c_uint32), ("max_seqs", C.c_uint32), ("max_rows", C.c_uint32),
+        ("max_len", C.c_uint32), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_uint64),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class KVChunk(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("n_seqs", C.c_uint32), ("n_rows", C.c_uint32), ("longest", C.c_uint32),
+        ("cu_rows", C.c_void_p), ("lens", C.c_void_p), ("pages", C.c_void_p), ("pages_ld", C.c_uint32),
+        ("decay", C.c_float), ("q", Rows), ("out", Rows), ("k_new", Rows), ("v_new", Rows), ("lse", C.c_void_p),
+        ("weights", C.c_void_p), ("positions", C.c_void_p), ("first", C.c_void_p), ("side_ld", C.c_uint64),
+        ("mods", C.POINTER(ScoreMods)),
+    ]
+
+
+class KVEviction(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("n_seqs", C.c_uint32), ("budget", C.c_uint32), ("recent", C.c_uint32),
+        ("sinks", C.c_uint32), ("pages_ld", C.c_uint32), ("new_pages_ld", C.c_uint32), ("lens", C.c_void_p),
+        ("pages", C.c_void_p), ("new_pages", C.c_void_p), ("new_lens", C.c_void_p), ("weights", C.c_void_p),
+        ("positions", C.c_void_p), ("side_ld", C.c_uint64), ("new_weights", C.c_void_p), ("new_positions", C.c_void_p),
+        ("new_side_ld", C.c_uint64), ("kept", C.c_void_p),
     ]
 
 
@@ -152,6 +195,19 @@ def lib():
         L.llmcache_shard_decide.argtypes = [vp, vp, u32, C.c_float, u32, u32, vp, C.POINTER(ProbeIO), vp]
         L.llmcache_bank_debug_knobs.argtypes = [vp, C.c_uint64, u32]
         L.llmcache_layer_debug_knobs.argtypes = [vp, C.c_uint64, u32]
+        rp, mp = C.POINTER(Rows), C.POINTER(ScoreMods)
+        L.llmcache_attention.argtypes = [rp, rp, rp, rp, u32, u32, u32, u32, vp, mp, vp, vp]
+        L.llmcache_attention_status.argtypes = []
+        L.llmcache_attention_debug_knobs.argtypes = [C.c_uint64, u32]
+        L.llmcache_kv_bytes.argtypes = [C.POINTER(KVDesc), C.POINTER(C.c_size_t)]
+        L.llmcache_kv_create.argtypes = [C.POINTER(KVDesc), C.POINTER(vp)]
+        L.llmcache_kv_destroy.argtypes = [vp]
+        L.llmcache_kv_attention.argtypes = [vp, C.POINTER(KVChunk), vp]
+        L.llmcache_kv_evict.argtypes = [vp, C.POINTER(KVEviction), vp]
+        L.llmcache_kv_status.argtypes = [vp]
+        L.llmcache_kv_debug_knobs.argtypes = [vp, C.c_uint64, u32]
+        L.llmcache_layer_score_mods.argtypes = [vp, mp]
+        L.llmcache_layer_extend.argtypes = [vp, vp, vp, C.POINTER(KVChunk), vp, vp]
         for name in EXPORTS:
             if name not in ("llmcache_abi_version", "llmcache_strerror", "llmcache_last_cuda_error",
                             "llmcache_fingerprint_static_error"):
@@ -576,6 +632,23 @@ class Layer:
     def forward(self, x, out, n_seqs=None, n_seqs_dev=None, stream=None):
         llmcache_layer_forward(self.handle, x, x.shape[0] if n_seqs is None else n_seqs, n_seqs_dev, out, stream)
 
+    def score_mods(self, mods: Optional[ScoreMods]):
+        """Score modifiers (make_score_mods) of the forward and extend calls that follow; None switches them off."""
+        llmcache_layer_score_mods(self.handle, mods)
+        self._mods = mods                                # keeps the arrays alive
+
+    def extend(self, cache: "KVCache", x, out, *, cu_rows, lens, pages, longest=0, weights=None, decay=1.0, positions=None,
+               first=None, stream=None):
+        """The layer on new tokens: x, out [n_rows, d]; the other arguments as in KVCache.attention."""
+        chunk = cache.chunk(x.shape[0], cu_rows=cu_rows, lens=lens, pages=pages, longest=longest, weights=weights, decay=decay,
+                            positions=positions, first=first)
+        _want(x, torch.bfloat16, 2, "x")
+        _want(out, torch.bfloat16, 2, "out")
+        if not (x.is_contiguous() and out.is_contiguous() and x.shape == out.shape and x.shape[1] == self.desc.d_model):
+            raise LLMCacheError(ERR_SHAPE, "llmcache_layer_extend: x and out are dense [n_rows, d_model]")
+        _check(lib().llmcache_layer_extend(self.handle, cache.handle, _ptr(x), C.byref(chunk), _ptr(out), _stream(stream)),
+               "llmcache_layer_extend")
+
     def status(self) -> int:
         return llmcache_layer_status(self.handle)
 
@@ -585,6 +658,277 @@ class Layer:
     def close(self):
         if getattr(self, "handle", None):
             llmcache_layer_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ----------------------------------------------------------------------------
+# Attention with score modifiers, paged key/value cache, eviction
+# ----------------------------------------------------------------------------
+def _want(t, dtype, dim, name, optional=False):
+    """Type and rank of a tensor argument; strides that the C side cannot see."""
+    if t is None and optional:
+        return
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.dim() != dim:
+        raise LLMCacheError(ERR_ARG, f"{name}: a {dtype} tensor of {dim} dimensions is expected")
+
+
+def _dense(t, dtype, dim, name, optional=False):
+    _want(t, dtype, dim, name, optional)
+    if t is not None and not t.is_contiguous():
+        raise LLMCacheError(ERR_ARG, f"{name}: must be contiguous")
+
+
+def _rows(t, name, dim) -> Rows:
+    """[seq, token, head, 64] or [token, head, 64] view of any strides."""
+    _want(t, torch.bfloat16, dim, name)
+    st = t.stride()
+    if t.shape[-1] != 64 or (st[-1] != 1 and t.numel()):
+        raise LLMCacheError(ERR_SHAPE, f"{name}: the last dimension holds 64 neighbouring elements")
+    return Rows(t.data_ptr(), st[0] if dim == 4 else 0, st[-3], st[-2])
+
+
+def make_score_mods(*, causal=False, scale=0.0, cap=0.0, slopes=None, table=None, doc=None, prefix=None) -> ScoreMods:
+    """llmcache_score_mods.  slopes f32 [heads]; table f32 [heads, 2 * reach + 1]; doc i32 [n_seqs, seq_len];
+    prefix i32 [n_seqs].  The struct keeps the tensors alive."""
+    _dense(slopes, torch.float32, 1, "slopes", True)
+    _dense(table, torch.float32, 2, "table", True)
+    _dense(doc, torch.int32, 2, "doc", True)
+    _dense(prefix, torch.int32, 1, "prefix", True)
+    m = ScoreMods()
+    m.struct_size = C.sizeof(ScoreMods)
+    m.causal, m.scale, m.cap = int(causal), scale, cap
+    if table is not None:
+        if table.shape[1] % 2 == 0:
+            raise LLMCacheError(ERR_SHAPE, "table: an odd number of distances, from -reach to reach")
+        m.reach = table.shape[1] // 2
+    m.slopes, m.table, m.doc, m.prefix = _ptr(slopes), _ptr(table), _ptr(doc), _ptr(prefix)
+    m.tensors = (slopes, table, doc, prefix)
+    return m
+
+
+def _check_heads(mods, heads):
+    if mods is not None and getattr(mods, "tensors", None):
+        slopes, table = mods.tensors[:2]
+        if (slopes is not None and slopes.shape[0] != heads) or (table is not None and table.shape[0] != heads):
+            raise LLMCacheError(ERR_SHAPE, "score modifiers: one row per query head")
+
+
+def llmcache_attention(q, k, v, out, mods: Optional[ScoreMods] = None, lse=None, n_seqs_dev=None, stream=None) -> None:
+    """out = softmax(modified q k^T) v.  q, out: bf16 [n_seqs, seq_len, heads, 64]; k, v: [n_seqs, seq_len, kv_heads, 64],
+    views of any strides (multiples of 8); lse: optional f32 [n_seqs, seq_len, heads]."""
+    rq, rk, rv, ro = _rows(q, "q", 4), _rows(k, "k", 4), _rows(v, "v", 4), _rows(out, "out", 4)
+    S, n, H, _ = q.shape
+    HK = k.shape[2]
+    if k.shape != (S, n, HK, 64) or v.shape != k.shape or out.shape != q.shape:
+        raise LLMCacheError(ERR_SHAPE, "llmcache_attention: q, out [S, n, H, 64], k, v [S, n, HK, 64]")
+    _dense(lse, torch.float32, 3, "lse", True)
+    if lse is not None and lse.shape != (S, n, H):
+        raise LLMCacheError(ERR_SHAPE, "lse: [n_seqs, seq_len, heads]")
+    _check_heads(mods, H)
+    if mods is not None and getattr(mods, "tensors", None):
+        doc, prefix = mods.tensors[2:]
+        if (doc is not None and doc.shape != (S, n)) or (prefix is not None and prefix.shape != (S,)):
+            raise LLMCacheError(ERR_SHAPE, "doc: [n_seqs, seq_len], prefix: [n_seqs]")
+    _check(lib().llmcache_attention(C.byref(rq), C.byref(rk), C.byref(rv), C.byref(ro), S, n, H, HK, _ptr(n_seqs_dev),
+                                    C.byref(mods) if mods is not None else None, _ptr(lse), _stream(stream)),
+           "llmcache_attention")
+
+
+def llmcache_attention_status() -> int:
+    return int(lib().llmcache_attention_status())
+
+
+def llmcache_attention_debug_knobs(wait_limit_ns: int, flags: int) -> None:
+    _check(lib().llmcache_attention_debug_knobs(wait_limit_ns, flags), "llmcache_attention_debug_knobs")
+
+
+def llmcache_kv_bytes(desc: KVDesc) -> int:
+    out = C.c_size_t(0)
+    _check(lib().llmcache_kv_bytes(C.byref(desc), C.byref(out)), "llmcache_kv_bytes")
+    return int(out.value)
+
+
+def llmcache_kv_create(desc: KVDesc) -> int:
+    out = C.c_void_p(None)
+    _check(lib().llmcache_kv_create(C.byref(desc), C.byref(out)), "llmcache_kv_create")
+    return out.value
+
+
+def llmcache_kv_destroy(kv: int) -> None:
+    _check(lib().llmcache_kv_destroy(kv), "llmcache_kv_destroy")
+
+
+def llmcache_kv_attention(kv, chunk: KVChunk, stream=None) -> None:
+    _check(lib().llmcache_kv_attention(kv, C.byref(chunk), _stream(stream)), "llmcache_kv_attention")
+
+
+def llmcache_kv_evict(kv, eviction: KVEviction, stream=None) -> None:
+    _check(lib().llmcache_kv_evict(kv, C.byref(eviction), _stream(stream)), "llmcache_kv_evict")
+
+
+def llmcache_kv_status(kv) -> int:
+    return int(lib().llmcache_kv_status(kv))
+
+
+def llmcache_kv_debug_knobs(kv, wait_limit_ns: int, flags: int) -> None:
+    _check(lib().llmcache_kv_debug_knobs(kv, wait_limit_ns, flags), "llmcache_kv_debug_knobs")
+
+
+def llmcache_layer_score_mods(layer, mods: Optional[ScoreMods]) -> None:
+    _check(lib().llmcache_layer_score_mods(layer, C.byref(mods) if mods is not None else None), "llmcache_layer_score_mods")
+
+
+def llmcache_layer_extend(layer, kv, x, chunk: KVChunk, out, stream=None) -> None:
+    _check(lib().llmcache_layer_extend(layer, kv, _ptr(x), C.byref(chunk), _ptr(out), _stream(stream)), "llmcache_layer_extend")
+
+
+def make_kv_desc(k_pages, v_pages, *, heads, max_seqs, max_rows, max_len, device=0, workspace=None) -> KVDesc:
+    """k_pages, v_pages: bf16 [num_pages, kv_heads, page_size, 64], dense within a page, equal strides between pages."""
+    _want(k_pages, torch.bfloat16, 4, "k_pages")
+    _want(v_pages, torch.bfloat16, 4, "v_pages")
+    num, hk, ps, dh = k_pages.shape
+    if v_pages.shape != k_pages.shape or dh != 64 or k_pages.stride() != v_pages.stride() or \
+            k_pages.stride()[1:] != (ps * 64, 64, 1):
+        raise LLMCacheError(ERR_SHAPE, "k_pages, v_pages: [num_pages, kv_heads, page_size, 64], dense within a page")
+    d = KVDesc()
+    d.struct_size, d.device = C.sizeof(KVDesc), device
+    d.heads, d.kv_heads, d.num_pages, d.page_size = heads, hk, num, ps
+    d.max_seqs, d.max_rows, d.max_len = max_seqs, max_rows, max_len
+    d.k_pages, d.v_pages, d.page_stride = k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride(0)
+    if workspace is not None:
+        d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return d
+
+
+class KVCache:
+    """Owner of one llmcache_kv_t handle; keeps the page tensors alive (the library borrows them)."""
+
+    def __init__(self, k_pages, v_pages, *, heads, max_seqs, max_rows, max_len, device=None, workspace=None):
+        self.k_pages, self.v_pages, self.workspace = k_pages, v_pages, workspace
+        self.desc = make_kv_desc(k_pages, v_pages, heads=heads, max_seqs=max_seqs, max_rows=max_rows, max_len=max_len,
+                                 device=(k_pages.device.index or 0) if device is None else device, workspace=workspace)
+        self.heads, self.kv_heads = heads, self.desc.kv_heads
+        self.handle = llmcache_kv_create(self.desc)
+
+    def _table(self, t, seqs, name):
+        _want(t, torch.int32, 2, name)
+        if t.shape[0] != seqs or (t.numel() and t.stride(1) != 1):
+            raise LLMCacheError(ERR_SHAPE, f"{name}: [n_seqs, pages], rows of neighbouring elements")
+        return t.data_ptr(), t.shape[1], t.stride(0)
+
+    def _side(self, t, dtype, seqs, name):
+        """[n_seqs, kv_heads, ld] side array: (address, ld)."""
+        _dense(t, dtype, 3, name)
+        if t.shape[:2] != (seqs, self.kv_heads):
+            raise LLMCacheError(ERR_SHAPE, f"{name}: [n_seqs, kv_heads, slots]")
+        return t.data_ptr(), t.shape[2]
+
+    def chunk(self, n_rows, *, cu_rows, lens, pages, longest=0, weights=None, decay=1.0, positions=None, first=None) -> KVChunk:
+        """What llmcache_kv_attention and llmcache_layer_extend take alike."""
+        c = KVChunk()
+        c.struct_size = C.sizeof(KVChunk)
+        _dense(lens, torch.int32, 1, "lens")
+        _dense(cu_rows, torch.int32, 1, "cu_rows")
+        S = lens.shape[0]
+        if cu_rows.shape[0] != S + 1:
+            raise LLMCacheError(ERR_SHAPE, "cu_rows: [n_seqs + 1]")
+        c.n_seqs, c.n_rows, c.longest = S, n_rows, longest
+        c.cu_rows, c.lens = cu_rows.data_ptr(), lens.data_ptr()
+        c.pages, width, c.pages_ld = self._table(pages, S, "pages")
+        if width != c.pages_ld and S > 1:
+            raise LLMCacheError(ERR_ARG, "pages: must be contiguous")
+        c.pages_ld = width
+        if weights is not None:
+            c.weights, c.side_ld = self._side(weights, torch.float32, S, "weights")
+            c.decay = decay
+        if positions is not None:
+            c.positions, ld = self._side(positions, torch.int32, S, "positions")
+            if weights is not None and ld != c.side_ld:
+                raise LLMCacheError(ERR_SHAPE, "weights, positions: rows of one length")
+            c.side_ld = ld
+        if first is not None:
+            _dense(first, torch.int32, 1, "first")
+            if first.shape[0] != S:
+                raise LLMCacheError(ERR_SHAPE, "first: [n_seqs]")
+            c.first = first.data_ptr()
+        return c
+
+    def attention(self, q, out, *, cu_rows, lens, pages, longest=0, k_new=None, v_new=None, lse=None, mods=None, weights=None,
+                  decay=1.0, positions=None, first=None, stream=None):
+        """Stores k_new, v_new [n_rows, kv_heads, 64] in the pages and lets q [n_rows, heads, 64] attend to all that its
+        sequences have there (llmcache_kv_attention).  cu_rows i32 [n_seqs + 1], lens i32 [n_seqs], pages i32
+        [n_seqs, pages]; lse f32 [n_rows, heads]; weights f32 and positions i32 [n_seqs, kv_heads, slots]."""
+        c = self.chunk(q.shape[0], cu_rows=cu_rows, lens=lens, pages=pages, longest=longest, weights=weights, decay=decay,
+                       positions=positions, first=first)
+        c.q, c.out = _rows(q, "q", 3), _rows(out, "out", 3)
+        T = q.shape[0]
+        if q.shape != (T, self.heads, 64) or out.shape != q.shape:
+            raise LLMCacheError(ERR_SHAPE, "q, out: [n_rows, heads, 64]")
+        if (k_new is None) != (v_new is None):
+            raise LLMCacheError(ERR_ARG, "k_new and v_new come together")
+        if k_new is not None:
+            c.k_new, c.v_new = _rows(k_new, "k_new", 3), _rows(v_new, "v_new", 3)
+            if k_new.shape != (T, self.kv_heads, 64) or v_new.shape != k_new.shape:
+                raise LLMCacheError(ERR_SHAPE, "k_new, v_new: [n_rows, kv_heads, 64]")
+        _dense(lse, torch.float32, 2, "lse", True)
+        if lse is not None:
+            if lse.shape != (T, self.heads):
+                raise LLMCacheError(ERR_SHAPE, "lse: [n_rows, heads]")
+            c.lse = lse.data_ptr()
+        if mods is not None:
+            _check_heads(mods, self.heads)
+            c.mods = C.pointer(mods)
+        llmcache_kv_attention(self.handle, c, stream)
+
+    def evict(self, *, lens, pages, weights, new_pages, new_lens, budget, recent=0, sinks=0, positions=None, new_weights=None,
+              new_positions=None, kept=None, stream=None):
+        """Copies the `budget` entries per sequence and head that received the most attention, the newest and the first ones
+        to new_pages (llmcache_kv_evict)."""
+        e = KVEviction()
+        e.struct_size = C.sizeof(KVEviction)
+        _dense(lens, torch.int32, 1, "lens")
+        _dense(new_lens, torch.int32, 1, "new_lens")
+        S = lens.shape[0]
+        if new_lens.shape[0] != S:
+            raise LLMCacheError(ERR_SHAPE, "new_lens: [n_seqs]")
+        e.n_seqs, e.budget, e.recent, e.sinks = S, budget, recent, sinks
+        e.lens, e.new_lens = lens.data_ptr(), new_lens.data_ptr()
+        _dense(pages, torch.int32, 2, "pages")
+        _dense(new_pages, torch.int32, 2, "new_pages")
+        e.pages, e.pages_ld, _ = self._table(pages, S, "pages")
+        e.new_pages, e.new_pages_ld, _ = self._table(new_pages, S, "new_pages")
+        e.weights, e.side_ld = self._side(weights, torch.float32, S, "weights")
+        for name, t, dtype, to in (("positions", positions, torch.int32, "side_ld"), ("new_weights", new_weights, torch.float32, "new_side_ld"),
+                                   ("new_positions", new_positions, torch.int32, "new_side_ld")):
+            if t is None:
+                continue
+            addr, ld = self._side(t, dtype, S, name)
+            if getattr(e, to) not in (0, ld):
+                raise LLMCacheError(ERR_SHAPE, f"{name}: rows of another length")
+            setattr(e, name, addr)
+            setattr(e, to, ld)
+        if kept is not None:
+            _dense(kept, torch.int32, 3, "kept")
+            if kept.shape != (S, self.kv_heads, budget):
+                raise LLMCacheError(ERR_SHAPE, "kept: [n_seqs, kv_heads, budget]")
+            e.kept = kept.data_ptr()
+        llmcache_kv_evict(self.handle, e, stream)
+
+    def status(self) -> int:
+        return llmcache_kv_status(self.handle)
+
+    def debug_knobs(self, wait_limit_ns: int = 0, flags: int = 0):
+        llmcache_kv_debug_knobs(self.handle, wait_limit_ns, flags)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            llmcache_kv_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

@@ -1,0 +1,92 @@
+// Attention operators (score modifiers, paged key/value cache, eviction): shared declarations.
+#pragma once
+#include "llmcache_internal.cuh"
+
+namespace llmc {
+
+constexpr float LOG2E_F = 1.4426950408889634f;
+constexpr float LN2_F = 0.6931471805599453f;
+
+// llmcache_score_mods, checked; positions are those of the header
+struct ScoreArgs {
+  float scale, cap;
+  uint32_t causal;
+  int32_t reach;
+  const float* slopes;
+  const float* table;
+  const int32_t* doc;
+  const int32_t* prefix;
+};
+
+struct RowsArgs {
+  __nv_bfloat16* ptr;
+  long long seq, tok, head;      // strides in elements
+};
+
+// One call of the attention over whole sequences (pages == nullptr) or over a paged cache.
+struct AttnArgs {
+  RowsArgs q, out, k, v;         // paged: k, v are the new rows (ptr may be null), seq strides unused
+  float* lse;
+  uint32_t heads, kv_heads, group, n_seqs;
+  const uint32_t* n_seqs_dev;
+  ScoreArgs m;
+  uint32_t* status;
+  uint32_t n;                    // whole sequences: tokens of one; paged: most rows of one sequence
+  // paged
+  const int32_t *cu, *lens, *pages, *first;
+  int32_t* positions;
+  float* weights;
+  float decay;
+  uint32_t n_rows, pages_ld, num_pages, page_shift, max_len;
+  unsigned long long side_ld, page_stride;
+  __nv_bfloat16 *k_pages, *v_pages;
+};
+
+// A sequence of a paged call: its rows row0 .. row0 + cnt - 1 take the slots slot0 .. of len slots.  Whatever the
+// arrays hold, rows stay inside [0, n_rows) and slots inside the page table.
+struct SeqGeo { uint32_t row0, cnt, len; int32_t slot0; };
+__device__ __forceinline__ SeqGeo seq_geo(const AttnArgs& a, uint32_t s) {
+  SeqGeo g;
+  const int32_t c0 = a.cu[s], c1 = a.cu[s + 1], len = a.lens[s];
+  const uint32_t cap = min((unsigned long long)a.max_len, (unsigned long long)a.pages_ld << a.page_shift);
+  g.len = len > 0 ? min((uint32_t)len, cap) : 0u;
+  const bool sane = c0 >= 0 && c1 >= c0 && (uint32_t)c1 <= a.n_rows;
+  g.row0 = sane ? (uint32_t)c0 : 0u;
+  const uint32_t cnt = sane ? (uint32_t)(c1 - c0) : 0u;
+  g.slot0 = (int32_t)g.len - (int32_t)cnt;
+  g.cnt = min(cnt, a.n);
+  return g;
+}
+// page of a slot, or -1 where the table has none
+__device__ __forceinline__ int32_t page_of(const AttnArgs& a, uint32_t s, uint32_t slot) {
+  const int32_t p = a.pages[(size_t)s * a.pages_ld + (slot >> a.page_shift)];
+  return (uint32_t)p < a.num_pages ? p : -1;
+}
+__device__ __forceinline__ size_t page_row(const AttnArgs& a, int32_t page, uint32_t hk, uint32_t slot) {
+  return (size_t)page * a.page_stride + (((size_t)hk << a.page_shift) + (slot & ((1u << a.page_shift) - 1u))) * 64;
+}
+
+cudaError_t setup_attn_kernels();
+cudaError_t launch_attn(const AttnArgs& a, int sm_count, cudaStream_t st);
+// received weights of a paged call whose lse is complete
+cudaError_t launch_attn_weights(const AttnArgs& a, int sm_count, cudaStream_t st);
+cudaError_t launch_kv_append(const AttnArgs& a, int sm_count, cudaStream_t st);
+
+struct EvictArgs {
+  uint32_t n_seqs, kv_heads, budget, recent, sinks, pages_ld, new_pages_ld, num_pages, page_shift, max_len;
+  unsigned long long side_ld, new_side_ld, page_stride;
+  const int32_t *lens, *pages, *new_pages;
+  int32_t* new_lens;
+  const float* weights;
+  const int32_t* positions;
+  float* new_weights;
+  int32_t* new_positions;
+  int32_t* kept_out;             // optional
+  int32_t* kept;                 // scratch [n_seqs, kv_heads, budget]
+  uint32_t* count;               // scratch [n_seqs]
+  __nv_bfloat16 *k_pages, *v_pages;
+};
+cudaError_t setup_evict_kernels();
+cudaError_t launch_evict_tokens(const EvictArgs& a, int sm_count, cudaStream_t st);
+
+}  // namespace llmc

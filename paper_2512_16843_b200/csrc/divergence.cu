@@ -5,6 +5,7 @@
 #include "llmcache_internal.cuh"
 
 struct llmcache_layer;
+namespace llmc { bool layer_masks_by_sequence(const llmcache_layer* L); }
 extern "C" int llmcache_layer_forward(llmcache_layer* layer, const void* x, uint32_t n_seqs,
                                       const uint32_t* n_seqs_dev, void* out, void* stream);
 
@@ -86,6 +87,7 @@ extern "C" int llmcache_divergence_check(llmcache_bank_t* bk, llmcache_layer* la
   using namespace llmc;
   if (!bk || !layer || !h_in || !io || !h_sample || !out_sample || !rel_out || !counters_dev || stride == 0)
     return LLMCACHE_ERR_ARG;
+  if (layer_masks_by_sequence(layer)) return LLMCACHE_ERR_UNSUPPORTED;
   if (!bk->a.act || bk->desc.hidden_dtype != LLMCACHE_BF16) return LLMCACHE_ERR_UNSUPPORTED;
   if (bk->probe_open && bk->last_B) return LLMCACHE_ERR_STATE;        // run it after the commit
   if (!(bound >= 0.f)) return LLMCACHE_ERR_ARG;

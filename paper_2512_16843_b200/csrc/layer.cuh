@@ -33,4 +33,7 @@ cudaError_t launch_attention_tc(const __nv_bfloat16* qkv, const __nv_bfloat16* v
                                 uint32_t n, uint32_t d, uint32_t heads, uint32_t seq_max, const uint32_t* m_seq_dev,
                                 int causal, cudaStream_t st);
 
+// whether llmcache_layer_score_mods gave the layer masks that belong to single sequences
+bool layer_masks_by_sequence(const llmcache_layer* L);
+
 }  // namespace llmc

@@ -3,6 +3,7 @@
 #include <cstring>
 #include <new>
 #include "layer.cuh"
+#include "attn_host.cuh"
 
 using namespace llmc;
 
@@ -13,7 +14,13 @@ struct llmcache_layer {
   bool owns_ws = false;
   __nv_bfloat16 *qkv = nullptr, *a = nullptr, *t = nullptr, *y = nullptr, *f = nullptr, *vt = nullptr;
   uint32_t* status = nullptr;    // device word: a bounded wait expired
+  bool has_mods = false;         // llmcache_layer_score_mods
+  ScoreArgs mods{};
 };
+
+namespace llmc {
+bool layer_masks_by_sequence(const llmcache_layer* L) { return L && L->has_mods && (L->mods.doc || L->mods.prefix); }
+}
 
 namespace {
 constexpr size_t WS_ALIGN = 256;
@@ -37,6 +44,24 @@ size_t layer_ws_bytes(const llmcache_layer_desc& d) {
   const size_t T = (size_t)d.max_seqs * d.seq_len;
   const size_t vt = (size_t)d.max_seqs * d.d_model * attention_vt_pitch(d.seq_len) * 2;      // per-head transposes of V
   return up256(T * 3 * d.d_model * 2) + 3 * up256(T * d.d_model * 2) + up256(T * d.ffn * 2) + up256(vt) + WS_ALIGN;
+}
+
+// attention over the sequences of one forward call: q|k|v rows of 3d columns in, rows of d columns out
+AttnArgs layer_attn_args(const llmcache_layer* L, uint32_t n_seqs, const uint32_t* n_seqs_dev) {
+  const long long d = L->desc.d_model, n = L->desc.seq_len;
+  AttnArgs a{};
+  a.q = RowsArgs{L->qkv, n * 3 * d, 3 * d, 64};
+  a.k = RowsArgs{L->qkv + d, n * 3 * d, 3 * d, 64};
+  a.v = RowsArgs{L->qkv + 2 * d, n * 3 * d, 3 * d, 64};
+  a.out = RowsArgs{L->a, n * d, d, 64};
+  a.heads = a.kv_heads = L->desc.heads;
+  a.group = 1;
+  a.n_seqs = n_seqs;
+  a.n_seqs_dev = n_seqs_dev;
+  a.n = L->desc.seq_len;
+  a.m = L->mods;
+  a.status = L->status;
+  return a;
 }
 }  // namespace
 
@@ -90,6 +115,7 @@ int llmcache_layer_create(const llmcache_layer_desc* desc, llmcache_layer_t** la
   }
   if (e == cudaSuccess) e = setup_gemm_kernel();
   if (e == cudaSuccess) e = setup_attention_kernel();
+  if (e == cudaSuccess) e = setup_attn_kernels();
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   cudaSetDevice(prev);
   if (e != cudaSuccess) {
@@ -135,14 +161,19 @@ int llmcache_layer_forward(llmcache_layer_t* L, const void* x, uint32_t n_seqs, 
                   __nv_bfloat16* o, uint32_t N, uint32_t K, uint32_t a_, VtOut vt = VtOut{nullptr, 0, 0, 0}) {
     return launch_gemm(a, (const __nv_bfloat16*)w, bias, res, o, L->status, T, N, K, n_seqs_dev, n, a_, sm, st, vt);
   };
-  // the V third of the q|k|v product is written transposed per head (what the attention kernel reads)
-  const VtOut vt_out{L->vt, 2 * d, attention_vt_pitch(n), D.heads};
+  // the V third of the q|k|v product is written transposed per head (what the attention kernel reads); the kernel with
+  // score modifiers reads all of q|k|v from the one matrix
+  const VtOut vt_out = L->has_mods ? VtOut{nullptr, 0, 0, 0} : VtOut{L->vt, 2 * d, attention_vt_pitch(n), D.heads};
+  auto attend = [&]() -> cudaError_t {
+    if (!L->has_mods) return launch_attention_tc(L->qkv, L->vt, L->a, L->status, n, d, D.heads, n_seqs, n_seqs_dev, D.causal, st);
+    return launch_attn(layer_attn_args(L, n_seqs, n_seqs_dev), sm, st);
+  };
   auto ln = [&](const __nv_bfloat16* in, const float* g, const float* b, __nv_bfloat16* o) {
     return launch_layernorm(in, g, b, o, T, d, n_seqs_dev, n, D.eps, sm, st);
   };
   if (!D.pre_ln) {
     e = gemm(X, D.w_qkv, D.b_qkv, nullptr, L->qkv, 3 * d, d, LAYER_ACT_NONE, vt_out);
-    if (e == cudaSuccess) e = launch_attention_tc(L->qkv, L->vt, L->a, L->status, n, d, D.heads, n_seqs, n_seqs_dev, D.causal, st);
+    if (e == cudaSuccess) e = attend();
     if (e == cudaSuccess) e = gemm(L->a, D.w_o, D.b_o, X, L->t, d, d, LAYER_ACT_NONE);
     if (e == cudaSuccess) e = ln(L->t, D.ln1_g, D.ln1_b, L->y);
     if (e == cudaSuccess) e = gemm(L->y, D.w_1, D.b_1, nullptr, L->f, D.ffn, d, act);
@@ -151,7 +182,7 @@ int llmcache_layer_forward(llmcache_layer_t* L, const void* x, uint32_t n_seqs, 
   } else {
     e = ln(X, D.ln1_g, D.ln1_b, L->y);
     if (e == cudaSuccess) e = gemm(L->y, D.w_qkv, D.b_qkv, nullptr, L->qkv, 3 * d, d, LAYER_ACT_NONE, vt_out);
-    if (e == cudaSuccess) e = launch_attention_tc(L->qkv, L->vt, L->a, L->status, n, d, D.heads, n_seqs, n_seqs_dev, D.causal, st);
+    if (e == cudaSuccess) e = attend();
     if (e == cudaSuccess) e = gemm(L->a, D.w_o, D.b_o, X, L->t, d, d, LAYER_ACT_NONE);
     if (e == cudaSuccess) e = ln(L->t, D.ln2_g, D.ln2_b, L->y);
     if (e == cudaSuccess) e = gemm(L->y, D.w_1, D.b_1, nullptr, L->f, D.ffn, d, act);
@@ -160,6 +191,77 @@ int llmcache_layer_forward(llmcache_layer_t* L, const void* x, uint32_t n_seqs, 
   if (prev != L->desc.device) cudaSetDevice(prev);
   if (e != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
   return LLMCACHE_OK;
+}
+
+int llmcache_layer_score_mods(llmcache_layer_t* L, const llmcache_score_mods* mods) {
+  if (!L) return LLMCACHE_ERR_ARG;
+  if (!mods) { L->has_mods = false; return LLMCACHE_OK; }
+  ScoreArgs m;
+  const int rc = check_score_mods(mods, &m);
+  if (rc != LLMCACHE_OK) return rc;
+  if ((m.causal != 0) != (L->desc.causal != 0)) return LLMCACHE_ERR_ARG;
+  L->mods = m;
+  L->has_mods = true;
+  return LLMCACHE_OK;
+}
+
+int llmcache_layer_extend(llmcache_layer_t* L, llmcache_kv_t* kv, const void* x, const llmcache_kv_chunk* chunk,
+                          void* out, void* stream) {
+  if (!L || !kv || !chunk || chunk->struct_size != sizeof(llmcache_kv_chunk)) return LLMCACHE_ERR_ARG;
+  const llmcache_layer_desc& D = L->desc;
+  if (!D.causal || layer_masks_by_sequence(L)) return LLMCACHE_ERR_UNSUPPORTED;
+  int rc = kv_fits_layer(kv, D.device, D.heads);
+  if (rc != LLMCACHE_OK) return rc;
+  const uint32_t T = chunk->n_rows, d = D.d_model;
+  if ((uint64_t)T > (uint64_t)D.max_seqs * D.seq_len) return LLMCACHE_ERR_SHAPE;
+  if (T && chunk->n_seqs && (!x || !out || !chunk->cu_rows)) return LLMCACHE_ERR_ARG;
+  if (((uintptr_t)x | (uintptr_t)out) & 15u) return LLMCACHE_ERR_ARG;
+  // the attention's arguments: q, k and v are the thirds of the rows that the first product writes
+  llmcache_score_mods m{};
+  m.struct_size = sizeof(m);
+  m.causal = 1;
+  if (L->has_mods) { m.scale = L->mods.scale; m.cap = L->mods.cap; m.reach = (uint32_t)L->mods.reach; m.slopes = L->mods.slopes; m.table = L->mods.table; }
+  llmcache_kv_chunk c = *chunk;
+  c.q = llmcache_rows{L->qkv, 0, 3ll * d, 64};
+  c.k_new = llmcache_rows{L->qkv + d, 0, 3ll * d, 64};
+  c.v_new = llmcache_rows{L->qkv + 2 * d, 0, 3ll * d, 64};
+  c.out = llmcache_rows{L->a, 0, (int64_t)d, 64};
+  c.mods = &m;
+  rc = kv_check_chunk(kv, &c);
+  if (rc != LLMCACHE_OK || T == 0 || c.n_seqs == 0) return rc;
+
+  int prev = 0;
+  cudaGetDevice(&prev);
+  if (prev != D.device && cudaSetDevice(D.device) != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
+  cudaStream_t st = (cudaStream_t)stream;
+  const int sm = L->sm_count;
+  const uint32_t act = D.tanh_gelu ? LAYER_ACT_GELU_TANH : LAYER_ACT_GELU_ERF;
+  // rows behind the last sequence are neither computed nor written
+  const uint32_t* rows = (const uint32_t*)(c.cu_rows + c.n_seqs);
+  const __nv_bfloat16* X = (const __nv_bfloat16*)x;
+  __nv_bfloat16* O = (__nv_bfloat16*)out;
+  cudaError_t e = cudaSuccess;
+  auto gemm = [&](const __nv_bfloat16* a, const void* w, const float* bias, const __nv_bfloat16* res, __nv_bfloat16* o,
+                  uint32_t N, uint32_t K, uint32_t a_) {
+    if (e == cudaSuccess)
+      e = launch_gemm(a, (const __nv_bfloat16*)w, bias, res, o, L->status, T, N, K, rows, 1, a_, sm, st);
+  };
+  auto ln = [&](const __nv_bfloat16* in, const float* g, const float* b, __nv_bfloat16* o) {
+    if (e == cudaSuccess) e = launch_layernorm(in, g, b, o, T, d, rows, 1, D.eps, sm, st);
+  };
+  if (D.pre_ln) ln(X, D.ln1_g, D.ln1_b, L->y);
+  gemm(D.pre_ln ? L->y : X, D.w_qkv, D.b_qkv, nullptr, L->qkv, 3 * d, d, LAYER_ACT_NONE);
+  if (e == cudaSuccess) rc = llmcache_kv_attention(kv, &c, stream);
+  if (rc == LLMCACHE_OK) {
+    gemm(L->a, D.w_o, D.b_o, X, L->t, d, d, LAYER_ACT_NONE);
+    ln(L->t, D.pre_ln ? D.ln2_g : D.ln1_g, D.pre_ln ? D.ln2_b : D.ln1_b, L->y);
+    gemm(L->y, D.w_1, D.b_1, nullptr, L->f, D.ffn, d, act);
+    gemm(L->f, D.w_2, D.b_2, D.pre_ln ? L->t : L->y, D.pre_ln ? O : L->t, d, D.ffn, LAYER_ACT_NONE);
+    if (!D.pre_ln) ln(L->t, D.ln2_g, D.ln2_b, O);
+  }
+  if (prev != D.device) cudaSetDevice(prev);
+  if (e != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
+  return rc;
 }
 
 int llmcache_layer_status(llmcache_layer_t* L) {
@@ -219,6 +321,9 @@ int llmcache_infer(llmcache_bank_t** banks, llmcache_layer_t** layers, uint32_t 
                    void** h_final, void* stream) {
   if (!layers || !h0 || !buf_a || !buf_b || !h_final || n_layers == 0) return LLMCACHE_ERR_ARG;
   if (banks && (!io || !h_miss || !miss_out)) return LLMCACHE_ERR_ARG;
+  // masks of single sequences: the misses change their places, and a match does not look at masks
+  for (uint32_t l = 0; banks && l < n_layers; ++l)
+    if (layer_masks_by_sequence(layers[l])) return LLMCACHE_ERR_UNSUPPORTED;
   if (banks) {
     // banks created with fused_pool (all of them, same width) take the fingerprint-on-write path by themselves
     bool fused = true;
@@ -254,6 +359,8 @@ int llmcache_infer_pooled(llmcache_bank_t** banks, llmcache_layer_t** layers, ui
                           llmcache_probe_io* io, float* pooled, void** h_final, void* stream) {
   if (!banks || !layers || !h0 || !buf_a || !buf_b || !h_final || n_layers == 0) return LLMCACHE_ERR_ARG;
   if (!io || !h_miss || !miss_out || !pooled) return LLMCACHE_ERR_ARG;
+  for (uint32_t l = 0; l < n_layers; ++l)
+    if (layer_masks_by_sequence(layers[l])) return LLMCACHE_ERR_UNSUPPORTED;
   return infer_fused(banks, layers, n_layers, h0, B, tau, buf_a, buf_b, h_miss, miss_out, io, pooled, h_final, stream);
 }
 
