@@ -475,7 +475,7 @@ typedef struct llmcache_rows {
 } llmcache_rows;
 
 /* out = softmax(z) v over whole sequences of seq_len tokens.  q, out: heads heads; k, v: kv_heads heads, a divisor of
- * heads (query head h reads key/value head h / (heads / kv_heads)); lse: optional f32 [n_seqs, seq_len, heads], natural
+ * heads, at least a 128th of them (query head h reads key/value head h / (heads / kv_heads)); lse: optional f32 [n_seqs, seq_len, heads], natural
  * logarithm of the sum of exp(z).  mods: NULL = plain attention.  n_seqs_dev: optional DEVICE u32, only
  * min(n_seqs, *n_seqs_dev) sequences are processed and the rows of the others stay as they were.  Takes no object:
  * runs on the CURRENT device, allocates nothing, does not synchronise.  out must not overlap an input.  A stride
@@ -499,7 +499,7 @@ typedef struct llmcache_kv llmcache_kv_t;
 typedef struct llmcache_kv_desc {
   uint32_t struct_size;
   int32_t  device;
-  uint32_t heads, kv_heads;  /* heads: a multiple of kv_heads */
+  uint32_t heads, kv_heads;  /* heads: a multiple of kv_heads, at most 128 times it */
   uint32_t num_pages;
   uint32_t page_size;        /* 16, 32, 64, 128 or 256 */
   uint32_t max_seqs;         /* most sequences of one call */

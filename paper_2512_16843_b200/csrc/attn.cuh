@@ -66,8 +66,23 @@ __device__ __forceinline__ size_t page_row(const AttnArgs& a, int32_t page, uint
   return (size_t)page * a.page_stride + (((size_t)hk << a.page_shift) + (slot & ((1u << a.page_shift) - 1u))) * 64;
 }
 
+// sequence whose rows include `row`: the last one whose first row is not behind it
+__device__ __forceinline__ uint32_t seq_of_row(const AttnArgs& a, uint32_t row) {
+  uint32_t lo = 0, hi = a.n_seqs;
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    if (a.cu[mid] <= (int32_t)row) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+constexpr size_t PART_FLOATS = 66;                 // one (row, head, share of the keys): 64 sums, the maximum, the sum of weights
+constexpr uint32_t ATTN_MAX_GROUP = 128;           // query heads per key/value head: rows of one query tile
+cudaError_t setup_attn_tc();
+cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, int sm_count, cudaStream_t st);
 cudaError_t setup_attn_kernels();
-cudaError_t launch_attn(const AttnArgs& a, int sm_count, cudaStream_t st);
+// part: scratch of a paged call for part_units x PART_FLOATS floats, or null
+cudaError_t launch_attn(const AttnArgs& a, float* part, size_t part_units, int sm_count, cudaStream_t st);
 // received weights of a paged call whose lse is complete
 cudaError_t launch_attn_weights(const AttnArgs& a, int sm_count, cudaStream_t st);
 cudaError_t launch_kv_append(const AttnArgs& a, int sm_count, cudaStream_t st);

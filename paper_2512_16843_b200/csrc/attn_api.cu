@@ -128,6 +128,7 @@ int check_kv_desc(const llmcache_kv_desc* d) {
   if (!d->k_pages || !d->v_pages || !aligned(d->k_pages, 16) || !aligned(d->v_pages, 16)) return LLMCACHE_ERR_ARG;
   if (!aligned(d->workspace, WS_ALIGN)) return LLMCACHE_ERR_ARG;
   if (!d->heads || !d->kv_heads || d->heads % d->kv_heads || d->heads > 65536) return LLMCACHE_ERR_SHAPE;
+  if (d->heads / d->kv_heads > ATTN_MAX_GROUP) return LLMCACHE_ERR_UNSUPPORTED;
   if (!d->num_pages || !d->max_seqs || !d->max_rows || !d->max_len) return LLMCACHE_ERR_SHAPE;
   if (d->page_size < 16 || d->page_size > 256 || (d->page_size & (d->page_size - 1))) return LLMCACHE_ERR_SHAPE;
   if (d->num_pages > 0x7FFFFFFFu || d->max_len > (1u << 30) || d->max_seqs > (1u << 20) || d->max_rows > (1u << 28)) return LLMCACHE_ERR_SHAPE;
@@ -138,12 +139,16 @@ int check_kv_desc(const llmcache_kv_desc* d) {
   return LLMCACHE_OK;
 }
 
-struct KvLayout { size_t status, lse, kept, count, total; };
+// (row, head, share of the keys) results of one call.  Keys are split only while rows alone leave SMs idle, so the shares of
+// all rows never exceed 2 x 256 rows per SM.
+constexpr size_t KV_PART_UNITS = 2 * 256 * 160;
+struct KvLayout { size_t status, part, lse, kept, count, total; };
 KvLayout kv_layout(const llmcache_kv_desc& d) {
   KvLayout L{};
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
   L.status = take(16);
+  L.part = take(KV_PART_UNITS * PART_FLOATS * 4);
   L.lse = take((size_t)d.max_rows * d.heads * 4);
   L.kept = take((size_t)d.max_seqs * d.kv_heads * d.max_len * 4);
   L.count = take((size_t)d.max_seqs * 4);
@@ -217,6 +222,7 @@ int llmcache_attention(const llmcache_rows* q, const llmcache_rows* k, const llm
   AttnArgs a{};
   int rc = check_score_mods(mods, &a.m);
   if (rc != LLMCACHE_OK) return rc;
+  if (heads && kv_heads && heads % kv_heads == 0 && heads / kv_heads > ATTN_MAX_GROUP) return LLMCACHE_ERR_UNSUPPORTED;
   if (!heads || !kv_heads || heads % kv_heads || heads > 65536 || !seq_len || seq_len > (1u << 30)) return LLMCACHE_ERR_SHAPE;
   if (n_seqs == 0) return LLMCACHE_OK;                     // an empty batch has no buffers to check
   if ((rc = take_rows(q, n_seqs, seq_len, heads, &a.q)) != LLMCACHE_OK) return rc;
@@ -233,7 +239,7 @@ int llmcache_attention(const llmcache_rows* q, const llmcache_rows* k, const llm
   a.heads = heads; a.kv_heads = kv_heads; a.group = heads / kv_heads;
   a.n_seqs = n_seqs; a.n_seqs_dev = n_seqs_dev; a.n = seq_len;
   a.status = d.status;
-  return launch_attn_checked(a, d.sm_count, (cudaStream_t)stream);
+  return launch_attn_checked(a, nullptr, 0, d.sm_count, (cudaStream_t)stream);
 }
 
 int llmcache_attention_status(void) {
@@ -293,6 +299,7 @@ int llmcache_kv_create(const llmcache_kv_desc* desc, llmcache_kv_t** kv_out) {
     kv->owns_ws = true;
   }
   kv->status = (uint32_t*)(kv->ws + lay.status);
+  kv->part = (float*)(kv->ws + lay.part);
   kv->lse = (float*)(kv->ws + lay.lse);
   kv->kept = (int32_t*)(kv->ws + lay.kept);
   kv->count = (uint32_t*)(kv->ws + lay.count);
@@ -331,7 +338,7 @@ int llmcache_kv_attention(llmcache_kv_t* kv, const llmcache_kv_chunk* c, void* s
     const cudaError_t e = launch_kv_append(a, kv->sm_count, st);
     if (e != cudaSuccess) return done(e);
   }
-  rc = launch_attn_checked(a, kv->sm_count, st);
+  rc = launch_attn_checked(a, kv->part, KV_PART_UNITS, kv->sm_count, st);
   if (rc == LLMCACHE_OK && a.weights) rc = done(launch_attn_weights(a, kv->sm_count, st));
   return rc;
 }

@@ -1,0 +1,844 @@
+// Attention on the 5th-generation tensor cores: whole sequences with score modifiers, and chunks over a paged cache.
+//
+//   S = Q K^T      tcgen05.mma 128 x 128 x 64, operands in shared memory (TMA, 128-byte swizzle), S in tensor memory
+//   P = exp2(t - m) t: score in base-2 units with its modifiers; P as bf16 over S in tensor memory
+//   O += P V       tcgen05.mma 128 x 64 x 128, P from tensor memory, V as it lies in memory (MN-major), O in tensor memory
+//
+// A block works on two tiles of up to 128 query rows that share the key and value tiles.  The query heads that share a
+// key/value head are rows of one tile (row = token * group + head of the group), so grouped heads read their keys once and
+// few tokens still fill the tile.  Roles: warp 0 loads (TMA) and decides which key tiles are needed; warp 1 issues the
+// products; warps 2-3 look after what comes with a key tile (document or position of every key, missing pages, values
+// that are not numbers); warps 4-7 and 8-11 do the softmax of one query tile each, one thread per row.  While one tile's
+// softmax runs, the other tile's products do.  The block walks its items (a sequence, a key/value head, 256 rows, and
+// a share of the keys where the rows alone do not fill the GPU), so the loads of the next item overlap the end of this one.
+//
+// Maximum: O and the sums refer to a maximum m that is raised, and O scaled, only when a tile's maximum exceeds it by more
+// than 2^8: factors up to 2^8 lose nothing in f32 sums and in bf16 P (relative rounding), and O stays in tensor memory.
+// Rounding: S, m, sums and O are f32; P is rounded to bf16 (2^-8 relative per weight, averaged over the keys) because the
+// product takes bf16 operands; the sums are of the unrounded weights.
+//
+// Values that are not numbers: P is zero where a key is not seen, but 0 * inf is not.  So infinities and NaN are taken
+// out of a V tile before its product (warps 2-3 scan it: 3 instructions per 4 bytes, hidden behind the exponentials) and
+// listed; a row that sees a listed key gets them in its output at the end.
+// Every wait is bounded (status word).
+#include <cuda.h>
+#include <algorithm>
+#include "attn.cuh"
+#include "ptx.cuh"
+
+namespace llmc {
+
+// bf16 rows of 64 columns (llmcache_rows), boxes of box_heads x box_toks rows, 128-byte swizzle, zero fill outside
+bool make_tensor_map_rows(CUtensorMap* map, const RowsArgs& r, uint64_t heads, uint64_t toks, uint64_t seqs, uint32_t box_heads,
+                          uint32_t box_toks);
+
+namespace {
+
+constexpr int TC_THREADS = 384;
+constexpr uint32_t TC_ST = 4;                                // stages of the ring of key and value tiles
+constexpr uint32_t TC_TILE = 16384;                          // 128 x 64 bf16
+constexpr uint32_t TC_KEYS = 128;
+constexpr uint32_t TC_TMEM = 512;                            // S0 | S1 (128 columns each, P over them) | O0 | O1 (64 each)
+enum : uint32_t { F_NEED0 = 1, F_NEED1 = 2, F_FIRST = 4, F_LAST = 8 };
+struct TcSmem {
+  static constexpr uint32_t Q = 0;                           // [item parity][query tile]
+  static constexpr uint32_t K = Q + 4 * TC_TILE;
+  static constexpr uint32_t V = K + TC_ST * TC_TILE;
+  static constexpr uint32_t POISON = V + TC_ST * TC_TILE;    // u64 [stage][key][NaN, +inf, -inf]: columns
+  static constexpr uint32_t ROWP = POISON + TC_ST * 128 * 24;// u64 [row][3]: the same, seen by a row
+  static constexpr uint32_t KINFO = ROWP + 256 * 24;         // i32 [stage][key]: document or position
+  static constexpr uint32_t KMASK = KINFO + TC_ST * 512;     // u32 [stage][4]: keys that exist
+  static constexpr uint32_t DIRTY = KMASK + TC_ST * 16;      // u32 [stage][4]: keys listed in POISON
+  static constexpr uint32_t INFO = DIRTY + TC_ST * 16;       // u32 [stage][2]: key tile, flags
+  static constexpr uint32_t BAR = INFO + TC_ST * 8;
+  static constexpr uint32_t MISC = BAR + 32 * 8;
+  static constexpr uint32_t TOTAL = MISC + 64;
+};
+constexpr uint32_t TC_SMEM = TcSmem::TOTAL + 1024;
+static_assert(TC_SMEM <= 232448, "shared memory of one block");
+// kind::f16, f32 accumulator, bf16 operands, M = 128; PV: B is MN-major (bit 16)
+constexpr uint32_t TC_IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+constexpr uint32_t TC_IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
+
+__device__ __forceinline__ float ex2f(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float lg2f(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max3f(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// D[tmem] (+)= A[tmem] * B[smem], bf16 inputs, f32 accumulate
+__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// the loads before it are complete and their registers may be read (they pass through the statement)
+__device__ __forceinline__ void tc_wait_ld32(uint32_t (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                 "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+               :: "memory");
+  asm volatile("" : "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
+                    "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]) :: "memory");
+}
+__device__ __forceinline__ void tc_st_16(uint32_t taddr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
+}
+// mbar_wait by a whole warp: all lanes get the same answer, so that they leave together when a wait runs out
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, unsigned long long limit_ns,
+                                          uint32_t backoff_ns) {
+  return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, limit_ns, backoff_ns));
+}
+__device__ __forceinline__ unsigned long long f2_dup(float x) { return f2_pack(x, x); }
+
+// Launch shape, the same for every role.
+struct TcPlan {
+  uint32_t rt;                   // rows of a query tile: the largest multiple of the group up to 128
+  uint32_t qtiles, splits;       // pairs of query tiles per sequence and head; shares of the keys
+  uint32_t n_items, page_box;    // page_box: rows of a page's box
+  int page_rows, oob_row;        // rows of 64 elements between pages; a row behind the last page
+  float* part_o;                 // [split][row][head][64], [split][row][head][2] (m, l) when splits > 1
+  float* part_ml;
+};
+
+struct TcItem {
+  uint32_t s, hk, sp, r0, rows;  // rows: those of the sequence (tokens * group)
+  SeqGeo g;
+  int32_t pre;
+  uint32_t ts, te;               // its key tiles
+  bool live;                     // rows of this item exist
+};
+__device__ __forceinline__ uint32_t keys_to(const AttnArgs& a, const TcItem& it, uint32_t token) {
+  // keys below this bound may be seen by the row of a token
+  if (!a.m.causal) return it.g.len;
+  const int32_t hi = max(it.g.slot0 + (int32_t)token + 1, it.pre);
+  return hi <= 0 ? 0u : min((uint32_t)hi, it.g.len);
+}
+__device__ __forceinline__ TcItem tc_item(const AttnArgs& a, const TcPlan& p, uint32_t i, uint32_t n_seqs) {
+  TcItem it;
+  it.sp = i % p.splits; i /= p.splits;
+  it.hk = i % a.kv_heads; i /= a.kv_heads;
+  it.s = i % a.n_seqs; i /= a.n_seqs;
+  const uint32_t qt = p.qtiles - 1 - i;                      // the tiles with the most keys (causal) first
+  it.r0 = qt * 2 * p.rt;
+  it.g = SeqGeo{0, a.n, a.n, 0};
+  if (it.s < n_seqs && a.pages) it.g = seq_geo(a, it.s);
+  it.pre = a.m.prefix && it.s < n_seqs ? a.m.prefix[it.s] : 0;
+  it.rows = it.g.cnt * a.group;
+  it.live = it.s < n_seqs && it.r0 < it.rows;
+  it.ts = it.te = 0;
+  if (it.live) {
+    const uint32_t nt = (keys_to(a, it, (min(it.rows, it.r0 + 2 * p.rt) - 1) / a.group) + TC_KEYS - 1) / TC_KEYS;
+    const uint32_t per = (nt + p.splits - 1) / p.splits;
+    it.ts = min(nt, it.sp * per);
+    it.te = min(nt, it.ts + per);
+  }
+  return it;
+}
+// key tiles that query tile w of an item needs
+__device__ __forceinline__ uint32_t tiles_of(const AttnArgs& a, const TcPlan& p, const TcItem& it, uint32_t w) {
+  const uint32_t first = it.r0 + w * p.rt;
+  if (first >= it.rows) return 0;
+  return (keys_to(a, it, (min(it.rows, first + p.rt) - 1) / a.group) + TC_KEYS - 1) / TC_KEYS;
+}
+
+// tanh of two values: an odd polynomial on |u| <= 0.75 (tanh_fit.py, relative error 1.4e-7)
+__device__ __forceinline__ unsigned long long tanh_small2(unsigned long long u) {
+  const unsigned long long s = f2_mul(u, u);
+  unsigned long long q = f2_fma(f2_dup(-4.723952152e-03f), s, f2_dup(1.959378645e-02f));
+  q = f2_fma(q, s, f2_dup(-5.334981903e-02f));
+  q = f2_fma(q, s, f2_dup(1.332551539e-01f));
+  q = f2_fma(q, s, f2_dup(-3.333296776e-01f));
+  q = f2_fma(q, s, f2_dup(1.0f));
+  return f2_mul(u, q);
+}
+// 1 - 2 / (1 + e^2u): for |u| > 0.75, where the difference loses nothing
+__device__ __forceinline__ float tanh_large(float u) { return 1.f - __fdividef(2.f, 1.f + ex2f(2.f * LOG2E_F * u)); }
+
+}  // namespace
+
+__global__ void __launch_bounds__(TC_THREADS, 1)
+k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+          const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a, const __grid_constant__ TcPlan p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gbase = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t sQ = base + TcSmem::Q, sK = base + TcSmem::K, sV = base + TcSmem::V;
+  const uint32_t bar0 = base + TcSmem::BAR;
+  auto k_full = [&](uint32_t s) { return bar0 + 8 * s; };
+  auto v_full = [&](uint32_t s) { return bar0 + 8 * (TC_ST + s); };
+  auto side_full = [&](uint32_t s) { return bar0 + 8 * (2 * TC_ST + s); };
+  auto empty = [&](uint32_t s) { return bar0 + 8 * (3 * TC_ST + s); };
+  const uint32_t bar1 = bar0 + 8 * 4 * TC_ST;
+  auto q_full = [&](uint32_t b) { return bar1 + 8 * b; };
+  auto q_empty = [&](uint32_t b) { return bar1 + 8 * (2 + b); };
+  auto s_full = [&](uint32_t w) { return bar1 + 8 * (4 + w); };
+  auto p_full = [&](uint32_t w) { return bar1 + 8 * (6 + w); };
+  auto pv_done = [&](uint32_t w) { return bar1 + 8 * (8 + w); };
+  const uint32_t drain = bar1 + 8 * 10;
+  volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(gbase + TcSmem::MISC);
+  volatile uint32_t* abort_flag = misc + 1;
+  volatile uint32_t* info = reinterpret_cast<volatile uint32_t*>(gbase + TcSmem::INFO);
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < TC_ST; ++s) {
+      mbar_init(k_full(s), 1); mbar_init(v_full(s), 1); mbar_init(side_full(s), 2); mbar_init(empty(s), 1 + 8);
+    }
+    for (uint32_t b = 0; b < 2; ++b) {
+      mbar_init(q_full(b), 1); mbar_init(q_empty(b), 1); mbar_init(s_full(b), 1); mbar_init(p_full(b), 128); mbar_init(pv_done(b), 1);
+    }
+    mbar_init(drain, 1);
+    misc[1] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32((const void*)misc)), "r"(TC_TMEM) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = misc[0];
+  griddep_sync();                                            // what the preceding kernels wrote may be read from here on
+  const unsigned long long lim = wait_limit(a.status);
+  uint32_t n_seqs = a.n_seqs;
+  if (a.n_seqs_dev) n_seqs = min(n_seqs, *a.n_seqs_dev);
+  const bool paged = a.pages != nullptr;
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- loads
+    bool ok = true;
+    uint32_t e = 0, qc = 0;
+    for (uint32_t i = producer_idle(a.status) ? p.n_items : blockIdx.x; i < p.n_items && ok; i += gridDim.x) {
+      const TcItem it = tc_item(a, p, i, n_seqs);
+      if (it.ts >= it.te) continue;
+      const uint32_t nt0 = tiles_of(a, p, it, 0), nt1 = tiles_of(a, p, it, 1);
+      // smallest and largest document of either query tile (padding left out)
+      int32_t lo0 = INT32_MAX, hi0 = -1, lo1 = INT32_MAX, hi1 = -1;
+      const int32_t* doc = a.m.doc ? a.m.doc + (size_t)it.s * a.n : nullptr;
+      if (doc) {
+        const uint32_t t0 = it.r0 / a.group, t1 = (it.r0 + p.rt) / a.group, t2 = (it.r0 + 2 * p.rt) / a.group;
+        for (uint32_t t = t0 + lane; t < min(t1, a.n); t += 32) { const int32_t d = doc[t]; if (d >= 0) { lo0 = min(lo0, d); hi0 = max(hi0, d); } }
+        for (uint32_t t = t1 + lane; t < min(t2, a.n); t += 32) { const int32_t d = doc[t]; if (d >= 0) { lo1 = min(lo1, d); hi1 = max(hi1, d); } }
+        lo0 = __reduce_min_sync(0xFFFFFFFFu, lo0); hi0 = __reduce_max_sync(0xFFFFFFFFu, hi0);
+        lo1 = __reduce_min_sync(0xFFFFFFFFu, lo1); hi1 = __reduce_max_sync(0xFFFFFFFFu, hi1);
+      }
+      // flags of key tile j (0: nobody needs it)
+      auto needs = [&](uint32_t j) -> uint32_t {
+        uint32_t f = (j < nt0 ? F_NEED0 : 0u) | (j < nt1 ? F_NEED1 : 0u);
+        if (!doc || !f) return f;
+        int32_t lo = INT32_MAX, hi = -1;
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+          const uint32_t k = j * TC_KEYS + u * 32 + lane;
+          const int32_t d = k < a.n ? doc[k] : -1;
+          if (d >= 0) { lo = min(lo, d); hi = max(hi, d); }
+        }
+        lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+        hi = __reduce_max_sync(0xFFFFFFFFu, hi);
+        if (lo > hi0 || hi < lo0) f &= ~F_NEED0;
+        if (lo > hi1 || hi < lo1) f &= ~F_NEED1;
+        return f;
+      };
+      uint32_t j = it.ts, f = needs(j);
+      while (!f && j + 1 < it.te) f = needs(++j);
+      if (!f) f = nt0 > j ? F_NEED0 : F_NEED1;               // every item has at least one tile, here a hidden one
+      f |= F_FIRST;
+      {
+        const uint32_t b = qc & 1u;
+        ok = warp_wait(q_empty(b), ((qc >> 1) & 1u) ^ 1u, abort_flag, lim, 64);
+        if (!ok) break;
+        if (lane == 0) {
+          const uint32_t per = p.rt / a.group, bytes = p.rt * 128;
+          const int tok = (int)(it.r0 / a.group) + (paged ? (int)it.g.row0 : 0), seq = paged ? 0 : (int)it.s;
+          mbar_expect_tx(q_full(b), 2 * bytes);
+          tma_load_4d(sQ + (b * 2) * TC_TILE, &map_q, 0, (int)(it.hk * a.group), tok, seq, q_full(b));
+          tma_load_4d(sQ + (b * 2 + 1) * TC_TILE, &map_q, 0, (int)(it.hk * a.group), tok + (int)per, seq, q_full(b));
+        }
+        ++qc;
+      }
+      for (;;) {
+        // the next tile that is needed
+        uint32_t jn = j + 1, fn = 0;
+        for (; jn < it.te; ++jn)
+          if ((fn = needs(jn)) != 0) break;
+        if (jn >= it.te) f |= F_LAST;
+        const uint32_t s = e % TC_ST;
+        int row = 0;
+        const uint32_t boxes = paged ? TC_KEYS / p.page_box : 1u;
+        if (paged && lane < boxes) {
+          const uint32_t slot = j * TC_KEYS + lane * p.page_box;
+          const int32_t pg = slot < it.g.len ? page_of(a, it.s, slot) : -1;
+          row = pg < 0 ? p.oob_row
+                       : pg * p.page_rows + (int)((it.hk << a.page_shift) + (slot & ((1u << a.page_shift) - 1u)));
+        }
+        ok = warp_wait(empty(s), ((e / TC_ST) & 1u) ^ 1u, abort_flag, lim, 64);
+        if (!ok) break;
+        if (lane == 0) {
+          info[s * 2] = j;
+          info[s * 2 + 1] = f;
+          mbar_expect_tx(k_full(s), TC_TILE);
+          mbar_expect_tx(v_full(s), TC_TILE);
+        }
+        __syncwarp();
+        if (paged) {
+          if (lane < boxes) {
+            const uint32_t off = s * TC_TILE + lane * p.page_box * 128;
+            tma_load_2d(sK + off, &map_k, 0, row, k_full(s));
+            tma_load_2d(sV + off, &map_v, 0, row, v_full(s));
+          }
+        } else if (lane == 0) {
+          tma_load_4d(sK + s * TC_TILE, &map_k, 0, (int)it.hk, (int)(j * TC_KEYS), (int)it.s, k_full(s));
+          tma_load_4d(sV + s * TC_TILE, &map_v, 0, (int)it.hk, (int)(j * TC_KEYS), (int)it.s, v_full(s));
+        }
+        ++e;
+        if (f & F_LAST) break;
+        j = jn;
+        f = fn;
+      }
+    }
+    if (!ok && lane == 0) { *abort_flag = 1; atomicExch(a.status, 1u); }
+    __syncwarp();
+    if (lane == 0 && *abort_flag) {
+      // a wait ran out: loads in flight must land before the block's shared memory is released
+      volatile uint32_t never = 0;
+      for (uint32_t b = 0; b < 2 && b < qc; ++b) mbar_wait(q_full((qc - 1 - b) & 1u), ((qc - 1 - b) >> 1) & 1u, &never, 200000000ull);
+      for (uint32_t b = 0; b < TC_ST && b < e; ++b) {
+        const uint32_t x = e - 1 - b;
+        mbar_wait(k_full(x % TC_ST), (x / TC_ST) & 1u, &never, 200000000ull);
+        mbar_wait(v_full(x % TC_ST), (x / TC_ST) & 1u, &never, 200000000ull);
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- products
+    if (lane == 0) {
+      auto next_item = [&](uint32_t i) {                     // the first item from i on that has key tiles
+        for (; i < p.n_items; i += gridDim.x) {
+          const TcItem it = tc_item(a, p, i, n_seqs);
+          if (it.ts < it.te) break;
+        }
+        return i;
+      };
+      uint32_t i = next_item(blockIdx.x), e = 0, qc = 0, n_pv[2] = {0, 0};
+      bool ok = true, started[2] = {false, false};
+      auto issue_s = [&](uint32_t entry, uint32_t q, uint32_t w) {
+        const uint64_t dq = smem_desc_sw128(sQ + ((q & 1u) * 2 + w) * TC_TILE), dk = smem_desc_sw128(sK + (entry % TC_ST) * TC_TILE);
+#pragma unroll
+        for (uint32_t kk = 0; kk < 4; ++kk) tc_mma_bf16(tmem + w * 128, dq + kk * 2, dk + kk * 2, TC_IDESC_S, kk != 0u);
+        tc_commit(s_full(w));
+      };
+      uint32_t f = 0;
+      if (i < p.n_items) {
+        ok = mbar_wait(q_full(0), 0u, abort_flag, lim, 32) && mbar_wait(k_full(0), 0u, abort_flag, lim, 32);
+        if (ok) {
+          tc_fence_after();
+          f = info[1];
+          if (f & F_NEED0) issue_s(0, 0, 0);
+          if (f & F_NEED1) issue_s(0, 0, 1);
+        }
+      }
+      while (ok && i < p.n_items) {
+        const uint32_t s = e % TC_ST;
+        if (f & F_FIRST) started[0] = started[1] = false;
+        if (!mbar_wait(side_full(s), (e / TC_ST) & 1u, abort_flag, lim, 32)) { ok = false; break; }
+        const bool last = (f & F_LAST) != 0;
+        const uint32_t in = last ? next_item(i + gridDim.x) : i;
+        const bool more = in < p.n_items;
+        const uint32_t qn = last ? qc + 1 : qc;
+        uint32_t fn = 0;
+        bool known = false;
+#pragma unroll
+        for (uint32_t w = 0; w < 2; ++w) {
+          if (f & (F_NEED0 << w)) {
+            if (!mbar_wait(p_full(w), n_pv[w] & 1u, abort_flag, lim, 20)) { ok = false; break; }
+            tc_fence_after();
+            const uint64_t dv = smem_desc_sw128(sV + s * TC_TILE);
+#pragma unroll
+            for (uint32_t kk = 0; kk < 8; ++kk)              // 16 keys a step: 2,048 bytes of V, 8 columns of P
+              tc_mma_ts(tmem + 256 + w * 64, tmem + w * 128 + kk * 8, dv + kk * 128, TC_IDESC_PV, (started[w] || kk != 0u) ? 1u : 0u);
+            tc_commit(pv_done(w));
+            started[w] = true;
+            ++n_pv[w];
+          }
+          if (more) {
+            if (!known) {
+              if (last && !mbar_wait(q_full(qn & 1u), (qn >> 1) & 1u, abort_flag, lim, 20)) { ok = false; break; }
+              if (!mbar_wait(k_full((e + 1) % TC_ST), ((e + 1) / TC_ST) & 1u, abort_flag, lim, 20)) { ok = false; break; }
+              tc_fence_after();
+              fn = info[((e + 1) % TC_ST) * 2 + 1];
+              known = true;
+            }
+            if (fn & (F_NEED0 << w)) {
+              // S overwrites P: the product that reads P must be complete
+              if (n_pv[w] && !mbar_wait(pv_done(w), (n_pv[w] - 1) & 1u, abort_flag, lim, 20)) { ok = false; break; }
+              tc_fence_after();
+              issue_s(e + 1, qn, w);
+            }
+          }
+        }
+        if (!ok) break;
+        tc_commit(empty(s));
+        if (last) tc_commit(q_empty(qc & 1u));
+        qc = qn;
+        i = in;
+        f = fn;
+        ++e;
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        atomicExch(a.status, 1u);
+        volatile uint32_t never = 0;
+        tc_commit(drain);                                    // products in flight end before tensor memory is released
+        mbar_wait(drain, 0u, &never, 200000000ull);
+      }
+    }
+  } else if (warp < 4) {
+    // ---------------------------------------------------------------- what comes with a key tile
+    const uint32_t sw = warp - 2;                            // keys sw * 32 + lane and 64 + sw * 32 + lane
+    bool ok = true;
+    uint32_t e = 0;
+    for (uint32_t i = blockIdx.x; i < p.n_items && ok; i += gridDim.x) {
+      const TcItem it = tc_item(a, p, i, n_seqs);
+      if (it.ts >= it.te) continue;
+      const int32_t* src = a.m.doc ? a.m.doc + (size_t)it.s * a.n
+                                   : a.positions ? a.positions + ((size_t)it.s * a.kv_heads + it.hk) * a.side_ld : nullptr;
+      for (;;) {
+        const uint32_t s = e % TC_ST, ph = (e / TC_ST) & 1u;
+        ok = warp_wait(k_full(s), ph, abort_flag, lim, 64);
+        if (!ok) break;
+        const uint32_t j = info[s * 2], f = info[s * 2 + 1];
+        int32_t* kinfo = reinterpret_cast<int32_t*>(gbase + TcSmem::KINFO) + s * 128;
+        uint32_t* kmask = reinterpret_cast<uint32_t*>(gbase + TcSmem::KMASK) + s * 4;
+        uint32_t* dirty = reinterpret_cast<uint32_t*>(gbase + TcSmem::DIRTY) + s * 4;
+#pragma unroll
+        for (uint32_t u = 0; u < 2; ++u) {
+          const uint32_t c = u * 64 + sw * 32 + lane, key = j * TC_KEYS + c;
+          if (src) kinfo[c] = key < it.g.len ? src[key] : -1;
+          if (paged) {
+            const bool there = key < it.g.len && page_of(a, it.s, key) >= 0;
+            const uint32_t word = __ballot_sync(0xFFFFFFFFu, there);
+            if (lane == 0) kmask[u * 2 + sw] = word;
+          }
+        }
+        ok = warp_wait(v_full(s), ph, abort_flag, lim, 64);
+        if (!ok) break;
+#pragma unroll
+        for (uint32_t u = 0; u < 2; ++u) {
+          const uint32_t c = u * 64 + sw * 32 + lane;
+          uint8_t* vrow = gbase + TcSmem::V + s * TC_TILE + c * 128;
+          // a half with all exponent bits set overflows into its top bit
+          uint32_t acc = 0;
+#pragma unroll
+          for (uint32_t q = 0; q < 8; ++q) {
+            const uint4 x = *reinterpret_cast<const uint4*>(vrow + ((q ^ (c & 7u)) << 4));
+            acc |= ((x.x & 0x7FFF7FFFu) + 0x00800080u) | ((x.y & 0x7FFF7FFFu) + 0x00800080u) | ((x.z & 0x7FFF7FFFu) + 0x00800080u) |
+                   ((x.w & 0x7FFF7FFFu) + 0x00800080u);
+          }
+          const bool bad = (acc & 0x80008000u) != 0u;
+          const uint32_t word = __ballot_sync(0xFFFFFFFFu, bad);
+          if (lane == 0) dirty[u * 2 + sw] = word;
+          if (bad) {
+            unsigned long long* ps = reinterpret_cast<unsigned long long*>(gbase + TcSmem::POISON) + (s * 128 + c) * 3;
+            unsigned long long nan = 0, pos = 0, neg = 0;
+            for (uint32_t q = 0; q < 8; ++q) {
+              uint16_t* h = reinterpret_cast<uint16_t*>(vrow + ((q ^ (c & 7u)) << 4));
+              for (uint32_t x = 0; x < 8; ++x) {
+                const uint16_t v = h[x];
+                if ((v & 0x7F80u) != 0x7F80u) continue;
+                const unsigned long long bit = 1ull << (q * 8 + x);
+                if (v & 0x7Fu) nan |= bit; else if (v & 0x8000u) neg |= bit; else pos |= bit;
+                h[x] = 0;
+              }
+            }
+            ps[0] = nan; ps[1] = pos; ps[2] = neg;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(side_full(s));
+        ++e;
+        if (f & F_LAST) break;
+      }
+    }
+    if (!ok && lane == 0) { *abort_flag = 1; atomicExch(a.status, 1u); }
+  } else {
+    // ---------------------------------------------------------------- softmax and output, one thread per query row
+    const uint32_t w = (warp - 4) >> 2, quarter = warp & 3u, r = quarter * 32 + lane;
+    const uint32_t t_s = tmem + w * 128 + ((quarter * 32u) << 16), t_o = tmem + 256 + w * 64 + ((quarter * 32u) << 16);
+    unsigned long long* rowp = reinterpret_cast<unsigned long long*>(gbase + TcSmem::ROWP) + (w * 128 + r) * 3;
+    const float sc = a.m.scale * LOG2E_F;
+    const bool modified = a.m.cap > 0.f || a.m.slopes || a.m.table;
+    bool ok = true;
+    uint32_t e = 0, n_s = 0;
+    for (uint32_t i = blockIdx.x; i < p.n_items && ok; i += gridDim.x) {
+      const TcItem it = tc_item(a, p, i, n_seqs);
+      if (!it.live) continue;
+      const uint32_t R = it.r0 + w * p.rt + r, token = R / a.group, h = it.hk * a.group + R % a.group;
+      const bool mine = r < p.rt && R < it.rows;             // the row exists
+      uint32_t hi = mine ? keys_to(a, it, token) : 0u;
+      int32_t qdoc = 0;
+      if (a.m.doc && mine) { qdoc = a.m.doc[(size_t)it.s * a.n + token]; if (qdoc < 0) hi = 0; }
+      const int32_t qpos = a.first && mine ? a.first[it.s] + (int32_t)token : it.g.slot0 + (int32_t)token;
+      const float slope = a.m.slopes && mine ? a.m.slopes[h] * LOG2E_F : 0.f;
+      const float* table = a.m.table ? a.m.table + (size_t)(mine ? h : 0u) * (2 * a.m.reach + 1) + a.m.reach : nullptr;
+      // keys that every row of this tile sees
+      const uint32_t first_row = it.r0 + w * p.rt;
+      const uint32_t all_see = first_row < it.rows ? keys_to(a, it, first_row / a.group) : 0u;
+      float m_ref = -INFINITY, l = 0.f;
+      bool any = false, poisoned = false;
+      for (bool last = it.ts >= it.te; !last;) {
+        const uint32_t s = e % TC_ST;
+        ok = warp_wait(side_full(s), (e / TC_ST) & 1u, abort_flag, lim, 32);
+        if (!ok) break;
+        const uint32_t j = info[s * 2], f = info[s * 2 + 1];
+        last = (f & F_LAST) != 0;
+        ++e;
+        if (f & (F_NEED0 << w)) {
+          const uint4 km = paged ? *reinterpret_cast<const uint4*>(gbase + TcSmem::KMASK + s * 16)
+                                 : make_uint4(~0u, ~0u, ~0u, ~0u);
+          const bool plain = !modified && !a.m.doc && (j + 1) * TC_KEYS <= all_see && (km.x & km.y & km.z & km.w) == ~0u;
+          ok = warp_wait(s_full(w), n_s & 1u, abort_flag, lim, 20);
+          if (!ok) break;
+          ++n_s;
+          tc_fence_after();
+          float mt = -INFINITY;
+          if (plain) {
+#pragma unroll 1
+            for (uint32_t c = 0; c < 128; c += 32) {
+              uint32_t v[32];
+              tc_ld_32x32(t_s + c, v);
+              tc_wait_ld32(v);
+              float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+              for (uint32_t x = 0; x < 32; x += 8) {
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u) m4[u] = max3f(m4[u], __uint_as_float(v[x + 2 * u]), __uint_as_float(v[x + 2 * u + 1]));
+              }
+              mt = fmaxf(max3f(mt, m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            }
+            mt *= sc;
+          } else {
+            // modified and masked scores go back to tensor memory in base-2 units
+            const int32_t* kinfo = reinterpret_cast<const int32_t*>(gbase + TcSmem::KINFO) + s * 128;
+#pragma unroll 1
+            for (uint32_t c = 0; c < 128; c += 32) {
+              uint32_t v[32];
+              tc_ld_32x32(t_s + c, v);
+              const uint32_t k0 = j * TC_KEYS + c;
+              const uint32_t left = hi > k0 ? hi - k0 : 0u;
+              uint32_t word = left >= 32 ? ~0u : (1u << left) - 1u;
+              word &= c == 0 ? km.x : c == 32 ? km.y : c == 64 ? km.z : km.w;
+              if (a.m.doc) {
+                uint32_t same = 0;
+#pragma unroll
+                for (uint32_t x = 0; x < 32; ++x) same |= (kinfo[c + x] == qdoc ? 1u : 0u) << x;
+                word &= same;
+              }
+              tc_wait_ld32(v);
+              unsigned long long t[16];
+              const unsigned long long sc2 = f2_dup(a.m.cap > 0.f ? a.m.scale / a.m.cap : sc);
+#pragma unroll
+              for (uint32_t x = 0; x < 16; ++x) t[x] = f2_mul(f2_pack(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), sc2);
+              if (a.m.cap > 0.f) {
+                float big = 0.f;
+#pragma unroll
+                for (uint32_t x = 0; x < 16; ++x) big = max3f(big, fabsf(f2_lo(t[x])), fabsf(f2_hi(t[x])));
+                const unsigned long long cap2 = f2_dup(a.m.cap * LOG2E_F);
+                if (__any_sync(0xFFFFFFFFu, !(big <= 0.75f))) {
+#pragma unroll
+                  for (uint32_t x = 0; x < 16; ++x) {
+                    const unsigned long long y = tanh_small2(t[x]);
+                    const float u0 = f2_lo(t[x]), u1 = f2_hi(t[x]);
+                    t[x] = f2_mul(f2_pack(fabsf(u0) <= 0.75f ? f2_lo(y) : tanh_large(u0), fabsf(u1) <= 0.75f ? f2_hi(y) : tanh_large(u1)), cap2);
+                  }
+                } else {
+#pragma unroll
+                  for (uint32_t x = 0; x < 16; ++x) t[x] = f2_mul(tanh_small2(t[x]), cap2);
+                }
+              }
+              if (a.m.slopes) {
+                const unsigned long long ns2 = f2_dup(-slope);
+                if (a.positions) {
+#pragma unroll
+                  for (uint32_t x = 0; x < 16; ++x)
+                    t[x] = f2_fma(f2_pack(fabsf((float)(kinfo[c + 2 * x] - qpos)), fabsf((float)(kinfo[c + 2 * x + 1] - qpos))), ns2, t[x]);
+                } else {
+                  const float d0 = (float)((int32_t)k0 - qpos);
+#pragma unroll
+                  for (uint32_t x = 0; x < 16; ++x)
+                    t[x] = f2_fma(f2_pack(fabsf(d0 + (float)(2 * x)), fabsf(d0 + (float)(2 * x + 1))), ns2, t[x]);
+                }
+              }
+              if (table) {
+                const int32_t R_ = a.m.reach;
+#pragma unroll
+                for (uint32_t x = 0; x < 16; ++x) {
+                  float b2[2];
+#pragma unroll
+                  for (uint32_t u = 0; u < 2; ++u) {
+                    const int32_t d = (a.positions ? kinfo[c + 2 * x + u] : (int32_t)(k0 + 2 * x + u)) - qpos;
+                    const float b = __ldg(table + min(max(d, -R_), R_));
+                    b2[u] = b < -1e38f ? b : b * LOG2E_F;    // the type's lowest value stays finite
+                  }
+                  t[x] = f2_add(t[x], f2_pack(b2[0], b2[1]));
+                }
+              }
+              float m2[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+              for (uint32_t x = 0; x < 16; ++x) {
+                const float t0 = (word >> (2 * x)) & 1u ? f2_lo(t[x]) : -INFINITY;
+                const float t1 = (word >> (2 * x + 1)) & 1u ? f2_hi(t[x]) : -INFINITY;
+                m2[x & 1u] = max3f(m2[x & 1u], t0, t1);
+                v[2 * x] = __float_as_uint(t0);
+                v[2 * x + 1] = __float_as_uint(t1);
+              }
+              mt = max3f(mt, m2[0], m2[1]);
+              tc_st_16(t_s + c, v);
+              tc_st_16(t_s + c + 16, v + 16);
+            }
+            tc_wait_st();
+          }
+          // raise the reference maximum?
+          const bool raise = !any ? true : mt > m_ref + 8.f;
+          if (!any) {
+            m_ref = mt;
+            any = true;
+          } else if (__any_sync(0xFFFFFFFFu, raise)) {
+            const float m_new = raise ? mt : m_ref;
+            const float corr = raise ? ex2f(m_ref - m_new) : 1.f;
+            l *= corr;
+            m_ref = m_new;
+            const unsigned long long c2 = f2_dup(corr);
+#pragma unroll 1
+            for (uint32_t c = 0; c < 64; c += 32) {
+              uint32_t v[32];
+              tc_ld_32x32(t_o + c, v);
+              tc_wait_ld32(v);
+#pragma unroll
+              for (uint32_t x = 0; x < 16; ++x) {
+                const unsigned long long y = f2_mul(f2_pack(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), c2);
+                v[2 * x] = __float_as_uint(f2_lo(y));
+                v[2 * x + 1] = __float_as_uint(f2_hi(y));
+              }
+              tc_st_16(t_o + c, v);
+              tc_st_16(t_o + c + 16, v + 16);
+            }
+          }
+          const unsigned long long nm2 = f2_dup(m_ref == -INFINITY ? 0.f : -m_ref), sc2 = f2_dup(plain ? sc : 1.f);
+          float l0 = 0.f, l1 = 0.f;
+#pragma unroll 1
+          for (uint32_t c = 0; c < 128; c += 32) {
+            uint32_t v[32], pk[16];
+            tc_ld_32x32(t_s + c, v);
+            tc_wait_ld32(v);
+#pragma unroll
+            for (uint32_t x = 0; x < 16; ++x) {
+              const unsigned long long t2 = f2_fma(f2_pack(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), sc2, nm2);
+              const float pa = ex2f(f2_lo(t2)), pb = ex2f(f2_hi(t2));
+              l0 += pa;
+              l1 += pb;
+              pk[x] = pack2(pa, pb);
+            }
+            tc_st_16(t_s + c / 2, pk);
+          }
+          l += l0 + l1;
+          tc_wait_st();
+          const uint4 dw = *reinterpret_cast<const uint4*>(gbase + TcSmem::DIRTY + s * 16);
+          if (dw.x | dw.y | dw.z | dw.w) {
+            // values that are not numbers: note the columns in which this row sees them
+            const uint32_t words[4] = {dw.x & km.x, dw.y & km.y, dw.z & km.z, dw.w & km.w};
+            const int32_t* kinfo = reinterpret_cast<const int32_t*>(gbase + TcSmem::KINFO) + s * 128;
+            for (uint32_t q = 0; q < 4; ++q)
+              for (uint32_t bits = words[q]; bits; bits &= bits - 1) {
+                const uint32_t c = q * 32 + __ffs(bits) - 1;
+                if (j * TC_KEYS + c >= hi || (a.m.doc && kinfo[c] != qdoc)) continue;
+                const unsigned long long* ps = reinterpret_cast<const unsigned long long*>(gbase + TcSmem::POISON) + (s * 128 + c) * 3;
+                for (uint32_t x = 0; x < 3; ++x) rowp[x] = (poisoned ? rowp[x] : 0ull) | ps[x];
+                poisoned = true;
+              }
+          }
+          tc_fence_before();
+          mbar_arrive(p_full(w));
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(s));
+      }
+      if (!ok) break;
+      // ---- output
+      uint32_t v[32];
+      const bool dead = l == 0.f;                            // nothing seen
+      const float inv = dead ? 0.f : 1.f / l;
+      if (any) {
+        ok = warp_wait(pv_done(w), (n_s - 1) & 1u, abort_flag, lim, 20);
+        if (!ok) break;
+        tc_fence_after();
+      }
+      const size_t row = paged ? (size_t)it.g.row0 + token : (size_t)token;
+      const size_t rowid = ((paged ? row : (size_t)it.s * a.n + token) * a.heads + h);
+      const size_t n_rowids = (size_t)a.n_rows * a.heads;    // of a paged call
+      __nv_bfloat16* out = a.out.ptr + (paged ? 0ll : (long long)it.s * a.out.seq) + (long long)row * a.out.tok + (long long)h * a.out.head;
+#pragma unroll 1
+      for (uint32_t c = 0; c < 64; c += 32) {
+        if (any) {
+          tc_ld_32x32(t_o + c, v);
+          tc_wait_ld32(v);
+        }
+        float o[32];
+#pragma unroll
+        for (uint32_t x = 0; x < 32; ++x) o[x] = dead ? 0.f : __uint_as_float(v[x]);
+        if (poisoned && !dead) {
+#pragma unroll
+          for (uint32_t x = 0; x < 32; ++x) {
+            const bool nan = (rowp[0] >> (c + x)) & 1ull, pos = (rowp[1] >> (c + x)) & 1ull, neg = (rowp[2] >> (c + x)) & 1ull;
+            if (nan || (pos && neg)) o[x] = NAN;
+            else if (pos) o[x] += INFINITY;
+            else if (neg) o[x] -= INFINITY;
+          }
+        }
+        if (!mine) {
+        } else if (p.splits > 1) {
+          float4* dst = reinterpret_cast<float4*>(p.part_o + ((size_t)it.sp * n_rowids + rowid) * 64 + c);
+#pragma unroll
+          for (uint32_t x = 0; x < 8; ++x) dst[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+        } else {
+          uint4* dst = reinterpret_cast<uint4*>(out + c);
+#pragma unroll
+          for (uint32_t x = 0; x < 4; ++x)
+            dst[x] = make_uint4(pack2(o[8 * x] * inv, o[8 * x + 1] * inv), pack2(o[8 * x + 2] * inv, o[8 * x + 3] * inv),
+                                pack2(o[8 * x + 4] * inv, o[8 * x + 5] * inv), pack2(o[8 * x + 6] * inv, o[8 * x + 7] * inv));
+        }
+        __syncwarp();
+      }
+      if (mine) {
+        if (p.splits > 1) {
+          float2* ml = reinterpret_cast<float2*>(p.part_ml) + (size_t)it.sp * n_rowids + rowid;
+          *ml = make_float2(l != l && m_ref == -INFINITY ? 0.f : m_ref, l);
+        } else if (a.lse) {
+          a.lse[rowid] = dead ? -INFINITY : (m_ref + lg2f(l)) * LN2_F;
+        }
+      }
+    }
+    if (!ok) { *abort_flag = 1; atomicExch(a.status, 1u); }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TC_TMEM) : "memory");
+  }
+}
+
+// The shares of the keys of one row joined: one warp per row and head of a paged call, two columns per lane.
+__global__ void __launch_bounds__(256) k_attn_join(const AttnArgs a, const float* part_o, const float* part_ml, uint32_t splits) {
+  griddep_sync();
+  const uint32_t lane = threadIdx.x & 31;
+  const size_t n_rowids = (size_t)a.n_rows * a.heads;
+  for (size_t id = ((size_t)blockIdx.x * 256 + threadIdx.x) >> 5; id < n_rowids; id += (size_t)gridDim.x * 8) {
+    const uint32_t row = (uint32_t)(id / a.heads), h = (uint32_t)(id % a.heads);
+    const SeqGeo g = seq_geo(a, seq_of_row(a, row));
+    if (row < g.row0 || row - g.row0 >= g.cnt) continue;     // belongs to no sequence of the call
+    float m = -INFINITY;
+    for (uint32_t s = 0; s < splits; ++s) m = fmaxf(m, part_ml[((size_t)s * n_rowids + id) * 2]);
+    float l = 0.f;
+    float2 o = make_float2(0.f, 0.f);
+    if (m != -INFINITY) {
+      for (uint32_t s = 0; s < splits; ++s) {
+        const float2 ml = *reinterpret_cast<const float2*>(part_ml + ((size_t)s * n_rowids + id) * 2);
+        if (ml.y == 0.f) continue;                           // nothing seen in this share
+        const float c = ex2f(ml.x - m);
+        const float2 x = *reinterpret_cast<const float2*>(part_o + ((size_t)s * n_rowids + id) * 64 + lane * 2);
+        l = fmaf(ml.y, c, l);
+        o.x = fmaf(x.x, c, o.x);
+        o.y = fmaf(x.y, c, o.y);
+      }
+    }
+    const float inv = m == -INFINITY ? 0.f : 1.f / l;
+    *reinterpret_cast<uint32_t*>(a.out.ptr + (long long)row * a.out.tok + (long long)h * a.out.head + lane * 2) = pack2(o.x * inv, o.y * inv);
+    if (a.lse && lane == 0) a.lse[id] = m == -INFINITY ? -INFINITY : (m + lg2f(l)) * LN2_F;
+  }
+}
+
+cudaError_t setup_attn_tc() {
+  cudaError_t e = tensor_map_setup();
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(k_attn_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM);
+}
+
+// A call over whole sequences, or over a paged cache.  part: scratch for part_units x (row, head, share) results of a
+// paged call (66 floats each), or null: the keys are not split.
+cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, int sm_count, cudaStream_t st) {
+  if (a.n_seqs == 0 || a.n == 0) return cudaSuccess;
+  const bool paged = a.pages != nullptr;
+  alignas(64) CUtensorMap map_q, map_k, map_v;
+  TcPlan p{};
+  p.rt = 128 / a.group * a.group;
+  const uint64_t seq_rows = (uint64_t)a.n * a.group;
+  p.qtiles = (uint32_t)((seq_rows + 2 * p.rt - 1) / (2 * p.rt));
+  p.splits = 1;
+  const uint64_t items = (uint64_t)p.qtiles * a.n_seqs * a.kv_heads;
+  if (paged && part) {
+    // shares of at least two key tiles, as many as it takes to give every SM an item
+    const uint64_t cap = std::min<uint64_t>(a.max_len, (uint64_t)a.pages_ld << a.page_shift), tiles = (cap + TC_KEYS - 1) / TC_KEYS;
+    const uint64_t rows = (uint64_t)a.n_rows * a.heads;
+    uint64_t sp = (uint64_t)sm_count / items;
+    sp = std::min(sp, (tiles + 1) / 2);
+    sp = std::min<uint64_t>(sp, part_units / rows);
+    if (sp > 1) p.splits = (uint32_t)sp;
+    p.part_o = part;
+    p.part_ml = part + (size_t)p.splits * rows * 64;
+  }
+  if (items * p.splits > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+  p.n_items = (uint32_t)(items * p.splits);
+  const uint64_t seqs = paged ? 1 : a.n_seqs, toks = paged ? a.n_rows : a.n;
+  if (!make_tensor_map_rows(&map_q, a.q, a.heads, toks, seqs, a.group, p.rt / a.group)) return cudaErrorInvalidValue;
+  if (paged) {
+    const uint32_t ps = 1u << a.page_shift;
+    p.page_box = ps < TC_KEYS ? ps : TC_KEYS;
+    p.page_rows = (int)(a.page_stride / 64);
+    const uint64_t rows = (uint64_t)(a.num_pages - 1) * (a.page_stride / 64) + (uint64_t)a.kv_heads * ps;
+    p.oob_row = (int)rows;
+    if (!make_tensor_map_bf16(&map_k, a.k_pages, rows, 64, p.page_box) || !make_tensor_map_bf16(&map_v, a.v_pages, rows, 64, p.page_box))
+      return cudaErrorInvalidValue;
+  } else {
+    if (!make_tensor_map_rows(&map_k, a.k, a.kv_heads, a.n, a.n_seqs, 1, TC_KEYS) ||
+        !make_tensor_map_rows(&map_v, a.v, a.kv_heads, a.n, a.n_seqs, 1, TC_KEYS))
+      return cudaErrorInvalidValue;
+  }
+  const uint32_t grid = p.n_items < (uint32_t)sm_count ? p.n_items : (uint32_t)sm_count;
+  cudaError_t e = launch_k(k_attn_tc, dim3(grid), dim3(TC_THREADS), TC_SMEM, st, map_q, map_k, map_v, a, p);
+  if (e != cudaSuccess || p.splits == 1) return e;
+  const uint64_t warps = (uint64_t)a.n_rows * a.heads;
+  const uint64_t blocks = std::min<uint64_t>((warps + 7) / 8, (uint64_t)sm_count * 8);
+  return launch_k(k_attn_join, dim3((uint32_t)blocks), dim3(256), 0, st, a, (const float*)p.part_o, (const float*)p.part_ml, p.splits);
+}
+
+}  // namespace llmc

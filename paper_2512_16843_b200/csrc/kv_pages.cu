@@ -15,12 +15,7 @@ __global__ void __launch_bounds__(256) k_kv_append(const AttnArgs a) {
   const unsigned long long items = (unsigned long long)a.n_rows * a.kv_heads * 16;
   for (unsigned long long id = (unsigned long long)blockIdx.x * 256 + threadIdx.x; id < items; id += (unsigned long long)gridDim.x * 256) {
     const uint32_t part = id & 15u, hk = (uint32_t)((id >> 4) % a.kv_heads), row = (uint32_t)((id >> 4) / a.kv_heads);
-    // the sequence of this row: the last one whose first row is not behind it
-    uint32_t lo = 0, hi = a.n_seqs;
-    while (hi - lo > 1) {
-      const uint32_t mid = (lo + hi) / 2;
-      if (a.cu[mid] <= (int32_t)row) lo = mid; else hi = mid;
-    }
+    const uint32_t lo = seq_of_row(a, row);
     const SeqGeo g = seq_geo(a, lo);
     if (row < g.row0 || row - g.row0 >= g.cnt) continue;             // behind the last sequence
     const long long slot = (long long)g.slot0 + (row - g.row0);

@@ -1,6 +1,7 @@
 // Host-side construction of TMA tensor maps.
 #include "llmcache_internal.cuh"
 #include "ptx.cuh"
+#include "attn.cuh"
 
 namespace llmc {
 
@@ -44,6 +45,20 @@ bool make_tensor_map_bf16_box32(CUtensorMap* map, const void* ptr, uint64_t rows
   const cuuint32_t estr[2] = {1, 1};
   return g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool make_tensor_map_rows(CUtensorMap* map, const RowsArgs& r, uint64_t heads, uint64_t toks, uint64_t seqs, uint32_t box_heads,
+                          uint32_t box_toks) {
+  if (!g_encode) return false;
+  // (the stride of a dimension of size one is never used: any valid one will do)
+  const cuuint64_t dims[4] = {64, heads, toks, seqs};
+  const cuuint64_t strides[3] = {heads > 1 ? (cuuint64_t)r.head * 2 : 128, toks > 1 ? (cuuint64_t)r.tok * 2 : 128,
+                                 seqs > 1 ? (cuuint64_t)r.seq * 2 : 128};
+  const cuuint32_t box[4] = {64u, box_heads, box_toks, 1u};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, r.ptr, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
