@@ -23,14 +23,9 @@
 // Every wait is bounded (status word).
 #include <cuda.h>
 #include <algorithm>
-#include "attn.cuh"
-#include "ptx.cuh"
+#include "attn_dev.cuh"
 
 namespace llmc {
-
-// bf16 rows of 64 columns (llmcache_rows), boxes of box_heads x box_toks rows, 128-byte swizzle, zero fill outside
-bool make_tensor_map_rows(CUtensorMap* map, const RowsArgs& r, uint64_t heads, uint64_t toks, uint64_t seqs, uint32_t box_heads,
-                          uint32_t box_toks);
 
 namespace {
 
@@ -60,25 +55,6 @@ static_assert(TC_SMEM <= 232448, "shared memory of one block");
 constexpr uint32_t TC_IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
 constexpr uint32_t TC_IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
 
-__device__ __forceinline__ float ex2f(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float lg2f(float x) {
-  float y;
-  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float max3f(float a, float b, float c) {
-  float y;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
 // D[tmem] (+)= A[tmem] * B[smem], bf16 inputs, f32 accumulate
 __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -86,15 +62,6 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
-}
-// the loads before it are complete and their registers may be read (they pass through the statement)
-__device__ __forceinline__ void tc_wait_ld32(uint32_t (&v)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
-                 "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
-               :: "memory");
-  asm volatile("" : "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
-                    "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]) :: "memory");
 }
 __device__ __forceinline__ void tc_st_16(uint32_t taddr, const uint32_t* v) {
   asm volatile(
@@ -104,18 +71,6 @@ __device__ __forceinline__ void tc_st_16(uint32_t taddr, const uint32_t* v) {
         "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
-}
-// mbar_wait by a whole warp: all lanes get the same answer, so that they leave together when a wait runs out
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, unsigned long long limit_ns,
-                                          uint32_t backoff_ns) {
-  return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, limit_ns, backoff_ns));
-}
-__device__ __forceinline__ unsigned long long f2_dup(float x) { return f2_pack(x, x); }
-
 // Launch shape, the same for every role.
 struct TcPlan {
   uint32_t rt;                   // rows of a query tile: the largest multiple of the group up to 128
@@ -166,19 +121,6 @@ __device__ __forceinline__ uint32_t tiles_of(const AttnArgs& a, const TcPlan& p,
   if (first >= it.rows) return 0;
   return (keys_to(a, it, (min(it.rows, first + p.rt) - 1) / a.group) + TC_KEYS - 1) / TC_KEYS;
 }
-
-// tanh of two values: an odd polynomial on |u| <= 0.75 (tanh_fit.py, relative error 1.4e-7)
-__device__ __forceinline__ unsigned long long tanh_small2(unsigned long long u) {
-  const unsigned long long s = f2_mul(u, u);
-  unsigned long long q = f2_fma(f2_dup(-4.723952152e-03f), s, f2_dup(1.959378645e-02f));
-  q = f2_fma(q, s, f2_dup(-5.334981903e-02f));
-  q = f2_fma(q, s, f2_dup(1.332551539e-01f));
-  q = f2_fma(q, s, f2_dup(-3.333296776e-01f));
-  q = f2_fma(q, s, f2_dup(1.0f));
-  return f2_mul(u, q);
-}
-// 1 - 2 / (1 + e^2u): for |u| > 0.75, where the difference loses nothing
-__device__ __forceinline__ float tanh_large(float u) { return 1.f - __fdividef(2.f, 1.f + ex2f(2.f * LOG2E_F * u)); }
 
 }  // namespace
 

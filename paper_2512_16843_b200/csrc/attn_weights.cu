@@ -1,82 +1,356 @@
-// Received weights of a paged call, one thread per key.
-#include "attn.cuh"
-#include "ptx.cuh"
+// Received weights of a paged call: weights[key] = decay * weights[key] + sum over the call's rows, and over the query heads
+// that share the key, of exp(z - lse).  The scores are formed again, with the keys as the rows of the product:
+//   S^T = K Q^T    tcgen05.mma 128 keys x up to 128 query rows x 64
+// so that a thread owns a key and its sum over the rows needs no exchange and no atomics (same bits every time).  A block
+// takes a sequence and head and every parts-th key tile of it; the query rows stream past each key tile (they come from
+// L2).  Two groups of four warps take turns with the query tiles, two blocks per SM.  Reads K once more (128 bytes per
+// key and head) and the queries; one exponential per score, as in the attention itself.
+// f32 throughout; every wait is bounded (status word).
+#include <algorithm>
+#include "attn_dev.cuh"
 
 namespace llmc {
 
 namespace {
 
-// softmax exponent of a score in base-2 units; apart: key position - query position
-__device__ __forceinline__ float modified(const ScoreArgs& m, float dot, uint32_t h, int32_t apart) {
-  float z = dot * m.scale;
-  if (m.cap > 0.f) z = m.cap * tanhf(z / m.cap);
-  if (m.slopes) z -= m.slopes[h] * (float)abs(apart);
-  if (m.table) z += m.table[(size_t)h * (2 * m.reach + 1) + min(max(apart, -m.reach), m.reach) + m.reach];
-  return z;
-}
+constexpr int WT_THREADS = 384;                              // warp 0: loads, 1: products, 2-3: row data, 4-11: sums
+constexpr uint32_t WT_ST = 3, WT_TILE = 16384, WT_KEYS = 128, WT_TMEM = 256;
+struct WtSmem {
+  static constexpr uint32_t K = 0;                           // [2]
+  static constexpr uint32_t Q = K + 2 * WT_TILE;             // [WT_ST]
+  static constexpr uint32_t LSE = Q + WT_ST * WT_TILE;       // f32 [stage][128], base 2; +inf: the row gives nothing
+  static constexpr uint32_t SLOPE = LSE + WT_ST * 512;       // f32 [stage][128]
+  static constexpr uint32_t QPOS = SLOPE + WT_ST * 512;      // i32 [stage][128]
+  static constexpr uint32_t HI = QPOS + WT_ST * 512;         // i32 [stage][128]: keys below it are seen
+  static constexpr uint32_t TAB = HI + WT_ST * 512;          // i32 [stage][128]: middle of the head's row of the table
+  static constexpr uint32_t XCH = TAB + WT_ST * 512;         // f32 [2][128]
+  static constexpr uint32_t BAR = XCH + 1024;
+  static constexpr uint32_t MISC = BAR + 24 * 8;
+  static constexpr uint32_t TOTAL = MISC + 64;
+};
+constexpr uint32_t WT_SMEM = WtSmem::TOTAL + 1024;
 
-__device__ __forceinline__ float dot64(const __nv_bfloat16* a, const float* b) {
-  float s = 0.f;
-  const uint4* p = reinterpret_cast<const uint4*>(a);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint4 w = p[i];
-    const uint32_t q[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      s = fmaf(__uint_as_float(q[u] << 16), b[i * 8 + 2 * u], s);
-      s = fmaf(__uint_as_float(q[u] & 0xFFFF0000u), b[i * 8 + 2 * u + 1], s);
-    }
-  }
-  return s;
-}
-
-// one thread per (sequence, key/value head, slot)
-__global__ void __launch_bounds__(128) k_attn_weights_rows(AttnArgs a, uint32_t cap) {
-  griddep_sync();
-  const unsigned long long total = (unsigned long long)a.n_seqs * a.kv_heads * cap;
-  for (unsigned long long id = (unsigned long long)blockIdx.x * 128 + threadIdx.x; id < total; id += (unsigned long long)gridDim.x * 128) {
-    const uint32_t j = id % cap, hk = (id / cap) % a.kv_heads, s = id / cap / a.kv_heads;
-    const SeqGeo g = seq_geo(a, s);
-    if (j >= g.len) continue;
-    float sum = 0.f;
-    const int32_t p = page_of(a, s, j);
-    const size_t side = ((size_t)s * a.kv_heads + hk) * a.side_ld + j;
-    if (p >= 0) {
-      float kk[64];
-      const __nv_bfloat16* krow = a.k_pages + page_row(a, p, hk, j);
-      for (int c = 0; c < 64; ++c) kk[c] = __bfloat162float(krow[c]);
-      const int32_t kpos = a.positions ? a.positions[side] : (int32_t)j;
-      for (uint32_t i = 0; i < g.cnt; ++i) {
-        const long long my_slot = (long long)g.slot0 + i;
-        if (a.m.causal && (long long)j > my_slot) continue;
-        const long long qpos = a.first ? (long long)a.first[s] + i : my_slot;
-        for (uint32_t h = hk * a.group; h < (hk + 1) * a.group; ++h) {
-          const __nv_bfloat16* q = a.q.ptr + (long long)(g.row0 + i) * a.q.tok + (long long)h * a.q.head;
-          const float lse = a.lse[(size_t)(g.row0 + i) * a.heads + h];
-          const float z = modified(a.m, dot64(q, kk), h, (int32_t)(kpos - qpos));
-          if (lse != -INFINITY) sum += expf(z - lse);
-        }
-      }
-    }
-    a.weights[side] = a.decay == 0.f ? sum : a.decay * a.weights[side] + sum;
-  }
-}
+struct WtPlan {
+  uint32_t rt, cols;             // query rows per tile; columns of the product (rt rounded up to 16)
+  uint32_t parts, page_box;
+  int page_rows, oob_row;
+};
 
 }  // namespace
 
-cudaError_t setup_attn_kernels() { return setup_attn_tc(); }
+__global__ void __launch_bounds__(WT_THREADS, 2)
+k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+               const __grid_constant__ AttnArgs a, const __grid_constant__ WtPlan p) {
+  griddep_sync();
+  const uint32_t part = blockIdx.x % p.parts, hk = (blockIdx.x / p.parts) % a.kv_heads, sq = blockIdx.x / p.parts / a.kv_heads;
+  const SeqGeo g = seq_geo(a, sq);
+  const uint32_t rows = g.cnt * a.group, nt = (g.len + WT_KEYS - 1) / WT_KEYS, qtiles = (rows + p.rt - 1) / p.rt;
+  if (part >= nt) return;                                    // uniform over the block; nothing allocated yet
+  const size_t side0 = ((size_t)sq * a.kv_heads + hk) * a.side_ld;
+  if (rows == 0) {                                           // no rows: what was received before fades
+    for (uint32_t j = part; j < nt; j += p.parts)
+      for (uint32_t c = threadIdx.x; c < WT_KEYS; c += WT_THREADS)
+        if (j * WT_KEYS + c < g.len) {
+          float& w = a.weights[side0 + j * WT_KEYS + c];
+          w = a.decay == 0.f ? 0.f : a.decay * w;
+        }
+    return;
+  }
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gbase = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t bar0 = base + WtSmem::BAR;
+  auto q_full = [&](uint32_t s) { return bar0 + 8 * s; };
+  auto side_full = [&](uint32_t s) { return bar0 + 8 * (WT_ST + s); };
+  auto empty = [&](uint32_t s) { return bar0 + 8 * (2 * WT_ST + s); };
+  const uint32_t bar1 = bar0 + 8 * 3 * WT_ST;
+  auto k_full = [&](uint32_t b) { return bar1 + 8 * b; };
+  auto k_empty = [&](uint32_t b) { return bar1 + 8 * (2 + b); };
+  auto s_full = [&](uint32_t w) { return bar1 + 8 * (4 + w); };
+  auto s_empty = [&](uint32_t w) { return bar1 + 8 * (6 + w); };
+  auto x_full = [&](uint32_t b) { return bar1 + 8 * (8 + b); };
+  auto x_empty = [&](uint32_t b) { return bar1 + 8 * (10 + b); };
+  const uint32_t drain = bar1 + 8 * 12;
+  volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(gbase + WtSmem::MISC);
+  volatile uint32_t* abort_flag = misc + 1;
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const unsigned long long lim = wait_limit(a.status);
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < WT_ST; ++s) { mbar_init(q_full(s), 1); mbar_init(side_full(s), 2); mbar_init(empty(s), 1 + 4); }
+    for (uint32_t b = 0; b < 2; ++b) {
+      mbar_init(k_full(b), 1); mbar_init(k_empty(b), 1); mbar_init(s_full(b), 1); mbar_init(s_empty(b), 128);
+      mbar_init(x_full(b), 128); mbar_init(x_empty(b), 128);
+    }
+    mbar_init(drain, 1);
+    misc[1] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32((const void*)misc)), "r"(WT_TMEM) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = misc[0];
+
+  // entry n of the block: key tile number n / qtiles of its own, query tile n % qtiles; group n % 2 of the summing warps
+  if (warp == 0) {
+    bool ok = true;
+    uint32_t n = 0, t = 0;
+    for (uint32_t j = producer_idle(a.status) ? nt : part; j < nt && ok; j += p.parts, ++t) {
+      const uint32_t boxes = WT_KEYS / p.page_box;
+      int row = 0;
+      if (lane < boxes) {
+        const uint32_t slot = j * WT_KEYS + lane * p.page_box;
+        const int32_t pg = slot < g.len ? page_of(a, sq, slot) : -1;
+        row = pg < 0 ? p.oob_row : pg * p.page_rows + (int)((hk << a.page_shift) + (slot & ((1u << a.page_shift) - 1u)));
+      }
+      ok = warp_wait(k_empty(t & 1u), ((t >> 1) & 1u) ^ 1u, abort_flag, lim, 32);
+      if (!ok) break;
+      if (lane == 0) mbar_expect_tx(k_full(t & 1u), WT_TILE);
+      __syncwarp();
+      if (lane < boxes) tma_load_2d(base + WtSmem::K + (t & 1u) * WT_TILE + lane * p.page_box * 128, &map_k, 0, row, k_full(t & 1u));
+      for (uint32_t qt = 0; qt < qtiles; ++qt, ++n) {
+        const uint32_t s = n % WT_ST;
+        ok = warp_wait(empty(s), ((n / WT_ST) & 1u) ^ 1u, abort_flag, lim, 32);
+        if (!ok) break;
+        if (lane == 0) {
+          mbar_expect_tx(q_full(s), p.rt * 128);
+          tma_load_4d(base + WtSmem::Q + s * WT_TILE, &map_q, 0, (int)(hk * a.group), (int)(g.row0 + qt * (p.rt / a.group)), 0, q_full(s));
+        }
+      }
+    }
+    if (!ok && lane == 0) { *abort_flag = 1; atomicExch(a.status, 1u); }
+    __syncwarp();
+    if (lane == 0 && *abort_flag) {                          // loads in flight must land before shared memory is released
+      volatile uint32_t never = 0;
+      const uint32_t tk = ok ? t : t + 1;
+      for (uint32_t b = 0; b < 2 && b < tk; ++b) mbar_wait(k_full((tk - 1 - b) & 1u), ((tk - 1 - b) >> 1) & 1u, &never, 200000000ull);
+      for (uint32_t b = 0; b < WT_ST && b < n; ++b) mbar_wait(q_full((n - 1 - b) % WT_ST), ((n - 1 - b) / WT_ST) & 1u, &never, 200000000ull);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((p.cols >> 3) << 17) | ((128u >> 4) << 24);
+      bool ok = true;
+      uint32_t n = 0, t = 0;
+      for (uint32_t j = part; j < nt && ok; j += p.parts, ++t) {
+        if (!mbar_wait(k_full(t & 1u), (t >> 1) & 1u, abort_flag, lim, 32)) { ok = false; break; }
+        const uint64_t dk = smem_desc_sw128(base + WtSmem::K + (t & 1u) * WT_TILE);
+        for (uint32_t qt = 0; qt < qtiles; ++qt, ++n) {
+          const uint32_t s = n % WT_ST, w = n & 1u;
+          if (!mbar_wait(q_full(s), (n / WT_ST) & 1u, abort_flag, lim, 32) ||
+              !mbar_wait(s_empty(w), ((n >> 1) & 1u) ^ 1u, abort_flag, lim, 20)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t dq = smem_desc_sw128(base + WtSmem::Q + s * WT_TILE);
+#pragma unroll
+          for (uint32_t kk = 0; kk < 4; ++kk) tc_mma_bf16(tmem + w * 128, dk + kk * 2, dq + kk * 2, idesc, kk != 0u);
+          tc_commit(s_full(w));
+          tc_commit(empty(s));
+        }
+        if (ok) tc_commit(k_empty(t & 1u));
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        atomicExch(a.status, 1u);
+        volatile uint32_t never = 0;
+        tc_commit(drain);
+        mbar_wait(drain, 0u, &never, 200000000ull);
+      }
+    }
+  } else if (warp < 4) {
+    bool ok = true;
+    const uint32_t total = ((nt - part + p.parts - 1) / p.parts) * qtiles;
+    for (uint32_t n = 0; n < total; ++n) {
+      const uint32_t s = n % WT_ST, qt = n % qtiles;
+      ok = warp_wait(empty(s), ((n / WT_ST) & 1u) ^ 1u, abort_flag, lim, 32);
+      if (!ok) break;
+#pragma unroll
+      for (uint32_t u = 0; u < 2; ++u) {
+        const uint32_t c = u * 64 + threadIdx.x - 64, R = qt * p.rt + c;
+        const uint32_t token = R / a.group, h = hk * a.group + R % a.group;
+        const bool real = c < p.rt && R < rows;
+        float lse = INFINITY;
+        if (real) {
+          lse = a.lse[(size_t)(g.row0 + token) * a.heads + h] * LOG2E_F;
+          if (lse == -INFINITY) lse = INFINITY;
+        }
+        const uint32_t at = s * 128 + c;
+        reinterpret_cast<float*>(gbase + WtSmem::LSE)[at] = lse;
+        if (a.m.slopes) reinterpret_cast<float*>(gbase + WtSmem::SLOPE)[at] = real ? a.m.slopes[h] * LOG2E_F : 0.f;
+        if (a.m.table) reinterpret_cast<int32_t*>(gbase + WtSmem::TAB)[at] = (int32_t)((real ? h : 0u) * (2 * a.m.reach + 1)) + a.m.reach;
+        reinterpret_cast<int32_t*>(gbase + WtSmem::QPOS)[at] = a.first ? a.first[sq] + (int32_t)token : g.slot0 + (int32_t)token;
+        reinterpret_cast<int32_t*>(gbase + WtSmem::HI)[at] =
+            !real ? 0 : a.m.causal ? min(g.slot0 + (int32_t)token + 1, (int32_t)g.len) : (int32_t)g.len;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(side_full(s));
+    }
+    if (!ok && lane == 0) { *abort_flag = 1; atomicExch(a.status, 1u); }
+  } else {
+    const uint32_t w = (warp - 4) >> 2, quarter = warp & 3u, key_in = quarter * 32 + lane;
+    const uint32_t t_s = tmem + w * 128 + ((quarter * 32u) << 16);
+    const bool modified = a.m.cap > 0.f || a.m.slopes || a.m.table;
+    const float sc = a.m.scale * LOG2E_F, sc_in = a.m.cap > 0.f ? a.m.scale / a.m.cap : sc;
+    float* xch = reinterpret_cast<float*>(gbase + WtSmem::XCH);
+    bool ok = true;
+    uint32_t n = 0, mine = 0, t = 0;                         // entries of the block, of this group; key tiles
+    for (uint32_t j = part; j < nt && ok; j += p.parts, ++t) {
+      const uint32_t key = j * WT_KEYS + key_in;
+      const bool real = key < g.len;
+      const bool there = real && page_of(a, sq, key) >= 0;
+      const int32_t kpos = a.positions && real ? a.positions[side0 + key] : (int32_t)key;
+      float sum = 0.f;
+      for (uint32_t qt = 0; qt < qtiles; ++qt, ++n) {
+        if ((n & 1u) != w) continue;
+        const uint32_t s = n % WT_ST;
+        ok = warp_wait(side_full(s), (n / WT_ST) & 1u, abort_flag, lim, 32) && warp_wait(s_full(w), mine & 1u, abort_flag, lim, 20);
+        if (!ok) break;
+        ++mine;
+        tc_fence_after();
+        const float* lse = reinterpret_cast<const float*>(gbase + WtSmem::LSE) + s * 128;
+        const float* slope = reinterpret_cast<const float*>(gbase + WtSmem::SLOPE) + s * 128;
+        const int32_t* qpos = reinterpret_cast<const int32_t*>(gbase + WtSmem::QPOS) + s * 128;
+        const int32_t* hi = reinterpret_cast<const int32_t*>(gbase + WtSmem::HI) + s * 128;
+        const int32_t* tab = reinterpret_cast<const int32_t*>(gbase + WtSmem::TAB) + s * 128;
+        const uint32_t n_rows = min(p.rt, rows - qt * p.rt);
+        float s0 = 0.f, s1 = 0.f;
+#pragma unroll 1
+        for (uint32_t c = 0; c < n_rows; c += 32) {
+          uint32_t v[32];
+          tc_ld_32x32(t_s + c, v);
+          tc_wait_ld32(v);
+          unsigned long long x[16];
+          const unsigned long long sc2 = f2_dup(sc_in);
+#pragma unroll
+          for (uint32_t i = 0; i < 16; ++i) x[i] = f2_mul(f2_pack(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), sc2);
+          if (modified) {
+            if (a.m.cap > 0.f) {
+              float big = 0.f;
+#pragma unroll
+              for (uint32_t i = 0; i < 16; ++i) big = max3f(big, fabsf(f2_lo(x[i])), fabsf(f2_hi(x[i])));
+              const unsigned long long cap2 = f2_dup(a.m.cap * LOG2E_F);
+              const bool large = __any_sync(0xFFFFFFFFu, !(big <= 0.75f));
+#pragma unroll
+              for (uint32_t i = 0; i < 16; ++i) {
+                unsigned long long y = tanh_small2(x[i]);
+                if (large) {
+                  const float u0 = f2_lo(x[i]), u1 = f2_hi(x[i]);
+                  y = f2_pack(fabsf(u0) <= 0.75f ? f2_lo(y) : tanh_large(u0), fabsf(u1) <= 0.75f ? f2_hi(y) : tanh_large(u1));
+                }
+                x[i] = f2_mul(y, cap2);
+              }
+            }
+            if (a.m.slopes) {
+#pragma unroll
+              for (uint32_t i = 0; i < 16; ++i) {
+                const int2 q = *reinterpret_cast<const int2*>(qpos + c + 2 * i);
+                const float2 sl = *reinterpret_cast<const float2*>(slope + c + 2 * i);
+                x[i] = f2_fma(f2_pack(fabsf((float)(kpos - q.x)), fabsf((float)(kpos - q.y))), f2_pack(-sl.x, -sl.y), x[i]);
+              }
+            }
+            if (a.m.table) {
+              const int32_t reach = a.m.reach;
+#pragma unroll
+              for (uint32_t i = 0; i < 16; ++i) {
+                const int2 q = *reinterpret_cast<const int2*>(qpos + c + 2 * i), o = *reinterpret_cast<const int2*>(tab + c + 2 * i);
+                // (rows that do not exist point at head 0)
+                const float b0 = __ldg(a.m.table + o.x + min(max(kpos - q.x, -reach), reach));
+                const float b1 = __ldg(a.m.table + o.y + min(max(kpos - q.y, -reach), reach));
+                x[i] = f2_add(x[i], f2_pack(b0 < -1e38f ? b0 : b0 * LOG2E_F, b1 < -1e38f ? b1 : b1 * LOG2E_F));
+              }
+            }
+          }
+          // (the rows of a tile see ever more keys: the first row of the chunk sees the fewest)
+          const bool all = c + 32 <= n_rows && hi[c] >= (int32_t)((j + 1) * WT_KEYS);
+#pragma unroll
+          for (uint32_t i = 0; i < 16; ++i) {
+            const float2 ls = *reinterpret_cast<const float2*>(lse + c + 2 * i);
+            float p0 = ex2f(f2_lo(x[i]) - ls.x), p1 = ex2f(f2_hi(x[i]) - ls.y);
+            if (!all) {
+              const int2 b = *reinterpret_cast<const int2*>(hi + c + 2 * i);
+              if ((int32_t)key >= b.x) p0 = 0.f;
+              if ((int32_t)key >= b.y) p1 = 0.f;
+            }
+            s0 += p0;
+            s1 += p1;
+          }
+        }
+        sum += s0 + s1;
+        tc_fence_before();
+        mbar_arrive(s_empty(w));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(s));
+      }
+      if (!ok) break;
+      // several query tiles: the two groups' sums are added; one: the group that had it stores
+      bool store = real && ((n - 1) & 1u) == w;
+      if (qtiles > 1) {
+        float* x = xch + (t & 1u) * 128;
+        const uint32_t ph = (t >> 1) & 1u;
+        if (w == 1) {
+          ok = warp_wait(x_empty(t & 1u), ph ^ 1u, abort_flag, lim, 20);
+          if (!ok) break;
+          x[key_in] = sum;
+          mbar_arrive(x_full(t & 1u));
+        } else {
+          ok = warp_wait(x_full(t & 1u), ph, abort_flag, lim, 20);
+          if (!ok) break;
+          sum += x[key_in];
+          mbar_arrive(x_empty(t & 1u));
+        }
+        store = real && w == 0;
+      }
+      if (store) {
+        float& dst = a.weights[side0 + key];
+        const float got = there ? sum : 0.f;
+        dst = a.decay == 0.f ? got : fmaf(a.decay, dst, got);
+      }
+    }
+    if (!ok) { *abort_flag = 1; atomicExch(a.status, 1u); }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(WT_TMEM) : "memory");
+  }
+}
+
+cudaError_t setup_attn_kernels() {
+  const cudaError_t e = setup_attn_tc();
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(k_attn_weights, cudaFuncAttributeMaxDynamicSharedMemorySize, WT_SMEM);
+}
 
 cudaError_t launch_attn(const AttnArgs& a, float* part, size_t part_units, int sm_count, cudaStream_t st) {
   return launch_attn_tc(a, part, part_units, sm_count, st);
 }
 
 cudaError_t launch_attn_weights(const AttnArgs& a, int sm_count, cudaStream_t st) {
-  const unsigned long long cap = (unsigned long long)a.pages_ld << a.page_shift;
-  const uint32_t c = cap < a.max_len ? (uint32_t)cap : a.max_len;
-  const unsigned long long blocks = ((unsigned long long)a.n_seqs * a.kv_heads * c + 127) / 128, most = (unsigned long long)sm_count * 16;
-  if (blocks == 0) return cudaSuccess;
-  return launch_k(k_attn_weights_rows, dim3((uint32_t)(blocks < most ? blocks : most)), dim3(128), 0, st, a, c);
+  if (a.n_seqs == 0) return cudaSuccess;
+  alignas(64) CUtensorMap map_q, map_k;
+  WtPlan p{};
+  const uint32_t toks = std::min(128 / a.group, a.n);        // tokens of a query tile
+  p.rt = toks * a.group;
+  p.cols = (p.rt + 15) / 16 * 16;
+  const uint32_t ps = 1u << a.page_shift;
+  p.page_box = std::min(ps, WT_KEYS);
+  p.page_rows = (int)(a.page_stride / 64);
+  const uint64_t rows = (uint64_t)(a.num_pages - 1) * (a.page_stride / 64) + (uint64_t)a.kv_heads * ps;
+  p.oob_row = (int)rows;
+  const uint64_t cap = std::min<uint64_t>(a.max_len, (uint64_t)a.pages_ld << a.page_shift), tiles = (cap + WT_KEYS - 1) / WT_KEYS;
+  // about eight blocks per SM: enough for even shares, few enough that the ends of wide tables cost little
+  const uint64_t pairs = (uint64_t)a.n_seqs * a.kv_heads, want = ((uint64_t)sm_count * 8 + pairs - 1) / pairs;
+  p.parts = (uint32_t)std::min(tiles, want);
+  if (pairs * p.parts > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+  if (!make_tensor_map_rows(&map_q, a.q, a.heads, a.n_rows, 1, a.group, toks) ||
+      !make_tensor_map_bf16(&map_k, a.k_pages, rows, 64, p.page_box))
+    return cudaErrorInvalidValue;
+  return launch_k(k_attn_weights, dim3((uint32_t)(pairs * p.parts)), dim3(WT_THREADS), WT_SMEM, st, map_q, map_k, a, p);
 }
 
 }  // namespace llmc

@@ -328,7 +328,9 @@ def run_chunk(p, rows, mine, ref, *, seed, weights=None, decay=1.0, positions=No
         got = f64(w)
         # each of the summed softmax values is relatively exact (see above); decay * w and the sum round once each
         terms = max(rows) * (p.H // p.HK)
-        tol = rw * (2 * d + 2.0 ** -20 + (n + terms) * 2.0 ** -24) + 2.0 ** -126
+        # (f32 has no normal numbers below 2^-126 and the exponential flushes there: each of the `terms` summed values may
+        # lose up to 2^-126, so the sum up to terms * 2^-126)
+        tol = rw * (2 * d + 2.0 ** -20 + (n + terms) * 2.0 ** -24) + terms * 2.0 ** -126
         assert np.all(np.abs(got - rw) <= tol), float(np.max(np.abs(got - rw) - tol))
     if cache is None:
         kv.close()
