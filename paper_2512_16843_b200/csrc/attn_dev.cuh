@@ -45,10 +45,31 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
       ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0u;
+}
+// The loop of a wait, out of line: what is not ready at once has time for a call, and the code around stays together.
+__device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, unsigned long long limit_ns,
+                                       uint32_t backoff_ns) {
+  return mbar_wait(bar, parity, abort_flag, limit_ns, backoff_ns);
+}
+__device__ __forceinline__ bool wait_one(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, unsigned long long limit_ns) {
+  return mbar_try(bar, parity) || wait_long(bar, parity, abort_flag, limit_ns, 0);
+}
 // mbar_wait by a whole warp: all lanes get the same answer, so that they leave together when a wait runs out
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, unsigned long long limit_ns,
                                           uint32_t backoff_ns) {
-  return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, limit_ns, backoff_ns));
+  if (__all_sync(0xFFFFFFFFu, mbar_try(bar, parity))) return true;
+  return __all_sync(0xFFFFFFFFu, wait_long(bar, parity, abort_flag, limit_ns, backoff_ns));
 }
 __device__ __forceinline__ unsigned long long f2_dup(float x) { return f2_pack(x, x); }
 

@@ -6,11 +6,15 @@
 //
 // A block works on two tiles of up to 128 query rows that share the key and value tiles.  The query heads that share a
 // key/value head are rows of one tile (row = token * group + head of the group), so grouped heads read their keys once and
-// few tokens still fill the tile.  Roles: warp 0 loads (TMA) and decides which key tiles are needed; warp 1 issues the
-// products; warps 2-3 look after what comes with a key tile (document or position of every key, missing pages, values
-// that are not numbers); warps 4-7 and 8-11 do the softmax of one query tile each, one thread per row.  While one tile's
-// softmax runs, the other tile's products do.  The block walks its items (a sequence, a key/value head, 256 rows, and
-// a share of the keys where the rows alone do not fill the GPU), so the loads of the next item overlap the end of this one.
+// few tokens still fill the tile.  Roles: warp 0 walks the block's items (a sequence, a key/value head, 256 rows, and a
+// share of the keys where the rows alone do not fill the GPU), decides which key tiles they need and loads them (TMA);
+// warps 1 and 2 issue the products of one query tile each; warp 3 looks after what comes with a key tile (document or
+// position of every key, missing pages, values that are not numbers); warps 4-7 and 8-11 do the softmax of one query tile
+// each, one thread per row: a pass for the maximum (which leaves modified and masked scores in tensor memory) and one for the
+// exponentials.  P has columns of its own, so S is free for the next key tile as soon as the second pass has read it, and
+// neither product holds up the other.
+// What bounds it: the exponentials (16 per cycle and SM, 1,024 cycles per query and key tile, against 256 + 256 for the
+// two products).
 //
 // Maximum: O and the sums refer to a maximum m that is raised, and O scaled, only when a tile's maximum exceeds it by more
 // than 2^8: factors up to 2^8 lose nothing in f32 sums and in bf16 P (relative rounding), and O stays in tensor memory.
@@ -18,7 +22,7 @@
 // product takes bf16 operands; the sums are of the unrounded weights.
 //
 // Values that are not numbers: P is zero where a key is not seen, but 0 * inf is not.  So infinities and NaN are taken
-// out of a V tile before its product (warps 2-3 scan it: 3 instructions per 4 bytes, hidden behind the exponentials) and
+// out of a V tile before its product (warp 3 scans it: 3 instructions per 4 bytes, hidden behind the exponentials) and
 // listed; a row that sees a listed key gets them in its output at the end.
 // Every wait is bounded (status word).
 #include <cuda.h>
@@ -33,8 +37,10 @@ constexpr int TC_THREADS = 384;
 constexpr uint32_t TC_ST = 4;                                // stages of the ring of key and value tiles
 constexpr uint32_t TC_TILE = 16384;                          // 128 x 64 bf16
 constexpr uint32_t TC_KEYS = 128;
-constexpr uint32_t TC_TMEM = 512;                            // S0 | S1 (128 columns each, P over them) | O0 | O1 (64 each)
-enum : uint32_t { F_NEED0 = 1, F_NEED1 = 2, F_FIRST = 4, F_LAST = 8 };
+constexpr uint32_t TC_TMEM = 512;                            // S0 | S1 (128 columns each) | O0 | O1 | P0 | P1 (64 each)
+constexpr uint32_t TC_O = 256, TC_P = 384;
+enum : uint32_t { F_NEED0 = 1, F_NEED1 = 2, F_LAST = 4 };            // of a key tile
+enum : uint32_t { I_TILES = 1, I_STOP = 2 };                         // of an item: it has key tiles; there are no more items
 struct TcSmem {
   static constexpr uint32_t Q = 0;                           // [item parity][query tile]
   static constexpr uint32_t K = Q + 4 * TC_TILE;
@@ -44,9 +50,12 @@ struct TcSmem {
   static constexpr uint32_t KINFO = ROWP + 256 * 24;         // i32 [stage][key]: document or position
   static constexpr uint32_t KMASK = KINFO + TC_ST * 512;     // u32 [stage][4]: keys that exist
   static constexpr uint32_t DIRTY = KMASK + TC_ST * 16;      // u32 [stage][4]: keys listed in POISON
-  static constexpr uint32_t INFO = DIRTY + TC_ST * 16;       // u32 [stage][2]: key tile, flags
-  static constexpr uint32_t BAR = INFO + TC_ST * 8;
-  static constexpr uint32_t MISC = BAR + 32 * 8;
+  static constexpr uint32_t ONEDOC = DIRTY + TC_ST * 16;     // i32 [stage]: the document of all keys, -1: they differ
+  static constexpr uint32_t INFO = ONEDOC + TC_ST * 4;       // u32 [stage][2]: key tile, flags
+  static constexpr uint32_t ITEM = INFO + TC_ST * 8;         // ItemInfo [2]
+  static constexpr uint32_t MAIL = ITEM + 128;               // u32 [query tile][2]: number of the key tile in the block's stream (~0: the item's end), key tile
+  static constexpr uint32_t BAR = MAIL + 32;
+  static constexpr uint32_t MISC = BAR + 40 * 8;
   static constexpr uint32_t TOTAL = MISC + 64;
 };
 constexpr uint32_t TC_SMEM = TcSmem::TOTAL + 1024;
@@ -70,10 +79,24 @@ __device__ __forceinline__ void tc_st_16(uint32_t taddr, const uint32_t* v) {
       ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
         "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr) : "memory");
 }
+__device__ __forceinline__ void tc_ld_16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tc_wait_ld16(uint32_t (&v)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                 "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+               :: "memory");
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // Launch shape, the same for every role.
 struct TcPlan {
   uint32_t rt;                   // rows of a query tile: the largest multiple of the group up to 128
+  uint32_t inv_group;            // ceil(65536 / group): x / group = x * inv_group >> 16 for x < 256
   uint32_t qtiles, splits;       // pairs of query tiles per sequence and head; shares of the keys
   uint32_t n_items, page_box;    // page_box: rows of a page's box
   int page_rows, oob_row;        // rows of 64 elements between pages; a row behind the last page
@@ -88,11 +111,11 @@ struct TcItem {
   uint32_t ts, te;               // its key tiles
   bool live;                     // rows of this item exist
 };
-__device__ __forceinline__ uint32_t keys_to(const AttnArgs& a, const TcItem& it, uint32_t token) {
-  // keys below this bound may be seen by the row of a token
-  if (!a.m.causal) return it.g.len;
-  const int32_t hi = max(it.g.slot0 + (int32_t)token + 1, it.pre);
-  return hi <= 0 ? 0u : min((uint32_t)hi, it.g.len);
+// keys below this bound may be seen by the row of a token
+__device__ __forceinline__ uint32_t keys_to(const AttnArgs& a, uint32_t len, int32_t slot0, int32_t pre, uint32_t token) {
+  if (!a.m.causal) return len;
+  const int32_t hi = max(slot0 + (int32_t)token + 1, pre);
+  return hi <= 0 ? 0u : min((uint32_t)hi, len);
 }
 __device__ __forceinline__ TcItem tc_item(const AttnArgs& a, const TcPlan& p, uint32_t i, uint32_t n_seqs) {
   TcItem it;
@@ -108,22 +131,29 @@ __device__ __forceinline__ TcItem tc_item(const AttnArgs& a, const TcPlan& p, ui
   it.live = it.s < n_seqs && it.r0 < it.rows;
   it.ts = it.te = 0;
   if (it.live) {
-    const uint32_t nt = (keys_to(a, it, (min(it.rows, it.r0 + 2 * p.rt) - 1) / a.group) + TC_KEYS - 1) / TC_KEYS;
+    const uint32_t nt = (keys_to(a, it.g.len, it.g.slot0, it.pre, (min(it.rows, it.r0 + 2 * p.rt) - 1) / a.group) + TC_KEYS - 1) / TC_KEYS;
     const uint32_t per = (nt + p.splits - 1) / p.splits;
     it.ts = min(nt, it.sp * per);
     it.te = min(nt, it.ts + per);
   }
   return it;
 }
+// What the other warps have to know about an item.
+struct ItemInfo { uint32_t flags, s, hk, sp, r0, tok0, rows, row0, len; int32_t slot0, pre; };
+static_assert(sizeof(ItemInfo) <= 64, "two fit their place in shared memory");
 // key tiles that query tile w of an item needs
 __device__ __forceinline__ uint32_t tiles_of(const AttnArgs& a, const TcPlan& p, const TcItem& it, uint32_t w) {
   const uint32_t first = it.r0 + w * p.rt;
   if (first >= it.rows) return 0;
-  return (keys_to(a, it, (min(it.rows, first + p.rt) - 1) / a.group) + TC_KEYS - 1) / TC_KEYS;
+  return (keys_to(a, it.g.len, it.g.slot0, it.pre, (min(it.rows, first + p.rt) - 1) / a.group) + TC_KEYS - 1) / TC_KEYS;
 }
 
 }  // namespace
 
+// PAGED: keys and values lie in pages; DOC: documents; MOD: scores are capped or biased.  Compiled for each combination that
+// a call can have: the roles of a block share an instruction cache that the code of all of them does not fit (with one kernel
+// for everything the warps waited for instructions more than for anything else).
+template <bool PAGED, bool DOC, bool MOD>
 __global__ void __launch_bounds__(TC_THREADS, 1)
 k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
           const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a, const __grid_constant__ TcPlan p) {
@@ -142,20 +172,23 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   auto s_full = [&](uint32_t w) { return bar1 + 8 * (4 + w); };
   auto p_full = [&](uint32_t w) { return bar1 + 8 * (6 + w); };
   auto pv_done = [&](uint32_t w) { return bar1 + 8 * (8 + w); };
-  const uint32_t drain = bar1 + 8 * 10;
+  auto s_free = [&](uint32_t w) { return bar1 + 8 * (10 + w); };
+  auto drain = [&](uint32_t w) { return bar1 + 8 * (12 + w); };
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(gbase + TcSmem::MISC);
   volatile uint32_t* abort_flag = misc + 1;
+  volatile ItemInfo* items = reinterpret_cast<volatile ItemInfo*>(gbase + TcSmem::ITEM);
   volatile uint32_t* info = reinterpret_cast<volatile uint32_t*>(gbase + TcSmem::INFO);
+  volatile uint32_t* mail = reinterpret_cast<volatile uint32_t*>(gbase + TcSmem::MAIL);
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < TC_ST; ++s) {
-      mbar_init(k_full(s), 1); mbar_init(v_full(s), 1); mbar_init(side_full(s), 2); mbar_init(empty(s), 1 + 8);
+      mbar_init(k_full(s), 1); mbar_init(v_full(s), 1); mbar_init(side_full(s), 1); mbar_init(empty(s), 2 + 8);
     }
     for (uint32_t b = 0; b < 2; ++b) {
-      mbar_init(q_full(b), 1); mbar_init(q_empty(b), 1); mbar_init(s_full(b), 1); mbar_init(p_full(b), 128); mbar_init(pv_done(b), 1);
+      mbar_init(q_full(b), 1); mbar_init(q_empty(b), 2 + 1 + 8); mbar_init(s_full(b), 2); mbar_init(p_full(b), 128);
+      mbar_init(pv_done(b), 1); mbar_init(s_free(b), 128); mbar_init(drain(b), 1);
     }
-    mbar_init(drain, 1);
     misc[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -173,22 +206,46 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   const unsigned long long lim = wait_limit(a.status);
   uint32_t n_seqs = a.n_seqs;
   if (a.n_seqs_dev) n_seqs = min(n_seqs, *a.n_seqs_dev);
-  const bool paged = a.pages != nullptr;
+  constexpr bool paged = PAGED;
 
+  if (warp < 4) {
   if (warp == 0) {
     // ---------------------------------------------------------------- loads
     bool ok = true;
     uint32_t e = 0, qc = 0;
+#pragma unroll 1
     for (uint32_t i = producer_idle(a.status) ? p.n_items : blockIdx.x; i < p.n_items && ok; i += gridDim.x) {
       const TcItem it = tc_item(a, p, i, n_seqs);
+      if (!it.live) continue;
+      const uint32_t b = qc & 1u;
+      ok = warp_wait(q_empty(b), ((qc >> 1) & 1u) ^ 1u, abort_flag, lim, 64);
+      if (!ok) break;
+      if (lane == 0) {
+        volatile ItemInfo& o = items[b];
+        o.flags = it.ts < it.te ? I_TILES : 0u;
+        o.s = it.s; o.hk = it.hk; o.sp = it.sp; o.r0 = it.r0; o.tok0 = it.r0 / a.group; o.rows = it.rows; o.row0 = it.g.row0; o.len = it.g.len;
+        o.slot0 = it.g.slot0; o.pre = it.pre;
+        if (it.ts < it.te) {
+          const uint32_t per = p.rt / a.group, bytes = p.rt * 128;
+          const int tok = (int)o.tok0 + (paged ? (int)it.g.row0 : 0), seq = paged ? 0 : (int)it.s;
+          mbar_expect_tx(q_full(b), 2 * bytes);
+          tma_load_4d(sQ + (b * 2) * TC_TILE, &map_q, 0, (int)(it.hk * a.group), tok, seq, q_full(b));
+          tma_load_4d(sQ + (b * 2 + 1) * TC_TILE, &map_q, 0, (int)(it.hk * a.group), tok + (int)per, seq, q_full(b));
+        } else {
+          mbar_arrive(q_full(b));
+        }
+      }
+      ++qc;
       if (it.ts >= it.te) continue;
       const uint32_t nt0 = tiles_of(a, p, it, 0), nt1 = tiles_of(a, p, it, 1);
       // smallest and largest document of either query tile (padding left out)
       int32_t lo0 = INT32_MAX, hi0 = -1, lo1 = INT32_MAX, hi1 = -1;
-      const int32_t* doc = a.m.doc ? a.m.doc + (size_t)it.s * a.n : nullptr;
-      if (doc) {
+      const int32_t* doc = DOC ? a.m.doc + (size_t)it.s * a.n : nullptr;
+      if constexpr (DOC) {
         const uint32_t t0 = it.r0 / a.group, t1 = (it.r0 + p.rt) / a.group, t2 = (it.r0 + 2 * p.rt) / a.group;
+#pragma unroll 1
         for (uint32_t t = t0 + lane; t < min(t1, a.n); t += 32) { const int32_t d = doc[t]; if (d >= 0) { lo0 = min(lo0, d); hi0 = max(hi0, d); } }
+#pragma unroll 1
         for (uint32_t t = t1 + lane; t < min(t2, a.n); t += 32) { const int32_t d = doc[t]; if (d >= 0) { lo1 = min(lo1, d); hi1 = max(hi1, d); } }
         lo0 = __reduce_min_sync(0xFFFFFFFFu, lo0); hi0 = __reduce_max_sync(0xFFFFFFFFu, hi0);
         lo1 = __reduce_min_sync(0xFFFFFFFFu, lo1); hi1 = __reduce_max_sync(0xFFFFFFFFu, hi1);
@@ -196,7 +253,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       // flags of key tile j (0: nobody needs it)
       auto needs = [&](uint32_t j) -> uint32_t {
         uint32_t f = (j < nt0 ? F_NEED0 : 0u) | (j < nt1 ? F_NEED1 : 0u);
-        if (!doc || !f) return f;
+        if (!DOC || !f) return f;
         int32_t lo = INT32_MAX, hi = -1;
 #pragma unroll
         for (uint32_t u = 0; u < 4; ++u) {
@@ -210,61 +267,57 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         if (lo > hi1 || hi < lo1) f &= ~F_NEED1;
         return f;
       };
-      uint32_t j = it.ts, f = needs(j);
-      while (!f && j + 1 < it.te) f = needs(++j);
-      if (!f) f = nt0 > j ? F_NEED0 : F_NEED1;               // every item has at least one tile, here a hidden one
-      f |= F_FIRST;
-      {
-        const uint32_t b = qc & 1u;
-        ok = warp_wait(q_empty(b), ((qc >> 1) & 1u) ^ 1u, abort_flag, lim, 64);
-        if (!ok) break;
-        if (lane == 0) {
-          const uint32_t per = p.rt / a.group, bytes = p.rt * 128;
-          const int tok = (int)(it.r0 / a.group) + (paged ? (int)it.g.row0 : 0), seq = paged ? 0 : (int)it.s;
-          mbar_expect_tx(q_full(b), 2 * bytes);
-          tma_load_4d(sQ + (b * 2) * TC_TILE, &map_q, 0, (int)(it.hk * a.group), tok, seq, q_full(b));
-          tma_load_4d(sQ + (b * 2 + 1) * TC_TILE, &map_q, 0, (int)(it.hk * a.group), tok + (int)per, seq, q_full(b));
-        }
-        ++qc;
-      }
-      for (;;) {
-        // the next tile that is needed
-        uint32_t jn = j + 1, fn = 0;
-        for (; jn < it.te; ++jn)
-          if ((fn = needs(jn)) != 0) break;
-        if (jn >= it.te) f |= F_LAST;
-        const uint32_t s = e % TC_ST;
-        int row = 0;
-        const uint32_t boxes = paged ? TC_KEYS / p.page_box : 1u;
-        if (paged && lane < boxes) {
-          const uint32_t slot = j * TC_KEYS + lane * p.page_box;
-          const int32_t pg = slot < it.g.len ? page_of(a, it.s, slot) : -1;
-          row = pg < 0 ? p.oob_row
-                       : pg * p.page_rows + (int)((it.hk << a.page_shift) + (slot & ((1u << a.page_shift) - 1u)));
-        }
-        ok = warp_wait(empty(s), ((e / TC_ST) & 1u) ^ 1u, abort_flag, lim, 64);
-        if (!ok) break;
-        if (lane == 0) {
-          info[s * 2] = j;
-          info[s * 2 + 1] = f;
-          mbar_expect_tx(k_full(s), TC_TILE);
-          mbar_expect_tx(v_full(s), TC_TILE);
-        }
-        __syncwarp();
-        if (paged) {
-          if (lane < boxes) {
-            const uint32_t off = s * TC_TILE + lane * p.page_box * 128;
-            tma_load_2d(sK + off, &map_k, 0, row, k_full(s));
-            tma_load_2d(sV + off, &map_v, 0, row, v_full(s));
+      // a tile is sent when the next one is known, so that the last one can say so; every item has at least one tile (where
+      // documents hide all of them, the last one)
+      bool have = false;
+      uint32_t j = 0, f = 0;
+#pragma unroll 1
+      for (uint32_t c = it.ts; c <= it.te; ++c) {
+        uint32_t fc = c < it.te ? needs(c) : 0u;
+        if (!fc && c + 1 == it.te && !have) fc = nt0 > c ? F_NEED0 : F_NEED1;
+        if (!fc && c < it.te) continue;
+        if (have) {
+          if (c == it.te) f |= F_LAST;
+          const uint32_t s = e % TC_ST;
+          int row = 0;
+          const uint32_t boxes = paged ? TC_KEYS / p.page_box : 1u;
+          if (paged && lane < boxes) {
+            const uint32_t slot = j * TC_KEYS + lane * p.page_box;
+            const int32_t pg = slot < it.g.len ? page_of(a, it.s, slot) : -1;
+            row = pg < 0 ? p.oob_row
+                         : pg * p.page_rows + (int)((it.hk << a.page_shift) + (slot & ((1u << a.page_shift) - 1u)));
           }
-        } else if (lane == 0) {
-          tma_load_4d(sK + s * TC_TILE, &map_k, 0, (int)it.hk, (int)(j * TC_KEYS), (int)it.s, k_full(s));
-          tma_load_4d(sV + s * TC_TILE, &map_v, 0, (int)it.hk, (int)(j * TC_KEYS), (int)it.s, v_full(s));
+          ok = warp_wait(empty(s), ((e / TC_ST) & 1u) ^ 1u, abort_flag, lim, 64);
+          if (!ok) break;
+          if (lane == 0) {
+            info[s * 2] = j;
+            info[s * 2 + 1] = f;
+            mbar_expect_tx(k_full(s), TC_TILE);
+            mbar_expect_tx(v_full(s), TC_TILE);
+          }
+          __syncwarp();
+          if (paged) {
+            if (lane < boxes) {
+              const uint32_t off = s * TC_TILE + lane * p.page_box * 128;
+              tma_load_2d(sK + off, &map_k, 0, row, k_full(s));
+              tma_load_2d(sV + off, &map_v, 0, row, v_full(s));
+            }
+          } else if (lane == 0) {
+            tma_load_4d(sK + s * TC_TILE, &map_k, 0, (int)it.hk, (int)(j * TC_KEYS), (int)it.s, k_full(s));
+            tma_load_4d(sV + s * TC_TILE, &map_v, 0, (int)it.hk, (int)(j * TC_KEYS), (int)it.s, v_full(s));
+          }
+          ++e;
         }
-        ++e;
-        if (f & F_LAST) break;
-        j = jn;
-        f = fn;
+        have = true;
+        j = c;
+        f = fc;
+      }
+    }
+    if (ok && !producer_idle(a.status)) {
+      ok = warp_wait(q_empty(qc & 1u), ((qc >> 1) & 1u) ^ 1u, abort_flag, lim, 64);
+      if (ok && lane == 0) {
+        items[qc & 1u].flags = I_STOP;
+        mbar_arrive(q_full(qc & 1u));
       }
     }
     if (!ok && lane == 0) { *abort_flag = 1; atomicExch(a.status, 1u); }
@@ -272,129 +325,137 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     if (lane == 0 && *abort_flag) {
       // a wait ran out: loads in flight must land before the block's shared memory is released
       volatile uint32_t never = 0;
-      for (uint32_t b = 0; b < 2 && b < qc; ++b) mbar_wait(q_full((qc - 1 - b) & 1u), ((qc - 1 - b) >> 1) & 1u, &never, 200000000ull);
+#pragma unroll 1
+      for (uint32_t b = 0; b < 2 && b < qc; ++b) wait_long(q_full((qc - 1 - b) & 1u), ((qc - 1 - b) >> 1) & 1u, &never, 200000000ull, 0);
+#pragma unroll 1
       for (uint32_t b = 0; b < TC_ST && b < e; ++b) {
         const uint32_t x = e - 1 - b;
-        mbar_wait(k_full(x % TC_ST), (x / TC_ST) & 1u, &never, 200000000ull);
-        mbar_wait(v_full(x % TC_ST), (x / TC_ST) & 1u, &never, 200000000ull);
+        wait_long(k_full(x % TC_ST), (x / TC_ST) & 1u, &never, 200000000ull, 0);
+        wait_long(v_full(x % TC_ST), (x / TC_ST) & 1u, &never, 200000000ull, 0);
       }
     }
-  } else if (warp == 1) {
-    // ---------------------------------------------------------------- products
+  } else if (warp < 3) {
+    // ---------------------------------------------------------------- products of query tile w
+    // Order: S of a key tile, then P V of the tile before it, so that S is there when its softmax asks for it.
     if (lane == 0) {
-      auto next_item = [&](uint32_t i) {                     // the first item from i on that has key tiles
-        for (; i < p.n_items; i += gridDim.x) {
-          const TcItem it = tc_item(a, p, i, n_seqs);
-          if (it.ts < it.te) break;
-        }
-        return i;
-      };
-      uint32_t i = next_item(blockIdx.x), e = 0, qc = 0, n_pv[2] = {0, 0};
-      bool ok = true, started[2] = {false, false};
-      auto issue_s = [&](uint32_t entry, uint32_t q, uint32_t w) {
-        const uint64_t dq = smem_desc_sw128(sQ + ((q & 1u) * 2 + w) * TC_TILE), dk = smem_desc_sw128(sK + (entry % TC_ST) * TC_TILE);
+      const uint32_t w = warp - 1, need = F_NEED0 << w;
+      bool ok = true;
+      uint32_t e = 0, n = 0, sent = 0;                       // key tiles of the block; products P V; messages
+#pragma unroll 1
+      for (uint32_t qc = 0; ok; ++qc) {
+        if (!wait_one(q_full(qc & 1u), (qc >> 1) & 1u, abort_flag, lim)) { ok = false; break; }
+        const uint32_t flags = items[qc & 1u].flags;
+        if (flags & I_STOP) break;
+        bool open = false, started = false;                  // a P V is due (of key tile open_e); O has been written
+        uint32_t open_e = 0;
+        // one turn per key tile and one for the item's end
+#pragma unroll 1
+        for (bool last = !(flags & I_TILES), end = false; !end;) {
+          end = last;
+          const uint32_t s = e % TC_ST;
+          uint32_t f = 0;
+          if (!end) {
+            if (!wait_one(k_full(s), (e / TC_ST) & 1u, abort_flag, lim)) { ok = false; break; }
+            f = info[s * 2 + 1];
+            last = (f & F_LAST) != 0;
+          }
+          const bool now = (f & need) != 0;
+          if (now || end) {
+            // a message to the softmax, which has read the one before (and with it the row of S)
+            if (sent && !wait_one(s_free(w), (sent - 1) & 1u, abort_flag, lim)) { ok = false; break; }
+            ++sent;
+            mail[w * 2] = end ? ~0u : e;
+            mail[w * 2 + 1] = end ? 0u : info[s * 2];
+            if (now) {
+              tc_fence_after();
+              const uint64_t dq = smem_desc_sw128(sQ + ((qc & 1u) * 2 + w) * TC_TILE), dk = smem_desc_sw128(sK + s * TC_TILE);
 #pragma unroll
-        for (uint32_t kk = 0; kk < 4; ++kk) tc_mma_bf16(tmem + w * 128, dq + kk * 2, dk + kk * 2, TC_IDESC_S, kk != 0u);
-        tc_commit(s_full(w));
-      };
-      uint32_t f = 0;
-      if (i < p.n_items) {
-        ok = mbar_wait(q_full(0), 0u, abort_flag, lim, 32) && mbar_wait(k_full(0), 0u, abort_flag, lim, 32);
-        if (ok) {
-          tc_fence_after();
-          f = info[1];
-          if (f & F_NEED0) issue_s(0, 0, 0);
-          if (f & F_NEED1) issue_s(0, 0, 1);
-        }
-      }
-      while (ok && i < p.n_items) {
-        const uint32_t s = e % TC_ST;
-        if (f & F_FIRST) started[0] = started[1] = false;
-        if (!mbar_wait(side_full(s), (e / TC_ST) & 1u, abort_flag, lim, 32)) { ok = false; break; }
-        const bool last = (f & F_LAST) != 0;
-        const uint32_t in = last ? next_item(i + gridDim.x) : i;
-        const bool more = in < p.n_items;
-        const uint32_t qn = last ? qc + 1 : qc;
-        uint32_t fn = 0;
-        bool known = false;
-#pragma unroll
-        for (uint32_t w = 0; w < 2; ++w) {
-          if (f & (F_NEED0 << w)) {
-            if (!mbar_wait(p_full(w), n_pv[w] & 1u, abort_flag, lim, 20)) { ok = false; break; }
+              for (uint32_t kk = 0; kk < 4; ++kk) tc_mma_bf16(tmem + w * 128, dq + kk * 2, dk + kk * 2, TC_IDESC_S, kk != 0u);
+              tc_commit(s_full(w));
+            }
+            mbar_arrive_n(s_full(w), now ? 1u : 2u);
+          }
+          if (open) {
+            const uint32_t so = open_e % TC_ST;
+            if (!wait_one(side_full(so), (open_e / TC_ST) & 1u, abort_flag, lim) ||
+                !wait_one(p_full(w), n & 1u, abort_flag, lim)) { ok = false; break; }
             tc_fence_after();
-            const uint64_t dv = smem_desc_sw128(sV + s * TC_TILE);
+            const uint64_t dv = smem_desc_sw128(sV + so * TC_TILE);
 #pragma unroll
             for (uint32_t kk = 0; kk < 8; ++kk)              // 16 keys a step: 2,048 bytes of V, 8 columns of P
-              tc_mma_ts(tmem + 256 + w * 64, tmem + w * 128 + kk * 8, dv + kk * 128, TC_IDESC_PV, (started[w] || kk != 0u) ? 1u : 0u);
+              tc_mma_ts(tmem + TC_O + w * 64, tmem + TC_P + w * 64 + kk * 8, dv + kk * 128, TC_IDESC_PV, (started || kk != 0u) ? 1u : 0u);
             tc_commit(pv_done(w));
-            started[w] = true;
-            ++n_pv[w];
+            tc_commit(empty(so));
+            started = true;
+            ++n;
           }
-          if (more) {
-            if (!known) {
-              if (last && !mbar_wait(q_full(qn & 1u), (qn >> 1) & 1u, abort_flag, lim, 20)) { ok = false; break; }
-              if (!mbar_wait(k_full((e + 1) % TC_ST), ((e + 1) / TC_ST) & 1u, abort_flag, lim, 20)) { ok = false; break; }
-              tc_fence_after();
-              fn = info[((e + 1) % TC_ST) * 2 + 1];
-              known = true;
-            }
-            if (fn & (F_NEED0 << w)) {
-              // S overwrites P: the product that reads P must be complete
-              if (n_pv[w] && !mbar_wait(pv_done(w), (n_pv[w] - 1) & 1u, abort_flag, lim, 20)) { ok = false; break; }
-              tc_fence_after();
-              issue_s(e + 1, qn, w);
-            }
+          open = now;
+          open_e = e;
+          if (!end) {
+            if (!now) mbar_arrive_n(empty(s), 1 + 4);        // this query tile does not need it, and its softmax does not see it
+            ++e;
           }
         }
-        if (!ok) break;
-        tc_commit(empty(s));
-        if (last) tc_commit(q_empty(qc & 1u));
-        qc = qn;
-        i = in;
-        f = fn;
-        ++e;
+        if (ok) mbar_arrive(q_empty(qc & 1u));
       }
       if (!ok) {
         *abort_flag = 1;
         atomicExch(a.status, 1u);
         volatile uint32_t never = 0;
-        tc_commit(drain);                                    // products in flight end before tensor memory is released
-        mbar_wait(drain, 0u, &never, 200000000ull);
+        tc_commit(drain(w));                                 // products in flight end before tensor memory is released
+        wait_long(drain(w), 0u, &never, 200000000ull, 0);
       }
     }
-  } else if (warp < 4) {
+  } else {
     // ---------------------------------------------------------------- what comes with a key tile
-    const uint32_t sw = warp - 2;                            // keys sw * 32 + lane and 64 + sw * 32 + lane
     bool ok = true;
     uint32_t e = 0;
-    for (uint32_t i = blockIdx.x; i < p.n_items && ok; i += gridDim.x) {
-      const TcItem it = tc_item(a, p, i, n_seqs);
-      if (it.ts >= it.te) continue;
-      const int32_t* src = a.m.doc ? a.m.doc + (size_t)it.s * a.n
-                                   : a.positions ? a.positions + ((size_t)it.s * a.kv_heads + it.hk) * a.side_ld : nullptr;
-      for (;;) {
+#pragma unroll 1
+    for (uint32_t qc = 0; ok; ++qc) {
+      ok = warp_wait(q_full(qc & 1u), (qc >> 1) & 1u, abort_flag, lim, 64);
+      if (!ok) break;
+      volatile ItemInfo& it = items[qc & 1u];
+      const uint32_t flags = it.flags, sq = it.s, hk = it.hk, len = it.len;
+      if (flags & I_STOP) break;
+      const int32_t* src = DOC ? a.m.doc + (size_t)sq * a.n
+                           : PAGED && MOD && a.positions ? a.positions + ((size_t)sq * a.kv_heads + hk) * a.side_ld : nullptr;
+#pragma unroll 1
+      for (bool last = !(flags & I_TILES); !last; ++e) {
         const uint32_t s = e % TC_ST, ph = (e / TC_ST) & 1u;
         ok = warp_wait(k_full(s), ph, abort_flag, lim, 64);
         if (!ok) break;
-        const uint32_t j = info[s * 2], f = info[s * 2 + 1];
+        const uint32_t j = info[s * 2];
+        last = (info[s * 2 + 1] & F_LAST) != 0;
         int32_t* kinfo = reinterpret_cast<int32_t*>(gbase + TcSmem::KINFO) + s * 128;
         uint32_t* kmask = reinterpret_cast<uint32_t*>(gbase + TcSmem::KMASK) + s * 4;
         uint32_t* dirty = reinterpret_cast<uint32_t*>(gbase + TcSmem::DIRTY) + s * 4;
+        if ((DOC || (PAGED && MOD)) && src) {
+          int32_t lo = INT32_MAX, hi = INT32_MIN;
 #pragma unroll
-        for (uint32_t u = 0; u < 2; ++u) {
-          const uint32_t c = u * 64 + sw * 32 + lane, key = j * TC_KEYS + c;
-          if (src) kinfo[c] = key < it.g.len ? src[key] : -1;
-          if (paged) {
-            const bool there = key < it.g.len && page_of(a, it.s, key) >= 0;
-            const uint32_t word = __ballot_sync(0xFFFFFFFFu, there);
-            if (lane == 0) kmask[u * 2 + sw] = word;
+          for (uint32_t u = 0; u < 4; ++u) {
+            const uint32_t key = j * TC_KEYS + u * 32 + lane;
+            const int32_t x = key < len ? src[key] : -1;
+            kinfo[u * 32 + lane] = x;
+            lo = min(lo, x);
+            hi = max(hi, x);
+          }
+          lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+          hi = __reduce_max_sync(0xFFFFFFFFu, hi);
+          if (lane == 0) reinterpret_cast<int32_t*>(gbase + TcSmem::ONEDOC)[s] = lo == hi ? lo : -1;
+        }
+        if (paged) {
+#pragma unroll
+          for (uint32_t u = 0; u < 4; ++u) {
+            const uint32_t key = j * TC_KEYS + u * 32 + lane;
+            const uint32_t word = __ballot_sync(0xFFFFFFFFu, key < len && page_of(a, sq, key) >= 0);
+            if (lane == 0) kmask[u] = word;
           }
         }
         ok = warp_wait(v_full(s), ph, abort_flag, lim, 64);
         if (!ok) break;
-#pragma unroll
-        for (uint32_t u = 0; u < 2; ++u) {
-          const uint32_t c = u * 64 + sw * 32 + lane;
+#pragma unroll 1
+        for (uint32_t u = 0; u < 4; ++u) {
+          const uint32_t c = u * 32 + lane;
           uint8_t* vrow = gbase + TcSmem::V + s * TC_TILE + c * 128;
           // a half with all exponent bits set overflows into its top bit
           uint32_t acc = 0;
@@ -406,12 +467,14 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           }
           const bool bad = (acc & 0x80008000u) != 0u;
           const uint32_t word = __ballot_sync(0xFFFFFFFFu, bad);
-          if (lane == 0) dirty[u * 2 + sw] = word;
+          if (lane == 0) dirty[u] = word;
           if (bad) {
             unsigned long long* ps = reinterpret_cast<unsigned long long*>(gbase + TcSmem::POISON) + (s * 128 + c) * 3;
             unsigned long long nan = 0, pos = 0, neg = 0;
+#pragma unroll 1
             for (uint32_t q = 0; q < 8; ++q) {
               uint16_t* h = reinterpret_cast<uint16_t*>(vrow + ((q ^ (c & 7u)) << 4));
+#pragma unroll 1
               for (uint32_t x = 0; x < 8; ++x) {
                 const uint16_t v = h[x];
                 if ((v & 0x7F80u) != 0x7F80u) continue;
@@ -426,229 +489,298 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(side_full(s));
-        ++e;
-        if (f & F_LAST) break;
       }
+      if (ok && lane == 0) mbar_arrive(q_empty(qc & 1u));
     }
     if (!ok && lane == 0) { *abort_flag = 1; atomicExch(a.status, 1u); }
+  }
   } else {
     // ---------------------------------------------------------------- softmax and output, one thread per query row
     const uint32_t w = (warp - 4) >> 2, quarter = warp & 3u, r = quarter * 32 + lane;
-    const uint32_t t_s = tmem + w * 128 + ((quarter * 32u) << 16), t_o = tmem + 256 + w * 64 + ((quarter * 32u) << 16);
+    const uint32_t lanes = (quarter * 32u) << 16;
+    const uint32_t t_s = tmem + w * 128 + lanes, t_o = tmem + TC_O + w * 64 + lanes, t_p = tmem + TC_P + w * 64 + lanes;
     unsigned long long* rowp = reinterpret_cast<unsigned long long*>(gbase + TcSmem::ROWP) + (w * 128 + r) * 3;
     const float sc = a.m.scale * LOG2E_F;
-    const bool modified = a.m.cap > 0.f || a.m.slopes || a.m.table;
+    constexpr bool side = PAGED || DOC;                      // warp 3's data are needed before the scores are
+    // the row's place in its item: an item starts at a multiple of the group
+    const uint32_t in_item = w * p.rt + r, my_tok = (in_item * p.inv_group) >> 16, my_head = in_item - my_tok * a.group;
     bool ok = true;
-    uint32_t e = 0, n_s = 0;
-    for (uint32_t i = blockIdx.x; i < p.n_items && ok; i += gridDim.x) {
-      const TcItem it = tc_item(a, p, i, n_seqs);
-      if (!it.live) continue;
-      const uint32_t R = it.r0 + w * p.rt + r, token = R / a.group, h = it.hk * a.group + R % a.group;
-      const bool mine = r < p.rt && R < it.rows;             // the row exists
-      uint32_t hi = mine ? keys_to(a, it, token) : 0u;
-      int32_t qdoc = 0;
-      if (a.m.doc && mine) { qdoc = a.m.doc[(size_t)it.s * a.n + token]; if (qdoc < 0) hi = 0; }
-      const int32_t qpos = a.first && mine ? a.first[it.s] + (int32_t)token : it.g.slot0 + (int32_t)token;
-      const float slope = a.m.slopes && mine ? a.m.slopes[h] * LOG2E_F : 0.f;
-      const float* table = a.m.table ? a.m.table + (size_t)(mine ? h : 0u) * (2 * a.m.reach + 1) + a.m.reach : nullptr;
+    uint32_t n_msg = 0, n_s = 0;                             // messages; tiles
+#pragma unroll 1
+    for (uint32_t qc = 0; ok; ++qc) {
+      ok = warp_wait(q_full(qc & 1u), (qc >> 1) & 1u, abort_flag, lim, 0);
+      if (!ok) break;
+      volatile ItemInfo& it = items[qc & 1u];
+      if (it.flags & I_STOP) break;
+      const uint32_t sq = it.s, hk = it.hk, r0 = it.r0, rows = it.rows, row0 = it.row0, len = it.len, token = it.tok0 + my_tok;
+      const int32_t slot0 = it.slot0;
+      const uint32_t h = hk * a.group + my_head, left_rows = rows - r0;      // rows of the sequence from the item on
+      const bool mine = r < p.rt && in_item < left_rows;     // the row exists
+      const int32_t pre = it.pre;
+      const uint32_t hi = mine ? keys_to(a, len, slot0, pre, token) : 0u;
       // keys that every row of this tile sees
-      const uint32_t first_row = it.r0 + w * p.rt;
-      const uint32_t all_see = first_row < it.rows ? keys_to(a, it, first_row / a.group) : 0u;
+      const uint32_t all_see = w * p.rt < left_rows ? keys_to(a, len, slot0, pre, it.tok0 + ((w * p.rt * p.inv_group) >> 16)) : 0u;
+      const int32_t qdoc = DOC && mine ? a.m.doc[(size_t)sq * a.n + token] : -1;
+      const int32_t qpos = (PAGED && MOD && a.first ? a.first[sq] : slot0) + (int32_t)token;
+      const float slope = MOD && a.m.slopes && mine ? a.m.slopes[h] * LOG2E_F : 0.f;
+      const float* table = MOD && a.m.table ? a.m.table + (size_t)(mine ? h : 0u) * (2 * a.m.reach + 1) + a.m.reach : nullptr;
       float m_ref = -INFINITY, l = 0.f;
       bool any = false, poisoned = false;
-      for (bool last = it.ts >= it.te; !last;) {
-        const uint32_t s = e % TC_ST;
-        ok = warp_wait(side_full(s), (e / TC_ST) & 1u, abort_flag, lim, 32);
+#pragma unroll 1
+      for (;;) {
+        ok = warp_wait(s_full(w), n_msg & 1u, abort_flag, lim, 0);
         if (!ok) break;
-        const uint32_t j = info[s * 2], f = info[s * 2 + 1];
-        last = (f & F_LAST) != 0;
-        ++e;
-        if (f & (F_NEED0 << w)) {
-          const uint4 km = paged ? *reinterpret_cast<const uint4*>(gbase + TcSmem::KMASK + s * 16)
-                                 : make_uint4(~0u, ~0u, ~0u, ~0u);
-          const bool plain = !modified && !a.m.doc && (j + 1) * TC_KEYS <= all_see && (km.x & km.y & km.z & km.w) == ~0u;
-          ok = warp_wait(s_full(w), n_s & 1u, abort_flag, lim, 20);
+        ++n_msg;
+        const uint32_t e = mail[w * 2], j = mail[w * 2 + 1], s = e % TC_ST;
+        if (e == ~0u) {                                      // no more tiles of this item
+          mbar_arrive(s_free(w));
+          break;
+        }
+        if (side) {
+          ok = warp_wait(side_full(s), (e / TC_ST) & 1u, abort_flag, lim, 0);
           if (!ok) break;
-          ++n_s;
-          tc_fence_after();
-          float mt = -INFINITY;
-          if (plain) {
+        }
+        const int32_t* kinfo = reinterpret_cast<const int32_t*>(gbase + TcSmem::KINFO) + s * 128;
+        uint4 km = make_uint4(~0u, ~0u, ~0u, ~0u);
+        if (paged) km = *reinterpret_cast<const uint4*>(gbase + TcSmem::KMASK + s * 16);
+        // which keys of the tile the row sees: all, those below a bound, or (documents that differ) each by itself
+        bool full = (j + 1) * TC_KEYS <= all_see && (km.x & km.y & km.z & km.w) == ~0u, mixed = false;
+        uint32_t hi_here = hi;
+        if constexpr (DOC) {
+          const int32_t one = reinterpret_cast<const int32_t*>(gbase + TcSmem::ONEDOC)[s];
+          mixed = one < 0;
+          if (qdoc < 0 || (!mixed && qdoc != one)) hi_here = 0;
+          full = full && !mixed && __all_sync(0xFFFFFFFFu, !mine || qdoc == one);
+        }
+        tc_fence_after();
+        // distances: the bias is linear over the tile where no seen key lies on the other side of the query, constant where
+        // all keys lie beyond the table's reach
+        const int32_t d0 = (int32_t)(j * TC_KEYS) - qpos;
+        const bool by_key = MOD && PAGED && a.positions && (a.m.slopes || a.m.table);
+        const bool linear = MOD && a.m.slopes && !by_key &&
+                            __all_sync(0xFFFFFFFFu, (a.m.causal && pre == 0) || d0 >= 0 || d0 + (int32_t)TC_KEYS <= 1);
+        // (a causal row's keys beyond the query are masked: their side does not matter)
+        const float rise = d0 >= 0 && !(a.m.causal && pre == 0) ? -slope : slope;
+        bool look_up = MOD && a.m.table != nullptr;
+        float bias = 0.f;
+        if (look_up && !by_key &&
+            __all_sync(0xFFFFFFFFu, d0 >= a.m.reach || d0 + (int32_t)TC_KEYS - 1 <= -a.m.reach)) {
+          const float b = __ldg(table + (d0 >= a.m.reach ? a.m.reach : -a.m.reach));
+          bias = b < -1e38f ? b : b * LOG2E_F;               // the type's lowest value stays finite
+          look_up = false;
+        }
+        float mt = -INFINITY;
+        if (!MOD && full) {
 #pragma unroll 1
-            for (uint32_t c = 0; c < 128; c += 32) {
-              uint32_t v[32];
-              tc_ld_32x32(t_s + c, v);
-              tc_wait_ld32(v);
-              float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          for (uint32_t c = 0; c < 128; c += 32) {
+            uint32_t v[32];
+            tc_ld_32x32(t_s + c, v);
+            tc_wait_ld32(v);
+            float m4[4] = {mt, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-              for (uint32_t x = 0; x < 32; x += 8) {
+            for (uint32_t x = 0; x < 32; x += 8) {
 #pragma unroll
-                for (uint32_t u = 0; u < 4; ++u) m4[u] = max3f(m4[u], __uint_as_float(v[x + 2 * u]), __uint_as_float(v[x + 2 * u + 1]));
-              }
-              mt = fmaxf(max3f(mt, m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+              for (uint32_t u = 0; u < 4; ++u) m4[u] = max3f(m4[u], __uint_as_float(v[x + 2 * u]), __uint_as_float(v[x + 2 * u + 1]));
             }
-            mt *= sc;
-          } else {
-            // modified and masked scores go back to tensor memory in base-2 units
-            const int32_t* kinfo = reinterpret_cast<const int32_t*>(gbase + TcSmem::KINFO) + s * 128;
+            mt = fmaxf(max3f(m4[0], m4[1], m4[2]), m4[3]);
+          }
+        } else {
 #pragma unroll 1
-            for (uint32_t c = 0; c < 128; c += 32) {
-              uint32_t v[32];
-              tc_ld_32x32(t_s + c, v);
-              const uint32_t k0 = j * TC_KEYS + c;
-              const uint32_t left = hi > k0 ? hi - k0 : 0u;
-              uint32_t word = left >= 32 ? ~0u : (1u << left) - 1u;
-              word &= c == 0 ? km.x : c == 32 ? km.y : c == 64 ? km.z : km.w;
-              if (a.m.doc) {
+          for (uint32_t c = 0; c < 128; c += 32) {
+            uint32_t v[32];
+            tc_ld_32x32(t_s + c, v);
+            uint32_t word = ~0u;
+            if (!full) {
+              const uint32_t k0 = j * TC_KEYS + c, left = hi_here > k0 ? hi_here - k0 : 0u;
+              word = left >= 32 ? ~0u : (1u << left) - 1u;
+              if (paged) word &= reinterpret_cast<const uint32_t*>(gbase + TcSmem::KMASK)[s * 4 + (c >> 5)];
+              if (DOC && mixed) {
                 uint32_t same = 0;
 #pragma unroll
-                for (uint32_t x = 0; x < 32; ++x) same |= (kinfo[c + x] == qdoc ? 1u : 0u) << x;
+                for (uint32_t x = 0; x < 32; x += 4) {
+                  const int4 d = *reinterpret_cast<const int4*>(kinfo + c + x);
+                  same |= (d.x == qdoc ? 1u << x : 0u) | (d.y == qdoc ? 2u << x : 0u) | (d.z == qdoc ? 4u << x : 0u) | (d.w == qdoc ? 8u << x : 0u);
+                }
                 word &= same;
               }
-              tc_wait_ld32(v);
+            }
+            tc_wait_ld32(v);
+            if constexpr (MOD) {
               unsigned long long t[16];
-              const unsigned long long sc2 = f2_dup(a.m.cap > 0.f ? a.m.scale / a.m.cap : sc);
+              const unsigned long long in2 = f2_dup(a.m.cap > 0.f ? a.m.scale / a.m.cap : sc);
 #pragma unroll
-              for (uint32_t x = 0; x < 16; ++x) t[x] = f2_mul(f2_pack(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), sc2);
+              for (uint32_t x = 0; x < 16; ++x) t[x] = f2_mul(f2_pack(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), in2);
+              float unit = 1.f;
               if (a.m.cap > 0.f) {
-                float big = 0.f;
+                float big[2] = {0.f, 0.f};
 #pragma unroll
-                for (uint32_t x = 0; x < 16; ++x) big = max3f(big, fabsf(f2_lo(t[x])), fabsf(f2_hi(t[x])));
-                const unsigned long long cap2 = f2_dup(a.m.cap * LOG2E_F);
-                if (__any_sync(0xFFFFFFFFu, !(big <= 0.75f))) {
+                for (uint32_t x = 0; x < 16; ++x) big[x & 1u] = max3f(big[x & 1u], fabsf(f2_lo(t[x])), fabsf(f2_hi(t[x])));
+                unit = a.m.cap * LOG2E_F;
+                const bool large = __any_sync(0xFFFFFFFFu, !(fmaxf(big[0], big[1]) <= 0.75f));
+                if (!large) {
+#pragma unroll
+                  for (uint32_t x = 0; x < 16; ++x) t[x] = tanh_small2(t[x]);
+                } else {
 #pragma unroll
                   for (uint32_t x = 0; x < 16; ++x) {
                     const unsigned long long y = tanh_small2(t[x]);
                     const float u0 = f2_lo(t[x]), u1 = f2_hi(t[x]);
-                    t[x] = f2_mul(f2_pack(fabsf(u0) <= 0.75f ? f2_lo(y) : tanh_large(u0), fabsf(u1) <= 0.75f ? f2_hi(y) : tanh_large(u1)), cap2);
+                    t[x] = f2_pack(fabsf(u0) <= 0.75f ? f2_lo(y) : tanh_large(u0), fabsf(u1) <= 0.75f ? f2_hi(y) : tanh_large(u1));
                   }
-                } else {
-#pragma unroll
-                  for (uint32_t x = 0; x < 16; ++x) t[x] = f2_mul(tanh_small2(t[x]), cap2);
                 }
               }
-              if (a.m.slopes) {
-                const unsigned long long ns2 = f2_dup(-slope);
-                if (a.positions) {
+              const unsigned long long u2 = f2_dup(unit), b2 = f2_dup(bias);
+              if (linear) {
+                const unsigned long long k2 = f2_dup(rise);
+                const float d = (float)(d0 + (int32_t)c);
 #pragma unroll
-                  for (uint32_t x = 0; x < 16; ++x)
-                    t[x] = f2_fma(f2_pack(fabsf((float)(kinfo[c + 2 * x] - qpos)), fabsf((float)(kinfo[c + 2 * x + 1] - qpos))), ns2, t[x]);
-                } else {
-                  const float d0 = (float)((int32_t)k0 - qpos);
+                for (uint32_t x = 0; x < 16; ++x)
+                  t[x] = f2_fma(f2_add(f2_dup(d), f2_pack((float)(2 * x), (float)(2 * x + 1))), k2, f2_fma(t[x], u2, b2));
+              } else {
 #pragma unroll
-                  for (uint32_t x = 0; x < 16; ++x)
-                    t[x] = f2_fma(f2_pack(fabsf(d0 + (float)(2 * x)), fabsf(d0 + (float)(2 * x + 1))), ns2, t[x]);
+                for (uint32_t x = 0; x < 16; ++x) t[x] = f2_fma(t[x], u2, b2);
+                if (a.m.slopes) {
+                  const unsigned long long ns2 = f2_dup(-slope);
+#pragma unroll
+                  for (uint32_t x = 0; x < 16; ++x) {
+                    const int32_t e0 = by_key ? kinfo[c + 2 * x] - qpos : d0 + (int32_t)(c + 2 * x);
+                    const int32_t e1 = by_key ? kinfo[c + 2 * x + 1] - qpos : d0 + (int32_t)(c + 2 * x + 1);
+                    t[x] = f2_fma(f2_pack(fabsf((float)e0), fabsf((float)e1)), ns2, t[x]);
+                  }
                 }
               }
-              if (table) {
+              if (look_up) {
                 const int32_t R_ = a.m.reach;
 #pragma unroll
                 for (uint32_t x = 0; x < 16; ++x) {
-                  float b2[2];
+                  float l2[2];
 #pragma unroll
                   for (uint32_t u = 0; u < 2; ++u) {
-                    const int32_t d = (a.positions ? kinfo[c + 2 * x + u] : (int32_t)(k0 + 2 * x + u)) - qpos;
+                    const int32_t d = by_key ? kinfo[c + 2 * x + u] - qpos : d0 + (int32_t)(c + 2 * x + u);
                     const float b = __ldg(table + min(max(d, -R_), R_));
-                    b2[u] = b < -1e38f ? b : b * LOG2E_F;    // the type's lowest value stays finite
+                    l2[u] = b < -1e38f ? b : b * LOG2E_F;
                   }
-                  t[x] = f2_add(t[x], f2_pack(b2[0], b2[1]));
+                  t[x] = f2_add(t[x], f2_pack(l2[0], l2[1]));
                 }
               }
-              float m2[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-              for (uint32_t x = 0; x < 16; ++x) {
-                const float t0 = (word >> (2 * x)) & 1u ? f2_lo(t[x]) : -INFINITY;
-                const float t1 = (word >> (2 * x + 1)) & 1u ? f2_hi(t[x]) : -INFINITY;
-                m2[x & 1u] = max3f(m2[x & 1u], t0, t1);
-                v[2 * x] = __float_as_uint(t0);
-                v[2 * x + 1] = __float_as_uint(t1);
-              }
-              mt = max3f(mt, m2[0], m2[1]);
-              tc_st_16(t_s + c, v);
-              tc_st_16(t_s + c + 16, v + 16);
+              for (uint32_t x = 0; x < 16; ++x) { v[2 * x] = __float_as_uint(f2_lo(t[x])); v[2 * x + 1] = __float_as_uint(f2_hi(t[x])); }
             }
-            tc_wait_st();
-          }
-          // raise the reference maximum?
-          const bool raise = !any ? true : mt > m_ref + 8.f;
-          if (!any) {
-            m_ref = mt;
-            any = true;
-          } else if (__any_sync(0xFFFFFFFFu, raise)) {
-            const float m_new = raise ? mt : m_ref;
-            const float corr = raise ? ex2f(m_ref - m_new) : 1.f;
-            l *= corr;
-            m_ref = m_new;
-            const unsigned long long c2 = f2_dup(corr);
-#pragma unroll 1
-            for (uint32_t c = 0; c < 64; c += 32) {
-              uint32_t v[32];
-              tc_ld_32x32(t_o + c, v);
-              tc_wait_ld32(v);
+            if (!full) {
 #pragma unroll
-              for (uint32_t x = 0; x < 16; ++x) {
-                const unsigned long long y = f2_mul(f2_pack(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), c2);
-                v[2 * x] = __float_as_uint(f2_lo(y));
-                v[2 * x + 1] = __float_as_uint(f2_hi(y));
-              }
-              tc_st_16(t_o + c, v);
-              tc_st_16(t_o + c + 16, v + 16);
+              for (uint32_t x = 0; x < 32; ++x) v[x] = word & (1u << x) ? v[x] : __float_as_uint(-INFINITY);
             }
-          }
-          const unsigned long long nm2 = f2_dup(m_ref == -INFINITY ? 0.f : -m_ref), sc2 = f2_dup(plain ? sc : 1.f);
-          float l0 = 0.f, l1 = 0.f;
-#pragma unroll 1
-          for (uint32_t c = 0; c < 128; c += 32) {
-            uint32_t v[32], pk[16];
-            tc_ld_32x32(t_s + c, v);
-            tc_wait_ld32(v);
+            float m4[4] = {mt, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (uint32_t x = 0; x < 16; ++x) {
-              const unsigned long long t2 = f2_fma(f2_pack(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), sc2, nm2);
-              const float pa = ex2f(f2_lo(t2)), pb = ex2f(f2_hi(t2));
-              l0 += pa;
-              l1 += pb;
-              pk[x] = pack2(pa, pb);
+            for (uint32_t x = 0; x < 32; x += 8) {
+#pragma unroll
+              for (uint32_t u = 0; u < 4; ++u) m4[u] = max3f(m4[u], __uint_as_float(v[x + 2 * u]), __uint_as_float(v[x + 2 * u + 1]));
             }
-            tc_st_16(t_s + c / 2, pk);
+            mt = fmaxf(max3f(m4[0], m4[1], m4[2]), m4[3]);
+            tc_st_16(t_s + c, v);                              // for the second pass
+            tc_st_16(t_s + c + 16, v + 16);
           }
-          l += l0 + l1;
           tc_wait_st();
-          const uint4 dw = *reinterpret_cast<const uint4*>(gbase + TcSmem::DIRTY + s * 16);
-          if (dw.x | dw.y | dw.z | dw.w) {
-            // values that are not numbers: note the columns in which this row sees them
-            const uint32_t words[4] = {dw.x & km.x, dw.y & km.y, dw.z & km.z, dw.w & km.w};
-            const int32_t* kinfo = reinterpret_cast<const int32_t*>(gbase + TcSmem::KINFO) + s * 128;
-            for (uint32_t q = 0; q < 4; ++q)
-              for (uint32_t bits = words[q]; bits; bits &= bits - 1) {
-                const uint32_t c = q * 32 + __ffs(bits) - 1;
-                if (j * TC_KEYS + c >= hi || (a.m.doc && kinfo[c] != qdoc)) continue;
-                const unsigned long long* ps = reinterpret_cast<const unsigned long long*>(gbase + TcSmem::POISON) + (s * 128 + c) * 3;
-                for (uint32_t x = 0; x < 3; ++x) rowp[x] = (poisoned ? rowp[x] : 0ull) | ps[x];
-                poisoned = true;
-              }
+        }
+        const float unit = MOD ? 1.f : sc;              // base-2 units of what tensor memory holds now
+        mt *= unit;
+        // P may be written, and O changed, when the product of the tile before has read the one and written the other
+        if (any) {
+          ok = warp_wait(pv_done(w), (n_s - 1) & 1u, abort_flag, lim, 0);
+          if (!ok) break;
+          tc_fence_after();
+        }
+        ++n_s;
+        // raise the reference maximum?
+        const bool raise = mt > m_ref + 8.f;
+        if (!any) {
+          m_ref = mt;
+          any = true;
+        } else if (__any_sync(0xFFFFFFFFu, raise)) {
+          const float m_new = raise ? mt : m_ref;
+          const float corr = raise ? ex2f(m_ref - m_new) : 1.f;
+          l *= corr;
+          m_ref = m_new;
+          const unsigned long long c2 = f2_dup(corr);
+#pragma unroll 1
+          for (uint32_t c = 0; c < 64; c += 16) {
+            uint32_t o[16];
+            tc_ld_16(t_o + c, o);
+            tc_wait_ld16(o);
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x) {
+              const unsigned long long y = f2_mul(f2_pack(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1])), c2);
+              o[2 * x] = __float_as_uint(f2_lo(y));
+              o[2 * x + 1] = __float_as_uint(f2_hi(y));
+            }
+            tc_st_16(t_o + c, o);
           }
-          tc_fence_before();
-          mbar_arrive(p_full(w));
+        }
+        const unsigned long long nm2 = f2_dup(m_ref == -INFINITY ? 0.f : -m_ref), sc2 = f2_dup(unit);
+        float l0 = 0.f, l1 = 0.f;
+#pragma unroll 1
+        for (uint32_t c = 0; c < 128; c += 32) {
+          uint32_t v[32], pk[16];
+          tc_ld_32x32(t_s + c, v);
+          tc_wait_ld32(v);
+          if (c == 96) {                                     // the row is read: the next key tile's S may come
+            tc_fence_before();
+            mbar_arrive(s_free(w));
+          }
+#pragma unroll
+          for (uint32_t x = 0; x < 16; ++x) {
+            const unsigned long long t2 = f2_fma(f2_pack(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), sc2, nm2);
+            const float pa = ex2f(f2_lo(t2)), pb = ex2f(f2_hi(t2));
+            l0 += pa;
+            l1 += pb;
+            pk[x] = pack2(pa, pb);
+          }
+          tc_st_16(t_p + c / 2, pk);
+        }
+        l += l0 + l1;
+        tc_wait_st();
+        tc_fence_before();
+        mbar_arrive(p_full(w));
+        if (!side) {
+          ok = warp_wait(side_full(s), (e / TC_ST) & 1u, abort_flag, lim, 0);
+          if (!ok) break;
+        }
+        const uint4 dw = *reinterpret_cast<const uint4*>(gbase + TcSmem::DIRTY + s * 16);
+        if (dw.x | dw.y | dw.z | dw.w) {
+          // values that are not numbers: note the columns in which this row sees them
+            const uint32_t* exist = reinterpret_cast<const uint32_t*>(gbase + TcSmem::KMASK) + s * 4;
+          const uint32_t* listed = reinterpret_cast<const uint32_t*>(gbase + TcSmem::DIRTY) + s * 4;
+#pragma unroll 1
+          for (uint32_t q = 0; q < 4; ++q)
+#pragma unroll 1
+            for (uint32_t bits = listed[q] & (paged ? exist[q] : ~0u); bits; bits &= bits - 1) {
+              const uint32_t c = q * 32 + __ffs(bits) - 1;
+              if (j * TC_KEYS + c >= hi_here || (DOC && kinfo[c] != qdoc)) continue;
+              const unsigned long long* ps = reinterpret_cast<const unsigned long long*>(gbase + TcSmem::POISON) + (s * 128 + c) * 3;
+#pragma unroll 1
+              for (uint32_t x = 0; x < 3; ++x) rowp[x] = (poisoned ? rowp[x] : 0ull) | ps[x];
+              poisoned = true;
+            }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(empty(s));
       }
       if (!ok) break;
       // ---- output
-      uint32_t v[32];
       const bool dead = l == 0.f;                            // nothing seen
       const float inv = dead ? 0.f : 1.f / l;
       if (any) {
-        ok = warp_wait(pv_done(w), (n_s - 1) & 1u, abort_flag, lim, 20);
+        ok = warp_wait(pv_done(w), (n_s - 1) & 1u, abort_flag, lim, 0);
         if (!ok) break;
         tc_fence_after();
       }
-      const size_t row = paged ? (size_t)it.g.row0 + token : (size_t)token;
-      const size_t rowid = ((paged ? row : (size_t)it.s * a.n + token) * a.heads + h);
+      const uint32_t sp = it.sp;
       const size_t n_rowids = (size_t)a.n_rows * a.heads;    // of a paged call
-      __nv_bfloat16* out = a.out.ptr + (paged ? 0ll : (long long)it.s * a.out.seq) + (long long)row * a.out.tok + (long long)h * a.out.head;
+      // rows of 128 bytes go through shared memory (the item's queries are no longer needed), so that eight lanes store a row
+      uint8_t* stage = gbase + TcSmem::Q + ((qc & 1u) * 2 + w) * TC_TILE + quarter * 32 * 128;
 #pragma unroll 1
       for (uint32_t c = 0; c < 64; c += 32) {
+        uint32_t v[32];
         if (any) {
           tc_ld_32x32(t_o + c, v);
           tc_wait_ld32(v);
@@ -656,35 +788,61 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         float o[32];
 #pragma unroll
         for (uint32_t x = 0; x < 32; ++x) o[x] = dead ? 0.f : __uint_as_float(v[x]);
-        if (poisoned && !dead) {
+        if (p.splits > 1) {
+          if (mine) {
+            const size_t rowid = ((size_t)row0 + token) * a.heads + h;
+            float4* dst = reinterpret_cast<float4*>(p.part_o + ((size_t)sp * n_rowids + rowid) * 64 + c);
 #pragma unroll
-          for (uint32_t x = 0; x < 32; ++x) {
-            const bool nan = (rowp[0] >> (c + x)) & 1ull, pos = (rowp[1] >> (c + x)) & 1ull, neg = (rowp[2] >> (c + x)) & 1ull;
-            if (nan || (pos && neg)) o[x] = NAN;
-            else if (pos) o[x] += INFINITY;
-            else if (neg) o[x] -= INFINITY;
+            for (uint32_t x = 0; x < 8; ++x) dst[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
           }
-        }
-        if (!mine) {
-        } else if (p.splits > 1) {
-          float4* dst = reinterpret_cast<float4*>(p.part_o + ((size_t)it.sp * n_rowids + rowid) * 64 + c);
-#pragma unroll
-          for (uint32_t x = 0; x < 8; ++x) dst[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
         } else {
-          uint4* dst = reinterpret_cast<uint4*>(out + c);
 #pragma unroll
           for (uint32_t x = 0; x < 4; ++x)
-            dst[x] = make_uint4(pack2(o[8 * x] * inv, o[8 * x + 1] * inv), pack2(o[8 * x + 2] * inv, o[8 * x + 3] * inv),
-                                pack2(o[8 * x + 4] * inv, o[8 * x + 5] * inv), pack2(o[8 * x + 6] * inv, o[8 * x + 7] * inv));
+            *reinterpret_cast<uint4*>(stage + lane * 128 + (((c / 8 + x) ^ (lane & 7u)) << 4)) =
+                make_uint4(pack2(o[8 * x] * inv, o[8 * x + 1] * inv), pack2(o[8 * x + 2] * inv, o[8 * x + 3] * inv),
+                           pack2(o[8 * x + 4] * inv, o[8 * x + 5] * inv), pack2(o[8 * x + 6] * inv, o[8 * x + 7] * inv));
         }
         __syncwarp();
       }
+      if (poisoned && !dead && mine) {
+        // columns in which the row saw values that are not numbers (a row whose sum is NaN keeps it)
+#pragma unroll 1
+        for (unsigned long long bits = rowp[0] | rowp[1] | rowp[2]; bits; bits &= bits - 1) {
+          const uint32_t c = __ffsll((long long)bits) - 1;
+          const bool nan = ((rowp[0] | (rowp[1] & rowp[2])) >> c) & 1ull || l != l, neg = (rowp[2] >> c) & 1ull;
+          const float x = nan ? NAN : neg ? -INFINITY : INFINITY;
+          if (p.splits > 1) p.part_o[((size_t)sp * n_rowids + ((size_t)row0 + token) * a.heads + h) * 64 + c] = x;
+          else *reinterpret_cast<__nv_bfloat16*>(stage + lane * 128 + (((c >> 3) ^ (lane & 7u)) << 4) + (c & 7u) * 2) = __float2bfloat16_rn(x);
+        }
+      }
+      __syncwarp();
       if (mine) {
-        if (p.splits > 1) {
-          float2* ml = reinterpret_cast<float2*>(p.part_ml) + (size_t)it.sp * n_rowids + rowid;
-          *ml = make_float2(l != l && m_ref == -INFINITY ? 0.f : m_ref, l);
-        } else if (a.lse) {
+        const size_t rowid = (paged ? (size_t)row0 + token : (size_t)sq * a.n + token) * a.heads + h;
+        if (p.splits > 1)
+          reinterpret_cast<float2*>(p.part_ml)[(size_t)sp * n_rowids + rowid] = make_float2(l != l && m_ref == -INFINITY ? 0.f : m_ref, l);
+        else if (a.lse)
           a.lse[rowid] = dead ? -INFINITY : (m_ref + lg2f(l)) * LN2_F;
+      }
+      uint4 orow[8];
+      if (p.splits == 1) {
+#pragma unroll
+        for (uint32_t x = 0; x < 8; ++x) {
+          const uint32_t rr = x * 4 + (lane >> 3);
+          orow[x] = *reinterpret_cast<const uint4*>(stage + rr * 128 + (((lane & 7u) ^ (rr & 7u)) << 4));
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the next queries come by TMA
+      }
+      const uint32_t tok0 = it.tok0;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_empty(qc & 1u));
+      if (p.splits == 1) {
+        __nv_bfloat16* out0 = a.out.ptr + (paged ? (long long)row0 * a.out.tok : (long long)sq * a.out.seq) + (long long)tok0 * a.out.tok +
+                              (long long)hk * a.group * a.out.head + (lane & 7u) * 8;
+#pragma unroll
+        for (uint32_t x = 0; x < 8; ++x) {
+          const uint32_t in_tile = quarter * 32 + x * 4 + (lane >> 3), ii = w * p.rt + in_tile, tk = (ii * p.inv_group) >> 16;
+          if (in_tile < p.rt && ii < left_rows)
+            *reinterpret_cast<uint4*>(out0 + (long long)tk * a.out.tok + (long long)(ii - tk * a.group) * a.out.head) = orow[x];
         }
       }
     }
@@ -729,10 +887,20 @@ __global__ void __launch_bounds__(256) k_attn_join(const AttnArgs a, const float
   }
 }
 
+namespace {
+using TcKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const AttnArgs, const TcPlan);
+TcKernel tc_kernel(bool paged, bool doc, bool mod) {
+  if (paged) return mod ? k_attn_tc<true, false, true> : k_attn_tc<true, false, false>;
+  if (doc) return mod ? k_attn_tc<false, true, true> : k_attn_tc<false, true, false>;
+  return mod ? k_attn_tc<false, false, true> : k_attn_tc<false, false, false>;
+}
+}  // namespace
+
 cudaError_t setup_attn_tc() {
   cudaError_t e = tensor_map_setup();
-  if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(k_attn_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM);
+  for (int i = 0; i < 6 && e == cudaSuccess; ++i)
+    e = cudaFuncSetAttribute(tc_kernel(i / 2 == 2, i / 2 == 1, i & 1), cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM);
+  return e;
 }
 
 // A call over whole sequences, or over a paged cache.  part: scratch for part_units x (row, head, share) results of a
@@ -743,6 +911,7 @@ cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, in
   alignas(64) CUtensorMap map_q, map_k, map_v;
   TcPlan p{};
   p.rt = 128 / a.group * a.group;
+  p.inv_group = (65536 + a.group - 1) / a.group;
   const uint64_t seq_rows = (uint64_t)a.n * a.group;
   p.qtiles = (uint32_t)((seq_rows + 2 * p.rt - 1) / (2 * p.rt));
   p.splits = 1;
@@ -776,7 +945,8 @@ cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, in
       return cudaErrorInvalidValue;
   }
   const uint32_t grid = p.n_items < (uint32_t)sm_count ? p.n_items : (uint32_t)sm_count;
-  cudaError_t e = launch_k(k_attn_tc, dim3(grid), dim3(TC_THREADS), TC_SMEM, st, map_q, map_k, map_v, a, p);
+  const bool mod = a.m.cap > 0.f || a.m.slopes || a.m.table;
+  cudaError_t e = launch_k(tc_kernel(paged, a.m.doc != nullptr, mod), dim3(grid), dim3(TC_THREADS), TC_SMEM, st, map_q, map_k, map_v, a, p);
   if (e != cudaSuccess || p.splits == 1) return e;
   const uint64_t warps = (uint64_t)a.n_rows * a.heads;
   const uint64_t blocks = std::min<uint64_t>((warps + 7) / 8, (uint64_t)sm_count * 8);
