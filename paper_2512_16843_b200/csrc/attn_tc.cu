@@ -34,7 +34,7 @@ namespace llmc {
 namespace {
 
 constexpr int TC_THREADS = 384;
-constexpr uint32_t TC_ST = 4;                                // stages of the ring of key and value tiles
+constexpr uint32_t TC_ST = 3;                                // stages of the ring of key and value tiles
 constexpr uint32_t TC_TILE = 16384;                          // 128 x 64 bf16
 constexpr uint32_t TC_KEYS = 128;
 constexpr uint32_t TC_TMEM = 512;                            // S0 | S1 (128 columns each) | O0 | O1 | P0 | P1 (64 each)
@@ -45,14 +45,16 @@ struct TcSmem {
   static constexpr uint32_t Q = 0;                           // [item parity][query tile]
   static constexpr uint32_t K = Q + 4 * TC_TILE;
   static constexpr uint32_t V = K + TC_ST * TC_TILE;
-  static constexpr uint32_t POISON = V + TC_ST * TC_TILE;    // u64 [stage][key][NaN, +inf, -inf]: columns
+  static constexpr uint32_t OUT = V + TC_ST * TC_TILE;       // [query tile]: rows on their way out
+  static constexpr uint32_t POISON = OUT + 2 * TC_TILE;      // u64 [stage][key][NaN, +inf, -inf]: columns
   static constexpr uint32_t ROWP = POISON + TC_ST * 128 * 24;// u64 [row][3]: the same, seen by a row
   static constexpr uint32_t KINFO = ROWP + 256 * 24;         // i32 [stage][key]: document or position
   static constexpr uint32_t KMASK = KINFO + TC_ST * 512;     // u32 [stage][4]: keys that exist
   static constexpr uint32_t DIRTY = KMASK + TC_ST * 16;      // u32 [stage][4]: keys listed in POISON
-  static constexpr uint32_t ONEDOC = DIRTY + TC_ST * 16;     // i32 [stage]: the document of all keys, -1: they differ
-  static constexpr uint32_t INFO = ONEDOC + TC_ST * 4;       // u32 [stage][2]: key tile, flags
-  static constexpr uint32_t ITEM = INFO + TC_ST * 8;         // ItemInfo [2]
+  static constexpr uint32_t NRUNS = DIRTY + TC_ST * 16;      // u32 [stage]: runs of keys of one document ...
+  static constexpr uint32_t RUNS = NRUNS + 16;               // i32 [stage][128][2]: ... document, first key | end << 16
+  static constexpr uint32_t INFO = RUNS + TC_ST * 1024;       // u32 [stage][2]: key tile, flags
+  static constexpr uint32_t ITEM = INFO + TC_ST * 8 + 8;         // ItemInfo [2]
   static constexpr uint32_t MAIL = ITEM + 128;               // u32 [query tile][2]: number of the key tile in the block's stream (~0: the item's end), key tile
   static constexpr uint32_t BAR = MAIL + 32;
   static constexpr uint32_t MISC = BAR + 40 * 8;
@@ -92,7 +94,22 @@ __device__ __forceinline__ void tc_wait_ld16(uint32_t (&v)[16]) {
                  "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
                :: "memory");
 }
+__device__ __forceinline__ void tc_ld_8(uint32_t taddr, uint32_t (&v)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tc_wait_ld8(uint32_t (&v)[8]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]) :: "memory");
+}
+__device__ __forceinline__ void tc_st_8(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+               ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// bits 0 .. n - 1
+__device__ __forceinline__ uint32_t below(int32_t n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+
 // Launch shape, the same for every role.
 struct TcPlan {
   uint32_t rt;                   // rows of a query tile: the largest multiple of the group up to 128
@@ -430,18 +447,39 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         uint32_t* kmask = reinterpret_cast<uint32_t*>(gbase + TcSmem::KMASK) + s * 4;
         uint32_t* dirty = reinterpret_cast<uint32_t*>(gbase + TcSmem::DIRTY) + s * 4;
         if ((DOC || (PAGED && MOD)) && src) {
-          int32_t lo = INT32_MAX, hi = INT32_MIN;
 #pragma unroll
           for (uint32_t u = 0; u < 4; ++u) {
             const uint32_t key = j * TC_KEYS + u * 32 + lane;
-            const int32_t x = key < len ? src[key] : -1;
-            kinfo[u * 32 + lane] = x;
-            lo = min(lo, x);
-            hi = max(hi, x);
+            kinfo[u * 32 + lane] = key < len ? src[key] : -1;
           }
-          lo = __reduce_min_sync(0xFFFFFFFFu, lo);
-          hi = __reduce_max_sync(0xFFFFFFFFu, hi);
-          if (lane == 0) reinterpret_cast<int32_t*>(gbase + TcSmem::ONEDOC)[s] = lo == hi ? lo : -1;
+          if constexpr (DOC) {
+            // runs of equal documents: a row's keys are whole runs
+            __syncwarp();
+            int2* runs = reinterpret_cast<int2*>(gbase + TcSmem::RUNS) + s * 128;
+            uint32_t start[4];
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u) {
+              const uint32_t c = u * 32 + lane;
+              start[u] = __ballot_sync(0xFFFFFFFFu, c == 0 || kinfo[c] != kinfo[c - 1]);
+            }
+            uint32_t before = 0;
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u) {
+              if (start[u] & (1u << lane)) {
+                // it ends where the next run starts
+                uint32_t end = 128;
+                const uint32_t more = start[u] & ~((2u << lane) - 1u);
+                if (more) end = u * 32 + __ffs(more) - 1;
+                else {
+                  for (uint32_t x = u + 1; x < 4; ++x)
+                    if (start[x]) { end = x * 32 + __ffs(start[x]) - 1; break; }
+                }
+                runs[before + __popc(start[u] & ((1u << lane) - 1u))] = make_int2(kinfo[u * 32 + lane], (int)((u * 32 + lane) | (end << 16)));
+              }
+              before += __popc(start[u]);
+            }
+            if (lane == 0) reinterpret_cast<uint32_t*>(gbase + TcSmem::NRUNS)[s] = before;
+          }
         }
         if (paged) {
 #pragma unroll
@@ -543,14 +581,31 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         const int32_t* kinfo = reinterpret_cast<const int32_t*>(gbase + TcSmem::KINFO) + s * 128;
         uint4 km = make_uint4(~0u, ~0u, ~0u, ~0u);
         if (paged) km = *reinterpret_cast<const uint4*>(gbase + TcSmem::KMASK + s * 16);
-        // which keys of the tile the row sees: all, those below a bound, or (documents that differ) each by itself
-        bool full = (j + 1) * TC_KEYS <= all_see && (km.x & km.y & km.z & km.w) == ~0u, mixed = false;
-        uint32_t hi_here = hi;
+        // which keys of the tile the row sees, one bit each where it is not all of them
+        bool full = (j + 1) * TC_KEYS <= all_see && (km.x & km.y & km.z & km.w) == ~0u;
+        uint4 see = km;
         if constexpr (DOC) {
-          const int32_t one = reinterpret_cast<const int32_t*>(gbase + TcSmem::ONEDOC)[s];
-          mixed = one < 0;
-          if (qdoc < 0 || (!mixed && qdoc != one)) hi_here = 0;
-          full = full && !mixed && __all_sync(0xFFFFFFFFu, !mine || qdoc == one);
+          const int2* runs = reinterpret_cast<const int2*>(gbase + TcSmem::RUNS) + s * 128;
+          const uint32_t n_runs = reinterpret_cast<const uint32_t*>(gbase + TcSmem::NRUNS)[s];
+          full = full && n_runs == 1 && __all_sync(0xFFFFFFFFu, !mine || (qdoc >= 0 && runs[0].x == qdoc));
+          if (!full) {
+            see = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 1
+            for (uint32_t x = 0; x < n_runs; ++x) {
+              const int2 run = runs[x];
+              if (run.x == qdoc && qdoc >= 0) {
+                const uint32_t first = run.y & 0xFFFFu, end = (uint32_t)run.y >> 16;
+                see.x |= below(end) & ~below(first);
+                see.y |= below((int)end - 32) & ~below((int)first - 32);
+                see.z |= below((int)end - 64) & ~below((int)first - 64);
+                see.w |= below((int)end - 96) & ~below((int)first - 96);
+              }
+            }
+          }
+        }
+        if (!full) {
+          const int32_t left = hi > j * TC_KEYS ? (int32_t)min(hi - j * TC_KEYS, TC_KEYS) : 0;
+          see.x &= below(left); see.y &= below(left - 32); see.z &= below(left - 64); see.w &= below(left - 96);
         }
         tc_fence_after();
         // distances: the bias is linear over the tile where no seen key lies on the other side of the query, constant where
@@ -560,7 +615,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         const bool linear = MOD && a.m.slopes && !by_key &&
                             __all_sync(0xFFFFFFFFu, (a.m.causal && pre == 0) || d0 >= 0 || d0 + (int32_t)TC_KEYS <= 1);
         // (a causal row's keys beyond the query are masked: their side does not matter)
-        const float rise = d0 >= 0 && !(a.m.causal && pre == 0) ? -slope : slope;
+        const float rise = d0 >= 0 && !(a.m.causal && pre == 0) ? -slope : slope;    // (0 without slopes)
         bool look_up = MOD && a.m.table != nullptr;
         float bias = 0.f;
         if (look_up && !by_key &&
@@ -587,98 +642,79 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         } else {
 #pragma unroll 1
           for (uint32_t c = 0; c < 128; c += 32) {
+            const uint32_t word = c == 0 ? see.x : c == 32 ? see.y : c == 64 ? see.z : see.w;
             uint32_t v[32];
             tc_ld_32x32(t_s + c, v);
-            uint32_t word = ~0u;
-            if (!full) {
-              const uint32_t k0 = j * TC_KEYS + c, left = hi_here > k0 ? hi_here - k0 : 0u;
-              word = left >= 32 ? ~0u : (1u << left) - 1u;
-              if (paged) word &= reinterpret_cast<const uint32_t*>(gbase + TcSmem::KMASK)[s * 4 + (c >> 5)];
-              if (DOC && mixed) {
-                uint32_t same = 0;
-#pragma unroll
-                for (uint32_t x = 0; x < 32; x += 4) {
-                  const int4 d = *reinterpret_cast<const int4*>(kinfo + c + x);
-                  same |= (d.x == qdoc ? 1u << x : 0u) | (d.y == qdoc ? 2u << x : 0u) | (d.z == qdoc ? 4u << x : 0u) | (d.w == qdoc ? 8u << x : 0u);
-                }
-                word &= same;
-              }
-            }
             tc_wait_ld32(v);
+            bool by_hand = MOD && (by_key || look_up || (a.m.slopes && !linear));
             if constexpr (MOD) {
-              unsigned long long t[16];
               const unsigned long long in2 = f2_dup(a.m.cap > 0.f ? a.m.scale / a.m.cap : sc);
+              unsigned long long t[16];
 #pragma unroll
               for (uint32_t x = 0; x < 16; ++x) t[x] = f2_mul(f2_pack(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), in2);
-              float unit = 1.f;
               if (a.m.cap > 0.f) {
                 float big[2] = {0.f, 0.f};
 #pragma unroll
                 for (uint32_t x = 0; x < 16; ++x) big[x & 1u] = max3f(big[x & 1u], fabsf(f2_lo(t[x])), fabsf(f2_hi(t[x])));
-                unit = a.m.cap * LOG2E_F;
-                const bool large = __any_sync(0xFFFFFFFFu, !(fmaxf(big[0], big[1]) <= 0.75f));
-                if (!large) {
+                by_hand = by_hand || !(fmaxf(big[0], big[1]) <= 0.75f);
 #pragma unroll
-                  for (uint32_t x = 0; x < 16; ++x) t[x] = tanh_small2(t[x]);
-                } else {
-#pragma unroll
-                  for (uint32_t x = 0; x < 16; ++x) {
-                    const unsigned long long y = tanh_small2(t[x]);
-                    const float u0 = f2_lo(t[x]), u1 = f2_hi(t[x]);
-                    t[x] = f2_pack(fabsf(u0) <= 0.75f ? f2_lo(y) : tanh_large(u0), fabsf(u1) <= 0.75f ? f2_hi(y) : tanh_large(u1));
-                  }
-                }
+                for (uint32_t x = 0; x < 16; ++x) t[x] = tanh_small2(t[x]);
               }
-              const unsigned long long u2 = f2_dup(unit), b2 = f2_dup(bias);
-              if (linear) {
-                const unsigned long long k2 = f2_dup(rise);
-                const float d = (float)(d0 + (int32_t)c);
+              const unsigned long long u2 = f2_dup(a.m.cap > 0.f ? a.m.cap * LOG2E_F : 1.f), k2 = f2_dup(rise);
+              // bias + rise * distance, two keys at a time
+              unsigned long long d2 = f2_pack((float)(d0 + (int32_t)c), (float)(d0 + (int32_t)c + 1));
+              const unsigned long long b2 = f2_dup(bias), two = f2_dup(2.f);
 #pragma unroll
-                for (uint32_t x = 0; x < 16; ++x)
-                  t[x] = f2_fma(f2_add(f2_dup(d), f2_pack((float)(2 * x), (float)(2 * x + 1))), k2, f2_fma(t[x], u2, b2));
-              } else {
-#pragma unroll
-                for (uint32_t x = 0; x < 16; ++x) t[x] = f2_fma(t[x], u2, b2);
-                if (a.m.slopes) {
-                  const unsigned long long ns2 = f2_dup(-slope);
-#pragma unroll
-                  for (uint32_t x = 0; x < 16; ++x) {
-                    const int32_t e0 = by_key ? kinfo[c + 2 * x] - qpos : d0 + (int32_t)(c + 2 * x);
-                    const int32_t e1 = by_key ? kinfo[c + 2 * x + 1] - qpos : d0 + (int32_t)(c + 2 * x + 1);
-                    t[x] = f2_fma(f2_pack(fabsf((float)e0), fabsf((float)e1)), ns2, t[x]);
-                  }
-                }
+              for (uint32_t x = 0; x < 16; ++x) {
+                t[x] = f2_fma(t[x], u2, f2_fma(d2, k2, b2));
+                d2 = f2_add(d2, two);
+                v[2 * x] = __float_as_uint(f2_lo(t[x]));
+                v[2 * x + 1] = __float_as_uint(f2_hi(t[x]));
               }
-              if (look_up) {
-                const int32_t R_ = a.m.reach;
-#pragma unroll
-                for (uint32_t x = 0; x < 16; ++x) {
-                  float l2[2];
-#pragma unroll
-                  for (uint32_t u = 0; u < 2; ++u) {
-                    const int32_t d = by_key ? kinfo[c + 2 * x + u] - qpos : d0 + (int32_t)(c + 2 * x + u);
-                    const float b = __ldg(table + min(max(d, -R_), R_));
-                    l2[u] = b < -1e38f ? b : b * LOG2E_F;
-                  }
-                  t[x] = f2_add(t[x], f2_pack(l2[0], l2[1]));
-                }
-              }
-#pragma unroll
-              for (uint32_t x = 0; x < 16; ++x) { v[2 * x] = __float_as_uint(f2_lo(t[x])); v[2 * x + 1] = __float_as_uint(f2_hi(t[x])); }
             }
             if (!full) {
 #pragma unroll
               for (uint32_t x = 0; x < 32; ++x) v[x] = word & (1u << x) ? v[x] : __float_as_uint(-INFINITY);
             }
-            float m4[4] = {mt, -INFINITY, -INFINITY, -INFINITY};
+            if (MOD && __any_sync(0xFFFFFFFFu, by_hand)) {
+              // scores beyond the polynomial, distances on both sides, positions, table entries: eight keys at a time
+#pragma unroll 1
+              for (uint32_t g = 0; g < 32; g += 8) {
+                uint32_t u8[8];
+                tc_ld_8(t_s + c + g, u8);
+                tc_wait_ld8(u8);
 #pragma unroll
-            for (uint32_t x = 0; x < 32; x += 8) {
+                for (uint32_t x = 0; x < 8; ++x) {
+                  const uint32_t key = c + g + x;
+                  const int32_t d = by_key ? kinfo[key] - qpos : d0 + (int32_t)key;
+                  float z = __uint_as_float(u8[x]) * a.m.scale;
+                  if (a.m.cap > 0.f) {
+                    const float q = z / a.m.cap;
+                    z = a.m.cap * (fabsf(q) <= 0.75f ? f2_lo(tanh_small2(f2_dup(q))) : tanh_large(q));
+                  }
+                  z *= LOG2E_F;
+                  z = fmaf(-slope, fabsf((float)d), z) + bias;
+                  if (look_up) {
+                    const float b = __ldg(table + min(max(d, -a.m.reach), a.m.reach));
+                    z += b < -1e38f ? b : b * LOG2E_F;
+                  }
+                  z = word & (1u << (g + x)) ? z : -INFINITY;
+                  u8[x] = __float_as_uint(z);
+                  mt = fmaxf(mt, z);
+                }
+                tc_st_8(t_s + c + g, u8);
+              }
+            } else {
+              float m4[4] = {mt, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-              for (uint32_t u = 0; u < 4; ++u) m4[u] = max3f(m4[u], __uint_as_float(v[x + 2 * u]), __uint_as_float(v[x + 2 * u + 1]));
+              for (uint32_t x = 0; x < 32; x += 8) {
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u) m4[u] = max3f(m4[u], __uint_as_float(v[x + 2 * u]), __uint_as_float(v[x + 2 * u + 1]));
+              }
+              mt = fmaxf(max3f(m4[0], m4[1], m4[2]), m4[3]);
+              tc_st_16(t_s + c, v);                          // for the second pass
+              tc_st_16(t_s + c + 16, v + 16);
             }
-            mt = fmaxf(max3f(m4[0], m4[1], m4[2]), m4[3]);
-            tc_st_16(t_s + c, v);                              // for the second pass
-            tc_st_16(t_s + c + 16, v + 16);
           }
           tc_wait_st();
         }
@@ -748,19 +784,16 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         const uint4 dw = *reinterpret_cast<const uint4*>(gbase + TcSmem::DIRTY + s * 16);
         if (dw.x | dw.y | dw.z | dw.w) {
           // values that are not numbers: note the columns in which this row sees them
-            const uint32_t* exist = reinterpret_cast<const uint32_t*>(gbase + TcSmem::KMASK) + s * 4;
-          const uint32_t* listed = reinterpret_cast<const uint32_t*>(gbase + TcSmem::DIRTY) + s * 4;
+          const uint32_t listed[4] = {full ? dw.x : dw.x & see.x, full ? dw.y : dw.y & see.y, full ? dw.z : dw.z & see.z, full ? dw.w : dw.w & see.w};
 #pragma unroll 1
-          for (uint32_t q = 0; q < 4; ++q)
+          for (uint32_t c = 0; c < 128; ++c) {
+            const uint32_t word = c < 32 ? listed[0] : c < 64 ? listed[1] : c < 96 ? listed[2] : listed[3];
+            if (!((word >> (c & 31u)) & 1u)) continue;
+            const unsigned long long* ps = reinterpret_cast<const unsigned long long*>(gbase + TcSmem::POISON) + (s * 128 + c) * 3;
 #pragma unroll 1
-            for (uint32_t bits = listed[q] & (paged ? exist[q] : ~0u); bits; bits &= bits - 1) {
-              const uint32_t c = q * 32 + __ffs(bits) - 1;
-              if (j * TC_KEYS + c >= hi_here || (DOC && kinfo[c] != qdoc)) continue;
-              const unsigned long long* ps = reinterpret_cast<const unsigned long long*>(gbase + TcSmem::POISON) + (s * 128 + c) * 3;
-#pragma unroll 1
-              for (uint32_t x = 0; x < 3; ++x) rowp[x] = (poisoned ? rowp[x] : 0ull) | ps[x];
-              poisoned = true;
-            }
+            for (uint32_t x = 0; x < 3; ++x) rowp[x] = (poisoned ? rowp[x] : 0ull) | ps[x];
+            poisoned = true;
+          }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(empty(s));
@@ -776,31 +809,33 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       }
       const uint32_t sp = it.sp;
       const size_t n_rowids = (size_t)a.n_rows * a.heads;    // of a paged call
-      // rows of 128 bytes go through shared memory (the item's queries are no longer needed), so that eight lanes store a row
-      uint8_t* stage = gbase + TcSmem::Q + ((qc & 1u) * 2 + w) * TC_TILE + quarter * 32 * 128;
+      const size_t rowid = (paged ? (size_t)row0 + token : (size_t)sq * a.n + token) * a.heads + h;
+      const uint32_t tok0 = it.tok0;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_empty(qc & 1u));          // the item's description has been read
+      // rows of 128 bytes go through shared memory, so that eight lanes store one (each warp its own 32 rows)
+      uint8_t* stage = gbase + TcSmem::OUT + w * TC_TILE + quarter * 32 * 128;
+      float* part = p.part_o + ((size_t)sp * n_rowids + rowid) * 64;
 #pragma unroll 1
-      for (uint32_t c = 0; c < 64; c += 32) {
-        uint32_t v[32];
+      for (uint32_t c = 0; c < 64; c += 16) {
+        uint32_t v[16];
         if (any) {
-          tc_ld_32x32(t_o + c, v);
-          tc_wait_ld32(v);
+          tc_ld_16(t_o + c, v);
+          tc_wait_ld16(v);
         }
-        float o[32];
 #pragma unroll
-        for (uint32_t x = 0; x < 32; ++x) o[x] = dead ? 0.f : __uint_as_float(v[x]);
+        for (uint32_t x = 0; x < 16; ++x) v[x] = dead ? 0u : v[x];
         if (p.splits > 1) {
           if (mine) {
-            const size_t rowid = ((size_t)row0 + token) * a.heads + h;
-            float4* dst = reinterpret_cast<float4*>(p.part_o + ((size_t)sp * n_rowids + rowid) * 64 + c);
 #pragma unroll
-            for (uint32_t x = 0; x < 8; ++x) dst[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+            for (uint32_t x = 0; x < 16; x += 4)
+              *reinterpret_cast<uint4*>(part + c + x) = make_uint4(v[x], v[x + 1], v[x + 2], v[x + 3]);
           }
         } else {
 #pragma unroll
-          for (uint32_t x = 0; x < 4; ++x)
-            *reinterpret_cast<uint4*>(stage + lane * 128 + (((c / 8 + x) ^ (lane & 7u)) << 4)) =
-                make_uint4(pack2(o[8 * x] * inv, o[8 * x + 1] * inv), pack2(o[8 * x + 2] * inv, o[8 * x + 3] * inv),
-                           pack2(o[8 * x + 4] * inv, o[8 * x + 5] * inv), pack2(o[8 * x + 6] * inv, o[8 * x + 7] * inv));
+          for (uint32_t x = 0; x < 8; ++x) v[x] = pack2(__uint_as_float(v[2 * x]) * inv, __uint_as_float(v[2 * x + 1]) * inv);
+          *reinterpret_cast<uint4*>(stage + lane * 128 + (((c >> 3) ^ (lane & 7u)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<uint4*>(stage + lane * 128 + (((c >> 3) + 1 ^ (lane & 7u)) << 4)) = make_uint4(v[4], v[5], v[6], v[7]);
         }
         __syncwarp();
       }
@@ -811,40 +846,29 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           const uint32_t c = __ffsll((long long)bits) - 1;
           const bool nan = ((rowp[0] | (rowp[1] & rowp[2])) >> c) & 1ull || l != l, neg = (rowp[2] >> c) & 1ull;
           const float x = nan ? NAN : neg ? -INFINITY : INFINITY;
-          if (p.splits > 1) p.part_o[((size_t)sp * n_rowids + ((size_t)row0 + token) * a.heads + h) * 64 + c] = x;
+          if (p.splits > 1) part[c] = x;
           else *reinterpret_cast<__nv_bfloat16*>(stage + lane * 128 + (((c >> 3) ^ (lane & 7u)) << 4) + (c & 7u) * 2) = __float2bfloat16_rn(x);
         }
       }
       __syncwarp();
       if (mine) {
-        const size_t rowid = (paged ? (size_t)row0 + token : (size_t)sq * a.n + token) * a.heads + h;
         if (p.splits > 1)
           reinterpret_cast<float2*>(p.part_ml)[(size_t)sp * n_rowids + rowid] = make_float2(l != l && m_ref == -INFINITY ? 0.f : m_ref, l);
         else if (a.lse)
           a.lse[rowid] = dead ? -INFINITY : (m_ref + lg2f(l)) * LN2_F;
       }
-      uint4 orow[8];
-      if (p.splits == 1) {
-#pragma unroll
-        for (uint32_t x = 0; x < 8; ++x) {
-          const uint32_t rr = x * 4 + (lane >> 3);
-          orow[x] = *reinterpret_cast<const uint4*>(stage + rr * 128 + (((lane & 7u) ^ (rr & 7u)) << 4));
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the next queries come by TMA
-      }
-      const uint32_t tok0 = it.tok0;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(q_empty(qc & 1u));
       if (p.splits == 1) {
         __nv_bfloat16* out0 = a.out.ptr + (paged ? (long long)row0 * a.out.tok : (long long)sq * a.out.seq) + (long long)tok0 * a.out.tok +
                               (long long)hk * a.group * a.out.head + (lane & 7u) * 8;
-#pragma unroll
-        for (uint32_t x = 0; x < 8; ++x) {
-          const uint32_t in_tile = quarter * 32 + x * 4 + (lane >> 3), ii = w * p.rt + in_tile, tk = (ii * p.inv_group) >> 16;
+#pragma unroll 1
+        for (uint32_t rr = lane >> 3; rr < 32; rr += 4) {
+          const uint32_t in_tile = quarter * 32 + rr, ii = w * p.rt + in_tile, tk = (ii * p.inv_group) >> 16;
           if (in_tile < p.rt && ii < left_rows)
-            *reinterpret_cast<uint4*>(out0 + (long long)tk * a.out.tok + (long long)(ii - tk * a.group) * a.out.head) = orow[x];
+            *reinterpret_cast<uint4*>(out0 + (long long)tk * a.out.tok + (long long)(ii - tk * a.group) * a.out.head) =
+                *reinterpret_cast<const uint4*>(stage + rr * 128 + (((lane & 7u) ^ (rr & 7u)) << 4));
         }
       }
+      __syncwarp();                                          // (the next item's rows come to the same place)
     }
     if (!ok) { *abort_flag = 1; atomicExch(a.status, 1u); }
   }
