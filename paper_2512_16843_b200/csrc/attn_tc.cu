@@ -94,18 +94,6 @@ __device__ __forceinline__ void tc_wait_ld16(uint32_t (&v)[16]) {
                  "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
                :: "memory");
 }
-__device__ __forceinline__ void tc_ld_8(uint32_t taddr, uint32_t (&v)[8]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tc_wait_ld8(uint32_t (&v)[8]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]) :: "memory");
-}
-__device__ __forceinline__ void tc_st_8(uint32_t taddr, const uint32_t (&v)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
-               ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(taddr) : "memory");
-}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // bits 0 .. n - 1
 __device__ __forceinline__ uint32_t below(int32_t n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
@@ -677,32 +665,42 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
               for (uint32_t x = 0; x < 32; ++x) v[x] = word & (1u << x) ? v[x] : __float_as_uint(-INFINITY);
             }
             if (MOD && __any_sync(0xFFFFFFFFu, by_hand)) {
-              // scores beyond the polynomial, distances on both sides, positions, table entries: eight keys at a time
+              // scores beyond the polynomial, distances on both sides, positions, table entries: 16 keys at a time
 #pragma unroll 1
-              for (uint32_t g = 0; g < 32; g += 8) {
-                uint32_t u8[8];
-                tc_ld_8(t_s + c + g, u8);
-                tc_wait_ld8(u8);
+              for (uint32_t g = 0; g < 32; g += 16) {
+                uint32_t u16[16];
+                tc_ld_16(t_s + c + g, u16);
+                int32_t d[16];
+                float b[16];
 #pragma unroll
-                for (uint32_t x = 0; x < 8; ++x) {
-                  const uint32_t key = c + g + x;
-                  const int32_t d = by_key ? kinfo[key] - qpos : d0 + (int32_t)key;
-                  float z = __uint_as_float(u8[x]) * a.m.scale;
-                  if (a.m.cap > 0.f) {
-                    const float q = z / a.m.cap;
-                    z = a.m.cap * (fabsf(q) <= 0.75f ? f2_lo(tanh_small2(f2_dup(q))) : tanh_large(q));
-                  }
-                  z *= LOG2E_F;
-                  z = fmaf(-slope, fabsf((float)d), z) + bias;
-                  if (look_up) {
-                    const float b = __ldg(table + min(max(d, -a.m.reach), a.m.reach));
-                    z += b < -1e38f ? b : b * LOG2E_F;
-                  }
-                  z = word & (1u << (g + x)) ? z : -INFINITY;
-                  u8[x] = __float_as_uint(z);
-                  mt = fmaxf(mt, z);
+                for (uint32_t x = 0; x < 16; ++x) d[x] = d0 + (int32_t)(c + g + x);
+                if (by_key) {
+#pragma unroll
+                  for (uint32_t x = 0; x < 16; ++x) d[x] = kinfo[c + g + x] - qpos;
                 }
-                tc_st_8(t_s + c + g, u8);
+#pragma unroll
+                for (uint32_t x = 0; x < 16; ++x) b[x] = 0.f;
+                if (look_up) {
+#pragma unroll
+                  for (uint32_t x = 0; x < 16; ++x) b[x] = __ldg(table + min(max(d[x], -a.m.reach), a.m.reach));
+                }
+                tc_wait_ld16(u16);
+                float z[16];
+#pragma unroll
+                for (uint32_t x = 0; x < 16; ++x) z[x] = __uint_as_float(u16[x]) * (a.m.cap > 0.f ? a.m.scale / a.m.cap : sc);
+                if (a.m.cap > 0.f) {
+#pragma unroll
+                  for (uint32_t x = 0; x < 16; ++x)
+                    z[x] = (fabsf(z[x]) <= 0.75f ? f2_lo(tanh_small2(f2_dup(z[x]))) : tanh_large(z[x])) * (a.m.cap * LOG2E_F);
+                }
+#pragma unroll
+                for (uint32_t x = 0; x < 16; ++x) {
+                  z[x] = fmaf(-slope, fabsf((float)d[x]), z[x]) + bias + (b[x] < -1e38f ? b[x] : b[x] * LOG2E_F);
+                  z[x] = word & (1u << (g + x)) ? z[x] : -INFINITY;
+                  u16[x] = __float_as_uint(z[x]);
+                  mt = fmaxf(mt, z[x]);
+                }
+                tc_st_16(t_s + c + g, u16);
               }
             } else {
               float m4[4] = {mt, -INFINITY, -INFINITY, -INFINITY};
