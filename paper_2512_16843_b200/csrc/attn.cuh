@@ -80,9 +80,15 @@ constexpr size_t PART_FLOATS = 66;                 // one (row, head, share of t
 constexpr uint32_t ATTN_MAX_GROUP = 128;           // query heads per key/value head: rows of one query tile
 cudaError_t setup_attn_tc();
 cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, int sm_count, cudaStream_t st);
+constexpr uint32_t FEW_ROWS = 16;                  // rows of a sequence and key/value head that k_attn_few takes
+cudaError_t setup_attn_few();
+size_t attn_few_part_floats(int sm_count);
+cudaError_t launch_attn_few(const AttnArgs& a, float* part, uint32_t* arrived, int sm_count, cudaStream_t st);
 cudaError_t setup_attn_kernels();
-// part: scratch of a paged call for part_units x PART_FLOATS floats, or null
-cudaError_t launch_attn(const AttnArgs& a, float* part, size_t part_units, int sm_count, cudaStream_t st);
+// Scratch of a paged call: part for part_units x PART_FLOATS floats, arrived for [n_seqs, kv_heads] words that are zero
+// between calls.  Null for whole sequences.
+struct AttnScratch { float* part = nullptr; size_t part_units = 0; uint32_t* arrived = nullptr; };
+cudaError_t launch_attn(const AttnArgs& a, const AttnScratch& s, int sm_count, cudaStream_t st);
 // received weights of a paged call whose lse is complete
 cudaError_t launch_attn_weights(const AttnArgs& a, int sm_count, cudaStream_t st);
 cudaError_t launch_kv_append(const AttnArgs& a, int sm_count, cudaStream_t st);

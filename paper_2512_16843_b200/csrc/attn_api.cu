@@ -142,12 +142,13 @@ int check_kv_desc(const llmcache_kv_desc* d) {
 // (row, head, share of the keys) results of one call.  Keys are split only while rows alone leave SMs idle, so the shares of
 // all rows never exceed 2 x 256 rows per SM.
 constexpr size_t KV_PART_UNITS = 2 * 256 * 160;
-struct KvLayout { size_t status, part, lse, kept, count, total; };
+struct KvLayout { size_t status, arrived, part, lse, kept, count, total; };
 KvLayout kv_layout(const llmcache_kv_desc& d) {
   KvLayout L{};
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
   L.status = take(16);
+  L.arrived = take((size_t)d.max_seqs * d.kv_heads * 4);
   L.part = take(KV_PART_UNITS * PART_FLOATS * 4);
   L.lse = take((size_t)d.max_rows * d.heads * 4);
   L.kept = take((size_t)d.max_seqs * d.kv_heads * d.max_len * 4);
@@ -239,7 +240,7 @@ int llmcache_attention(const llmcache_rows* q, const llmcache_rows* k, const llm
   a.heads = heads; a.kv_heads = kv_heads; a.group = heads / kv_heads;
   a.n_seqs = n_seqs; a.n_seqs_dev = n_seqs_dev; a.n = seq_len;
   a.status = d.status;
-  return launch_attn_checked(a, nullptr, 0, d.sm_count, (cudaStream_t)stream);
+  return launch_attn_checked(a, AttnScratch{}, d.sm_count, (cudaStream_t)stream);
 }
 
 int llmcache_attention_status(void) {
@@ -299,13 +300,15 @@ int llmcache_kv_create(const llmcache_kv_desc* desc, llmcache_kv_t** kv_out) {
     kv->owns_ws = true;
   }
   kv->status = (uint32_t*)(kv->ws + lay.status);
+  kv->arrived = (uint32_t*)(kv->ws + lay.arrived);
   kv->part = (float*)(kv->ws + lay.part);
   kv->lse = (float*)(kv->ws + lay.lse);
   kv->kept = (int32_t*)(kv->ws + lay.kept);
   kv->count = (uint32_t*)(kv->ws + lay.count);
-  cudaError_t e = cudaMemset(kv->status, 0, 16);
+  cudaError_t e = cudaMemset(kv->status, 0, lay.part);     // status and arrival counts
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&kv->sm_count, cudaDevAttrMultiProcessorCount, desc->device);
   if (e == cudaSuccess) e = setup_attn_kernels();
+  if (e == cudaSuccess && attn_few_part_floats(kv->sm_count) > KV_PART_UNITS * PART_FLOATS) e = cudaErrorInvalidConfiguration;
   if (e == cudaSuccess) e = setup_evict_kernels();
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {
@@ -338,7 +341,7 @@ int llmcache_kv_attention(llmcache_kv_t* kv, const llmcache_kv_chunk* c, void* s
     const cudaError_t e = launch_kv_append(a, kv->sm_count, st);
     if (e != cudaSuccess) return done(e);
   }
-  rc = launch_attn_checked(a, kv->part, KV_PART_UNITS, kv->sm_count, st);
+  rc = launch_attn_checked(a, AttnScratch{kv->part, KV_PART_UNITS, kv->arrived}, kv->sm_count, st);
   if (rc == LLMCACHE_OK && a.weights) rc = done(launch_attn_weights(a, kv->sm_count, st));
   return rc;
 }

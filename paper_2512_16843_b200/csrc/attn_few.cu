@@ -1,0 +1,519 @@
+// Attention of few query rows over a paged cache (the next token of every sequence, a handful of drafted ones): up to 16
+// rows of a sequence and key/value head, token * group + head of the group.
+//
+// Such a call reads every cached key and value once (256 bytes per key and head) and computes next to nothing, so it is
+// bound by HBM: what counts is bytes in flight and an even share of the keys for every SM.  The key tiles of all sequences
+// and heads form one list of W tiles of 128 keys; block c of N takes the tiles W c / N .. W (c + 1) / N - 1, whichever
+// sequences they belong to.  A sequence and head that one block has whole is finished there; the others leave their shares
+// (sums, maximum, weighted values) in scratch and the block that comes last joins them, in the order of the blocks, so
+// that the result does not depend on who was last.
+// In a block one warp keeps three tiles of keys and values on their way (TMA, 32 KB each, two blocks per SM: 192 KB in
+// flight per SM) and four warps take 32 keys of a tile each, with mma.sync m16n8k16: the 16 rows of the smallest
+// tcgen05 shape's 64 or 128 would be all that is used, and there the scores would go through tensor memory for nothing.
+// Softmax statistics and sums are f32; the weights feed the second product as bf16.
+#include <algorithm>
+#include "attn_dev.cuh"
+
+namespace llmc {
+
+namespace {
+
+constexpr int FW_THREADS = 160;                              // warps 0-3: products and softmax, warp 4: loads
+constexpr uint32_t FW_ST = 3, FW_TILE = 16384, FW_KEYS = 128;
+struct FwSmem {
+  static constexpr uint32_t K = 0;
+  static constexpr uint32_t V = K + FW_ST * FW_TILE;
+  static constexpr uint32_t O = V + FW_ST * FW_TILE;         // f32 [warp][row][32]: half of the columns, at the end of a sequence
+  static constexpr uint32_t STAT = O + 4 * 16 * 32 * 4;      // f32 [warp][row][2]
+  static constexpr uint32_t KMASK = STAT + 4 * 16 * 2 * 4;   // u32 [stage][4]: keys that exist
+  static constexpr uint32_t BAR = KMASK + FW_ST * 16;
+  static constexpr uint32_t MISC = BAR + 16 * 8;
+  static constexpr uint32_t TOTAL = MISC + 32;
+};
+constexpr uint32_t FW_SMEM = FwSmem::TOTAL + 1024;
+static_assert(2 * (FW_SMEM + 1024) <= 233472, "two blocks per SM");
+
+struct FwPlan {
+  uint32_t page_box;
+  int page_rows, oob_row;
+  float* part;                   // [block][2][16][66]
+  uint32_t* arrived;             // [n_seqs, kv_heads]: blocks that have left a share; zero between calls
+};
+constexpr uint32_t FW_SLOT = 16 * 66;
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// key tiles of a sequence: none without rows, else at least one
+__device__ __forceinline__ uint32_t seq_tiles(const SeqGeo& g) { return g.cnt ? max(1u, (g.len + FW_KEYS - 1) / FW_KEYS) : 0u; }
+
+// Where in the list of tiles a block is.
+struct FwPlace { uint32_t s, hk, nt; unsigned long long first; SeqGeo g; };     // first: number of (s, hk)'s tile 0
+
+// all key tiles of the call (a warp together)
+__device__ __forceinline__ unsigned long long all_tiles(const AttnArgs& a) {
+  const uint32_t lane = threadIdx.x & 31;
+  unsigned long long sum = 0;
+  for (uint32_t s = lane; s < a.n_seqs; s += 32) sum += seq_tiles(seq_geo(a, s));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  return sum * a.kv_heads;
+}
+// the sequence and head of tile t (a warp together)
+__device__ __forceinline__ FwPlace place_of(const AttnArgs& a, unsigned long long t) {
+  const uint32_t lane = threadIdx.x & 31;
+  unsigned long long before = 0;
+  FwPlace p;
+  p.s = 0;
+  for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += 32) {
+    const unsigned long long mine = s0 + lane < a.n_seqs ? (unsigned long long)seq_tiles(seq_geo(a, s0 + lane)) * a.kv_heads : 0ull;
+    unsigned long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned long long y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= (uint32_t)o) incl += y;
+    }
+    const uint32_t hit = __ballot_sync(0xFFFFFFFFu, before + incl > t);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      p.s = s0 + l;
+      before += __shfl_sync(0xFFFFFFFFu, incl - mine, l);
+      break;
+    }
+    before += __shfl_sync(0xFFFFFFFFu, incl, 31);
+  }
+  p.g = seq_geo(a, p.s);
+  p.nt = seq_tiles(p.g);
+  p.hk = p.nt ? (uint32_t)((t - before) / p.nt) : 0u;
+  p.first = before + (unsigned long long)p.hk * p.nt;
+  return p;
+}
+__device__ __forceinline__ void next_place(const AttnArgs& a, FwPlace& p) {
+  p.first += p.nt;
+  if (++p.hk < a.kv_heads) return;
+  p.hk = 0;
+  do {
+    if (++p.s >= a.n_seqs) { p.nt = 0; return; }
+    p.g = seq_geo(a, p.s);
+    p.nt = seq_tiles(p.g);
+  } while (!p.nt);
+}
+
+}  // namespace
+
+template <bool MOD>
+__global__ void __launch_bounds__(FW_THREADS, 2)
+k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+           const __grid_constant__ AttnArgs a, const __grid_constant__ FwPlan p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gbase = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t bar0 = base + FwSmem::BAR;
+  auto full = [&](uint32_t s) { return bar0 + 8 * s; };
+  auto empty = [&](uint32_t s) { return bar0 + 8 * (FW_ST + s); };
+  const uint32_t together = bar0 + 8 * 2 * FW_ST;
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(gbase + FwSmem::MISC);
+  volatile uint32_t* last_flag = abort_flag + 1;
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < FW_ST; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 4); }
+    mbar_init(together, 4);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncthreads();
+  griddep_sync();
+  const unsigned long long lim = wait_limit(a.status);
+  const unsigned long long W = all_tiles(a);
+  const unsigned long long N = min((unsigned long long)gridDim.x, W);      // blocks with work
+  const bool work = blockIdx.x < N;
+  const unsigned long long t0 = work ? W * blockIdx.x / N : 0ull, t1 = work ? W * (blockIdx.x + 1) / N : 0ull;
+
+  if (warp == 4) {
+    // ---------------------------------------------------------------- loads
+    bool ok = true;
+    uint32_t e = 0;
+    if (t0 < t1 && !producer_idle(a.status)) {
+      FwPlace at = place_of(a, t0);
+#pragma unroll 1
+      for (unsigned long long t = t0; t < t1 && ok; ) {
+        const uint32_t j0 = (uint32_t)(t - at.first), j1 = (uint32_t)min((unsigned long long)at.nt, t1 - at.first);
+#pragma unroll 1
+        for (uint32_t j = j0; j < j1; ++j, ++e) {
+          const uint32_t s = e % FW_ST, boxes = FW_KEYS / p.page_box, per_word = max(1u, 32u / p.page_box);
+          int row = p.oob_row;
+          if (lane < boxes) {
+            const uint32_t slot = j * FW_KEYS + lane * p.page_box;
+            const int32_t pg = slot < at.g.len ? page_of(a, at.s, slot) : -1;
+            if (pg >= 0) row = pg * p.page_rows + (int)((at.hk << a.page_shift) + (slot & ((1u << a.page_shift) - 1u)));
+          }
+          const uint32_t exist = __ballot_sync(0xFFFFFFFFu, row != p.oob_row);
+          ok = warp_wait(empty(s), ((e / FW_ST) & 1u) ^ 1u, abort_flag, lim, 32);
+          if (!ok) break;
+          if (lane < 4) {
+            // 32 keys: part of one box, one box, or two boxes of 16
+            uint32_t word = 0;
+            if (p.page_box >= 32) word = (exist >> (lane * 32 / p.page_box)) & 1u ? ~0u : 0u;
+            else for (uint32_t x = 0; x < per_word; ++x) word |= (exist >> (lane * per_word + x)) & 1u ? 0xFFFFu << (16 * x) : 0u;
+            reinterpret_cast<volatile uint32_t*>(gbase + FwSmem::KMASK)[s * 4 + lane] = word;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_expect_tx(full(s), 2 * FW_TILE);
+          __syncwarp();
+          if (lane < boxes) {
+            const uint32_t off = s * FW_TILE + lane * p.page_box * 128;
+            tma_load_2d(base + FwSmem::K + off, &map_k, 0, row, full(s));
+            tma_load_2d(base + FwSmem::V + off, &map_v, 0, row, full(s));
+          }
+        }
+        t = at.first + j1;
+        if (t < t1) next_place(a, at);
+      }
+    }
+    if (!ok && lane == 0) { *abort_flag = 1; atomicExch(a.status, 1u); }
+    __syncwarp();
+    if (lane == 0 && *abort_flag) {                          // loads in flight must land before shared memory is released
+      volatile uint32_t never = 0;
+#pragma unroll 1
+      for (uint32_t b = 0; b < FW_ST && b < e; ++b) mbar_wait(full((e - 1 - b) % FW_ST), ((e - 1 - b) / FW_ST) & 1u, &never, 200000000ull);
+    }
+  } else if (t0 < t1) {
+    // ---------------------------------------------------------------- products and softmax: 32 keys of a tile per warp
+    const uint32_t quad = lane >> 2, pair = (lane & 3u) * 2; // rows quad and quad + 8, columns pair and pair + 1 of every 8
+    const float sc = a.m.scale * LOG2E_F;
+    bool ok = true;
+    uint32_t e = 0, n_meet = 0;
+    auto meet = [&]() -> bool {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(together);
+      const bool met = warp_wait(together, n_meet & 1u, abort_flag, lim, 0);
+      ++n_meet;
+      return met;
+    };
+    FwPlace at = place_of(a, t0);
+#pragma unroll 1
+    for (unsigned long long t = t0; t < t1 && ok; ) {
+      const uint32_t j0 = (uint32_t)(t - at.first), j1 = (uint32_t)min((unsigned long long)at.nt, t1 - at.first);
+      const uint32_t rows = at.g.cnt * a.group;
+      // the two rows of this thread
+      uint32_t qf[4][4];
+      int32_t hi[2], qpos[2];
+      float slope[2] = {0.f, 0.f};
+      const float* table[2] = {nullptr, nullptr};
+#pragma unroll
+      for (uint32_t u = 0; u < 2; ++u) {
+        const uint32_t R = quad + u * 8;
+        const bool mine = R < rows;
+        const uint32_t token = mine ? R / a.group : 0u, h = at.hk * a.group + (mine ? R % a.group : 0u);
+        hi[u] = !mine ? 0 : a.m.causal ? min(at.g.slot0 + (int32_t)token + 1, (int32_t)at.g.len) : (int32_t)at.g.len;
+        qpos[u] = (a.first ? a.first[at.s] : at.g.slot0) + (int32_t)token;
+        if (MOD && a.m.slopes) slope[u] = a.m.slopes[h] * LOG2E_F;
+        if (MOD && a.m.table) table[u] = a.m.table + (size_t)h * (2 * a.m.reach + 1) + a.m.reach;
+        const __nv_bfloat16* q = a.q.ptr + (long long)(at.g.row0 + token) * a.q.tok + (long long)h * a.q.head;
+#pragma unroll
+        for (uint32_t kk = 0; kk < 4; ++kk) {
+          qf[kk][u] = mine ? *reinterpret_cast<const uint32_t*>(q + kk * 16 + pair) : 0u;
+          qf[kk][2 + u] = mine ? *reinterpret_cast<const uint32_t*>(q + kk * 16 + 8 + pair) : 0u;
+        }
+      }
+      float o[8][4];
+#pragma unroll
+      for (uint32_t x = 0; x < 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
+      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll 1
+      for (uint32_t j = j0; j < j1; ++j, ++e) {
+        const uint32_t s = e % FW_ST, k0 = j * FW_KEYS + warp * 32;
+        ok = warp_wait(full(s), (e / FW_ST) & 1u, abort_flag, lim, 32);
+        if (!ok) break;
+        const uint32_t exist = reinterpret_cast<volatile const uint32_t*>(gbase + FwSmem::KMASK)[s * 4 + warp];
+        if (k0 < at.g.len) {
+          // S = Q K^T: four blocks of eight keys
+          float c[4][4];
+#pragma unroll
+          for (uint32_t n = 0; n < 4; ++n) {
+            c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.f;
+            const uint32_t key = warp * 32 + n * 8 + (lane & 7u), row = base + FwSmem::K + s * FW_TILE + key * 128;
+#pragma unroll
+            for (uint32_t half = 0; half < 2; ++half) {
+              uint32_t b[4];
+              ldsm4(row + (((half * 4 + (lane >> 3)) ^ (key & 7u)) << 4), b);
+              mma16816(c[n], qf[half * 2], b[0], b[1]);
+              mma16816(c[n], qf[half * 2 + 1], b[2], b[3]);
+            }
+          }
+          // scores in base-2 units, masked
+          if (MOD) {
+#pragma unroll
+            for (uint32_t n = 0; n < 4; ++n) {
+#pragma unroll
+              for (uint32_t x = 0; x < 4; ++x) c[n][x] *= a.m.cap > 0.f ? a.m.scale / a.m.cap : sc;
+            }
+            if (a.m.cap > 0.f) {
+#pragma unroll
+              for (uint32_t n = 0; n < 4; ++n) {
+#pragma unroll
+                for (uint32_t x = 0; x < 4; ++x)
+                  c[n][x] = (fabsf(c[n][x]) <= 0.75f ? f2_lo(tanh_small2(f2_dup(c[n][x]))) : tanh_large(c[n][x])) * (a.m.cap * LOG2E_F);
+              }
+            }
+            if (a.m.slopes || a.m.table) {
+              const int32_t* positions = a.positions ? a.positions + ((size_t)at.s * a.kv_heads + at.hk) * a.side_ld : nullptr;
+#pragma unroll
+              for (uint32_t n = 0; n < 4; ++n) {
+#pragma unroll
+                for (uint32_t y = 0; y < 2; ++y) {
+                  const uint32_t key = k0 + n * 8 + pair + y;
+                  const int32_t kpos = positions ? positions[min(key, at.g.len - 1)] : (int32_t)key;
+#pragma unroll
+                  for (uint32_t u = 0; u < 2; ++u) {
+                    const int32_t d = kpos - qpos[u];
+                    float z = fmaf(-slope[u], fabsf((float)d), c[n][u * 2 + y]);
+                    if (a.m.table) {
+                      const float b = __ldg(table[u] + min(max(d, -a.m.reach), a.m.reach));
+                      z += b < -1e38f ? b : b * LOG2E_F;     // the type's lowest value stays finite
+                    }
+                    c[n][u * 2 + y] = z;
+                  }
+                }
+              }
+            }
+          } else {
+#pragma unroll
+            for (uint32_t n = 0; n < 4; ++n) {
+#pragma unroll
+              for (uint32_t x = 0; x < 4; ++x) c[n][x] *= sc;
+            }
+          }
+          float mt[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+          for (uint32_t n = 0; n < 4; ++n) {
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) {
+              const uint32_t in = n * 8 + pair + (x & 1u);
+              const bool see = (int32_t)(k0 + in) < hi[x >> 1] && ((exist >> in) & 1u);
+              c[n][x] = see ? c[n][x] : -INFINITY;
+              mt[x >> 1] = fmaxf(mt[x >> 1], c[n][x]);
+            }
+          }
+          float nm[2];
+#pragma unroll
+          for (uint32_t u = 0; u < 2; ++u) {
+            mt[u] = fmaxf(mt[u], __shfl_xor_sync(0xFFFFFFFFu, mt[u], 1));
+            mt[u] = fmaxf(mt[u], __shfl_xor_sync(0xFFFFFFFFu, mt[u], 2));
+            const float m_new = fmaxf(m[u], mt[u]);
+            const float corr = m_new == -INFINITY ? 1.f : ex2f(m[u] - m_new);
+            m[u] = m_new;
+            nm[u] = m_new == -INFINITY ? 0.f : -m_new;
+            l[u] *= corr;
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x) { o[x][u * 2] *= corr; o[x][u * 2 + 1] *= corr; }
+          }
+          // P, its sums, and O += P V for 16 keys at a time
+#pragma unroll
+          for (uint32_t g = 0; g < 2; ++g) {
+            uint32_t pa[4];
+#pragma unroll
+            for (uint32_t y = 0; y < 2; ++y) {
+#pragma unroll
+              for (uint32_t u = 0; u < 2; ++u) {
+                const float p0 = ex2f(c[g * 2 + y][u * 2] + nm[u]), p1 = ex2f(c[g * 2 + y][u * 2 + 1] + nm[u]);
+                l[u] += p0 + p1;
+                pa[y * 2 + u] = pack2(p0, p1);
+              }
+            }
+            const uint32_t key = warp * 32 + g * 16 + (lane & 15u), row = base + FwSmem::V + s * FW_TILE + key * 128;
+            uint32_t vb[4][4], acc = 0;
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) {
+              ldsm4t(row + (((x * 2 + (lane >> 4)) ^ (key & 7u)) << 4), vb[x]);
+#pragma unroll
+              for (uint32_t y = 0; y < 4; ++y) acc |= (vb[x][y] & 0x7FFF7FFFu) + 0x00800080u;
+            }
+            if (__any_sync(0xFFFFFFFFu, (acc & 0x80008000u) != 0u)) {
+              // infinities and NaN among the values: out of the product, and into the rows that see them
+#pragma unroll
+              for (uint32_t x = 0; x < 4; ++x) {
+#pragma unroll
+                for (uint32_t y = 0; y < 4; ++y) {
+                  const uint32_t bad = ((vb[x][y] & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;
+                  if (bad & 0x8000u) vb[x][y] &= 0xFFFF0000u;
+                  if (bad & 0x80000000u) vb[x][y] &= 0x0000FFFFu;
+                }
+              }
+#pragma unroll 1
+              for (uint32_t k = 0; k < 16; ++k) {
+                const uint32_t in = g * 16 + k, kr = warp * 32 + in;
+                const uint8_t* vrow = gbase + FwSmem::V + s * FW_TILE + kr * 128;
+#pragma unroll
+                for (uint32_t x = 0; x < 8; ++x) {
+                  const uint32_t w2 = *reinterpret_cast<const uint32_t*>(vrow + ((x ^ (kr & 7u)) << 4) + pair * 2);
+#pragma unroll
+                  for (uint32_t y = 0; y < 2; ++y) {
+                    const float v = __uint_as_float(y ? w2 & 0xFFFF0000u : w2 << 16);
+#pragma unroll
+                    for (uint32_t u = 0; u < 2; ++u)
+                      if (!(fabsf(v) < INFINITY) && (int32_t)(k0 + in) < hi[u] && ((exist >> in) & 1u)) o[x][u * 2 + y] += v;
+                  }
+                }
+              }
+            }
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) {
+              mma16816(o[x * 2], pa, vb[x][0], vb[x][1]);
+              mma16816(o[x * 2 + 1], pa, vb[x][2], vb[x][3]);
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(s));
+      }
+      if (!ok) break;
+      // ---- the four warps' parts of the keys, joined
+      float* so = reinterpret_cast<float*>(gbase + FwSmem::O);
+      float* stat = reinterpret_cast<float*>(gbase + FwSmem::STAT);
+#pragma unroll
+      for (uint32_t u = 0; u < 2; ++u) {
+        l[u] += __shfl_xor_sync(0xFFFFFFFFu, l[u], 1);
+        l[u] += __shfl_xor_sync(0xFFFFFFFFu, l[u], 2);
+        if ((lane & 3u) == 0) {
+          // (a sum that is not a number has no maximum to refer to)
+          stat[(warp * 16 + quad + u * 8) * 2] = l[u] != l[u] && m[u] == -INFINITY ? 0.f : m[u];
+          stat[(warp * 16 + quad + u * 8) * 2 + 1] = l[u];
+        }
+      }
+      // a row belongs to eight threads (eight columns each); the columns come in two halves
+      const uint32_t R = threadIdx.x >> 3, c0 = (threadIdx.x & 7u) * 8;
+      float mx = -INFINITY, lt = 0.f, x[8];
+#pragma unroll
+      for (uint32_t y = 0; y < 8; ++y) x[y] = 0.f;
+#pragma unroll
+      for (uint32_t half = 0; half < 2; ++half) {
+#pragma unroll
+        for (uint32_t u = 0; u < 2; ++u) {
+#pragma unroll
+          for (uint32_t y = 0; y < 4; ++y)
+            *reinterpret_cast<float2*>(so + (warp * 16 + quad + u * 8) * 32 + y * 8 + pair) = make_float2(o[half * 4 + y][u * 2], o[half * 4 + y][u * 2 + 1]);
+        }
+        ok = meet();
+        if (!ok) break;
+        if (R < rows && (c0 >> 5) == half) {
+#pragma unroll
+          for (uint32_t w = 0; w < 4; ++w) mx = fmaxf(mx, stat[(w * 16 + R) * 2]);
+#pragma unroll
+          for (uint32_t w = 0; w < 4; ++w) {
+            const float lw = stat[(w * 16 + R) * 2 + 1];
+            if (lw == 0.f) continue;                         // nothing seen
+            const float f = ex2f(stat[(w * 16 + R) * 2] - mx);
+            lt = fmaf(lw, f, lt);
+            const float* src = so + (w * 16 + R) * 32 + (c0 & 31u);
+#pragma unroll
+            for (uint32_t y = 0; y < 8; ++y) x[y] = fmaf(src[y], f, x[y]);
+          }
+        }
+        ok = meet();                                         // (shared memory may be written again)
+        if (!ok) break;
+      }
+      if (!ok) break;
+      const bool whole = j0 == 0 && j1 == at.nt;
+      const unsigned long long c_lo = ((at.first + 1) * N - 1) / W, c_hi = ((at.first + at.nt) * N - 1) / W;
+      float* slot = p.part + ((size_t)blockIdx.x * 2 + (blockIdx.x == c_lo ? 1 : 0)) * FW_SLOT;
+      const uint32_t token = R / a.group, h = at.hk * a.group + R % a.group;
+      auto finish = [&](float mx, float lt, const float (&x)[8]) {
+        const bool dead = lt == 0.f;
+        const float inv = dead ? 0.f : 1.f / lt;
+        uint32_t w[4];
+#pragma unroll
+        for (uint32_t y = 0; y < 4; ++y) w[y] = pack2(dead ? 0.f : x[2 * y] * inv, dead ? 0.f : x[2 * y + 1] * inv);
+        const size_t row = (size_t)at.g.row0 + token;
+        *reinterpret_cast<uint4*>(a.out.ptr + (long long)row * a.out.tok + (long long)h * a.out.head + c0) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (a.lse && c0 == 0) a.lse[row * a.heads + h] = dead ? -INFINITY : (mx + lg2f(lt)) * LN2_F;
+      };
+      if (R < rows) {
+        if (whole) {
+          finish(mx, lt, x);
+        } else {
+          float* dst = slot + R * 64 + c0;
+          *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]);
+          *reinterpret_cast<float4*>(dst + 4) = make_float4(x[4], x[5], x[6], x[7]);
+          if (c0 == 0) *reinterpret_cast<float2*>(slot + 1024 + R * 2) = make_float2(mx, lt);
+        }
+      }
+      if (!whole) {
+        __threadfence();
+        ok = meet();
+        if (!ok) break;
+        if (threadIdx.x == 0) {
+          uint32_t* count = p.arrived + (size_t)at.s * a.kv_heads + at.hk;
+          const bool last = atomicAdd(count, 1u) + 1 == (uint32_t)(c_hi - c_lo + 1);
+          if (last) *count = 0;                              // for the next call
+          *last_flag = last ? 1u : 0u;
+          __threadfence();
+        }
+        ok = meet();
+        if (!ok) break;
+      }
+      if (!whole && *last_flag && R < rows) {
+        mx = -INFINITY;
+        lt = 0.f;
+        for (unsigned long long b = c_lo; b <= c_hi; ++b) mx = fmaxf(mx, __ldcg(p.part + (b * 2 + (b == c_lo ? 1 : 0)) * FW_SLOT + 1024 + R * 2));
+#pragma unroll
+        for (uint32_t y = 0; y < 8; ++y) x[y] = 0.f;
+        for (unsigned long long b = c_lo; b <= c_hi; ++b) {
+          const float* src = p.part + (b * 2 + (b == c_lo ? 1 : 0)) * FW_SLOT;
+          const float2 ml = __ldcg(reinterpret_cast<const float2*>(src + 1024 + R * 2));
+          if (ml.y == 0.f) continue;
+          const float f = ex2f(ml.x - mx);
+          lt = fmaf(ml.y, f, lt);
+          const float4 v0 = __ldcg(reinterpret_cast<const float4*>(src + R * 64 + c0)), v1 = __ldcg(reinterpret_cast<const float4*>(src + R * 64 + c0 + 4));
+          x[0] = fmaf(v0.x, f, x[0]); x[1] = fmaf(v0.y, f, x[1]); x[2] = fmaf(v0.z, f, x[2]); x[3] = fmaf(v0.w, f, x[3]);
+          x[4] = fmaf(v1.x, f, x[4]); x[5] = fmaf(v1.y, f, x[5]); x[6] = fmaf(v1.z, f, x[6]); x[7] = fmaf(v1.w, f, x[7]);
+        }
+        finish(mx, lt, x);
+      }
+      t = at.first + j1;                                     // (the flag is next written behind two meetings)
+      if (t < t1) next_place(a, at);
+    }
+    if (!ok) { *abort_flag = 1; atomicExch(a.status, 1u); }
+  }
+  __syncthreads();
+}
+
+cudaError_t setup_attn_few() {
+  cudaError_t e = cudaFuncSetAttribute(k_attn_few<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, FW_SMEM);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attn_few<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, FW_SMEM);
+  return e;
+}
+
+size_t attn_few_part_floats(int sm_count) { return (size_t)sm_count * 2 * 2 * FW_SLOT; }
+
+cudaError_t launch_attn_few(const AttnArgs& a, float* part, uint32_t* arrived, int sm_count, cudaStream_t st) {
+  alignas(64) CUtensorMap map_k, map_v;
+  FwPlan p{};
+  const uint32_t ps = 1u << a.page_shift;
+  p.page_box = std::min(ps, FW_KEYS);
+  p.page_rows = (int)(a.page_stride / 64);
+  const uint64_t rows = (uint64_t)(a.num_pages - 1) * (a.page_stride / 64) + (uint64_t)a.kv_heads * ps;
+  p.oob_row = (int)rows;
+  p.part = part;
+  p.arrived = arrived;
+  if (!make_tensor_map_bf16(&map_k, a.k_pages, rows, 64, p.page_box) || !make_tensor_map_bf16(&map_v, a.v_pages, rows, 64, p.page_box))
+    return cudaErrorInvalidValue;
+  // two blocks per SM, but no more than there can be tiles
+  const uint64_t cap = std::min<uint64_t>(a.max_len, (uint64_t)a.pages_ld << a.page_shift), tiles = (cap + FW_KEYS - 1) / FW_KEYS;
+  const uint64_t grid = std::min<uint64_t>((uint64_t)sm_count * 2, std::max<uint64_t>(1, tiles * a.n_seqs * a.kv_heads));
+  const bool mod = a.m.cap > 0.f || a.m.slopes || a.m.table;
+  return launch_k(mod ? k_attn_few<true> : k_attn_few<false>, dim3((uint32_t)grid), dim3(FW_THREADS), FW_SMEM, st, map_k, map_v, a, p);
+}
+
+}  // namespace llmc

@@ -9,6 +9,7 @@ struct llmcache_kv {
   bool owns_ws = false;
   uint32_t* status = nullptr;    // a bounded wait expired; diagnostic knobs behind it
   float* part = nullptr;         // shares of the keys of one call
+  uint32_t* arrived = nullptr;   // [max_seqs, kv_heads], zero between calls
   float* lse = nullptr;          // [max_rows, heads] where the caller takes none
   int32_t* kept = nullptr;       // eviction: slots kept [max_seqs, kv_heads, <= max_len] ...
   uint32_t* count = nullptr;     // ... and how many per sequence
@@ -25,10 +26,10 @@ int kv_fits_layer(const llmcache_kv* kv, int device, uint32_t heads);
 int kv_check_chunk(const llmcache_kv* kv, const llmcache_kv_chunk* c);
 
 // launch_attn behind the check of its grid
-inline int launch_attn_checked(const AttnArgs& a, float* part, size_t part_units, int sm_count, cudaStream_t st) {
+inline int launch_attn_checked(const AttnArgs& a, const AttnScratch& s, int sm_count, cudaStream_t st) {
   const uint64_t tiles = ((uint64_t)a.n * a.group + 127) / 128 * a.kv_heads * a.n_seqs;
   if (tiles > 0x7FFFFFFFull) return LLMCACHE_ERR_SHAPE;
-  if (launch_attn(a, part, part_units, sm_count, st) == cudaSuccess) return LLMCACHE_OK;
+  if (launch_attn(a, s, sm_count, st) == cudaSuccess) return LLMCACHE_OK;
   cudaGetLastError();
   return LLMCACHE_ERR_CUDA;
 }

@@ -321,13 +321,15 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 }
 
 cudaError_t setup_attn_kernels() {
-  const cudaError_t e = setup_attn_tc();
+  cudaError_t e = setup_attn_tc();
+  if (e == cudaSuccess) e = setup_attn_few();
   if (e != cudaSuccess) return e;
   return cudaFuncSetAttribute(k_attn_weights, cudaFuncAttributeMaxDynamicSharedMemorySize, WT_SMEM);
 }
 
-cudaError_t launch_attn(const AttnArgs& a, float* part, size_t part_units, int sm_count, cudaStream_t st) {
-  return launch_attn_tc(a, part, part_units, sm_count, st);
+cudaError_t launch_attn(const AttnArgs& a, const AttnScratch& s, int sm_count, cudaStream_t st) {
+  if (a.pages && (uint64_t)a.n * a.group <= FEW_ROWS) return launch_attn_few(a, s.part, s.arrived, sm_count, st);
+  return launch_attn_tc(a, s.part, s.part_units, sm_count, st);
 }
 
 cudaError_t launch_attn_weights(const AttnArgs& a, int sm_count, cudaStream_t st) {

@@ -166,7 +166,7 @@ int llmcache_layer_forward(llmcache_layer_t* L, const void* x, uint32_t n_seqs, 
   const VtOut vt_out = L->has_mods ? VtOut{nullptr, 0, 0, 0} : VtOut{L->vt, 2 * d, attention_vt_pitch(n), D.heads};
   auto attend = [&]() -> cudaError_t {
     if (!L->has_mods) return launch_attention_tc(L->qkv, L->vt, L->a, L->status, n, d, D.heads, n_seqs, n_seqs_dev, D.causal, st);
-    return launch_attn(layer_attn_args(L, n_seqs, n_seqs_dev), nullptr, 0, sm, st);
+    return launch_attn(layer_attn_args(L, n_seqs, n_seqs_dev), AttnScratch{}, sm, st);
   };
   auto ln = [&](const __nv_bfloat16* in, const float* g, const float* b, __nv_bfloat16* o) {
     return launch_layernorm(in, g, b, o, T, d, n_seqs_dev, n, D.eps, sm, st);
