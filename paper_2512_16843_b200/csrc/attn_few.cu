@@ -3,8 +3,8 @@
 //
 // Such a call reads every cached key and value once (256 bytes per key and head) and computes next to nothing, so it is
 // bound by HBM: what counts is bytes in flight and an even share of the keys for every SM.  The key tiles of all sequences
-// and heads form one list of W tiles of 128 keys; block c of N takes the tiles W c / N .. W (c + 1) / N - 1, whichever
-// sequences they belong to.  A sequence and head that one block has whole is finished there; the others leave their shares
+// and heads form one list of W tiles of 128 keys, and each of N blocks takes W / N of them in a row (the first W mod N one
+// more), whichever sequences they belong to.  A sequence and head that one block has whole is finished there; the others leave their shares
 // (sums, maximum, weighted values) in scratch and the block that comes last joins them, in the order of the blocks, so
 // that the result does not depend on who was last.
 // In a block one warp keeps three tiles of keys and values on their way (TMA, 32 KB each, two blocks per SM: 192 KB in
@@ -57,32 +57,44 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
 // key tiles of a sequence: none without rows, else at least one
 __device__ __forceinline__ uint32_t seq_tiles(const SeqGeo& g) { return g.cnt ? max(1u, (g.len + FW_KEYS - 1) / FW_KEYS) : 0u; }
 
-// Where in the list of tiles a block is.
-struct FwPlace { uint32_t s, hk, nt; unsigned long long first; SeqGeo g; };     // first: number of (s, hk)'s tile 0
+// The list of tiles: W in all, block c's share begins at begin(c); `longer` blocks have one more than `each`.
+struct FwList {
+  uint32_t W, N, each, longer;
+  __device__ __forceinline__ uint32_t begin(uint32_t c) const { return c * each + min(c, longer); }
+  __device__ __forceinline__ uint32_t block_of(uint32_t t) const {
+    const uint32_t in_longer = longer * (each + 1);
+    return t < in_longer ? t / (each + 1) : longer + (t - in_longer) / each;
+  }
+};
+// A sequence and head in it: first = number of its tile 0 of nt.
+struct FwPlace { uint32_t s, hk, nt, first; SeqGeo g; };
 
-// all key tiles of the call (a warp together)
-__device__ __forceinline__ unsigned long long all_tiles(const AttnArgs& a) {
+__device__ __forceinline__ uint32_t warp_scan(uint32_t x) {  // inclusive sum over the lanes
   const uint32_t lane = threadIdx.x & 31;
-  unsigned long long sum = 0;
-  for (uint32_t s = lane; s < a.n_seqs; s += 32) sum += seq_tiles(seq_geo(a, s));
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-  return sum * a.kv_heads;
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+    if (lane >= (uint32_t)o) x += y;
+  }
+  return x;
 }
-// the sequence and head of tile t (a warp together)
-__device__ __forceinline__ FwPlace place_of(const AttnArgs& a, unsigned long long t) {
+// The list, and the place of its tile number begin(block) (one warp together).
+__device__ __noinline__ void find_place(const AttnArgs& a, uint32_t block, uint32_t blocks, FwList& L, FwPlace& p) {
   const uint32_t lane = threadIdx.x & 31;
-  unsigned long long before = 0;
-  FwPlace p;
-  p.s = 0;
+  uint32_t sum = 0;
+#pragma unroll 1
+  for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += 32) sum += s0 + lane < a.n_seqs ? seq_tiles(seq_geo(a, s0 + lane)) * a.kv_heads : 0u;
+  L.W = __reduce_add_sync(0xFFFFFFFFu, sum);
+  L.N = min(blocks, L.W);                                    // blocks with work
+  L.each = L.N ? L.W / L.N : 0u;
+  L.longer = L.W - L.N * L.each;
+  if (block >= L.N) return;
+  const uint32_t t = L.begin(block);
+  uint32_t before = 0;
+#pragma unroll 1
   for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += 32) {
-    const unsigned long long mine = s0 + lane < a.n_seqs ? (unsigned long long)seq_tiles(seq_geo(a, s0 + lane)) * a.kv_heads : 0ull;
-    unsigned long long incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const unsigned long long y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-      if (lane >= (uint32_t)o) incl += y;
-    }
+    const uint32_t mine = s0 + lane < a.n_seqs ? seq_tiles(seq_geo(a, s0 + lane)) * a.kv_heads : 0u;
+    const uint32_t incl = warp_scan(mine);
     const uint32_t hit = __ballot_sync(0xFFFFFFFFu, before + incl > t);
     if (hit) {
       const int l = __ffs(hit) - 1;
@@ -94,11 +106,10 @@ __device__ __forceinline__ FwPlace place_of(const AttnArgs& a, unsigned long lon
   }
   p.g = seq_geo(a, p.s);
   p.nt = seq_tiles(p.g);
-  p.hk = p.nt ? (uint32_t)((t - before) / p.nt) : 0u;
-  p.first = before + (unsigned long long)p.hk * p.nt;
-  return p;
+  p.hk = (t - before) / p.nt;
+  p.first = before + p.hk * p.nt;
 }
-__device__ __forceinline__ void next_place(const AttnArgs& a, FwPlace& p) {
+__device__ __noinline__ void next_place(const AttnArgs& a, FwPlace& p) {
   p.first += p.nt;
   if (++p.hk < a.kv_heads) return;
   p.hk = 0;
@@ -135,20 +146,20 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
   __syncthreads();
   griddep_sync();
   const unsigned long long lim = wait_limit(a.status);
-  const unsigned long long W = all_tiles(a);
-  const unsigned long long N = min((unsigned long long)gridDim.x, W);      // blocks with work
-  const bool work = blockIdx.x < N;
-  const unsigned long long t0 = work ? W * blockIdx.x / N : 0ull, t1 = work ? W * (blockIdx.x + 1) / N : 0ull;
+  FwList L;
+  FwPlace at;
+  find_place(a, blockIdx.x, gridDim.x, L, at);
+  const bool work = blockIdx.x < L.N;
+  const uint32_t t0 = work ? L.begin(blockIdx.x) : 0u, t1 = work ? L.begin(blockIdx.x + 1) : 0u;
 
   if (warp == 4) {
     // ---------------------------------------------------------------- loads
     bool ok = true;
     uint32_t e = 0;
     if (t0 < t1 && !producer_idle(a.status)) {
-      FwPlace at = place_of(a, t0);
 #pragma unroll 1
-      for (unsigned long long t = t0; t < t1 && ok; ) {
-        const uint32_t j0 = (uint32_t)(t - at.first), j1 = (uint32_t)min((unsigned long long)at.nt, t1 - at.first);
+      for (uint32_t t = t0; t < t1 && ok; ) {
+        const uint32_t j0 = t - at.first, j1 = min(at.nt, t1 - at.first);
 #pragma unroll 1
         for (uint32_t j = j0; j < j1; ++j, ++e) {
           const uint32_t s = e % FW_ST, boxes = FW_KEYS / p.page_box, per_word = max(1u, 32u / p.page_box);
@@ -201,10 +212,9 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
       ++n_meet;
       return met;
     };
-    FwPlace at = place_of(a, t0);
 #pragma unroll 1
-    for (unsigned long long t = t0; t < t1 && ok; ) {
-      const uint32_t j0 = (uint32_t)(t - at.first), j1 = (uint32_t)min((unsigned long long)at.nt, t1 - at.first);
+    for (uint32_t t = t0; t < t1 && ok; ) {
+      const uint32_t j0 = t - at.first, j1 = min(at.nt, t1 - at.first);
       const uint32_t rows = at.g.cnt * a.group;
       // the two rows of this thread
       uint32_t qf[4][4];
@@ -241,16 +251,19 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
           // S = Q K^T: four blocks of eight keys
           float c[4][4];
 #pragma unroll
-          for (uint32_t n = 0; n < 4; ++n) {
-            c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.f;
-            const uint32_t key = warp * 32 + n * 8 + (lane & 7u), row = base + FwSmem::K + s * FW_TILE + key * 128;
+          for (uint32_t n = 0; n < 4; ++n) c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.f;
 #pragma unroll
-            for (uint32_t half = 0; half < 2; ++half) {
-              uint32_t b[4];
-              ldsm4(row + (((half * 4 + (lane >> 3)) ^ (key & 7u)) << 4), b);
-              mma16816(c[n], qf[half * 2], b[0], b[1]);
-              mma16816(c[n], qf[half * 2 + 1], b[2], b[3]);
+          for (uint32_t half = 0; half < 2; ++half) {
+            uint32_t b[4][4];
+#pragma unroll
+            for (uint32_t n = 0; n < 4; ++n) {
+              const uint32_t key = warp * 32 + n * 8 + (lane & 7u);
+              ldsm4(base + FwSmem::K + s * FW_TILE + key * 128 + (((half * 4 + (lane >> 3)) ^ (key & 7u)) << 4), b[n]);
             }
+#pragma unroll
+            for (uint32_t n = 0; n < 4; ++n) mma16816(c[n], qf[half * 2], b[n][0], b[n][1]);
+#pragma unroll
+            for (uint32_t n = 0; n < 4; ++n) mma16816(c[n], qf[half * 2 + 1], b[n][2], b[n][3]);
           }
           // scores in base-2 units, masked
           if (MOD) {
@@ -319,19 +332,26 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 #pragma unroll
             for (uint32_t x = 0; x < 8; ++x) { o[x][u * 2] *= corr; o[x][u * 2 + 1] *= corr; }
           }
-          // P, its sums, and O += P V for 16 keys at a time
+          // P and its sums
+          uint32_t pa[2][4];
 #pragma unroll
           for (uint32_t g = 0; g < 2; ++g) {
-            uint32_t pa[4];
 #pragma unroll
             for (uint32_t y = 0; y < 2; ++y) {
 #pragma unroll
               for (uint32_t u = 0; u < 2; ++u) {
                 const float p0 = ex2f(c[g * 2 + y][u * 2] + nm[u]), p1 = ex2f(c[g * 2 + y][u * 2 + 1] + nm[u]);
                 l[u] += p0 + p1;
-                pa[y * 2 + u] = pack2(p0, p1);
+                pa[g][y * 2 + u] = pack2(p0, p1);
               }
             }
+          }
+          // O += P V, 16 keys at a time (one copy of the code)
+#pragma unroll 1
+          for (uint32_t g = 0; g < 2; ++g) {
+            uint32_t pg[4];
+#pragma unroll
+            for (uint32_t y = 0; y < 4; ++y) pg[y] = g ? pa[1][y] : pa[0][y];
             const uint32_t key = warp * 32 + g * 16 + (lane & 15u), row = base + FwSmem::V + s * FW_TILE + key * 128;
             uint32_t vb[4][4], acc = 0;
 #pragma unroll
@@ -347,31 +367,28 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 #pragma unroll
                 for (uint32_t y = 0; y < 4; ++y) {
                   const uint32_t bad = ((vb[x][y] & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;
-                  if (bad & 0x8000u) vb[x][y] &= 0xFFFF0000u;
-                  if (bad & 0x80000000u) vb[x][y] &= 0x0000FFFFu;
+                  vb[x][y] &= ~((bad >> 15) * 0xFFFFu);
                 }
               }
 #pragma unroll 1
               for (uint32_t k = 0; k < 16; ++k) {
                 const uint32_t in = g * 16 + k, kr = warp * 32 + in;
+                const bool see0 = (int32_t)(k0 + in) < hi[0] && ((exist >> in) & 1u), see1 = (int32_t)(k0 + in) < hi[1] && ((exist >> in) & 1u);
                 const uint8_t* vrow = gbase + FwSmem::V + s * FW_TILE + kr * 128;
 #pragma unroll
                 for (uint32_t x = 0; x < 8; ++x) {
                   const uint32_t w2 = *reinterpret_cast<const uint32_t*>(vrow + ((x ^ (kr & 7u)) << 4) + pair * 2);
-#pragma unroll
-                  for (uint32_t y = 0; y < 2; ++y) {
-                    const float v = __uint_as_float(y ? w2 & 0xFFFF0000u : w2 << 16);
-#pragma unroll
-                    for (uint32_t u = 0; u < 2; ++u)
-                      if (!(fabsf(v) < INFINITY) && (int32_t)(k0 + in) < hi[u] && ((exist >> in) & 1u)) o[x][u * 2 + y] += v;
-                  }
+                  const float v0 = __uint_as_float(w2 << 16), v1 = __uint_as_float(w2 & 0xFFFF0000u);
+                  const float a0 = fabsf(v0) < INFINITY ? 0.f : v0, a1 = fabsf(v1) < INFINITY ? 0.f : v1;
+                  if (see0) { o[x][0] += a0; o[x][1] += a1; }
+                  if (see1) { o[x][2] += a0; o[x][3] += a1; }
                 }
               }
             }
 #pragma unroll
             for (uint32_t x = 0; x < 4; ++x) {
-              mma16816(o[x * 2], pa, vb[x][0], vb[x][1]);
-              mma16816(o[x * 2 + 1], pa, vb[x][2], vb[x][3]);
+              mma16816(o[x * 2], pg, vb[x][0], vb[x][1]);
+              mma16816(o[x * 2 + 1], pg, vb[x][2], vb[x][3]);
             }
           }
         }
@@ -425,11 +442,53 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
         if (!ok) break;
       }
       if (!ok) break;
-      const bool whole = j0 == 0 && j1 == at.nt;
-      const unsigned long long c_lo = ((at.first + 1) * N - 1) / W, c_hi = ((at.first + at.nt) * N - 1) / W;
-      float* slot = p.part + ((size_t)blockIdx.x * 2 + (blockIdx.x == c_lo ? 1 : 0)) * FW_SLOT;
-      const uint32_t token = R / a.group, h = at.hk * a.group + R % a.group;
-      auto finish = [&](float mx, float lt, const float (&x)[8]) {
+      bool output = j0 == 0 && j1 == at.nt;                  // the block has all of it
+      if (!output) {
+        const uint32_t c_lo = L.block_of(at.first), c_hi = L.block_of(at.first + at.nt - 1);
+        // a block has one share that began in it and one that began before
+        float* slot = p.part + ((size_t)blockIdx.x * 2 + (blockIdx.x == c_lo ? 1 : 0)) * FW_SLOT;
+        if (R < rows) {
+          float* dst = slot + R * 64 + c0;
+          *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]);
+          *reinterpret_cast<float4*>(dst + 4) = make_float4(x[4], x[5], x[6], x[7]);
+          if (c0 == 0) *reinterpret_cast<float2*>(slot + 1024 + R * 2) = make_float2(mx, lt);
+        }
+        __threadfence();
+        ok = meet();
+        if (!ok) break;
+        if (threadIdx.x == 0) {
+          uint32_t* count = p.arrived + (size_t)at.s * a.kv_heads + at.hk;
+          const bool last = atomicAdd(count, 1u) + 1 == c_hi - c_lo + 1;
+          if (last) *count = 0;                              // for the next call
+          *last_flag = last ? 1u : 0u;
+          __threadfence();
+        }
+        ok = meet();
+        if (!ok) break;
+        output = *last_flag != 0u;
+        if (output && R < rows) {
+          // one pass, the sums brought to the larger maximum on the way
+          mx = -INFINITY;
+          lt = 0.f;
+#pragma unroll
+          for (uint32_t y = 0; y < 8; ++y) x[y] = 0.f;
+#pragma unroll 1
+          for (uint32_t b = c_lo; b <= c_hi; ++b) {
+            const float* src = p.part + ((size_t)b * 2 + (b == c_lo ? 1 : 0)) * FW_SLOT;
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(src + 1024 + R * 2));
+            const float4 v0 = __ldcg(reinterpret_cast<const float4*>(src + R * 64 + c0)), v1 = __ldcg(reinterpret_cast<const float4*>(src + R * 64 + c0 + 4));
+            if (ml.y == 0.f) continue;
+            const float m_new = fmaxf(mx, ml.x), f0 = ex2f(mx - m_new), f = ex2f(ml.x - m_new);
+            const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+#pragma unroll
+            for (uint32_t y = 0; y < 8; ++y) x[y] = fmaf(v[y], f, mx == -INFINITY ? 0.f : x[y] * f0);
+            lt = fmaf(ml.y, f, mx == -INFINITY ? 0.f : lt * f0);
+            mx = m_new;
+          }
+        }
+      }
+      if (output && R < rows) {
+        const uint32_t token = R / a.group, h = at.hk * a.group + R % a.group;
         const bool dead = lt == 0.f;
         const float inv = dead ? 0.f : 1.f / lt;
         uint32_t w[4];
@@ -438,48 +497,6 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
         const size_t row = (size_t)at.g.row0 + token;
         *reinterpret_cast<uint4*>(a.out.ptr + (long long)row * a.out.tok + (long long)h * a.out.head + c0) = make_uint4(w[0], w[1], w[2], w[3]);
         if (a.lse && c0 == 0) a.lse[row * a.heads + h] = dead ? -INFINITY : (mx + lg2f(lt)) * LN2_F;
-      };
-      if (R < rows) {
-        if (whole) {
-          finish(mx, lt, x);
-        } else {
-          float* dst = slot + R * 64 + c0;
-          *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]);
-          *reinterpret_cast<float4*>(dst + 4) = make_float4(x[4], x[5], x[6], x[7]);
-          if (c0 == 0) *reinterpret_cast<float2*>(slot + 1024 + R * 2) = make_float2(mx, lt);
-        }
-      }
-      if (!whole) {
-        __threadfence();
-        ok = meet();
-        if (!ok) break;
-        if (threadIdx.x == 0) {
-          uint32_t* count = p.arrived + (size_t)at.s * a.kv_heads + at.hk;
-          const bool last = atomicAdd(count, 1u) + 1 == (uint32_t)(c_hi - c_lo + 1);
-          if (last) *count = 0;                              // for the next call
-          *last_flag = last ? 1u : 0u;
-          __threadfence();
-        }
-        ok = meet();
-        if (!ok) break;
-      }
-      if (!whole && *last_flag && R < rows) {
-        mx = -INFINITY;
-        lt = 0.f;
-        for (unsigned long long b = c_lo; b <= c_hi; ++b) mx = fmaxf(mx, __ldcg(p.part + (b * 2 + (b == c_lo ? 1 : 0)) * FW_SLOT + 1024 + R * 2));
-#pragma unroll
-        for (uint32_t y = 0; y < 8; ++y) x[y] = 0.f;
-        for (unsigned long long b = c_lo; b <= c_hi; ++b) {
-          const float* src = p.part + (b * 2 + (b == c_lo ? 1 : 0)) * FW_SLOT;
-          const float2 ml = __ldcg(reinterpret_cast<const float2*>(src + 1024 + R * 2));
-          if (ml.y == 0.f) continue;
-          const float f = ex2f(ml.x - mx);
-          lt = fmaf(ml.y, f, lt);
-          const float4 v0 = __ldcg(reinterpret_cast<const float4*>(src + R * 64 + c0)), v1 = __ldcg(reinterpret_cast<const float4*>(src + R * 64 + c0 + 4));
-          x[0] = fmaf(v0.x, f, x[0]); x[1] = fmaf(v0.y, f, x[1]); x[2] = fmaf(v0.z, f, x[2]); x[3] = fmaf(v0.w, f, x[3]);
-          x[4] = fmaf(v1.x, f, x[4]); x[5] = fmaf(v1.y, f, x[5]); x[6] = fmaf(v1.z, f, x[6]); x[7] = fmaf(v1.w, f, x[7]);
-        }
-        finish(mx, lt, x);
       }
       t = at.first + j1;                                     // (the flag is next written behind two meetings)
       if (t < t1) next_place(a, at);
