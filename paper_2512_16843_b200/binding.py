@@ -233,8 +233,14 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+# the current stream's handle without a Stream object around it (a tenth of the time), where torch has that
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -670,27 +676,30 @@ class Layer:
 # ----------------------------------------------------------------------------
 # Attention with score modifiers, paged key/value cache, eviction
 # ----------------------------------------------------------------------------
-def _want(t, dtype, dim, name, optional=False):
+def _want(t, dtype, dim, name):
     """Type and rank of a tensor argument; strides that the C side cannot see."""
-    if t is None and optional:
-        return
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.dim() != dim:
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != dim:
         raise LLMCacheError(ERR_ARG, f"{name}: a {dtype} tensor of {dim} dimensions is expected")
 
 
 def _dense(t, dtype, dim, name, optional=False):
-    _want(t, dtype, dim, name, optional)
-    if t is not None and not t.is_contiguous():
-        raise LLMCacheError(ERR_ARG, f"{name}: must be contiguous")
+    if t is None and optional:
+        return
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != dim or not t.is_contiguous():
+        raise LLMCacheError(ERR_ARG, f"{name}: a contiguous {dtype} tensor of {dim} dimensions is expected")
+
+
+_BF16 = torch.bfloat16
 
 
 def _rows(t, name, dim) -> Rows:
     """[seq, token, head, 64] or [token, head, 64] view of any strides."""
-    _want(t, torch.bfloat16, dim, name)
+    if not isinstance(t, torch.Tensor) or t.dtype is not _BF16 or t.dim() != dim:
+        raise LLMCacheError(ERR_ARG, f"{name}: a {_BF16} tensor of {dim} dimensions is expected")
     st = t.stride()
-    if t.shape[-1] != 64 or (st[-1] != 1 and t.numel()):
+    if t.size(-1) != 64 or (st[-1] != 1 and t.numel()):
         raise LLMCacheError(ERR_SHAPE, f"{name}: the last dimension holds 64 neighbouring elements")
-    return Rows(t.data_ptr(), st[0] if dim == 4 else 0, st[-3], st[-2])
+    return Rows(t.data_ptr(), st[0], st[1], st[2]) if dim == 4 else Rows(t.data_ptr(), 0, st[0], st[1])
 
 
 def make_score_mods(*, causal=False, scale=0.0, cap=0.0, slopes=None, table=None, doc=None, prefix=None) -> ScoreMods:
@@ -712,29 +721,29 @@ def make_score_mods(*, causal=False, scale=0.0, cap=0.0, slopes=None, table=None
     return m
 
 
-def _check_heads(mods, heads):
-    if mods is not None and getattr(mods, "tensors", None):
-        slopes, table = mods.tensors[:2]
-        if (slopes is not None and slopes.shape[0] != heads) or (table is not None and table.shape[0] != heads):
-            raise LLMCacheError(ERR_SHAPE, "score modifiers: one row per query head")
+def _check_mods(mods, heads, S=0, n=0):
+    """The shapes of the modifiers' arrays (S, n: of whole sequences)."""
+    slopes, table, doc, prefix = getattr(mods, "tensors", (None, None, None, None))
+    if (slopes is not None and slopes.size(0) != heads) or (table is not None and table.size(0) != heads):
+        raise LLMCacheError(ERR_SHAPE, "score modifiers: one row per query head")
+    if S and ((doc is not None and doc.shape != (S, n)) or (prefix is not None and prefix.shape != (S,))):
+        raise LLMCacheError(ERR_SHAPE, "doc: [n_seqs, seq_len], prefix: [n_seqs]")
 
 
 def llmcache_attention(q, k, v, out, mods: Optional[ScoreMods] = None, lse=None, n_seqs_dev=None, stream=None) -> None:
     """out = softmax(modified q k^T) v.  q, out: bf16 [n_seqs, seq_len, heads, 64]; k, v: [n_seqs, seq_len, kv_heads, 64],
     views of any strides (multiples of 8); lse: optional f32 [n_seqs, seq_len, heads]."""
     rq, rk, rv, ro = _rows(q, "q", 4), _rows(k, "k", 4), _rows(v, "v", 4), _rows(out, "out", 4)
-    S, n, H, _ = q.shape
-    HK = k.shape[2]
-    if k.shape != (S, n, HK, 64) or v.shape != k.shape or out.shape != q.shape:
+    (S, n, H, _), kv = q.shape, k.shape
+    HK = kv[2]
+    if kv[0] != S or kv[1] != n or v.shape != kv or out.shape != q.shape:
         raise LLMCacheError(ERR_SHAPE, "llmcache_attention: q, out [S, n, H, 64], k, v [S, n, HK, 64]")
-    _dense(lse, torch.float32, 3, "lse", True)
-    if lse is not None and lse.shape != (S, n, H):
-        raise LLMCacheError(ERR_SHAPE, "lse: [n_seqs, seq_len, heads]")
-    _check_heads(mods, H)
-    if mods is not None and getattr(mods, "tensors", None):
-        doc, prefix = mods.tensors[2:]
-        if (doc is not None and doc.shape != (S, n)) or (prefix is not None and prefix.shape != (S,)):
-            raise LLMCacheError(ERR_SHAPE, "doc: [n_seqs, seq_len], prefix: [n_seqs]")
+    if lse is not None:
+        _dense(lse, torch.float32, 3, "lse")
+        if lse.shape != (S, n, H):
+            raise LLMCacheError(ERR_SHAPE, "lse: [n_seqs, seq_len, heads]")
+    if mods is not None:
+        _check_mods(mods, H, S, n)
     _check(lib().llmcache_attention(C.byref(rq), C.byref(rk), C.byref(rv), C.byref(ro), S, n, H, HK, _ptr(n_seqs_dev),
                                     C.byref(mods) if mods is not None else None, _ptr(lse), _stream(stream)),
            "llmcache_attention")
@@ -806,6 +815,9 @@ def make_kv_desc(k_pages, v_pages, *, heads, max_seqs, max_rows, max_len, device
     return d
 
 
+_CHUNK_BYTES = C.sizeof(KVChunk)
+
+
 class KVCache:
     """Owner of one llmcache_kv_t handle; keeps the page tensors alive (the library borrows them)."""
 
@@ -816,34 +828,22 @@ class KVCache:
         self.heads, self.kv_heads = heads, self.desc.kv_heads
         self.handle = llmcache_kv_create(self.desc)
 
-    def _table(self, t, seqs, name):
-        _want(t, torch.int32, 2, name)
-        if t.shape[0] != seqs or (t.numel() and t.stride(1) != 1):
-            raise LLMCacheError(ERR_SHAPE, f"{name}: [n_seqs, pages], rows of neighbouring elements")
-        return t.data_ptr(), t.shape[1], t.stride(0)
-
     def _side(self, t, dtype, seqs, name):
         """[n_seqs, kv_heads, ld] side array: (address, ld)."""
         _dense(t, dtype, 3, name)
-        if t.shape[:2] != (seqs, self.kv_heads):
+        if t.size(0) != seqs or t.size(1) != self.kv_heads:
             raise LLMCacheError(ERR_SHAPE, f"{name}: [n_seqs, kv_heads, slots]")
-        return t.data_ptr(), t.shape[2]
+        return t.data_ptr(), t.size(2)
 
     def chunk(self, n_rows, *, cu_rows, lens, pages, longest=0, weights=None, decay=1.0, positions=None, first=None) -> KVChunk:
         """What llmcache_kv_attention and llmcache_layer_extend take alike."""
-        c = KVChunk()
-        c.struct_size = C.sizeof(KVChunk)
         _dense(lens, torch.int32, 1, "lens")
         _dense(cu_rows, torch.int32, 1, "cu_rows")
-        S = lens.shape[0]
-        if cu_rows.shape[0] != S + 1:
-            raise LLMCacheError(ERR_SHAPE, "cu_rows: [n_seqs + 1]")
-        c.n_seqs, c.n_rows, c.longest = S, n_rows, longest
-        c.cu_rows, c.lens = cu_rows.data_ptr(), lens.data_ptr()
-        c.pages, width, c.pages_ld = self._table(pages, S, "pages")
-        if width != c.pages_ld and S > 1:
-            raise LLMCacheError(ERR_ARG, "pages: must be contiguous")
-        c.pages_ld = width
+        _dense(pages, torch.int32, 2, "pages")
+        S = lens.size(0)
+        if cu_rows.size(0) != S + 1 or pages.size(0) != S:
+            raise LLMCacheError(ERR_SHAPE, "cu_rows: [n_seqs + 1], pages: [n_seqs, pages]")
+        c = KVChunk(_CHUNK_BYTES, S, n_rows, longest, cu_rows.data_ptr(), lens.data_ptr(), pages.data_ptr(), pages.size(1))
         if weights is not None:
             c.weights, c.side_ld = self._side(weights, torch.float32, S, "weights")
             c.decay = decay
@@ -854,7 +854,7 @@ class KVCache:
             c.side_ld = ld
         if first is not None:
             _dense(first, torch.int32, 1, "first")
-            if first.shape[0] != S:
+            if first.size(0) != S:
                 raise LLMCacheError(ERR_SHAPE, "first: [n_seqs]")
             c.first = first.data_ptr()
         return c
@@ -867,22 +867,22 @@ class KVCache:
         c = self.chunk(q.shape[0], cu_rows=cu_rows, lens=lens, pages=pages, longest=longest, weights=weights, decay=decay,
                        positions=positions, first=first)
         c.q, c.out = _rows(q, "q", 3), _rows(out, "out", 3)
-        T = q.shape[0]
-        if q.shape != (T, self.heads, 64) or out.shape != q.shape:
+        T = q.size(0)
+        if q.size(1) != self.heads or out.shape != q.shape:
             raise LLMCacheError(ERR_SHAPE, "q, out: [n_rows, heads, 64]")
         if (k_new is None) != (v_new is None):
             raise LLMCacheError(ERR_ARG, "k_new and v_new come together")
         if k_new is not None:
             c.k_new, c.v_new = _rows(k_new, "k_new", 3), _rows(v_new, "v_new", 3)
-            if k_new.shape != (T, self.kv_heads, 64) or v_new.shape != k_new.shape:
+            if k_new.size(0) != T or k_new.size(1) != self.kv_heads or v_new.shape != k_new.shape:
                 raise LLMCacheError(ERR_SHAPE, "k_new, v_new: [n_rows, kv_heads, 64]")
-        _dense(lse, torch.float32, 2, "lse", True)
         if lse is not None:
-            if lse.shape != (T, self.heads):
+            _dense(lse, torch.float32, 2, "lse")
+            if lse.size(0) != T or lse.size(1) != self.heads:
                 raise LLMCacheError(ERR_SHAPE, "lse: [n_rows, heads]")
             c.lse = lse.data_ptr()
         if mods is not None:
-            _check_heads(mods, self.heads)
+            _check_mods(mods, self.heads)
             c.mods = C.pointer(mods)
         llmcache_kv_attention(self.handle, c, stream)
 
@@ -890,19 +890,15 @@ class KVCache:
               new_positions=None, kept=None, stream=None):
         """Copies the `budget` entries per sequence and head that received the most attention, the newest and the first ones
         to new_pages (llmcache_kv_evict)."""
-        e = KVEviction()
-        e.struct_size = C.sizeof(KVEviction)
         _dense(lens, torch.int32, 1, "lens")
         _dense(new_lens, torch.int32, 1, "new_lens")
-        S = lens.shape[0]
-        if new_lens.shape[0] != S:
-            raise LLMCacheError(ERR_SHAPE, "new_lens: [n_seqs]")
-        e.n_seqs, e.budget, e.recent, e.sinks = S, budget, recent, sinks
-        e.lens, e.new_lens = lens.data_ptr(), new_lens.data_ptr()
         _dense(pages, torch.int32, 2, "pages")
         _dense(new_pages, torch.int32, 2, "new_pages")
-        e.pages, e.pages_ld, _ = self._table(pages, S, "pages")
-        e.new_pages, e.new_pages_ld, _ = self._table(new_pages, S, "new_pages")
+        S = lens.size(0)
+        if new_lens.size(0) != S or pages.size(0) != S or new_pages.size(0) != S:
+            raise LLMCacheError(ERR_SHAPE, "lens, new_lens: [n_seqs], pages, new_pages: [n_seqs, pages]")
+        e = KVEviction(C.sizeof(KVEviction), S, budget, recent, sinks, pages.size(1), new_pages.size(1), lens.data_ptr(),
+                       pages.data_ptr(), new_pages.data_ptr(), new_lens.data_ptr())
         e.weights, e.side_ld = self._side(weights, torch.float32, S, "weights")
         for name, t, dtype, to in (("positions", positions, torch.int32, "side_ld"), ("new_weights", new_weights, torch.float32, "new_side_ld"),
                                    ("new_positions", new_positions, torch.int32, "new_side_ld")):

@@ -81,6 +81,8 @@ constexpr uint32_t ATTN_MAX_GROUP = 128;           // query heads per key/value 
 cudaError_t setup_attn_tc();
 cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, int sm_count, cudaStream_t st);
 constexpr uint32_t FEW_ROWS = 16;                  // rows of a sequence and key/value head that k_attn_few takes
+// Whether a paged call goes to k_attn_few: at most 16 rows per sequence and key/value head.  It stores the new rows itself.
+bool attn_is_few(const AttnArgs& a);
 cudaError_t setup_attn_few();
 size_t attn_few_part_floats(int sm_count);
 cudaError_t launch_attn_few(const AttnArgs& a, float* part, uint32_t* arrived, int sm_count, cudaStream_t st);

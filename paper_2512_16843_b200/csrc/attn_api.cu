@@ -337,7 +337,7 @@ int llmcache_kv_attention(llmcache_kv_t* kv, const llmcache_kv_chunk* c, void* s
   OnDevice on(kv->desc.device);
   if (!on.ok) return LLMCACHE_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;
-  if (a.k.ptr || a.positions || (a.weights && a.decay != 0.f)) {
+  if (!attn_is_few(a) && (a.k.ptr || a.positions || (a.weights && a.decay != 0.f))) {
     const cudaError_t e = launch_kv_append(a, kv->sm_count, st);
     if (e != cudaSuccess) return done(e);
   }

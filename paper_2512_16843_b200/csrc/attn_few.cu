@@ -10,6 +10,8 @@
 // In a block one warp keeps three tiles of keys and values on their way (TMA, 32 KB each, two blocks per SM: 192 KB in
 // flight per SM) and four warps take 32 keys of a tile each, with mma.sync m16n8k16: the 16 rows of the smallest
 // tcgen05 shape's 64 or 128 would be all that is used, and there the scores would go through tensor memory for nothing.
+// The call's new rows are stored here, too: whoever works on the tile that they belong to writes them into their page and
+// over what was loaded from there.
 // Softmax statistics and sums are f32; the weights feed the second product as bf16.
 #include <algorithm>
 #include "attn_dev.cuh"
@@ -109,6 +111,32 @@ __device__ __noinline__ void find_place(const AttnArgs& a, uint32_t block, uint3
   p.hk = (t - before) / p.nt;
   p.first = before + p.hk * p.nt;
 }
+// The new rows among the 32 slots from k0 on.  tile_k == nullptr: into their page and the side arrays (before the tile has
+// arrived); else into the tile, from row r0 on.  Two rows at a time: eight lanes each for a key and a value.
+__device__ __noinline__ void store_new(const AttnArgs& a, const FwPlace& at, uint8_t* tile_k, uint8_t* tile_v, uint32_t k0, uint32_t r0) {
+  const uint32_t lane = threadIdx.x & 31, part = lane & 15u, c = part & 7u;
+  const bool is_v = part >= 8;
+  const RowsArgs& src = is_v ? a.v : a.k;
+  const uint32_t begin = (uint32_t)max(at.g.slot0, (int32_t)k0), end = min(min(k0 + 32, at.g.len), (uint32_t)(at.g.slot0 + (int32_t)at.g.cnt));
+#pragma unroll 1
+  for (uint32_t slot = begin + (lane >> 4); slot < end; slot += 2) {
+    const uint32_t i = (uint32_t)((int32_t)slot - at.g.slot0);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (a.k.ptr) v = ld_nc16(src.ptr + (long long)(at.g.row0 + i) * src.tok + (long long)at.hk * src.head + c * 8);
+    if (tile_k) {
+      const uint32_t r = r0 + slot - k0;
+      if (a.k.ptr) *reinterpret_cast<uint4*>((is_v ? tile_v : tile_k) + r * 128 + ((c ^ (r & 7u)) << 4)) = v;
+      continue;
+    }
+    const size_t side = ((size_t)at.s * a.kv_heads + at.hk) * a.side_ld + slot;
+    if (part == 0 && a.positions) a.positions[side] = a.first ? a.first[at.s] + (int32_t)i : (int32_t)slot;
+    if (part == 1 && a.weights && a.decay != 0.f) a.weights[side] = 0.f;
+    if (!a.k.ptr) continue;
+    const int32_t pg = page_of(a, at.s, slot);
+    if (pg >= 0) *reinterpret_cast<uint4*>((is_v ? a.v_pages : a.k_pages) + page_row(a, pg, at.hk, slot) + c * 8) = v;
+  }
+  if (tile_k) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the next tile there comes by TMA)
+}
 __device__ __noinline__ void next_place(const AttnArgs& a, FwPlace& p) {
   p.first += p.nt;
   if (++p.hk < a.kv_heads) return;
@@ -203,6 +231,7 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
     // ---------------------------------------------------------------- products and softmax: 32 keys of a tile per warp
     const uint32_t quad = lane >> 2, pair = (lane & 3u) * 2; // rows quad and quad + 8, columns pair and pair + 1 of every 8
     const float sc = a.m.scale * LOG2E_F;
+    const bool fresh = a.k.ptr || a.positions || (a.weights && a.decay != 0.f);
     bool ok = true;
     uint32_t e = 0, n_meet = 0;
     auto meet = [&]() -> bool {
@@ -217,6 +246,7 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
       const uint32_t j0 = t - at.first, j1 = min(at.nt, t1 - at.first);
       const uint32_t rows = at.g.cnt * a.group;
       // the two rows of this thread
+      const int32_t pos0 = a.first ? a.first[at.s] : at.g.slot0;
       uint32_t qf[4][4];
       int32_t hi[2], qpos[2];
       float slope[2] = {0.f, 0.f};
@@ -227,7 +257,7 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
         const bool mine = R < rows;
         const uint32_t token = mine ? R / a.group : 0u, h = at.hk * a.group + (mine ? R % a.group : 0u);
         hi[u] = !mine ? 0 : a.m.causal ? min(at.g.slot0 + (int32_t)token + 1, (int32_t)at.g.len) : (int32_t)at.g.len;
-        qpos[u] = (a.first ? a.first[at.s] : at.g.slot0) + (int32_t)token;
+        qpos[u] = pos0 + (int32_t)token;
         if (MOD && a.m.slopes) slope[u] = a.m.slopes[h] * LOG2E_F;
         if (MOD && a.m.table) table[u] = a.m.table + (size_t)h * (2 * a.m.reach + 1) + a.m.reach;
         const __nv_bfloat16* q = a.q.ptr + (long long)(at.g.row0 + token) * a.q.tok + (long long)h * a.q.head;
@@ -244,9 +274,16 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 #pragma unroll 1
       for (uint32_t j = j0; j < j1; ++j, ++e) {
         const uint32_t s = e % FW_ST, k0 = j * FW_KEYS + warp * 32;
+        // (TMA reads of the page rows being written: they are replaced in the tile)
+        const bool news = fresh && (int32_t)(k0 + 32) > at.g.slot0 && k0 < at.g.len;
+        if (news) store_new(a, at, nullptr, nullptr, k0, 0);
         ok = warp_wait(full(s), (e / FW_ST) & 1u, abort_flag, lim, 32);
         if (!ok) break;
         const uint32_t exist = reinterpret_cast<volatile const uint32_t*>(gbase + FwSmem::KMASK)[s * 4 + warp];
+        if (news) {
+          store_new(a, at, gbase + FwSmem::K + s * FW_TILE, gbase + FwSmem::V + s * FW_TILE, k0, warp * 32);
+          __syncwarp();
+        }
         if (k0 < at.g.len) {
           // S = Q K^T: four blocks of eight keys
           float c[4][4];
@@ -287,7 +324,9 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 #pragma unroll
                 for (uint32_t y = 0; y < 2; ++y) {
                   const uint32_t key = k0 + n * 8 + pair + y;
-                  const int32_t kpos = positions ? positions[min(key, at.g.len - 1)] : (int32_t)key;
+                  // (a new row's position follows from its slot: it is being written)
+                  const int32_t kpos = (int32_t)key >= at.g.slot0 ? pos0 + ((int32_t)key - at.g.slot0)
+                                       : positions ? positions[key] : (int32_t)key;
 #pragma unroll
                   for (uint32_t u = 0; u < 2; ++u) {
                     const int32_t d = kpos - qpos[u];
@@ -472,11 +511,18 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
           lt = 0.f;
 #pragma unroll
           for (uint32_t y = 0; y < 8; ++y) x[y] = 0.f;
+          auto share = [&](uint32_t b) { return p.part + ((size_t)b * 2 + (b == c_lo ? 1 : 0)) * FW_SLOT; };
+          float2 ml_n = __ldcg(reinterpret_cast<const float2*>(share(c_lo) + 1024 + R * 2));
+          float4 v0_n = __ldcg(reinterpret_cast<const float4*>(share(c_lo) + R * 64 + c0)), v1_n = __ldcg(reinterpret_cast<const float4*>(share(c_lo) + R * 64 + c0 + 4));
 #pragma unroll 1
           for (uint32_t b = c_lo; b <= c_hi; ++b) {
-            const float* src = p.part + ((size_t)b * 2 + (b == c_lo ? 1 : 0)) * FW_SLOT;
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(src + 1024 + R * 2));
-            const float4 v0 = __ldcg(reinterpret_cast<const float4*>(src + R * 64 + c0)), v1 = __ldcg(reinterpret_cast<const float4*>(src + R * 64 + c0 + 4));
+            const float2 ml = ml_n;
+            const float4 v0 = v0_n, v1 = v1_n;
+            if (b < c_hi) {                                  // the next share is on its way
+              ml_n = __ldcg(reinterpret_cast<const float2*>(share(b + 1) + 1024 + R * 2));
+              v0_n = __ldcg(reinterpret_cast<const float4*>(share(b + 1) + R * 64 + c0));
+              v1_n = __ldcg(reinterpret_cast<const float4*>(share(b + 1) + R * 64 + c0 + 4));
+            }
             if (ml.y == 0.f) continue;
             const float m_new = fmaxf(mx, ml.x), f0 = ex2f(mx - m_new), f = ex2f(ml.x - m_new);
             const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};

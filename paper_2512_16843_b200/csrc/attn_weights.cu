@@ -327,11 +327,14 @@ cudaError_t setup_attn_kernels() {
   return cudaFuncSetAttribute(k_attn_weights, cudaFuncAttributeMaxDynamicSharedMemorySize, WT_SMEM);
 }
 
+bool attn_is_few(const AttnArgs& a) {
+  if (!a.pages || (uint64_t)a.n * a.group > FEW_ROWS) return false;
+  const uint64_t cap = std::min<uint64_t>(a.max_len, (uint64_t)a.pages_ld << a.page_shift);
+  return (cap / 128 + 1) * a.n_seqs * a.kv_heads < (1ull << 31);          // (its tiles are counted in 32 bits)
+}
+
 cudaError_t launch_attn(const AttnArgs& a, const AttnScratch& s, int sm_count, cudaStream_t st) {
-  const uint64_t cap = a.pages ? std::min<uint64_t>(a.max_len, (uint64_t)a.pages_ld << a.page_shift) : 0;
-  // (the tiles of a call are counted in 32 bits there)
-  if (a.pages && (uint64_t)a.n * a.group <= FEW_ROWS && (cap / 128 + 1) * a.n_seqs * a.kv_heads < (1ull << 31))
-    return launch_attn_few(a, s.part, s.arrived, sm_count, st);
+  if (attn_is_few(a)) return launch_attn_few(a, s.part, s.arrived, sm_count, st);
   return launch_attn_tc(a, s.part, s.part_units, sm_count, st);
 }
 
