@@ -10,8 +10,11 @@
 // In a block one warp keeps three tiles of keys and values on their way (TMA, 32 KB each, two blocks per SM: 192 KB in
 // flight per SM) and four warps take 32 keys of a tile each, with mma.sync m16n8k16: the 16 rows of the smallest
 // tcgen05 shape's 64 or 128 would be all that is used, and there the scores would go through tensor memory for nothing.
-// The call's new rows are stored here, too: whoever works on the tile that they belong to writes them into their page and
-// over what was loaded from there.
+// The call's new rows are stored here, too: the block that has the tile they belong to writes them into their page (warp 5)
+// and over what was loaded from there (the warp that has these keys; with the stores to memory in the same warp the proxy
+// fence behind the change waited for them, 4 us per sequence).
+// A sequence's end costs a chain of round trips to memory (the share out, the count, the others' shares); warp 5 takes it,
+// and the queries of the next sequence come with its first tile, so that the four warps go on at once.
 // Softmax statistics and sums are f32; the weights feed the second product as bf16.
 #include <algorithm>
 #include "attn_dev.cuh"
@@ -20,16 +23,18 @@ namespace llmc {
 
 namespace {
 
-constexpr int FW_THREADS = 160;                              // warps 0-3: products and softmax, warp 4: loads
+constexpr int FW_THREADS = 192;                              // warps 0-3: products and softmax, 4: loads, 5: joins shares
 constexpr uint32_t FW_ST = 3, FW_TILE = 16384, FW_KEYS = 128;
 struct FwSmem {
   static constexpr uint32_t K = 0;
   static constexpr uint32_t V = K + FW_ST * FW_TILE;
   static constexpr uint32_t O = V + FW_ST * FW_TILE;         // f32 [warp][row][32]: half of the columns, at the end of a sequence
   static constexpr uint32_t STAT = O + 4 * 16 * 32 * 4;      // f32 [warp][row][2]
-  static constexpr uint32_t KMASK = STAT + 4 * 16 * 2 * 4;   // u32 [stage][4]: keys that exist
+  static constexpr uint32_t Q = STAT + 4 * 16 * 2 * 4;       // [2][row][64] bf16: queries of a sequence and head
+  static constexpr uint32_t SEG = Q + 2 * 2048;              // FwSeg [2]
+  static constexpr uint32_t KMASK = SEG + 128;               // u32 [stage][4]: keys that exist
   static constexpr uint32_t BAR = KMASK + FW_ST * 16;
-  static constexpr uint32_t MISC = BAR + 16 * 8;
+  static constexpr uint32_t MISC = BAR + 24 * 8;
   static constexpr uint32_t TOTAL = MISC + 32;
 };
 constexpr uint32_t FW_SMEM = FwSmem::TOTAL + 1024;
@@ -70,6 +75,9 @@ struct FwList {
 };
 // A sequence and head in it: first = number of its tile 0 of nt.
 struct FwPlace { uint32_t s, hk, nt, first; SeqGeo g; };
+// What the load warp tells the others about it: tiles j0 .. j1 - 1 are this block's; nt == 0: there is no more.
+struct FwSeg { FwPlace at; uint32_t j0, j1; int32_t pos0; };
+static_assert(sizeof(FwSeg) <= 64, "two fit their place in shared memory");
 
 __device__ __forceinline__ uint32_t warp_scan(uint32_t x) {  // inclusive sum over the lanes
   const uint32_t lane = threadIdx.x & 31;
@@ -111,31 +119,38 @@ __device__ __noinline__ void find_place(const AttnArgs& a, uint32_t block, uint3
   p.hk = (t - before) / p.nt;
   p.first = before + p.hk * p.nt;
 }
-// The new rows among the 32 slots from k0 on.  tile_k == nullptr: into their page and the side arrays (before the tile has
-// arrived); else into the tile, from row r0 on.  Two rows at a time: eight lanes each for a key and a value.
-__device__ __noinline__ void store_new(const AttnArgs& a, const FwPlace& at, uint8_t* tile_k, uint8_t* tile_v, uint32_t k0, uint32_t r0) {
-  const uint32_t lane = threadIdx.x & 31, part = lane & 15u, c = part & 7u;
-  const bool is_v = part >= 8;
-  const RowsArgs& src = is_v ? a.v : a.k;
-  const uint32_t begin = (uint32_t)max(at.g.slot0, (int32_t)k0), end = min(min(k0 + 32, at.g.len), (uint32_t)(at.g.slot0 + (int32_t)at.g.cnt));
+// eight columns of a finished row
+__device__ __noinline__ void few_output(const AttnArgs& a, const FwPlace& at, uint32_t R, uint32_t c0, float mx, float lt, const float (&x)[8]) {
+  const uint32_t token = R / a.group, h = at.hk * a.group + R % a.group;
+  const bool dead = lt == 0.f;                               // nothing seen
+  const float inv = dead ? 0.f : 1.f / lt;
+  uint32_t w[4];
+#pragma unroll
+  for (uint32_t y = 0; y < 4; ++y) w[y] = pack2(dead ? 0.f : x[2 * y] * inv, dead ? 0.f : x[2 * y + 1] * inv);
+  const size_t row = (size_t)at.g.row0 + token;
+  *reinterpret_cast<uint4*>(a.out.ptr + (long long)row * a.out.tok + (long long)h * a.out.head + c0) = make_uint4(w[0], w[1], w[2], w[3]);
+  if (a.lse && c0 == 0) a.lse[row * a.heads + h] = dead ? -INFINITY : (mx + lg2f(lt)) * LN2_F;
+}
+// One of the 16-byte pieces of the new row of a slot: eight lanes have its key, eight its value.
+__device__ __forceinline__ uint4 new_piece(const AttnArgs& a, const FwPlace& at, uint32_t slot) {
+  const uint32_t part = threadIdx.x & 15u;
+  const RowsArgs& src = part < 8 ? a.k : a.v;
+  return ld_nc16(src.ptr + (long long)(at.g.row0 + (uint32_t)((int32_t)slot - at.g.slot0)) * src.tok + (long long)at.hk * src.head + (part & 7u) * 8);
+}
+// The new rows with slots from .. to - 1: into their pages and the side arrays (one warp, two rows at a time).
+__device__ __noinline__ void store_new(const AttnArgs& a, const FwPlace& at, uint32_t from, uint32_t to) {
+  const uint32_t lane = threadIdx.x & 31, part = lane & 15u;
 #pragma unroll 1
-  for (uint32_t slot = begin + (lane >> 4); slot < end; slot += 2) {
-    const uint32_t i = (uint32_t)((int32_t)slot - at.g.slot0);
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (a.k.ptr) v = ld_nc16(src.ptr + (long long)(at.g.row0 + i) * src.tok + (long long)at.hk * src.head + c * 8);
-    if (tile_k) {
-      const uint32_t r = r0 + slot - k0;
-      if (a.k.ptr) *reinterpret_cast<uint4*>((is_v ? tile_v : tile_k) + r * 128 + ((c ^ (r & 7u)) << 4)) = v;
-      continue;
-    }
+  for (uint32_t slot = from + (lane >> 4); slot < to; slot += 2) {
     const size_t side = ((size_t)at.s * a.kv_heads + at.hk) * a.side_ld + slot;
-    if (part == 0 && a.positions) a.positions[side] = a.first ? a.first[at.s] + (int32_t)i : (int32_t)slot;
+    const int32_t i = (int32_t)slot - at.g.slot0;
+    if (part == 0 && a.positions) a.positions[side] = a.first ? a.first[at.s] + i : (int32_t)slot;
     if (part == 1 && a.weights && a.decay != 0.f) a.weights[side] = 0.f;
     if (!a.k.ptr) continue;
+    const uint4 v = new_piece(a, at, slot);
     const int32_t pg = page_of(a, at.s, slot);
-    if (pg >= 0) *reinterpret_cast<uint4*>((is_v ? a.v_pages : a.k_pages) + page_row(a, pg, at.hk, slot) + c * 8) = v;
+    if (pg >= 0) *reinterpret_cast<uint4*>((part < 8 ? a.k_pages : a.v_pages) + page_row(a, pg, at.hk, slot) + (part & 7u) * 8) = v;
   }
-  if (tile_k) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the next tile there comes by TMA)
 }
 __device__ __noinline__ void next_place(const AttnArgs& a, FwPlace& p) {
   p.first += p.nt;
@@ -161,12 +176,18 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
   auto full = [&](uint32_t s) { return bar0 + 8 * s; };
   auto empty = [&](uint32_t s) { return bar0 + 8 * (FW_ST + s); };
   const uint32_t together = bar0 + 8 * 2 * FW_ST;
+  auto share_out = [&](uint32_t b) { return together + 48 + 8 * b; };      // each completes once at most
+  auto seg_full = [&](uint32_t b) { return together + 16 + 8 * b; };
+  auto seg_empty = [&](uint32_t b) { return together + 32 + 8 * b; };
+  FwSeg* segs = reinterpret_cast<FwSeg*>(gbase + FwSmem::SEG);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(gbase + FwSmem::MISC);
-  volatile uint32_t* last_flag = abort_flag + 1;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < FW_ST; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 4); }
     mbar_init(together, 4);
+    for (uint32_t b = 0; b < 2; ++b) {
+      mbar_init(share_out(b), 4); mbar_init(seg_full(b), 1); mbar_init(seg_empty(b), 4 + 1);
+    }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -174,22 +195,27 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
   __syncthreads();
   griddep_sync();
   const unsigned long long lim = wait_limit(a.status);
-  FwList L;
-  FwPlace at;
-  find_place(a, blockIdx.x, gridDim.x, L, at);
-  const bool work = blockIdx.x < L.N;
-  const uint32_t t0 = work ? L.begin(blockIdx.x) : 0u, t1 = work ? L.begin(blockIdx.x + 1) : 0u;
 
   if (warp == 4) {
     // ---------------------------------------------------------------- loads
+    FwList L;
+    FwPlace at;
+    find_place(a, blockIdx.x, gridDim.x, L, at);
+    const bool work = blockIdx.x < L.N && !producer_idle(a.status);
+    const uint32_t t0 = work ? L.begin(blockIdx.x) : 0u, t1 = work ? L.begin(blockIdx.x + 1) : 0u;
     bool ok = true;
-    uint32_t e = 0;
-    if (t0 < t1 && !producer_idle(a.status)) {
+    uint32_t e = 0, n = 0;
 #pragma unroll 1
-      for (uint32_t t = t0; t < t1 && ok; ) {
-        const uint32_t j0 = t - at.first, j1 = min(at.nt, t1 - at.first);
+    for (uint32_t t = t0;;) {
+      const bool end = t >= t1;
+      if (end && producer_idle(a.status)) break;
+      const uint32_t j0 = end ? 0u : t - at.first, j1 = end ? 0u : min(at.nt, t1 - at.first), b = n & 1u;
+      ok = warp_wait(seg_empty(b), ((n >> 1) & 1u) ^ 1u, abort_flag, lim, 32);
+      if (!ok) break;
+      if (end) at.nt = 0;
 #pragma unroll 1
-        for (uint32_t j = j0; j < j1; ++j, ++e) {
+      for (uint32_t j = j0; j <= j1 && ok; ++j) {
+        if (j < j1) {
           const uint32_t s = e % FW_ST, boxes = FW_KEYS / p.page_box, per_word = max(1u, 32u / p.page_box);
           int row = p.oob_row;
           if (lane < boxes) {
@@ -215,10 +241,28 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
             tma_load_2d(base + FwSmem::K + off, &map_k, 0, row, full(s));
             tma_load_2d(base + FwSmem::V + off, &map_v, 0, row, full(s));
           }
+          ++e;
         }
-        t = at.first + j1;
-        if (t < t1) next_place(a, at);
+        if (j == j0) {
+          // behind the first tile's loads: the queries (zeros in rows that do not exist), then the description
+          const uint32_t rows = end ? 0u : at.g.cnt * a.group;
+#pragma unroll
+          for (uint32_t u = 0; u < 4; ++u) {
+            const uint32_t R = u * 4 + (lane >> 3), c = lane & 7u;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (R < rows)
+              v = ld_nc16(a.q.ptr + (long long)(at.g.row0 + R / a.group) * a.q.tok + (long long)(at.hk * a.group + R % a.group) * a.q.head + c * 8);
+            *reinterpret_cast<uint4*>(gbase + FwSmem::Q + b * 2048 + R * 128 + ((c ^ (R & 7u)) << 4)) = v;
+          }
+          if (lane == 0) segs[b] = FwSeg{at, j0, j1, end ? 0 : a.first ? a.first[at.s] : at.g.slot0};
+          __syncwarp();
+          if (lane == 0) mbar_arrive(seg_full(b));
+        }
       }
+      if (!ok || end) break;
+      ++n;
+      t = at.first + j1;
+      if (t < t1) next_place(a, at);
     }
     if (!ok && lane == 0) { *abort_flag = 1; atomicExch(a.status, 1u); }
     __syncwarp();
@@ -227,11 +271,77 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 #pragma unroll 1
       for (uint32_t b = 0; b < FW_ST && b < e; ++b) mbar_wait(full((e - 1 - b) % FW_ST), ((e - 1 - b) / FW_ST) & 1u, &never, 200000000ull);
     }
-  } else if (t0 < t1) {
+  } else if (warp == 5) {
+    // ---------------------------------------------------------------- shares of sequences that several blocks work on
+    FwList L;
+    FwPlace unused;
+    find_place(a, blockIdx.x, gridDim.x, L, unused);
+    const bool fresh = a.k.ptr || a.positions || (a.weights && a.decay != 0.f);
+    bool ok = true;
+#pragma unroll 1
+    for (uint32_t n = 0;; ++n) {
+      ok = warp_wait(seg_full(n & 1u), (n >> 1) & 1u, abort_flag, lim, 64);
+      if (!ok) break;
+      const FwSeg seg = segs[n & 1u];
+      const FwPlace& at = seg.at;
+      if (!at.nt) break;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(seg_empty(n & 1u));
+      if (fresh) {
+        const uint32_t from = (uint32_t)max(at.g.slot0, (int32_t)(seg.j0 * FW_KEYS));
+        const uint32_t to = min(min(at.g.len, seg.j1 * FW_KEYS), (uint32_t)max(0, at.g.slot0 + (int32_t)at.g.cnt));
+        if (from < to) store_new(a, at, from, to);
+        __syncwarp();
+      }
+      if (seg.j0 == 0 && seg.j1 == at.nt) continue;
+      ok = warp_wait(share_out(seg.j0 == 0 ? 1u : 0u), 0u, abort_flag, lim, 64);
+      if (!ok) break;
+      const uint32_t c_lo = L.block_of(at.first), c_hi = L.block_of(at.first + at.nt - 1);
+      uint32_t last = 0;
+      if (lane == 0) {
+        __threadfence();                                     // the block's share before its count (the barrier orders it before this)
+        uint32_t* count = p.arrived + (size_t)at.s * a.kv_heads + at.hk;
+        last = atomicAdd(count, 1u) == c_hi - c_lo ? 1u : 0u;
+        if (last) *count = 0;                                // for the next call
+        __threadfence();
+      }
+      last = __shfl_sync(0xFFFFFFFFu, last, 0);
+      if (!last) continue;
+      // four rows at a time, eight lanes (of eight columns) each
+#pragma unroll 1
+      for (uint32_t R = lane >> 3; R < at.g.cnt * a.group; R += 4) {
+        const uint32_t c0 = (lane & 7u) * 8;
+        auto share = [&](uint32_t b) { return p.part + ((size_t)b * 2 + (b == c_lo ? 1 : 0)) * FW_SLOT; };
+        float mx = -INFINITY, lt = 0.f, x[8];
+#pragma unroll
+        for (uint32_t y = 0; y < 8; ++y) x[y] = 0.f;
+        float2 ml_n = __ldcg(reinterpret_cast<const float2*>(share(c_lo) + 1024 + R * 2));
+        float4 v0_n = __ldcg(reinterpret_cast<const float4*>(share(c_lo) + R * 64 + c0)), v1_n = __ldcg(reinterpret_cast<const float4*>(share(c_lo) + R * 64 + c0 + 4));
+#pragma unroll 1
+        for (uint32_t b = c_lo; b <= c_hi; ++b) {
+          const float2 ml = ml_n;
+          const float v[8] = {v0_n.x, v0_n.y, v0_n.z, v0_n.w, v1_n.x, v1_n.y, v1_n.z, v1_n.w};
+          if (b < c_hi) {                                    // the next share is on its way
+            ml_n = __ldcg(reinterpret_cast<const float2*>(share(b + 1) + 1024 + R * 2));
+            v0_n = __ldcg(reinterpret_cast<const float4*>(share(b + 1) + R * 64 + c0));
+            v1_n = __ldcg(reinterpret_cast<const float4*>(share(b + 1) + R * 64 + c0 + 4));
+          }
+          if (ml.y == 0.f) continue;                         // nothing seen in this share
+          const float m_new = fmaxf(mx, ml.x), f0 = ex2f(mx - m_new), f = ex2f(ml.x - m_new);
+#pragma unroll
+          for (uint32_t y = 0; y < 8; ++y) x[y] = fmaf(v[y], f, mx == -INFINITY ? 0.f : x[y] * f0);
+          lt = fmaf(ml.y, f, mx == -INFINITY ? 0.f : lt * f0);
+          mx = m_new;
+        }
+        few_output(a, at, R, c0, mx, lt, x);
+      }
+      __syncwarp();
+    }
+    if (!ok && lane == 0) { *abort_flag = 1; atomicExch(a.status, 1u); }
+  } else {
     // ---------------------------------------------------------------- products and softmax: 32 keys of a tile per warp
     const uint32_t quad = lane >> 2, pair = (lane & 3u) * 2; // rows quad and quad + 8, columns pair and pair + 1 of every 8
     const float sc = a.m.scale * LOG2E_F;
-    const bool fresh = a.k.ptr || a.positions || (a.weights && a.decay != 0.f);
     bool ok = true;
     uint32_t e = 0, n_meet = 0;
     auto meet = [&]() -> bool {
@@ -242,12 +352,24 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
       return met;
     };
 #pragma unroll 1
-    for (uint32_t t = t0; t < t1 && ok; ) {
-      const uint32_t j0 = t - at.first, j1 = min(at.nt, t1 - at.first);
-      const uint32_t rows = at.g.cnt * a.group;
-      // the two rows of this thread
-      const int32_t pos0 = a.first ? a.first[at.s] : at.g.slot0;
+    for (uint32_t n = 0;; ++n) {
+      ok = warp_wait(seg_full(n & 1u), (n >> 1) & 1u, abort_flag, lim, 32);
+      if (!ok) break;
+      const FwSeg seg = segs[n & 1u];
+      const FwPlace& at = seg.at;
+      if (!at.nt) break;
+      const uint32_t j0 = seg.j0, j1 = seg.j1, rows = at.g.cnt * a.group;
+      const uint32_t new_end = min(at.g.len, (uint32_t)max(0, at.g.slot0 + (int32_t)at.g.cnt));      // behind the last new row's slot
+      const int32_t pos0 = seg.pos0;
       uint32_t qf[4][4];
+#pragma unroll
+      for (uint32_t kk = 0; kk < 4; ++kk) {
+        const uint32_t R = lane & 15u;
+        ldsm4(base + FwSmem::Q + (n & 1u) * 2048 + R * 128 + (((kk * 2 + (lane >> 4)) ^ (R & 7u)) << 4), qf[kk]);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(seg_empty(n & 1u));
+      // the two rows of this thread
       int32_t hi[2], qpos[2];
       float slope[2] = {0.f, 0.f};
       const float* table[2] = {nullptr, nullptr};
@@ -260,12 +382,6 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
         qpos[u] = pos0 + (int32_t)token;
         if (MOD && a.m.slopes) slope[u] = a.m.slopes[h] * LOG2E_F;
         if (MOD && a.m.table) table[u] = a.m.table + (size_t)h * (2 * a.m.reach + 1) + a.m.reach;
-        const __nv_bfloat16* q = a.q.ptr + (long long)(at.g.row0 + token) * a.q.tok + (long long)h * a.q.head;
-#pragma unroll
-        for (uint32_t kk = 0; kk < 4; ++kk) {
-          qf[kk][u] = mine ? *reinterpret_cast<const uint32_t*>(q + kk * 16 + pair) : 0u;
-          qf[kk][2 + u] = mine ? *reinterpret_cast<const uint32_t*>(q + kk * 16 + 8 + pair) : 0u;
-        }
       }
       float o[8][4];
 #pragma unroll
@@ -274,14 +390,23 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 #pragma unroll 1
       for (uint32_t j = j0; j < j1; ++j, ++e) {
         const uint32_t s = e % FW_ST, k0 = j * FW_KEYS + warp * 32;
-        // (TMA reads of the page rows being written: they are replaced in the tile)
-        const bool news = fresh && (int32_t)(k0 + 32) > at.g.slot0 && k0 < at.g.len;
-        if (news) store_new(a, at, nullptr, nullptr, k0, 0);
+        // new rows among this warp's keys replace what TMA reads of their (not yet written) places
+        const uint32_t new0 = (uint32_t)max(at.g.slot0, (int32_t)k0) + (lane >> 4), new1 = min(k0 + 32, new_end);
+        const bool news = a.k.ptr && (int32_t)(k0 + 32) > at.g.slot0 && k0 < new_end;
+        uint4 piece = make_uint4(0, 0, 0, 0);
+        if (news && new0 < new1) piece = new_piece(a, at, new0);
         ok = warp_wait(full(s), (e / FW_ST) & 1u, abort_flag, lim, 32);
         if (!ok) break;
         const uint32_t exist = reinterpret_cast<volatile const uint32_t*>(gbase + FwSmem::KMASK)[s * 4 + warp];
         if (news) {
-          store_new(a, at, gbase + FwSmem::K + s * FW_TILE, gbase + FwSmem::V + s * FW_TILE, k0, warp * 32);
+          uint8_t* tile = gbase + ((lane & 15u) < 8 ? FwSmem::K : FwSmem::V) + s * FW_TILE;
+#pragma unroll 1
+          for (uint32_t slot = new0; slot < new1; slot += 2) {
+            const uint32_t r = slot - j * FW_KEYS;
+            *reinterpret_cast<uint4*>(tile + r * 128 + (((lane & 7u) ^ (r & 7u)) << 4)) = piece;
+            if (slot + 2 < new1) piece = new_piece(a, at, slot + 2);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // (the next tile there comes by TMA)
           __syncwarp();
         }
         if (k0 < at.g.len) {
@@ -481,71 +606,20 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
         if (!ok) break;
       }
       if (!ok) break;
-      bool output = j0 == 0 && j1 == at.nt;                  // the block has all of it
-      if (!output) {
-        const uint32_t c_lo = L.block_of(at.first), c_hi = L.block_of(at.first + at.nt - 1);
-        // a block has one share that began in it and one that began before
-        float* slot = p.part + ((size_t)blockIdx.x * 2 + (blockIdx.x == c_lo ? 1 : 0)) * FW_SLOT;
-        if (R < rows) {
-          float* dst = slot + R * 64 + c0;
-          *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]);
-          *reinterpret_cast<float4*>(dst + 4) = make_float4(x[4], x[5], x[6], x[7]);
-          if (c0 == 0) *reinterpret_cast<float2*>(slot + 1024 + R * 2) = make_float2(mx, lt);
-        }
-        __threadfence();
-        ok = meet();
-        if (!ok) break;
-        if (threadIdx.x == 0) {
-          uint32_t* count = p.arrived + (size_t)at.s * a.kv_heads + at.hk;
-          const bool last = atomicAdd(count, 1u) + 1 == c_hi - c_lo + 1;
-          if (last) *count = 0;                              // for the next call
-          *last_flag = last ? 1u : 0u;
-          __threadfence();
-        }
-        ok = meet();
-        if (!ok) break;
-        output = *last_flag != 0u;
-        if (output && R < rows) {
-          // one pass, the sums brought to the larger maximum on the way
-          mx = -INFINITY;
-          lt = 0.f;
-#pragma unroll
-          for (uint32_t y = 0; y < 8; ++y) x[y] = 0.f;
-          auto share = [&](uint32_t b) { return p.part + ((size_t)b * 2 + (b == c_lo ? 1 : 0)) * FW_SLOT; };
-          float2 ml_n = __ldcg(reinterpret_cast<const float2*>(share(c_lo) + 1024 + R * 2));
-          float4 v0_n = __ldcg(reinterpret_cast<const float4*>(share(c_lo) + R * 64 + c0)), v1_n = __ldcg(reinterpret_cast<const float4*>(share(c_lo) + R * 64 + c0 + 4));
-#pragma unroll 1
-          for (uint32_t b = c_lo; b <= c_hi; ++b) {
-            const float2 ml = ml_n;
-            const float4 v0 = v0_n, v1 = v1_n;
-            if (b < c_hi) {                                  // the next share is on its way
-              ml_n = __ldcg(reinterpret_cast<const float2*>(share(b + 1) + 1024 + R * 2));
-              v0_n = __ldcg(reinterpret_cast<const float4*>(share(b + 1) + R * 64 + c0));
-              v1_n = __ldcg(reinterpret_cast<const float4*>(share(b + 1) + R * 64 + c0 + 4));
-            }
-            if (ml.y == 0.f) continue;
-            const float m_new = fmaxf(mx, ml.x), f0 = ex2f(mx - m_new), f = ex2f(ml.x - m_new);
-            const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
-#pragma unroll
-            for (uint32_t y = 0; y < 8; ++y) x[y] = fmaf(v[y], f, mx == -INFINITY ? 0.f : x[y] * f0);
-            lt = fmaf(ml.y, f, mx == -INFINITY ? 0.f : lt * f0);
-            mx = m_new;
-          }
-        }
+      if (j0 == 0 && j1 == at.nt) {                          // the block has all of it
+        if (R < rows) few_output(a, at, R, c0, mx, lt, x);
+        continue;
       }
-      if (output && R < rows) {
-        const uint32_t token = R / a.group, h = at.hk * a.group + R % a.group;
-        const bool dead = lt == 0.f;
-        const float inv = dead ? 0.f : 1.f / lt;
-        uint32_t w[4];
-#pragma unroll
-        for (uint32_t y = 0; y < 4; ++y) w[y] = pack2(dead ? 0.f : x[2 * y] * inv, dead ? 0.f : x[2 * y + 1] * inv);
-        const size_t row = (size_t)at.g.row0 + token;
-        *reinterpret_cast<uint4*>(a.out.ptr + (long long)row * a.out.tok + (long long)h * a.out.head + c0) = make_uint4(w[0], w[1], w[2], w[3]);
-        if (a.lse && c0 == 0) a.lse[row * a.heads + h] = dead ? -INFINITY : (mx + lg2f(lt)) * LN2_F;
+      if (R < rows) {
+        // a block has one share that began in it (j0 == 0) and one that began before
+        float* slot = p.part + ((size_t)blockIdx.x * 2 + (j0 == 0 ? 1 : 0)) * FW_SLOT;
+        float* dst = slot + R * 64 + c0;
+        *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<float4*>(dst + 4) = make_float4(x[4], x[5], x[6], x[7]);
+        if (c0 == 0) *reinterpret_cast<float2*>(slot + 1024 + R * 2) = make_float2(mx, lt);
       }
-      t = at.first + j1;                                     // (the flag is next written behind two meetings)
-      if (t < t1) next_place(a, at);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(share_out(j0 == 0 ? 1u : 0u));
     }
     if (!ok) { *abort_flag = 1; atomicExch(a.status, 1u); }
   }
