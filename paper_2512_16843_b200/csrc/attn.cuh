@@ -40,6 +40,9 @@ struct AttnArgs {
   uint32_t n_rows, pages_ld, num_pages, page_shift, max_len;
   unsigned long long side_ld, page_stride;
   __nv_bfloat16 *k_pages, *v_pages;
+  // few rows whose weights are asked for: modified scores (base 2, -inf: not seen) [n_seqs, kv_heads, row][score_ld], or null
+  float* scores;
+  uint32_t score_ld, score_rows;
 };
 
 // A sequence of a paged call: its rows row0 .. row0 + cnt - 1 take the slots slot0 .. of len slots.  Whatever the
@@ -89,7 +92,11 @@ cudaError_t launch_attn_few(const AttnArgs& a, float* part, uint32_t* arrived, i
 cudaError_t setup_attn_kernels();
 // Scratch of a paged call: part for part_units x PART_FLOATS floats, arrived for [n_seqs, kv_heads] words that are zero
 // between calls.  Null for whole sequences.
-struct AttnScratch { float* part = nullptr; size_t part_units = 0; uint32_t* arrived = nullptr; };
+struct AttnScratch {
+  float* part = nullptr;
+  size_t part_units = 0;
+  uint32_t* arrived = nullptr;
+};
 cudaError_t launch_attn(const AttnArgs& a, const AttnScratch& s, int sm_count, cudaStream_t st);
 // received weights of a paged call whose lse is complete
 cudaError_t launch_attn_weights(const AttnArgs& a, int sm_count, cudaStream_t st);

@@ -1,4 +1,5 @@
 // C ABI of the attention operators: llmcache_attention and the paged key/value cache (llmcache_kv_*).
+#include <algorithm>
 #include <cstring>
 #include <mutex>
 #include <new>
@@ -142,7 +143,15 @@ int check_kv_desc(const llmcache_kv_desc* d) {
 // (row, head, share of the keys) results of one call.  Keys are split only while rows alone leave SMs idle, so the shares of
 // all rows never exceed 2 x 256 rows per SM.
 constexpr size_t KV_PART_UNITS = 2 * 256 * 160;
-struct KvLayout { size_t status, arrived, part, lse, kept, count, total; };
+// Scores of few rows are kept for the weights where they fit: 4 bytes per row and key, up to 64 MB.  (A call that needs more
+// has its scores formed again from the keys.)
+constexpr size_t KV_SCORE_FLOATS = 16u << 20;
+size_t kv_score_floats(const llmcache_kv_desc& d) {
+  // a token for every sequence, its tiles filled up
+  const size_t most = (size_t)d.max_seqs * d.heads * (((size_t)d.max_len + 127) / 128 * 128);
+  return most < KV_SCORE_FLOATS ? most : KV_SCORE_FLOATS;
+}
+struct KvLayout { size_t status, arrived, part, scores, lse, kept, count, total; };
 KvLayout kv_layout(const llmcache_kv_desc& d) {
   KvLayout L{};
   size_t o = 0;
@@ -150,6 +159,7 @@ KvLayout kv_layout(const llmcache_kv_desc& d) {
   L.status = take(16);
   L.arrived = take((size_t)d.max_seqs * d.kv_heads * 4);
   L.part = take(KV_PART_UNITS * PART_FLOATS * 4);
+  L.scores = take(kv_score_floats(d) * 4);
   L.lse = take((size_t)d.max_rows * d.heads * 4);
   L.kept = take((size_t)d.max_seqs * d.kv_heads * d.max_len * 4);
   L.count = take((size_t)d.max_seqs * 4);
@@ -302,6 +312,8 @@ int llmcache_kv_create(const llmcache_kv_desc* desc, llmcache_kv_t** kv_out) {
   kv->status = (uint32_t*)(kv->ws + lay.status);
   kv->arrived = (uint32_t*)(kv->ws + lay.arrived);
   kv->part = (float*)(kv->ws + lay.part);
+  kv->scores = (float*)(kv->ws + lay.scores);
+  kv->score_floats = kv_score_floats(*desc);
   kv->lse = (float*)(kv->ws + lay.lse);
   kv->kept = (int32_t*)(kv->ws + lay.kept);
   kv->count = (uint32_t*)(kv->ws + lay.count);
@@ -334,6 +346,15 @@ int llmcache_kv_attention(llmcache_kv_t* kv, const llmcache_kv_chunk* c, void* s
   AttnArgs a{};
   int rc = chunk_args(kv, c, &a);
   if (rc != LLMCACHE_OK || a.n_seqs == 0) return rc;
+  if (a.weights && attn_is_few(a)) {
+    const uint64_t cap = std::min<uint64_t>(a.max_len, (uint64_t)a.pages_ld << a.page_shift), ld = (cap + 127) / 128 * 128;
+    const uint64_t rows = (uint64_t)a.n * a.group;
+    if ((uint64_t)a.n_seqs * a.kv_heads * rows * ld <= kv->score_floats) {
+      a.scores = kv->scores;
+      a.score_ld = (uint32_t)ld;
+      a.score_rows = (uint32_t)rows;
+    }
+  }
   OnDevice on(kv->desc.device);
   if (!on.ok) return LLMCACHE_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;

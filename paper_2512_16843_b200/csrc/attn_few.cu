@@ -91,9 +91,12 @@ __device__ __forceinline__ uint32_t warp_scan(uint32_t x) {  // inclusive sum ov
 // The list, and the place of its tile number begin(block) (one warp together).
 __device__ __noinline__ void find_place(const AttnArgs& a, uint32_t block, uint32_t blocks, FwList& L, FwPlace& p) {
   const uint32_t lane = threadIdx.x & 31;
-  uint32_t sum = 0;
+  uint32_t sum = 0, kept = 0;
 #pragma unroll 1
-  for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += 32) sum += s0 + lane < a.n_seqs ? seq_tiles(seq_geo(a, s0 + lane)) * a.kv_heads : 0u;
+  for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += 32) {
+    kept = s0 + lane < a.n_seqs ? seq_tiles(seq_geo(a, s0 + lane)) * a.kv_heads : 0u;
+    sum += kept;
+  }
   L.W = __reduce_add_sync(0xFFFFFFFFu, sum);
   L.N = min(blocks, L.W);                                    // blocks with work
   L.each = L.N ? L.W / L.N : 0u;
@@ -103,7 +106,7 @@ __device__ __noinline__ void find_place(const AttnArgs& a, uint32_t block, uint3
   uint32_t before = 0;
 #pragma unroll 1
   for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += 32) {
-    const uint32_t mine = s0 + lane < a.n_seqs ? seq_tiles(seq_geo(a, s0 + lane)) * a.kv_heads : 0u;
+    const uint32_t mine = a.n_seqs <= 32 ? kept : s0 + lane < a.n_seqs ? seq_tiles(seq_geo(a, s0 + lane)) * a.kv_heads : 0u;
     const uint32_t incl = warp_scan(mine);
     const uint32_t hit = __ballot_sync(0xFFFFFFFFu, before + incl > t);
     if (hit) {
@@ -481,6 +484,17 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
               const bool see = (int32_t)(k0 + in) < hi[x >> 1] && ((exist >> in) & 1u);
               c[n][x] = see ? c[n][x] : -INFINITY;
               mt[x >> 1] = fmaxf(mt[x >> 1], c[n][x]);
+            }
+          }
+          if (a.scores) {
+            // for the received weights: 16 rows * 4 bytes per key at most, against 256 that were read
+#pragma unroll
+            for (uint32_t u = 0; u < 2; ++u) {
+              const uint32_t R = quad + u * 8;
+              if (R >= rows) continue;
+              float* dst = a.scores + (((size_t)at.s * a.kv_heads + at.hk) * a.score_rows + R) * a.score_ld + k0 + pair;
+#pragma unroll
+              for (uint32_t n = 0; n < 4; ++n) *reinterpret_cast<float2*>(dst + n * 8) = make_float2(c[n][u * 2], c[n][u * 2 + 1]);
             }
           }
           float nm[2];

@@ -10,6 +10,8 @@ struct llmcache_kv {
   uint32_t* status = nullptr;    // a bounded wait expired; diagnostic knobs behind it
   float* part = nullptr;         // shares of the keys of one call
   uint32_t* arrived = nullptr;   // [max_seqs, kv_heads], zero between calls
+  float* scores = nullptr;       // of few rows whose weights are recorded: score_floats of them
+  size_t score_floats = 0;
   float* lse = nullptr;          // [max_rows, heads] where the caller takes none
   int32_t* kept = nullptr;       // eviction: slots kept [max_seqs, kv_heads, <= max_len] ...
   uint32_t* count = nullptr;     // ... and how many per sequence

@@ -338,8 +338,38 @@ cudaError_t launch_attn(const AttnArgs& a, const AttnScratch& s, int sm_count, c
   return launch_attn_tc(a, s.part, s.part_units, sm_count, st);
 }
 
+// The weights of a call whose scores k_attn_few left: one thread per key, blocks in turn over the keys of a sequence and
+// head.  Reads 4 bytes per row and key, once (they are still in L2 as a rule).
+__global__ void __launch_bounds__(256) k_weights_of_scores(const __grid_constant__ AttnArgs a, uint32_t parts) {
+  griddep_sync();
+  const uint32_t part = blockIdx.x % parts, hk = (blockIdx.x / parts) % a.kv_heads, sq = blockIdx.x / parts / a.kv_heads;
+  const SeqGeo g = seq_geo(a, sq);
+  const uint32_t rows = g.cnt * a.group;
+  __shared__ float lse[FEW_ROWS];
+  if (threadIdx.x < rows) {
+    const float x = a.lse[(size_t)(g.row0 + threadIdx.x / a.group) * a.heads + hk * a.group + threadIdx.x % a.group] * LOG2E_F;
+    lse[threadIdx.x] = x == -INFINITY ? INFINITY : x;        // a row that sees nothing gives nothing
+  }
+  __syncthreads();
+  const size_t pair = (size_t)sq * a.kv_heads + hk;
+  const float* scores = a.scores + pair * a.score_rows * a.score_ld;
+  for (uint32_t key = part * 256 + threadIdx.x; key < g.len; key += parts * 256) {
+    float sum = 0.f;
+#pragma unroll 4
+    for (uint32_t R = 0; R < rows; ++R) sum += ex2f(__ldcg(scores + (size_t)R * a.score_ld + key) - lse[R]);
+    float& w = a.weights[pair * a.side_ld + key];
+    w = a.decay == 0.f ? sum : fmaf(a.decay, w, sum);
+  }
+}
+
 cudaError_t launch_attn_weights(const AttnArgs& a, int sm_count, cudaStream_t st) {
   if (a.n_seqs == 0) return cudaSuccess;
+  if (a.scores) {
+    const uint64_t pairs = (uint64_t)a.n_seqs * a.kv_heads, chunks = (a.score_ld + 255) / 256;
+    const uint32_t parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(chunks, ((uint64_t)sm_count * 8 + pairs - 1) / pairs));
+    if (pairs * parts > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+    return launch_k(k_weights_of_scores, dim3((uint32_t)(pairs * parts)), dim3(256), 0, st, a, parts);
+  }
   alignas(64) CUtensorMap map_q, map_k;
   WtPlan p{};
   const uint32_t toks = std::min(128 / a.group, a.n);        // tokens of a query tile
