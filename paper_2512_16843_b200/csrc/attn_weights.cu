@@ -1,7 +1,9 @@
 // Received weights of a paged call: weights[key] = decay * weights[key] + sum over the call's rows, and over the query heads
 // that share the key, of exp(z - lse).  The scores are formed again, with the keys as the rows of the product:
 //   S^T = K Q^T    tcgen05.mma 128 keys x up to 128 query rows x 64
-// so that a thread owns a key and its sum over the rows needs no exchange and no atomics (same bits every time).  A block
+// so that a thread owns a key and its sum over the rows needs no exchange and no atomics (same bits every time).  What a
+// row adds to a score is prepared once per tile: -lse, and with a linear bias slope * (first key - query) with the slope
+// beside it, so that a score costs one or two multiply-adds and its exponential.  A block
 // takes a sequence and head and every parts-th key tile of it; the query rows stream past each key tile (they come from
 // L2).  Two groups of four warps take turns with the query tiles, two blocks per SM.  Reads K once more (128 bytes per
 // key and head) and the queries; one exponential per score, as in the attention itself.
@@ -18,7 +20,8 @@ constexpr uint32_t WT_ST = 3, WT_TILE = 16384, WT_KEYS = 128, WT_TMEM = 256;
 struct WtSmem {
   static constexpr uint32_t K = 0;                           // [2]
   static constexpr uint32_t Q = K + 2 * WT_TILE;             // [WT_ST]
-  static constexpr uint32_t LSE = Q + WT_ST * WT_TILE;       // f32 [stage][128], base 2; +inf: the row gives nothing
+  static constexpr uint32_t ADD = Q + WT_ST * WT_TILE;       // f32 [stage][128], base 2: - lse (- inf: the row gives nothing) + linear bias
+  static constexpr uint32_t LSE = ADD + WT_ST * 512;         // f32 [stage][128]: - lse alone
   static constexpr uint32_t SLOPE = LSE + WT_ST * 512;       // f32 [stage][128]
   static constexpr uint32_t QPOS = SLOPE + WT_ST * 512;      // i32 [stage][128]
   static constexpr uint32_t HI = QPOS + WT_ST * 512;         // i32 [stage][128]: keys below it are seen
@@ -38,6 +41,8 @@ struct WtPlan {
 
 }  // namespace
 
+// MOD: scores are capped or biased.
+template <bool MOD>
 __global__ void __launch_bounds__(WT_THREADS, 2)
 k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                const __grid_constant__ AttnArgs a, const __grid_constant__ WtPlan p) {
@@ -162,28 +167,34 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     }
   } else if (warp < 4) {
     bool ok = true;
+    const int32_t pos0 = a.first ? a.first[sq] : g.slot0;
     const uint32_t total = ((nt - part + p.parts - 1) / p.parts) * qtiles;
     for (uint32_t n = 0; n < total; ++n) {
-      const uint32_t s = n % WT_ST, qt = n % qtiles;
+      const uint32_t s = n % WT_ST, qt = n % qtiles, j = part + n / qtiles * p.parts;
       ok = warp_wait(empty(s), ((n / WT_ST) & 1u) ^ 1u, abort_flag, lim, 32);
       if (!ok) break;
-#pragma unroll
+#pragma unroll 1
       for (uint32_t u = 0; u < 2; ++u) {
         const uint32_t c = u * 64 + threadIdx.x - 64, R = qt * p.rt + c;
         const uint32_t token = R / a.group, h = hk * a.group + R % a.group;
         const bool real = c < p.rt && R < rows;
-        float lse = INFINITY;
+        float add = -INFINITY;
         if (real) {
-          lse = a.lse[(size_t)(g.row0 + token) * a.heads + h] * LOG2E_F;
-          if (lse == -INFINITY) lse = INFINITY;
+          add = -a.lse[(size_t)(g.row0 + token) * a.heads + h] * LOG2E_F;
+          if (add == INFINITY) add = -INFINITY;              // a row that sees nothing gives nothing
         }
         const uint32_t at = s * 128 + c;
-        reinterpret_cast<float*>(gbase + WtSmem::LSE)[at] = lse;
-        if (a.m.slopes) reinterpret_cast<float*>(gbase + WtSmem::SLOPE)[at] = real ? a.m.slopes[h] * LOG2E_F : 0.f;
-        if (a.m.table) reinterpret_cast<int32_t*>(gbase + WtSmem::TAB)[at] = (int32_t)((real ? h : 0u) * (2 * a.m.reach + 1)) + a.m.reach;
-        reinterpret_cast<int32_t*>(gbase + WtSmem::QPOS)[at] = a.first ? a.first[sq] + (int32_t)token : g.slot0 + (int32_t)token;
+        const int32_t qpos = pos0 + (int32_t)token;
+        const float slope = MOD && a.m.slopes && real ? a.m.slopes[h] * LOG2E_F : 0.f;
+        reinterpret_cast<float*>(gbase + WtSmem::ADD)[at] = fmaf(slope, (float)((int32_t)(j * WT_KEYS) - qpos), add);
         reinterpret_cast<int32_t*>(gbase + WtSmem::HI)[at] =
             !real ? 0 : a.m.causal ? min(g.slot0 + (int32_t)token + 1, (int32_t)g.len) : (int32_t)g.len;
+        if constexpr (MOD) {
+          reinterpret_cast<float*>(gbase + WtSmem::LSE)[at] = add;
+          reinterpret_cast<float*>(gbase + WtSmem::SLOPE)[at] = slope;
+          reinterpret_cast<int32_t*>(gbase + WtSmem::QPOS)[at] = qpos;
+          if (a.m.table) reinterpret_cast<int32_t*>(gbase + WtSmem::TAB)[at] = (int32_t)((real ? h : 0u) * (2 * a.m.reach + 1)) + a.m.reach;
+        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(side_full(s));
@@ -192,8 +203,9 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   } else {
     const uint32_t w = (warp - 4) >> 2, quarter = warp & 3u, key_in = quarter * 32 + lane;
     const uint32_t t_s = tmem + w * 128 + ((quarter * 32u) << 16);
-    const bool modified = a.m.cap > 0.f || a.m.slopes || a.m.table;
-    const float sc = a.m.scale * LOG2E_F, sc_in = a.m.cap > 0.f ? a.m.scale / a.m.cap : sc;
+    const float unit = a.m.cap > 0.f ? a.m.cap * LOG2E_F : a.m.scale * LOG2E_F;
+    // the straight path needs keys that lie before their queries, at their slots
+    const bool odd = MOD && (a.m.table || (a.m.slopes && (a.positions || !a.m.causal)));
     float* xch = reinterpret_cast<float*>(gbase + WtSmem::XCH);
     bool ok = true;
     uint32_t n = 0, mine = 0, t = 0;                         // entries of the block, of this group; key tiles
@@ -210,72 +222,90 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         if (!ok) break;
         ++mine;
         tc_fence_after();
-        const float* lse = reinterpret_cast<const float*>(gbase + WtSmem::LSE) + s * 128;
+        const float* add = reinterpret_cast<const float*>(gbase + WtSmem::ADD) + s * 128;
         const float* slope = reinterpret_cast<const float*>(gbase + WtSmem::SLOPE) + s * 128;
-        const int32_t* qpos = reinterpret_cast<const int32_t*>(gbase + WtSmem::QPOS) + s * 128;
         const int32_t* hi = reinterpret_cast<const int32_t*>(gbase + WtSmem::HI) + s * 128;
-        const int32_t* tab = reinterpret_cast<const int32_t*>(gbase + WtSmem::TAB) + s * 128;
         const uint32_t n_rows = min(p.rt, rows - qt * p.rt);
         float s0 = 0.f, s1 = 0.f;
 #pragma unroll 1
         for (uint32_t c = 0; c < n_rows; c += 32) {
           uint32_t v[32];
           tc_ld_32x32(t_s + c, v);
-          tc_wait_ld32(v);
-          unsigned long long x[16];
-          const unsigned long long sc2 = f2_dup(sc_in);
-#pragma unroll
-          for (uint32_t i = 0; i < 16; ++i) x[i] = f2_mul(f2_pack(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), sc2);
-          if (modified) {
-            if (a.m.cap > 0.f) {
-              float big = 0.f;
-#pragma unroll
-              for (uint32_t i = 0; i < 16; ++i) big = max3f(big, fabsf(f2_lo(x[i])), fabsf(f2_hi(x[i])));
-              const unsigned long long cap2 = f2_dup(a.m.cap * LOG2E_F);
-              const bool large = __any_sync(0xFFFFFFFFu, !(big <= 0.75f));
-#pragma unroll
-              for (uint32_t i = 0; i < 16; ++i) {
-                unsigned long long y = tanh_small2(x[i]);
-                if (large) {
-                  const float u0 = f2_lo(x[i]), u1 = f2_hi(x[i]);
-                  y = f2_pack(fabsf(u0) <= 0.75f ? f2_lo(y) : tanh_large(u0), fabsf(u1) <= 0.75f ? f2_hi(y) : tanh_large(u1));
-                }
-                x[i] = f2_mul(y, cap2);
-              }
-            }
-            if (a.m.slopes) {
-#pragma unroll
-              for (uint32_t i = 0; i < 16; ++i) {
-                const int2 q = *reinterpret_cast<const int2*>(qpos + c + 2 * i);
-                const float2 sl = *reinterpret_cast<const float2*>(slope + c + 2 * i);
-                x[i] = f2_fma(f2_pack(fabsf((float)(kpos - q.x)), fabsf((float)(kpos - q.y))), f2_pack(-sl.x, -sl.y), x[i]);
-              }
-            }
-            if (a.m.table) {
-              const int32_t reach = a.m.reach;
-#pragma unroll
-              for (uint32_t i = 0; i < 16; ++i) {
-                const int2 q = *reinterpret_cast<const int2*>(qpos + c + 2 * i), o = *reinterpret_cast<const int2*>(tab + c + 2 * i);
-                // (rows that do not exist point at head 0)
-                const float b0 = __ldg(a.m.table + o.x + min(max(kpos - q.x, -reach), reach));
-                const float b1 = __ldg(a.m.table + o.y + min(max(kpos - q.y, -reach), reach));
-                x[i] = f2_add(x[i], f2_pack(b0 < -1e38f ? b0 : b0 * LOG2E_F, b1 < -1e38f ? b1 : b1 * LOG2E_F));
-              }
-            }
-          }
           // (the rows of a tile see ever more keys: the first row of the chunk sees the fewest)
           const bool all = c + 32 <= n_rows && hi[c] >= (int32_t)((j + 1) * WT_KEYS);
+          bool by_hand = odd;
+          tc_wait_ld32(v);
+          if constexpr (MOD) {
+            if (a.m.cap > 0.f) {
+              const unsigned long long in2 = f2_dup(a.m.scale / a.m.cap);
+              float big[2] = {0.f, 0.f};
 #pragma unroll
-          for (uint32_t i = 0; i < 16; ++i) {
-            const float2 ls = *reinterpret_cast<const float2*>(lse + c + 2 * i);
-            float p0 = ex2f(f2_lo(x[i]) - ls.x), p1 = ex2f(f2_hi(x[i]) - ls.y);
-            if (!all) {
-              const int2 b = *reinterpret_cast<const int2*>(hi + c + 2 * i);
-              if ((int32_t)key >= b.x) p0 = 0.f;
-              if ((int32_t)key >= b.y) p1 = 0.f;
+              for (uint32_t i = 0; i < 16; ++i) {
+                const unsigned long long t = f2_mul(f2_pack(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), in2);
+                // (columns behind the last row hold whatever was there before)
+                if (c + 2 * i < n_rows) big[i & 1u] = max3f(big[i & 1u], fabsf(f2_lo(t)), c + 2 * i + 1 < n_rows ? fabsf(f2_hi(t)) : 0.f);
+                const unsigned long long y = tanh_small2(t);
+                v[2 * i] = __float_as_uint(f2_lo(y));
+                v[2 * i + 1] = __float_as_uint(f2_hi(y));
+              }
+              by_hand = by_hand || !(fmaxf(big[0], big[1]) <= 0.75f);
             }
-            s0 += p0;
-            s1 += p1;
+          }
+          if (!MOD || !__any_sync(0xFFFFFFFFu, by_hand)) {
+            const unsigned long long u2 = f2_dup(unit), k2 = f2_dup((float)key_in);
+#pragma unroll
+            for (uint32_t i = 0; i < 32; i += 4) {
+              const float4 b = *reinterpret_cast<const float4*>(add + c + i);
+              unsigned long long x0 = f2_fma(f2_pack(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), u2, f2_pack(b.x, b.y));
+              unsigned long long x1 = f2_fma(f2_pack(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), u2, f2_pack(b.z, b.w));
+              if (MOD) {
+                const float4 sl = *reinterpret_cast<const float4*>(slope + c + i);
+                x0 = f2_fma(f2_pack(sl.x, sl.y), k2, x0);
+                x1 = f2_fma(f2_pack(sl.z, sl.w), k2, x1);
+              }
+              float p0 = ex2f(f2_lo(x0)), p1 = ex2f(f2_hi(x0)), p2 = ex2f(f2_lo(x1)), p3 = ex2f(f2_hi(x1));
+              if (!all) {
+                const int4 q = *reinterpret_cast<const int4*>(hi + c + i);
+                p0 = (int32_t)key < q.x ? p0 : 0.f;
+                p1 = (int32_t)key < q.y ? p1 : 0.f;
+                p2 = (int32_t)key < q.z ? p2 : 0.f;
+                p3 = (int32_t)key < q.w ? p3 : 0.f;
+              }
+              s0 += p0 + p2;
+              s1 += p1 + p3;
+            }
+          } else {
+            // scores beyond the polynomial, positions, distances on both sides, table entries: 16 rows at a time
+            const float* lse = reinterpret_cast<const float*>(gbase + WtSmem::LSE) + s * 128;
+            const int32_t* qpos = reinterpret_cast<const int32_t*>(gbase + WtSmem::QPOS) + s * 128;
+            const int32_t* tab = reinterpret_cast<const int32_t*>(gbase + WtSmem::TAB) + s * 128;
+#pragma unroll 1
+            for (uint32_t o = c; o < c + 32; o += 16) {
+              uint32_t u[16];
+              tc_ld_16(t_s + o, u);
+              float b[16], z[16];
+#pragma unroll
+              for (uint32_t i = 0; i < 16; ++i) b[i] = 0.f;
+              if (a.m.table) {
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i)
+                  b[i] = o + i < n_rows ? __ldg(a.m.table + tab[o + i] + min(max(kpos - qpos[o + i], -a.m.reach), a.m.reach)) : 0.f;
+              }
+              tc_wait_ld16(u);
+#pragma unroll
+              for (uint32_t i = 0; i < 16; ++i) z[i] = __uint_as_float(u[i]) * (a.m.cap > 0.f ? a.m.scale / a.m.cap : unit);
+              if (a.m.cap > 0.f) {
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i)
+                  z[i] = (fabsf(z[i]) <= 0.75f ? f2_lo(tanh_small2(f2_dup(z[i]))) : tanh_large(z[i])) * unit;
+              }
+#pragma unroll
+              for (uint32_t i = 0; i < 16; ++i) {
+                z[i] = fmaf(-slope[o + i], fabsf((float)(kpos - qpos[o + i])), z[i]) + (b[i] < -1e38f ? b[i] : b[i] * LOG2E_F) + lse[o + i];
+                const float x = ex2f(z[i]);
+                s0 += (int32_t)key < hi[o + i] ? x : 0.f;
+              }
+            }
           }
         }
         sum += s0 + s1;
@@ -323,8 +353,9 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 cudaError_t setup_attn_kernels() {
   cudaError_t e = setup_attn_tc();
   if (e == cudaSuccess) e = setup_attn_few();
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attn_weights<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, WT_SMEM);
   if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(k_attn_weights, cudaFuncAttributeMaxDynamicSharedMemorySize, WT_SMEM);
+  return cudaFuncSetAttribute(k_attn_weights<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, WT_SMEM);
 }
 
 bool attn_is_few(const AttnArgs& a) {
@@ -388,7 +419,8 @@ cudaError_t launch_attn_weights(const AttnArgs& a, int sm_count, cudaStream_t st
   if (!make_tensor_map_rows(&map_q, a.q, a.heads, a.n_rows, 1, a.group, toks) ||
       !make_tensor_map_bf16(&map_k, a.k_pages, rows, 64, p.page_box))
     return cudaErrorInvalidValue;
-  return launch_k(k_attn_weights, dim3((uint32_t)(pairs * p.parts)), dim3(WT_THREADS), WT_SMEM, st, map_q, map_k, a, p);
+  const bool mod = a.m.cap > 0.f || a.m.slopes || a.m.table;
+  return launch_k(mod ? k_attn_weights<true> : k_attn_weights<false>, dim3((uint32_t)(pairs * p.parts)), dim3(WT_THREADS), WT_SMEM, st, map_q, map_k, a, p);
 }
 
 }  // namespace llmc
