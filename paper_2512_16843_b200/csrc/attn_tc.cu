@@ -89,7 +89,9 @@ __device__ __forceinline__ uint32_t below(int32_t n) { return n >= 32 ? ~0u : n 
 struct TcPlan {
   uint32_t rt;                   // rows of a query tile: the largest multiple of the group up to 128
   uint32_t inv_group;            // ceil(65536 / group): x / group = x * inv_group >> 16 for x < 256
-  uint32_t qtiles, splits;       // pairs of query tiles per sequence and head; shares of the keys
+  uint32_t qtiles, splits;       // pairs of query tiles per sequence and head; shares of the keys per item ...
+  uint32_t narrow;               // ... and the block's two halves share an item's keys, too (the rows fill one query tile)
+  uint32_t shares;               // shares of a row's keys: splits, or twice that
   uint32_t n_items, page_box;    // page_box: rows of a page's box
   int page_rows, oob_row;        // rows of 64 elements between pages; a row behind the last page
   float* part_o;                 // [split][row][head][64], [split][row][head][2] (m, l) when splits > 1
@@ -100,7 +102,8 @@ struct TcItem {
   uint32_t s, hk, sp, r0, rows;  // rows: those of the sequence (tokens * group)
   SeqGeo g;
   int32_t pre;
-  uint32_t ts, te;               // its key tiles
+  uint32_t ts, te;               // its key tiles ...
+  uint32_t mid;                  // ... of which, if narrow, the second half of the block takes those from here on
   bool live;                     // rows of this item exist
 };
 // keys below this bound may be seen by the row of a token
@@ -121,12 +124,13 @@ __device__ __forceinline__ TcItem tc_item(const AttnArgs& a, const TcPlan& p, ui
   it.pre = a.m.prefix && it.s < n_seqs ? a.m.prefix[it.s] : 0;
   it.rows = it.g.cnt * a.group;
   it.live = it.s < n_seqs && it.r0 < it.rows;
-  it.ts = it.te = 0;
+  it.ts = it.te = it.mid = 0;
   if (it.live) {
     const uint32_t nt = (keys_to(a, it.g.len, it.g.slot0, it.pre, (min(it.rows, it.r0 + 2 * p.rt) - 1) / a.group) + TC_KEYS - 1) / TC_KEYS;
-    const uint32_t per = (nt + p.splits - 1) / p.splits;
-    it.ts = min(nt, it.sp * per);
-    it.te = min(nt, it.ts + per);
+    const uint32_t halves = p.narrow ? 2u : 1u, per = (nt + p.shares - 1) / p.shares;
+    it.ts = min(nt, it.sp * halves * per);
+    it.mid = min(nt, it.ts + per);
+    it.te = min(nt, it.ts + halves * per);
   }
   return it;
 }
@@ -222,7 +226,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           const int tok = (int)o.tok0 + (paged ? (int)it.g.row0 : 0), seq = paged ? 0 : (int)it.s;
           mbar_expect_tx(q_full(b), 2 * bytes);
           tma_load_4d(sQ + (b * 2) * TC_TILE, &map_q, 0, (int)(it.hk * a.group), tok, seq, q_full(b));
-          tma_load_4d(sQ + (b * 2 + 1) * TC_TILE, &map_q, 0, (int)(it.hk * a.group), tok + (int)per, seq, q_full(b));
+          tma_load_4d(sQ + (b * 2 + 1) * TC_TILE, &map_q, 0, (int)(it.hk * a.group), tok + (p.narrow ? 0 : (int)per), seq, q_full(b));
         } else {
           mbar_arrive(q_full(b));
         }
@@ -230,6 +234,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       ++qc;
       if (it.ts >= it.te) continue;
       const uint32_t nt0 = tiles_of(a, p, it, 0), nt1 = tiles_of(a, p, it, 1);
+      const uint32_t n_second = p.narrow ? it.te - it.mid : 0u;
       // smallest and largest document of either query tile (padding left out)
       int32_t lo0 = INT32_MAX, hi0 = -1, lo1 = INT32_MAX, hi1 = -1;
       const int32_t* doc = DOC ? a.m.doc + (size_t)it.s * a.n : nullptr;
@@ -244,6 +249,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       }
       // flags of key tile j (0: nobody needs it)
       auto needs = [&](uint32_t j) -> uint32_t {
+        if (PAGED && p.narrow) return j < it.mid ? F_NEED0 : F_NEED1;
         uint32_t f = (j < nt0 ? F_NEED0 : 0u) | (j < nt1 ? F_NEED1 : 0u);
         if (!DOC || !f) return f;
         int32_t lo = INT32_MAX, hi = -1;
@@ -265,7 +271,13 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       uint32_t j = 0, f = 0;
 #pragma unroll 1
       for (uint32_t c = it.ts; c <= it.te; ++c) {
-        uint32_t fc = c < it.te ? needs(c) : 0u;
+        // (narrow: the halves' tiles in turn, then the rest of the first's)
+        uint32_t jc = c;
+        if (PAGED && p.narrow) {
+          const uint32_t x = c - it.ts;
+          jc = x < 2 * n_second ? ((x & 1u) ? it.mid : it.ts) + x / 2 : it.ts + x - n_second;
+        }
+        uint32_t fc = c < it.te ? needs(jc) : 0u;
         if (!fc && c + 1 == it.te && !have) fc = nt0 > c ? F_NEED0 : F_NEED1;
         if (!fc && c < it.te) continue;
         if (have) {
@@ -301,7 +313,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           ++e;
         }
         have = true;
-        j = c;
+        j = jc;
         f = fc;
       }
     }
@@ -516,7 +528,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     const float sc = a.m.scale * LOG2E_F;
     constexpr bool side = PAGED || DOC;                      // warp 3's data are needed before the scores are
     // the row's place in its item: an item starts at a multiple of the group
-    const uint32_t in_item = w * p.rt + r, my_tok = (in_item * p.inv_group) >> 16, my_head = in_item - my_tok * a.group;
+    const uint32_t row0_in = p.narrow ? 0u : w * p.rt, in_item = row0_in + r, my_tok = (in_item * p.inv_group) >> 16, my_head = in_item - my_tok * a.group;
     bool ok = true;
     uint32_t n_msg = 0, n_s = 0;                             // messages; tiles
 #pragma unroll 1
@@ -532,7 +544,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       const int32_t pre = it.pre;
       const uint32_t hi = mine ? keys_to(a, len, slot0, pre, token) : 0u;
       // keys that every row of this tile sees
-      const uint32_t all_see = w * p.rt < left_rows ? keys_to(a, len, slot0, pre, it.tok0 + ((w * p.rt * p.inv_group) >> 16)) : 0u;
+      const uint32_t all_see = row0_in < left_rows ? keys_to(a, len, slot0, pre, it.tok0 + ((row0_in * p.inv_group) >> 16)) : 0u;
       const int32_t qdoc = DOC && mine ? a.m.doc[(size_t)sq * a.n + token] : -1;
       const int32_t qpos = (PAGED && MOD && a.first ? a.first[sq] : slot0) + (int32_t)token;
       const float slope = MOD && a.m.slopes && mine ? a.m.slopes[h] * LOG2E_F : 0.f;
@@ -792,7 +804,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         if (!ok) break;
         tc_fence_after();
       }
-      const uint32_t sp = it.sp;
+      const uint32_t sp = p.narrow ? it.sp * 2 + w : it.sp;
       const size_t n_rowids = (size_t)a.n_rows * a.heads;    // of a paged call
       const size_t rowid = (paged ? (size_t)row0 + token : (size_t)sq * a.n + token) * a.heads + h;
       const uint32_t tok0 = it.tok0;
@@ -810,7 +822,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         }
 #pragma unroll
         for (uint32_t x = 0; x < 16; ++x) v[x] = dead ? 0u : v[x];
-        if (p.splits > 1) {
+        if (p.shares > 1) {
           if (mine) {
 #pragma unroll
             for (uint32_t x = 0; x < 16; x += 4)
@@ -831,23 +843,23 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           const uint32_t c = __ffsll((long long)bits) - 1;
           const bool nan = ((rowp[0] | (rowp[1] & rowp[2])) >> c) & 1ull || l != l, neg = (rowp[2] >> c) & 1ull;
           const float x = nan ? NAN : neg ? -INFINITY : INFINITY;
-          if (p.splits > 1) part[c] = x;
+          if (p.shares > 1) part[c] = x;
           else *reinterpret_cast<__nv_bfloat16*>(stage + lane * 128 + (((c >> 3) ^ (lane & 7u)) << 4) + (c & 7u) * 2) = __float2bfloat16_rn(x);
         }
       }
       __syncwarp();
       if (mine) {
-        if (p.splits > 1)
+        if (p.shares > 1)
           reinterpret_cast<float2*>(p.part_ml)[(size_t)sp * n_rowids + rowid] = make_float2(l != l && m_ref == -INFINITY ? 0.f : m_ref, l);
         else if (a.lse)
           a.lse[rowid] = dead ? -INFINITY : (m_ref + lg2f(l)) * LN2_F;
       }
-      if (p.splits == 1) {
+      if (p.shares == 1) {
         __nv_bfloat16* out0 = a.out.ptr + (paged ? (long long)row0 * a.out.tok : (long long)sq * a.out.seq) + (long long)tok0 * a.out.tok +
                               (long long)hk * a.group * a.out.head + (lane & 7u) * 8;
 #pragma unroll 1
         for (uint32_t rr = lane >> 3; rr < 32; rr += 4) {
-          const uint32_t in_tile = quarter * 32 + rr, ii = w * p.rt + in_tile, tk = (ii * p.inv_group) >> 16;
+          const uint32_t in_tile = quarter * 32 + rr, ii = row0_in + in_tile, tk = (ii * p.inv_group) >> 16;
           if (in_tile < p.rt && ii < left_rows)
             *reinterpret_cast<uint4*>(out0 + (long long)tk * a.out.tok + (long long)(ii - tk * a.group) * a.out.head) =
                 *reinterpret_cast<const uint4*>(stage + rr * 128 + (((lane & 7u) ^ (rr & 7u)) << 4));
@@ -925,16 +937,22 @@ cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, in
   p.qtiles = (uint32_t)((seq_rows + 2 * p.rt - 1) / (2 * p.rt));
   p.splits = 1;
   const uint64_t items = (uint64_t)p.qtiles * a.n_seqs * a.kv_heads;
+  p.shares = 1;
   if (paged && part) {
-    // shares of at least two key tiles, as many as it takes to give every SM an item
     const uint64_t cap = std::min<uint64_t>(a.max_len, (uint64_t)a.pages_ld << a.page_shift), tiles = (cap + TC_KEYS - 1) / TC_KEYS;
     const uint64_t rows = (uint64_t)a.n_rows * a.heads;
-    uint64_t sp = (uint64_t)sm_count / items;
-    sp = std::min(sp, (tiles + 1) / 2);
-    sp = std::min<uint64_t>(sp, part_units / rows);
+    // rows that fill one query tile: both halves of a block work on them, with the keys shared out between them
+    p.narrow = seq_rows <= p.rt && tiles >= 4 && part_units / rows >= 2;
+    const uint64_t halves = p.narrow ? 2 : 1;
+    // as many shares as it takes to give every SM an item (of two key tiles at least), and up to three items per SM where they
+    // stay long (16 tiles), because sequences of uneven lengths then end together
+    uint64_t sp = std::min<uint64_t>((uint64_t)sm_count / items, (tiles + 1) / 2 / halves);
+    sp = std::max<uint64_t>(sp, std::min<uint64_t>(3ull * sm_count / items, tiles / 16 / halves));
+    sp = std::min<uint64_t>(sp, part_units / rows / halves);
     if (sp > 1) p.splits = (uint32_t)sp;
+    p.shares = p.splits * (uint32_t)halves;
     p.part_o = part;
-    p.part_ml = part + (size_t)p.splits * rows * 64;
+    p.part_ml = part + (size_t)p.shares * rows * 64;
   }
   if (items * p.splits > 0x7FFFFFFFull) return cudaErrorInvalidValue;
   p.n_items = (uint32_t)(items * p.splits);
@@ -956,10 +974,10 @@ cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, in
   const uint32_t grid = p.n_items < (uint32_t)sm_count ? p.n_items : (uint32_t)sm_count;
   const bool mod = a.m.cap > 0.f || a.m.slopes || a.m.table;
   cudaError_t e = launch_k(tc_kernel(paged, a.m.doc != nullptr, mod), dim3(grid), dim3(TC_THREADS), TC_SMEM, st, map_q, map_k, map_v, a, p);
-  if (e != cudaSuccess || p.splits == 1) return e;
+  if (e != cudaSuccess || p.shares == 1) return e;
   const uint64_t warps = (uint64_t)a.n_rows * a.heads;
   const uint64_t blocks = std::min<uint64_t>((warps + 7) / 8, (uint64_t)sm_count * 8);
-  return launch_k(k_attn_join, dim3((uint32_t)blocks), dim3(256), 0, st, a, (const float*)p.part_o, (const float*)p.part_ml, p.splits);
+  return launch_k(k_attn_join, dim3((uint32_t)blocks), dim3(256), 0, st, a, (const float*)p.part_o, (const float*)p.part_ml, p.shares);
 }
 
 }  // namespace llmc
