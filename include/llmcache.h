@@ -461,7 +461,7 @@ typedef struct llmcache_score_mods {
   float    cap;              /* 0 => scores are not capped; at least 1e-3 otherwise */
   uint32_t reach;            /* table: largest distance with an entry of its own, <= 1,024 */
   const float*   slopes;     /* f32 [heads], or NULL */
-  const float*   table;      /* f32 [heads, 2 * reach + 1], or NULL; entries may be -inf */
+  const float*   table;      /* f32 [heads, 2 * reach + 1], or NULL; an entry of -inf hides the key like a mask */
   const int32_t* doc;        /* i32 [n_seqs, seq_len] document of every token, < 0: padding; or NULL */
   const int32_t* prefix;     /* i32 [n_seqs], keys below it are seen by every query (causal only); or NULL */
 } llmcache_score_mods;
@@ -478,7 +478,8 @@ typedef struct llmcache_rows {
  * heads, at least a 128th of them (query head h reads key/value head h / (heads / kv_heads)); lse: optional f32 [n_seqs, seq_len, heads], natural
  * logarithm of the sum of exp(z).  mods: NULL = plain attention.  n_seqs_dev: optional DEVICE u32, only
  * min(n_seqs, *n_seqs_dev) sequences are processed and the rows of the others stay as they were.  Takes no object:
- * runs on the CURRENT device, allocates nothing, does not synchronise.  out must not overlap an input.  A stride
+ * runs on the CURRENT device, where all arrays have to be (q elsewhere: LLMCACHE_ERR_ARG), allocates nothing, does not
+ * synchronise.  out and lse must not overlap an input.  A stride
  * must be positive where its dimension is larger than one.  The first call on a device looks up an address and sets
  * kernel attributes: make it outside any stream capture. */
 int llmcache_attention(const llmcache_rows* q, const llmcache_rows* k, const llmcache_rows* v, const llmcache_rows* out,
@@ -493,7 +494,8 @@ int llmcache_attention_debug_knobs(uint64_t wait_limit_ns, uint32_t flags);
 /* A paged key/value cache.  The caller owns the pages and hands them out; the object holds what describes them and
  * scratch for one call.  Slot j of a sequence lies in page pages[j / page_size] at place j % page_size; the page
  * arrays are bf16 [num_pages][kv_heads][page_size][64], page_stride elements from page to page.  Sequences may share
- * pages.  An object must be driven from one stream at a time (graphs captured from it included). */
+ * pages, but the place of a new row belongs to one slot of the call alone.  An object must be driven from one stream at a
+ * time (graphs captured from it included); after LLMCACHE_ERR_TIMEOUT it is to be destroyed. */
 typedef struct llmcache_kv llmcache_kv_t;
 
 typedef struct llmcache_kv_desc {
@@ -508,7 +510,9 @@ typedef struct llmcache_kv_desc {
   void*    k_pages;          /* DEVICE, 16-byte aligned, borrowed: they must outlive the object */
   void*    v_pages;
   uint64_t page_stride;      /* elements, a multiple of 64; 0 => kv_heads * page_size * 64 */
-  void*    workspace;        /* device scratch (256-byte aligned) or NULL => the library cudaMallocs it */
+  void*    workspace;        /* device scratch (256-byte aligned) or NULL => the library cudaMallocs it: 22 MB for shares of
+                                the keys, up to 64 MB of scores (4 bytes per query head and slot), 4 bytes per new row and
+                                head, 4 bytes per key/value head and slot for evictions */
   size_t   workspace_bytes;  /* llmcache_kv_bytes tells how much is needed */
 } llmcache_kv_desc;
 
@@ -526,14 +530,15 @@ typedef struct llmcache_kv_chunk {
                                 and rows that belong there are not stored */
   uint32_t pages_ld;
   float    decay;            /* weights: factor of what is there, 0 <= decay <= 1; 0 does not read it */
-  llmcache_rows q, out;      /* heads heads; seq_stride is not used */
+  llmcache_rows q, out;      /* heads heads; seq_stride is not used; out overlaps no input */
   llmcache_rows k_new, v_new;/* kv_heads heads, stored in the pages before the attention; ptr NULL (both): they are there */
   float*   lse;              /* optional f32 [n_rows, heads] */
   float*   weights;          /* optional f32 [n_seqs, kv_heads, side_ld]: slots below lens[s] become decay * weight + the
-                                sum of the softmax over this call's rows and the heads that share the key */
+                                sum of the softmax over this call's rows and the heads that share the key (the weights of
+                                the new rows' own slots count as 0 before) */
   int32_t* positions;        /* optional i32 [n_seqs, kv_heads, side_ld]: position of every slot for the distance bias
                                 (NULL: the slot); written for new rows: first[s] + row of the sequence */
-  const int32_t* first;      /* i32 [n_seqs], position of a sequence's first new row; NULL: its slot */
+  const int32_t* first;      /* i32 [n_seqs], position of a sequence's first new row, only with positions; NULL: its slot */
   uint64_t side_ld;          /* at least min(max_len, pages_ld * page_size) where weights or positions are given */
   const llmcache_score_mods* mods;   /* NULL: plain causal; doc and prefix are refused (LLMCACHE_ERR_UNSUPPORTED) */
 } llmcache_kv_chunk;
@@ -541,7 +546,8 @@ typedef struct llmcache_kv_chunk {
 /* Keeps, per sequence and key/value head, at most `budget` of the lens[s] slots: first those with a position below
  * `sinks` or among the last `recent` positions (above the head's largest position - recent), then those of the largest
  * weight (not a number and below zero count as zero), the lower slot on equal weights.  They are copied in slot order
- * to the slots 0 .. new_lens[s]-1 of new_pages, new_lens[s] = min(lens[s], budget); the old pages stay as they are. */
+ * to the slots 0 .. new_lens[s]-1 of new_pages, new_lens[s] = min(lens[s], budget); the old pages stay as they are.  A
+ * kept slot whose page id is outside [0, num_pages) becomes a row of zeros.  Outputs must not overlap inputs, new_lens apart. */
 typedef struct llmcache_kv_eviction {
   uint32_t struct_size;
   uint32_t n_seqs;

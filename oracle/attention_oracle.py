@@ -37,7 +37,8 @@ def scores(q, k, m: Mods, h: int, qpos, kpos) -> np.ndarray:
             z = z - np.float64(m.slopes[h]) * np.abs(gap)
         if m.table is not None:
             R = m.table.shape[1] // 2
-            z = z + m.table[h].astype(np.float64)[np.clip(gap, -R, R) + R]
+            entry = m.table[h].astype(np.float64)[np.clip(gap, -R, R) + R]
+            z = np.where(entry == -np.inf, -np.inf, z + entry)      # hidden, whatever the key holds
     return z
 
 

@@ -237,11 +237,12 @@ def _ptr(t) -> Optional[int]:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream) -> Optional[int]:
+def _stream(stream, device=None) -> Optional[int]:
+    """Handle of a stream; None: the current one of the current (or the given) device."""
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
-        return torch.cuda.current_stream().cuda_stream
+            return _raw_stream(torch.cuda.current_device() if device is None else device)
+        return torch.cuda.current_stream(device).cuda_stream
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -652,7 +653,8 @@ class Layer:
         _want(out, torch.bfloat16, 2, "out")
         if not (x.is_contiguous() and out.is_contiguous() and x.shape == out.shape and x.shape[1] == self.desc.d_model):
             raise LLMCacheError(ERR_SHAPE, "llmcache_layer_extend: x and out are dense [n_rows, d_model]")
-        _check(lib().llmcache_layer_extend(self.handle, cache.handle, _ptr(x), C.byref(chunk), _ptr(out), _stream(stream)),
+        _same_device(cache.device, x, out)
+        _check(lib().llmcache_layer_extend(self.handle, cache.handle, _ptr(x), C.byref(chunk), _ptr(out), _stream(stream, cache.device)),
                "llmcache_layer_extend")
 
     def status(self) -> int:
@@ -721,9 +723,16 @@ def make_score_mods(*, causal=False, scale=0.0, cap=0.0, slopes=None, table=None
     return m
 
 
-def _check_mods(mods, heads, S=0, n=0):
+def _same_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise LLMCacheError(ERR_ARG, f"a tensor on device {t.get_device()} where device {device} is expected (-1: the host)")
+
+
+def _check_mods(mods, heads, device, S=0, n=0):
     """The shapes of the modifiers' arrays (S, n: of whole sequences)."""
-    slopes, table, doc, prefix = getattr(mods, "tensors", (None, None, None, None))
+    slopes, table, doc, prefix = tensors = getattr(mods, "tensors", (None, None, None, None))
+    _same_device(device, *tensors)
     if (slopes is not None and slopes.size(0) != heads) or (table is not None and table.size(0) != heads):
         raise LLMCacheError(ERR_SHAPE, "score modifiers: one row per query head")
     if S and ((doc is not None and doc.shape != (S, n)) or (prefix is not None and prefix.shape != (S,))):
@@ -742,8 +751,10 @@ def llmcache_attention(q, k, v, out, mods: Optional[ScoreMods] = None, lse=None,
         _dense(lse, torch.float32, 3, "lse")
         if lse.shape != (S, n, H):
             raise LLMCacheError(ERR_SHAPE, "lse: [n_seqs, seq_len, heads]")
+    device = q.get_device()
+    _same_device(device, k, v, out, lse, n_seqs_dev if isinstance(n_seqs_dev, torch.Tensor) else None)
     if mods is not None:
-        _check_mods(mods, H, S, n)
+        _check_mods(mods, H, device, S, n)
     _check(lib().llmcache_attention(C.byref(rq), C.byref(rk), C.byref(rv), C.byref(ro), S, n, H, HK, _ptr(n_seqs_dev),
                                     C.byref(mods) if mods is not None else None, _ptr(lse), _stream(stream)),
            "llmcache_attention")
@@ -825,7 +836,8 @@ class KVCache:
         self.k_pages, self.v_pages, self.workspace = k_pages, v_pages, workspace
         self.desc = make_kv_desc(k_pages, v_pages, heads=heads, max_seqs=max_seqs, max_rows=max_rows, max_len=max_len,
                                  device=(k_pages.device.index or 0) if device is None else device, workspace=workspace)
-        self.heads, self.kv_heads = heads, self.desc.kv_heads
+        self.heads, self.kv_heads, self.device = heads, self.desc.kv_heads, self.desc.device
+        _same_device(self.device, k_pages, v_pages, workspace)
         self.handle = llmcache_kv_create(self.desc)
 
     def _side(self, t, dtype, seqs, name):
@@ -857,6 +869,7 @@ class KVCache:
             if first.size(0) != S:
                 raise LLMCacheError(ERR_SHAPE, "first: [n_seqs]")
             c.first = first.data_ptr()
+        _same_device(self.device, lens, cu_rows, pages, weights, positions, first)
         return c
 
     def attention(self, q, out, *, cu_rows, lens, pages, longest=0, k_new=None, v_new=None, lse=None, mods=None, weights=None,
@@ -882,9 +895,10 @@ class KVCache:
                 raise LLMCacheError(ERR_SHAPE, "lse: [n_rows, heads]")
             c.lse = lse.data_ptr()
         if mods is not None:
-            _check_mods(mods, self.heads)
+            _check_mods(mods, self.heads, self.device)
             c.mods = C.pointer(mods)
-        llmcache_kv_attention(self.handle, c, stream)
+        _same_device(self.device, q, out, k_new, v_new, lse)
+        llmcache_kv_attention(self.handle, c, _stream(stream, self.device))
 
     def evict(self, *, lens, pages, weights, new_pages, new_lens, budget, recent=0, sinks=0, positions=None, new_weights=None,
               new_positions=None, kept=None, stream=None):
@@ -914,7 +928,8 @@ class KVCache:
             if kept.shape != (S, self.kv_heads, budget):
                 raise LLMCacheError(ERR_SHAPE, "kept: [n_seqs, kv_heads, budget]")
             e.kept = kept.data_ptr()
-        llmcache_kv_evict(self.handle, e, stream)
+        _same_device(self.device, lens, new_lens, pages, new_pages, weights, positions, new_weights, new_positions, kept)
+        llmcache_kv_evict(self.handle, e, _stream(stream, self.device))
 
     def status(self) -> int:
         return llmcache_kv_status(self.handle)

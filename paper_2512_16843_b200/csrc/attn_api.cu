@@ -49,6 +49,13 @@ int write_knobs(uint32_t* status, uint64_t wait_limit_ns, uint32_t flags) {
   return LLMCACHE_OK;
 }
 
+// whether kernels on `device` can read what p points at without further ado: a tensor of another GPU, or of the host, would fault
+bool lies_on(const void* p, int device) {
+  cudaPointerAttributes at{};
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) { cudaGetLastError(); return false; }
+  return at.type == cudaMemoryTypeManaged || ((at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeHost) && at.device == device);
+}
+
 // strides of a row array; dimensions of size one need none
 int take_rows(const llmcache_rows* r, uint64_t seqs, uint64_t toks, uint64_t heads, RowsArgs* o) {
   if (!r || !r->ptr || !aligned(r->ptr, 16)) return LLMCACHE_ERR_ARG;
@@ -196,6 +203,7 @@ int chunk_args(const llmcache_kv* kv, const llmcache_kv_chunk* c, AttnArgs* o) {
   if (!c->cu_rows || !aligned(c->cu_rows, 4) || !aligned(c->lse, 4) || !aligned(c->weights, 4) || !aligned(c->positions, 4) ||
       !aligned(c->first, 4))
     return LLMCACHE_ERR_ARG;
+  if (c->first && !c->positions) return LLMCACHE_ERR_ARG;
   if (c->weights && !(c->decay >= 0.f && c->decay <= 1.f)) return LLMCACHE_ERR_ARG;
   if ((rc = take_rows(&c->q, 1, c->n_rows, D.heads, &a.q)) != LLMCACHE_OK) return rc;
   if ((rc = take_rows(&c->out, 1, c->n_rows, D.heads, &a.out)) != LLMCACHE_OK) return rc;
@@ -246,6 +254,7 @@ int llmcache_attention(const llmcache_rows* q, const llmcache_rows* k, const llm
   Dev d;
   cudaError_t e = device_setup(dev, &d);
   if (e != cudaSuccess) return done(e);
+  if (!lies_on(q->ptr, dev)) return LLMCACHE_ERR_ARG;
   a.lse = lse;
   a.heads = heads; a.kv_heads = kv_heads; a.group = heads / kv_heads;
   a.n_seqs = n_seqs; a.n_seqs_dev = n_seqs_dev; a.n = seq_len;

@@ -22,6 +22,8 @@ __device__ __forceinline__ float lg2f(float x) {
   asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// A table entry in base-2 units.  The type's lowest value, a mask in some programs, stays finite; -inf is dealt with apart.
+__device__ __forceinline__ float entry2(float b) { return fmaxf(b, -2.3e38f) * LOG2E_F; }
 __device__ __forceinline__ float max3f(float a, float b, float c) {
   float y;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));

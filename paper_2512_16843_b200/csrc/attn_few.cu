@@ -386,6 +386,10 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
         if (MOD && a.m.slopes) slope[u] = a.m.slopes[h] * LOG2E_F;
         if (MOD && a.m.table) table[u] = a.m.table + (size_t)h * (2 * a.m.reach + 1) + a.m.reach;
       }
+      const int32_t* positions = MOD && a.positions ? a.positions + ((size_t)at.s * a.kv_heads + at.hk) * a.side_ld : nullptr;
+      auto key_pos = [&](uint32_t key) -> int32_t {          // (a new row's position follows from its slot: it is being written)
+        return (int32_t)key >= at.g.slot0 ? pos0 + ((int32_t)key - at.g.slot0) : positions && key < at.g.len ? positions[key] : (int32_t)key;
+      };
       float o[8][4];
 #pragma unroll
       for (uint32_t x = 0; x < 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
@@ -446,22 +450,19 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
               }
             }
             if (a.m.slopes || a.m.table) {
-              const int32_t* positions = a.positions ? a.positions + ((size_t)at.s * a.kv_heads + at.hk) * a.side_ld : nullptr;
 #pragma unroll
               for (uint32_t n = 0; n < 4; ++n) {
 #pragma unroll
                 for (uint32_t y = 0; y < 2; ++y) {
                   const uint32_t key = k0 + n * 8 + pair + y;
-                  // (a new row's position follows from its slot: it is being written)
-                  const int32_t kpos = (int32_t)key >= at.g.slot0 ? pos0 + ((int32_t)key - at.g.slot0)
-                                       : positions ? positions[key] : (int32_t)key;
+                  const int32_t kpos = key_pos(key);
 #pragma unroll
                   for (uint32_t u = 0; u < 2; ++u) {
                     const int32_t d = kpos - qpos[u];
                     float z = fmaf(-slope[u], fabsf((float)d), c[n][u * 2 + y]);
                     if (a.m.table) {
                       const float b = __ldg(table[u] + min(max(d, -a.m.reach), a.m.reach));
-                      z += b < -1e38f ? b : b * LOG2E_F;     // the type's lowest value stays finite
+                      z = b == -INFINITY ? b : z + entry2(b);
                     }
                     c[n][u * 2 + y] = z;
                   }
@@ -551,7 +552,12 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 #pragma unroll 1
               for (uint32_t k = 0; k < 16; ++k) {
                 const uint32_t in = g * 16 + k, kr = warp * 32 + in;
-                const bool see0 = (int32_t)(k0 + in) < hi[0] && ((exist >> in) & 1u), see1 = (int32_t)(k0 + in) < hi[1] && ((exist >> in) & 1u);
+                bool see0 = (int32_t)(k0 + in) < hi[0] && ((exist >> in) & 1u), see1 = (int32_t)(k0 + in) < hi[1] && ((exist >> in) & 1u);
+                if (MOD && a.m.table) {
+                  const int32_t kpos = key_pos(k0 + in);
+                  see0 = see0 && __ldg(table[0] + min(max(kpos - qpos[0], -a.m.reach), a.m.reach)) != -INFINITY;
+                  see1 = see1 && __ldg(table[1] + min(max(kpos - qpos[1], -a.m.reach), a.m.reach)) != -INFINITY;
+                }
                 const uint8_t* vrow = gbase + FwSmem::V + s * FW_TILE + kr * 128;
 #pragma unroll
                 for (uint32_t x = 0; x < 8; ++x) {

@@ -608,8 +608,9 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         if (look_up && !by_key &&
             __all_sync(0xFFFFFFFFu, d0 >= a.m.reach || d0 + (int32_t)TC_KEYS - 1 <= -a.m.reach)) {
           const float b = __ldg(table + (d0 >= a.m.reach ? a.m.reach : -a.m.reach));
-          bias = b < -1e38f ? b : b * LOG2E_F;               // the type's lowest value stays finite
+          bias = entry2(b);
           look_up = false;
+          if (b == -INFINITY) { see = make_uint4(0u, 0u, 0u, 0u); full = false; }
         }
         float mt = -INFINITY;
         if (!MOD && full) {
@@ -694,8 +695,8 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
                 }
 #pragma unroll
                 for (uint32_t x = 0; x < 16; ++x) {
-                  z[x] = fmaf(-slope, fabsf((float)d[x]), z[x]) + bias + (b[x] < -1e38f ? b[x] : b[x] * LOG2E_F);
-                  z[x] = word & (1u << (g + x)) ? z[x] : -INFINITY;
+                  z[x] = fmaf(-slope, fabsf((float)d[x]), z[x]) + bias + entry2(b[x]);
+                  z[x] = (word & (1u << (g + x))) && b[x] != -INFINITY ? z[x] : -INFINITY;
                   u16[x] = __float_as_uint(z[x]);
                   mt = fmaxf(mt, z[x]);
                 }
@@ -786,6 +787,10 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           for (uint32_t c = 0; c < 128; ++c) {
             const uint32_t word = c < 32 ? listed[0] : c < 64 ? listed[1] : c < 96 ? listed[2] : listed[3];
             if (!((word >> (c & 31u)) & 1u)) continue;
+            if (MOD && look_up) {
+              const int32_t d = by_key ? kinfo[c] - qpos : d0 + (int32_t)c;
+              if (__ldg(table + min(max(d, -a.m.reach), a.m.reach)) == -INFINITY) continue;
+            }
             const unsigned long long* ps = reinterpret_cast<const unsigned long long*>(gbase + TcSmem::POISON) + (s * 128 + c) * 3;
 #pragma unroll 1
             for (uint32_t x = 0; x < 3; ++x) rowp[x] = (poisoned ? rowp[x] : 0ull) | ps[x];

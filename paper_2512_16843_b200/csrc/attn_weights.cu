@@ -301,9 +301,9 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
               }
 #pragma unroll
               for (uint32_t i = 0; i < 16; ++i) {
-                z[i] = fmaf(-slope[o + i], fabsf((float)(kpos - qpos[o + i])), z[i]) + (b[i] < -1e38f ? b[i] : b[i] * LOG2E_F) + lse[o + i];
+                z[i] = fmaf(-slope[o + i], fabsf((float)(kpos - qpos[o + i])), z[i]) + entry2(b[i]) + lse[o + i];
                 const float x = ex2f(z[i]);
-                s0 += (int32_t)key < hi[o + i] ? x : 0.f;
+                s0 += (int32_t)key < hi[o + i] && b[i] != -INFINITY ? x : 0.f;
               }
             }
           }

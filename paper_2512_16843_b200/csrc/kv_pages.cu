@@ -255,9 +255,10 @@ __global__ void __launch_bounds__(256) k_evict_move(const EvictArgs a) {
     if (j >= count) continue;
     const uint32_t slot = (uint32_t)kept[j];
     const int32_t p = a.pages[(size_t)s * a.pages_ld + (slot >> a.page_shift)];
-    if ((uint32_t)p >= a.num_pages) continue;             // a slot without a page has no row to move
     go[u] = true;
-    x[u] = ld_stream16(from + (size_t)p * a.page_stride + (((size_t)hk << a.page_shift) + (slot & mask)) * 64 + (part & 7u) * 8);
+    x[u] = make_uint4(0, 0, 0, 0);                        // a slot without a page has no row: zeros
+    if ((uint32_t)p < a.num_pages)
+      x[u] = ld_stream16(from + (size_t)p * a.page_stride + (((size_t)hk << a.page_shift) + (slot & mask)) * 64 + (part & 7u) * 8);
   }
 #pragma unroll
   for (uint32_t u = 0; u < U; ++u) {
