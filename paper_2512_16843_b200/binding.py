@@ -752,7 +752,8 @@ def llmcache_attention(q, k, v, out, mods: Optional[ScoreMods] = None, lse=None,
         if lse.shape != (S, n, H):
             raise LLMCacheError(ERR_SHAPE, "lse: [n_seqs, seq_len, heads]")
     device = q.get_device()
-    _same_device(device, k, v, out, lse, n_seqs_dev if isinstance(n_seqs_dev, torch.Tensor) else None)
+    if k.get_device() != device or v.get_device() != device or out.get_device() != device or lse is not None or n_seqs_dev is not None:
+        _same_device(device, k, v, out, lse, n_seqs_dev if isinstance(n_seqs_dev, torch.Tensor) else None)
     if mods is not None:
         _check_mods(mods, H, device, S, n)
     _check(lib().llmcache_attention(C.byref(rq), C.byref(rk), C.byref(rv), C.byref(ro), S, n, H, HK, _ptr(n_seqs_dev),

@@ -5,6 +5,7 @@
 #include <new>
 #include "attn.cuh"
 #include "attn_host.cuh"
+#include "ptx.cuh"
 
 using namespace llmc;
 
@@ -47,13 +48,6 @@ int write_knobs(uint32_t* status, uint64_t wait_limit_ns, uint32_t flags) {
     return LLMCACHE_ERR_CUDA;
   }
   return LLMCACHE_OK;
-}
-
-// whether kernels on `device` can read what p points at without further ado: a tensor of another GPU, or of the host, would fault
-bool lies_on(const void* p, int device) {
-  cudaPointerAttributes at{};
-  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) { cudaGetLastError(); return false; }
-  return at.type == cudaMemoryTypeManaged || ((at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeHost) && at.device == device);
 }
 
 // strides of a row array; dimensions of size one need none
@@ -254,7 +248,7 @@ int llmcache_attention(const llmcache_rows* q, const llmcache_rows* k, const llm
   Dev d;
   cudaError_t e = device_setup(dev, &d);
   if (e != cudaSuccess) return done(e);
-  if (!lies_on(q->ptr, dev)) return LLMCACHE_ERR_ARG;
+  if (!pointer_on_device(q->ptr, dev)) return LLMCACHE_ERR_ARG;      // (a tensor of another GPU, or of the host, would fault)
   a.lse = lse;
   a.heads = heads; a.kv_heads = kv_heads; a.group = heads / kv_heads;
   a.n_seqs = n_seqs; a.n_seqs_dev = n_seqs_dev; a.n = seq_len;

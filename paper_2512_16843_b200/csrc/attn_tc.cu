@@ -612,6 +612,8 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           look_up = false;
           if (b == -INFINITY) { see = make_uint4(0u, 0u, 0u, 0u); full = false; }
         }
+        // whether no score of the tile can go the straight way
+        const bool hand = MOD && (by_key || look_up || (a.m.slopes && !linear));
         float mt = -INFINITY;
         if (!MOD && full) {
 #pragma unroll 1
@@ -632,9 +634,10 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           for (uint32_t c = 0; c < 128; c += 32) {
             const uint32_t word = c == 0 ? see.x : c == 32 ? see.y : c == 64 ? see.z : see.w;
             uint32_t v[32];
+            bool by_hand = hand;
+            if (!MOD || !hand) {
             tc_ld_32x32(t_s + c, v);
             tc_wait_ld32(v);
-            bool by_hand = MOD && (by_key || look_up || (a.m.slopes && !linear));
             if constexpr (MOD) {
               const unsigned long long in2 = f2_dup(a.m.cap > 0.f ? a.m.scale / a.m.cap : sc);
               unsigned long long t[16];
@@ -663,6 +666,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
             if (!full) {
 #pragma unroll
               for (uint32_t x = 0; x < 32; ++x) v[x] = word & (1u << x) ? v[x] : __float_as_uint(-INFINITY);
+            }
             }
             if (MOD && __any_sync(0xFFFFFFFFu, by_hand)) {
               // scores beyond the polynomial, distances on both sides, positions, table entries: 16 keys at a time

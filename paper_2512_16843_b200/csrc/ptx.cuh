@@ -160,6 +160,8 @@ __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr) {
 // ---- host side: TMA tensor maps ------------------------------------------------
 // Looks up cuTensorMapEncodeTiled through the runtime (no link-time dependency on libcuda).
 cudaError_t tensor_map_setup();
+// whether p points into memory of `device` (one driver attribute: 0.1 us); false before tensor_map_setup
+bool pointer_on_device(const void* p, int device);
 // bf16 [rows, k] row-major matrix, boxes of box_rows x 64 elements, 128-byte swizzle, zero fill outside.
 bool make_tensor_map_bf16(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t k, uint32_t box_rows);
 // the same for rows that are `pitch` elements apart (pitch >= k, a multiple of 8); columns k..pitch-1 are not part

@@ -9,6 +9,8 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 static EncodeTiledFn g_encode = nullptr;
+typedef CUresult (*PointerAttributeFn)(void*, CUpointer_attribute, CUdeviceptr);
+static PointerAttributeFn g_pointer = nullptr;
 
 cudaError_t tensor_map_setup() {
   if (g_encode) return cudaSuccess;
@@ -17,8 +19,18 @@ cudaError_t tensor_map_setup() {
   cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
   if (e != cudaSuccess) return e;
   if (!fn || q != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
+  void* pointer = nullptr;
+  e = cudaGetDriverEntryPoint("cuPointerGetAttribute", &pointer, cudaEnableDefault, &q);
+  if (e != cudaSuccess) return e;
+  if (!pointer || q != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
+  g_pointer = (PointerAttributeFn)pointer;
   g_encode = (EncodeTiledFn)fn;
   return cudaSuccess;
+}
+
+bool pointer_on_device(const void* p, int device) {
+  int at = -1;
+  return g_pointer && g_pointer(&at, CU_POINTER_ATTRIBUTE_DEVICE_ORDINAL, (CUdeviceptr)p) == CUDA_SUCCESS && at == device;
 }
 
 bool make_tensor_map_bf16(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t k, uint32_t box_rows) {
