@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -195,18 +196,18 @@ def lib():
         L.llmcache_shard_decide.argtypes = [vp, vp, u32, C.c_float, u32, u32, vp, C.POINTER(ProbeIO), vp]
         L.llmcache_bank_debug_knobs.argtypes = [vp, C.c_uint64, u32]
         L.llmcache_layer_debug_knobs.argtypes = [vp, C.c_uint64, u32]
-        rp, mp = C.POINTER(Rows), C.POINTER(ScoreMods)
-        L.llmcache_attention.argtypes = [rp, rp, rp, rp, u32, u32, u32, u32, vp, mp, vp, vp]
+        # (structs of the calls that a step makes are packed into bytes: a fifth of the time of a ctypes structure)
+        L.llmcache_attention.argtypes = [vp, vp, vp, vp, u32, u32, u32, u32, vp, vp, vp, vp]
         L.llmcache_attention_status.argtypes = []
         L.llmcache_attention_debug_knobs.argtypes = [C.c_uint64, u32]
         L.llmcache_kv_bytes.argtypes = [C.POINTER(KVDesc), C.POINTER(C.c_size_t)]
         L.llmcache_kv_create.argtypes = [C.POINTER(KVDesc), C.POINTER(vp)]
         L.llmcache_kv_destroy.argtypes = [vp]
-        L.llmcache_kv_attention.argtypes = [vp, C.POINTER(KVChunk), vp]
-        L.llmcache_kv_evict.argtypes = [vp, C.POINTER(KVEviction), vp]
+        L.llmcache_kv_attention.argtypes = [vp, vp, vp]
+        L.llmcache_kv_evict.argtypes = [vp, vp, vp]
         L.llmcache_kv_status.argtypes = [vp]
         L.llmcache_kv_debug_knobs.argtypes = [vp, C.c_uint64, u32]
-        L.llmcache_layer_score_mods.argtypes = [vp, mp]
+        L.llmcache_layer_score_mods.argtypes = [vp, C.POINTER(ScoreMods)]
         L.llmcache_layer_extend.argtypes = [vp, vp, vp, C.POINTER(KVChunk), vp, vp]
         for name in EXPORTS:
             if name not in ("llmcache_abi_version", "llmcache_strerror", "llmcache_last_cuda_error",
@@ -694,14 +695,58 @@ def _dense(t, dtype, dim, name, optional=False):
 _BF16 = torch.bfloat16
 
 
-def _rows(t, name, dim) -> Rows:
-    """[seq, token, head, 64] or [token, head, 64] view of any strides."""
+def _other_device(t, device):
+    raise LLMCacheError(ERR_ARG, f"a tensor on device {t.get_device()} where device {device} is expected (-1: the host)")
+
+
+def _rows(t, name, dim, shape, device):
+    """[seq, token, head, 64] or [token, head, 64] view of any strides: (address, strides of sequence, token and head)."""
     if not isinstance(t, torch.Tensor) or t.dtype is not _BF16 or t.dim() != dim:
         raise LLMCacheError(ERR_ARG, f"{name}: a {_BF16} tensor of {dim} dimensions is expected")
-    st = t.stride()
-    if t.size(-1) != 64 or (st[-1] != 1 and t.numel()):
+    st, sh = t.stride(), t.shape
+    if sh[-1] != 64 or (st[-1] != 1 and t.numel()):
         raise LLMCacheError(ERR_SHAPE, f"{name}: the last dimension holds 64 neighbouring elements")
-    return Rows(t.data_ptr(), st[0], st[1], st[2]) if dim == 4 else Rows(t.data_ptr(), 0, st[0], st[1])
+    if shape is not None and sh != shape:
+        raise LLMCacheError(ERR_SHAPE, f"{name}: {tuple(sh)} where {tuple(shape)} is expected")
+    if t.get_device() != device:
+        _other_device(t, device)
+    return (t.data_ptr(), *st[:3]) if dim == 4 else (t.data_ptr(), 0, st[0], st[1])
+
+
+def _addr(t, dtype, shape, name, device) -> int:
+    """Address of a dense tensor of one type, shape and device; None: 0.  (A length of -1 may be anything.)"""
+    if t is None:
+        return 0
+    try:
+        if t.dtype is dtype and t.get_device() == device and t.is_contiguous():
+            have = t.shape
+            if have == shape:
+                return t.data_ptr()
+            if shape[-1] < 0 and len(have) == len(shape) and have[:-1] == shape[:-1]:
+                return t.data_ptr()
+    except AttributeError:
+        pass
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != len(shape) or not t.is_contiguous():
+        raise LLMCacheError(ERR_ARG, f"{name}: a contiguous {dtype} tensor of {len(shape)} dimensions is expected")
+    if t.get_device() != device:
+        _other_device(t, device)
+    raise LLMCacheError(ERR_SHAPE, f"{name}: {tuple(t.shape)} where {shape} is expected")
+
+
+class _Packed(struct.Struct):
+    """A C structure as bytes; numbers that do not fit their fields are refused."""
+
+    def __call__(self, *values) -> bytes:
+        try:
+            return self.pack(*values)
+        except struct.error as e:
+            raise LLMCacheError(ERR_ARG, str(e)) from None
+
+
+_ROWS = struct.Struct("@Q3q")
+_CHUNK = _Packed("@4I3QIf" + "Q3q" * 4 + "6Q")
+_EVICTION = _Packed("@7I4x6QQ2QQQ")
+_NO_ROWS = (0, 0, 0, 0)
 
 
 def make_score_mods(*, causal=False, scale=0.0, cap=0.0, slopes=None, table=None, doc=None, prefix=None) -> ScoreMods:
@@ -726,7 +771,7 @@ def make_score_mods(*, causal=False, scale=0.0, cap=0.0, slopes=None, table=None
 def _same_device(device, *tensors):
     for t in tensors:
         if t is not None and t.get_device() != device:
-            raise LLMCacheError(ERR_ARG, f"a tensor on device {t.get_device()} where device {device} is expected (-1: the host)")
+            _other_device(t, device)
 
 
 def _check_mods(mods, heads, device, S=0, n=0):
@@ -742,22 +787,22 @@ def _check_mods(mods, heads, device, S=0, n=0):
 def llmcache_attention(q, k, v, out, mods: Optional[ScoreMods] = None, lse=None, n_seqs_dev=None, stream=None) -> None:
     """out = softmax(modified q k^T) v.  q, out: bf16 [n_seqs, seq_len, heads, 64]; k, v: [n_seqs, seq_len, kv_heads, 64],
     views of any strides (multiples of 8); lse: optional f32 [n_seqs, seq_len, heads]."""
-    rq, rk, rv, ro = _rows(q, "q", 4), _rows(k, "k", 4), _rows(v, "v", 4), _rows(out, "out", 4)
-    (S, n, H, _), kv = q.shape, k.shape
-    HK = kv[2]
-    if kv[0] != S or kv[1] != n or v.shape != kv or out.shape != q.shape:
+    if not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor):
+        raise LLMCacheError(ERR_ARG, "llmcache_attention: q and k are tensors")
+    device, shape, kv = q.get_device(), q.shape, k.shape
+    rq, rk = _rows(q, "q", 4, None, device), _rows(k, "k", 4, None, device)
+    S, n, H, _ = shape
+    if kv[0] != S or kv[1] != n:
         raise LLMCacheError(ERR_SHAPE, "llmcache_attention: q, out [S, n, H, 64], k, v [S, n, HK, 64]")
-    if lse is not None:
-        _dense(lse, torch.float32, 3, "lse")
-        if lse.shape != (S, n, H):
-            raise LLMCacheError(ERR_SHAPE, "lse: [n_seqs, seq_len, heads]")
-    device = q.get_device()
-    if k.get_device() != device or v.get_device() != device or out.get_device() != device or lse is not None or n_seqs_dev is not None:
-        _same_device(device, k, v, out, lse, n_seqs_dev if isinstance(n_seqs_dev, torch.Tensor) else None)
+    rv, ro = _rows(v, "v", 4, kv, device), _rows(out, "out", 4, shape, device)
+    lse_at = _addr(lse, torch.float32, (S, n, H), "lse", device)
+    if n_seqs_dev is not None and isinstance(n_seqs_dev, torch.Tensor):
+        _same_device(device, n_seqs_dev)
     if mods is not None:
         _check_mods(mods, H, device, S, n)
-    _check(lib().llmcache_attention(C.byref(rq), C.byref(rk), C.byref(rv), C.byref(ro), S, n, H, HK, _ptr(n_seqs_dev),
-                                    C.byref(mods) if mods is not None else None, _ptr(lse), _stream(stream)),
+    pack = _ROWS.pack
+    _check(lib().llmcache_attention(pack(*rq), pack(*rk), pack(*rv), pack(*ro), S, n, H, kv[2], _ptr(n_seqs_dev),
+                                    C.addressof(mods) if mods is not None else None, lse_at or None, _stream(stream)),
            "llmcache_attention")
 
 
@@ -841,96 +886,73 @@ class KVCache:
         _same_device(self.device, k_pages, v_pages, workspace)
         self.handle = llmcache_kv_create(self.desc)
 
-    def _side(self, t, dtype, seqs, name):
-        """[n_seqs, kv_heads, ld] side array: (address, ld)."""
-        _dense(t, dtype, 3, name)
-        if t.size(0) != seqs or t.size(1) != self.kv_heads:
-            raise LLMCacheError(ERR_SHAPE, f"{name}: [n_seqs, kv_heads, slots]")
-        return t.data_ptr(), t.size(2)
+    def _pack_chunk(self, n_rows, cu_rows, lens, pages, longest, weights, decay, positions, first, q=_NO_ROWS, out=_NO_ROWS,
+                    k_new=_NO_ROWS, v_new=_NO_ROWS, lse=0, mods=None) -> bytes:
+        """A llmcache_kv_chunk."""
+        device = self.device
+        if lens is None or pages is None or cu_rows is None:
+            raise LLMCacheError(ERR_ARG, "cu_rows, lens and pages are needed")
+        lens_at = _addr(lens, torch.int32, (-1,), "lens", device)
+        S = lens.shape[0]
+        pages_at = _addr(pages, torch.int32, (S, -1), "pages", device)
+        side_ld = w_at = p_at = 0
+        if weights is not None:
+            w_at, side_ld = _addr(weights, torch.float32, (S, self.kv_heads, -1), "weights", device), weights.shape[-1]
+        if positions is not None:
+            p_at = _addr(positions, torch.int32, (S, self.kv_heads, side_ld if weights is not None else -1), "positions", device)
+            side_ld = positions.shape[-1]
+        return _CHUNK(_CHUNK_BYTES, S, n_rows, longest, _addr(cu_rows, torch.int32, (S + 1,), "cu_rows", device), lens_at, pages_at,
+                           pages.shape[1], decay if weights is not None else 0.0, *q, *out, *k_new, *v_new, lse, w_at, p_at,
+                           _addr(first, torch.int32, (S,), "first", device), side_ld, 0 if mods is None else C.addressof(mods))
 
     def chunk(self, n_rows, *, cu_rows, lens, pages, longest=0, weights=None, decay=1.0, positions=None, first=None) -> KVChunk:
         """What llmcache_kv_attention and llmcache_layer_extend take alike."""
-        _dense(lens, torch.int32, 1, "lens")
-        _dense(cu_rows, torch.int32, 1, "cu_rows")
-        _dense(pages, torch.int32, 2, "pages")
-        S = lens.size(0)
-        if cu_rows.size(0) != S + 1 or pages.size(0) != S:
-            raise LLMCacheError(ERR_SHAPE, "cu_rows: [n_seqs + 1], pages: [n_seqs, pages]")
-        c = KVChunk(_CHUNK_BYTES, S, n_rows, longest, cu_rows.data_ptr(), lens.data_ptr(), pages.data_ptr(), pages.size(1))
-        if weights is not None:
-            c.weights, c.side_ld = self._side(weights, torch.float32, S, "weights")
-            c.decay = decay
-        if positions is not None:
-            c.positions, ld = self._side(positions, torch.int32, S, "positions")
-            if weights is not None and ld != c.side_ld:
-                raise LLMCacheError(ERR_SHAPE, "weights, positions: rows of one length")
-            c.side_ld = ld
-        if first is not None:
-            _dense(first, torch.int32, 1, "first")
-            if first.size(0) != S:
-                raise LLMCacheError(ERR_SHAPE, "first: [n_seqs]")
-            c.first = first.data_ptr()
-        _same_device(self.device, lens, cu_rows, pages, weights, positions, first)
-        return c
+        return KVChunk.from_buffer_copy(self._pack_chunk(n_rows, cu_rows, lens, pages, longest, weights, decay, positions, first))
 
     def attention(self, q, out, *, cu_rows, lens, pages, longest=0, k_new=None, v_new=None, lse=None, mods=None, weights=None,
                   decay=1.0, positions=None, first=None, stream=None):
         """Stores k_new, v_new [n_rows, kv_heads, 64] in the pages and lets q [n_rows, heads, 64] attend to all that its
         sequences have there (llmcache_kv_attention).  cu_rows i32 [n_seqs + 1], lens i32 [n_seqs], pages i32
         [n_seqs, pages]; lse f32 [n_rows, heads]; weights f32 and positions i32 [n_seqs, kv_heads, slots]."""
-        c = self.chunk(q.shape[0], cu_rows=cu_rows, lens=lens, pages=pages, longest=longest, weights=weights, decay=decay,
-                       positions=positions, first=first)
-        c.q, c.out = _rows(q, "q", 3), _rows(out, "out", 3)
-        T = q.size(0)
-        if q.size(1) != self.heads or out.shape != q.shape:
+        device = self.device
+        rq = _rows(q, "q", 3, None, device)
+        T = q.shape[0]
+        ro = _rows(out, "out", 3, (T, self.heads, 64), device)
+        if q.shape[1] != self.heads:
             raise LLMCacheError(ERR_SHAPE, "q, out: [n_rows, heads, 64]")
         if (k_new is None) != (v_new is None):
             raise LLMCacheError(ERR_ARG, "k_new and v_new come together")
+        rk = rv = _NO_ROWS
         if k_new is not None:
-            c.k_new, c.v_new = _rows(k_new, "k_new", 3), _rows(v_new, "v_new", 3)
-            if k_new.size(0) != T or k_new.size(1) != self.kv_heads or v_new.shape != k_new.shape:
-                raise LLMCacheError(ERR_SHAPE, "k_new, v_new: [n_rows, kv_heads, 64]")
-        if lse is not None:
-            _dense(lse, torch.float32, 2, "lse")
-            if lse.size(0) != T or lse.size(1) != self.heads:
-                raise LLMCacheError(ERR_SHAPE, "lse: [n_rows, heads]")
-            c.lse = lse.data_ptr()
+            new = (T, self.kv_heads, 64)
+            rk, rv = _rows(k_new, "k_new", 3, new, device), _rows(v_new, "v_new", 3, new, device)
         if mods is not None:
-            _check_mods(mods, self.heads, self.device)
-            c.mods = C.pointer(mods)
-        _same_device(self.device, q, out, k_new, v_new, lse)
-        llmcache_kv_attention(self.handle, c, _stream(stream, self.device))
+            _check_mods(mods, self.heads, device)
+        c = self._pack_chunk(T, cu_rows, lens, pages, longest, weights, decay, positions, first, rq, ro, rk, rv,
+                             _addr(lse, torch.float32, (T, self.heads), "lse", device), mods)
+        _check(lib().llmcache_kv_attention(self.handle, c, _stream(stream, device)), "llmcache_kv_attention")
 
     def evict(self, *, lens, pages, weights, new_pages, new_lens, budget, recent=0, sinks=0, positions=None, new_weights=None,
               new_positions=None, kept=None, stream=None):
         """Copies the `budget` entries per sequence and head that received the most attention, the newest and the first ones
         to new_pages (llmcache_kv_evict)."""
-        _dense(lens, torch.int32, 1, "lens")
-        _dense(new_lens, torch.int32, 1, "new_lens")
-        _dense(pages, torch.int32, 2, "pages")
-        _dense(new_pages, torch.int32, 2, "new_pages")
-        S = lens.size(0)
-        if new_lens.size(0) != S or pages.size(0) != S or new_pages.size(0) != S:
-            raise LLMCacheError(ERR_SHAPE, "lens, new_lens: [n_seqs], pages, new_pages: [n_seqs, pages]")
-        e = KVEviction(C.sizeof(KVEviction), S, budget, recent, sinks, pages.size(1), new_pages.size(1), lens.data_ptr(),
-                       pages.data_ptr(), new_pages.data_ptr(), new_lens.data_ptr())
-        e.weights, e.side_ld = self._side(weights, torch.float32, S, "weights")
-        for name, t, dtype, to in (("positions", positions, torch.int32, "side_ld"), ("new_weights", new_weights, torch.float32, "new_side_ld"),
-                                   ("new_positions", new_positions, torch.int32, "new_side_ld")):
-            if t is None:
-                continue
-            addr, ld = self._side(t, dtype, S, name)
-            if getattr(e, to) not in (0, ld):
-                raise LLMCacheError(ERR_SHAPE, f"{name}: rows of another length")
-            setattr(e, name, addr)
-            setattr(e, to, ld)
-        if kept is not None:
-            _dense(kept, torch.int32, 3, "kept")
-            if kept.shape != (S, self.kv_heads, budget):
-                raise LLMCacheError(ERR_SHAPE, "kept: [n_seqs, kv_heads, budget]")
-            e.kept = kept.data_ptr()
-        _same_device(self.device, lens, new_lens, pages, new_pages, weights, positions, new_weights, new_positions, kept)
-        llmcache_kv_evict(self.handle, e, _stream(stream, self.device))
+        device, HK = self.device, self.kv_heads
+        I32, F32 = torch.int32, torch.float32
+        if lens is None or pages is None or weights is None or new_pages is None or new_lens is None:
+            raise LLMCacheError(ERR_ARG, "lens, pages, weights, new_pages and new_lens are needed")
+        lens_at = _addr(lens, I32, (-1,), "lens", device)
+        S = lens.shape[0]
+        pages_at, w_at = _addr(pages, I32, (S, -1), "pages", device), _addr(weights, F32, (S, HK, -1), "weights", device)
+        fresh_at, ld = _addr(new_pages, I32, (S, -1), "new_pages", device), weights.shape[2]
+        new_w = _addr(new_weights, F32, (S, HK, -1), "new_weights", device)
+        new_ld = -1 if new_weights is None else new_weights.shape[2]
+        new_p = _addr(new_positions, I32, (S, HK, new_ld), "new_positions", device)
+        if new_positions is not None:
+            new_ld = new_positions.shape[2]
+        e = _EVICTION(_EVICTION.size, S, budget, recent, sinks, pages.shape[1], new_pages.shape[1], lens_at, pages_at, fresh_at,
+                           _addr(new_lens, I32, (S,), "new_lens", device), w_at, _addr(positions, I32, (S, HK, ld), "positions", device),
+                           ld, new_w, new_p, max(new_ld, 0), _addr(kept, I32, (S, HK, budget), "kept", device))
+        _check(lib().llmcache_kv_evict(self.handle, e, _stream(stream, device)), "llmcache_kv_evict")
 
     def status(self) -> int:
         return llmcache_kv_status(self.handle)
