@@ -896,19 +896,29 @@ __global__ void __launch_bounds__(256) k_attn_join(const AttnArgs a, const float
     const uint32_t row = (uint32_t)(id / a.heads), h = (uint32_t)(id % a.heads);
     const SeqGeo g = seq_geo(a, seq_of_row(a, row));
     if (row < g.row0 || row - g.row0 >= g.cnt) continue;     // belongs to no sequence of the call
+    // a lane looks after every 32nd share: the maximum first, then the factors, which all lanes need
+    const float2* ml = reinterpret_cast<const float2*>(part_ml) + id;
     float m = -INFINITY;
-    for (uint32_t s = 0; s < splits; ++s) m = fmaxf(m, part_ml[((size_t)s * n_rowids + id) * 2]);
+    for (uint32_t s = lane; s < splits; s += 32) m = fmaxf(m, ml[(size_t)s * n_rowids].x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
     float l = 0.f;
     float2 o = make_float2(0.f, 0.f);
     if (m != -INFINITY) {
-      for (uint32_t s = 0; s < splits; ++s) {
-        const float2 ml = *reinterpret_cast<const float2*>(part_ml + ((size_t)s * n_rowids + id) * 2);
-        if (ml.y == 0.f) continue;                           // nothing seen in this share
-        const float c = ex2f(ml.x - m);
-        const float2 x = *reinterpret_cast<const float2*>(part_o + ((size_t)s * n_rowids + id) * 64 + lane * 2);
-        l = fmaf(ml.y, c, l);
-        o.x = fmaf(x.x, c, o.x);
-        o.y = fmaf(x.y, c, o.y);
+      for (uint32_t s0 = 0; s0 < splits; s0 += 32) {
+        float2 mine = make_float2(0.f, 0.f);
+        if (s0 + lane < splits) mine = ml[(size_t)(s0 + lane) * n_rowids];
+        const float c = mine.y == 0.f ? 0.f : ex2f(mine.x - m);      // nothing seen in this share: it takes no part
+        const uint32_t n = min(32u, splits - s0);
+#pragma unroll 4
+        for (uint32_t u = 0; u < n; ++u) {
+          const float2 x = *reinterpret_cast<const float2*>(part_o + ((size_t)(s0 + u) * n_rowids + id) * 64 + lane * 2);
+          const float f = __shfl_sync(0xFFFFFFFFu, c, u), y = __shfl_sync(0xFFFFFFFFu, mine.y, u);
+          if (y == 0.f) continue;
+          l = fmaf(y, f, l);
+          o.x = fmaf(x.x, f, o.x);
+          o.y = fmaf(x.y, f, o.y);
+        }
       }
     }
     const float inv = m == -INFINITY ? 0.f : 1.f / l;

@@ -280,7 +280,7 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             const int32_t* qpos = reinterpret_cast<const int32_t*>(gbase + WtSmem::QPOS) + s * 128;
             const int32_t* tab = reinterpret_cast<const int32_t*>(gbase + WtSmem::TAB) + s * 128;
 #pragma unroll 1
-            for (uint32_t o = c; o < c + 32; o += 16) {
+            for (uint32_t o = c; o < min(c + 32, n_rows); o += 16) {
               uint32_t u[16];
               tc_ld_16(t_s + o, u);
               float b[16], z[16];
