@@ -1,7 +1,7 @@
 // Attention on the 5th-generation tensor cores: whole sequences with score modifiers, and chunks over a paged cache.
 //
 //   S = Q K^T      tcgen05.mma 128 x 128 x 64, operands in shared memory (TMA, 128-byte swizzle), S in tensor memory
-//   P = exp2(t - m) t: score in base-2 units with its modifiers; P as bf16 over S in tensor memory
+//   P = exp2(t - m) t: score in base-2 units with its modifiers; P as bf16 in tensor memory
 //   O += P V       tcgen05.mma 128 x 64 x 128, P from tensor memory, V as it lies in memory (MN-major), O in tensor memory
 //
 // A block works on two tiles of up to 128 query rows that share the key and value tiles.  The query heads that share a
@@ -13,8 +13,18 @@
 // each, one thread per row: a pass for the maximum (which leaves modified and masked scores in tensor memory) and one for the
 // exponentials.  P has columns of its own, so S is free for the next key tile as soon as the second pass has read it, and
 // neither product holds up the other.
-// What bounds it: the exponentials (16 per cycle and SM, 1,024 cycles per query and key tile, against 256 + 256 for the
-// two products).
+// What bounds it: the exponentials could be done at 16 per cycle and SM, 1,024 cycles per query and key tile (256 + 256 for
+// the two products).  As built a pair of query tiles takes 4,700 cycles per key tile: 870 for the maximum, 2,700 for the
+// exponentials (two warps share a scheduler's special function unit, which is busy for 2,050 of them), 500 to 900 until
+// the next S is there, the rest barriers.  Measured: 32 prompts of 1,024 tokens, 12 heads, prefix of 512: 145 us (444 TFLOP/s, exponentials
+// at 39 % of their rate); 64 rows of 384 tokens in documents: 103 us (1.5 TB/s); 2 rows of 4,001 tokens, 16 heads on 4,
+// capped and biased: 209 us; 512 tokens behind 512, 32 sequences, 12 heads: 122 us (297 TFLOP/s); 250 tokens over 17,003
+// and 30,001 keys, 16 heads on 4, capped and biased: 260 us.
+// Tried and dropped (the first of these cases, 144 us at the time): maximum and exponentials in one pass over S (160; 384
+// instead of 208 with a linear bias, whose growth from key to key makes it start over), S in two halves of 64 keys so that the next one comes
+// earlier (153), a quarter of the exponentials by a polynomial on the multiply-add units (148: the time saved goes to the
+// wait for S), barriers arrived at by one lane per warp (163), rows kept in registers (195 to 285), two threads per row
+// (225), tensor memory read one chunk ahead (155), the two tiles held apart in phase (142).
 //
 // Maximum: O and the sums refer to a maximum m that is raised, and O scaled, only when a tile's maximum exceeds it by more
 // than 2^8: factors up to 2^8 lose nothing in f32 sums and in bf16 P (relative rounding), and O stays in tensor memory.
@@ -960,11 +970,13 @@ cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, in
   if (paged && part) {
     const uint64_t cap = std::min<uint64_t>(a.max_len, (uint64_t)a.pages_ld << a.page_shift), tiles = (cap + TC_KEYS - 1) / TC_KEYS;
     const uint64_t rows = (uint64_t)a.n_rows * a.heads;
-    // rows that fill one query tile: both halves of a block work on them, with the keys shared out between them
+    // rows that fill one query tile: both halves of a block work on them, with the keys shared out between them (33 rows over
+    // 640 keys, 192 items: 117 us without, 102 with)
     p.narrow = seq_rows <= p.rt && tiles >= 4 && part_units / rows >= 2;
     const uint64_t halves = p.narrow ? 2 : 1;
     // as many shares as it takes to give every SM an item (of two key tiles at least), and up to three items per SM where they
-    // stay long (16 tiles), because sequences of uneven lengths then end together
+    // stay long (16 tiles), because sequences of uneven lengths then end together (17,003 and 30,001 keys: 437 us with one
+    // item per SM, 401 with up to three)
     uint64_t sp = std::min<uint64_t>((uint64_t)sm_count / items, (tiles + 1) / 2 / halves);
     sp = std::max<uint64_t>(sp, std::min<uint64_t>(3ull * sm_count / items, tiles / 16 / halves));
     sp = std::min<uint64_t>(sp, part_units / rows / halves);

@@ -7,6 +7,8 @@
 // takes a sequence and head and every parts-th key tile of it; the query rows stream past each key tile (they come from
 // L2).  Two groups of four warps take turns with the query tiles, two blocks per SM.  Reads K once more (128 bytes per
 // key and head) and the queries; one exponential per score, as in the attention itself.
+// Measured: 250 tokens over 17,003 and 30,001 keys, 16 heads on 4, capped and biased: 135 us (147 million scores; the
+// schedulers issue in 64 % of their cycles, the capped score's multiply-adds above all).
 // f32 throughout; every wait is bounded (status word).
 #include <algorithm>
 #include "attn_dev.cuh"
@@ -370,7 +372,8 @@ cudaError_t launch_attn(const AttnArgs& a, const AttnScratch& s, int sm_count, c
 }
 
 // The weights of a call whose scores k_attn_few left: one thread per key, blocks in turn over the keys of a sequence and
-// head.  Reads 4 bytes per row and key, once (they are still in L2 as a rule).
+// head.  Reads 4 bytes per row and key, once (they are still in L2 as a rule).  9 us for 64
+// sequences of 301 to 4,100 slots, 16 heads on 4; forming those scores again took 36.
 __global__ void __launch_bounds__(256) k_weights_of_scores(const __grid_constant__ AttnArgs a, uint32_t parts) {
   griddep_sync();
   const uint32_t part = blockIdx.x % parts, hk = (blockIdx.x / parts) % a.kv_heads, sq = blockIdx.x / parts / a.kv_heads;
