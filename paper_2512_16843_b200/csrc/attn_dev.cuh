@@ -98,6 +98,14 @@ __device__ __forceinline__ unsigned long long tanh_small2(unsigned long long u) 
   q = f2_fma(q, s, f2_dup(1.0f));
   return f2_mul(u, q);
 }
+// The same on |u| <= 0.4, with two terms less (2.1e-7).
+__device__ __forceinline__ unsigned long long tanh_tiny2(unsigned long long u) {
+  const unsigned long long s = f2_mul(u, u);
+  unsigned long long q = f2_fma(f2_dup(-4.756107554e-02f), s, f2_dup(1.327115595e-01f));
+  q = f2_fma(q, s, f2_dup(-3.333137333e-01f));
+  q = f2_fma(q, s, f2_dup(9.999998808e-01f));
+  return f2_mul(u, q);
+}
 // 1 - 2 / (1 + e^2u): for |u| > 0.75, where the difference loses nothing
 __device__ __forceinline__ float tanh_large(float u) { return 1.f - __fdividef(2.f, 1.f + ex2f(2.f * LOG2E_F * u)); }
 

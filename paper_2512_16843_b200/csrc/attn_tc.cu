@@ -657,18 +657,29 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
                 float big[2] = {0.f, 0.f};
 #pragma unroll
                 for (uint32_t x = 0; x < 16; ++x) big[x & 1u] = max3f(big[x & 1u], fabsf(f2_lo(t[x])), fabsf(f2_hi(t[x])));
-                by_hand = by_hand || !(fmaxf(big[0], big[1]) <= 0.75f);
+                const float most = fmaxf(big[0], big[1]);
+                by_hand = by_hand || !(most <= 0.75f);
+                if (__all_sync(0xFFFFFFFFu, most <= 0.4f)) {
 #pragma unroll
-                for (uint32_t x = 0; x < 16; ++x) t[x] = tanh_small2(t[x]);
+                  for (uint32_t x = 0; x < 16; ++x) t[x] = tanh_tiny2(t[x]);
+                } else {
+#pragma unroll
+                  for (uint32_t x = 0; x < 16; ++x) t[x] = tanh_small2(t[x]);
+                }
               }
               const unsigned long long u2 = f2_dup(a.m.cap > 0.f ? a.m.cap * LOG2E_F : 1.f), k2 = f2_dup(rise);
-              // bias + rise * distance, two keys at a time
-              unsigned long long d2 = f2_pack((float)(d0 + (int32_t)c), (float)(d0 + (int32_t)c + 1));
-              const unsigned long long b2 = f2_dup(bias), two = f2_dup(2.f);
+              // bias + rise * distance, two keys at a time; each fourth pair anew, so that few roundings add up
+              unsigned long long d2 = f2_pack((float)(d0 + (int32_t)c), (float)(d0 + (int32_t)c + 1)), line = 0;
+              const unsigned long long b2 = f2_dup(bias), eight = f2_dup(8.f), step = f2_dup(2.f * rise);
 #pragma unroll
               for (uint32_t x = 0; x < 16; ++x) {
-                t[x] = f2_fma(t[x], u2, f2_fma(d2, k2, b2));
-                d2 = f2_add(d2, two);
+                if (x % 4 == 0) {
+                  line = f2_fma(d2, k2, b2);
+                  d2 = f2_add(d2, eight);
+                } else {
+                  line = f2_add(line, step);
+                }
+                t[x] = f2_fma(t[x], u2, line);
                 v[2 * x] = __float_as_uint(f2_lo(t[x]));
                 v[2 * x + 1] = __float_as_uint(f2_hi(t[x]));
               }

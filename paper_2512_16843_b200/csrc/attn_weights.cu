@@ -241,16 +241,28 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             if (a.m.cap > 0.f) {
               const unsigned long long in2 = f2_dup(a.m.scale / a.m.cap);
               float big[2] = {0.f, 0.f};
+              unsigned long long t[16];
+              const uint32_t left = n_rows - c;
 #pragma unroll
               for (uint32_t i = 0; i < 16; ++i) {
-                const unsigned long long t = f2_mul(f2_pack(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), in2);
+                t[i] = f2_mul(f2_pack(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), in2);
                 // (columns behind the last row hold whatever was there before)
-                if (c + 2 * i < n_rows) big[i & 1u] = max3f(big[i & 1u], fabsf(f2_lo(t)), c + 2 * i + 1 < n_rows ? fabsf(f2_hi(t)) : 0.f);
-                const unsigned long long y = tanh_small2(t);
-                v[2 * i] = __float_as_uint(f2_lo(y));
-                v[2 * i + 1] = __float_as_uint(f2_hi(y));
+                big[i & 1u] = max3f(big[i & 1u], 2 * i < left ? fabsf(f2_lo(t[i])) : 0.f, 2 * i + 1 < left ? fabsf(f2_hi(t[i])) : 0.f);
               }
-              by_hand = by_hand || !(fmaxf(big[0], big[1]) <= 0.75f);
+              const float most = fmaxf(big[0], big[1]);
+              by_hand = by_hand || !(most <= 0.75f);
+              if (__all_sync(0xFFFFFFFFu, most <= 0.4f)) {
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) t[i] = tanh_tiny2(t[i]);
+              } else {
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) t[i] = tanh_small2(t[i]);
+              }
+#pragma unroll
+              for (uint32_t i = 0; i < 16; ++i) {
+                v[2 * i] = __float_as_uint(f2_lo(t[i]));
+                v[2 * i + 1] = __float_as_uint(f2_hi(t[i]));
+              }
             }
           }
           if (!MOD || !__any_sync(0xFFFFFFFFu, by_hand)) {

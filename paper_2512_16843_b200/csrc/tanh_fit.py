@@ -1,17 +1,17 @@
-"""Coefficients of the odd polynomial that stands for tanh on |u| <= 0.75 in the attention kernel (attn_tc.cu).
+"""Coefficients of the odd polynomials that stand for tanh on |u| <= 0.4 and |u| <= 0.75 in the attention kernels (attn_dev.cuh).
 
-tanh(u) = u P(u^2): P of degree 5 fitted to tanh(sqrt s) / sqrt s on s in [0, 0.5625] at Chebyshev nodes (within a factor of
-two of the best uniform fit; the nearest singularity, u = i pi / 2, lies far enough away for an error that falls by a
-factor of about 20 per coefficient).  Prints the f32 coefficients, lowest first, and the largest relative error of the
-f32 evaluation (Horner, fused multiply-add): 1.4e-7.
+tanh(u) = u P(u^2): P of degree 3 or 5 fitted to tanh(sqrt s) / sqrt s on s in [0, limit^2] at Chebyshev nodes (within a
+factor of two of the best uniform fit; the nearest singularity, u = i pi / 2, lies far enough away for an error that falls by a
+factor of about 20 per coefficient on the longer range, 60 on the shorter).  Prints the f32 coefficients, lowest first, and the
+largest relative error of the f32 evaluation (Horner, fused multiply-add): 2.1e-7 and 1.4e-7.
 """
 import numpy as np
 from numpy.polynomial import chebyshev as Ch
 
-LIMIT, DEGREE = 0.75, 5
+RANGES = ((0.4, 3), (0.75, 5))
 
 
-def fit():
+def fit(LIMIT, DEGREE):
     n = 4000
     s = (np.cos((np.arange(n) + 0.5) * np.pi / n) + 1) / 2 * LIMIT * LIMIT
     u = np.sqrt(s)
@@ -19,7 +19,7 @@ def fit():
     return Ch.Chebyshev(c, domain=[0, LIMIT * LIMIT]).convert(kind=np.polynomial.Polynomial).coef.astype(np.float32)
 
 
-def error(p):
+def error(p, LIMIT, DEGREE):
     u = np.linspace(1e-4, LIMIT, 200001).astype(np.float32)
     s = u * u
     a = np.full_like(u, p[-1])
@@ -30,5 +30,6 @@ def error(p):
 
 
 if __name__ == "__main__":
-    p = fit()
-    print(["%.9ef" % x for x in p], error(p))
+    for r in RANGES:
+        p = fit(*r)
+        print(r, ["%.9ef" % x for x in p], error(p, *r))
