@@ -16,10 +16,12 @@
 // What bounds it: the exponentials could be done at 16 per cycle and SM, 1,024 cycles per query and key tile (256 + 256 for
 // the two products).  As built a pair of query tiles takes 4,700 cycles per key tile: 870 for the maximum, 2,700 for the
 // exponentials (two warps share a scheduler's special function unit, which is busy for 2,050 of them), 500 to 900 until
-// the next S is there, the rest barriers.  Measured: 32 prompts of 1,024 tokens, 12 heads, prefix of 512: 145 us (444 TFLOP/s, exponentials
-// at 39 % of their rate); 64 rows of 384 tokens in documents: 103 us (1.5 TB/s); 2 rows of 4,001 tokens, 16 heads on 4,
-// capped and biased: 209 us; 512 tokens behind 512, 32 sequences, 12 heads: 122 us (297 TFLOP/s); 250 tokens over 17,003
-// and 30,001 keys, 16 heads on 4, capped and biased: 260 us.
+// the next S is there, the rest barriers.  Measured: 32 prompts of 1,024 tokens, 12 heads, prefix of 512: 139 us (463 TFLOP/s, exponentials
+// at 40 % of their rate); 64 rows of 384 tokens in documents: 101 us (1.5 TB/s); 2 rows of 4,001 tokens, 16 heads on 4,
+// capped and biased: 196 us; 512 tokens behind 512, 32 sequences, 12 heads: 119 us with the new rows stored; 250 tokens over
+// 17,003 and 30,001 keys, 16 heads on 4, capped and biased: 357 us with the weights (135), the join and the new rows (16).
+// Work is handed out by the hardware (cluster launch control): a block for every item is launched, those that run cancel the
+// others one by one and do their items.  With item i, i + 148, .. for a block instead the cases took 103, 144, 201, 132 and 389.
 // Tried and dropped (the first of these cases, 144 us at the time): maximum and exponentials in one pass over S (160; 384
 // instead of 208 with a linear bias, whose growth from key to key makes it start over), S in two halves of 64 keys so that the next one comes
 // earlier (153), a quarter of the exponentials by a polynomial on the multiply-add units (148: the time saved goes to the
@@ -67,9 +69,11 @@ struct TcSmem {
   static constexpr uint32_t ITEM = INFO + TC_ST * 8 + 8;         // ItemInfo [2]
   static constexpr uint32_t MAIL = ITEM + 128;               // u32 [query tile][2]: number of the key tile in the block's stream (~0: the item's end), key tile
   static constexpr uint32_t BAR = MAIL + 32;
-  static constexpr uint32_t MISC = BAR + 40 * 8;
+  static constexpr uint32_t MISC = BAR + 40 * 8;             // [2] words of the block, then the answer to a request for work
+  static constexpr uint32_t NEXT = MISC + 32;
   static constexpr uint32_t TOTAL = MISC + 64;
 };
+static_assert(TcSmem::NEXT % 16 == 0, "an answer of 16 bytes");
 constexpr uint32_t TC_SMEM = TcSmem::TOTAL + 1024;
 static_assert(TC_SMEM <= 232448, "shared memory of one block");
 // kind::f16, f32 accumulator, bf16 operands, M = 128; PV: B is MN-major (bit 16)
@@ -94,6 +98,25 @@ __device__ __forceinline__ void tc_st_16(uint32_t taddr, const uint32_t* v) {
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // bits 0 .. n - 1
 __device__ __forceinline__ uint32_t below(int32_t n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// Asks for a block of the grid that has not started: its number arrives at `to` (16 bytes, counted on the barrier).
+__device__ __forceinline__ void ask_for_work(uint32_t to, uint32_t bar) {
+  mbar_expect_tx(bar, 16);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(to), "r"(bar) : "memory");
+}
+// The answer: the block's number, or `none` when all have started (nothing may be asked after that).
+__device__ __forceinline__ uint32_t work_answer(uint32_t at, uint32_t none) {
+  uint32_t x;
+  asm volatile(
+      "{\n\t.reg .b128 h;\n\t.reg .pred p;\n\t"
+      "ld.shared.b128 h, [%1];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n\t"
+      "mov.u32 %0, %2;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, h;\n\t"
+      "fence.proxy.async.shared::cta;\n\t}"                 // (the next answer may come to the same place)
+      : "=r"(x) : "r"(at), "r"(none) : "memory");
+  return x;
+}
 
 // Launch shape, the same for every role.
 struct TcPlan {
@@ -180,6 +203,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   auto pv_done = [&](uint32_t w) { return bar1 + 8 * (8 + w); };
   auto s_free = [&](uint32_t w) { return bar1 + 8 * (10 + w); };
   auto drain = [&](uint32_t w) { return bar1 + 8 * (12 + w); };
+  const uint32_t asked = bar1 + 8 * 14;
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(gbase + TcSmem::MISC);
   volatile uint32_t* abort_flag = misc + 1;
   volatile ItemInfo* items = reinterpret_cast<volatile ItemInfo*>(gbase + TcSmem::ITEM);
@@ -195,6 +219,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       mbar_init(q_full(b), 1); mbar_init(q_empty(b), 2 + 1 + 8); mbar_init(s_full(b), 2); mbar_init(p_full(b), 128);
       mbar_init(pv_done(b), 1); mbar_init(s_free(b), 128); mbar_init(drain(b), 1);
     }
+    mbar_init(asked, 1);
     misc[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -218,9 +243,21 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   if (warp == 0) {
     // ---------------------------------------------------------------- loads
     bool ok = true;
-    uint32_t e = 0, qc = 0;
+    // The grid has a block for every item; those that fit the GPU run, and take over the others' items one by one before they
+    // start.  The next one is asked for before the work on one begins.
+    uint32_t e = 0, qc = 0, n_asked = 0, n_answers = 0;
+    const uint32_t sNext = base + TcSmem::NEXT;
+    auto next_item = [&]() -> uint32_t {
+      ok = warp_wait(asked, (n_asked - 1) & 1u, abort_flag, lim, 64);
+      uint32_t x = p.n_items;
+      if (ok && lane == 0) x = work_answer(sNext, p.n_items);
+      n_answers += ok ? 1u : 0u;
+      return __shfl_sync(0xFFFFFFFFu, x, 0);
+    };
 #pragma unroll 1
-    for (uint32_t i = producer_idle(a.status) ? p.n_items : blockIdx.x; i < p.n_items && ok; i += gridDim.x) {
+    for (uint32_t i = producer_idle(a.status) ? p.n_items : blockIdx.x; i < p.n_items; i = next_item()) {
+      if (lane == 0) ask_for_work(sNext, asked);
+      ++n_asked;
       const TcItem it = tc_item(a, p, i, n_seqs);
       if (!it.live) continue;
       const uint32_t b = qc & 1u;
@@ -326,6 +363,7 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         j = jc;
         f = fc;
       }
+      if (!ok) break;
     }
     if (ok && !producer_idle(a.status)) {
       ok = warp_wait(q_empty(qc & 1u), ((qc >> 1) & 1u) ^ 1u, abort_flag, lim, 64);
@@ -346,6 +384,13 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         const uint32_t x = e - 1 - b;
         wait_long(k_full(x % TC_ST), (x / TC_ST) & 1u, &never, 200000000ull, 0);
         wait_long(v_full(x % TC_ST), (x / TC_ST) & 1u, &never, 200000000ull, 0);
+      }
+      // and an answer on its way; the items that nobody has begun are taken and left, so that the grid ends
+      bool more = n_asked > n_answers;
+#pragma unroll 1
+      while (more && wait_long(asked, (n_asked - 1) & 1u, &never, 200000000ull, 0)) {
+        more = work_answer(sNext, p.n_items) < p.n_items;
+        if (more) { ask_for_work(sNext, asked); ++n_asked; }
       }
     }
   } else if (warp < 3) {
@@ -987,7 +1032,7 @@ cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, in
     const uint64_t halves = p.narrow ? 2 : 1;
     // as many shares as it takes to give every SM an item (of two key tiles at least), and up to three items per SM where they
     // stay long (16 tiles), because sequences of uneven lengths then end together (17,003 and 30,001 keys: 437 us with one
-    // item per SM, 401 with up to three)
+    // item per SM, 401 with up to three, in an earlier form; two to eight make no difference any more)
     uint64_t sp = std::min<uint64_t>((uint64_t)sm_count / items, (tiles + 1) / 2 / halves);
     sp = std::max<uint64_t>(sp, std::min<uint64_t>(3ull * sm_count / items, tiles / 16 / halves));
     sp = std::min<uint64_t>(sp, part_units / rows / halves);
@@ -1013,9 +1058,8 @@ cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, in
         !make_tensor_map_rows(&map_v, a.v, a.kv_heads, a.n, a.n_seqs, 1, TC_KEYS))
       return cudaErrorInvalidValue;
   }
-  const uint32_t grid = p.n_items < (uint32_t)sm_count ? p.n_items : (uint32_t)sm_count;
   const bool mod = a.m.cap > 0.f || a.m.slopes || a.m.table;
-  cudaError_t e = launch_k(tc_kernel(paged, a.m.doc != nullptr, mod), dim3(grid), dim3(TC_THREADS), TC_SMEM, st, map_q, map_k, map_v, a, p);
+  cudaError_t e = launch_k(tc_kernel(paged, a.m.doc != nullptr, mod), dim3(p.n_items), dim3(TC_THREADS), TC_SMEM, st, map_q, map_k, map_v, a, p);
   if (e != cudaSuccess || p.shares == 1) return e;
   const uint64_t warps = (uint64_t)a.n_rows * a.heads;
   const uint64_t blocks = std::min<uint64_t>((warps + 7) / 8, (uint64_t)sm_count * 8);
