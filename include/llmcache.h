@@ -523,7 +523,8 @@ typedef struct llmcache_kv_chunk {
   uint32_t struct_size;
   uint32_t n_seqs;
   uint32_t n_rows;           /* rows of q, out, lse */
-  uint32_t longest;          /* most rows of one sequence (rows beyond it are not computed); 0 => n_rows */
+  uint32_t longest;          /* most rows of one sequence; 0 => n_rows.  A sequence's rows beyond it are stored (keys, values,
+                                positions), but not computed: out and lse stay as they were there, and they add no weight */
   const int32_t* cu_rows;    /* i32 [n_seqs + 1], ascending from 0 to at most n_rows */
   const int32_t* lens;       /* i32 [n_seqs], at most max_len and pages_ld * page_size (more is taken as that) */
   const int32_t* pages;      /* i32 [n_seqs, pages_ld]; an id outside [0, num_pages): its slots are seen by nobody
@@ -586,7 +587,8 @@ int llmcache_layer_score_mods(llmcache_layer_t* layer, const llmcache_score_mods
 /* The layer on new tokens only: out[r] = f_l(x[r]) for the rows of `chunk` (x, out: bf16 [n_rows, d], not overlapping),
  * whose keys and values are stored in kv and which attend to everything their sequences have there.  For causal layers;
  * kv must have the layer's heads as heads and kv_heads.  chunk->q, k_new, v_new, out and mods are not looked at (the
- * layer's own take their place; doc and prefix are refused); n_rows <= max_seqs * seq_len of the layer. */
+ * layer's own take their place; doc and prefix are refused); n_rows <= max_seqs * seq_len of the layer.  For rows beyond
+ * `longest`, out is what the layer gives with zeros for the attention. */
 int llmcache_layer_extend(llmcache_layer_t* layer, llmcache_kv_t* kv, const void* x, const llmcache_kv_chunk* chunk,
                           void* out, void* stream);
 

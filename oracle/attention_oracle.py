@@ -104,9 +104,10 @@ class Cache:
         return (p, slot % ps) if 0 <= p < self.k.shape[0] else (None, None)
 
 
-def chunk(c: Cache, q, m: Mods, cu, lens, pages, k_new=None, v_new=None, weights=None, decay=1.0, positions=None, first=None):
+def chunk(c: Cache, q, m: Mods, cu, lens, pages, k_new=None, v_new=None, weights=None, decay=1.0, positions=None, first=None,
+          longest=None):
     """New rows of a batch over the paged cache; writes c, weights and positions.  q [T, H, dh] -> out, lse, spread, written:
-    rows that belong to a sequence."""
+    rows that belong to a sequence and are computed (the first `longest` of it)."""
     T, H, dh = q.shape
     HK, ps = c.k.shape[1], c.k.shape[2]
     G = H // HK
@@ -127,10 +128,11 @@ def chunk(c: Cache, q, m: Mods, cu, lens, pages, k_new=None, v_new=None, weights
                 p, at = c.place(pages[s], slot)
                 if p is not None:
                     c.k[p, :, at], c.v[p, :, at] = k_new[r], v_new[r]
+        new, r1 = r1 - r0, r1 if longest is None else min(r1, r0 + longest)
         written[r0:r1] = True
         there = np.array([c.place(pages[s], j)[0] is not None for j in range(n)], dtype=bool)
         slots = np.arange(n)
-        mine = n - (r1 - r0) + np.arange(r1 - r0)
+        mine = n - new + np.arange(r1 - r0)
         see = np.broadcast_to(there[None, :], (r1 - r0, n)).copy()
         if m.causal:
             see &= slots[None, :] <= mine[:, None]

@@ -43,11 +43,14 @@ struct AttnArgs {
   // few rows whose weights are asked for: modified scores (base 2, -inf: not seen) [n_seqs, kv_heads, row][score_ld], or null
   float* scores;
   uint32_t score_ld, score_rows;
+  // rows of a sequence beyond the n that are computed get zeros in out (they are left as they were otherwise)
+  uint32_t zero_rest;
 };
 
-// A sequence of a paged call: its rows row0 .. row0 + cnt - 1 take the slots slot0 .. of len slots.  Whatever the
-// arrays hold, rows stay inside [0, n_rows) and slots inside the page table.
-struct SeqGeo { uint32_t row0, cnt, len; int32_t slot0; };
+// A sequence of a paged call: its rows row0 .. row0 + all - 1 take the slots slot0 .. of len slots; the first cnt of them
+// are computed, the others stored only.  Whatever the arrays hold, rows stay inside [0, n_rows) and slots inside the page
+// table.
+struct SeqGeo { uint32_t row0, cnt, len; int32_t slot0; uint32_t all; };
 __device__ __forceinline__ SeqGeo seq_geo(const AttnArgs& a, uint32_t s) {
   SeqGeo g;
   const int32_t c0 = a.cu[s], c1 = a.cu[s + 1], len = a.lens[s];
@@ -55,9 +58,9 @@ __device__ __forceinline__ SeqGeo seq_geo(const AttnArgs& a, uint32_t s) {
   g.len = len > 0 ? min((uint32_t)len, cap) : 0u;
   const bool sane = c0 >= 0 && c1 >= c0 && (uint32_t)c1 <= a.n_rows;
   g.row0 = sane ? (uint32_t)c0 : 0u;
-  const uint32_t cnt = sane ? (uint32_t)(c1 - c0) : 0u;
-  g.slot0 = (int32_t)g.len - (int32_t)cnt;
-  g.cnt = min(cnt, a.n);
+  g.all = sane ? (uint32_t)(c1 - c0) : 0u;
+  g.slot0 = (int32_t)g.len - (int32_t)g.all;
+  g.cnt = min(g.all, a.n);
   return g;
 }
 // page of a slot, or -1 where the table has none

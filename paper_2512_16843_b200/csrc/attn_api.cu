@@ -225,6 +225,31 @@ int kv_check_chunk(const llmcache_kv* kv, const llmcache_kv_chunk* c) {
   AttnArgs a{};
   return chunk_args(kv, c, &a);
 }
+
+int kv_attend(llmcache_kv* kv, const llmcache_kv_chunk* c, bool zero_rest, cudaStream_t st) {
+  AttnArgs a{};
+  int rc = chunk_args(kv, c, &a);
+  if (rc != LLMCACHE_OK || a.n_seqs == 0) return rc;
+  a.zero_rest = zero_rest && a.n < a.n_rows;
+  if (a.weights && attn_is_few(a)) {
+    const uint64_t cap = std::min<uint64_t>(a.max_len, (uint64_t)a.pages_ld << a.page_shift), ld = (cap + 127) / 128 * 128;
+    const uint64_t rows = (uint64_t)a.n * a.group;
+    if ((uint64_t)a.n_seqs * a.kv_heads * rows * ld <= kv->score_floats) {
+      a.scores = kv->scores;
+      a.score_ld = (uint32_t)ld;
+      a.score_rows = (uint32_t)rows;
+    }
+  }
+  OnDevice on(kv->desc.device);
+  if (!on.ok) return LLMCACHE_ERR_CUDA;
+  if (!attn_is_few(a) && (a.k.ptr || a.positions || (a.weights && a.decay != 0.f))) {
+    const cudaError_t e = launch_kv_append(a, kv->sm_count, st);
+    if (e != cudaSuccess) return done(e);
+  }
+  rc = launch_attn_checked(a, AttnScratch{kv->part, KV_PART_UNITS, kv->arrived}, kv->sm_count, st);
+  if (rc == LLMCACHE_OK && a.weights) rc = done(launch_attn_weights(a, kv->sm_count, st));
+  return rc;
+}
 }  // namespace llmc
 
 extern "C" {
@@ -346,28 +371,7 @@ int llmcache_kv_destroy(llmcache_kv_t* kv) {
 }
 
 int llmcache_kv_attention(llmcache_kv_t* kv, const llmcache_kv_chunk* c, void* stream) {
-  AttnArgs a{};
-  int rc = chunk_args(kv, c, &a);
-  if (rc != LLMCACHE_OK || a.n_seqs == 0) return rc;
-  if (a.weights && attn_is_few(a)) {
-    const uint64_t cap = std::min<uint64_t>(a.max_len, (uint64_t)a.pages_ld << a.page_shift), ld = (cap + 127) / 128 * 128;
-    const uint64_t rows = (uint64_t)a.n * a.group;
-    if ((uint64_t)a.n_seqs * a.kv_heads * rows * ld <= kv->score_floats) {
-      a.scores = kv->scores;
-      a.score_ld = (uint32_t)ld;
-      a.score_rows = (uint32_t)rows;
-    }
-  }
-  OnDevice on(kv->desc.device);
-  if (!on.ok) return LLMCACHE_ERR_CUDA;
-  cudaStream_t st = (cudaStream_t)stream;
-  if (!attn_is_few(a) && (a.k.ptr || a.positions || (a.weights && a.decay != 0.f))) {
-    const cudaError_t e = launch_kv_append(a, kv->sm_count, st);
-    if (e != cudaSuccess) return done(e);
-  }
-  rc = launch_attn_checked(a, AttnScratch{kv->part, KV_PART_UNITS, kv->arrived}, kv->sm_count, st);
-  if (rc == LLMCACHE_OK && a.weights) rc = done(launch_attn_weights(a, kv->sm_count, st));
-  return rc;
+  return kv_attend(kv, c, false, (cudaStream_t)stream);
 }
 
 int llmcache_kv_evict(llmcache_kv_t* kv, const llmcache_kv_eviction* v, void* stream) {

@@ -157,6 +157,15 @@ __device__ __noinline__ void store_new(const AttnArgs& a, const FwPlace& at, uin
     if (pg >= 0) *reinterpret_cast<uint4*>((part < 8 ? a.k_pages : a.v_pages) + page_row(a, pg, at.hk, slot) + (part & 7u) * 8) = v;
   }
 }
+// Zeros for the rows that are not computed, in the heads of one key/value head (one warp).
+__device__ __noinline__ void zero_rest(const AttnArgs& a, const FwPlace& at) {
+  const unsigned long long pieces = (unsigned long long)(at.g.all - at.g.cnt) * a.group * 8;
+#pragma unroll 1
+  for (unsigned long long i = threadIdx.x & 31; i < pieces; i += 32) {
+    const uint32_t R = (uint32_t)(i >> 3), token = at.g.cnt + R / a.group, h = at.hk * a.group + R % a.group;
+    *reinterpret_cast<uint4*>(a.out.ptr + (long long)(at.g.row0 + token) * a.out.tok + (long long)h * a.out.head + (i & 7u) * 8) = make_uint4(0, 0, 0, 0);
+  }
+}
 __device__ __noinline__ void next_place(const AttnArgs& a, FwPlace& p) {
   p.first += p.nt;
   if (++p.hk < a.kv_heads) return;
@@ -294,10 +303,11 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
       if (lane == 0) mbar_arrive(seg_empty(n & 1u));
       if (fresh) {
         const uint32_t from = (uint32_t)max(at.g.slot0, (int32_t)(seg.j0 * FW_KEYS));
-        const uint32_t to = min(min(at.g.len, seg.j1 * FW_KEYS), (uint32_t)max(0, at.g.slot0 + (int32_t)at.g.cnt));
+        const uint32_t to = min(min(at.g.len, seg.j1 * FW_KEYS), (uint32_t)max(0, at.g.slot0 + (int32_t)at.g.all));
         if (from < to) store_new(a, at, from, to);
         __syncwarp();
       }
+      if (a.zero_rest && seg.j0 == 0) zero_rest(a, at);
       if (seg.j0 == 0 && seg.j1 == at.nt) continue;
       ok = warp_wait(share_out(seg.j0 == 0 ? 1u : 0u), 0u, abort_flag, lim, 64);
       if (!ok) break;
@@ -364,7 +374,7 @@ k_attn_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
       const FwPlace& at = seg.at;
       if (!at.nt) break;
       const uint32_t j0 = seg.j0, j1 = seg.j1, rows = at.g.cnt * a.group;
-      const uint32_t new_end = min(at.g.len, (uint32_t)max(0, at.g.slot0 + (int32_t)at.g.cnt));      // behind the last new row's slot
+      const uint32_t new_end = min(at.g.len, (uint32_t)max(0, at.g.slot0 + (int32_t)at.g.all));      // behind the last new row's slot
       const int32_t pos0 = seg.pos0;
       uint32_t qf[4][4];
 #pragma unroll

@@ -26,6 +26,8 @@ int kv_fits_layer(const llmcache_kv* kv, int device, uint32_t heads);
 
 // the checks of llmcache_kv_attention alone
 int kv_check_chunk(const llmcache_kv* kv, const llmcache_kv_chunk* c);
+// llmcache_kv_attention; zero_rest: zeros in the rows of out that `longest` leaves out
+int kv_attend(llmcache_kv* kv, const llmcache_kv_chunk* c, bool zero_rest, cudaStream_t st);
 
 // launch_attn behind the check of its grid
 inline int launch_attn_checked(const AttnArgs& a, const AttnScratch& s, int sm_count, cudaStream_t st) {

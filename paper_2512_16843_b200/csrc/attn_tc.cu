@@ -152,7 +152,7 @@ __device__ __forceinline__ TcItem tc_item(const AttnArgs& a, const TcPlan& p, ui
   it.s = i % a.n_seqs; i /= a.n_seqs;
   const uint32_t qt = p.qtiles - 1 - i;                      // the tiles with the most keys (causal) first
   it.r0 = qt * 2 * p.rt;
-  it.g = SeqGeo{0, a.n, a.n, 0};
+  it.g = SeqGeo{0, a.n, a.n, 0, a.n};
   if (it.s < n_seqs && a.pages) it.g = seq_geo(a, it.s);
   it.pre = a.m.prefix && it.s < n_seqs ? a.m.prefix[it.s] : 0;
   it.rows = it.g.cnt * a.group;

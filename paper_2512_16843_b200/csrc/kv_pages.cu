@@ -28,7 +28,12 @@ __global__ void __launch_bounds__(256) k_kv_append(const AttnArgs a, uint32_t he
     }
     const uint32_t s = seq_of_row(a, row);
     const SeqGeo g = seq_geo(a, s);
-    if (row < g.row0 || row - g.row0 >= g.cnt) continue;             // behind the last sequence
+    if (row < g.row0 || row - g.row0 >= g.all) continue;             // behind the last sequence
+    if (a.zero_rest && row - g.row0 >= g.cnt) {                      // stored, but not computed
+      const uint32_t heads = min(AP_HEADS, a.kv_heads - h0) * a.group;
+      for (uint32_t i = lane; i < heads * 8; i += 32)
+        *reinterpret_cast<uint4*>(a.out.ptr + (long long)row * a.out.tok + (long long)(h0 * a.group + (i >> 3)) * a.out.head + (i & 7u) * 8) = make_uint4(0, 0, 0, 0);
+    }
     const long long slot = (long long)g.slot0 + (row - g.row0);
     if (slot < 0) continue;
     if (lane < AP_HEADS && h0 + lane < a.kv_heads) {

@@ -251,7 +251,7 @@ int llmcache_layer_extend(llmcache_layer_t* L, llmcache_kv_t* kv, const void* x,
   };
   if (D.pre_ln) ln(X, D.ln1_g, D.ln1_b, L->y);
   gemm(D.pre_ln ? L->y : X, D.w_qkv, D.b_qkv, nullptr, L->qkv, 3 * d, d, LAYER_ACT_NONE);
-  if (e == cudaSuccess) rc = llmcache_kv_attention(kv, &c, stream);
+  if (e == cudaSuccess) rc = kv_attend(kv, &c, true, st);
   if (rc == LLMCACHE_OK) {
     gemm(L->a, D.w_o, D.b_o, X, L->t, d, d, LAYER_ACT_NONE);
     ln(L->t, D.pre_ln ? D.ln2_g : D.ln1_g, D.pre_ln ? D.ln2_b : D.ln1_b, L->y);
