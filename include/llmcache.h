@@ -460,6 +460,8 @@ typedef struct llmcache_score_mods {
   float    scale;            /* 0 => 1/8 = 1/sqrt(64); must not be negative */
   float    cap;              /* 0 => scores are not capped; at least 1e-3 otherwise */
   uint32_t reach;            /* table: largest distance with an entry of its own, <= 1,024 */
+  uint32_t mask_seqs;        /* sequences that doc and prefix have entries for: a call with more is refused
+                                (LLMCACHE_ERR_SHAPE); 0 => not checked */
   const float*   slopes;     /* f32 [heads], or NULL */
   const float*   table;      /* f32 [heads, 2 * reach + 1], or NULL; an entry of -inf hides the key like a mask */
   const int32_t* doc;        /* i32 [n_seqs, seq_len] document of every token, < 0: padding; or NULL */
@@ -579,7 +581,8 @@ int llmcache_kv_status(llmcache_kv_t* kv);
 int llmcache_kv_debug_knobs(llmcache_kv_t* kv, uint64_t wait_limit_ns, uint32_t flags);
 
 /* Score modifiers of the layer's attention in the forward calls that follow; NULL switches them off.  The struct is
- * copied, the arrays it points at are borrowed.  causal must equal the layer's.  doc and prefix are indexed by the
+ * copied, the arrays it points at are borrowed and have to be on the layer's device (LLMCACHE_ERR_ARG).  causal must equal
+ * the layer's.  doc and prefix are indexed by the
  * sequence's place in the forward call; a layer that has them is refused (LLMCACHE_ERR_UNSUPPORTED) by llmcache_infer
  * with banks and by llmcache_divergence_check, where sequences change their places and a match does not look at masks. */
 int llmcache_layer_score_mods(llmcache_layer_t* layer, const llmcache_score_mods* mods);

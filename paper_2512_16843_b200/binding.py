@@ -86,7 +86,7 @@ class LayerDesc(C.Structure):
 class ScoreMods(C.Structure):
     _fields_ = [
         ("struct_size", C.c_uint32), ("causal", C.c_uint32), ("scale", C.c_float), ("cap", C.c_float),
-        ("reach", C.c_uint32), ("slopes", C.c_void_p), ("table", C.c_void_p), ("doc", C.c_void_p), ("prefix", C.c_void_p),
+        ("reach", C.c_uint32), ("mask_seqs", C.c_uint32), ("slopes", C.c_void_p), ("table", C.c_void_p), ("doc", C.c_void_p), ("prefix", C.c_void_p),
     ]
 
 
@@ -641,7 +641,10 @@ class Layer:
         llmcache_layer_forward(self.handle, x, x.shape[0] if n_seqs is None else n_seqs, n_seqs_dev, out, stream)
 
     def score_mods(self, mods: Optional[ScoreMods]):
-        """Score modifiers (make_score_mods) of the forward and extend calls that follow; None switches them off."""
+        """Score modifiers (make_score_mods) of the forward and extend calls that follow; None switches them off.  doc is
+        [n_seqs, seq_len of the layer], and forward calls bring at most that many sequences."""
+        if mods is not None:
+            _check_mods(mods, self.desc.heads, self.desc.device, layer_len=self.desc.seq_len)
         llmcache_layer_score_mods(self.handle, mods)
         self._mods = mods                                # keeps the arrays alive
 
@@ -763,6 +766,10 @@ def make_score_mods(*, causal=False, scale=0.0, cap=0.0, slopes=None, table=None
         if table.shape[1] % 2 == 0:
             raise LLMCacheError(ERR_SHAPE, "table: an odd number of distances, from -reach to reach")
         m.reach = table.shape[1] // 2
+    if doc is not None and prefix is not None and doc.shape[0] != prefix.shape[0]:
+        raise LLMCacheError(ERR_SHAPE, "doc and prefix: as many sequences in one as in the other")
+    masks = doc if doc is not None else prefix
+    m.mask_seqs = 0 if masks is None else masks.shape[0]
     m.slopes, m.table, m.doc, m.prefix = _ptr(slopes), _ptr(table), _ptr(doc), _ptr(prefix)
     m.tensors = (slopes, table, doc, prefix)
     return m
@@ -774,14 +781,16 @@ def _same_device(device, *tensors):
             _other_device(t, device)
 
 
-def _check_mods(mods, heads, device, S=0, n=0):
-    """The shapes of the modifiers' arrays (S, n: of whole sequences)."""
+def _check_mods(mods, heads, device, S=0, n=0, layer_len=0):
+    """The shapes of the modifiers' arrays (S, n: of whole sequences; layer_len: of a layer, for any number of them)."""
     slopes, table, doc, prefix = tensors = getattr(mods, "tensors", (None, None, None, None))
     _same_device(device, *tensors)
     if (slopes is not None and slopes.size(0) != heads) or (table is not None and table.size(0) != heads):
         raise LLMCacheError(ERR_SHAPE, "score modifiers: one row per query head")
     if S and ((doc is not None and doc.shape != (S, n)) or (prefix is not None and prefix.shape != (S,))):
         raise LLMCacheError(ERR_SHAPE, "doc: [n_seqs, seq_len], prefix: [n_seqs]")
+    if layer_len and ((doc is not None and (doc.size(0) == 0 or doc.size(1) != layer_len)) or (prefix is not None and prefix.size(0) == 0)):
+        raise LLMCacheError(ERR_SHAPE, "doc: [n_seqs, seq_len of the layer], prefix: [n_seqs], of one sequence at least")
 
 
 def llmcache_attention(q, k, v, out, mods: Optional[ScoreMods] = None, lse=None, n_seqs_dev=None, stream=None) -> None:

@@ -16,6 +16,7 @@ struct ScoreArgs {
   const float* table;
   const int32_t* doc;
   const int32_t* prefix;
+  uint32_t mask_seqs;            // entries of doc and prefix; 0: unknown
 };
 
 struct RowsArgs {

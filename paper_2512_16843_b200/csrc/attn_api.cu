@@ -99,7 +99,7 @@ int current_device(int* dev) {
 namespace llmc {
 
 int check_score_mods(const llmcache_score_mods* m, ScoreArgs* o) {
-  *o = ScoreArgs{0.125f, 0.f, 0u, 0, nullptr, nullptr, nullptr, nullptr};
+  *o = ScoreArgs{0.125f, 0.f, 0u, 0, nullptr, nullptr, nullptr, nullptr, 0u};
   if (!m) return LLMCACHE_OK;
   if (m->struct_size != sizeof(llmcache_score_mods)) return LLMCACHE_ERR_ARG;
   if (!(m->scale >= 0.f) || m->scale > 1e30f) return LLMCACHE_ERR_ARG;
@@ -113,6 +113,7 @@ int check_score_mods(const llmcache_score_mods* m, ScoreArgs* o) {
   o->causal = m->causal;
   o->reach = (int32_t)m->reach;
   o->slopes = m->slopes; o->table = m->table; o->doc = m->doc; o->prefix = m->prefix;
+  o->mask_seqs = m->doc || m->prefix ? m->mask_seqs : 0u;
   return LLMCACHE_OK;
 }
 
@@ -263,6 +264,7 @@ int llmcache_attention(const llmcache_rows* q, const llmcache_rows* k, const llm
   if (heads && kv_heads && heads % kv_heads == 0 && heads / kv_heads > ATTN_MAX_GROUP) return LLMCACHE_ERR_UNSUPPORTED;
   if (!heads || !kv_heads || heads % kv_heads || heads > 65536 || !seq_len || seq_len > (1u << 30)) return LLMCACHE_ERR_SHAPE;
   if (n_seqs == 0) return LLMCACHE_OK;                     // an empty batch has no buffers to check
+  if (a.m.mask_seqs && n_seqs > a.m.mask_seqs) return LLMCACHE_ERR_SHAPE;
   if ((rc = take_rows(q, n_seqs, seq_len, heads, &a.q)) != LLMCACHE_OK) return rc;
   if ((rc = take_rows(k, n_seqs, seq_len, kv_heads, &a.k)) != LLMCACHE_OK) return rc;
   if ((rc = take_rows(v, n_seqs, seq_len, kv_heads, &a.v)) != LLMCACHE_OK) return rc;

@@ -4,6 +4,7 @@
 #include <new>
 #include "layer.cuh"
 #include "attn_host.cuh"
+#include "ptx.cuh"
 
 using namespace llmc;
 
@@ -146,6 +147,7 @@ int llmcache_layer_forward(llmcache_layer_t* L, const void* x, uint32_t n_seqs, 
   if (n_seqs > L->desc.max_seqs) return LLMCACHE_ERR_SHAPE;
   if (((uintptr_t)x | (uintptr_t)out) & 15u) return LLMCACHE_ERR_ARG;
   if (n_seqs == 0) return LLMCACHE_OK;
+  if (L->has_mods && L->mods.mask_seqs && n_seqs > L->mods.mask_seqs) return LLMCACHE_ERR_SHAPE;
   int prev = 0;
   cudaGetDevice(&prev);
   if (prev != L->desc.device && cudaSetDevice(L->desc.device) != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
@@ -200,6 +202,8 @@ int llmcache_layer_score_mods(llmcache_layer_t* L, const llmcache_score_mods* mo
   const int rc = check_score_mods(mods, &m);
   if (rc != LLMCACHE_OK) return rc;
   if ((m.causal != 0) != (L->desc.causal != 0)) return LLMCACHE_ERR_ARG;
+  for (const void* p : {(const void*)m.slopes, (const void*)m.table, (const void*)m.doc, (const void*)m.prefix})
+    if (p && !pointer_on_device(p, L->desc.device)) return LLMCACHE_ERR_ARG;
   L->mods = m;
   L->has_mods = true;
   return LLMCACHE_OK;
