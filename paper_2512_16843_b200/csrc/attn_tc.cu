@@ -224,6 +224,9 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  // Tensor memory is taken behind the wait for the preceding kernels: a block of theirs on this SM may not have its own yet, and
+  // would wait for these columns while this block waits for it.
+  griddep_sync();                                            // what the preceding kernels wrote may be read from here on
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(smem_u32((const void*)misc)), "r"(TC_TMEM) : "memory");
@@ -233,7 +236,6 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = misc[0];
-  griddep_sync();                                            // what the preceding kernels wrote may be read from here on
   const unsigned long long lim = wait_limit(a.status);
   uint32_t n_seqs = a.n_seqs;
   if (a.n_seqs_dev) n_seqs = min(n_seqs, *a.n_seqs_dev);
