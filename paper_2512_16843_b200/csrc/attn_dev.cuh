@@ -106,8 +106,17 @@ __device__ __forceinline__ unsigned long long tanh_tiny2(unsigned long long u) {
   q = f2_fma(q, s, f2_dup(9.999998808e-01f));
   return f2_mul(u, q);
 }
+constexpr float TANH_TINY = 0.4f, TANH_SMALL = 0.75f;        // largest arguments of the two
 // 1 - 2 / (1 + e^2u): for |u| > 0.75, where the difference loses nothing
 __device__ __forceinline__ float tanh_large(float u) { return 1.f - __fdividef(2.f, 1.f + ex2f(2.f * LOG2E_F * u)); }
+// tanh of any two values.  Which form a value takes depends on the value alone: where a whole group of scores is small a kernel
+// may call tanh_tiny2 for all of it, and no bit depends on what else the group holds (keys that a row does not see, rows that
+// do not exist).
+__device__ __forceinline__ unsigned long long tanh_any2(unsigned long long u) {
+  const unsigned long long a = tanh_tiny2(u), b = tanh_small2(u);
+  const float x = f2_lo(u), y = f2_hi(u), p = fabsf(x) <= TANH_TINY ? f2_lo(a) : f2_lo(b), q = fabsf(y) <= TANH_TINY ? f2_hi(a) : f2_hi(b);
+  return f2_pack(fabsf(x) <= TANH_SMALL ? p : tanh_large(x), fabsf(y) <= TANH_SMALL ? q : tanh_large(y));
+}
 
 }  // namespace
 }  // namespace llmc

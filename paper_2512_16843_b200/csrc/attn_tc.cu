@@ -704,15 +704,11 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
                 float big[2] = {0.f, 0.f};
 #pragma unroll
                 for (uint32_t x = 0; x < 16; ++x) big[x & 1u] = max3f(big[x & 1u], fabsf(f2_lo(t[x])), fabsf(f2_hi(t[x])));
+                // (keys that are not seen and rows that do not exist have their say here: it decides how, not what is computed)
                 const float most = fmaxf(big[0], big[1]);
-                by_hand = by_hand || !(most <= 0.75f);
-                if (__all_sync(0xFFFFFFFFu, most <= 0.4f)) {
+                by_hand = by_hand || (mine && !(most <= TANH_TINY));
 #pragma unroll
-                  for (uint32_t x = 0; x < 16; ++x) t[x] = tanh_tiny2(t[x]);
-                } else {
-#pragma unroll
-                  for (uint32_t x = 0; x < 16; ++x) t[x] = tanh_small2(t[x]);
-                }
+                for (uint32_t x = 0; x < 16; ++x) t[x] = tanh_tiny2(t[x]);
               }
               const unsigned long long u2 = f2_dup(a.m.cap > 0.f ? a.m.cap * LOG2E_F : 1.f), k2 = f2_dup(rise);
               // bias + rise * distance, two keys at a time; each fourth pair anew, so that few roundings add up
@@ -762,12 +758,35 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
                 for (uint32_t x = 0; x < 16; ++x) z[x] = __uint_as_float(u16[x]) * (a.m.cap > 0.f ? a.m.scale / a.m.cap : sc);
                 if (a.m.cap > 0.f) {
 #pragma unroll
-                  for (uint32_t x = 0; x < 16; ++x)
-                    z[x] = (fabsf(z[x]) <= 0.75f ? f2_lo(tanh_small2(f2_dup(z[x]))) : tanh_large(z[x])) * (a.m.cap * LOG2E_F);
+                  for (uint32_t x = 0; x < 16; x += 2) {
+                    const unsigned long long t = tanh_any2(f2_pack(z[x], z[x + 1]));
+                    z[x] = f2_lo(t) * (hand ? a.m.cap * LOG2E_F : 1.f);
+                    z[x + 1] = f2_hi(t) * (hand ? a.m.cap * LOG2E_F : 1.f);
+                  }
+                }
+                if (hand) {
+#pragma unroll
+                  for (uint32_t x = 0; x < 16; ++x) z[x] = fmaf(-slope, fabsf((float)d[x]), z[x]) + bias + entry2(b[x]);
+                } else {
+                  // only large scores brought the chunk here: the rest as it is on the straight way, bit for bit
+                  const unsigned long long k2 = f2_dup(rise), b2 = f2_dup(bias), eight = f2_dup(8.f), step = f2_dup(2.f * rise);
+                  unsigned long long d2 = f2_pack((float)(d0 + (int32_t)c), (float)(d0 + (int32_t)c + 1)), line = 0;
+                  if (g) d2 = f2_add(f2_add(d2, eight), eight);
+#pragma unroll
+                  for (uint32_t x = 0; x < 8; ++x) {
+                    if (x % 4 == 0) {
+                      line = f2_fma(d2, k2, b2);
+                      d2 = f2_add(d2, eight);
+                    } else {
+                      line = f2_add(line, step);
+                    }
+                    const unsigned long long t = f2_fma(f2_pack(z[2 * x], z[2 * x + 1]), f2_dup(a.m.cap * LOG2E_F), line);
+                    z[2 * x] = f2_lo(t);
+                    z[2 * x + 1] = f2_hi(t);
+                  }
                 }
 #pragma unroll
                 for (uint32_t x = 0; x < 16; ++x) {
-                  z[x] = fmaf(-slope, fabsf((float)d[x]), z[x]) + bias + entry2(b[x]);
                   z[x] = (word & (1u << (g + x))) && b[x] != -INFINITY ? z[x] : -INFINITY;
                   u16[x] = __float_as_uint(z[x]);
                   mt = fmaxf(mt, z[x]);

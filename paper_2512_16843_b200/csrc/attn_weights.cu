@@ -250,14 +250,9 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 big[i & 1u] = max3f(big[i & 1u], 2 * i < left ? fabsf(f2_lo(t[i])) : 0.f, 2 * i + 1 < left ? fabsf(f2_hi(t[i])) : 0.f);
               }
               const float most = fmaxf(big[0], big[1]);
-              by_hand = by_hand || !(most <= 0.75f);
-              if (__all_sync(0xFFFFFFFFu, most <= 0.4f)) {
+              by_hand = by_hand || (real && !(most <= TANH_TINY));
 #pragma unroll
-                for (uint32_t i = 0; i < 16; ++i) t[i] = tanh_tiny2(t[i]);
-              } else {
-#pragma unroll
-                for (uint32_t i = 0; i < 16; ++i) t[i] = tanh_small2(t[i]);
-              }
+              for (uint32_t i = 0; i < 16; ++i) t[i] = tanh_tiny2(t[i]);
 #pragma unroll
               for (uint32_t i = 0; i < 16; ++i) {
                 v[2 * i] = __float_as_uint(f2_lo(t[i]));
@@ -310,8 +305,25 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
               for (uint32_t i = 0; i < 16; ++i) z[i] = __uint_as_float(u[i]) * (a.m.cap > 0.f ? a.m.scale / a.m.cap : unit);
               if (a.m.cap > 0.f) {
 #pragma unroll
-                for (uint32_t i = 0; i < 16; ++i)
-                  z[i] = (fabsf(z[i]) <= 0.75f ? f2_lo(tanh_small2(f2_dup(z[i]))) : tanh_large(z[i])) * unit;
+                for (uint32_t i = 0; i < 16; i += 2) {
+                  const unsigned long long t = tanh_any2(f2_pack(z[i], z[i + 1]));
+                  z[i] = f2_lo(t) * (odd ? unit : 1.f);
+                  z[i + 1] = f2_hi(t) * (odd ? unit : 1.f);
+                }
+              }
+              if (!odd) {
+                // only large scores brought the chunk here: the rest as it is on the straight way, bit for bit
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) {
+                  z[i] = ex2f(fmaf(slope[o + i], (float)key_in, fmaf(z[i], unit, add[o + i])));
+                  z[i] = (int32_t)key < hi[o + i] ? z[i] : 0.f;
+                }
+#pragma unroll
+                for (uint32_t i = 0; i < 16; i += 4) {
+                  s0 += z[i] + z[i + 2];
+                  s1 += z[i + 1] + z[i + 3];
+                }
+                continue;
               }
 #pragma unroll
               for (uint32_t i = 0; i < 16; ++i) {
