@@ -463,7 +463,8 @@ typedef struct llmcache_score_mods {
   uint32_t mask_seqs;        /* sequences that doc and prefix have entries for: a call with more is refused
                                 (LLMCACHE_ERR_SHAPE); 0 => not checked */
   const float*   slopes;     /* f32 [heads], or NULL */
-  const float*   table;      /* f32 [heads, 2 * reach + 1], or NULL; an entry of -inf hides the key like a mask */
+  const float*   table;      /* f32 [heads, 2 * reach + 1], or NULL; an entry of -inf hides the key like a mask;
+                                entries below -2.29e38 count as the type's lowest value */
   const int32_t* doc;        /* i32 [n_seqs, seq_len] document of every token, < 0: padding; or NULL */
   const int32_t* prefix;     /* i32 [n_seqs], keys below it are seen by every query (causal only); or NULL */
 } llmcache_score_mods;
@@ -513,7 +514,7 @@ typedef struct llmcache_kv_desc {
   void*    v_pages;
   uint64_t page_stride;      /* elements, a multiple of 64; 0 => kv_heads * page_size * 64 */
   void*    workspace;        /* device scratch (256-byte aligned) or NULL => the library cudaMallocs it: 22 MB for shares of
-                                the keys, up to 64 MB of scores (4 bytes per query head and slot), 4 bytes per new row and
+                                the keys, up to 64 MB of scores (4 bytes per query head and slot), 8 bytes per new row and
                                 head, 4 bytes per key/value head and slot for evictions */
   size_t   workspace_bytes;  /* llmcache_kv_bytes tells how much is needed */
 } llmcache_kv_desc;

@@ -27,7 +27,8 @@ struct RowsArgs {
 // One call of the attention over whole sequences (pages == nullptr) or over a paged cache.
 struct AttnArgs {
   RowsArgs q, out, k, v;         // paged: k, v are the new rows (ptr may be null), seq strides unused
-  float* lse;
+  float* lse;                    // or null
+  float2* stat;                  // calls that record weights: (maximum, sum) of a row's exponentials, base 2 [n_rows, heads]; or null
   uint32_t heads, kv_heads, group, n_seqs;
   const uint32_t* n_seqs_dev;
   ScoreArgs m;
@@ -102,7 +103,7 @@ struct AttnScratch {
   uint32_t* arrived = nullptr;
 };
 cudaError_t launch_attn(const AttnArgs& a, const AttnScratch& s, int sm_count, cudaStream_t st);
-// received weights of a paged call whose lse is complete
+// received weights of a paged call whose stat is complete
 cudaError_t launch_attn_weights(const AttnArgs& a, int sm_count, cudaStream_t st);
 cudaError_t launch_kv_append(const AttnArgs& a, int sm_count, cudaStream_t st);
 

@@ -153,7 +153,7 @@ size_t kv_score_floats(const llmcache_kv_desc& d) {
   const size_t most = (size_t)d.max_seqs * d.heads * (((size_t)d.max_len + 127) / 128 * 128);
   return most < KV_SCORE_FLOATS ? most : KV_SCORE_FLOATS;
 }
-struct KvLayout { size_t status, arrived, part, scores, lse, kept, count, total; };
+struct KvLayout { size_t status, arrived, part, scores, stat, kept, count, total; };
 KvLayout kv_layout(const llmcache_kv_desc& d) {
   KvLayout L{};
   size_t o = 0;
@@ -162,7 +162,7 @@ KvLayout kv_layout(const llmcache_kv_desc& d) {
   L.arrived = take((size_t)d.max_seqs * d.kv_heads * 4);
   L.part = take(KV_PART_UNITS * PART_FLOATS * 4);
   L.scores = take(kv_score_floats(d) * 4);
-  L.lse = take((size_t)d.max_rows * d.heads * 4);
+  L.stat = take((size_t)d.max_rows * d.heads * 8);
   L.kept = take((size_t)d.max_seqs * d.kv_heads * d.max_len * 4);
   L.count = take((size_t)d.max_seqs * 4);
   L.total = o;
@@ -207,7 +207,8 @@ int chunk_args(const llmcache_kv* kv, const llmcache_kv_chunk* c, AttnArgs* o) {
     if ((rc = take_rows(&c->k_new, 1, c->n_rows, D.kv_heads, &a.k)) != LLMCACHE_OK) return rc;
     if ((rc = take_rows(&c->v_new, 1, c->n_rows, D.kv_heads, &a.v)) != LLMCACHE_OK) return rc;
   }
-  a.lse = c->lse ? c->lse : kv->lse;
+  a.lse = c->lse;
+  a.stat = c->weights ? kv->stat : nullptr;
   a.heads = D.heads; a.kv_heads = D.kv_heads; a.group = D.heads / D.kv_heads;
   a.n_seqs = c->n_seqs; a.n = c->longest ? c->longest : c->n_rows;
   a.status = kv->status;
@@ -344,7 +345,7 @@ int llmcache_kv_create(const llmcache_kv_desc* desc, llmcache_kv_t** kv_out) {
   kv->part = (float*)(kv->ws + lay.part);
   kv->scores = (float*)(kv->ws + lay.scores);
   kv->score_floats = kv_score_floats(*desc);
-  kv->lse = (float*)(kv->ws + lay.lse);
+  kv->stat = (float2*)(kv->ws + lay.stat);
   kv->kept = (int32_t*)(kv->ws + lay.kept);
   kv->count = (uint32_t*)(kv->ws + lay.count);
   cudaError_t e = cudaMemset(kv->status, 0, lay.part);     // status and arrival counts

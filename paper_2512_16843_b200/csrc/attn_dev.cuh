@@ -22,8 +22,14 @@ __device__ __forceinline__ float lg2f(float x) {
   asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// A table entry in base-2 units.  The type's lowest value, a mask in some programs, stays finite; -inf is dealt with apart.
-__device__ __forceinline__ float entry2(float b) { return fmaxf(b, -2.3e38f) * LOG2E_F; }
+// A table entry in base-2 units.  The type's lowest value, a mask in some programs, stays finite, and entries near it count as
+// it; -inf is dealt with apart.
+__device__ __forceinline__ float entry2(float b) { return (b < -2.3e38f ? -2.3e38f : b) * LOG2E_F; }
+// natural logarithm of the sum l of exponentials that refer to the maximum m (base 2)
+__device__ __forceinline__ float log_sum(float m, float l) {
+  const float x = (m + lg2f(l)) * LN2_F;
+  return x < -2.29e38f ? -3.402823466e38f : x;               // (nothing but entries that count as the lowest value)
+}
 __device__ __forceinline__ float max3f(float a, float b, float c) {
   float y;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));

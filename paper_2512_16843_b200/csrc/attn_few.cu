@@ -134,7 +134,8 @@ __device__ __noinline__ void few_output(const AttnArgs& a, const FwPlace& at, ui
   for (uint32_t y = 0; y < 4; ++y) w[y] = pack2(dead ? 0.f : x[2 * y] * inv, dead ? 0.f : x[2 * y + 1] * inv);
   const size_t row = (size_t)at.g.row0 + token;
   *reinterpret_cast<uint4*>(a.out.ptr + (long long)row * a.out.tok + (long long)h * a.out.head + c0) = make_uint4(w[0], w[1], w[2], w[3]);
-  if (a.lse && c0 == 0) a.lse[row * a.heads + h] = dead ? -INFINITY : (mx + lg2f(lt)) * LN2_F;
+  if (a.lse && c0 == 0) a.lse[row * a.heads + h] = dead ? -INFINITY : log_sum(mx, lt);
+  if (a.stat && c0 == 0) a.stat[row * a.heads + h] = make_float2(mx, lt);
 }
 // One of the 16-byte pieces of the new row of a slot: eight lanes have its key, eight its value.
 __device__ __forceinline__ uint4 new_piece(const AttnArgs& a, const FwPlace& at, uint32_t slot) {

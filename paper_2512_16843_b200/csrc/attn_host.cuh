@@ -12,7 +12,7 @@ struct llmcache_kv {
   uint32_t* arrived = nullptr;   // [max_seqs, kv_heads], zero between calls
   float* scores = nullptr;       // of few rows whose weights are recorded: score_floats of them
   size_t score_floats = 0;
-  float* lse = nullptr;          // [max_rows, heads] where the caller takes none
+  float2* stat = nullptr;        // [max_rows, heads] of a call that records weights
   int32_t* kept = nullptr;       // eviction: slots kept [max_seqs, kv_heads, <= max_len] ...
   uint32_t* count = nullptr;     // ... and how many per sequence
 };

@@ -947,8 +947,10 @@ k_attn_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       if (mine) {
         if (p.shares > 1)
           reinterpret_cast<float2*>(p.part_ml)[(size_t)sp * n_rowids + rowid] = make_float2(l != l && m_ref == -INFINITY ? 0.f : m_ref, l);
-        else if (a.lse)
-          a.lse[rowid] = dead ? -INFINITY : (m_ref + lg2f(l)) * LN2_F;
+        else {
+          if (a.lse) a.lse[rowid] = dead ? -INFINITY : log_sum(m_ref, l);
+          if (a.stat) a.stat[rowid] = make_float2(m_ref, l);
+        }
       }
       if (p.shares == 1) {
         __nv_bfloat16* out0 = a.out.ptr + (paged ? (long long)row0 * a.out.tok : (long long)sq * a.out.seq) + (long long)tok0 * a.out.tok +
@@ -1010,7 +1012,8 @@ __global__ void __launch_bounds__(256) k_attn_join(const AttnArgs a, const float
     }
     const float inv = m == -INFINITY ? 0.f : 1.f / l;
     *reinterpret_cast<uint32_t*>(a.out.ptr + (long long)row * a.out.tok + (long long)h * a.out.head + lane * 2) = pack2(o.x * inv, o.y * inv);
-    if (a.lse && lane == 0) a.lse[id] = m == -INFINITY ? -INFINITY : (m + lg2f(l)) * LN2_F;
+    if (a.lse && lane == 0) a.lse[id] = m == -INFINITY ? -INFINITY : log_sum(m, l);
+    if (a.stat && lane == 0) a.stat[id] = make_float2(m, l);
   }
 }
 

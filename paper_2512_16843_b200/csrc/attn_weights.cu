@@ -1,8 +1,8 @@
 // Received weights of a paged call: weights[key] = decay * weights[key] + sum over the call's rows, and over the query heads
-// that share the key, of exp(z - lse).  The scores are formed again, with the keys as the rows of the product:
+// that share the key, of exp(z - m) / l (m, l: maximum and sum of the row, as the attention left them).  The scores are formed again, with the keys as the rows of the product:
 //   S^T = K Q^T    tcgen05.mma 128 keys x up to 128 query rows x 64
 // so that a thread owns a key and its sum over the rows needs no exchange and no atomics (same bits every time).  What a
-// row adds to a score is prepared once per tile: -lse, and with a linear bias slope * (first key - query) with the slope
+// row adds to a score is prepared once per tile: -(m + log l), and with a linear bias slope * (first key - query) with the slope
 // beside it, so that a score costs one or two multiply-adds and its exponential.  A block
 // takes a sequence and head and every parts-th key tile of it; the query rows stream past each key tile (they come from
 // L2).  Two groups of four warps take turns with the query tiles, two blocks per SM.  Reads K once more (128 bytes per
@@ -22,9 +22,9 @@ constexpr uint32_t WT_ST = 3, WT_TILE = 16384, WT_KEYS = 128, WT_TMEM = 256;
 struct WtSmem {
   static constexpr uint32_t K = 0;                           // [2]
   static constexpr uint32_t Q = K + 2 * WT_TILE;             // [WT_ST]
-  static constexpr uint32_t ADD = Q + WT_ST * WT_TILE;       // f32 [stage][128], base 2: - lse (- inf: the row gives nothing) + linear bias
-  static constexpr uint32_t LSE = ADD + WT_ST * 512;         // f32 [stage][128]: - lse alone
-  static constexpr uint32_t SLOPE = LSE + WT_ST * 512;       // f32 [stage][128]
+  static constexpr uint32_t ADD = Q + WT_ST * WT_TILE;       // f32 [stage][128], base 2: - (m + log l) (- inf: the row gives nothing) + linear bias
+  static constexpr uint32_t TOP = ADD + WT_ST * 512;         // f32 [stage][128][2]: - m and 1 / l (where scores are large, log l is lost beside m)
+  static constexpr uint32_t SLOPE = TOP + WT_ST * 1024;      // f32 [stage][128]
   static constexpr uint32_t QPOS = SLOPE + WT_ST * 512;      // i32 [stage][128]
   static constexpr uint32_t HI = QPOS + WT_ST * 512;         // i32 [stage][128]: keys below it are seen
   static constexpr uint32_t TAB = HI + WT_ST * 512;          // i32 [stage][128]: middle of the head's row of the table
@@ -180,11 +180,10 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         const uint32_t c = u * 64 + threadIdx.x - 64, R = qt * p.rt + c;
         const uint32_t token = R / a.group, h = hk * a.group + R % a.group;
         const bool real = c < p.rt && R < rows;
-        float add = -INFINITY;
-        if (real) {
-          add = -a.lse[(size_t)(g.row0 + token) * a.heads + h] * LOG2E_F;
-          if (add == INFINITY) add = -INFINITY;              // a row that sees nothing gives nothing
-        }
+        float2 ml = make_float2(0.f, 0.f);
+        if (real) ml = a.stat[(size_t)(g.row0 + token) * a.heads + h];
+        const bool none = ml.y == 0.f;                       // a row that sees nothing gives nothing
+        const float add = none ? -INFINITY : -(ml.x + lg2f(ml.y));
         const uint32_t at = s * 128 + c;
         const int32_t qpos = pos0 + (int32_t)token;
         const float slope = MOD && a.m.slopes && real ? a.m.slopes[h] * LOG2E_F : 0.f;
@@ -192,7 +191,7 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         reinterpret_cast<int32_t*>(gbase + WtSmem::HI)[at] =
             !real ? 0 : a.m.causal ? min(g.slot0 + (int32_t)token + 1, (int32_t)g.len) : (int32_t)g.len;
         if constexpr (MOD) {
-          reinterpret_cast<float*>(gbase + WtSmem::LSE)[at] = add;
+          reinterpret_cast<float2*>(gbase + WtSmem::TOP)[at] = none ? make_float2(0.f, 0.f) : make_float2(-ml.x, 1.f / ml.y);
           reinterpret_cast<float*>(gbase + WtSmem::SLOPE)[at] = slope;
           reinterpret_cast<int32_t*>(gbase + WtSmem::QPOS)[at] = qpos;
           if (a.m.table) reinterpret_cast<int32_t*>(gbase + WtSmem::TAB)[at] = (int32_t)((real ? h : 0u) * (2 * a.m.reach + 1)) + a.m.reach;
@@ -285,7 +284,7 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
           } else {
             // scores beyond the polynomial, positions, distances on both sides, table entries: 16 rows at a time
-            const float* lse = reinterpret_cast<const float*>(gbase + WtSmem::LSE) + s * 128;
+            const float2* top = reinterpret_cast<const float2*>(gbase + WtSmem::TOP) + s * 128;
             const int32_t* qpos = reinterpret_cast<const int32_t*>(gbase + WtSmem::QPOS) + s * 128;
             const int32_t* tab = reinterpret_cast<const int32_t*>(gbase + WtSmem::TAB) + s * 128;
 #pragma unroll 1
@@ -327,8 +326,8 @@ k_attn_weights(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
               }
 #pragma unroll
               for (uint32_t i = 0; i < 16; ++i) {
-                z[i] = fmaf(-slope[o + i], fabsf((float)(kpos - qpos[o + i])), z[i]) + entry2(b[i]) + lse[o + i];
-                const float x = ex2f(z[i]);
+                z[i] = fmaf(-slope[o + i], fabsf((float)(kpos - qpos[o + i])), z[i]) + entry2(b[i]) + top[o + i].x;
+                const float x = ex2f(z[i]) * top[o + i].y;
                 s0 += (int32_t)key < hi[o + i] && b[i] != -INFINITY ? x : 0.f;
               }
             }
@@ -403,10 +402,12 @@ __global__ void __launch_bounds__(256) k_weights_of_scores(const __grid_constant
   const uint32_t part = blockIdx.x % parts, hk = (blockIdx.x / parts) % a.kv_heads, sq = blockIdx.x / parts / a.kv_heads;
   const SeqGeo g = seq_geo(a, sq);
   const uint32_t rows = g.cnt * a.group;
-  __shared__ float lse[FEW_ROWS];
+  __shared__ float top[FEW_ROWS], inv[FEW_ROWS];
   if (threadIdx.x < rows) {
-    const float x = a.lse[(size_t)(g.row0 + threadIdx.x / a.group) * a.heads + hk * a.group + threadIdx.x % a.group] * LOG2E_F;
-    lse[threadIdx.x] = x == -INFINITY ? INFINITY : x;        // a row that sees nothing gives nothing
+    const float2 ml = a.stat[(size_t)(g.row0 + threadIdx.x / a.group) * a.heads + hk * a.group + threadIdx.x % a.group];
+    const bool none = ml.y == 0.f;                           // a row that sees nothing gives nothing
+    top[threadIdx.x] = none ? 0.f : ml.x;
+    inv[threadIdx.x] = none ? 0.f : 1.f / ml.y;
   }
   __syncthreads();
   const size_t pair = (size_t)sq * a.kv_heads + hk;
@@ -414,7 +415,7 @@ __global__ void __launch_bounds__(256) k_weights_of_scores(const __grid_constant
   for (uint32_t key = part * 256 + threadIdx.x; key < g.len; key += parts * 256) {
     float sum = 0.f;
 #pragma unroll 4
-    for (uint32_t R = 0; R < rows; ++R) sum += ex2f(__ldcg(scores + (size_t)R * a.score_ld + key) - lse[R]);
+    for (uint32_t R = 0; R < rows; ++R) sum = fmaf(ex2f(__ldcg(scores + (size_t)R * a.score_ld + key) - top[R]), inv[R], sum);
     float& w = a.weights[pair * a.side_ld + key];
     w = a.decay == 0.f ? sum : fmaf(a.decay, w, sum);
   }
