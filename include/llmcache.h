@@ -453,6 +453,8 @@ int llmcache_divergence_check(llmcache_bank_t* bank, llmcache_layer_t* layer, co
  *     (not causal, or j <= i, or j < prefix[s])  and  (no doc, or doc[s][i] == doc[s][j] >= 0).
  * A key that a query does not see takes no part in that query's output, whatever the key's row holds (infinities
  * and NaN included).  A query that sees no key, or only keys of score -inf, gets a row of zeros and lse = -inf.
+ * Sums of weighted values are f32 and relate to a maximum that may lag by a factor of 2^8: values of magnitude above
+ * 2^119 / keys may overflow.
  * Zero-initialise, set struct_size = sizeof, fill in; all pointers are DEVICE memory. */
 typedef struct llmcache_score_mods {
   uint32_t struct_size;
@@ -521,7 +523,7 @@ typedef struct llmcache_kv_desc {
 
 /* New tokens of a batch: sequence s brings the rows cu_rows[s] .. cu_rows[s+1]-1 of q (and k_new, v_new).  lens[s] counts
  * its slots with these tokens included: row r takes slot lens[s] - (cu_rows[s+1] - r).  Rows behind
- * cu_rows[n_seqs] are left as they were.  Zero-initialise, set struct_size = sizeof, fill in. */
+ * cu_rows[n_seqs] are left as they were.  n_seqs == 0 or n_rows == 0: nothing happens.  Zero-initialise, set struct_size = sizeof, fill in. */
 typedef struct llmcache_kv_chunk {
   uint32_t struct_size;
   uint32_t n_seqs;

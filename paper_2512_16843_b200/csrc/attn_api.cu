@@ -142,8 +142,9 @@ int check_kv_desc(const llmcache_kv_desc* d) {
   return LLMCACHE_OK;
 }
 
-// (row, head, share of the keys) results of one call.  Keys are split only while rows alone leave SMs idle, so the shares of
-// all rows never exceed 2 x 256 rows per SM.
+// (row, head, share of the keys) results of one call: a fixed budget of 22 MB, and a limit of the shares.  Where a call's rows
+// and heads leave room for fewer shares than the launch would like, it takes as many as fit (250 and 166 rows of 16 heads: 12,
+// where three items per SM would be 13).
 constexpr size_t KV_PART_UNITS = 2 * 256 * 160;
 // Scores of few rows are kept for the weights where they fit: 4 bytes per row and key, up to 64 MB.  (A call that needs more
 // has its scores formed again from the keys.)

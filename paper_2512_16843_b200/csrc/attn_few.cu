@@ -1,8 +1,9 @@
 // Attention of few query rows over a paged cache (the next token of every sequence, a handful of drafted ones): up to 16
 // rows of a sequence and key/value head, token * group + head of the group.
 //
-// Such a call reads every cached key and value once (256 bytes per key and head) and computes next to nothing, so it is
-// bound by HBM: what counts is bytes in flight and an even share of the keys for every SM.  The key tiles of all sequences
+// Such a call reads every cached key and value once (256 bytes per key and head) and computes next to nothing, so its floor is
+// HBM, and every SM has to have an even share of the keys.  What bounds it as built is a tile's chain in the four warps (scores,
+// maximum, exponentials, product, one tile after the other: some 3 us): the loads in flight would do for twice the rate.  The key tiles of all sequences
 // and heads form one list of W tiles of 128 keys, and each of N blocks takes W / N of them in a row (the first W mod N one
 // more), whichever sequences they belong to.  A sequence and head that one block has whole is finished there; the others leave their shares
 // (sums, maximum, weighted values) in scratch and the block that comes last joins them, in the order of the blocks, so
@@ -16,8 +17,8 @@
 // A sequence's end costs a chain of round trips to memory (the share out, the count, the others' shares); warp 5 takes it,
 // and the queries of the next sequence come with its first tile, so that the four warps go on at once.
 // Softmax statistics and sums are f32; the weights feed the second product as bf16.
-// Measured: one token of 64 sequences of 301 to 4,100 slots, 16 heads on 4, with the scores written: 52 us (147 MB read, 5
-// written: 2.9 TB/s); one token behind 516 slots, 12 heads: 12.6 us, launch and the chain load - product - join.
+// Measured: one token of 64 sequences of 301 to 4,100 slots, 16 heads on 4, with the scores written: 48 us (147 MB read, 5
+// written: 3.2 TB/s); one token behind 516 slots, 12 heads: 12.6 us, launch and the chain load - product - join.
 #include <algorithm>
 #include "attn_dev.cuh"
 

@@ -16,10 +16,10 @@
 // What bounds it: the exponentials could be done at 16 per cycle and SM, 1,024 cycles per query and key tile (256 + 256 for
 // the two products).  As built a pair of query tiles takes 4,700 cycles per key tile: 870 for the maximum, 2,700 for the
 // exponentials (two warps share a scheduler's special function unit, which is busy for 2,050 of them), 500 to 900 until
-// the next S is there, the rest barriers.  Measured: 32 prompts of 1,024 tokens, 12 heads, prefix of 512: 139 us (463 TFLOP/s, exponentials
-// at 40 % of their rate); 64 rows of 384 tokens in documents: 101 us (1.5 TB/s); 2 rows of 4,001 tokens, 16 heads on 4,
-// capped and biased: 196 us; 512 tokens behind 512, 32 sequences, 12 heads: 119 us with the new rows stored; 250 tokens over
-// 17,003 and 30,001 keys, 16 heads on 4, capped and biased: 357 us with the weights (135), the join and the new rows (16).
+// the next S is there, the rest barriers.  Measured: 32 prompts of 1,024 tokens, 12 heads, prefix of 512: 144 us (447 TFLOP/s, exponentials
+// at 39 % of their rate); 64 rows of 384 tokens in documents: 101 us (1.5 TB/s); 2 rows of 4,001 tokens, 16 heads on 4,
+// capped and biased: 195 us; 512 tokens behind 512, 32 sequences, 12 heads: 120 us with the new rows stored; 250 tokens over
+// 17,003 and 30,001 keys, 16 heads on 4, capped and biased: 350 us with the weights (123), the join and the new rows.
 // Work is handed out by the hardware (cluster launch control): a block for every item is launched, those that run cancel the
 // others one by one and do their items.  With item i, i + 148, .. for a block instead the cases took 103, 144, 201, 132 and 389.
 // Tried and dropped (the first of these cases, 144 us at the time): maximum and exponentials in one pass over S (160; 384
@@ -1050,13 +1050,17 @@ cudaError_t launch_attn_tc(const AttnArgs& a, float* part, size_t part_units, in
   if (paged && part) {
     const uint64_t cap = std::min<uint64_t>(a.max_len, (uint64_t)a.pages_ld << a.page_shift), tiles = (cap + TC_KEYS - 1) / TC_KEYS;
     const uint64_t rows = (uint64_t)a.n_rows * a.heads;
-    // rows that fill one query tile: both halves of a block work on them, with the keys shared out between them (33 rows over
-    // 640 keys, 192 items: 117 us without, 102 with)
+    // rows that fill one query tile: both halves of a block work on them, with the keys shared out between them.  33 rows, 12
+    // heads, 64 sequences, without and with: capped and biased over 640 keys 124 and 114 us, over 2,560 404 and 312; positions and a
+    // table over 640 200 and 171; plain over 640 79 and 81, over 2,600 298 and 279.  Few items pay for it (4 sequences, 640
+    // keys: capped and biased 27 and 32, plain 24 and 26), and below four key tiles nobody gains (300 keys: 116 and 128)
     p.narrow = seq_rows <= p.rt && tiles >= 4 && part_units / rows >= 2;
     const uint64_t halves = p.narrow ? 2 : 1;
     // as many shares as it takes to give every SM an item (of two key tiles at least), and up to three items per SM where they
-    // stay long (16 tiles), because sequences of uneven lengths then end together (17,003 and 30,001 keys: 437 us with one
-    // item per SM, 401 with up to three, in an earlier form; two to eight make no difference any more)
+    // stay long (16 tiles), because sequences of uneven lengths then end together.  One, two, three items per SM: 250 rows over
+    // 17,003 and 30,001 keys, capped and biased, 288, 245, 246 us (230 with four, for which the scratch has no room); 200 rows over
+    // 3,000 to 30,000 keys 148, 124, 116; 100 over 4,000 to 16,000 146, 151, 134; even lengths pay for it: 250 rows over twice
+    // 24,000 keys 117, 114, 128, 512 over 30,000 110, 118, 140
     uint64_t sp = std::min<uint64_t>((uint64_t)sm_count / items, (tiles + 1) / 2 / halves);
     sp = std::max<uint64_t>(sp, std::min<uint64_t>(3ull * sm_count / items, tiles / 16 / halves));
     sp = std::min<uint64_t>(sp, part_units / rows / halves);

@@ -7,7 +7,7 @@
 // takes a sequence and head and every parts-th key tile of it; the query rows stream past each key tile (they come from
 // L2).  Two groups of four warps take turns with the query tiles, two blocks per SM.  Reads K once more (128 bytes per
 // key and head) and the queries; one exponential per score, as in the attention itself.
-// Measured: 250 tokens over 17,003 and 30,001 keys, 16 heads on 4, capped and biased: 135 us (147 million scores; the
+// Measured: 250 tokens over 17,003 and 30,001 keys, 16 heads on 4, capped and biased: 123 us (147 million scores; the
 // schedulers issue in 64 % of their cycles, the capped score's multiply-adds above all).
 // f32 throughout; every wait is bounded (status word).
 #include <algorithm>
