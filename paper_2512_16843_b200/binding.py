@@ -650,7 +650,8 @@ class Layer:
 
     def extend(self, cache: "KVCache", x, out, *, cu_rows, lens, pages, longest=0, weights=None, decay=1.0, positions=None,
                first=None, stream=None):
-        """The layer on new tokens: x, out [n_rows, d]; the other arguments as in KVCache.attention."""
+        """The layer on new tokens: x, out [n_rows, d]; the other arguments as in KVCache.attention (rows beyond `longest` get
+        the layer's result for an attention of zero)."""
         chunk = cache.chunk(x.shape[0], cu_rows=cu_rows, lens=lens, pages=pages, longest=longest, weights=weights, decay=decay,
                             positions=positions, first=first)
         _want(x, torch.bfloat16, 2, "x")
@@ -922,7 +923,8 @@ class KVCache:
                   decay=1.0, positions=None, first=None, stream=None):
         """Stores k_new, v_new [n_rows, kv_heads, 64] in the pages and lets q [n_rows, heads, 64] attend to all that its
         sequences have there (llmcache_kv_attention).  cu_rows i32 [n_seqs + 1], lens i32 [n_seqs], pages i32
-        [n_seqs, pages]; lse f32 [n_rows, heads]; weights f32 and positions i32 [n_seqs, kv_heads, slots]."""
+        [n_seqs, pages]; lse f32 [n_rows, heads]; weights f32 and positions i32 [n_seqs, kv_heads, slots].  longest: most rows
+        of one sequence (0: not known); its rows beyond that are stored, but out and lse stay as they were there."""
         device = self.device
         rq = _rows(q, "q", 3, None, device)
         T = q.shape[0]
