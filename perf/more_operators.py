@@ -6,7 +6,7 @@ output channel of weights):
 
   norm     h = x + residual, kept on request; root-mean-square or layer norm of h, or h itself; the result in bf16, in 8 bits with
            a scale per row, or in both                                                              llmcache_norm
-  dense    act(a w^T) + residual for a and w in 8 bits; int8 is summed in whole numbers              llmcache_dense8
+  dense    act(a w^T) + residual for a and w in 8 bits; int8 is summed in whole numbers              llmcache_dense
   append   queries and keys of new tokens are rotated by their positions, keys and values go to their places in a paged cache
                                                                                                      llmcache_kv_append
 
@@ -209,7 +209,7 @@ def run(st):
                 torch.mul(st["q"], st["scale"].unsqueeze(1), out=st["values"])
             return _norm_answer(st, st["total"], st["out"], st["values"] if case["to"] == "int8" else st["q"], st["scale"])
         if case["op"] == "dense":
-            L.llmcache_dense8(st["a"], st["a_scale"], st["w"], st["w_scale"], st["out"], bias=st["bias"], act=case["act"],
+            L.llmcache_dense(st["a"], st["a_scale"], st["w"], st["w_scale"], st["out"], bias=st["bias"], act=case["act"],
                               residual=st["residual"])
             return {"out": st["out"]}
         st["cache"].append(st["k_new"], st["v_new"], cu_rows=st["cu"], lens=st["lens"], pages=st["pages"], q=st["q"], q_out=st["q_out"],
