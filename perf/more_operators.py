@@ -129,7 +129,7 @@ def _normal(g, *shape):
 
 def _eight(case, x):
     """x in the case's 8-bit type."""
-    return x.round().clamp(-127, 127).to(torch.int8) if case["to"] == "int8" else x.to(E4M3)
+    return x.round().clamp(-127, 127).to(torch.int8) if case["to"] == "int8" else x.clamp(-448, 448).to(E4M3)
 
 
 def prepare(case, seed):
