@@ -58,7 +58,8 @@ typedef enum {
                                      (sticky, see bank_status); the access was skipped */
 } llmcache_status;
 
-enum { LLMCACHE_F32 = 0, LLMCACHE_BF16 = 1 };                 /* dtype of probe inputs h_in */
+enum { LLMCACHE_F32 = 0, LLMCACHE_BF16 = 1,                   /* dtype of probe inputs h_in */
+       LLMCACHE_I8 = 2, LLMCACHE_E4M3 = 3 };                  /* 8-bit values with a scale per row (llmcache_norm, llmcache_dense) */
 enum { LLMCACHE_GT = 0, LLMCACHE_GE = 1 };                    /* hit iff sim > tau  |  sim >= tau */
 enum { LLMCACHE_LRU = 0, LLMCACHE_LRU_STALENESS = 1 };        /* eviction policy */
 enum { LLMCACHE_EVICT_STALE = 0, LLMCACHE_EVICT_IDLE = 1, LLMCACHE_EVICT_ALL = 2, LLMCACHE_EVICT_SLOTS = 3 };
@@ -597,6 +598,121 @@ int llmcache_layer_score_mods(llmcache_layer_t* layer, const llmcache_score_mods
  * `longest`, out is what the layer gives with zeros for the attention. */
 int llmcache_layer_extend(llmcache_layer_t* layer, llmcache_kv_t* kv, const void* x, const llmcache_kv_chunk* chunk,
                           void* out, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * A layer around its attention in 8 bits and with positions by rotation: the norm with an output in 8 bits
+ * (llmcache_norm), the product of two 8-bit matrices (llmcache_dense), new keys and values stored with
+ * their rotation (llmcache_kv_append), and the three inside the layer (llmcache_layer_quantise, llmcache_layer_rms,
+ * llmcache_layer_rotation).  An 8-bit matrix has rows of int8 (LLMCACHE_I8) or e4m3 (LLMCACHE_E4M3) and an f32 scale
+ * per row: it stands for scale[r] * q[r][c].  llmcache_norm and llmcache_dense take no object: they run on the CURRENT device, where all
+ * arrays have to be (x or a elsewhere: LLMCACHE_ERR_ARG), allocate nothing and do not synchronise.  The first call on a device
+ * looks up an address and sets kernel attributes: make it outside any stream capture.
+ * ------------------------------------------------------------------------------------------------ */
+enum { LLMCACHE_NORM_NONE = 0, LLMCACHE_NORM_LAYER = 1, LLMCACHE_NORM_RMS = 2 };
+enum { LLMCACHE_ACT_NONE = 0, LLMCACHE_ACT_GELU_ERF = 1, LLMCACHE_ACT_GELU_TANH = 2 };
+
+/* Per row, in f32:  h = x + residual;
+ *     NONE: y = h      LAYER: y = (h - mean(h)) / sqrt(var(h) + eps) * gain + bias     RMS: y = h / sqrt(mean(h^2) + eps) * gain + bias
+ *     total = bf16(h)      out = bf16(y)
+ *     scale = max |y| / 127 (LLMCACHE_I8) or / 448 (LLMCACHE_E4M3), q = y / scale rounded to nearest even
+ * A row of y below 1e-30 has scale 0 and zeros; a row with an infinity or NaN has a scale of NaN and zeros, so that products of
+ * it are NaN.  Any of total, out and q may be left out, not all.  Leading dimensions (`_ld`) count elements from row to row,
+ * multiples of 8 and at least cols; they are not looked at where there is one row.  x, residual, total, out, gain and bias are 16-byte aligned, q is
+ * 8-byte aligned.  total and out may be x or residual itself (same address, same leading dimension); outputs overlap nothing otherwise.
+ * Zero-initialise, set struct_size = sizeof, fill in. */
+typedef struct llmcache_norm_args {
+  uint32_t struct_size;
+  uint32_t kind;             /* LLMCACHE_NORM_* */
+  uint32_t format;           /* of q: LLMCACHE_I8 | LLMCACHE_E4M3 */
+  uint32_t n_rows;           /* < 2^31; 0: nothing happens */
+  uint32_t cols;             /* a multiple of 8, <= 16,384 */
+  uint32_t rows_per_count;   /* 0 => 1 */
+  float    eps;              /* <= 0 => 1e-5 */
+  const uint32_t* count_dev; /* optional DEVICE u32: only min(n_rows, *count_dev * rows_per_count) rows are processed,
+                                the others stay as they were */
+  const void*  x;         int64_t x_ld;          /* bf16 */
+  const void*  residual;  int64_t residual_ld;   /* bf16, or NULL */
+  void*        total;     int64_t total_ld;      /* bf16, or NULL */
+  void*        out;       int64_t out_ld;        /* bf16, or NULL */
+  void*        q;         int64_t q_ld;          /* 8 bits, or NULL */
+  float*       scale;                            /* f32 [n_rows], with q */
+  const float* gain;                             /* f32 [cols], or NULL: 1; not with NONE */
+  const float* bias;                             /* f32 [cols], or NULL: 0; not with NONE */
+} llmcache_norm_args;
+
+/* out[i][j] = bf16( act( a_scale[i] * w_scale[j] * sum_c a[i][c] * w[j][c] + bias[j] ) + residual[i][j] ),  i < m, j < n, c < k.
+ * The sum is exact for LLMCACHE_I8 (32-bit integers) and f32 for LLMCACHE_E4M3; the rest is f32.  a and w have the same format.  a_ld and
+ * w_ld count bytes from row to row, multiples of 16 and at least k; out_ld and residual_ld count elements, multiples of 8 and at
+ * least n, which may be any number (columns n.. of out stay as they were).  They are not looked at where there is one row.  a, w, out and residual are 16-byte aligned.
+ * residual may be out itself (same address, same leading dimension); out overlaps nothing otherwise.  GELU with erf
+ * is within 8.2e-5 of the function for arguments below 26 in magnitude (beyond that within 3.2e-6 times the argument), as in the layer. */
+typedef struct llmcache_dense_args {
+  uint32_t struct_size;
+  uint32_t format;           /* LLMCACHE_I8 | LLMCACHE_E4M3 */
+  uint32_t m, n;             /* < 2^31; m == 0: nothing happens */
+  uint32_t k;                /* a multiple of 16, <= 131,056 */
+  uint32_t act;              /* LLMCACHE_ACT_* */
+  uint32_t rows_per_count;   /* 0 => 1 */
+  const uint32_t* count_dev; /* optional DEVICE u32: only min(m, *count_dev * rows_per_count) rows, the others stay as they were */
+  const void*  a;         int64_t a_ld;
+  const float* a_scale;                          /* f32 [m] */
+  const void*  w;         int64_t w_ld;
+  const float* w_scale;                          /* f32 [n] */
+  const float* bias;                             /* f32 [n], or NULL */
+  const void*  residual;  int64_t residual_ld;   /* bf16, or NULL */
+  void*        out;       int64_t out_ld;        /* bf16 */
+} llmcache_dense_args;
+
+int llmcache_norm(const llmcache_norm_args* args, void* stream);
+int llmcache_dense(const llmcache_dense_args* args, void* stream);
+/* LLMCACHE_OK, or LLMCACHE_ERR_TIMEOUT once a bounded device-side wait of llmcache_dense has expired on the current device
+ * (sticky).  Synchronises the device. */
+int llmcache_dense_status(void);
+/* As llmcache_bank_debug_knobs, for llmcache_dense on the current device (which it must have run on before). */
+int llmcache_dense_debug_knobs(uint64_t wait_limit_ns, uint32_t flags);
+
+/* Rotation of a head's columns by position: the pairs of columns (i, i + dims / 2) -- or (2 i, 2 i + 1), interleaved --, i < dims / 2,
+ * turn by the angle position * inv_freq[i]; columns from dims on stay.  Angles are formed in f64, products in f32. */
+typedef struct llmcache_rotation {
+  uint32_t struct_size;
+  uint32_t dims;             /* 16, 32, 48 or 64 */
+  uint32_t interleaved;
+  const double* inv_freq;    /* DEVICE f64 [dims / 2], angle per position */
+} llmcache_rotation;
+
+/* New rows of a paged cache, numbered and placed as in llmcache_kv_chunk: row r of sequence s has the position first[s] + (r -
+ * cu_rows[s]), or its slot where first is NULL.  k_new is rotated by it and stored, v_new is stored, q is rotated into q_out
+ * (which may be q itself).  A row without a page, or before slot 0, is not stored, but its q is rotated.  Rows behind
+ * cu_rows[n_seqs] are left as they were.  llmcache_kv_attention follows with k_new and v_new NULL.  n_seqs == 0 or n_rows == 0: nothing happens.
+ * Zero-initialise, set struct_size = sizeof, fill in. */
+typedef struct llmcache_kv_new {
+  uint32_t struct_size;
+  uint32_t n_seqs, n_rows, pages_ld;
+  const int32_t* cu_rows;    /* i32 [n_seqs + 1] */
+  const int32_t* lens;       /* i32 [n_seqs], the new rows included */
+  const int32_t* pages;      /* i32 [n_seqs, pages_ld] */
+  llmcache_rows k_new, v_new;/* kv_heads heads; seq_stride is not used */
+  llmcache_rows q, q_out;    /* heads heads; ptr NULL (both): none */
+  int32_t* positions;        /* optional i32 [n_seqs, kv_heads, side_ld]: written for the new rows' slots */
+  const int32_t* first;      /* i32 [n_seqs], or NULL */
+  uint64_t side_ld;          /* at least min(max_len, pages_ld * page_size) where positions are given */
+  const llmcache_rotation* rotation;   /* NULL: rows are stored, and q copied, as they are */
+} llmcache_kv_new;
+
+int llmcache_kv_append(llmcache_kv_t* kv, const llmcache_kv_new* rows, void* stream);
+
+/* The layer's four products in 8 bits in the forward and extend calls that follow: the weights are brought to `format` once, on
+ * `stream`, with a scale per output channel, the rows that enter a product get a scale per token.  format LLMCACHE_BF16: back to the
+ * bf16 weights (workspace is not looked at).  workspace: device memory, 256-byte aligned, borrowed, of the size that
+ * llmcache_layer_quantise_bytes tells; NULL => the library cudaMallocs it.  Attention, norms and residuals stay as they are.  Entries
+ * that a bank stored before have the other weights' outputs: flush it (llmcache_evict).  Calling it again replaces the weights (and waits for the device). */
+int llmcache_layer_quantise_bytes(llmcache_layer_t* layer, size_t* bytes_out);
+int llmcache_layer_quantise(llmcache_layer_t* layer, uint32_t format, void* workspace, size_t workspace_bytes, void* stream);
+/* Root-mean-square norms (on != 0) in place of both layer norms, with the layer's gains, biases and eps, in the calls that follow. */
+int llmcache_layer_rms(llmcache_layer_t* layer, uint32_t on);
+/* Queries and keys are rotated by their positions (forward: the place in the sequence; extend: as llmcache_kv_append) in the
+ * calls that follow; NULL switches it off.  The struct is copied, inv_freq is borrowed and has to be on the layer's device. */
+int llmcache_layer_rotation(llmcache_layer_t* layer, const llmcache_rotation* rotation);
 
 #ifdef __cplusplus
 }

@@ -21,7 +21,9 @@ LIB_PATH = os.environ.get("LLMCACHE_LIB") or os.path.join(_HERE, "libllmcache.so
 
 OK = 0
 ERR_ARG, ERR_SHAPE, ERR_NOMEM, ERR_CUDA, ERR_STATE, ERR_TIMEOUT, ERR_UNSUPPORTED, ERR_BOUNDS = -1, -2, -3, -4, -5, -6, -7, -8
-F32, BF16 = 0, 1
+F32, BF16, I8, E4M3 = 0, 1, 2, 3
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
+ACT_NONE, ACT_GELU_ERF, ACT_GELU_TANH = 0, 1, 2
 GT, GE = 0, 1
 LRU, LRU_STALENESS = 0, 1
 EVICT_STALE, EVICT_IDLE, EVICT_ALL, EVICT_SLOTS = 0, 1, 2, 3
@@ -43,6 +45,8 @@ EXPORTS = [
     "llmcache_attention", "llmcache_attention_status", "llmcache_attention_debug_knobs", "llmcache_kv_bytes",
     "llmcache_kv_create", "llmcache_kv_destroy", "llmcache_kv_attention", "llmcache_kv_evict", "llmcache_kv_status",
     "llmcache_kv_debug_knobs", "llmcache_layer_score_mods", "llmcache_layer_extend",
+    "llmcache_norm", "llmcache_dense", "llmcache_dense_status", "llmcache_dense_debug_knobs", "llmcache_kv_append",
+    "llmcache_layer_quantise_bytes", "llmcache_layer_quantise", "llmcache_layer_rms", "llmcache_layer_rotation",
 ]
 KNOB_PRODUCER_IDLE = 1
 FINGERPRINT_STATIC_MAX_FLOATS = 2 * 1024 * 1024
@@ -120,6 +124,38 @@ class KVEviction(C.Structure):
         ("pages", C.c_void_p), ("new_pages", C.c_void_p), ("new_lens", C.c_void_p), ("weights", C.c_void_p),
         ("positions", C.c_void_p), ("side_ld", C.c_uint64), ("new_weights", C.c_void_p), ("new_positions", C.c_void_p),
         ("new_side_ld", C.c_uint64), ("kept", C.c_void_p),
+    ]
+
+
+class NormArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("kind", C.c_uint32), ("format", C.c_uint32), ("n_rows", C.c_uint32), ("cols", C.c_uint32),
+        ("rows_per_count", C.c_uint32), ("eps", C.c_float), ("count_dev", C.c_void_p), ("x", C.c_void_p), ("x_ld", C.c_int64),
+        ("residual", C.c_void_p), ("residual_ld", C.c_int64), ("total", C.c_void_p), ("total_ld", C.c_int64),
+        ("out", C.c_void_p), ("out_ld", C.c_int64), ("q", C.c_void_p), ("q_ld", C.c_int64), ("scale", C.c_void_p),
+        ("gain", C.c_void_p), ("bias", C.c_void_p),
+    ]
+
+
+class DenseArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("format", C.c_uint32), ("m", C.c_uint32), ("n", C.c_uint32), ("k", C.c_uint32),
+        ("act", C.c_uint32), ("rows_per_count", C.c_uint32), ("count_dev", C.c_void_p), ("a", C.c_void_p), ("a_ld", C.c_int64),
+        ("a_scale", C.c_void_p), ("w", C.c_void_p), ("w_ld", C.c_int64), ("w_scale", C.c_void_p), ("bias", C.c_void_p),
+        ("residual", C.c_void_p), ("residual_ld", C.c_int64), ("out", C.c_void_p), ("out_ld", C.c_int64),
+    ]
+
+
+class Rotation(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dims", C.c_uint32), ("interleaved", C.c_uint32), ("inv_freq", C.c_void_p)]
+
+
+class KVNew(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("n_seqs", C.c_uint32), ("n_rows", C.c_uint32), ("pages_ld", C.c_uint32),
+        ("cu_rows", C.c_void_p), ("lens", C.c_void_p), ("pages", C.c_void_p), ("k_new", Rows), ("v_new", Rows), ("q", Rows),
+        ("q_out", Rows), ("positions", C.c_void_p), ("first", C.c_void_p), ("side_ld", C.c_uint64),
+        ("rotation", C.POINTER(Rotation)),
     ]
 
 
@@ -209,6 +245,15 @@ def lib():
         L.llmcache_kv_debug_knobs.argtypes = [vp, C.c_uint64, u32]
         L.llmcache_layer_score_mods.argtypes = [vp, C.POINTER(ScoreMods)]
         L.llmcache_layer_extend.argtypes = [vp, vp, vp, C.POINTER(KVChunk), vp, vp]
+        L.llmcache_norm.argtypes = [vp, vp]
+        L.llmcache_dense.argtypes = [vp, vp]
+        L.llmcache_dense_status.argtypes = []
+        L.llmcache_dense_debug_knobs.argtypes = [C.c_uint64, u32]
+        L.llmcache_kv_append.argtypes = [vp, vp, vp]
+        L.llmcache_layer_quantise_bytes.argtypes = [vp, C.POINTER(C.c_size_t)]
+        L.llmcache_layer_quantise.argtypes = [vp, u32, vp, C.c_size_t, vp]
+        L.llmcache_layer_rms.argtypes = [vp, u32]
+        L.llmcache_layer_rotation.argtypes = [vp, C.POINTER(Rotation)]
         for name in EXPORTS:
             if name not in ("llmcache_abi_version", "llmcache_strerror", "llmcache_last_cuda_error",
                             "llmcache_fingerprint_static_error"):
@@ -648,10 +693,33 @@ class Layer:
         llmcache_layer_score_mods(self.handle, mods)
         self._mods = mods                                # keeps the arrays alive
 
+    def quantise(self, to="int8", workspace=None, stream=None):
+        """The layer's products in 8 bits (to: "int8" or "e4m3") in the calls that follow, from weights that this call brings to
+        that type on the stream; None: back to bf16.  workspace: a tensor of llmcache_layer_quantise_bytes bytes, or None."""
+        if to is not None and to not in _FORMATS:
+            raise LLMCacheError(ERR_ARG, 'quantise: "int8", "e4m3" or None')
+        if workspace is not None:
+            _same_device(self.desc.device, workspace)
+            if not workspace.is_contiguous():
+                raise LLMCacheError(ERR_ARG, "quantise: a contiguous workspace")
+        llmcache_layer_quantise(self.handle, BF16 if to is None else _FORMATS[to][0], workspace, _stream(stream, self.desc.device))
+        self._workspace8 = None if to is None else workspace
+
+    def rms(self, on=True):
+        """Root-mean-square norms in place of both layer norms in the calls that follow."""
+        llmcache_layer_rms(self.handle, int(bool(on)))
+
+    def rotation(self, rotation: Optional[Rotation]):
+        """Queries and keys turned by their positions (make_rotation) in the calls that follow; None switches it off."""
+        if rotation is not None:
+            _same_device(self.desc.device, *getattr(rotation, "tensors", ()))
+        llmcache_layer_rotation(self.handle, rotation)
+        self._rotation = rotation                        # keeps the angles alive
+
     def extend(self, cache: "KVCache", x, out, *, cu_rows, lens, pages, longest=0, weights=None, decay=1.0, positions=None,
                first=None, stream=None):
         """The layer on new tokens: x, out [n_rows, d]; the other arguments as in KVCache.attention (rows beyond `longest` get
-        the layer's result for an attention of zero)."""
+        the layer's result for an attention of zero; a layer with a rotation takes `first` without positions too)."""
         chunk = cache.chunk(x.shape[0], cu_rows=cu_rows, lens=lens, pages=pages, longest=longest, weights=weights, decay=decay,
                             positions=positions, first=first)
         _want(x, torch.bfloat16, 2, "x")
@@ -794,6 +862,114 @@ def _check_mods(mods, heads, device, S=0, n=0, layer_len=0):
         raise LLMCacheError(ERR_SHAPE, "doc: [n_seqs, seq_len of the layer], prefix: [n_seqs], of one sequence at least")
 
 
+# 8-bit types by name: format, torch type
+_FORMATS = {"int8": (I8, torch.int8), "e4m3": (E4M3, torch.float8_e4m3fn)}
+_FORMAT_OF = {torch.int8: I8, torch.float8_e4m3fn: E4M3}
+_NORMS = {"none": NORM_NONE, "layer": NORM_LAYER, "rms": NORM_RMS}
+_ACTS = {"none": ACT_NONE, "gelu_erf": ACT_GELU_ERF, "gelu_tanh": ACT_GELU_TANH}
+_NORM = _Packed("@6If4xQ" + "Qq" * 5 + "3Q")
+_DENSE = _Packed("@7I4xQ" + "QqQ" * 2 + "Q" + "Qq" * 2)
+_NEW = _Packed("@4I3Q" + "Q3q" * 4 + "4Q")
+
+
+def _matrix(t, dtype, name, device, shape=None):
+    """(address, leading dimension) of a matrix whose rows are dense."""
+    if t is None:
+        return 0, 0
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != 2:
+        raise LLMCacheError(ERR_ARG, f"{name}: a {dtype} tensor of 2 dimensions is expected")
+    if shape is not None and t.shape != shape:
+        raise LLMCacheError(ERR_SHAPE, f"{name}: {tuple(t.shape)} where {tuple(shape)} is expected")
+    rows, cols = t.shape
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1 and rows:
+        raise LLMCacheError(ERR_SHAPE, f"{name}: rows of neighbouring elements")
+    if t.get_device() != device:
+        _other_device(t, device)
+    return t.data_ptr(), ld
+
+
+def _count(n_rows_dev, device):
+    """Address of a row count in device memory."""
+    if n_rows_dev is None:
+        return 0
+    if not isinstance(n_rows_dev, torch.Tensor) or n_rows_dev.dtype is not torch.int32 or n_rows_dev.numel() < 1:
+        raise LLMCacheError(ERR_ARG, "n_rows_dev: an int32 tensor with one element")
+    _same_device(device, n_rows_dev)
+    return n_rows_dev.data_ptr()
+
+
+def llmcache_norm(x, *, kind="rms", gain=None, bias=None, eps=1e-5, residual=None, total=None, out=None, q=None, scale=None,
+                  n_rows_dev=None, stream=None) -> None:
+    """h = x + residual -> total; its norm (kind: "rms", "layer", "none") -> out in bf16, q in 8 bits with a scale per row.
+    x, residual, total, out: bf16 [rows, cols]; gain, bias: f32 [cols]; q: int8 or float8_e4m3fn [rows, cols], scale: f32
+    [rows].  n_rows_dev: int32 on the device, only that many rows are processed."""
+    if not isinstance(x, torch.Tensor):
+        raise LLMCacheError(ERR_ARG, "llmcache_norm: x is a tensor")
+    if kind not in _NORMS:
+        raise LLMCacheError(ERR_ARG, 'llmcache_norm: kind is "rms", "layer" or "none"')
+    device, shape = x.get_device(), x.shape
+    x_at, x_ld = _matrix(x, _BF16, "x", device)
+    rows, cols = shape
+    fmt = 0
+    if q is not None:
+        fmt = _FORMAT_OF.get(getattr(q, "dtype", None))
+        if fmt is None:
+            raise LLMCacheError(ERR_ARG, "q: an int8 or float8_e4m3fn tensor")
+    a = _NORM(_NORM.size, _NORMS[kind], fmt, rows, cols, 1, eps, _count(n_rows_dev, device), x_at, x_ld,
+              *_matrix(residual, _BF16, "residual", device, shape), *_matrix(total, _BF16, "total", device, shape),
+              *_matrix(out, _BF16, "out", device, shape), *_matrix(q, getattr(q, "dtype", None), "q", device, shape),
+              _addr(scale, torch.float32, (rows,), "scale", device), _addr(gain, torch.float32, (cols,), "gain", device),
+              _addr(bias, torch.float32, (cols,), "bias", device))
+    _check(lib().llmcache_norm(a, _stream(stream)), "llmcache_norm")
+
+
+def llmcache_dense(a, a_scale, w, w_scale, out, *, bias=None, act="none", residual=None, n_rows_dev=None, stream=None) -> None:
+    """out = act(a_scale w_scale (a w^T) + bias) + residual for 8-bit a [m, k] and w [n, k] of one type (int8: exact sums;
+    float8_e4m3fn) with f32 scales [m], [n]; bias f32 [n]; out, residual bf16 [m, n].  act: "none", "gelu_erf" or "gelu_tanh".
+    n_rows_dev: int32 on the device, only that many rows are processed."""
+    if not isinstance(a, torch.Tensor) or not isinstance(w, torch.Tensor) or _FORMAT_OF.get(a.dtype) is None or w.dtype is not a.dtype:
+        raise LLMCacheError(ERR_ARG, "llmcache_dense: a and w are both int8 or both float8_e4m3fn")
+    if act not in _ACTS:
+        raise LLMCacheError(ERR_ARG, 'llmcache_dense: act is "none", "gelu_erf" or "gelu_tanh"')
+    device, dt = a.get_device(), a.dtype
+    a_at, a_ld = _matrix(a, dt, "a", device)
+    m, k = a.shape
+    w_at, w_ld = _matrix(w, dt, "w", device)
+    n = w.shape[0]
+    if w.shape[1] != k:
+        raise LLMCacheError(ERR_SHAPE, "llmcache_dense: a [m, k], w [n, k]")
+    if a_scale is None or w_scale is None or out is None:
+        raise LLMCacheError(ERR_ARG, "llmcache_dense: a_scale, w_scale and out are needed")
+    F32 = torch.float32
+    p = _DENSE(_DENSE.size, _FORMAT_OF[dt], m, n, k, _ACTS[act], 1, _count(n_rows_dev, device), a_at, a_ld,
+               _addr(a_scale, F32, (m,), "a_scale", device), w_at, w_ld, _addr(w_scale, F32, (n,), "w_scale", device),
+               _addr(bias, F32, (n,), "bias", device), *_matrix(residual, _BF16, "residual", device, (m, n)),
+               *_matrix(out, _BF16, "out", device, (m, n)))
+    _check(lib().llmcache_dense(p, _stream(stream)), "llmcache_dense")
+
+
+def llmcache_dense_status() -> int:
+    return int(lib().llmcache_dense_status())
+
+
+def llmcache_dense_debug_knobs(wait_limit_ns: int, flags: int) -> None:
+    _check(lib().llmcache_dense_debug_knobs(wait_limit_ns, flags), "llmcache_dense_debug_knobs")
+
+
+def make_rotation(inv_freq, *, interleaved=False) -> Rotation:
+    """llmcache_rotation.  inv_freq: f64 [dims / 2], the angle of each pair of columns per position.  The struct keeps the tensor
+    alive."""
+    _dense(inv_freq, torch.float64, 1, "inv_freq")
+    r = Rotation()
+    r.struct_size, r.dims, r.interleaved = C.sizeof(Rotation), 2 * inv_freq.numel(), int(interleaved)
+    if r.dims not in (16, 32, 48, 64):
+        raise LLMCacheError(ERR_SHAPE, "inv_freq: 8, 16, 24 or 32 pairs")
+    r.inv_freq = inv_freq.data_ptr()
+    r.tensors = (inv_freq,)
+    return r
+
+
 def llmcache_attention(q, k, v, out, mods: Optional[ScoreMods] = None, lse=None, n_seqs_dev=None, stream=None) -> None:
     """out = softmax(modified q k^T) v.  q, out: bf16 [n_seqs, seq_len, heads, 64]; k, v: [n_seqs, seq_len, kv_heads, 64],
     views of any strides (multiples of 8); lse: optional f32 [n_seqs, seq_len, heads]."""
@@ -858,6 +1034,29 @@ def llmcache_kv_debug_knobs(kv, wait_limit_ns: int, flags: int) -> None:
 
 def llmcache_layer_score_mods(layer, mods: Optional[ScoreMods]) -> None:
     _check(lib().llmcache_layer_score_mods(layer, C.byref(mods) if mods is not None else None), "llmcache_layer_score_mods")
+
+
+def llmcache_kv_append(kv, rows: KVNew, stream=None) -> None:
+    _check(lib().llmcache_kv_append(kv, C.byref(rows), _stream(stream)), "llmcache_kv_append")
+
+
+def llmcache_layer_quantise_bytes(layer) -> int:
+    out = C.c_size_t(0)
+    _check(lib().llmcache_layer_quantise_bytes(layer, C.byref(out)), "llmcache_layer_quantise_bytes")
+    return int(out.value)
+
+
+def llmcache_layer_quantise(layer, format, workspace=None, stream=None) -> None:
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().llmcache_layer_quantise(layer, format, _ptr(workspace), size, _stream(stream)), "llmcache_layer_quantise")
+
+
+def llmcache_layer_rotation(layer, rotation: Optional[Rotation]) -> None:
+    _check(lib().llmcache_layer_rotation(layer, C.byref(rotation) if rotation is not None else None), "llmcache_layer_rotation")
+
+
+def llmcache_layer_rms(layer, on: int) -> None:
+    _check(lib().llmcache_layer_rms(layer, on), "llmcache_layer_rms")
 
 
 def llmcache_layer_extend(layer, kv, x, chunk: KVChunk, out, stream=None) -> None:
@@ -942,6 +1141,35 @@ class KVCache:
         c = self._pack_chunk(T, cu_rows, lens, pages, longest, weights, decay, positions, first, rq, ro, rk, rv,
                              _addr(lse, torch.float32, (T, self.heads), "lse", device), mods)
         _check(lib().llmcache_kv_attention(self.handle, c, _stream(stream, device)), "llmcache_kv_attention")
+
+    def append(self, k_new, v_new, *, cu_rows, lens, pages, q=None, q_out=None, rotation=None, positions=None, first=None, stream=None):
+        """Stores k_new, rotated by position (make_rotation; None: as it is), and v_new [n_rows, kv_heads, 64] in the pages, and
+        rotates q [n_rows, heads, 64] into q_out, which may be q (llmcache_kv_append); attention follows without k_new and
+        v_new.  cu_rows, lens, pages, positions and first as in attention; first also without positions."""
+        device = self.device
+        rk = _rows(k_new, "k_new", 3, None, device)
+        T = k_new.shape[0]
+        if k_new.shape[1] != self.kv_heads:
+            raise LLMCacheError(ERR_SHAPE, "k_new, v_new: [n_rows, kv_heads, 64]")
+        rv = _rows(v_new, "v_new", 3, k_new.shape, device)
+        if (q is None) != (q_out is None):
+            raise LLMCacheError(ERR_ARG, "q and q_out come together")
+        rq = ro = _NO_ROWS
+        if q is not None:
+            shape = (T, self.heads, 64)
+            rq, ro = _rows(q, "q", 3, shape, device), _rows(q_out, "q_out", 3, shape, device)
+        if lens is None or pages is None or cu_rows is None:
+            raise LLMCacheError(ERR_ARG, "cu_rows, lens and pages are needed")
+        I32 = torch.int32
+        lens_at = _addr(lens, I32, (-1,), "lens", device)
+        S = lens.shape[0]
+        pages_at = _addr(pages, I32, (S, -1), "pages", device)
+        if rotation is not None:
+            _same_device(device, *getattr(rotation, "tensors", ()))
+        c = _NEW(_NEW.size, S, T, pages.shape[1], _addr(cu_rows, I32, (S + 1,), "cu_rows", device), lens_at, pages_at, *rk, *rv, *rq, *ro,
+                 _addr(positions, I32, (S, self.kv_heads, -1), "positions", device), _addr(first, I32, (S,), "first", device),
+                 0 if positions is None else positions.shape[-1], 0 if rotation is None else C.addressof(rotation))
+        _check(lib().llmcache_kv_append(self.handle, c, _stream(stream, device)), "llmcache_kv_append")
 
     def evict(self, *, lens, pages, weights, new_pages, new_lens, budget, recent=0, sinks=0, positions=None, new_weights=None,
               new_positions=None, kept=None, stream=None):

@@ -5,6 +5,7 @@
 #include <new>
 #include "attn.cuh"
 #include "attn_host.cuh"
+#include "kv_rotate.cuh"
 #include "ptx.cuh"
 
 using namespace llmc;
@@ -221,9 +222,63 @@ int chunk_args(const llmcache_kv* kv, const llmcache_kv_chunk* c, AttnArgs* o) {
   return LLMCACHE_OK;
 }
 
+// Checks one llmcache_kv_append and fills in the kernel's arguments; o->n_seqs == 0: nothing to do.
+int append_args(const llmcache_kv* kv, const llmcache_kv_new* c, AttnArgs* o, RotateArgs* rot) {
+  if (!kv || !c || c->struct_size != sizeof(llmcache_kv_new)) return LLMCACHE_ERR_ARG;
+  const llmcache_kv_desc& D = kv->desc;
+  AttnArgs& a = *o;
+  int rc = check_rotation(c->rotation, rot);
+  if (rc != LLMCACHE_OK) return rc;
+  if (c->n_rows > D.max_rows || c->n_seqs > D.max_seqs) return LLMCACHE_ERR_SHAPE;
+  if (c->n_seqs == 0 || c->n_rows == 0) return LLMCACHE_OK;
+  if ((rc = check_side(kv, c->n_seqs, c->pages_ld, c->lens, c->pages, c->positions != nullptr, c->side_ld)) != LLMCACHE_OK) return rc;
+  if (!c->cu_rows || !aligned(c->cu_rows, 4) || !aligned(c->positions, 4) || !aligned(c->first, 4)) return LLMCACHE_ERR_ARG;
+  if ((rc = take_rows(&c->k_new, 1, c->n_rows, D.kv_heads, &a.k)) != LLMCACHE_OK) return rc;
+  if ((rc = take_rows(&c->v_new, 1, c->n_rows, D.kv_heads, &a.v)) != LLMCACHE_OK) return rc;
+  if ((c->q.ptr == nullptr) != (c->q_out.ptr == nullptr)) return LLMCACHE_ERR_ARG;
+  if (c->q.ptr) {
+    if ((rc = take_rows(&c->q, 1, c->n_rows, D.heads, &a.q)) != LLMCACHE_OK) return rc;
+    if ((rc = take_rows(&c->q_out, 1, c->n_rows, D.heads, &a.out)) != LLMCACHE_OK) return rc;
+  }
+  a.heads = D.heads; a.kv_heads = D.kv_heads; a.group = D.heads / D.kv_heads;
+  a.n_seqs = c->n_seqs; a.n = c->n_rows;
+  a.cu = c->cu_rows; a.lens = c->lens; a.pages = c->pages; a.first = c->first; a.positions = c->positions;
+  a.n_rows = c->n_rows; a.pages_ld = c->pages_ld; a.num_pages = D.num_pages; a.page_shift = log2_of(D.page_size);
+  a.max_len = D.max_len; a.side_ld = c->side_ld; a.page_stride = D.page_stride;
+  a.k_pages = (__nv_bfloat16*)D.k_pages; a.v_pages = (__nv_bfloat16*)D.v_pages;
+  if (rot->dims && !pointer_on_device(rot->inv_freq, D.device)) return LLMCACHE_ERR_ARG;
+  return LLMCACHE_OK;
+}
+
 }  // namespace
 
 namespace llmc {
+int check_rotation(const llmcache_rotation* r, RotateArgs* o) {
+  *o = RotateArgs{nullptr, 0u, 0u};
+  if (!r) return LLMCACHE_OK;
+  if (r->struct_size != sizeof(llmcache_rotation) || r->interleaved > 1 || !r->inv_freq || !aligned(r->inv_freq, 8)) return LLMCACHE_ERR_ARG;
+  if (r->dims == 0 || r->dims % 16 || r->dims > 64) return LLMCACHE_ERR_SHAPE;
+  *o = RotateArgs{r->inv_freq, r->dims, r->interleaved};
+  return LLMCACHE_OK;
+}
+
+int kv_check_append(const llmcache_kv* kv, const llmcache_kv_new* c) {
+  AttnArgs a{};
+  RotateArgs r;
+  return append_args(kv, c, &a, &r);
+}
+
+int kv_append(llmcache_kv* kv, const llmcache_kv_new* c, const RotateArgs* rotate, cudaStream_t st) {
+  AttnArgs a{};
+  RotateArgs r;
+  const int rc = append_args(kv, c, &a, &r);
+  if (rc != LLMCACHE_OK || a.n_seqs == 0) return rc;
+  if (rotate) r = *rotate;
+  OnDevice on(kv->desc.device);
+  if (!on.ok) return LLMCACHE_ERR_CUDA;
+  return done(launch_kv_rotate(a, r, kv->sm_count, st));
+}
+
 int kv_check_chunk(const llmcache_kv* kv, const llmcache_kv_chunk* c) {
   AttnArgs a{};
   return chunk_args(kv, c, &a);
@@ -245,7 +300,7 @@ int kv_attend(llmcache_kv* kv, const llmcache_kv_chunk* c, bool zero_rest, cudaS
   }
   OnDevice on(kv->desc.device);
   if (!on.ok) return LLMCACHE_ERR_CUDA;
-  if (!attn_is_few(a) && (a.k.ptr || a.positions || (a.weights && a.decay != 0.f))) {
+  if (!attn_is_few(a) && (a.k.ptr || a.positions || a.zero_rest || (a.weights && a.decay != 0.f))) {
     const cudaError_t e = launch_kv_append(a, kv->sm_count, st);
     if (e != cudaSuccess) return done(e);
   }
@@ -376,6 +431,10 @@ int llmcache_kv_destroy(llmcache_kv_t* kv) {
 
 int llmcache_kv_attention(llmcache_kv_t* kv, const llmcache_kv_chunk* c, void* stream) {
   return kv_attend(kv, c, false, (cudaStream_t)stream);
+}
+
+int llmcache_kv_append(llmcache_kv_t* kv, const llmcache_kv_new* c, void* stream) {
+  return kv_append(kv, c, nullptr, (cudaStream_t)stream);
 }
 
 int llmcache_kv_evict(llmcache_kv_t* kv, const llmcache_kv_eviction* v, void* stream) {

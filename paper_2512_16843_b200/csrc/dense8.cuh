@@ -1,0 +1,50 @@
+// 8-bit operators (norm with an 8-bit output, product of two 8-bit matrices): shared declarations.
+#pragma once
+#include "layer.cuh"
+
+namespace llmc {
+
+enum { NORM_NONE = LLMCACHE_NORM_NONE, NORM_LAYER = LLMCACHE_NORM_LAYER, NORM_RMS = LLMCACHE_NORM_RMS };
+
+// llmcache_norm_args, checked; leading dimensions in elements
+struct NormArgs {
+  const __nv_bfloat16 *x, *residual;
+  __nv_bfloat16 *total, *out;
+  const float *gain, *bias;
+  uint8_t* q;
+  float* scale;
+  long long x_ld, residual_ld, total_ld, out_ld, q_ld;
+  uint32_t n_rows, cols, kind, format;
+  float eps;
+  const uint32_t* count_dev;       // rows = min(n_rows, *count_dev * rows_per_count), or n_rows
+  uint32_t rows_per_count;
+};
+cudaError_t launch_norm(const NormArgs& a, int sm_count, cudaStream_t st);
+
+// llmcache_dense_args, checked; leading dimensions in elements
+struct DenseArgs {
+  const uint8_t *a, *w;
+  const float *a_scale, *w_scale, *bias;
+  const __nv_bfloat16* residual;
+  __nv_bfloat16* out;
+  long long a_ld, w_ld, residual_ld, out_ld;
+  uint32_t m, n, k, act, format;
+  const uint32_t* count_dev;       // rows = min(m, *count_dev * rows_per_count), or m
+  uint32_t rows_per_count;
+  uint32_t* status;
+  VtOut vt;                        // the layer's transposed V columns
+};
+cudaError_t setup_dense8_tc();
+cudaError_t launch_dense8_tc(const DenseArgs& a, int sm_count, cudaStream_t st);
+constexpr uint32_t DENSE_FEW = 64;                 // most rows that k_dense8_few takes
+cudaError_t launch_dense8_few(const DenseArgs& a, int sm_count, cudaStream_t st);
+cudaError_t launch_dense8(const DenseArgs& a, int sm_count, cudaStream_t st);
+
+// rows of a call whose number may stand in device memory
+__device__ __forceinline__ uint32_t rows_of(uint32_t most, const uint32_t* count_dev, uint32_t rows_per_count) {
+  if (!count_dev) return most;
+  const unsigned long long m = (unsigned long long)(*count_dev) * rows_per_count;
+  return m < most ? (uint32_t)m : most;
+}
+
+}  // namespace llmc

@@ -4,6 +4,8 @@
 #include <new>
 #include "layer.cuh"
 #include "attn_host.cuh"
+#include "dense8.cuh"
+#include "kv_rotate.cuh"
 #include "ptx.cuh"
 
 using namespace llmc;
@@ -17,6 +19,13 @@ struct llmcache_layer {
   uint32_t* status = nullptr;    // device word: a bounded wait expired
   bool has_mods = false;         // llmcache_layer_score_mods
   ScoreArgs mods{};
+  bool rms = false;              // llmcache_layer_rms
+  RotateArgs rotate{nullptr, 0u, 0u};            // llmcache_layer_rotation; dims 0: none
+  uint32_t format = LLMCACHE_BF16;               // of the products (llmcache_layer_quantise)
+  char* ws8 = nullptr;                           // 8-bit weights and their scales
+  bool owns_ws8 = false;
+  const uint8_t* w8[4] = {};                     // q|k|v, o, 1, 2
+  const float* s8[4] = {};
 };
 
 namespace llmc {
@@ -64,6 +73,105 @@ AttnArgs layer_attn_args(const llmcache_layer* L, uint32_t n_seqs, const uint32_
   a.status = L->status;
   return a;
 }
+
+enum { P_QKV = 0, P_O = 1, P_1 = 2, P_2 = 3 };                   // the layer's products
+struct Eight { uint8_t* q; float* scale; long long ld; };       // rows in 8 bits
+
+// The norms and products of one forward or extend call, in the layer's number format.  After an error nothing more is launched.
+struct LayerSteps {
+  const llmcache_layer* L;
+  uint32_t rows;
+  const uint32_t* count;         // rows = min(rows, *count * per)
+  uint32_t per;
+  cudaStream_t st;
+  cudaError_t e = cudaSuccess;
+
+  bool in8() const { return L->format != LLMCACHE_BF16; }
+  // rows of d bytes and their scales in the memory of a [rows, d] bf16 matrix: d >= 64, so the scales fit behind them
+  Eight eight_in(__nv_bfloat16* m) const {
+    const size_t most = (size_t)L->desc.max_seqs * L->desc.seq_len * L->desc.d_model;
+    return Eight{(uint8_t*)m, (float*)((char*)m + most), (long long)L->desc.d_model};
+  }
+  // rows of f in 8 bits: each in the first half of its own place (the kernel reads a row before it writes it); the scales
+  // where the q|k|v rows were
+  Eight eight_f() const { return Eight{(uint8_t*)L->f, (float*)L->qkv, 2ll * L->desc.ffn}; }
+
+  void run_norm(uint32_t kind, const __nv_bfloat16* x, uint32_t cols, const float* g, const float* b, __nv_bfloat16* y, const Eight* q) {
+    if (e != cudaSuccess) return;
+    NormArgs a{};
+    a.x = x; a.out = y; a.gain = g; a.bias = b;
+    a.x_ld = a.out_ld = cols;
+    if (q) { a.q = q->q; a.scale = q->scale; a.q_ld = q->ld; a.format = L->format; }
+    a.n_rows = rows; a.cols = cols; a.kind = kind; a.eps = L->desc.eps;
+    a.count_dev = count; a.rows_per_count = per;
+    e = launch_norm(a, L->sm_count, st);
+  }
+  // the layer's norm of x: y in bf16, q in 8 bits (either may be null)
+  void norm(const __nv_bfloat16* x, const float* g, const float* b, __nv_bfloat16* y, const Eight* q) {
+    if (e != cudaSuccess) return;
+    if (L->rms || q) run_norm(L->rms ? NORM_RMS : NORM_LAYER, x, L->desc.d_model, g, b, y, q);
+    else e = launch_layernorm(x, g, b, y, rows, L->desc.d_model, count, per, L->desc.eps, L->sm_count, st);
+  }
+  void to8(const __nv_bfloat16* x, uint32_t cols, const Eight& q) { run_norm(NORM_NONE, x, cols, nullptr, nullptr, nullptr, &q); }
+  // product `which` of x (8-bit layers: of q)
+  void product(int which, const __nv_bfloat16* x, const Eight& q, const void* w, const float* bias, const __nv_bfloat16* res,
+               __nv_bfloat16* o, uint32_t N, uint32_t K, uint32_t act, VtOut vt = VtOut{nullptr, 0, 0, 0}) {
+    if (e != cudaSuccess) return;
+    if (!in8()) {
+      e = launch_gemm(x, (const __nv_bfloat16*)w, bias, res, o, L->status, rows, N, K, count, per, act, L->sm_count, st, vt);
+      return;
+    }
+    DenseArgs a{};
+    a.a = q.q; a.a_scale = q.scale; a.a_ld = q.ld;
+    a.w = L->w8[which]; a.w_scale = L->s8[which]; a.w_ld = K;
+    a.bias = bias; a.residual = res; a.residual_ld = N; a.out = o; a.out_ld = N;
+    a.m = rows; a.n = N; a.k = K; a.act = act; a.format = L->format;
+    a.count_dev = count; a.rows_per_count = per;
+    a.status = L->status;
+    a.vt = vt;
+    e = launch_dense8(a, L->sm_count, st);
+  }
+
+  // from the layer's input to q|k|v
+  void before_attention(const __nv_bfloat16* X, VtOut vt) {
+    const llmcache_layer_desc& D = L->desc;
+    const Eight y8 = eight_in(L->y);
+    if (D.pre_ln) norm(X, D.ln1_g, D.ln1_b, in8() ? nullptr : L->y, in8() ? &y8 : nullptr);
+    else if (in8()) to8(X, D.d_model, y8);
+    product(P_QKV, D.pre_ln ? L->y : X, y8, D.w_qkv, D.b_qkv, nullptr, L->qkv, 3 * D.d_model, D.d_model, LAYER_ACT_NONE, vt);
+  }
+  // from the attention's output to the layer's
+  void behind_attention(const __nv_bfloat16* X, __nv_bfloat16* O) {
+    const llmcache_layer_desc& D = L->desc;
+    const uint32_t d = D.d_model, act = D.tanh_gelu ? LAYER_ACT_GELU_TANH : LAYER_ACT_GELU_ERF;
+    const Eight y8 = eight_in(L->y), a8 = eight_in(L->a), f8 = eight_f();
+    if (in8()) to8(L->a, d, y8);
+    product(P_O, L->a, y8, D.w_o, D.b_o, X, L->t, d, d, LAYER_ACT_NONE);
+    // post-norm: y is the next residual too, so its 8 bits go where the attention's output was
+    norm(L->t, D.pre_ln ? D.ln2_g : D.ln1_g, D.pre_ln ? D.ln2_b : D.ln1_b, in8() && D.pre_ln ? nullptr : L->y, in8() ? &a8 : nullptr);
+    product(P_1, L->y, a8, D.w_1, D.b_1, nullptr, L->f, D.ffn, d, act);
+    if (in8()) to8(L->f, D.ffn, f8);
+    product(P_2, L->f, f8, D.w_2, D.b_2, D.pre_ln ? L->t : L->y, D.pre_ln ? O : L->t, d, D.ffn, LAYER_ACT_NONE);
+    if (!D.pre_ln) norm(L->t, D.ln2_g, D.ln2_b, O, nullptr);
+  }
+};
+
+// sizes of the weight matrices: rows (output channels) and columns
+void weight_shape(const llmcache_layer_desc& D, int which, uint32_t* rows, uint32_t* cols) {
+  const uint32_t d = D.d_model;
+  *rows = which == P_QKV ? 3 * d : which == P_1 ? D.ffn : d;
+  *cols = which == P_2 ? D.ffn : d;
+}
+size_t layer_ws8_bytes(const llmcache_layer_desc& D) {
+  size_t total = 0;
+  for (int w = 0; w < 4; ++w) {
+    uint32_t r, c;
+    weight_shape(D, w, &r, &c);
+    total += up256((size_t)r * c) + up256((size_t)r * 4);
+  }
+  return total;
+}
+constexpr uint32_t NORM_MOST = 16384;      // columns of a row that k_norm takes
 }  // namespace
 
 extern "C" {
@@ -136,6 +244,7 @@ int llmcache_layer_destroy(llmcache_layer_t* L) {
   cudaSetDevice(L->desc.device);
   cudaError_t e = cudaDeviceSynchronize();
   if (L->owns_ws) cudaFree(L->ws);
+  if (L->owns_ws8) cudaFree(L->ws8);
   cudaSetDevice(prev);
   delete L;
   return e == cudaSuccess ? LLMCACHE_OK : LLMCACHE_ERR_CUDA;
@@ -153,43 +262,24 @@ int llmcache_layer_forward(llmcache_layer_t* L, const void* x, uint32_t n_seqs, 
   if (prev != L->desc.device && cudaSetDevice(L->desc.device) != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
   const llmcache_layer_desc& D = L->desc;
   const uint32_t n = D.seq_len, d = D.d_model, T = n_seqs * n;
-  const uint32_t act = D.tanh_gelu ? LAYER_ACT_GELU_TANH : LAYER_ACT_GELU_ERF;
   cudaStream_t st = (cudaStream_t)stream;
   const __nv_bfloat16* X = (const __nv_bfloat16*)x;
-  __nv_bfloat16* O = (__nv_bfloat16*)out;
-  const int sm = L->sm_count;
-  cudaError_t e;
-  auto gemm = [&](const __nv_bfloat16* a, const void* w, const float* bias, const __nv_bfloat16* res,
-                  __nv_bfloat16* o, uint32_t N, uint32_t K, uint32_t a_, VtOut vt = VtOut{nullptr, 0, 0, 0}) {
-    return launch_gemm(a, (const __nv_bfloat16*)w, bias, res, o, L->status, T, N, K, n_seqs_dev, n, a_, sm, st, vt);
-  };
+  LayerSteps steps{L, T, n_seqs_dev, n, st};
+  cudaError_t& e = steps.e;
   // the V third of the q|k|v product is written transposed per head (what the attention kernel reads); the kernel with
   // score modifiers reads all of q|k|v from the one matrix
-  const VtOut vt_out = L->has_mods ? VtOut{nullptr, 0, 0, 0} : VtOut{L->vt, 2 * d, attention_vt_pitch(n), D.heads};
-  auto attend = [&]() -> cudaError_t {
-    if (!L->has_mods) return launch_attention_tc(L->qkv, L->vt, L->a, L->status, n, d, D.heads, n_seqs, n_seqs_dev, D.causal, st);
-    return launch_attn(layer_attn_args(L, n_seqs, n_seqs_dev), AttnScratch{}, sm, st);
-  };
-  auto ln = [&](const __nv_bfloat16* in, const float* g, const float* b, __nv_bfloat16* o) {
-    return launch_layernorm(in, g, b, o, T, d, n_seqs_dev, n, D.eps, sm, st);
-  };
-  if (!D.pre_ln) {
-    e = gemm(X, D.w_qkv, D.b_qkv, nullptr, L->qkv, 3 * d, d, LAYER_ACT_NONE, vt_out);
-    if (e == cudaSuccess) e = attend();
-    if (e == cudaSuccess) e = gemm(L->a, D.w_o, D.b_o, X, L->t, d, d, LAYER_ACT_NONE);
-    if (e == cudaSuccess) e = ln(L->t, D.ln1_g, D.ln1_b, L->y);
-    if (e == cudaSuccess) e = gemm(L->y, D.w_1, D.b_1, nullptr, L->f, D.ffn, d, act);
-    if (e == cudaSuccess) e = gemm(L->f, D.w_2, D.b_2, L->y, L->t, d, D.ffn, LAYER_ACT_NONE);
-    if (e == cudaSuccess) e = ln(L->t, D.ln2_g, D.ln2_b, O);
-  } else {
-    e = ln(X, D.ln1_g, D.ln1_b, L->y);
-    if (e == cudaSuccess) e = gemm(L->y, D.w_qkv, D.b_qkv, nullptr, L->qkv, 3 * d, d, LAYER_ACT_NONE, vt_out);
-    if (e == cudaSuccess) e = attend();
-    if (e == cudaSuccess) e = gemm(L->a, D.w_o, D.b_o, X, L->t, d, d, LAYER_ACT_NONE);
-    if (e == cudaSuccess) e = ln(L->t, D.ln2_g, D.ln2_b, L->y);
-    if (e == cudaSuccess) e = gemm(L->y, D.w_1, D.b_1, nullptr, L->f, D.ffn, d, act);
-    if (e == cudaSuccess) e = gemm(L->f, D.w_2, D.b_2, L->t, O, d, D.ffn, LAYER_ACT_NONE);
+  steps.before_attention(X, L->has_mods ? VtOut{nullptr, 0, 0, 0} : VtOut{L->vt, 2 * d, attention_vt_pitch(n), D.heads});
+  if (e == cudaSuccess && L->rotate.dims) {
+    AttnArgs r = layer_attn_args(L, n_seqs, n_seqs_dev);
+    r.out = r.q;
+    r.n_rows = T;
+    r.q.seq = r.k.seq = r.out.seq = 0;                     // (rows are numbered through)
+    e = launch_kv_rotate(r, L->rotate, L->sm_count, st);
   }
+  if (e == cudaSuccess)
+    e = L->has_mods ? launch_attn(layer_attn_args(L, n_seqs, n_seqs_dev), AttnScratch{}, L->sm_count, st)
+                    : launch_attention_tc(L->qkv, L->vt, L->a, L->status, n, d, D.heads, n_seqs, n_seqs_dev, D.causal, st);
+  steps.behind_attention(X, (__nv_bfloat16*)out);
   if (prev != L->desc.device) cudaSetDevice(prev);
   if (e != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
   return LLMCACHE_OK;
@@ -207,6 +297,87 @@ int llmcache_layer_score_mods(llmcache_layer_t* L, const llmcache_score_mods* mo
   L->mods = m;
   L->has_mods = true;
   return LLMCACHE_OK;
+}
+
+int llmcache_layer_rms(llmcache_layer_t* L, uint32_t on) {
+  if (!L || on > 1) return LLMCACHE_ERR_ARG;
+  if (on && L->desc.d_model > NORM_MOST) return LLMCACHE_ERR_UNSUPPORTED;
+  L->rms = on != 0;
+  return LLMCACHE_OK;
+}
+
+int llmcache_layer_rotation(llmcache_layer_t* L, const llmcache_rotation* rotation) {
+  if (!L) return LLMCACHE_ERR_ARG;
+  RotateArgs r;
+  const int rc = check_rotation(rotation, &r);
+  if (rc != LLMCACHE_OK) return rc;
+  if (r.dims && !pointer_on_device(r.inv_freq, L->desc.device)) return LLMCACHE_ERR_ARG;
+  L->rotate = r;
+  return LLMCACHE_OK;
+}
+
+int llmcache_layer_quantise_bytes(llmcache_layer_t* L, size_t* bytes_out) {
+  if (!L || !bytes_out) return LLMCACHE_ERR_ARG;
+  *bytes_out = layer_ws8_bytes(L->desc);
+  return LLMCACHE_OK;
+}
+
+int llmcache_layer_quantise(llmcache_layer_t* L, uint32_t format, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!L) return LLMCACHE_ERR_ARG;
+  if (format != LLMCACHE_BF16 && format != LLMCACHE_I8 && format != LLMCACHE_E4M3) return LLMCACHE_ERR_ARG;
+  const llmcache_layer_desc& D = L->desc;
+  const size_t need = layer_ws8_bytes(D);
+  if (format != LLMCACHE_BF16) {
+    if (D.d_model > NORM_MOST || D.ffn > NORM_MOST) return LLMCACHE_ERR_UNSUPPORTED;
+    if ((uintptr_t)workspace % WS_ALIGN) return LLMCACHE_ERR_ARG;
+    if (workspace && workspace_bytes < need) return LLMCACHE_ERR_NOMEM;
+    if (workspace && !pointer_on_device(workspace, D.device)) return LLMCACHE_ERR_ARG;
+  }
+  int prev = 0;
+  cudaGetDevice(&prev);
+  if (prev != D.device && cudaSetDevice(D.device) != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
+  cudaError_t e = cudaSuccess;
+  int rc = LLMCACHE_OK;
+  if (L->format != LLMCACHE_BF16) {                        // calls in flight still read the weights that are there
+    e = cudaDeviceSynchronize();
+    if (L->owns_ws8) cudaFree(L->ws8);
+    L->ws8 = nullptr;
+    L->owns_ws8 = false;
+    L->format = LLMCACHE_BF16;
+  }
+  if (e == cudaSuccess && format != LLMCACHE_BF16) {
+    e = setup_dense8_tc();
+    L->ws8 = (char*)workspace;
+    if (e == cudaSuccess && !workspace) {
+      if (cudaMalloc((void**)&L->ws8, need) != cudaSuccess) { cudaGetLastError(); L->ws8 = nullptr; rc = LLMCACHE_ERR_NOMEM; }
+      else L->owns_ws8 = true;
+    }
+    char* at = L->ws8;
+    const void* from[4] = {D.w_qkv, D.w_o, D.w_1, D.w_2};
+    for (int w = 0; w < 4 && e == cudaSuccess && rc == LLMCACHE_OK; ++w) {
+      uint32_t r, c;
+      weight_shape(D, w, &r, &c);
+      NormArgs a{};
+      a.x = (const __nv_bfloat16*)from[w]; a.x_ld = c;
+      a.q = (uint8_t*)at; a.q_ld = c; at += up256((size_t)r * c);
+      a.scale = (float*)at; at += up256((size_t)r * 4);
+      a.n_rows = r; a.cols = c; a.kind = NORM_NONE; a.format = format; a.rows_per_count = 1;
+      e = launch_norm(a, L->sm_count, (cudaStream_t)stream);
+      L->w8[w] = a.q;
+      L->s8[w] = a.scale;
+    }
+    if (e == cudaSuccess && rc == LLMCACHE_OK) {
+      L->format = format;
+    } else if (L->owns_ws8) {
+      cudaDeviceSynchronize();
+      cudaFree(L->ws8);
+      L->ws8 = nullptr;
+      L->owns_ws8 = false;
+    }
+  }
+  if (prev != D.device) cudaSetDevice(prev);
+  if (e != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
+  return rc;
 }
 
 int llmcache_layer_extend(llmcache_layer_t* L, llmcache_kv_t* kv, const void* x, const llmcache_kv_chunk* chunk,
@@ -231,38 +402,32 @@ int llmcache_layer_extend(llmcache_layer_t* L, llmcache_kv_t* kv, const void* x,
   c.v_new = llmcache_rows{L->qkv + 2 * d, 0, 3ll * d, 64};
   c.out = llmcache_rows{L->a, 0, (int64_t)d, 64};
   c.mods = &m;
+  llmcache_kv_new nw{};                                    // rotated rows go into the cache ahead of the attention
+  if (L->rotate.dims) {
+    nw.struct_size = sizeof(nw);
+    nw.n_seqs = c.n_seqs; nw.n_rows = c.n_rows; nw.pages_ld = c.pages_ld;
+    nw.cu_rows = c.cu_rows; nw.lens = c.lens; nw.pages = c.pages;
+    nw.k_new = c.k_new; nw.v_new = c.v_new; nw.q = nw.q_out = c.q;
+    nw.positions = c.positions; nw.first = c.first; nw.side_ld = c.side_ld;
+    c.k_new = c.v_new = llmcache_rows{nullptr, 0, 0, 0};
+    if (!c.positions) c.first = nullptr;                   // (without positions only the rotation asks for it)
+  }
   rc = kv_check_chunk(kv, &c);
+  if (rc == LLMCACHE_OK && L->rotate.dims) rc = kv_check_append(kv, &nw);
   if (rc != LLMCACHE_OK || T == 0 || c.n_seqs == 0) return rc;
 
   int prev = 0;
   cudaGetDevice(&prev);
   if (prev != D.device && cudaSetDevice(D.device) != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
   cudaStream_t st = (cudaStream_t)stream;
-  const int sm = L->sm_count;
-  const uint32_t act = D.tanh_gelu ? LAYER_ACT_GELU_TANH : LAYER_ACT_GELU_ERF;
-  // rows behind the last sequence are neither computed nor written
-  const uint32_t* rows = (const uint32_t*)(c.cu_rows + c.n_seqs);
   const __nv_bfloat16* X = (const __nv_bfloat16*)x;
-  __nv_bfloat16* O = (__nv_bfloat16*)out;
-  cudaError_t e = cudaSuccess;
-  auto gemm = [&](const __nv_bfloat16* a, const void* w, const float* bias, const __nv_bfloat16* res, __nv_bfloat16* o,
-                  uint32_t N, uint32_t K, uint32_t a_) {
-    if (e == cudaSuccess)
-      e = launch_gemm(a, (const __nv_bfloat16*)w, bias, res, o, L->status, T, N, K, rows, 1, a_, sm, st);
-  };
-  auto ln = [&](const __nv_bfloat16* in, const float* g, const float* b, __nv_bfloat16* o) {
-    if (e == cudaSuccess) e = launch_layernorm(in, g, b, o, T, d, rows, 1, D.eps, sm, st);
-  };
-  if (D.pre_ln) ln(X, D.ln1_g, D.ln1_b, L->y);
-  gemm(D.pre_ln ? L->y : X, D.w_qkv, D.b_qkv, nullptr, L->qkv, 3 * d, d, LAYER_ACT_NONE);
-  if (e == cudaSuccess) rc = kv_attend(kv, &c, true, st);
-  if (rc == LLMCACHE_OK) {
-    gemm(L->a, D.w_o, D.b_o, X, L->t, d, d, LAYER_ACT_NONE);
-    ln(L->t, D.pre_ln ? D.ln2_g : D.ln1_g, D.pre_ln ? D.ln2_b : D.ln1_b, L->y);
-    gemm(L->y, D.w_1, D.b_1, nullptr, L->f, D.ffn, d, act);
-    gemm(L->f, D.w_2, D.b_2, D.pre_ln ? L->t : L->y, D.pre_ln ? O : L->t, d, D.ffn, LAYER_ACT_NONE);
-    if (!D.pre_ln) ln(L->t, D.ln2_g, D.ln2_b, O);
-  }
+  // rows behind the last sequence are neither computed nor written
+  LayerSteps steps{L, T, (const uint32_t*)(c.cu_rows + c.n_seqs), 1, st};
+  cudaError_t& e = steps.e;
+  steps.before_attention(X, VtOut{nullptr, 0, 0, 0});
+  if (e == cudaSuccess && L->rotate.dims) rc = kv_append(kv, &nw, &L->rotate, st);
+  if (e == cudaSuccess && rc == LLMCACHE_OK) rc = kv_attend(kv, &c, true, st);
+  if (rc == LLMCACHE_OK) steps.behind_attention(X, (__nv_bfloat16*)out);
   if (prev != D.device) cudaSetDevice(prev);
   if (e != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
   return rc;

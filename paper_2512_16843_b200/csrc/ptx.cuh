@@ -111,6 +111,21 @@ __device__ __forceinline__ void tc_mma_bf16(uint32_t d_tmem, uint64_t a_desc, ui
       "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
+// the same for 8-bit operands, 32 of them per step: signed integers summed in 32-bit integers, e4m3 in fp32
+__device__ __forceinline__ void tc_mma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
 // 32 lanes x 32 consecutive fp32 columns: thread i of the warp receives lane (base + i)
 __device__ __forceinline__ void tc_ld_32x32(uint32_t taddr, uint32_t (&v)[32]) {
   asm volatile(
@@ -171,5 +186,11 @@ bool make_tensor_map_bf16_pitch(CUtensorMap* map, const void* ptr, uint64_t rows
 // boxes of 32 columns x 32 rows (64 bytes per row, 64-byte swizzle) of a dense [rows, cols] bf16 matrix: the
 // pieces in which a warp of the dense layers' epilogue stores its output and fetches the residual
 bool make_tensor_map_bf16_box32(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t cols);
+// the same for rows that are `pitch` elements apart (a multiple of 8).  A store cuts off whole pieces of 16 bytes beyond cols:
+// where cols is no multiple of 8, the piece that holds the last column is written whole
+bool make_tensor_map_bf16_box32_pitch(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t cols, uint64_t pitch);
+// 8-bit [rows, k] matrix whose rows are `pitch` bytes apart (a multiple of 16), boxes of box_rows x 128 bytes, 128-byte
+// swizzle, zero fill outside
+bool make_tensor_map_8bit(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t k, uint64_t pitch, uint32_t box_rows);
 
 }  // namespace llmc
