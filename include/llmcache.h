@@ -643,9 +643,9 @@ typedef struct llmcache_norm_args {
 /* out[i][j] = bf16( act( a_scale[i] * w_scale[j] * sum_c a[i][c] * w[j][c] + bias[j] ) + residual[i][j] ),  i < m, j < n, c < k.
  * The sum is exact for LLMCACHE_I8 (32-bit integers) and f32 for LLMCACHE_E4M3; the rest is f32.  a and w have the same format.  a_ld and
  * w_ld count bytes from row to row, multiples of 16 and at least k; out_ld and residual_ld count elements, multiples of 8 and at
- * least n, which may be any number (columns n.. of out stay as they were).  They are not looked at where there is one row.  a, w, out and residual are 16-byte aligned.
- * residual may be out itself (same address, same leading dimension); out overlaps nothing otherwise.  GELU with erf
- * is within 8.2e-5 of the function for arguments below 26 in magnitude (beyond that within 3.2e-6 times the argument), as in the layer. */
+ * least n, which may be any number (columns n.. of out stay as they were).  They are not looked at where there is one row.  a, w,
+ * w_scale, bias, out and residual are 16-byte aligned.  residual may be out itself (same address, same leading dimension); out overlaps nothing
+ * otherwise.  GELU is within 3.8e-5 of the function. */
 typedef struct llmcache_dense_args {
   uint32_t struct_size;
   uint32_t format;           /* LLMCACHE_I8 | LLMCACHE_E4M3 */

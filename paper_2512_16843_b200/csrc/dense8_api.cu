@@ -110,7 +110,7 @@ int llmcache_dense(const llmcache_dense_args* v, void* stream) {
   for (const void* p : needed)
     if (!p) return LLMCACHE_ERR_ARG;
   if (!aligned(v->a, 16) || !aligned(v->w, 16) || !aligned(v->out, 16) || !aligned(v->residual, 16) || !aligned(v->a_scale, 4) ||
-      !aligned(v->w_scale, 4) || !aligned(v->bias, 4) || !aligned(v->count_dev, 4))
+      !aligned(v->w_scale, 16) || !aligned(v->bias, 16) || !aligned(v->count_dev, 4))
     return LLMCACHE_ERR_ARG;
   DenseArgs a{};
   if (!take_ld(v->a_ld, v->m, v->k, 16, &a.a_ld) || !take_ld(v->w_ld, v->n, v->k, 16, &a.w_ld) ||

@@ -89,10 +89,13 @@ __global__ void __launch_bounds__(512) k_dense8_few(const DenseArgs p) {
       for (uint32_t w = 0; w < warps; ++w) v += __uint_as_float(sums[w * NT * 8 * FEW_CH + e]);
     }
     // the same operations as in dense8_tc.cu
-    v = fmaf(v * p.a_scale[m], p.w_scale[n], p.bias ? p.bias[n] : 0.f);
-    if (p.act == LAYER_ACT_GELU_ERF) v = gelu_erf_f(v);
-    if (p.act == LAYER_ACT_GELU_TANH) v = gelu_tanh_f(v);
-    if (p.residual) v += __bfloat162float(p.residual[(long long)m * p.residual_ld + n]);
+    v = fmaf(__fmul_rn(v, p.a_scale[m]), p.w_scale[n], p.bias ? p.bias[n] : 0.f);
+    const float r = p.residual ? __bfloat162float(p.residual[(long long)m * p.residual_ld + n]) : 0.f;
+    if (p.act == LAYER_ACT_NONE) v = p.residual ? __fadd_rn(v, r) : v;
+    else {
+      const float phi = p.act == LAYER_ACT_GELU_ERF ? gelu_phi_f<false>(v) : gelu_phi_f<true>(v);
+      v = p.residual ? fmaf(v, phi, r) : __fmul_rn(v, phi);
+    }
     p.out[(long long)m * p.out_ld + n] = __float2bfloat16_rn(v);
   }
 }

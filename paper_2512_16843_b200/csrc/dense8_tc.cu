@@ -1,9 +1,17 @@
 // Product of two 8-bit matrices on the tensor cores:
 //   out[m, n] = act(a_scale[m] w_scale[n] sum_k a[m, k] w[n, k] + bias[n]) (+ residual[m, n]),   bf16 out
-// int8 is summed in 32-bit integers (exact: k <= 131,056), e4m3 in fp32.  Tiles of 128 rows x BN columns x 128 bytes of k come by
-// TMA (128-byte swizzle, zeros beyond the matrices' ends) into a ring, tcgen05.mma 128 x BN x 32 sums them in one of two
-// accumulators in tensor memory, and eight epilogue warps drain the other meanwhile: scales, bias, activation, residual; rows
-// leave and residuals arrive through boxes of 32 rows x 32 columns per warp that the bulk-copy engine moves.
+// int8 is summed in 32-bit integers (exact: k <= 131,056), e4m3 in fp32.
+//
+// Tiles of 128 bytes of k come by TMA (128-byte swizzle, zeros beyond the matrices' ends) into a ring; tcgen05.mma sums them in one
+// of two accumulators in tensor memory while the epilogue drains the other.  Large products take a pair of blocks per 256 x 256
+// tile (cta_group::2): each block loads its 128 rows of a and 128 of w and keeps 128 rows of the accumulator, so a block's copies are
+// 64 bytes per cycle at the tensor cores' full rate where a tile of its own would need 96.  Small ones take 128 x 128 or 128 x 64 per
+// block, so that every SM has one.
+//
+// An epilogue warp has 32 rows x 64 columns of its own and a box of 4 KB in shared memory for them: the residual comes into
+// the box by TMA while the tile is still being summed, the result takes its place and leaves by TMA in rows of 128 bytes.  Warps meet
+// nowhere but at the accumulator's barriers; scales and biases are read through L1, the same address in all lanes.  Four warps for each 64
+// columns: the steps of one (tensor memory, arithmetic, box, copy) are a chain that only other warps can cover.
 // The number of valid rows may come from device memory.  All mbarrier waits are bounded (status word).
 #include <cuda.h>
 #include "dense8.cuh"
@@ -12,80 +20,135 @@
 namespace llmc {
 
 namespace {
-constexpr int DM = 128, DK = 128;
-constexpr int D_THREADS = 320;                      // warp 0: TMA, warp 1: MMA, warps 2..9: epilogue (two sets of four)
-constexpr int D_EPI = 256;
+constexpr int DM = 128, DK = 128;                   // rows of a block's accumulator; bytes of k per step
 constexpr uint32_t DA_BYTES = DM * DK;
-constexpr uint32_t D_BOX = 32 * 64;                 // a warp's 32 rows of a 32-column group
+constexpr uint32_t D_BOX = 32 * 128;                // a warp's 32 rows of 64 columns
 
-template <int BN>
+// CTAS blocks share a tile of CTAS * 128 rows and BN columns
+template <int CTAS, int BN>
 struct D8 {
-  static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 5 : 7;
-  static constexpr uint32_t B_BYTES = BN * DK;
+  static constexpr int STAGES = CTAS == 2 ? 5 : BN == 128 ? 6 : 8;
+  static constexpr int EPI_WARPS = 4 * (BN / 64);
+  static constexpr int THREADS = 64 + 32 * EPI_WARPS;             // warp 0: TMA, warp 1: MMA, then the epilogue
+  static constexpr uint32_t B_BYTES = BN / CTAS * DK;
   static constexpr uint32_t A = 0;
   static constexpr uint32_t B = A + STAGES * DA_BYTES;
-  static constexpr uint32_t STG = B + STAGES * B_BYTES;          // one box per epilogue warp on its way out
-  static constexpr uint32_t RES = STG + 8 * D_BOX;               // the same for the residual on its way in
-  static constexpr uint32_t COL = RES + 8 * D_BOX;               // float w_scale [BN], float bias [BN]
-  static constexpr uint32_t BAR = COL + BN * 8;
-  static constexpr uint32_t MISC = BAR + (2 * STAGES + 12) * 8;
-  static constexpr uint32_t BYTES = MISC + 64;
+  static constexpr uint32_t BOX = B + STAGES * B_BYTES;           // one per epilogue warp
+  static constexpr uint32_t BAR = BOX + EPI_WARPS * D_BOX;
+  static constexpr uint32_t MISC = BAR + (2 * STAGES + 4 + EPI_WARPS) * 8;
+  static constexpr uint32_t BYTES = MISC + 16 + 1024;
   static constexpr uint32_t TMEM = 2 * BN;
   static_assert(BYTES <= 232448, "shared memory of one block");
 };
+
+__device__ __forceinline__ float4 ldg4(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
+
+__device__ const float d8_no_bias[64] = {};
+
+// 16 columns of a row: scales s, biases b, activation, residual r (pairs of bf16); y: pairs of neighbouring columns
+template <bool I8, uint32_t ACT, bool RES>
+__device__ __forceinline__ void finish16(const uint32_t (&v)[16], unsigned long long sa2, const float (&s)[16], const float (&b)[16],
+                                         const uint32_t (&r)[8], unsigned long long (&y)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const unsigned long long x = I8 ? f2_pack((float)(int32_t)v[2 * j], (float)(int32_t)v[2 * j + 1])
+                                    : f2_pack(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+    y[j] = f2_fma(f2_mul(x, sa2), f2_pack(s[2 * j], s[2 * j + 1]), f2_pack(b[2 * j], b[2 * j + 1]));
+  }
+  if (ACT != LAYER_ACT_NONE) {
+    gelu_phi2_x8<ACT == LAYER_ACT_GELU_TANH, RES>(y, r);
+  } else if (RES) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = f2_add(y[j], bf16_pair(r[j]));
+  }
+}
+__device__ __forceinline__ void put4(uint4 v, uint32_t* r) { r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w; }
+__device__ __forceinline__ uint4 bf16x8(const unsigned long long* y) {
+  return make_uint4(pack_bf16(f2_lo(y[0]), f2_hi(y[0])), pack_bf16(f2_lo(y[1]), f2_hi(y[1])), pack_bf16(f2_lo(y[2]), f2_hi(y[2])),
+                    pack_bf16(f2_lo(y[3]), f2_hi(y[3])));
+}
+// A warp's 32 rows of 64 columns between its box and memory by plain copies, two columns per lane: rows and columns beyond the ends
+// stay out.  TO_BOX: from memory.
+template <bool TO_BOX, typename T>
+__device__ __noinline__ void plain_box(T* at, long long ld, uint32_t row0, uint32_t col0, uint32_t M, uint32_t N, uint32_t box, uint32_t lane) {
+  const uint32_t col = col0 + 2 * lane, rows = min(32u, M - row0);
+#pragma unroll 1
+  for (uint32_t r = 0; r < rows; ++r) {
+    const uint32_t word = box + r * 128 + (((lane >> 2) ^ (r & 7u)) << 4) + (lane & 3u) * 4;
+    T* p = at + (long long)(row0 + r) * ld + col;
+    if constexpr (TO_BOX) {
+      uint32_t w = 0;
+      if (col + 1 < N) w = *reinterpret_cast<const uint32_t*>(p);
+      else if (col < N) w = __bfloat16_as_ushort(*p);
+      asm volatile("st.shared.u32 [%0], %1;" ::"r"(word), "r"(w) : "memory");
+    } else {
+      uint32_t w;
+      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(word) : "memory");
+      if (col + 1 < N) *reinterpret_cast<uint32_t*>(p) = w;
+      else if (col < N) *p = __ushort_as_bfloat16((unsigned short)w);
+    }
+  }
+  __syncwarp();
+}
 }  // namespace
 
 // I8: int8 or e4m3; ACT, RES, VT as in the bf16 product: each epilogue carries only its own code
-template <int BN, bool I8, uint32_t ACT, bool RES, bool VT>
-__global__ void __launch_bounds__(D_THREADS, 1)
+template <int CTAS, int BN, bool I8, uint32_t ACT, bool RES, bool VT>
+__global__ void __launch_bounds__((D8<CTAS, BN>::THREADS), 1)
 k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w,
             const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_res, const DenseArgs p) {
   griddep_sync();
-  using S = D8<BN>;
-  extern __shared__ __align__(1024) uint8_t gbase[];   // (the swizzle counts from multiples of 1,024 bytes; there is no room to round up)
-  const uint32_t base = smem_u32(gbase);
-  if (base & 1023u) {
-    if (threadIdx.x == 0) atomicExch(p.status, 1u);
-    return;
-  }
-  const uint32_t sA = base + S::A, sB = base + S::B;
-  float* scol = reinterpret_cast<float*>(gbase + S::COL);
-  const uint32_t bar0 = base + S::BAR;
-  auto full_bar = [&](uint32_t s) { return bar0 + 8 * s; };
+  using S = D8<CTAS, BN>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;           // (the same in both blocks of a pair)
+  uint8_t* gbase = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t sA = base + S::A, sB = base + S::B, bar0 = base + S::BAR;
+  auto full_bar = [&](uint32_t s) { return bar0 + 8 * s; };                              // pair: rank 0's counts both blocks' copies
   auto empty_bar = [&](uint32_t s) { return bar0 + 8 * (S::STAGES + s); };
   auto tfull_bar = [&](uint32_t b) { return bar0 + 8 * (2 * S::STAGES + b); };
-  auto tempty_bar = [&](uint32_t b) { return bar0 + 8 * (2 * S::STAGES + 2 + b); };
-  auto res_bar = [&](uint32_t w) { return bar0 + 8 * (2 * S::STAGES + 4 + w); };      // one per epilogue warp
+  auto tempty_bar = [&](uint32_t b) { return bar0 + 8 * (2 * S::STAGES + 2 + b); };      // pair: rank 0's counts both blocks' warps
+  auto res_bar = [&](uint32_t w) { return bar0 + 8 * (2 * S::STAGES + 4 + w); };         // one per epilogue warp
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(gbase + S::MISC);
   volatile uint32_t* tmem_slot = misc + 0;
   volatile uint32_t* abort_flag = misc + 1;
-  volatile uint32_t* epi_go = misc + 2;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CTAS == 2 ? pair_rank() : 0u;
   const unsigned long long lim = wait_limit(p.status);
 
   const uint32_t M = rows_of(p.m, p.count_dev, p.rows_per_count), N = p.n;
   const uint32_t KB = (p.k + DK - 1) / DK;
-  const uint32_t MB = (M + DM - 1) / DM, NB = (N + BN - 1) / BN;
-  const uint32_t n_tiles = MB * NB;
+  const uint32_t MB = (M + CTAS * DM - 1) / (CTAS * DM), NB = (N + BN - 1) / BN;
+  const uint32_t n_tiles = MB * NB, first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+  // neighbouring blocks work on neighbours along the shorter side, so that what they read at a time is small
+  auto tile_mb = [&](uint32_t t) { return MB <= NB ? t % MB : t / NB; };
+  auto tile_nb = [&](uint32_t t) { return MB <= NB ? t / MB : t % NB; };
 
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < (uint32_t)S::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (uint32_t b = 0; b < 2; ++b) {
       mbar_init(tfull_bar(b), 1);
-      mbar_init(tempty_bar(b), D_EPI);
+      mbar_init(tempty_bar(b), CTAS * S::EPI_WARPS);
     }
-    for (uint32_t w = 0; w < D_EPI / 32; ++w) mbar_init(res_bar(w), 1);
-    misc[1] = 0; misc[2] = 0; misc[3] = 0;
+    for (uint32_t w = 0; w < (uint32_t)S::EPI_WARPS; ++w) mbar_init(res_bar(w), 1);
+    misc[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                 ::"r"(smem_u32((const void*)tmem_slot)), "r"(S::TMEM) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if constexpr (CTAS == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                   ::"r"(smem_u32((const void*)tmem_slot)), "r"(S::TMEM) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                   ::"r"(smem_u32((const void*)tmem_slot)), "r"(S::TMEM) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   tc_fence_before();
   __syncthreads();
+  __syncwarp();
+  if constexpr (CTAS == 2) pair_meet();            // the other block's barriers are ready too
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
@@ -93,26 +156,38 @@ k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   if (warp == 0) {
     if (lane == 0 && !producer_idle(p.status)) {       // ---- TMA producer
       bool ok = true;
-      for (uint32_t t = blockIdx.x; t < n_tiles && ok; t += gridDim.x) {
-        const uint32_t mb = t / NB, nb = t % NB;       // consecutive blocks share the A tile in L2
+      for (uint32_t t = first; t < n_tiles && ok; t += step) {
+        const int row = (int)(tile_mb(t) * (CTAS * DM) + rank * DM), col = (int)(tile_nb(t) * BN + rank * (BN / CTAS));
         for (uint32_t kb = 0; kb < KB; ++kb) {
           const uint32_t s = issued % S::STAGES, ph = (issued / S::STAGES) & 1u;
           if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, lim)) { ok = false; break; }
-          mbar_expect_tx(full_bar(s), DA_BYTES + S::B_BYTES);
-          tma_load_2d(sA + s * DA_BYTES, &map_a, (int)(kb * DK), (int)(mb * DM), full_bar(s));
-          tma_load_2d(sB + s * S::B_BYTES, &map_w, (int)(kb * DK), (int)(nb * BN), full_bar(s));
+          if (rank == 0) mbar_expect_tx(full_bar(s), CTAS * (DA_BYTES + S::B_BYTES));
+          if constexpr (CTAS == 2) {
+            const uint32_t bar = of_rank0(full_bar(s));
+            tma_load_2d_pair(sA + s * DA_BYTES, &map_a, (int)(kb * DK), row, bar);
+            tma_load_2d_pair(sB + s * S::B_BYTES, &map_w, (int)(kb * DK), col, bar);
+          } else {
+            tma_load_2d(sA + s * DA_BYTES, &map_a, (int)(kb * DK), row, full_bar(s));
+            tma_load_2d(sB + s * S::B_BYTES, &map_w, (int)(kb * DK), col, full_bar(s));
+          }
           ++issued;
         }
+      }
+      // pair: what the other block's products signal here must have arrived before the block ends
+      for (uint32_t i = 0; CTAS == 2 && ok && i < (uint32_t)S::STAGES && i < issued; ++i) {
+        const uint32_t x = issued - 1 - i;
+        ok = mbar_wait(empty_bar(x % S::STAGES), (x / S::STAGES) & 1u, abort_flag, lim);
       }
       if (!ok) { *abort_flag = 1; atomicExch(p.status, 1u); }
     }
   } else if (warp == 1) {
-    if (lane == 0) {                                   // ---- MMA issuer
+    if (lane == 0 && rank == 0) {                      // ---- MMA issuer
       // operand types: signed 8-bit integers into 32-bit ones, or e4m3 into fp32
-      constexpr uint32_t idesc = (I8 ? (2u << 4) | (1u << 7) | (1u << 10) : (1u << 4)) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(DM >> 4) << 24);
+      constexpr uint32_t idesc = (I8 ? (2u << 4) | (1u << 7) | (1u << 10) : (1u << 4)) | ((uint32_t)(BN >> 3) << 17) |
+                                 ((uint32_t)((CTAS * DM) >> 4) << 24);
       bool ok = true;
       uint32_t it = 0, tile = 0;
-      for (uint32_t t = blockIdx.x; t < n_tiles && ok; t += gridDim.x, ++tile) {
+      for (uint32_t t = first; t < n_tiles && ok; t += step, ++tile) {
         const uint32_t buf = tile & 1u, bph = (tile >> 1) & 1u;
         if (!mbar_wait(tempty_bar(buf), bph ^ 1u, abort_flag, lim)) { ok = false; break; }
         tc_fence_after();
@@ -124,159 +199,151 @@ k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           const uint64_t da = smem_desc_sw128(sA + s * DA_BYTES), db = smem_desc_sw128(sB + s * S::B_BYTES);
 #pragma unroll
           for (uint32_t kk = 0; kk < DK / 32; ++kk) {
-            if (I8) tc_mma_i8(d_tmem, da + kk * 2, db + kk * 2, idesc, (kb | kk) != 0u);
-            else    tc_mma_f8(d_tmem, da + kk * 2, db + kk * 2, idesc, (kb | kk) != 0u);
+            const uint32_t more = (kb | kk) != 0u;
+            if constexpr (CTAS == 2) {
+              if (I8) tc_mma_i8_pair(d_tmem, da + kk * 2, db + kk * 2, idesc, more);
+              else    tc_mma_f8_pair(d_tmem, da + kk * 2, db + kk * 2, idesc, more);
+            } else {
+              if (I8) tc_mma_i8(d_tmem, da + kk * 2, db + kk * 2, idesc, more);
+              else    tc_mma_f8(d_tmem, da + kk * 2, db + kk * 2, idesc, more);
+            }
           }
-          tc_commit(empty_bar(s));
+          if constexpr (CTAS == 2) tc_commit_pair(empty_bar(s)); else tc_commit(empty_bar(s));
         }
-        if (ok) tc_commit(tfull_bar(buf));
+        if (ok) { if constexpr (CTAS == 2) tc_commit_pair(tfull_bar(buf)); else tc_commit(tfull_bar(buf)); }
       }
       if (!ok) { *abort_flag = 1; atomicExch(p.status, 1u); }
     }
   } else {
-    // ---- epilogue: thread = one row of the tile, 32 columns at a time; set 0 takes the even groups, set 1 the odd ones.
-    // Rows of a partial block of a device-counted M, ragged last columns and transposed V columns use plain stores.
-    const uint32_t et = threadIdx.x - 64, set = et >> 7, quarter = warp & 3u, ew = et >> 5;
-    const uint32_t box = ew * D_BOX;
-    const uint32_t row_in_tile = quarter * 32 + lane;
-    const uint32_t my_off = box + lane * 64u, sw = (lane >> 1) & 3u;
-    // Tiles that leave through the boxes: what they have beyond the last row is cut off by the copy.  Columns are cut off in
-    // pieces of 16 bytes only: a last group that ends inside one uses plain stores.
-    auto boxed = [&](uint32_t t) { return M == p.m || (t / NB + 1) * DM <= M; };
-    const uint32_t n_boxed = N % 8 ? N / 32 * 32 : N;
-    uint32_t r_issued = 0, r_used = 0;
-    uint32_t ct = blockIdx.x, cg = set;                // next residual rows to request (lane 0 of every warp)
-    auto res_issue = [&]() {
-      while (ct < n_tiles && (!boxed(ct) || (ct % NB) * BN + cg * 32 >= n_boxed)) { ct += gridDim.x; cg = set; }
-      if (ct >= n_tiles) return;
-      const uint32_t cmb = ct / NB, cnb = ct % NB;
-      mbar_expect_tx(res_bar(ew), D_BOX);
-      tma_load_2d(base + S::RES + box, &map_res, (int)(cnb * BN + cg * 32), (int)(cmb * DM + quarter * 32), res_bar(ew));
-      ++r_issued;
-      cg += 2;
-      if (cg >= BN / 32 || cnb * BN + cg * 32 >= n_boxed) { cg = set; ct += gridDim.x; }
+    // ---- epilogue: a lane = one row of the tile, 64 columns of it
+    const uint32_t ew = warp - 2, quarter = warp & 3u, col_in_tile = (ew >> 2) * 64;
+    const uint32_t row_in_tile = rank * DM + quarter * 32;
+    const uint32_t box = base + S::BOX + ew * D_BOX;
+    const uint32_t my_row = (box + lane * 128u) | ((lane & 7u) << 4);      // piece c of the row is at my_row ^ (c << 4): the swizzle
+    // Columns are cut off by the copy engine in pieces of 16 bytes: 64 columns that end inside one use plain stores, as do the
+    // rows of a partial block whose number came from the device, and transposed V columns.
+    const uint32_t n_boxed = N % 8 ? N / 64 * 64 : N;
+    auto boxed = [&](uint32_t row0, uint32_t col0) {
+      return row0 < M && col0 < n_boxed && (M == p.m || row0 + 32 <= M) && !(VT && col0 >= p.vt.col0);
     };
-    if (RES && lane == 0) res_issue();
+    uint32_t r_issued = 0, r_used = 0;
+    auto fetch_residual = [&](uint32_t t) {            // (lane 0; the box is free)
+      if (t >= n_tiles) return;
+      const uint32_t row0 = tile_mb(t) * (CTAS * DM) + row_in_tile, col0 = tile_nb(t) * BN + col_in_tile;
+      if (!boxed(row0, col0)) return;
+      mbar_expect_tx(res_bar(ew), D_BOX);
+      tma_load_2d(box, &map_res, (int)col0, (int)row0, res_bar(ew));
+      ++r_issued;
+    };
+    if (RES && lane == 0) fetch_residual(first);
     uint32_t tile = 0;
-    for (uint32_t t = blockIdx.x; t < n_tiles; t += gridDim.x, ++tile) {
-      const uint32_t mb = t / NB, nb = t % NB;
+    bool live = true;
+    for (uint32_t t = first; t < n_tiles && live; t += step, ++tile) {
       const uint32_t buf = tile & 1u, bph = (tile >> 1) & 1u;
-      for (uint32_t x = et; x < (uint32_t)BN; x += D_EPI) {
-        const uint32_t c = nb * BN + x;
-        scol[x] = c < N ? p.w_scale[c] : 0.f;
-        scol[BN + x] = (p.bias && c < N) ? p.bias[c] : 0.f;
+      const uint32_t row0 = tile_mb(t) * (CTAS * DM) + row_in_tile, col0 = tile_nb(t) * BN + col_in_tile;
+      const uint32_t row = row0 + lane;
+      const bool some = row0 < M && col0 < N, in_box = boxed(row0, col0);
+      const float sa = row < M ? __ldg(p.a_scale + row) : 0.f;
+      // a wait that ran out ends the warp's work: nothing more is read, and nothing asked for that is not waited for
+      live = __all_sync(0xFFFFFFFFu, mbar_wait(tfull_bar(buf), bph, abort_flag, lim));
+      if (live && RES && in_box) {
+        live = __all_sync(0xFFFFFFFFu, mbar_wait(res_bar(ew), r_used & 1u, abort_flag, lim));
+        if (live) ++r_used;
       }
-      const uint32_t row = mb * DM + row_in_tile;
-      const bool row_ok = row < M, tile_boxed = boxed(t);
-      const float sa = row_ok ? p.a_scale[row] : 0.f;
-      if (et == 0) *epi_go = *abort_flag;
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      if (*epi_go) break;
-      // a wait that ran out ends the warp's work on the tile: nothing is read, and nothing asked for that is not waited for
-      bool live = __all_sync(0xFFFFFFFFu, mbar_wait(tfull_bar(buf), bph, abort_flag, lim));
-      if (!live) { *abort_flag = 1; atomicExch(p.status, 1u); }
+      if (!live) { *abort_flag = 1; atomicExch(p.status, 1u); break; }
       tc_fence_after();
-      const uint32_t taddr = tmem_base + buf * BN + ((quarter * 32u) << 16);
+      const uint32_t taddr = tmem_base + buf * BN + col_in_tile + ((quarter * 32u) << 16);
       const unsigned long long sa2 = f2_pack(sa, sa);
+      const bool transposed = VT && col0 >= p.vt.col0;
+      const float* ws = p.w_scale + col0;
+      const float* bs = p.bias ? p.bias + col0 : d8_no_bias;
+      auto release = [&]() {                           // the accumulator's columns are in registers: it may be filled again
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (CTAS == 2) mbar_arrive_cluster(of_rank0(tempty_bar(buf))); else mbar_arrive(tempty_bar(buf));
+        }
+      };
+      auto sixteen = [&](uint32_t u, const uint32_t (&v)[16], const float (&s)[16], const float (&b)[16]) {
+        uint32_t r[8];
+        unsigned long long y[8];
+        if (RES) {
+          put4(lds16(my_row ^ ((u * 2) << 4)), r);
+          put4(lds16(my_row ^ ((u * 2 + 1) << 4)), r + 4);
+        }
+        finish16<I8, ACT, RES>(v, sa2, s, b, r, y);
+        if (!transposed) {
+          sts16(my_row ^ ((u * 2) << 4), bf16x8(y));
+          sts16(my_row ^ ((u * 2 + 1) << 4), bf16x8(y + 4));
+        } else if (row < M) {
+          // the V third of a q|k|v product, transposed per head (see the bf16 product); lanes are neighbouring positions
+          const uint32_t seq = row / p.rows_per_count, pos = row - seq * p.rows_per_count;
+          __nv_bfloat16* dst = p.vt.ptr + ((size_t)seq * p.vt.heads * 64 + (col0 + u * 16 - p.vt.col0)) * p.vt.pitch + pos;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) dst[(size_t)i * p.vt.pitch] = __float2bfloat16_rn(i & 1 ? f2_hi(y[i / 2]) : f2_lo(y[i / 2]));
+        }
+      };
+      if (!RES && some) {                              // the box's last rows have been read out
+        if (lane == 0) bulk_wait_read<0>();
+        __syncwarp();
+      }
+      if (some && col0 + 64 <= N) {                    // nearly all tiles
+        if (RES && !in_box) plain_box<true>(p.residual, p.residual_ld, row0, col0, M, N, box, lane);
+        uint32_t v[2][16];                             // one step ahead of the arithmetic
+        tc_ld_32x16(taddr, v[0]);
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+          float s[16], b[16];
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            *reinterpret_cast<float4*>(s + i) = ldg4(ws + u * 16 + i);
+            *reinterpret_cast<float4*>(b + i) = ldg4(bs + u * 16 + i);
+          }
+          tc_wait_ld_16(v[u & 1]);
+          if (u < 3) tc_ld_32x16(taddr + (u + 1) * 16, v[(u + 1) & 1]); else release();
+          sixteen(u, v[u & 1], s, b);
+        }
+      } else {
+        if (RES && some && !in_box) plain_box<true>(p.residual, p.residual_ld, row0, col0, M, N, box, lane);
 #pragma unroll 1
-      for (uint32_t c = set * 32; live && c < (uint32_t)BN; c += 64) {
-        const uint32_t col0 = nb * BN + c;
-        if (col0 >= N) break;
-        const bool staged = tile_boxed && col0 < n_boxed;
-        if (RES && staged) {
-          live = __all_sync(0xFFFFFFFFu, mbar_wait(res_bar(ew), r_used & 1u, abort_flag, lim));
-          if (!live) { *abort_flag = 1; atomicExch(p.status, 1u); break; }
-          ++r_used;
-        }
-        uint32_t v[32];
-        tc_ld_32x32(taddr + c, v);
-        // the residual of this group goes to registers first and its box is refilled at once, so that the next
-        // group's residual has this whole group's time to arrive
-        uint4 rr[4];
-        if (RES && staged) {
-          const uint8_t* rb = gbase + S::RES + my_off;
+        for (uint32_t u = 0; some && u < 4 && col0 + u * 16 < N; ++u) {
+          uint32_t v[16];
+          tc_ld_32x16(taddr + u * 16, v);
+          float s[16], b[16];
 #pragma unroll
-          for (uint32_t q = 0; q < 4; ++q) rr[q] = *reinterpret_cast<const uint4*>(rb + ((q ^ sw) << 4));
-          __syncwarp();
-          if (lane == 0) res_issue();
-        }
-        tc_wait_ld();
-        float f[32];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const float2* s2 = reinterpret_cast<const float2*>(scol + c) + half * 8;
-          const float2* b2 = reinterpret_cast<const float2*>(scol + BN + c) + half * 8;
-          unsigned long long y[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float2 s = s2[j], b = b2[j];
-            const uint32_t v0 = v[half * 16 + 2 * j], v1 = v[half * 16 + 2 * j + 1];
-            const unsigned long long x = I8 ? f2_pack((float)(int32_t)v0, (float)(int32_t)v1)
-                                            : f2_pack(__uint_as_float(v0), __uint_as_float(v1));
-            y[j] = f2_fma(f2_mul(x, sa2), f2_pack(s.x, s.y), f2_pack(b.x, b.y));
+          for (uint32_t i = 0; i < 16; ++i) {          // nothing is read beyond the last column
+            const bool there = col0 + u * 16 + i < N;
+            s[i] = there ? __ldg(ws + u * 16 + i) : 0.f;
+            b[i] = there ? __ldg(bs + u * 16 + i) : 0.f;
           }
-          if (ACT == LAYER_ACT_GELU_ERF) gelu_erf2_x8(y);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            f[half * 16 + 2 * j] = f2_lo(y[j]);
-            f[half * 16 + 2 * j + 1] = f2_hi(y[j]);
-          }
+          tc_wait_ld_16(v);
+          sixteen(u, v, s, b);
         }
-        if (ACT == LAYER_ACT_GELU_TANH) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) f[i] = gelu_tanh_f(f[i]);
-        }
-        if (VT && col0 >= p.vt.col0) {
-          // the V third of a q|k|v product, transposed per head (see the bf16 product)
-          if (row_ok) {
-            const uint32_t seq = row / p.rows_per_count, pos = row - seq * p.rows_per_count;
-            __nv_bfloat16* dst = p.vt.ptr + ((size_t)seq * p.vt.heads * 64 + (col0 - p.vt.col0)) * p.vt.pitch + pos;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) dst[(size_t)i * p.vt.pitch] = __float2bfloat16_rn(f[i]);
-          }
-          continue;
-        }
-        if (staged) {
-          if (RES) {
-#pragma unroll
-            for (uint32_t q = 0; q < 4; ++q) {
-              const uint32_t w[4] = {rr[q].x, rr[q].y, rr[q].z, rr[q].w};
-#pragma unroll
-              for (int u = 0; u < 4; ++u) {
-                f[q * 8 + 2 * u]     += __uint_as_float(w[u] << 16);
-                f[q * 8 + 2 * u + 1] += __uint_as_float(w[u] & 0xFFFF0000u);
-              }
-            }
-          }
-          if (lane == 0) bulk_wait_read<0>();           // the warp's previous rows have been read out
-          __syncwarp();
-          uint8_t* ob = gbase + S::STG + my_off;
-#pragma unroll
-          for (uint32_t q = 0; q < 4; ++q)
-            *reinterpret_cast<uint4*>(ob + ((q ^ sw) << 4)) =
-                make_uint4(pack_bf16(f[q * 8], f[q * 8 + 1]), pack_bf16(f[q * 8 + 2], f[q * 8 + 3]),
-                           pack_bf16(f[q * 8 + 4], f[q * 8 + 5]), pack_bf16(f[q * 8 + 6], f[q * 8 + 7]));
-          fence_async_smem();
-          __syncwarp();
+        release();
+      }
+      if (some && !transposed) {
+        fence_async_smem();
+        __syncwarp();
+        if (in_box) {
           if (lane == 0) {
-            tma_store_2d(&map_out, (int)col0, (int)(mb * DM + quarter * 32), base + S::STG + box);
+            tma_store_2d(&map_out, (int)col0, (int)row0, box);
             bulk_commit();
           }
-        } else if (row_ok) {
-          const __nv_bfloat16* r = RES ? p.residual + (size_t)row * p.residual_ld + col0 : nullptr;
-          __nv_bfloat16* o = p.out + (size_t)row * p.out_ld + col0;
-#pragma unroll
-          for (uint32_t i = 0; i < 32; ++i)
-            if (col0 + i < N) o[i] = __float2bfloat16_rn(RES ? f[i] + __bfloat162float(r[i]) : f[i]);
+        } else {
+          plain_box<false>(p.out, p.out_ld, row0, col0, M, N, box, lane);
+          fence_async_smem();
+          __syncwarp();
         }
       }
-      tc_fence_before();
-      mbar_arrive(tempty_bar(buf));
-      asm volatile("bar.sync 1, 256;" ::: "memory");   // the scales and biases of the next tile overwrite this one's
+      if (RES && lane == 0) {
+        bulk_wait_read<0>();
+        fetch_residual(t + step);
+      }
+      __syncwarp();
     }
     if (lane == 0) {
       bulk_wait_all();
-      // residual boxes still on their way (only after a wait ran out): they must land before the block ends
+      // a residual still on its way (only after a wait ran out) must land before the block ends
       volatile uint32_t never = 0;
       for (; r_used < r_issued; ++r_used) mbar_wait(res_bar(ew), r_used & 1u, &never, 200000000ull);
     }
@@ -284,79 +351,124 @@ k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && *abort_flag) {
+  if (threadIdx.x == 0 && *abort_flag) {               // (pair: rank 0's barriers count both blocks' copies)
     const uint32_t back = issued < (uint32_t)S::STAGES ? issued : (uint32_t)S::STAGES;
     volatile uint32_t never = 0;
-    for (uint32_t i = 0; i < back; ++i) {
+    for (uint32_t i = 0; i < back && rank == 0; ++i) {
       const uint32_t itx = issued - 1 - i;
       mbar_wait(full_bar(itx % S::STAGES), (itx / S::STAGES) & 1u, &never, 200000000ull);
     }
   }
   __syncthreads();
+  __syncwarp();
+  if constexpr (CTAS == 2) pair_meet();             // nobody reads or signals the other's memory any more
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(S::TMEM) : "memory");
+    if constexpr (CTAS == 2)
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(S::TMEM) : "memory");
+    else
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(S::TMEM) : "memory");
   }
 }
 
 namespace {
 using DenseKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const DenseArgs);
 
-template <int BN, bool I8>
+template <int CTAS, int BN, bool I8>
 DenseKernel kernel_of(uint32_t act, bool res, bool vt) {
-  if (vt) return !res && act == LAYER_ACT_NONE ? k_dense8_tc<BN, I8, LAYER_ACT_NONE, false, true> : nullptr;
+  if (vt) return !res && act == LAYER_ACT_NONE ? k_dense8_tc<CTAS, BN, I8, LAYER_ACT_NONE, false, true> : nullptr;
   switch (act) {
-    case LAYER_ACT_NONE: return res ? k_dense8_tc<BN, I8, LAYER_ACT_NONE, true, false> : k_dense8_tc<BN, I8, LAYER_ACT_NONE, false, false>;
-    case LAYER_ACT_GELU_ERF: return res ? k_dense8_tc<BN, I8, LAYER_ACT_GELU_ERF, true, false> : k_dense8_tc<BN, I8, LAYER_ACT_GELU_ERF, false, false>;
-    case LAYER_ACT_GELU_TANH: return res ? k_dense8_tc<BN, I8, LAYER_ACT_GELU_TANH, true, false> : k_dense8_tc<BN, I8, LAYER_ACT_GELU_TANH, false, false>;
+    case LAYER_ACT_NONE: return res ? k_dense8_tc<CTAS, BN, I8, LAYER_ACT_NONE, true, false> : k_dense8_tc<CTAS, BN, I8, LAYER_ACT_NONE, false, false>;
+    case LAYER_ACT_GELU_ERF: return res ? k_dense8_tc<CTAS, BN, I8, LAYER_ACT_GELU_ERF, true, false> : k_dense8_tc<CTAS, BN, I8, LAYER_ACT_GELU_ERF, false, false>;
+    case LAYER_ACT_GELU_TANH: return res ? k_dense8_tc<CTAS, BN, I8, LAYER_ACT_GELU_TANH, true, false> : k_dense8_tc<CTAS, BN, I8, LAYER_ACT_GELU_TANH, false, false>;
     default: return nullptr;
   }
 }
 
-template <int BN>
-cudaError_t setup_width() {
+// how many pairs of blocks the current device runs at a time (its SMs lie in groups, some with an odd number of them)
+constexpr int MAX_DEVICES = 64;
+int g_pairs[MAX_DEVICES];
+
+template <int CTAS, int BN>
+cudaLaunchConfig_t shape_config(cudaLaunchAttribute (&attr)[2], uint32_t grid, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(D8<CTAS, BN>::THREADS);
+  cfg.dynamicSmemBytes = D8<CTAS, BN>::BYTES;
+  cfg.stream = st;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CTAS;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = CTAS == 2 ? 2 : 1;
+  return cfg;
+}
+
+template <int CTAS, int BN>
+cudaError_t setup_shape() {
   for (uint32_t act = LAYER_ACT_NONE; act <= LAYER_ACT_GELU_TANH; ++act)
     for (int v = 0; v < 4; ++v) {
       const bool res = v & 1, vt = v & 2;
-      for (const DenseKernel k : {kernel_of<BN, true>(act, res, vt), kernel_of<BN, false>(act, res, vt)}) {
+      for (const DenseKernel k : {kernel_of<CTAS, BN, true>(act, res, vt), kernel_of<CTAS, BN, false>(act, res, vt)}) {
         if (!k) continue;
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, D8<BN>::BYTES);
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, D8<CTAS, BN>::BYTES);
         if (e != cudaSuccess) return e;
       }
     }
   return cudaSuccess;
 }
 
-template <int BN>
-cudaError_t launch_width(const DenseArgs& a, int sm_count, cudaStream_t st) {
-  const DenseKernel kern = a.format == LLMCACHE_I8 ? kernel_of<BN, true>(a.act, a.residual != nullptr, a.vt.ptr != nullptr)
-                                                   : kernel_of<BN, false>(a.act, a.residual != nullptr, a.vt.ptr != nullptr);
+template <int CTAS, int BN>
+cudaError_t launch_shape(const DenseArgs& a, int sm_count, cudaStream_t st) {
+  const DenseKernel kern = a.format == LLMCACHE_I8 ? kernel_of<CTAS, BN, true>(a.act, a.residual != nullptr, a.vt.ptr != nullptr)
+                                                   : kernel_of<CTAS, BN, false>(a.act, a.residual != nullptr, a.vt.ptr != nullptr);
   if (!kern) return cudaErrorInvalidValue;
   alignas(64) CUtensorMap map_a, map_w, map_out, map_res;
-  if (!make_tensor_map_8bit(&map_a, a.a, a.m, a.k, a.a_ld, DM) || !make_tensor_map_8bit(&map_w, a.w, a.n, a.k, a.w_ld, BN) ||
-      !make_tensor_map_bf16_box32_pitch(&map_out, a.out, a.m, a.n, a.out_ld) ||
-      !make_tensor_map_bf16_box32_pitch(&map_res, a.residual ? a.residual : a.out, a.m, a.n, a.residual ? a.residual_ld : a.out_ld))
+  if (!make_tensor_map_8bit(&map_a, a.a, a.m, a.k, a.a_ld, DM) || !make_tensor_map_8bit(&map_w, a.w, a.n, a.k, a.w_ld, BN / CTAS) ||
+      !make_tensor_map_bf16_box64_pitch(&map_out, a.out, a.m, a.n, a.out_ld) ||
+      !make_tensor_map_bf16_box64_pitch(&map_res, a.residual ? a.residual : a.out, a.m, a.n, a.residual ? a.residual_ld : a.out_ld))
     return cudaErrorInvalidValue;
-  const unsigned long long tiles = (unsigned long long)((a.m + DM - 1) / DM) * ((a.n + BN - 1) / BN);
-  const uint32_t grid = tiles < (unsigned long long)sm_count ? (uint32_t)tiles : (uint32_t)sm_count;
-  return launch_k(kern, dim3(grid), dim3(D_THREADS), D8<BN>::BYTES, st, map_a, map_w, map_out, map_res, a);
+  const unsigned long long tiles = (unsigned long long)((a.m + CTAS * DM - 1) / (CTAS * DM)) * ((a.n + BN - 1) / BN);
+  uint32_t most = (uint32_t)sm_count;
+  if (CTAS == 2) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES || !g_pairs[dev]) return cudaErrorInvalidDevice;
+    most = (uint32_t)g_pairs[dev];
+  }
+  cudaLaunchAttribute attr[2];
+  const cudaLaunchConfig_t cfg = shape_config<CTAS, BN>(attr, (tiles < most ? (uint32_t)tiles : most) * CTAS, st);
+  return cudaLaunchKernelEx(&cfg, kern, map_a, map_w, map_out, map_res, a);
 }
 }  // namespace
 
 cudaError_t setup_dense8_tc() {
   cudaError_t e = tensor_map_setup();
-  if (e == cudaSuccess) e = setup_width<256>();
-  if (e == cudaSuccess) e = setup_width<128>();
-  if (e == cudaSuccess) e = setup_width<64>();
+  if (e == cudaSuccess) e = setup_shape<2, 256>();
+  if (e == cudaSuccess) e = setup_shape<1, 128>();
+  if (e == cudaSuccess) e = setup_shape<1, 64>();
+  int dev = 0, pairs = 0;
+  if (e == cudaSuccess) e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev < 0 || dev >= MAX_DEVICES)) e = cudaErrorInvalidDevice;
+  if (e == cudaSuccess) {
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg = shape_config<2, 256>(attr, 2, nullptr);
+    cfg.attrs = attr + 1;                              // (the shape alone)
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&pairs, kernel_of<2, 256, true>(LAYER_ACT_NONE, false, false), &cfg);
+  }
+  if (e == cudaSuccess && pairs < 1) e = cudaErrorInvalidConfiguration;
+  if (e == cudaSuccess) g_pairs[dev] = pairs;
   return e;
 }
 
 cudaError_t launch_dense8_tc(const DenseArgs& a, int sm_count, cudaStream_t st) {
-  // the widest tile that gives every SM one
-  const unsigned long long mb = (a.m + DM - 1) / DM;
-  if (mb * ((a.n + 255) / 256) >= (unsigned long long)sm_count) return launch_width<256>(a, sm_count, st);
-  if (mb * ((a.n + 127) / 128) >= (unsigned long long)sm_count) return launch_width<128>(a, sm_count, st);
-  return launch_width<64>(a, sm_count, st);
+  // the largest tile that gives every SM one
+  const unsigned long long mb = (a.m + DM - 1) / DM, sms = (unsigned long long)sm_count;
+  if ((mb + 1) / 2 * ((a.n + 255) / 256) * 2 >= sms) return launch_shape<2, 256>(a, sm_count, st);
+  if (mb * ((a.n + 127) / 128) >= sms) return launch_shape<1, 128>(a, sm_count, st);
+  return launch_shape<1, 64>(a, sm_count, st);
 }
 
 }  // namespace llmc
