@@ -870,12 +870,20 @@ _ACTS = {"none": ACT_NONE, "gelu_erf": ACT_GELU_ERF, "gelu_tanh": ACT_GELU_TANH}
 _NORM = _Packed("@6If4xQ" + "Qq" * 5 + "3Q")
 _DENSE = _Packed("@7I4xQ" + "QqQ" * 2 + "Q" + "Qq" * 2)
 _NEW = _Packed("@4I3Q" + "Q3q" * 4 + "4Q")
+_NORM_BYTES, _DENSE_BYTES, _NEW_BYTES = _NORM.size, _DENSE.size, _NEW.size
+_F32, _I32 = torch.float32, torch.int32
 
 
 def _matrix(t, dtype, name, device, shape=None):
     """(address, leading dimension) of a matrix whose rows are dense."""
     if t is None:
         return 0, 0
+    try:                                                 # (the ordinary case in as few calls as it takes: they are most of a small call's time)
+        ld, inner = t.stride()
+        if inner == 1 and t.dtype is dtype and t.get_device() == device and (shape is None or t.shape == shape):
+            return t.data_ptr(), ld
+    except (AttributeError, TypeError, ValueError):
+        pass
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != 2:
         raise LLMCacheError(ERR_ARG, f"{name}: a {dtype} tensor of 2 dimensions is expected")
     if shape is not None and t.shape != shape:
@@ -891,12 +899,17 @@ def _matrix(t, dtype, name, device, shape=None):
 
 def _count(n_rows_dev, device):
     """Address of a row count in device memory."""
-    if n_rows_dev is None:
-        return 0
     if not isinstance(n_rows_dev, torch.Tensor) or n_rows_dev.dtype is not torch.int32 or n_rows_dev.numel() < 1:
         raise LLMCacheError(ERR_ARG, "n_rows_dev: an int32 tensor with one element")
     _same_device(device, n_rows_dev)
     return n_rows_dev.data_ptr()
+
+
+def _stream_of(stream, device):
+    """Handle of a stream; None: the current one of `device`, where a call's tensors are (the host: of the current device)."""
+    if stream is None and _raw_stream is not None and device >= 0:
+        return _raw_stream(device)
+    return _stream(stream)
 
 
 def llmcache_norm(x, *, kind="rms", gain=None, bias=None, eps=1e-5, residual=None, total=None, out=None, q=None, scale=None,
@@ -906,47 +919,60 @@ def llmcache_norm(x, *, kind="rms", gain=None, bias=None, eps=1e-5, residual=Non
     [rows].  n_rows_dev: int32 on the device, only that many rows are processed."""
     if not isinstance(x, torch.Tensor):
         raise LLMCacheError(ERR_ARG, "llmcache_norm: x is a tensor")
-    if kind not in _NORMS:
+    kind_id = _NORMS.get(kind)
+    if kind_id is None:
         raise LLMCacheError(ERR_ARG, 'llmcache_norm: kind is "rms", "layer" or "none"')
     device, shape = x.get_device(), x.shape
     x_at, x_ld = _matrix(x, _BF16, "x", device)
     rows, cols = shape
-    fmt = 0
+    fmt = q_at = q_ld = 0
     if q is not None:
-        fmt = _FORMAT_OF.get(getattr(q, "dtype", None))
+        dt = getattr(q, "dtype", None)
+        fmt = _FORMAT_OF.get(dt)
         if fmt is None:
             raise LLMCacheError(ERR_ARG, "q: an int8 or float8_e4m3fn tensor")
-    a = _NORM(_NORM.size, _NORMS[kind], fmt, rows, cols, 1, eps, _count(n_rows_dev, device), x_at, x_ld,
-              *_matrix(residual, _BF16, "residual", device, shape), *_matrix(total, _BF16, "total", device, shape),
-              *_matrix(out, _BF16, "out", device, shape), *_matrix(q, getattr(q, "dtype", None), "q", device, shape),
-              _addr(scale, torch.float32, (rows,), "scale", device), _addr(gain, torch.float32, (cols,), "gain", device),
-              _addr(bias, torch.float32, (cols,), "bias", device))
-    _check(lib().llmcache_norm(a, _stream(stream)), "llmcache_norm")
+        q_at, q_ld = _matrix(q, dt, "q", device, shape)
+    r_at, r_ld = (0, 0) if residual is None else _matrix(residual, _BF16, "residual", device, shape)
+    t_at, t_ld = (0, 0) if total is None else _matrix(total, _BF16, "total", device, shape)
+    o_at, o_ld = (0, 0) if out is None else _matrix(out, _BF16, "out", device, shape)
+    p = _NORM(_NORM_BYTES, kind_id, fmt, rows, cols, 1, eps, 0 if n_rows_dev is None else _count(n_rows_dev, device), x_at, x_ld,
+              r_at, r_ld, t_at, t_ld, o_at, o_ld, q_at, q_ld, 0 if scale is None else _addr(scale, _F32, (rows,), "scale", device),
+              0 if gain is None else _addr(gain, _F32, (cols,), "gain", device), 0 if bias is None else _addr(bias, _F32, (cols,), "bias", device))
+    rc = lib().llmcache_norm(p, _stream_of(stream, device))
+    if rc:
+        raise LLMCacheError(rc, "llmcache_norm")
 
 
 def llmcache_dense(a, a_scale, w, w_scale, out, *, bias=None, act="none", residual=None, n_rows_dev=None, stream=None) -> None:
     """out = act(a_scale w_scale (a w^T) + bias) + residual for 8-bit a [m, k] and w [n, k] of one type (int8: exact sums;
     float8_e4m3fn) with f32 scales [m], [n]; bias f32 [n]; out, residual bf16 [m, n].  act: "none", "gelu_erf" or "gelu_tanh".
     n_rows_dev: int32 on the device, only that many rows are processed."""
-    if not isinstance(a, torch.Tensor) or not isinstance(w, torch.Tensor) or _FORMAT_OF.get(a.dtype) is None or w.dtype is not a.dtype:
+    if not isinstance(a, torch.Tensor) or not isinstance(w, torch.Tensor):
+        raise LLMCacheError(ERR_ARG, "llmcache_dense: a and w are tensors")
+    dt = a.dtype
+    fmt = _FORMAT_OF.get(dt)
+    if fmt is None or w.dtype is not dt:
         raise LLMCacheError(ERR_ARG, "llmcache_dense: a and w are both int8 or both float8_e4m3fn")
-    if act not in _ACTS:
+    act_id = _ACTS.get(act)
+    if act_id is None:
         raise LLMCacheError(ERR_ARG, 'llmcache_dense: act is "none", "gelu_erf" or "gelu_tanh"')
-    device, dt = a.get_device(), a.dtype
+    device = a.get_device()
     a_at, a_ld = _matrix(a, dt, "a", device)
-    m, k = a.shape
     w_at, w_ld = _matrix(w, dt, "w", device)
-    n = w.shape[0]
-    if w.shape[1] != k:
+    m, k = a.shape
+    n, kw = w.shape
+    if kw != k:
         raise LLMCacheError(ERR_SHAPE, "llmcache_dense: a [m, k], w [n, k]")
     if a_scale is None or w_scale is None or out is None:
         raise LLMCacheError(ERR_ARG, "llmcache_dense: a_scale, w_scale and out are needed")
-    F32 = torch.float32
-    p = _DENSE(_DENSE.size, _FORMAT_OF[dt], m, n, k, _ACTS[act], 1, _count(n_rows_dev, device), a_at, a_ld,
-               _addr(a_scale, F32, (m,), "a_scale", device), w_at, w_ld, _addr(w_scale, F32, (n,), "w_scale", device),
-               _addr(bias, F32, (n,), "bias", device), *_matrix(residual, _BF16, "residual", device, (m, n)),
-               *_matrix(out, _BF16, "out", device, (m, n)))
-    _check(lib().llmcache_dense(p, _stream(stream)), "llmcache_dense")
+    o_at, o_ld = _matrix(out, _BF16, "out", device, (m, n))
+    r_at, r_ld = (0, 0) if residual is None else _matrix(residual, _BF16, "residual", device, (m, n))
+    p = _DENSE(_DENSE_BYTES, fmt, m, n, k, act_id, 1, 0 if n_rows_dev is None else _count(n_rows_dev, device), a_at, a_ld,
+               _addr(a_scale, _F32, (m,), "a_scale", device), w_at, w_ld, _addr(w_scale, _F32, (n,), "w_scale", device),
+               0 if bias is None else _addr(bias, _F32, (n,), "bias", device), r_at, r_ld, o_at, o_ld)
+    rc = lib().llmcache_dense(p, _stream_of(stream, device))
+    if rc:
+        raise LLMCacheError(rc, "llmcache_dense")
 
 
 def llmcache_dense_status() -> int:
@@ -955,6 +981,9 @@ def llmcache_dense_status() -> int:
 
 def llmcache_dense_debug_knobs(wait_limit_ns: int, flags: int) -> None:
     _check(lib().llmcache_dense_debug_knobs(wait_limit_ns, flags), "llmcache_dense_debug_knobs")
+
+
+_address_of = C.addressof
 
 
 def make_rotation(inv_freq, *, interleaved=False) -> Rotation:
@@ -1146,30 +1175,36 @@ class KVCache:
         """Stores k_new, rotated by position (make_rotation; None: as it is), and v_new [n_rows, kv_heads, 64] in the pages, and
         rotates q [n_rows, heads, 64] into q_out, which may be q (llmcache_kv_append); attention follows without k_new and
         v_new.  cu_rows, lens, pages, positions and first as in attention; first also without positions."""
-        device = self.device
+        device, HK = self.device, self.kv_heads
+        if lens is None or pages is None or cu_rows is None:
+            raise LLMCacheError(ERR_ARG, "cu_rows, lens and pages are needed")
         rk = _rows(k_new, "k_new", 3, None, device)
-        T = k_new.shape[0]
-        if k_new.shape[1] != self.kv_heads:
+        shape = k_new.shape
+        T = shape[0]
+        if shape[1] != HK:
             raise LLMCacheError(ERR_SHAPE, "k_new, v_new: [n_rows, kv_heads, 64]")
-        rv = _rows(v_new, "v_new", 3, k_new.shape, device)
+        rv = _rows(v_new, "v_new", 3, shape, device)
         if (q is None) != (q_out is None):
             raise LLMCacheError(ERR_ARG, "q and q_out come together")
         rq = ro = _NO_ROWS
         if q is not None:
-            shape = (T, self.heads, 64)
-            rq, ro = _rows(q, "q", 3, shape, device), _rows(q_out, "q_out", 3, shape, device)
-        if lens is None or pages is None or cu_rows is None:
-            raise LLMCacheError(ERR_ARG, "cu_rows, lens and pages are needed")
-        I32 = torch.int32
-        lens_at = _addr(lens, I32, (-1,), "lens", device)
+            wide = (T, self.heads, 64)
+            rq, ro = _rows(q, "q", 3, wide, device), _rows(q_out, "q_out", 3, wide, device)
+        lens_at = _addr(lens, _I32, (-1,), "lens", device)
         S = lens.shape[0]
-        pages_at = _addr(pages, I32, (S, -1), "pages", device)
+        pages_at = _addr(pages, _I32, (S, -1), "pages", device)
         if rotation is not None:
-            _same_device(device, *getattr(rotation, "tensors", ()))
-        c = _NEW(_NEW.size, S, T, pages.shape[1], _addr(cu_rows, I32, (S + 1,), "cu_rows", device), lens_at, pages_at, *rk, *rv, *rq, *ro,
-                 _addr(positions, I32, (S, self.kv_heads, -1), "positions", device), _addr(first, I32, (S,), "first", device),
-                 0 if positions is None else positions.shape[-1], 0 if rotation is None else C.addressof(rotation))
-        _check(lib().llmcache_kv_append(self.handle, c, _stream(stream, device)), "llmcache_kv_append")
+            for t in getattr(rotation, "tensors", ()):
+                if t.get_device() != device:
+                    _other_device(t, device)
+        p_at = side = 0
+        if positions is not None:
+            p_at, side = _addr(positions, _I32, (S, HK, -1), "positions", device), positions.shape[-1]
+        c = _NEW(_NEW_BYTES, S, T, pages.shape[1], _addr(cu_rows, _I32, (S + 1,), "cu_rows", device), lens_at, pages_at, *rk, *rv, *rq, *ro,
+                 p_at, 0 if first is None else _addr(first, _I32, (S,), "first", device), side, 0 if rotation is None else _address_of(rotation))
+        rc = lib().llmcache_kv_append(self.handle, c, _stream_of(stream, device))
+        if rc:
+            raise LLMCacheError(rc, "llmcache_kv_append")
 
     def evict(self, *, lens, pages, weights, new_pages, new_lens, budget, recent=0, sinks=0, positions=None, new_weights=None,
               new_positions=None, kept=None, stream=None):

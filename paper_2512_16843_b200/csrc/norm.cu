@@ -5,8 +5,10 @@
 //
 // Bound by HBM: 2 bytes per element for each of x, residual, total and out that a call has, 1 for q, each moved once.  A
 // row therefore stays in registers between its three reductions (mean, squares, largest magnitude).
+#include <atomic>
 #include <cuda_fp8.h>
 #include "dense8.cuh"
+#include "ptx.cuh"
 
 namespace llmc {
 
@@ -20,51 +22,55 @@ __device__ __forceinline__ uint4 ld16(const void* p) {
   asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
   return v;
 }
-__device__ __forceinline__ void add8(float (&h)[8], uint4 v) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    h[2 * u] += __uint_as_float(w[u] << 16);
-    h[2 * u + 1] += __uint_as_float(w[u] & 0xFFFF0000u);
-  }
+typedef unsigned long long f2;           // two neighbouring columns in f32
+__device__ __forceinline__ f2 bf16_2(uint32_t w) { return f2_pack(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+__device__ __forceinline__ uint32_t to_bf16(f2 v) {
+  const __nv_bfloat162 o = __floats2bfloat162_rn(f2_lo(v), f2_hi(v));
+  return *reinterpret_cast<const uint32_t*>(&o);
 }
-__device__ __forceinline__ uint4 to_bf16(const float (&h)[8]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(h[2 * u], h[2 * u + 1]);
-    w[u] = *reinterpret_cast<const uint32_t*>(&v);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+__device__ __forceinline__ uint4 to_bf16x8(const f2 (&h)[4]) { return make_uint4(to_bf16(h[0]), to_bf16(h[1]), to_bf16(h[2]), to_bf16(h[3])); }
+// the larger magnitude; NaN if there is one
+__device__ __forceinline__ float max_nan(float m, f2 v) {
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(m), "f"(fabsf(f2_lo(v))), "f"(fabsf(f2_hi(v))));
+  return m;
 }
-// Quotients, not products with an inverse: values of few bits often lie halfway between two of the 8-bit ones, and only the
-// correctly rounded quotient tells them apart from their neighbours.
-__device__ __forceinline__ uint2 to_int8(const float (&y)[8], float scale) {
+// y / scale, correctly rounded.  Quotients, not products with an inverse: values of few bits often lie halfway between two of
+// the 8-bit ones, and only the rounded quotient tells them apart from their neighbours.  Markstein's correction (IBM Journal of Research
+// and Development 34, 1990): with inv the rounded inverse of the scale and q = y inv, q + (y - q scale) inv is the rounded quotient,
+// the difference being exact in a fused multiply-add.  (Where it underflows, y is far below half a step.)  Three instructions for two
+// values; a division takes about ten for each, which took more time than the memory.
+__device__ __forceinline__ f2 quotient(f2 y, f2 inv, f2 minus_scale) {
+  const f2 q = f2_mul(y, inv);
+  return f2_fma(f2_fma(q, minus_scale, y), inv, q);
+}
+// Integers of up to 2^22 in magnitude added to 1.5 2^23 stand in the low bits of the sum, rounded to the nearest even one.
+__device__ __forceinline__ uint2 to_int8(const f2 (&y)[4], f2 inv, f2 minus_scale) {
   uint32_t w[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    uint32_t b[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = (uint32_t)__float2int_rn(y[4 * u + i] / scale) & 0xFFu;
-    w[u] = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+    const f2 magic = f2_pack(12582912.f, 12582912.f);
+    const f2 a = f2_add(quotient(y[2 * u], inv, minus_scale), magic), b = f2_add(quotient(y[2 * u + 1], inv, minus_scale), magic);
+    w[u] = __byte_perm(__byte_perm((uint32_t)a, (uint32_t)(a >> 32), 0x0040), __byte_perm((uint32_t)b, (uint32_t)(b >> 32), 0x0040), 0x5410);
   }
   return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ uint2 to_e4m3(const float (&y)[8], float scale) {
+__device__ __forceinline__ uint32_t e4m3_2(f2 v) {
+  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f2_lo(v), f2_hi(v)), __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ uint2 to_e4m3(const f2 (&y)[4], f2 inv, f2 minus_scale) {
   uint32_t w[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u)
-    w[u] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(y[4 * u] / scale, y[4 * u + 1] / scale), __NV_SATFINITE, __NV_E4M3) |
-           (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(y[4 * u + 2] / scale, y[4 * u + 3] / scale), __NV_SATFINITE, __NV_E4M3) << 16;
+    w[u] = e4m3_2(quotient(y[2 * u], inv, minus_scale)) | e4m3_2(quotient(y[2 * u + 1], inv, minus_scale)) << 16;
   return make_uint2(w[0], w[1]);
 }
 
-// Reductions over the TPR threads of a row: a warp, or a block whose warps meet in shared memory (slot: one of the three
-// reductions of a row; every slot is read before the barrier of the next one, so a row's slots can be written again).
+// Reductions over the TPR threads of a row: a part of a warp, a warp, or a block whose warps meet in shared memory (slot: one of
+// the three reductions of a row; every slot is read before the barrier of the next one, so a row's slots can be written again).
 template <int TPR>
 __device__ __forceinline__ float row_sum(float s, float* slot) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
   if constexpr (TPR > 32) {
     if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = s;
     __syncthreads();
@@ -76,7 +82,12 @@ __device__ __forceinline__ float row_sum(float s, float* slot) {
 }
 template <int TPR>
 __device__ __forceinline__ uint32_t row_max(uint32_t m, float* slot) {
-  m = __reduce_max_sync(0xFFFFFFFFu, m);
+  if constexpr (TPR >= 32) {
+    m = __reduce_max_sync(0xFFFFFFFFu, m);
+  } else {
+#pragma unroll
+    for (int o = TPR / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+  }
   if constexpr (TPR > 32) {
     if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = __uint_as_float(m);
     __syncthreads();
@@ -87,12 +98,21 @@ __device__ __forceinline__ uint32_t row_max(uint32_t m, float* slot) {
   return m;
 }
 
-// TPR threads per row, CH pieces of eight elements each
+// threads and rows of a block
+template <int TPR>
+struct Shape {
+  static constexpr uint32_t THREADS = TPR <= 32 ? 128 : TPR, ROWS = THREADS / TPR;
+};
+
+// TPR threads per row, CH pieces of eight elements each.  A thread's columns are the same in every row, so gains and biases stay in
+// registers where there is room for them (KEEP): read again for every row they keep the first-level cache busy for longer than the row takes
+// (1,536 columns, rms without residual: 94 us per 105 M elements, 73 with KEEP).
 template <int TPR, int CH, int KIND>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR)
+__global__ void __launch_bounds__(Shape<TPR>::THREADS)
 k_norm(const NormArgs a) {
   griddep_sync();
-  constexpr uint32_t ROWS = TPR == 32 ? 8 : 1;             // rows of a block at a time
+  constexpr uint32_t ROWS = Shape<TPR>::ROWS;
+  constexpr bool KEEP = KIND != NORM_NONE && (TPR <= 128 || (TPR == 256 && CH <= 3));
   __shared__ float slots[TPR > 32 ? 3 * (TPR / 32) : 1];
   float* const slot0 = slots;
   float* const slot1 = slots + (TPR > 32 ? TPR / 32 : 0);
@@ -100,93 +120,111 @@ k_norm(const NormArgs a) {
   const uint32_t rows = rows_of(a.n_rows, a.count_dev, a.rows_per_count);
   const uint32_t me = threadIdx.x % TPR, pieces = a.cols / 8;
   const float per = 1.0f / (float)a.cols;
-  for (uint32_t row = blockIdx.x * ROWS + threadIdx.x / TPR; row < rows; row += gridDim.x * ROWS) {
-    float h[CH][8];
-    uint4 v[CH], r[CH];
+  uint4 v[CH], r[CH];
+  auto fetch = [&](uint32_t row) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const uint32_t c = me + (uint32_t)i * TPR;
       v[i] = r[i] = make_uint4(0, 0, 0, 0);
-      if (c < pieces) {
+      if (c < pieces && row < rows) {
         v[i] = ld16(a.x + (long long)row * a.x_ld + c * 8);
         if (a.residual) r[i] = ld16(a.residual + (long long)row * a.residual_ld + c * 8);
       }
     }
+  };
+  auto weights = [&](uint32_t c, f2 (&g)[4], f2 (&b)[4]) {
+#pragma unroll
+    for (int u = 0; u < 4; u += 2) {
+      ulonglong2 w = make_ulonglong2(f2_pack(1.f, 1.f), f2_pack(1.f, 1.f)), z = make_ulonglong2(0, 0);
+      if (c < pieces && a.gain) w = __ldg(reinterpret_cast<const ulonglong2*>(a.gain + c * 8 + 2 * u));
+      if (c < pieces && a.bias) z = __ldg(reinterpret_cast<const ulonglong2*>(a.bias + c * 8 + 2 * u));
+      g[u] = w.x; g[u + 1] = w.y;
+      b[u] = z.x; b[u + 1] = z.y;
+    }
+  };
+  const uint32_t step = gridDim.x * ROWS;
+  uint32_t row = blockIdx.x * ROWS + threadIdx.x / TPR;
+  fetch(row);
+  f2 gain[KEEP ? CH : 1][4], bias[KEEP ? CH : 1][4];
+  if constexpr (KEEP) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) weights(me + (uint32_t)i * TPR, gain[i], bias[i]);
+  }
+  for (uint32_t first = blockIdx.x * ROWS; first < rows; first += step, row += step) {
+    const bool ok = row < rows;
+    f2 h[CH][4];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
+      const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w}, e[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
 #pragma unroll
-      for (int u = 0; u < 8; ++u) h[i][u] = 0.f;
-      add8(h[i], v[i]);
-      if (a.residual) add8(h[i], r[i]);
+      for (int u = 0; u < 4; ++u) h[i][u] = a.residual ? f2_add(bf16_2(w[u]), bf16_2(e[u])) : bf16_2(w[u]);
     }
+    // the next row is on its way while this one goes through its reductions
+    if (first + step < rows) fetch(row + step);
     if (a.total) {
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const uint32_t c = me + (uint32_t)i * TPR;
-        if (c < pieces) st_stream16(a.total + (long long)row * a.total_ld + c * 8, to_bf16(h[i]));
+        if (c < pieces && ok) st_stream16(a.total + (long long)row * a.total_ld + c * 8, to_bf16x8(h[i]));
       }
     }
     if constexpr (KIND != NORM_NONE) {
-      float mu = 0.f;
       if constexpr (KIND == NORM_LAYER) {
-        float s = 0.f;
+        f2 s = 0;
 #pragma unroll
         for (int i = 0; i < CH; ++i)
 #pragma unroll
-          for (int u = 0; u < 8; ++u) s += h[i][u];
-        mu = row_sum<TPR>(s, slot0) * per;
-      }
-      float s = 0.f;
+          for (int u = 0; u < 4; ++u) s = f2_add(s, h[i][u]);
+        const float mu = row_sum<TPR>(f2_lo(s) + f2_hi(s), slot0) * per;
 #pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        if (KIND == NORM_RMS || me + (uint32_t)i * TPR < pieces) {
+        for (int i = 0; i < CH; ++i) {
+          if (me + (uint32_t)i * TPR < pieces) {
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            h[i][u] -= mu;
-            s = fmaf(h[i][u], h[i][u], s);
+            for (int u = 0; u < 4; ++u) h[i][u] = f2_add(h[i][u], f2_pack(-mu, -mu));
           }
         }
       }
-      const float rstd = 1.0f / sqrtf(row_sum<TPR>(s, slot1) * per + a.eps);
+      f2 s = 0;
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s = f2_fma(h[i][u], h[i][u], s);
+      const float rstd = 1.0f / sqrtf(row_sum<TPR>(f2_lo(s) + f2_hi(s), slot1) * per + a.eps);
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
-        const uint32_t c = me + (uint32_t)i * TPR;
-        if (c < pieces) {
-          float g[8], b[8];
-          const float4 one = make_float4(1.f, 1.f, 1.f, 1.f), zero = make_float4(0.f, 0.f, 0.f, 0.f);
-          *reinterpret_cast<float4*>(g) = a.gain ? __ldg(reinterpret_cast<const float4*>(a.gain + c * 8)) : one;
-          *reinterpret_cast<float4*>(g + 4) = a.gain ? __ldg(reinterpret_cast<const float4*>(a.gain + c * 8 + 4)) : one;
-          *reinterpret_cast<float4*>(b) = a.bias ? __ldg(reinterpret_cast<const float4*>(a.bias + c * 8)) : zero;
-          *reinterpret_cast<float4*>(b + 4) = a.bias ? __ldg(reinterpret_cast<const float4*>(a.bias + c * 8 + 4)) : zero;
+        f2 g[4], b[4];
+        if constexpr (!KEEP) weights(me + (uint32_t)i * TPR, g, b);
 #pragma unroll
-          for (int u = 0; u < 8; ++u) h[i][u] = fmaf(h[i][u] * rstd, g[u], b[u]);
-        }
+        for (int u = 0; u < 4; ++u)                    // (beyond the last column: zero before, zero with its bias of zero)
+          h[i][u] = f2_fma(f2_mul(h[i][u], f2_pack(rstd, rstd)), KEEP ? gain[KEEP ? i : 0][u] : g[u], KEEP ? bias[KEEP ? i : 0][u] : b[u]);
       }
     }
     if (a.out) {
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const uint32_t c = me + (uint32_t)i * TPR;
-        if (c < pieces) st_stream16(a.out + (long long)row * a.out_ld + c * 8, to_bf16(h[i]));
+        if (c < pieces && ok) st_stream16(a.out + (long long)row * a.out_ld + c * 8, to_bf16x8(h[i]));
       }
     }
     if (a.q) {
-      // magnitudes compared as integers: infinities are above all numbers, and NaN above them
-      uint32_t m = 0;
+      float top = 0.f;
 #pragma unroll
       for (int i = 0; i < CH; ++i)
 #pragma unroll
-        for (int u = 0; u < 8; ++u) m = max(m, __float_as_uint(h[i][u]) & 0x7FFFFFFFu);
-      m = row_max<TPR>(m, slot2);
-      const bool bad = m >= 0x7F800000u;
-      const float top = __uint_as_float(m);
-      const float scale = bad ? __uint_as_float(0x7FC00000u) : top < NORM_TINY ? 0.f : top / (a.format == LLMCACHE_I8 ? 127.f : 448.f);
-      if (me == 0) a.scale[row] = scale;
+        for (int u = 0; u < 4; ++u) top = max_nan(top, h[i][u]);
+      // magnitudes compare as integers: infinities are above all numbers, and NaN above them
+      const uint32_t m = row_max<TPR>(__float_as_uint(top), slot2);
+      top = __uint_as_float(m);
+      const float scale = m >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : top < NORM_TINY ? 0.f : top / (a.format == LLMCACHE_I8 ? 127.f : 448.f);
+      const float inv = 1.0f / scale;
+      if (me == 0 && ok) a.scale[row] = scale;
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const uint32_t c = me + (uint32_t)i * TPR;
-        if (c < pieces) {
-          const uint2 e = !(scale > 0.f) ? make_uint2(0, 0) : a.format == LLMCACHE_I8 ? to_int8(h[i], scale) : to_e4m3(h[i], scale);
+        if (c < pieces && ok) {
+          uint2 e = make_uint2(0, 0);
+          if (scale > 0.f)
+            e = a.format == LLMCACHE_I8 ? to_int8(h[i], f2_pack(inv, inv), f2_pack(-scale, -scale)) : to_e4m3(h[i], f2_pack(inv, inv), f2_pack(-scale, -scale));
           *reinterpret_cast<uint2*>(a.q + (long long)row * a.q_ld + c * 8) = e;
         }
       }
@@ -196,24 +234,59 @@ k_norm(const NormArgs a) {
   }
 }
 
-template <int TPR, int KIND>
-cudaError_t launch_width(const NormArgs& a, uint32_t ch, int sm_count, cudaStream_t st) {
-  constexpr uint32_t ROWS = TPR == 32 ? 8 : 1, THREADS = TPR == 32 ? 256 : TPR;
-  const unsigned long long cap = (unsigned long long)sm_count * (2048 / THREADS);
+template <int TPR, int CH, int KIND>
+cudaError_t launch_shape(const NormArgs& a, int sm_count, cudaStream_t st) {
+  constexpr uint32_t ROWS = Shape<TPR>::ROWS, THREADS = Shape<TPR>::THREADS;
+  // as many blocks as run at a time: a second, partial wave of them would leave SMs idle
+  static std::atomic<int> resident{0};
+  int per_sm = resident.load(std::memory_order_relaxed);
+  if (!per_sm) {
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k_norm<TPR, CH, KIND>, THREADS, 0);
+    if (e != cudaSuccess) return e;
+    if (per_sm < 1) return cudaErrorInvalidConfiguration;
+    resident.store(per_sm, std::memory_order_relaxed);
+  }
+  // With three large arrays or more besides q, reads and writes of fewer rows at a time are easier on the memory (1,024 columns, residual
+  // and total: 124 us per 105 M elements with 12 blocks per SM, 114 with 10; with x and q alone 76 and 80).
+  if (1 + (a.residual != nullptr) + (a.total != nullptr) + (a.out != nullptr) >= 3) per_sm -= per_sm / 6;
+  const unsigned long long cap = (unsigned long long)sm_count * per_sm;
   unsigned long long blocks = ((unsigned long long)a.n_rows + ROWS - 1) / ROWS;
   if (blocks > cap) blocks = cap;
-  auto kern = ch <= 1 ? k_norm<TPR, 1, KIND> : ch == 2 ? k_norm<TPR, 2, KIND> : ch == 3 ? k_norm<TPR, 3, KIND> : k_norm<TPR, 4, KIND>;
-  return launch_k(kern, dim3((uint32_t)blocks), dim3(THREADS), 0, st, a);
+  return launch_k(k_norm<TPR, CH, KIND>, dim3((uint32_t)blocks), dim3(THREADS), 0, st, a);
+}
+
+template <int TPR, int KIND>
+cudaError_t launch_width(const NormArgs& a, uint32_t ch, int sm_count, cudaStream_t st) {
+  switch (ch) {
+    case 1: return launch_shape<TPR, 1, KIND>(a, sm_count, st);
+    case 2: return launch_shape<TPR, 2, KIND>(a, sm_count, st);
+    case 3: return launch_shape<TPR, 3, KIND>(a, sm_count, st);
+    case 4: if constexpr (TPR > 32) return launch_shape<TPR, 4, KIND>(a, sm_count, st);
+    default: return cudaErrorInvalidValue;
+  }
 }
 
 template <int KIND>
 cudaError_t launch_kind(const NormArgs& a, int sm_count, cudaStream_t st) {
-  // up to four pieces of eight elements per thread
+  // As few threads without a piece of eight elements as there may be, with up to four pieces per thread (5,000 columns: 256 threads of three
+  // pieces 104 us where 512 of two take 149); three per thread of a warp, whose registers hold the gains of no more (1,024 columns: 64
+  // threads of two 113 us, 32 of four 121).
   const uint32_t pieces = a.cols / 8;
-  auto per = [&](uint32_t threads) { return (pieces + threads - 1) / threads; };
-  if (pieces <= 32 * 4) return launch_width<32, KIND>(a, per(32), sm_count, st);
-  if (pieces <= 128 * 4) return launch_width<128, KIND>(a, per(128), sm_count, st);
-  return launch_width<512, KIND>(a, per(512), sm_count, st);
+  uint32_t best = 512, least = ~0u;
+  for (uint32_t threads = 8; threads <= 512; threads *= 2) {
+    const uint32_t ch = (pieces + threads - 1) / threads, idle = threads * ch - pieces;
+    if (ch <= (threads <= 32 ? 3 : 4) && idle < least) { best = threads; least = idle; }
+  }
+  const uint32_t ch = (pieces + best - 1) / best;
+  switch (best) {
+    case 8: return launch_width<8, KIND>(a, ch, sm_count, st);
+    case 16: return launch_width<16, KIND>(a, ch, sm_count, st);
+    case 32: return launch_width<32, KIND>(a, ch, sm_count, st);
+    case 64: return launch_width<64, KIND>(a, ch, sm_count, st);
+    case 128: return launch_width<128, KIND>(a, ch, sm_count, st);
+    case 256: return launch_width<256, KIND>(a, ch, sm_count, st);
+    default: return launch_width<512, KIND>(a, ch, sm_count, st);
+  }
 }
 
 }  // namespace
