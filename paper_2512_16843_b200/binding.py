@@ -773,6 +773,14 @@ def _other_device(t, device):
 
 def _rows(t, name, dim, shape, device):
     """[seq, token, head, 64] or [token, head, 64] view of any strides: (address, strides of sequence, token and head)."""
+    try:                                                 # (the ordinary case in as few calls as it takes)
+        st = t.stride()
+        if st[-1] == 1 and t.dtype is _BF16 and len(st) == dim and t.get_device() == device:
+            sh = t.shape
+            if sh[-1] == 64 and (shape is None or sh == shape):
+                return (t.data_ptr(), st[0], st[1], st[2]) if dim == 4 else (t.data_ptr(), 0, st[0], st[1])
+    except (AttributeError, IndexError, TypeError):
+        pass
     if not isinstance(t, torch.Tensor) or t.dtype is not _BF16 or t.dim() != dim:
         raise LLMCacheError(ERR_ARG, f"{name}: a {_BF16} tensor of {dim} dimensions is expected")
     st, sh = t.stride(), t.shape
@@ -867,10 +875,11 @@ _FORMATS = {"int8": (I8, torch.int8), "e4m3": (E4M3, torch.float8_e4m3fn)}
 _FORMAT_OF = {torch.int8: I8, torch.float8_e4m3fn: E4M3}
 _NORMS = {"none": NORM_NONE, "layer": NORM_LAYER, "rms": NORM_RMS}
 _ACTS = {"none": ACT_NONE, "gelu_erf": ACT_GELU_ERF, "gelu_tanh": ACT_GELU_TANH}
-_NORM = _Packed("@6If4xQ" + "Qq" * 5 + "3Q")
-_DENSE = _Packed("@7I4xQ" + "QqQ" * 2 + "Q" + "Qq" * 2)
-_NEW = _Packed("@4I3Q" + "Q3q" * 4 + "4Q")
+_NORM = struct.Struct("@6If4xQ" + "Qq" * 5 + "3Q")
+_DENSE = struct.Struct("@7I4xQ" + "QqQ" * 2 + "Q" + "Qq" * 2)
+_NEW = struct.Struct("@4I3Q" + "Q3q" * 4 + "4Q")
 _NORM_BYTES, _DENSE_BYTES, _NEW_BYTES = _NORM.size, _DENSE.size, _NEW.size
+_pack_norm, _pack_dense, _pack_new = _NORM.pack, _DENSE.pack, _NEW.pack
 _F32, _I32 = torch.float32, torch.int32
 
 
@@ -935,9 +944,13 @@ def llmcache_norm(x, *, kind="rms", gain=None, bias=None, eps=1e-5, residual=Non
     r_at, r_ld = (0, 0) if residual is None else _matrix(residual, _BF16, "residual", device, shape)
     t_at, t_ld = (0, 0) if total is None else _matrix(total, _BF16, "total", device, shape)
     o_at, o_ld = (0, 0) if out is None else _matrix(out, _BF16, "out", device, shape)
-    p = _NORM(_NORM_BYTES, kind_id, fmt, rows, cols, 1, eps, 0 if n_rows_dev is None else _count(n_rows_dev, device), x_at, x_ld,
-              r_at, r_ld, t_at, t_ld, o_at, o_ld, q_at, q_ld, 0 if scale is None else _addr(scale, _F32, (rows,), "scale", device),
-              0 if gain is None else _addr(gain, _F32, (cols,), "gain", device), 0 if bias is None else _addr(bias, _F32, (cols,), "bias", device))
+    try:
+        p = _pack_norm(_NORM_BYTES, kind_id, fmt, rows, cols, 1, eps, 0 if n_rows_dev is None else _count(n_rows_dev, device), x_at, x_ld,
+                       r_at, r_ld, t_at, t_ld, o_at, o_ld, q_at, q_ld, 0 if scale is None else _addr(scale, _F32, (rows,), "scale", device),
+                       0 if gain is None else _addr(gain, _F32, (cols,), "gain", device),
+                       0 if bias is None else _addr(bias, _F32, (cols,), "bias", device))
+    except struct.error as e:
+        raise LLMCacheError(ERR_ARG, str(e)) from None
     rc = lib().llmcache_norm(p, _stream_of(stream, device))
     if rc:
         raise LLMCacheError(rc, "llmcache_norm")
@@ -967,9 +980,12 @@ def llmcache_dense(a, a_scale, w, w_scale, out, *, bias=None, act="none", residu
         raise LLMCacheError(ERR_ARG, "llmcache_dense: a_scale, w_scale and out are needed")
     o_at, o_ld = _matrix(out, _BF16, "out", device, (m, n))
     r_at, r_ld = (0, 0) if residual is None else _matrix(residual, _BF16, "residual", device, (m, n))
-    p = _DENSE(_DENSE_BYTES, fmt, m, n, k, act_id, 1, 0 if n_rows_dev is None else _count(n_rows_dev, device), a_at, a_ld,
-               _addr(a_scale, _F32, (m,), "a_scale", device), w_at, w_ld, _addr(w_scale, _F32, (n,), "w_scale", device),
-               0 if bias is None else _addr(bias, _F32, (n,), "bias", device), r_at, r_ld, o_at, o_ld)
+    try:
+        p = _pack_dense(_DENSE_BYTES, fmt, m, n, k, act_id, 1, 0 if n_rows_dev is None else _count(n_rows_dev, device), a_at, a_ld,
+                        _addr(a_scale, _F32, (m,), "a_scale", device), w_at, w_ld, _addr(w_scale, _F32, (n,), "w_scale", device),
+                        0 if bias is None else _addr(bias, _F32, (n,), "bias", device), r_at, r_ld, o_at, o_ld)
+    except struct.error as e:
+        raise LLMCacheError(ERR_ARG, str(e)) from None
     rc = lib().llmcache_dense(p, _stream_of(stream, device))
     if rc:
         raise LLMCacheError(rc, "llmcache_dense")
@@ -1200,8 +1216,12 @@ class KVCache:
         p_at = side = 0
         if positions is not None:
             p_at, side = _addr(positions, _I32, (S, HK, -1), "positions", device), positions.shape[-1]
-        c = _NEW(_NEW_BYTES, S, T, pages.shape[1], _addr(cu_rows, _I32, (S + 1,), "cu_rows", device), lens_at, pages_at, *rk, *rv, *rq, *ro,
-                 p_at, 0 if first is None else _addr(first, _I32, (S,), "first", device), side, 0 if rotation is None else _address_of(rotation))
+        try:
+            c = _pack_new(_NEW_BYTES, S, T, pages.shape[1], _addr(cu_rows, _I32, (S + 1,), "cu_rows", device), lens_at, pages_at,
+                          *rk, *rv, *rq, *ro, p_at, 0 if first is None else _addr(first, _I32, (S,), "first", device), side,
+                          0 if rotation is None else _address_of(rotation))
+        except struct.error as e:
+            raise LLMCacheError(ERR_ARG, str(e)) from None
         rc = lib().llmcache_kv_append(self.handle, c, _stream_of(stream, device))
         if rc:
             raise LLMCacheError(rc, "llmcache_kv_append")

@@ -36,7 +36,7 @@ struct DenseArgs {
 };
 cudaError_t setup_dense8_tc();
 cudaError_t launch_dense8_tc(const DenseArgs& a, int sm_count, cudaStream_t st);
-constexpr uint32_t DENSE_FEW = 64;                 // most rows that k_dense8_few takes
+// up to 64 rows
 cudaError_t launch_dense8_few(const DenseArgs& a, int sm_count, cudaStream_t st);
 cudaError_t launch_dense8(const DenseArgs& a, int sm_count, cudaStream_t st);
 

@@ -1,11 +1,11 @@
 // Product of two 8-bit matrices for few rows of activations (next tokens): out[m, n] as in dense8_tc.cu, m <= 64.
 //
-// The weights are read once and nothing else is large, so the kernel is a stream of weights through registers: a block takes
-// 16 output channels and its warps share out k in pieces of 64 bytes.  mma.sync m16n8k32 sums with the channels as the rows of the
-// product and tokens as its columns, eight at a time: a tensor-memory tile would be 128 tokens high and wait for a ring of
-// copies to fill.  A lane loads 16 neighbouring bytes of a channel and of a token where the instruction's layout names four
-// words that are 16 bytes apart: the sum over k does not depend on its order as long as both operands have the same one.  The warps'
-// sums meet in shared memory; integers have one sum in any order, fp32 sums are added in the order of the warps.
+// The weights are read once and nothing else is large, so the kernel is a stream of weights through registers: a warp takes 16 output
+// channels and a share of k, in pieces of 64 bytes, with several pieces' loads in flight.  mma.sync m16n8k32 sums with the channels as the rows of the product and
+// tokens as its columns, eight at a time: a tensor-memory tile would be 128 tokens high and wait for a ring of copies to fill.  A
+// lane loads 16 neighbouring bytes of a channel and of a token where the instruction's layout names four words that are 16 bytes
+// apart: the sum over k does not depend on its order as long as both operands have the same one.  The warps' sums meet in shared memory;
+// integers have one sum in any order, fp32 sums are added in the order of the warps.
 #include "dense8.cuh"
 #include "layer_epi.cuh"
 
@@ -28,7 +28,7 @@ __device__ __forceinline__ uint4 ldw(const uint8_t* p, bool there) {
   return there ? ld_nc16(p) : make_uint4(0, 0, 0, 0);
 }
 
-// NT groups of eight tokens
+// NT groups of eight tokens; a block's warps share the k of its channels
 template <int NT, bool I8>
 __global__ void __launch_bounds__(512) k_dense8_few(const DenseArgs p) {
   griddep_sync();
@@ -49,7 +49,12 @@ __global__ void __launch_bounds__(512) k_dense8_few(const DenseArgs p) {
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) c[i][j] = 0;         // (zero bits are 0.0 too)
-  constexpr int U = NT <= 2 ? 4 : NT == 4 ? 2 : 1;                 // pieces of k in flight
+  constexpr uint32_t EACH = NT * 8 * FEW_CH;          // sums of a warp
+  // what the first result of this thread needs besides its sum, on its way behind the first weights (for eight tokens; more of them
+  // leave no registers: 64 tokens 29.6 -> 31.4 us)
+  constexpr bool AHEAD = NT == 1;
+  float sa_first = 0.f, sw_first = 0.f, b_first = 0.f, r_first = 0.f;
+  constexpr int U = NT <= 2 ? 4 : NT == 4 ? 2 : 1;   // pieces of k in flight
   const uint32_t pieces = (p.k + 63) / 64;
   for (uint32_t kb = warp; kb < pieces; kb += warps * U) {
     uint4 a[U], b[U], y[U][NT];
@@ -61,6 +66,15 @@ __global__ void __launch_bounds__(512) k_dense8_few(const DenseArgs p) {
       b[u] = ldw(w1 + k, there);
 #pragma unroll
       for (int i = 0; i < NT; ++i) y[u][i] = ldw(x[i] + k, there);
+    }
+    if (AHEAD && kb == warp) {
+      const uint32_t m = threadIdx.x / FEW_CH, n = n0 + threadIdx.x % FEW_CH;
+      if (threadIdx.x < EACH && m < M && n < p.n) {
+        sa_first = p.a_scale[m];
+        sw_first = p.w_scale[n];
+        if (p.bias) b_first = p.bias[n];
+        if (p.residual) r_first = __bfloat162float(p.residual[(long long)m * p.residual_ld + n]);
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -76,21 +90,25 @@ __global__ void __launch_bounds__(512) k_dense8_few(const DenseArgs p) {
     for (int j = 0; j < 4; ++j)                       // row of the product: g or g + 8; column: 2 t or 2 t + 1
       sums[(warp * NT * 8 + i * 8 + 2 * t + (j & 1)) * FEW_CH + g + (j >> 1) * 8] = c[i][j];
   __syncthreads();
-  for (uint32_t e = threadIdx.x; e < NT * 8 * FEW_CH; e += blockDim.x) {
+  for (uint32_t e = threadIdx.x; e < EACH; e += blockDim.x) {
     const uint32_t m = e / FEW_CH, n = n0 + e % FEW_CH;
     if (m >= M || n >= p.n) continue;
+    const uint32_t* from = sums + e;
     float v;
     if constexpr (I8) {
       int32_t s = 0;
-      for (uint32_t w = 0; w < warps; ++w) s += (int32_t)sums[w * NT * 8 * FEW_CH + e];
+      for (uint32_t w = 0; w < warps; ++w) s += (int32_t)from[w * EACH];
       v = (float)s;
     } else {
       v = 0.f;
-      for (uint32_t w = 0; w < warps; ++w) v += __uint_as_float(sums[w * NT * 8 * FEW_CH + e]);
+      for (uint32_t w = 0; w < warps; ++w) v += __uint_as_float(from[w * EACH]);
     }
     // the same operations as in dense8_tc.cu
-    v = fmaf(__fmul_rn(v, p.a_scale[m]), p.w_scale[n], p.bias ? p.bias[n] : 0.f);
-    const float r = p.residual ? __bfloat162float(p.residual[(long long)m * p.residual_ld + n]) : 0.f;
+    const bool is_first = AHEAD && e == threadIdx.x && warp < pieces;      // (a warp without a piece has not looked)
+    const float sa = is_first ? sa_first : p.a_scale[m], sw = is_first ? sw_first : p.w_scale[n];
+    const float b = is_first ? b_first : p.bias ? p.bias[n] : 0.f;
+    const float r = is_first ? r_first : p.residual ? __bfloat162float(p.residual[(long long)m * p.residual_ld + n]) : 0.f;
+    v = fmaf(__fmul_rn(v, sa), sw, b);
     if (p.act == LAYER_ACT_NONE) v = p.residual ? __fadd_rn(v, r) : v;
     else {
       const float phi = p.act == LAYER_ACT_GELU_ERF ? gelu_phi_f<false>(v) : gelu_phi_f<true>(v);
@@ -101,21 +119,24 @@ __global__ void __launch_bounds__(512) k_dense8_few(const DenseArgs p) {
 }
 
 template <int NT>
-cudaError_t launch_tokens(const DenseArgs& a, cudaStream_t st) {
-  const uint32_t pieces = (a.k + 63) / 64;
-  const uint32_t warps = pieces < 4 ? pieces : pieces < 16 ? 4 : pieces < 64 || NT == 8 ? 8 : 16;   // (at most 48 KB of sums)
+cudaError_t launch_tokens(const DenseArgs& a, int sm_count, cudaStream_t st) {
+  const uint32_t pieces = (a.k + 63) / 64, channels = (a.n + FEW_CH - 1) / FEW_CH;
+  // three pieces of k or more for a warp, up to 8 warps; 16 only where the channels do not fill the SMs (8,192 x 8,192: 17 us
+  // with 16, 14 with 8).  (48 KB of sums at most)
+  const uint32_t most = NT == 8 || channels * 8ull >= 24ull * (uint32_t)sm_count ? 8 : 16;
+  const uint32_t want = pieces < 4 ? pieces : pieces < 16 ? 4 : pieces < 64 ? 8 : 16, warps = want < most ? want : most;
   const size_t smem = (size_t)warps * NT * 8 * FEW_CH * 4;
   auto kern = a.format == LLMCACHE_I8 ? k_dense8_few<NT, true> : k_dense8_few<NT, false>;
-  return launch_k(kern, dim3((a.n + FEW_CH - 1) / FEW_CH), dim3(warps * 32), smem, st, a);
+  return launch_k(kern, dim3(channels), dim3(warps * 32), smem, st, a);
 }
 
 }  // namespace
 
-cudaError_t launch_dense8_few(const DenseArgs& a, int, cudaStream_t st) {
-  if (a.m <= 8) return launch_tokens<1>(a, st);
-  if (a.m <= 16) return launch_tokens<2>(a, st);
-  if (a.m <= 32) return launch_tokens<4>(a, st);
-  return launch_tokens<8>(a, st);
+cudaError_t launch_dense8_few(const DenseArgs& a, int sm_count, cudaStream_t st) {
+  if (a.m <= 8) return launch_tokens<1>(a, sm_count, st);
+  if (a.m <= 16) return launch_tokens<2>(a, sm_count, st);
+  if (a.m <= 32) return launch_tokens<4>(a, sm_count, st);
+  return launch_tokens<8>(a, sm_count, st);
 }
 
 }  // namespace llmc
