@@ -43,7 +43,7 @@ struct D8 {
 
 __device__ __forceinline__ float4 ldg4(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
 
-__device__ const float d8_no_bias[64] = {};
+__device__ __align__(16) const float d8_no_bias[64] = {};
 
 // 16 columns of a row: scales s, biases b, activation, residual r (pairs of bf16); y: pairs of neighbouring columns
 template <bool I8, uint32_t ACT, bool RES>

@@ -1,4 +1,4 @@
-"""Derives the coefficients of the erf polynomial in layer_gemm.cu (not part of the build; run by hand).
+"""Derives the coefficients of the erf polynomial in layer_epi.cuh (not part of the build; run by hand).
 
 GELU(x) = x/2 + |x|/2 * erf(|x| / sqrt 2).  On u = min(|x|, 3.3 sqrt 2) the odd polynomial u * Q(u^2) with nine
 coefficients replaces erf(u / sqrt 2); beyond the clamp erf is within 3.1e-6 of its value there.  The fit

@@ -172,6 +172,10 @@ size_t layer_ws8_bytes(const llmcache_layer_desc& D) {
   return total;
 }
 constexpr uint32_t NORM_MOST = 16384;      // columns of a row that k_norm takes
+// whether k_norm can stand in for the layer's norms (its rows are counted in 31 bits)
+bool norm_serves(const llmcache_layer_desc& D) {
+  return D.d_model <= NORM_MOST && (uint64_t)D.max_seqs * D.seq_len <= 0x7FFFFFFFull;
+}
 }  // namespace
 
 extern "C" {
@@ -301,7 +305,7 @@ int llmcache_layer_score_mods(llmcache_layer_t* L, const llmcache_score_mods* mo
 
 int llmcache_layer_rms(llmcache_layer_t* L, uint32_t on) {
   if (!L || on > 1) return LLMCACHE_ERR_ARG;
-  if (on && L->desc.d_model > NORM_MOST) return LLMCACHE_ERR_UNSUPPORTED;
+  if (on && !norm_serves(L->desc)) return LLMCACHE_ERR_UNSUPPORTED;
   L->rms = on != 0;
   return LLMCACHE_OK;
 }
@@ -328,7 +332,7 @@ int llmcache_layer_quantise(llmcache_layer_t* L, uint32_t format, void* workspac
   const llmcache_layer_desc& D = L->desc;
   const size_t need = layer_ws8_bytes(D);
   if (format != LLMCACHE_BF16) {
-    if (D.d_model > NORM_MOST || D.ffn > NORM_MOST) return LLMCACHE_ERR_UNSUPPORTED;
+    if (!norm_serves(D) || D.ffn > NORM_MOST) return LLMCACHE_ERR_UNSUPPORTED;
     if ((uintptr_t)workspace % WS_ALIGN) return LLMCACHE_ERR_ARG;
     if (workspace && workspace_bytes < need) return LLMCACHE_ERR_NOMEM;
     if (workspace && !pointer_on_device(workspace, D.device)) return LLMCACHE_ERR_ARG;
