@@ -36,6 +36,11 @@ struct DenseArgs {
 };
 cudaError_t setup_dense8_tc();
 cudaError_t launch_dense8_tc(const DenseArgs& a, int sm_count, cudaStream_t st);
+// a long k shared by clusters of blocks: how many blocks per tile (1: not worth it)
+constexpr uint32_t SPLIT_LEAST = 24;               // steps of 128 bytes of k, at least
+cudaError_t setup_dense8_split();
+uint32_t dense8_split_parts(const DenseArgs& a);
+cudaError_t launch_dense8_split(const DenseArgs& a, uint32_t parts, cudaStream_t st);
 // up to 64 rows
 cudaError_t launch_dense8_few(const DenseArgs& a, int sm_count, cudaStream_t st);
 cudaError_t launch_dense8(const DenseArgs& a, int sm_count, cudaStream_t st);

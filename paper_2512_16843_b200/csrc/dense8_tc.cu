@@ -448,6 +448,7 @@ cudaError_t setup_dense8_tc() {
   if (e == cudaSuccess) e = setup_shape<2, 256>();
   if (e == cudaSuccess) e = setup_shape<1, 128>();
   if (e == cudaSuccess) e = setup_shape<1, 64>();
+  if (e == cudaSuccess) e = setup_dense8_split();
   int dev = 0, pairs = 0;
   if (e == cudaSuccess) e = cudaGetDevice(&dev);
   if (e == cudaSuccess && (dev < 0 || dev >= MAX_DEVICES)) e = cudaErrorInvalidDevice;
@@ -468,7 +469,8 @@ cudaError_t launch_dense8_tc(const DenseArgs& a, int sm_count, cudaStream_t st) 
   const unsigned long long mb = (a.m + DM - 1) / DM, sms = (unsigned long long)sm_count;
   if ((mb + 1) / 2 * ((a.n + 255) / 256) * 2 >= sms) return launch_shape<2, 256>(a, sm_count, st);
   if (mb * ((a.n + 127) / 128) >= sms) return launch_shape<1, 128>(a, sm_count, st);
-  return launch_shape<1, 64>(a, sm_count, st);
+  const uint32_t parts = dense8_split_parts(a);
+  return parts > 1 ? launch_dense8_split(a, parts, st) : launch_shape<1, 64>(a, sm_count, st);
 }
 
 }  // namespace llmc

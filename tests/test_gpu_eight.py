@@ -231,6 +231,13 @@ DENSE = [
     (2500, 2304, 768, True, "gelu_erf", False),
     (5000, 1024, 4096, True, "none", True),
     (4001, 2047, 1040, True, "gelu_tanh", True),
+    # a long k shared by clusters of 8, 4 and 2 blocks
+    (100, 33, 8192, True, "gelu_erf", True),
+    (70, 2, 2960, False, "none", False),
+    (65, 1024, 4096, True, "none", True),
+    (300, 500, 3088, False, "gelu_tanh", False),
+    (513, 700, 4112, True, "none", True),
+    (129, 1983, 3200, True, "gelu_erf", False),
 ]
 
 
@@ -260,12 +267,13 @@ def test_dense_against_the_oracle(m, n, k, bias, act, residual, to):
         assert torch.equal(bits(r2[:, :n]), bits(out))
 
 
-def test_int8_rows_do_not_depend_on_how_many_there_are():
-    """Whole-number sums and one arithmetic behind them: the kernels for few and for many rows give the same bits."""
-    n, k = 777, 1040
+@pytest.mark.parametrize("n,k", [(777, 1040), (300, 4016)])
+def test_int8_rows_do_not_depend_on_how_many_there_are(n, k):
+    """Whole-number sums and one arithmetic behind them: all kernels give the same bits."""
     a, sa = eight_matrix(2000, k, "int8", 1)
     w, sw = eight_matrix(n, k, "int8", 2)
-    sa, sw, b, r = sa / 40, sw / 1300, torch.randn(n, device=DEV), rnd(2000, 784, seed=4)[:, :n]
+    b = torch.randn(n, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV)
+    sa, sw, r = sa / 40, sw / (40 * k ** 0.5), rnd(2000, 784, seed=4)[:, :n]
     for act in ("none", "gelu_erf", "gelu_tanh"):
         whole = torch.zeros((2000, 784), dtype=BF, device=DEV)[:, :n]
         L.llmcache_dense(a, sa, w, sw, whole, bias=b, act=act, residual=r)
@@ -290,10 +298,9 @@ def test_largest_sums(m):
         assert torch.equal(out, want.expand(rows, n))
 
 
-@pytest.mark.parametrize("m,n", [(20, 100), (300, 200), (1000, 2304)])
+@pytest.mark.parametrize("m,n,k", [(20, 100, 160), (300, 200, 160), (1000, 2304, 160), (300, 200, 4000)])
 @pytest.mark.parametrize("to", ["int8", "e4m3"])
-def test_dense_with_a_row_count(m, n, to):
-    k = 160
+def test_dense_with_a_row_count(m, n, k, to):
     a, sa = eight_matrix(m, k, to, 5)
     w, sw = eight_matrix(n, k, to, 6)
     r = rnd(m, n + (-n) % 8, seed=7)[:, :n]
@@ -382,14 +389,14 @@ def test_expired_wait_is_reported_and_the_next_call_runs():
         import torch
         from paper_2512_16843_b200 import binding as L
         g = torch.Generator(device="cuda").manual_seed(1)
-        for dtype, m, n in ((torch.int8, 200, 96), (torch.float8_e4m3fn, 5000, 1000)):
-            a, w = (torch.randn((r, 256), generator=g, device="cuda").mul(20).to(dtype) for r in (m, n))
+        for dtype, m, n, k in ((torch.int8, 200, 96, 256), (torch.float8_e4m3fn, 5000, 1000, 256), (torch.int8, 200, 96, 4096)):
+            a, w = (torch.randn((r, k), generator=g, device="cuda").mul(20).to(dtype) for r in (m, n))
             s = torch.ones(5000, device="cuda")
             r = torch.randn((m, n), generator=g, device="cuda").to(torch.bfloat16)
             call = lambda out: L.llmcache_dense(a, s[:m], w, s[:n], out, residual=r)
             want, out = torch.zeros_like(r), torch.zeros_like(r)
             call(want)
-            if dtype is torch.int8:
+            if dtype is torch.int8 and k == 256:
                 assert L.llmcache_dense_status() == L.OK
             L.llmcache_dense_debug_knobs(1_000_000, L.KNOB_PRODUCER_IDLE)
             call(out)
