@@ -41,7 +41,7 @@ constexpr uint32_t SPLIT_LEAST = 24;               // steps of 128 bytes of k, a
 cudaError_t setup_dense8_split();
 uint32_t dense8_split_parts(const DenseArgs& a);
 cudaError_t launch_dense8_split(const DenseArgs& a, uint32_t parts, cudaStream_t st);
-// up to 64 rows
+// up to 32 rows
 cudaError_t launch_dense8_few(const DenseArgs& a, int sm_count, cudaStream_t st);
 cudaError_t launch_dense8(const DenseArgs& a, int sm_count, cudaStream_t st);
 

@@ -57,11 +57,10 @@ namespace llmc {
 cudaError_t launch_dense8(const DenseArgs& a, int sm_count, cudaStream_t st) {
   if (a.m == 0) return cudaSuccess;
   // Up to 8 rows the weights are all there is to read.  Beyond that the other kernel's 128-row tiles pay once their copies come from
-  // half of the SMs or more (8,192 x 8,192: 16 rows of e4m3 29 us here, 22 there; 32 rows of int8 36 and 22); with fewer tiles
-  // the streams through registers are quicker up to 64 rows, up to 32 of e4m3, whose values their instruction widens first, or where
-  // clusters share a long k (4,096 x 1,024: 64 rows 5.9 and 6.1, of e4m3 7.1 and 6.2; 1,024 x 4,096: 32 rows 5.8 and 8.4, 64 rows 10.8 and 8.4).
-  const bool i8 = a.format == LLMCACHE_I8, wide = 2ull * ((a.n + 63) / 64) >= (unsigned long long)sm_count;
-  const uint32_t most = wide ? (i8 ? 16u : 8u) : i8 && dense8_split_parts(a) == 1 ? 64u : 32u;
+  // half of the SMs or more (8,192 x 8,192: 16 rows of e4m3 29 us here, 22 there; 32 rows of int8 36 and 22); with fewer tiles the
+  // streams through registers are quicker up to 32 rows (1,024 x 4,096: 5.8 and 8.4; 4,096 x 1,024: 4.4 and 6.1; 64 rows: 10.8 and 8.4, 5.8 and 6.1).
+  const bool wide = 2ull * ((a.n + 63) / 64) >= (unsigned long long)sm_count;
+  const uint32_t most = !wide ? 32u : a.format == LLMCACHE_I8 ? 16u : 8u;
   if (a.m <= most && !a.vt.ptr) return launch_dense8_few(a, sm_count, st);
   return launch_dense8_tc(a, sm_count, st);
 }

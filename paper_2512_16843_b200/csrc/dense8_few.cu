@@ -1,4 +1,4 @@
-// Product of two 8-bit matrices for few rows of activations (next tokens): out[m, n] as in dense8_tc.cu, m <= 64.
+// Product of two 8-bit matrices for few rows of activations (next tokens): out[m, n] as in dense8_tc.cu, m <= 32.
 //
 // The weights are read once and nothing else is large, so the kernel is a stream of weights through registers: a warp takes 16 output
 // channels and a share of k, in pieces of 64 bytes, with several pieces' loads in flight.  mma.sync m16n8k32 sums with the channels as the rows of the product and
@@ -50,11 +50,11 @@ __global__ void __launch_bounds__(512) k_dense8_few(const DenseArgs p) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) c[i][j] = 0;         // (zero bits are 0.0 too)
   constexpr uint32_t EACH = NT * 8 * FEW_CH;          // sums of a warp
-  // what the first result of this thread needs besides its sum, on its way behind the first weights (for eight tokens; more of them
-  // leave no registers: 64 tokens 29.6 -> 31.4 us)
+  // what the first result of this thread needs besides its sum, on its way behind the first weights (for eight tokens: 2,304 x 768 2.3 ->
+  // 2.0 us, 1,024 x 4,096 4.2 -> 2.9; with more of them it costs registers that the loads need)
   constexpr bool AHEAD = NT == 1;
   float sa_first = 0.f, sw_first = 0.f, b_first = 0.f, r_first = 0.f;
-  constexpr int U = NT <= 2 ? 4 : NT == 4 ? 2 : 1;   // pieces of k in flight
+  constexpr int U = NT <= 2 ? 4 : 2;                 // pieces of k in flight
   const uint32_t pieces = (p.k + 63) / 64;
   for (uint32_t kb = warp; kb < pieces; kb += warps * U) {
     uint4 a[U], b[U], y[U][NT];
@@ -122,8 +122,8 @@ template <int NT>
 cudaError_t launch_tokens(const DenseArgs& a, int sm_count, cudaStream_t st) {
   const uint32_t pieces = (a.k + 63) / 64, channels = (a.n + FEW_CH - 1) / FEW_CH;
   // three pieces of k or more for a warp, up to 8 warps; 16 only where the channels do not fill the SMs (8,192 x 8,192: 17 us
-  // with 16, 14 with 8).  (48 KB of sums at most)
-  const uint32_t most = NT == 8 || channels * 8ull >= 24ull * (uint32_t)sm_count ? 8 : 16;
+  // with 16, 15 with 8)
+  const uint32_t most = channels * 8ull >= 24ull * (uint32_t)sm_count ? 8 : 16;
   const uint32_t want = pieces < 4 ? pieces : pieces < 16 ? 4 : pieces < 64 ? 8 : 16, warps = want < most ? want : most;
   const size_t smem = (size_t)warps * NT * 8 * FEW_CH * 4;
   auto kern = a.format == LLMCACHE_I8 ? k_dense8_few<NT, true> : k_dense8_few<NT, false>;
@@ -135,8 +135,7 @@ cudaError_t launch_tokens(const DenseArgs& a, int sm_count, cudaStream_t st) {
 cudaError_t launch_dense8_few(const DenseArgs& a, int sm_count, cudaStream_t st) {
   if (a.m <= 8) return launch_tokens<1>(a, sm_count, st);
   if (a.m <= 16) return launch_tokens<2>(a, sm_count, st);
-  if (a.m <= 32) return launch_tokens<4>(a, sm_count, st);
-  return launch_tokens<8>(a, sm_count, st);
+  return a.m <= 32 ? launch_tokens<4>(a, sm_count, st) : cudaErrorInvalidValue;
 }
 
 }  // namespace llmc
