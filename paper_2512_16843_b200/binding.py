@@ -959,7 +959,7 @@ def llmcache_norm(x, *, kind="rms", gain=None, bias=None, eps=1e-5, residual=Non
 def llmcache_dense(a, a_scale, w, w_scale, out, *, bias=None, act="none", residual=None, n_rows_dev=None, stream=None) -> None:
     """out = act(a_scale w_scale (a w^T) + bias) + residual for 8-bit a [m, k] and w [n, k] of one type (int8: exact sums;
     float8_e4m3fn) with f32 scales [m], [n]; bias f32 [n]; out, residual bf16 [m, n].  act: "none", "gelu_erf" or "gelu_tanh".
-    n_rows_dev: int32 on the device, only that many rows are processed."""
+    n_rows_dev: int32 on the device, only that many rows are processed.  All but a_scale and n_rows_dev are 16-byte aligned."""
     if not isinstance(a, torch.Tensor) or not isinstance(w, torch.Tensor):
         raise LLMCacheError(ERR_ARG, "llmcache_dense: a and w are tensors")
     dt = a.dtype

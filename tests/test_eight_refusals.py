@@ -46,6 +46,8 @@ def rows(r=4, c=64, dtype=BF):
     (dict(kind="batch"), L.ERR_ARG),
     (dict(eps=float("nan")), L.ERR_ARG),
     (dict(eps=float("inf")), L.ERR_ARG),
+    (dict(eps=1e300), L.ERR_ARG),
+    (dict(eps="small"), L.ERR_ARG),
     (dict(n_rows_dev=torch.zeros(1)), L.ERR_ARG),
     (dict(n_rows_dev=torch.zeros(0, dtype=I32)), L.ERR_ARG),
 ])
@@ -70,6 +72,7 @@ def test_norm_refuses(change, status):
     (dict(out=rows(4, 9)), L.ERR_SHAPE), (dict(out=rows(4, 8, F32)), L.ERR_ARG),
     (dict(out=rows(4, 12)[:, :8]), L.ERR_SHAPE),                                             # a leading dimension of 12
     (dict(residual=rows(3, 8)), L.ERR_SHAPE), (dict(residual=rows(4, 12)[:, :8]), L.ERR_SHAPE),
+    (dict(w_scale=torch.zeros(9)[1:]), L.ERR_ARG), (dict(bias=torch.zeros(9)[1:]), L.ERR_ARG),     # 4-byte alignment
     (dict(act="relu"), L.ERR_ARG),
     (dict(n_rows_dev=3), L.ERR_ARG),
 ])

@@ -218,10 +218,11 @@ DENSE = [
     (9, 31, 4096, False, "none", True),
     (16, 129, 144, True, "gelu_tanh", True),
     (17, 64, 1040, True, "none", False),
+    (32, 72, 96, True, "gelu_erf", True),                    # the last size of the kernel for few rows
     (33, 100, 208, True, "gelu_erf", False),
     (64, 2304, 768, True, "none", False),
     (64, 33, 8192, True, "none", True),
-    (65, 40, 32, True, "none", True),                        # the first size of the other kernel
+    (65, 40, 32, True, "none", True),
     (65, 1, 16, True, "none", True),
     (128, 64, 128, False, "none", False),
     (129, 95, 144, True, "gelu_erf", True),
@@ -277,7 +278,7 @@ def test_int8_rows_do_not_depend_on_how_many_there_are(n, k):
     for act in ("none", "gelu_erf", "gelu_tanh"):
         whole = torch.zeros((2000, 784), dtype=BF, device=DEV)[:, :n]
         L.llmcache_dense(a, sa, w, sw, whole, bias=b, act=act, residual=r)
-        for m in (1, 5, 12, 30, 64, 65, 300, 700):
+        for m in (1, 5, 12, 30, 32, 33, 64, 65, 300, 700):
             out = torch.zeros((m, 784), dtype=BF, device=DEV)[:, :n]
             L.llmcache_dense(a[:m], sa[:m], w, sw, out, bias=b, act=act, residual=r[:m])
             assert torch.equal(out, whole[:m]), (act, m)
@@ -360,6 +361,64 @@ def test_both_on_another_stream_and_in_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+def test_two_streams_at_a_time():
+    """Calls share nothing but the status word: two chains of them, side by side, give what each gives alone."""
+    shapes, chains = ((300, 512, 640), (64, 4096, 1024)), []
+    for i, (m, d, n) in enumerate(shapes):
+        x, (w, sw) = rnd(m, d, seed=41 + i), eight_matrix(n, d, "int8", 43 + i)
+        q, s = torch.zeros((m, d), dtype=torch.int8, device=DEV), torch.zeros(m, device=DEV)
+        chains.append((x, w, sw, q, s, [torch.zeros((m, n), dtype=BF, device=DEV) for _ in range(20)], torch.cuda.Stream()))
+
+    def step(c, i, stream):
+        x, w, sw, q, s, outs, _ = c
+        L.llmcache_norm(x, kind="none", q=q, scale=s, stream=stream)
+        L.llmcache_dense(q, s, w, sw, outs[i], act="gelu_erf", stream=stream)
+
+    torch.cuda.synchronize()
+    want = []
+    for c in chains:
+        step(c, 0, None)
+        torch.cuda.synchronize()
+        want.append(c[5][0].clone())
+        c[5][0].zero_()
+    torch.cuda.synchronize()
+    for i in range(20):
+        for c in chains:
+            step(c, i, c[6])
+    torch.cuda.synchronize()
+    for c, w in zip(chains, want):
+        assert all(torch.equal(o, w) for o in c[5])
+    assert L.llmcache_dense_status() == L.OK
+
+
+def test_matrices_of_more_than_2_31_elements():
+    m, k = 40000, 64
+    for n, to in ((60000, "int8"), (60001, "e4m3")):
+        a, sa = eight_matrix(m, k, to, 51)
+        w, sw = eight_matrix(n, k, to, 52)
+        sa, sw = sa / 100, sw / 800
+        out, whole = filled(m, 60008, n, BF)
+        L.llmcache_dense(a, sa, w, sw, out, residual=out)
+        torch.cuda.synchronize()
+        rows = [0, 17895, 17896, 35786, 35787, 35791, 35792, m - 129, m - 1]
+        check_dense(out[rows], a[rows], sa[rows], w, sw, to, None, "none", torch.full((len(rows), n), 7.0, dtype=BF, device=DEV))
+        assert torch.all(whole[:, n:] == 7)
+        del out, whole
+    rows, cols = 140000, 16384
+    x = torch.randn((rows, cols), generator=torch.Generator(device=DEV).manual_seed(53), dtype=BF, device=DEV)
+    t, q, s = torch.zeros_like(x), torch.zeros((rows, cols), dtype=torch.int8, device=DEV), torch.zeros(rows, device=DEV)
+    L.llmcache_norm(x, total=t, q=q, scale=s)
+    torch.cuda.synchronize()
+    assert torch.equal(t, x)
+    some = [0, 65535, 65536, 131071, 131072, rows - 1]
+    _, y, tol = norm_bounds(f64(x[some]), None, "rms", None, None)
+    check_eight(q[some], s[some], y, tol, "int8")
+    q2, s2 = torch.zeros_like(q[130000:]), torch.zeros_like(s[130000:])
+    L.llmcache_norm(x[130000:], q=q2, scale=s2)
+    assert torch.equal(q2, q[130000:]) and torch.equal(s2, s[130000:])
+    assert L.llmcache_dense_status() == L.OK
 
 
 def test_norm_and_product_together():

@@ -374,3 +374,39 @@ def test_extend_of_a_quantised_layer_captured():
         assert torch.equal(out, want)
     kv.close()
     layer.close()
+
+
+@pytest.mark.parametrize("pre_ln", [False, True])
+def test_large_batches_equal_small_ones(pre_ln):
+    """Rows of int8 layers do not depend on what else is in the batch, whatever kernels its size takes."""
+    n, d, heads, S = 128, 768, 12, 40
+    layer = L.Layer(weights(d, 2048, 17), heads=heads, seq_len=n, max_seqs=S, pre_ln=pre_ln, causal=pre_ln, tanh_gelu=pre_ln)
+    layer.quantise("int8")
+    layer.rms()
+    layer.rotation(rotation(64, False))
+    x = rnd(S, n, d, seed=71)
+    out, part = torch.zeros_like(x), torch.zeros_like(x[:3])
+    layer.forward(x, out)
+    for s in (0, 17, 37):
+        layer.forward(x[s:s + 3].contiguous(), part)
+        torch.cuda.synchronize()
+        assert torch.equal(part, out[s:s + 3]), s
+    assert layer.status() == L.OK
+    layer.close()
+
+
+def test_settings_and_calls_on_another_stream():
+    n, d, heads, S = 40, 128, 2, 3
+    layer = L.Layer(weights(d, 256, 27), heads=heads, seq_len=n, max_seqs=S)
+    x = rnd(S, n, d, seed=81)
+    out, want = torch.zeros_like(x), torch.zeros_like(x)
+    layer.quantise("int8")
+    layer.forward(x, want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    layer.quantise(None)
+    layer.quantise("int8", stream=side)
+    layer.forward(x, out, stream=side)
+    side.synchronize()
+    assert torch.equal(out, want)
+    layer.close()

@@ -126,6 +126,37 @@ def test_append_against_the_oracle(rows, lens, H, HK, page, dims, interleaved):
     c.kv.close()
 
 
+@pytest.mark.parametrize("H,HK,dims,interleaved", [(24, 8, 64, False), (12, 4, 32, True), (33, 11, 48, False)])
+def test_long_prompts(H, HK, dims, interleaved):
+    """As many rows as fill the device: the lanes of a warp take four heads each."""
+    rows = [2500, 2411, 1]
+    c = Case(rows, [2600, 2411, 77], H, HK, 64, 13)
+    inv = freqs(dims)
+    q_out = torch.full((sum(rows), H, 64), 7.0, dtype=BF, device=DEV)
+    q, k, v, before = c.expected(None, inv.cpu().numpy(), interleaved)
+    c.kv.append(c.k_new, c.v_new, q=c.q, q_out=q_out, rotation=L.make_rotation(inv, interleaved=interleaved), **c.args)
+    close(q_out, q, f64(c.q))
+    close(c.k, k, before)
+    assert np.array_equal(f64(c.v), v)
+    c.kv.close()
+
+
+def test_pages_beyond_2_31_elements():
+    HK, page, num, n = 8, 64, 65540, 130                 # 32,768 elements in a page
+    k, v = (torch.zeros((num, HK, page, 64), dtype=BF, device=DEV) for _ in range(2))
+    kv = L.KVCache(k, v, heads=8, max_seqs=1, max_rows=n, max_len=192)
+    kn, vn, table = rnd(n, HK, 64, seed=61), rnd(n, HK, 64, seed=62), [65539, 65535, 65536]
+    inv = freqs(64)
+    kv.append(kn, vn, rotation=L.make_rotation(inv), cu_rows=i32([0, n]), lens=i32([n]), pages=i32([table]))
+    torch.cuda.synchronize()
+    flat = lambda t: t[table].transpose(1, 2).reshape(192, HK, 64)
+    close(flat(k)[:n], E.rotate(f64(kn), np.arange(n), inv.cpu().numpy()), f64(kn))
+    assert torch.equal(flat(v)[:n], vn) and not flat(k)[n:].any()
+    k[table], v[table] = 0, 0
+    assert not k.any() and not v.any()
+    kv.close()
+
+
 def test_positions_up_to_the_largest():
     """Angles of far positions, where an f32 product would have lost them, and negative ones."""
     B = 6
