@@ -67,25 +67,22 @@ __device__ __forceinline__ uint4 bf16x8(const unsigned long long* y) {
   return make_uint4(pack_bf16(f2_lo(y[0]), f2_hi(y[0])), pack_bf16(f2_lo(y[1]), f2_hi(y[1])), pack_bf16(f2_lo(y[2]), f2_hi(y[2])),
                     pack_bf16(f2_lo(y[3]), f2_hi(y[3])));
 }
-// A warp's 32 rows of 64 columns between its box and memory by plain copies, two columns per lane: rows and columns beyond the ends
-// stay out.  TO_BOX: from memory.
-template <bool TO_BOX, typename T>
-__device__ __noinline__ void plain_box(T* at, long long ld, uint32_t row0, uint32_t col0, uint32_t M, uint32_t N, uint32_t box, uint32_t lane) {
+// A warp's 32 rows of 64 columns from its box to memory by plain copies, two columns per lane, eight rows at a time: rows and columns beyond the
+// ends stay out.
+__device__ __noinline__ void plain_box(__nv_bfloat16* at, long long ld, uint32_t row0, uint32_t col0, uint32_t M, uint32_t N, uint32_t box, uint32_t lane) {
   const uint32_t col = col0 + 2 * lane, rows = min(32u, M - row0);
 #pragma unroll 1
-  for (uint32_t r = 0; r < rows; ++r) {
-    const uint32_t word = box + r * 128 + (((lane >> 2) ^ (r & 7u)) << 4) + (lane & 3u) * 4;
-    T* p = at + (long long)(row0 + r) * ld + col;
-    if constexpr (TO_BOX) {
-      uint32_t w = 0;
-      if (col + 1 < N) w = *reinterpret_cast<const uint32_t*>(p);
-      else if (col < N) w = __bfloat16_as_ushort(*p);
-      asm volatile("st.shared.u32 [%0], %1;" ::"r"(word), "r"(w) : "memory");
-    } else {
-      uint32_t w;
-      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(word) : "memory");
-      if (col + 1 < N) *reinterpret_cast<uint32_t*>(p) = w;
-      else if (col < N) *p = __ushort_as_bfloat16((unsigned short)w);
+  for (uint32_t r0 = 0; r0 < rows; r0 += 8) {
+    uint32_t w[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[i]) : "r"(box + (r0 + i) * 128 + (((lane >> 2) ^ i) << 4) + (lane & 3u) * 4) : "memory");
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      __nv_bfloat16* p = at + (long long)(row0 + r0 + i) * ld + col;
+      if (r0 + i >= rows) break;
+      if (col + 1 < N) *reinterpret_cast<uint32_t*>(p) = w[i];
+      else if (col < N) *p = __ushort_as_bfloat16((unsigned short)w[i]);
     }
   }
   __syncwarp();
@@ -153,8 +150,9 @@ k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   const uint32_t tmem_base = *tmem_slot;
 
   uint32_t issued = 0;
+  const bool leader = elect_one();
   if (warp == 0) {
-    if (lane == 0 && !producer_idle(p.status)) {       // ---- TMA producer
+    if (leader && !producer_idle(p.status)) {       // ---- TMA producer
       bool ok = true;
       for (uint32_t t = first; t < n_tiles && ok; t += step) {
         const int row = (int)(tile_mb(t) * (CTAS * DM) + rank * DM), col = (int)(tile_nb(t) * BN + rank * (BN / CTAS));
@@ -181,7 +179,7 @@ k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       if (!ok) { *abort_flag = 1; atomicExch(p.status, 1u); }
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {                      // ---- MMA issuer
+    if (leader && rank == 0) {                         // ---- MMA issuer
       // operand types: signed 8-bit integers into 32-bit ones, or e4m3 into fp32
       constexpr uint32_t idesc = (I8 ? (2u << 4) | (1u << 7) | (1u << 10) : (1u << 4)) | ((uint32_t)(BN >> 3) << 17) |
                                  ((uint32_t)((CTAS * DM) >> 4) << 24);
@@ -220,33 +218,30 @@ k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     const uint32_t row_in_tile = rank * DM + quarter * 32;
     const uint32_t box = base + S::BOX + ew * D_BOX;
     const uint32_t my_row = (box + lane * 128u) | ((lane & 7u) << 4);      // piece c of the row is at my_row ^ (c << 4): the swizzle
-    // Columns are cut off by the copy engine in pieces of 16 bytes: 64 columns that end inside one use plain stores, as do the
-    // rows of a partial block whose number came from the device, and transposed V columns.
-    const uint32_t n_boxed = N % 8 ? N / 64 * 64 : N;
-    auto boxed = [&](uint32_t row0, uint32_t col0) {
-      return row0 < M && col0 < n_boxed && (M == p.m || row0 + 32 <= M) && !(VT && col0 >= p.vt.col0);
-    };
+    // The copy engine cuts columns off in pieces of 16 bytes, so that it stores up to N8 and the lanes the rest, each of its row.  Plain
+    // stores for the rows of a partial block whose number came from the device.
+    const uint32_t N8 = N & ~7u;
     uint32_t r_issued = 0, r_used = 0;
-    auto fetch_residual = [&](uint32_t t) {            // (lane 0; the box is free)
+    auto fetch_residual = [&](uint32_t t) {            // (the leader; the box is free.  Rows from M to p.m are there too)
       if (t >= n_tiles) return;
       const uint32_t row0 = tile_mb(t) * (CTAS * DM) + row_in_tile, col0 = tile_nb(t) * BN + col_in_tile;
-      if (!boxed(row0, col0)) return;
+      if (row0 >= M || col0 >= N) return;
       mbar_expect_tx(res_bar(ew), D_BOX);
       tma_load_2d(box, &map_res, (int)col0, (int)row0, res_bar(ew));
       ++r_issued;
     };
-    if (RES && lane == 0) fetch_residual(first);
+    if (RES && leader) fetch_residual(first);
     uint32_t tile = 0;
     bool live = true;
     for (uint32_t t = first; t < n_tiles && live; t += step, ++tile) {
       const uint32_t buf = tile & 1u, bph = (tile >> 1) & 1u;
       const uint32_t row0 = tile_mb(t) * (CTAS * DM) + row_in_tile, col0 = tile_nb(t) * BN + col_in_tile;
       const uint32_t row = row0 + lane;
-      const bool some = row0 < M && col0 < N, in_box = boxed(row0, col0);
+      const bool some = row0 < M && col0 < N, whole_rows = M == p.m || row0 + 32 <= M;
       const float sa = row < M ? __ldg(p.a_scale + row) : 0.f;
       // a wait that ran out ends the warp's work: nothing more is read, and nothing asked for that is not waited for
       live = __all_sync(0xFFFFFFFFu, mbar_wait(tfull_bar(buf), bph, abort_flag, lim));
-      if (live && RES && in_box) {
+      if (live && RES && some) {
         live = __all_sync(0xFFFFFFFFu, mbar_wait(res_bar(ew), r_used & 1u, abort_flag, lim));
         if (live) ++r_used;
       }
@@ -260,7 +255,7 @@ k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       auto release = [&]() {                           // the accumulator's columns are in registers: it may be filled again
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
+        if (leader) {
           if constexpr (CTAS == 2) mbar_arrive_cluster(of_rank0(tempty_bar(buf))); else mbar_arrive(tempty_bar(buf));
         }
       };
@@ -284,11 +279,10 @@ k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         }
       };
       if (!RES && some) {                              // the box's last rows have been read out
-        if (lane == 0) bulk_wait_read<0>();
+        if (leader) bulk_wait_read<0>();
         __syncwarp();
       }
       if (some && col0 + 64 <= N) {                    // nearly all tiles
-        if (RES && !in_box) plain_box<true>(p.residual, p.residual_ld, row0, col0, M, N, box, lane);
         uint32_t v[2][16];                             // one step ahead of the arithmetic
         tc_ld_32x16(taddr, v[0]);
 #pragma unroll
@@ -304,17 +298,16 @@ k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           sixteen(u, v[u & 1], s, b);
         }
       } else {
-        if (RES && some && !in_box) plain_box<true>(p.residual, p.residual_ld, row0, col0, M, N, box, lane);
 #pragma unroll 1
         for (uint32_t u = 0; some && u < 4 && col0 + u * 16 < N; ++u) {
           uint32_t v[16];
           tc_ld_32x16(taddr + u * 16, v);
           float s[16], b[16];
 #pragma unroll
-          for (uint32_t i = 0; i < 16; ++i) {          // nothing is read beyond the last column
-            const bool there = col0 + u * 16 + i < N;
-            s[i] = there ? __ldg(ws + u * 16 + i) : 0.f;
-            b[i] = there ? __ldg(bs + u * 16 + i) : 0.f;
+          for (uint32_t i = 0; i < 16; ++i) {          // (beyond the last column: its values again, whose results are dropped)
+            const uint32_t c = min(u * 16 + i, N - 1 - col0);
+            s[i] = __ldg(ws + c);
+            b[i] = __ldg(bs + c);
           }
           tc_wait_ld_16(v);
           sixteen(u, v, s, b);
@@ -322,26 +315,35 @@ k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         release();
       }
       if (some && !transposed) {
+        const bool rest = N8 < N && N8 < col0 + 64;
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (rest) put4(lds16(my_row ^ ((N8 - col0) / 8 << 4)), w);
         fence_async_smem();
         __syncwarp();
-        if (in_box) {
-          if (lane == 0) {
+        if (whole_rows) {
+          if (leader && col0 < N8) {
             tma_store_2d(&map_out, (int)col0, (int)row0, box);
             bulk_commit();
           }
+          if (rest && row < M) {
+            __nv_bfloat16* at = p.out + (long long)row * p.out_ld + N8;
+#pragma unroll
+            for (uint32_t i = 0; i < 7; ++i)
+              if (N8 + i < N) at[i] = __ushort_as_bfloat16((unsigned short)(w[i / 2] >> (16 * (i & 1))));
+          }
         } else {
-          plain_box<false>(p.out, p.out_ld, row0, col0, M, N, box, lane);
+          plain_box(p.out, p.out_ld, row0, col0, M, N, box, lane);
           fence_async_smem();
           __syncwarp();
         }
       }
-      if (RES && lane == 0) {
+      if (RES && leader) {
         bulk_wait_read<0>();
         fetch_residual(t + step);
       }
       __syncwarp();
     }
-    if (lane == 0) {
+    if (leader) {
       bulk_wait_all();
       // a residual still on its way (only after a wait ran out) must land before the block ends
       volatile uint32_t never = 0;
@@ -349,6 +351,8 @@ k_dense8_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     }
   }
 
+  __syncwarp();
+  issued = __reduce_max_sync(0xFFFFFFFFu, issued);     // (the leader's)
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) {               // (pair: rank 0's barriers count both blocks' copies)
@@ -427,7 +431,7 @@ cudaError_t launch_shape(const DenseArgs& a, int sm_count, cudaStream_t st) {
   if (!kern) return cudaErrorInvalidValue;
   alignas(64) CUtensorMap map_a, map_w, map_out, map_res;
   if (!make_tensor_map_8bit(&map_a, a.a, a.m, a.k, a.a_ld, DM) || !make_tensor_map_8bit(&map_w, a.w, a.n, a.k, a.w_ld, BN / CTAS) ||
-      !make_tensor_map_bf16_box64_pitch(&map_out, a.out, a.m, a.n, a.out_ld) ||
+      !make_tensor_map_bf16_box64_pitch(&map_out, a.out, a.m, a.n >= 8 ? a.n & ~7u : 8u, a.out_ld) ||
       !make_tensor_map_bf16_box64_pitch(&map_res, a.residual ? a.residual : a.out, a.m, a.n, a.residual ? a.residual_ld : a.out_ld))
     return cudaErrorInvalidValue;
   const unsigned long long tiles = (unsigned long long)((a.m + CTAS * DM - 1) / (CTAS * DM)) * ((a.n + BN - 1) / BN);
