@@ -35,11 +35,13 @@ struct DenseArgs {
   VtOut vt;                        // the layer's transposed V columns
 };
 cudaError_t setup_dense8_tc();
-cudaError_t launch_dense8_tc(const DenseArgs& a, int sm_count, cudaStream_t st);
-// a long k shared by clusters of blocks: how many blocks per tile (1: not worth it)
-constexpr uint32_t SPLIT_LEAST = 24;               // steps of 128 bytes of k, at least
+// the form of the tensor-core kernels that takes least, and what it takes; dev: the current device, which has been set up
+struct DenseForm { int form; float us; };
+DenseForm choose_dense8_tc(const DenseArgs& a, int dev, int sm_count);
+cudaError_t launch_dense8_tc(const DenseArgs& a, int form, int dev, int sm_count, cudaStream_t st);
+// k shared by clusters of 2, 4 or 8 blocks; how many of them run at a time on device dev, which has been set up
 cudaError_t setup_dense8_split();
-uint32_t dense8_split_parts(const DenseArgs& a);
+uint32_t dense8_clusters(int dev, uint32_t parts);
 cudaError_t launch_dense8_split(const DenseArgs& a, uint32_t parts, cudaStream_t st);
 // up to 32 rows
 cudaError_t launch_dense8_few(const DenseArgs& a, int sm_count, cudaStream_t st);

@@ -54,15 +54,28 @@ constexpr uint32_t MOST_ROWS = 0x7FFFFFFFu;
 
 namespace llmc {
 
+// What k_dense8_few takes, in us: a launch, and the bytes of weights that the busiest SM has to read, at the rate at which its warps feed
+// mma.sync with 8, 16 or 32 tokens.  (Measured at 64 x 512 to 50,257 x 768 and 8,192 x 8,192.)
+static float few_time(const DenseArgs& a, int sm_count) {
+  constexpr float FIXED[2][3] = {{1.8f, 2.3f, 2.7f}, {1.8f, 2.3f, 3.9f}};
+  constexpr float PER_BYTE[2][3] = {{28e-6f, 38e-6f, 52e-6f}, {30e-6f, 55e-6f, 92e-6f}};        // int8, e4m3
+  const int t = a.format == LLMCACHE_I8 ? 0 : 1, n = a.m <= 8 ? 0 : a.m <= 16 ? 1 : 2;
+  const float one = 16.0f * a.k, all = (float)a.n * a.k / sm_count;
+  return FIXED[t][n] + PER_BYTE[t][n] * (one > all ? one : all);
+}
+
 cudaError_t launch_dense8(const DenseArgs& a, int sm_count, cudaStream_t st) {
   if (a.m == 0) return cudaSuccess;
-  // Up to 8 rows the weights are all there is to read.  Beyond that the other kernel's 128-row tiles pay once their copies come from
-  // half of the SMs or more (8,192 x 8,192: 16 rows of e4m3 29 us here, 22 there; 32 rows of int8 36 and 22); with fewer tiles the
-  // streams through registers are quicker up to 32 rows (1,024 x 4,096: 5.8 and 8.4; 4,096 x 1,024: 4.4 and 6.1; 64 rows: 10.8 and 8.4, 5.8 and 6.1).
-  const bool wide = 2ull * ((a.n + 63) / 64) >= (unsigned long long)sm_count;
-  const uint32_t most = !wide ? 32u : a.format == LLMCACHE_I8 ? 16u : 8u;
-  if (a.m <= most && !a.vt.ptr) return launch_dense8_few(a, sm_count, st);
-  return launch_dense8_tc(a, sm_count, st);
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return cudaErrorInvalidDevice;
+  // Up to 8 rows (16 of int8) the weights are all there is to read, and a stream of them through registers is never behind (1,024 x 4,096, 8 rows: 3.1 us, 6.6
+  // the other way; 8,192 x 8,192, 16 rows of int8 17 and 17); up to 32 it depends on how many there are (32 rows of int8, 1,024 x 4,096: 5.7 and
+  // 6.0; 4,096 x 1,024: 4.5 and 5.6; 8,192 x 8,192: 36 and 17; 50,257 x 768: 22 and 13).
+  const uint32_t always = a.format == LLMCACHE_I8 ? 16 : 8;
+  if (a.m <= always && !a.vt.ptr) return launch_dense8_few(a, sm_count, st);
+  const DenseForm f = choose_dense8_tc(a, dev, sm_count);
+  if (a.m <= 32 && !a.vt.ptr && few_time(a, sm_count) < f.us) return launch_dense8_few(a, sm_count, st);
+  return launch_dense8_tc(a, f.form, dev, sm_count, st);
 }
 
 }  // namespace llmc

@@ -272,17 +272,7 @@ cudaError_t setup_dense8_split() {
   return e;
 }
 
-uint32_t dense8_split_parts(const DenseArgs& a) {
-  int dev = 0;
-  if (a.vt.ptr || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return 1;
-  const unsigned long long tiles = (unsigned long long)((a.m + SM_ROWS - 1) / SM_ROWS) * ((a.n + SN - 1) / SN);
-  const uint32_t KB = (a.k + SK - 1) / SK;
-  // The largest cluster with which all tiles are at work at a time (a second wave costs more than it all), where k is long: meeting and
-  // sending costs about 3.5 us, a step of k 0.23 us (1,024 columns: k of 4,096 12.4 us alone, 8.4 with 4 blocks; k of 1,024 5.6 and 6.6).
-  for (int i = 2; i >= 0 && KB >= SPLIT_LEAST; --i)
-    if (tiles <= (unsigned long long)g_clusters[dev][i]) return 2u << i;
-  return 1;
-}
+uint32_t dense8_clusters(int dev, uint32_t parts) { return (uint32_t)g_clusters[dev][parts == 2 ? 0 : parts == 4 ? 1 : 2]; }
 
 cudaError_t launch_dense8_split(const DenseArgs& a, uint32_t parts, cudaStream_t st) {
   alignas(64) CUtensorMap map_a, map_w;

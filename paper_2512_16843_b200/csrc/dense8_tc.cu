@@ -424,23 +424,19 @@ cudaError_t setup_shape() {
   return cudaSuccess;
 }
 
+// most: pairs or blocks that run at a time
 template <int CTAS, int BN>
-cudaError_t launch_shape(const DenseArgs& a, int sm_count, cudaStream_t st) {
+cudaError_t launch_shape(const DenseArgs& a, uint32_t most, cudaStream_t st) {
   const DenseKernel kern = a.format == LLMCACHE_I8 ? kernel_of<CTAS, BN, true>(a.act, a.residual != nullptr, a.vt.ptr != nullptr)
                                                    : kernel_of<CTAS, BN, false>(a.act, a.residual != nullptr, a.vt.ptr != nullptr);
   if (!kern) return cudaErrorInvalidValue;
   alignas(64) CUtensorMap map_a, map_w, map_out, map_res;
   if (!make_tensor_map_8bit(&map_a, a.a, a.m, a.k, a.a_ld, DM) || !make_tensor_map_8bit(&map_w, a.w, a.n, a.k, a.w_ld, BN / CTAS) ||
-      !make_tensor_map_bf16_box64_pitch(&map_out, a.out, a.m, a.n >= 8 ? a.n & ~7u : 8u, a.out_ld) ||
-      !make_tensor_map_bf16_box64_pitch(&map_res, a.residual ? a.residual : a.out, a.m, a.n, a.residual ? a.residual_ld : a.out_ld))
+      !make_tensor_map_bf16_box64_pitch(&map_out, a.out, a.m, a.n >= 8 ? a.n & ~7u : 8u, a.out_ld))
     return cudaErrorInvalidValue;
+  if (!a.residual) map_res = map_out;                  // (not used)
+  else if (!make_tensor_map_bf16_box64_pitch(&map_res, a.residual, a.m, a.n, a.residual_ld)) return cudaErrorInvalidValue;
   const unsigned long long tiles = (unsigned long long)((a.m + CTAS * DM - 1) / (CTAS * DM)) * ((a.n + BN - 1) / BN);
-  uint32_t most = (uint32_t)sm_count;
-  if (CTAS == 2) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES || !g_pairs[dev]) return cudaErrorInvalidDevice;
-    most = (uint32_t)g_pairs[dev];
-  }
   cudaLaunchAttribute attr[2];
   const cudaLaunchConfig_t cfg = shape_config<CTAS, BN>(attr, (tiles < most ? (uint32_t)tiles : most) * CTAS, st);
   return cudaLaunchKernelEx(&cfg, kern, map_a, map_w, map_out, map_res, a);
@@ -468,13 +464,44 @@ cudaError_t setup_dense8_tc() {
   return e;
 }
 
-cudaError_t launch_dense8_tc(const DenseArgs& a, int sm_count, cudaStream_t st) {
-  // the largest tile that gives every SM one
-  const unsigned long long mb = (a.m + DM - 1) / DM, sms = (unsigned long long)sm_count;
-  if ((mb + 1) / 2 * ((a.n + 255) / 256) * 2 >= sms) return launch_shape<2, 256>(a, sm_count, st);
-  if (mb * ((a.n + 127) / 128) >= sms) return launch_shape<1, 128>(a, sm_count, st);
-  const uint32_t parts = dense8_split_parts(a);
-  return parts > 1 ? launch_dense8_split(a, parts, st) : launch_shape<1, 64>(a, sm_count, st);
+// What a form of the kernel takes, in us: `fixed` with the first tile's epilogue, a step for each 128 bytes of a tile's k, and for every further tile
+// of a block as many steps again, or the epilogue where that is longer (`tile`, more with a residual).  A block's step is bound by its
+// copies' rows of 128 bytes (0.8 ns each; 1.08 where rows do not start on 128 bytes, 1.5 where not on 32) or by its instructions.  Fitted to 114 products of 34
+// to 32,000 rows, 64 to 20,000 columns and k of 64 to 8,192, each timed in all forms; taking the least of these comes out 0.5 % above the best
+// form of each.  (The largest tile that gives every SM one, which was the rule before: 3,743 x 1,019 x 8,144 53 us where pairs take 34; 2,056 x 671 x 5,008
+// 27 and 20.5 in 128 x 128; 2,500 x 2,304 x 768 13.5 and 11.2.)
+struct FormTime { float fixed, instructions, tile, residual; };
+constexpr FormTime T_PAIR{8.4f, 0.272f, 2.9f, 1.6f}, T_128{4.8f, 0.f, 2.2f, 0.8f}, T_64{3.9f, 0.19f, 1.7f, 0.45f};
+constexpr FormTime T_SPLIT[3] = {{4.7f, 0.19f, 0.f, 0.f}, {4.75f, 0.19f, 0.f, 0.f}, {4.5f, 0.19f, 0.f, 0.f}};        // 2, 4, 8 blocks
+float form_time(const DenseArgs& a, const FormTime& f, uint32_t rows_a, uint32_t rows_w, unsigned long long tiles, unsigned long long at_a_time, uint32_t steps) {
+  auto row = [](long long ld) { return ld % 32 ? 1.5e-3f : ld % 128 ? 1.08e-3f : 0.8e-3f; };
+  const float copies = rows_a * row(a.a_ld) + rows_w * row(a.w_ld), k = steps * (copies > f.instructions ? copies : f.instructions);
+  const float further = f.tile + (a.residual ? f.residual : 0.f) + 0.12f * steps;
+  return f.fixed + k + (float)((tiles + at_a_time - 1) / at_a_time - 1) * (k > further ? k : further);
+}
+
+DenseForm choose_dense8_tc(const DenseArgs& a, int dev, int sm_count) {
+  const uint32_t steps = (a.k + DK - 1) / DK;
+  const unsigned long long mb = (a.m + DM - 1) / DM, sms = (unsigned long long)sm_count, tiles64 = mb * ((a.n + 63) / 64);
+  DenseForm best{0, form_time(a, T_PAIR, DM, 128, (mb + 1) / 2 * ((a.n + 255) / 256), (unsigned long long)g_pairs[dev], steps)};
+  auto consider = [&](int form, float us) { if (us < best.us) best = DenseForm{form, us}; };
+  consider(1, form_time(a, T_128, DM, 128, mb * ((a.n + 127) / 128), sms, steps));
+  consider(2, form_time(a, T_64, DM, 64, tiles64, sms, steps));
+  // clusters only where all tiles are at work at a time (a second wave costs more than it all), and every block has a step
+  for (int i = 0; i < 3 && !a.vt.ptr; ++i) {
+    const uint32_t parts = 2u << i;
+    if (steps >= parts && tiles64 <= dense8_clusters(dev, parts)) consider(3 + i, form_time(a, T_SPLIT[i], DM, 64, 1, 1, (steps + parts - 1) / parts));
+  }
+  return best;
+}
+
+cudaError_t launch_dense8_tc(const DenseArgs& a, int form, int dev, int sm_count, cudaStream_t st) {
+  switch (form) {
+    case 0: return launch_shape<2, 256>(a, (uint32_t)g_pairs[dev], st);
+    case 1: return launch_shape<1, 128>(a, (uint32_t)sm_count, st);
+    case 2: return launch_shape<1, 64>(a, (uint32_t)sm_count, st);
+    default: return launch_dense8_split(a, 2u << (form - 3), st);
+  }
 }
 
 }  // namespace llmc
