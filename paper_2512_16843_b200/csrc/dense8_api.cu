@@ -57,7 +57,7 @@ namespace llmc {
 // What k_dense8_few takes, in us: a launch, and the bytes of weights that the busiest SM has to read, at the rate at which its warps feed
 // mma.sync with 8, 16 or 32 tokens.  (Measured at 64 x 512 to 50,257 x 768 and 8,192 x 8,192.)
 static float few_time(const DenseArgs& a, int sm_count) {
-  constexpr float FIXED[2][3] = {{1.8f, 2.3f, 2.7f}, {1.8f, 2.3f, 3.9f}};
+  constexpr float FIXED[2][3] = {{1.8f, 2.3f, 2.7f}, {1.8f, 2.3f, 4.4f}};
   constexpr float PER_BYTE[2][3] = {{28e-6f, 38e-6f, 52e-6f}, {30e-6f, 55e-6f, 92e-6f}};        // int8, e4m3
   const int t = a.format == LLMCACHE_I8 ? 0 : 1, n = a.m <= 8 ? 0 : a.m <= 16 ? 1 : 2;
   const float one = 16.0f * a.k, all = (float)a.n * a.k / sm_count;

@@ -22,6 +22,11 @@ __device__ __forceinline__ uint4 ld16(const void* p) {
   asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
   return v;
 }
+// the same into shared memory while the thread goes on; not `there`: zeros
+__device__ __forceinline__ void ld16_async(uint32_t to, const void* p, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p), "r"(there ? 16u : 0u) : "memory");
+}
+__device__ __forceinline__ void ld16_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 typedef unsigned long long f2;           // two neighbouring columns in f32
 __device__ __forceinline__ f2 bf16_2(uint32_t w) { return f2_pack(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
 __device__ __forceinline__ uint32_t to_bf16(f2 v) {
@@ -104,11 +109,19 @@ struct Shape {
   static constexpr uint32_t THREADS = TPR <= 32 ? 128 : TPR, ROWS = THREADS / TPR;
 };
 
+// Rows of 256 threads with four pieces each and more: their next row waits in shared memory, each thread's pieces in its own place, so that
+// registers are left for more blocks, that is more rows on their way through the reductions at a time.
+template <int TPR, int CH>
+constexpr bool STAGED = TPR == 256 && CH >= 4;
+// blocks per SM that the registers are to be enough for (0: as many as come of it)
+template <int TPR, int CH>
+constexpr int BLOCKS = !STAGED<TPR, CH> ? (TPR == 256 && CH == 3 ? 2 : 0) : CH <= 6 ? 3 : 2;
+
 // TPR threads per row, CH pieces of eight elements each.  A thread's columns are the same in every row, so gains and biases stay in
 // registers where there is room for them (KEEP): read again for every row they keep the first-level cache busy for longer than the row takes
 // (1,536 columns, rms without residual: 94 us per 105 M elements, 73 with KEEP).
 template <int TPR, int CH, int KIND>
-__global__ void __launch_bounds__(Shape<TPR>::THREADS)
+__global__ void __launch_bounds__(Shape<TPR>::THREADS, (BLOCKS<TPR, CH>))
 k_norm(const NormArgs a) {
   griddep_sync();
   constexpr uint32_t ROWS = Shape<TPR>::ROWS;
@@ -120,15 +133,23 @@ k_norm(const NormArgs a) {
   const uint32_t rows = rows_of(a.n_rows, a.count_dev, a.rows_per_count);
   const uint32_t me = threadIdx.x % TPR, pieces = a.cols / 8;
   const float per = 1.0f / (float)a.cols;
-  uint4 v[CH], r[CH];
+  extern __shared__ __align__(16) uint8_t stage[];      // a thread's pieces of its next row; the residual's behind all threads'
+  const uint32_t mine = STAGED<TPR, CH> ? smem_u32(stage) + threadIdx.x * 16 : 0u;
+  uint4 v[STAGED<TPR, CH> ? 1 : CH], r[STAGED<TPR, CH> ? 1 : CH];
   auto fetch = [&](uint32_t row) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const uint32_t c = me + (uint32_t)i * TPR;
-      v[i] = r[i] = make_uint4(0, 0, 0, 0);
-      if (c < pieces && row < rows) {
-        v[i] = ld16(a.x + (long long)row * a.x_ld + c * 8);
-        if (a.residual) r[i] = ld16(a.residual + (long long)row * a.residual_ld + c * 8);
+      const bool there = c < pieces && row < rows;
+      if constexpr (STAGED<TPR, CH>) {
+        ld16_async(mine + i * TPR * 16, there ? a.x + (long long)row * a.x_ld + c * 8 : a.x, there);
+        if (a.residual) ld16_async(mine + (CH + i) * TPR * 16, there ? a.residual + (long long)row * a.residual_ld + c * 8 : a.residual, there);
+      } else {
+        v[i] = r[i] = make_uint4(0, 0, 0, 0);
+        if (there) {
+          v[i] = ld16(a.x + (long long)row * a.x_ld + c * 8);
+          if (a.residual) r[i] = ld16(a.residual + (long long)row * a.residual_ld + c * 8);
+        }
       }
     }
   };
@@ -153,9 +174,15 @@ k_norm(const NormArgs a) {
   for (uint32_t first = blockIdx.x * ROWS; first < rows; first += step, row += step) {
     const bool ok = row < rows;
     f2 h[CH][4];
+    if constexpr (STAGED<TPR, CH>) ld16_async_wait();
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w}, e[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
+      if constexpr (STAGED<TPR, CH>) {
+        v[0] = lds16(mine + i * TPR * 16);
+        r[0] = a.residual ? lds16(mine + (CH + i) * TPR * 16) : make_uint4(0, 0, 0, 0);
+      }
+      const uint4 &x = v[STAGED<TPR, CH> ? 0 : i], &z = r[STAGED<TPR, CH> ? 0 : i];
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w}, e[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
       for (int u = 0; u < 4; ++u) h[i][u] = a.residual ? f2_add(bf16_2(w[u]), bf16_2(e[u])) : bf16_2(w[u]);
     }
@@ -232,19 +259,24 @@ k_norm(const NormArgs a) {
     // rows with a single reduction: its slot may be written again only when all have read it
     if (TPR > 32 && (KIND == NORM_NONE || (KIND == NORM_RMS && !a.q))) __syncthreads();
   }
+  if constexpr (STAGED<TPR, CH>) ld16_async_wait();      // (a block without a row: nothing of it is on its way when the block ends)
 }
 
 template <int TPR, int CH, int KIND>
 cudaError_t launch_shape(const NormArgs& a, int sm_count, cudaStream_t st) {
   constexpr uint32_t ROWS = Shape<TPR>::ROWS, THREADS = Shape<TPR>::THREADS;
   // as many blocks as run at a time: a second, partial wave of them would leave SMs idle
-  static std::atomic<int> resident{0};
-  int per_sm = resident.load(std::memory_order_relaxed);
+  const bool res = a.residual != nullptr;
+  const uint32_t smem = STAGED<TPR, CH> ? THREADS * CH * 16 * (res ? 2 : 1) : 0;
+  static std::atomic<int> resident[2]{};
+  int per_sm = resident[res].load(std::memory_order_relaxed);
   if (!per_sm) {
-    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k_norm<TPR, CH, KIND>, THREADS, 0);
+    cudaError_t e = cudaSuccess;
+    if (smem) e = cudaFuncSetAttribute(k_norm<TPR, CH, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, THREADS * CH * 32);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k_norm<TPR, CH, KIND>, THREADS, smem);
     if (e != cudaSuccess) return e;
     if (per_sm < 1) return cudaErrorInvalidConfiguration;
-    resident.store(per_sm, std::memory_order_relaxed);
+    resident[res].store(per_sm, std::memory_order_relaxed);
   }
   // With three large arrays or more besides q, reads and writes of fewer rows at a time are easier on the memory (1,024 columns, residual
   // and total: 124 us per 105 M elements with 12 blocks per SM, 114 with 10; with x and q alone 76 and 80).
@@ -252,7 +284,7 @@ cudaError_t launch_shape(const NormArgs& a, int sm_count, cudaStream_t st) {
   const unsigned long long cap = (unsigned long long)sm_count * per_sm;
   unsigned long long blocks = ((unsigned long long)a.n_rows + ROWS - 1) / ROWS;
   if (blocks > cap) blocks = cap;
-  return launch_k(k_norm<TPR, CH, KIND>, dim3((uint32_t)blocks), dim3(THREADS), 0, st, a);
+  return launch_k(k_norm<TPR, CH, KIND>, dim3((uint32_t)blocks), dim3(THREADS), smem, st, a);
 }
 
 template <int TPR, int KIND>
@@ -262,6 +294,10 @@ cudaError_t launch_width(const NormArgs& a, uint32_t ch, int sm_count, cudaStrea
     case 2: return launch_shape<TPR, 2, KIND>(a, sm_count, st);
     case 3: return launch_shape<TPR, 3, KIND>(a, sm_count, st);
     case 4: if constexpr (TPR > 32) return launch_shape<TPR, 4, KIND>(a, sm_count, st);
+    case 5: if constexpr (TPR == 256) return launch_shape<TPR, 5, KIND>(a, sm_count, st);
+    case 6: if constexpr (TPR == 256) return launch_shape<TPR, 6, KIND>(a, sm_count, st);
+    case 7: if constexpr (TPR == 256) return launch_shape<TPR, 7, KIND>(a, sm_count, st);
+    case 8: if constexpr (TPR == 256) return launch_shape<TPR, 8, KIND>(a, sm_count, st);
     default: return cudaErrorInvalidValue;
   }
 }
@@ -270,12 +306,14 @@ template <int KIND>
 cudaError_t launch_kind(const NormArgs& a, int sm_count, cudaStream_t st) {
   // As few threads without a piece of eight elements as there may be, with up to four pieces per thread (5,000 columns: 256 threads of three
   // pieces 104 us where 512 of two take 149); three per thread of a warp, whose registers hold the gains of no more (1,024 columns: 64
-  // threads of two 113 us, 32 of four 121).
-  const uint32_t pieces = a.cols / 8;
-  uint32_t best = 512, least = ~0u;
-  for (uint32_t threads = 8; threads <= 512; threads *= 2) {
+  // threads of two 113 us, 32 of four 121).  Up to eight for 256 threads,
+  // with the next row in shared memory: 2,988 x 9,272, rms 31 us, with 512 threads and the next row in registers 41; 4,000 x 12,288 49 and 59; 512 threads
+  // only where there is an SM for every row (8 rows of 12,680: 4.0 us, 4.2 with 256).
+  const uint32_t pieces = a.cols / 8, widest = a.n_rows <= (uint32_t)sm_count ? 512 : 256;
+  uint32_t best = widest, least = ~0u;
+  for (uint32_t threads = 8; threads <= widest; threads *= 2) {
     const uint32_t ch = (pieces + threads - 1) / threads, idle = threads * ch - pieces;
-    if (ch <= (threads <= 32 ? 3 : 4) && idle < least) { best = threads; least = idle; }
+    if (ch <= (threads <= 32 ? 3 : threads < widest || widest == 512 ? 4 : 8) && idle < least) { best = threads; least = idle; }
   }
   const uint32_t ch = (pieces + best - 1) / best;
   switch (best) {

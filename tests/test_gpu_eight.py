@@ -89,6 +89,11 @@ NORMS = [
     (600, 12296, "rms", False, True, True, "e4m3"),
     (400, 16384, "layer", True, False, True, "int8"),
     (611, 16384, "none", True, False, False, "int8"),
+    # rows of 256 threads whose next row waits in shared memory, with 4 to 7 pieces each
+    (170, 8192, "rms", False, False, True, "int8"),
+    (301, 8200, "layer", True, True, True, "e4m3"),
+    (1203, 12280, "rms", True, True, False, "int8"),
+    (149, 14000, "layer", False, False, False, "e4m3"),
 ]
 
 
@@ -164,7 +169,7 @@ def test_rows_that_are_zero_tiny_infinite_or_nan(to, cols):
     assert torch.equal(o[0], b.to(BF))
 
 
-@pytest.mark.parametrize("rows,cols", [(50, 768), (9, 4096), (3, 16384)])
+@pytest.mark.parametrize("rows,cols", [(50, 768), (9, 4096), (3, 16384), (600, 9000)])
 def test_norm_in_place_and_with_a_row_count(rows, cols):
     x, r, gain = rnd(rows, cols, seed=11), rnd(rows, cols, seed=12), torch.rand(cols, device=DEV) + 0.5
     t, o = torch.zeros_like(x), torch.zeros_like(x)
