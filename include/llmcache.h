@@ -643,7 +643,8 @@ typedef struct llmcache_norm_args {
 /* out[i][j] = bf16( act( a_scale[i] * w_scale[j] * sum_c a[i][c] * w[j][c] + bias[j] ) + residual[i][j] ),  i < m, j < n, c < k.
  * The sum is exact for LLMCACHE_I8 (32-bit integers) and f32 for LLMCACHE_E4M3; the rest is f32.  a and w have the same format.  a_ld and
  * w_ld count bytes from row to row, multiples of 16 and at least k; out_ld and residual_ld count elements, multiples of 8 and at
- * least n, which may be any number (columns n.. of out stay as they were).  They are not looked at where there is one row.  a, w,
+ * least n, which may be any number (columns n.. of out stay as they were).  (Rows of a and w that start on 32 bytes are read twice as fast as
+ * others, on 128 a little faster still.)  They are not looked at where there is one row.  a, w,
  * w_scale, bias, out and residual are 16-byte aligned.  residual may be out itself (same address, same leading dimension); out overlaps nothing
  * otherwise.  GELU is within 3.8e-5 of the function. */
 typedef struct llmcache_dense_args {

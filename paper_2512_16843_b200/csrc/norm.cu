@@ -4,7 +4,8 @@
 // h, y and the statistics are f32; h and y leave as bf16 where they are asked for.
 //
 // Bound by HBM: 2 bytes per element for each of x, residual, total and out that a call has, 1 for q, each moved once.  A
-// row therefore stays in registers between its three reductions (mean, squares, largest magnitude).
+// row therefore stays in registers between its three reductions (mean, squares, largest magnitude).  131,072 x 1,024 with residual and total to e4m3 takes
+// 144 us (6.5 TB/s), 4,001 x 4,096 to e4m3 9.2 (5.4), 12,288 x 768 to bf16 and int8 9.9 (4.8), 2,988 x 9,272 rms to int8 32 (2.6: see STAGED).
 #include <atomic>
 #include <cuda_fp8.h>
 #include "dense8.cuh"
@@ -14,6 +15,7 @@ namespace llmc {
 
 namespace {
 
+constexpr int MAX_DEVICES = 64;
 constexpr float NORM_TINY = 1e-30f;      // a row below this counts as zeros: its scale would lose its bits
 
 // plain 16-byte load, kept in issue order.  (Not the read-only path: outputs may take the place of inputs row by row.)
@@ -268,15 +270,17 @@ cudaError_t launch_shape(const NormArgs& a, int sm_count, cudaStream_t st) {
   // as many blocks as run at a time: a second, partial wave of them would leave SMs idle
   const bool res = a.residual != nullptr;
   const uint32_t smem = STAGED<TPR, CH> ? THREADS * CH * 16 * (res ? 2 : 1) : 0;
-  static std::atomic<int> resident[2]{};
-  int per_sm = resident[res].load(std::memory_order_relaxed);
+  static std::atomic<int> resident[MAX_DEVICES][2];       // (attributes belong to a device)
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return cudaErrorInvalidDevice;
+  int per_sm = resident[dev][res].load(std::memory_order_relaxed);
   if (!per_sm) {
     cudaError_t e = cudaSuccess;
     if (smem) e = cudaFuncSetAttribute(k_norm<TPR, CH, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, THREADS * CH * 32);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k_norm<TPR, CH, KIND>, THREADS, smem);
     if (e != cudaSuccess) return e;
     if (per_sm < 1) return cudaErrorInvalidConfiguration;
-    resident[res].store(per_sm, std::memory_order_relaxed);
+    resident[dev][res].store(per_sm, std::memory_order_relaxed);
   }
   // With three large arrays or more besides q, reads and writes of fewer rows at a time are easier on the memory (1,024 columns, residual
   // and total: 124 us per 105 M elements with 12 blocks per SM, 114 with 10; with x and q alone 76 and 80).
