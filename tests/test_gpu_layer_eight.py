@@ -86,6 +86,7 @@ LAYERS = [
     (130, 192, 3, 320, 2, True, True, True),
     (70, 768, 12, 2048, 2, True, True, False),
     (90, 256, 4, 1152, 1, False, False, True),
+    (100, 128, 2, 6400, 2, True, True, True),                # hidden rows that wait in shared memory while others take their place in 8 bits
 ]
 
 
