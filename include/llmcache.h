@@ -707,7 +707,9 @@ int llmcache_kv_append(llmcache_kv_t* kv, const llmcache_kv_new* rows, void* str
  * bf16 weights (workspace is not looked at).  workspace: device memory, 256-byte aligned, borrowed, of the size that
  * llmcache_layer_quantise_bytes tells; NULL => the library cudaMallocs it.  Attention, norms and residuals stay as they are.  Entries
  * that a bank stored before have the other weights' outputs: flush it (llmcache_evict).  Calling it again replaces the weights and waits
- * for the device, so it belongs outside any stream capture; a graph captured before reads the weights that were there, and must not be replayed. */
+ * for the device, so it belongs outside any stream capture; a graph captured before reads the weights that were there, and must not be replayed.
+ * A call that fails leaves the layer as it was; only one that fails with LLMCACHE_ERR_CUDA while it replaces weights in their own memory
+ * (the same workspace, or the library's) may leave it in bf16. */
 int llmcache_layer_quantise_bytes(llmcache_layer_t* layer, size_t* bytes_out);
 int llmcache_layer_quantise(llmcache_layer_t* layer, uint32_t format, void* workspace, size_t workspace_bytes, void* stream);
 /* Root-mean-square norms (on != 0) in place of both layer norms, with the layer's gains, biases and eps, in the calls that follow. */

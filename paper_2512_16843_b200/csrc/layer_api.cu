@@ -340,25 +340,28 @@ int llmcache_layer_quantise(llmcache_layer_t* L, uint32_t format, void* workspac
   int prev = 0;
   cudaGetDevice(&prev);
   if (prev != D.device && cudaSetDevice(D.device) != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
-  cudaError_t e = cudaSuccess;
+  const bool eight = format != LLMCACHE_BF16, was_eight = L->format != LLMCACHE_BF16;
+  cudaError_t e = eight ? setup_dense8_tc() : cudaSuccess;
   int rc = LLMCACHE_OK;
-  if (L->format != LLMCACHE_BF16) {                        // calls in flight still read the weights that are there
-    e = cudaDeviceSynchronize();
-    if (L->owns_ws8) cudaFree(L->ws8);
-    L->ws8 = nullptr;
-    L->owns_ws8 = false;
-    L->format = LLMCACHE_BF16;
-  }
-  if (e == cudaSuccess && format != LLMCACHE_BF16) {
-    e = setup_dense8_tc();
-    L->ws8 = (char*)workspace;
-    if (e == cudaSuccess && !workspace) {
-      if (cudaMalloc((void**)&L->ws8, need) != cudaSuccess) { cudaGetLastError(); L->ws8 = nullptr; rc = LLMCACHE_ERR_NOMEM; }
-      else L->owns_ws8 = true;
+  // The new weights' memory before anything of the layer changes: the caller's, the library's that is there already (its size depends on
+  // the layer alone), or new.
+  char* to = (char*)workspace;
+  bool fresh = false;
+  if (eight && !workspace) {
+    to = L->owns_ws8 ? L->ws8 : nullptr;
+    if (!to && e == cudaSuccess) {
+      fresh = cudaMalloc((void**)&to, need) == cudaSuccess;
+      if (!fresh) { cudaGetLastError(); rc = LLMCACHE_ERR_NOMEM; }
     }
-    char* at = L->ws8;
+  }
+  if (e == cudaSuccess && rc == LLMCACHE_OK && was_eight) e = cudaDeviceSynchronize();      // calls in flight still read the weights that are there
+  if (e == cudaSuccess && rc == LLMCACHE_OK && eight) {
+    if (was_eight && to < L->ws8 + need && L->ws8 < to + need) L->format = LLMCACHE_BF16;   // (the old weights go while the new ones come)
     const void* from[4] = {D.w_qkv, D.w_o, D.w_1, D.w_2};
-    for (int w = 0; w < 4 && e == cudaSuccess && rc == LLMCACHE_OK; ++w) {
+    const uint8_t* w8[4];
+    const float* s8[4];
+    char* at = to;
+    for (int w = 0; w < 4 && e == cudaSuccess; ++w) {
       uint32_t r, c;
       weight_shape(D, w, &r, &c);
       NormArgs a{};
@@ -367,17 +370,26 @@ int llmcache_layer_quantise(llmcache_layer_t* L, uint32_t format, void* workspac
       a.scale = (float*)at; at += up256((size_t)r * 4);
       a.n_rows = r; a.cols = c; a.kind = NORM_NONE; a.format = format; a.rows_per_count = 1;
       e = launch_norm(a, L->sm_count, (cudaStream_t)stream);
-      L->w8[w] = a.q;
-      L->s8[w] = a.scale;
+      w8[w] = a.q;
+      s8[w] = a.scale;
     }
-    if (e == cudaSuccess && rc == LLMCACHE_OK) {
+    if (e == cudaSuccess) {
+      if (L->owns_ws8 && to != L->ws8) cudaFree(L->ws8);
+      L->ws8 = to;
+      L->owns_ws8 = !workspace;
       L->format = format;
-    } else if (L->owns_ws8) {
-      cudaDeviceSynchronize();
-      cudaFree(L->ws8);
-      L->ws8 = nullptr;
-      L->owns_ws8 = false;
+      for (int w = 0; w < 4; ++w) { L->w8[w] = w8[w]; L->s8[w] = s8[w]; }
     }
+  }
+  if (e != cudaSuccess && fresh) {
+    cudaDeviceSynchronize();
+    cudaFree(to);
+  }
+  if (e == cudaSuccess && !eight && was_eight) {
+    if (L->owns_ws8) cudaFree(L->ws8);
+    L->ws8 = nullptr;
+    L->owns_ws8 = false;
+    L->format = LLMCACHE_BF16;
   }
   if (prev != D.device) cudaSetDevice(prev);
   if (e != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
