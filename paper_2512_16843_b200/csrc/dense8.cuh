@@ -34,6 +34,8 @@ struct DenseArgs {
   uint32_t* status;
   VtOut vt;                        // the layer's transposed V columns
 };
+// Sets the current device up for the operators with 8-bit values, on the first call: what launch_norm and launch_dense8 need.  Any thread may call it.
+cudaError_t setup_eight();
 cudaError_t setup_dense8_tc();
 // the form of the tensor-core kernels that takes least, and what it takes; dev: the current device, which has been set up
 struct DenseForm { int form; float us; };

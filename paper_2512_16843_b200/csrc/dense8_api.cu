@@ -22,9 +22,12 @@ int done(cudaError_t e) {
   return LLMCACHE_ERR_CUDA;
 }
 
-// the current device's entry, set up on first use
-int device_of_call(int* dev, Dev* out) {
-  if (cudaGetDevice(dev) != cudaSuccess || *dev < 0 || *dev >= MAX_DEVICES) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
+// The current device's entry, set up on first use.  All of the library's set-up of these kernels is here, behind one lock: launches read
+// what it writes without the lock, each behind a call of this function.
+cudaError_t ready(int* dev, Dev* out) {
+  const cudaError_t at = cudaGetDevice(dev);
+  if (at != cudaSuccess) return at;
+  if (*dev < 0 || *dev >= MAX_DEVICES) return cudaErrorInvalidDevice;
   std::lock_guard<std::mutex> lock(g_mu);
   Dev& d = g_dev[*dev];
   if (!d.ready) {
@@ -32,12 +35,12 @@ int device_of_call(int* dev, Dev* out) {
     cudaError_t e = cudaGetSymbolAddress((void**)&p, g_dense_status);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&d.sm_count, cudaDevAttrMultiProcessorCount, *dev);
     if (e == cudaSuccess) e = setup_dense8_tc();
-    if (e != cudaSuccess) return done(e);
+    if (e != cudaSuccess) return e;
     d.status = p;
     d.ready = true;
   }
   *out = d;
-  return LLMCACHE_OK;
+  return cudaSuccess;
 }
 
 // a matrix of `rows` rows: its leading dimension, a multiple of `step` and at least `cols` (of no account for a single row)
@@ -53,6 +56,12 @@ constexpr uint32_t MOST_ROWS = 0x7FFFFFFFu;
 }  // namespace
 
 namespace llmc {
+
+cudaError_t setup_eight() {
+  int dev = -1;
+  Dev d;
+  return ready(&dev, &d);
+}
 
 // What k_dense8_few takes, in us: a launch, and the bytes of weights that the busiest SM has to read, at the rate at which its warps feed
 // mma.sync with 8, 16 or 32 tokens.  (Measured at 64 x 512 to 50,257 x 768 and 8,192 x 8,192.)
@@ -104,8 +113,8 @@ int llmcache_norm(const llmcache_norm_args* n, void* stream) {
     return LLMCACHE_ERR_SHAPE;
   int dev = -1;
   Dev d;
-  const int rc = device_of_call(&dev, &d);
-  if (rc != LLMCACHE_OK) return rc;
+  const cudaError_t e = ready(&dev, &d);
+  if (e != cudaSuccess) return done(e);
   if (!pointer_on_device(n->x, dev)) return LLMCACHE_ERR_ARG;
   a.x = (const __nv_bfloat16*)n->x; a.residual = (const __nv_bfloat16*)n->residual;
   a.total = (__nv_bfloat16*)n->total; a.out = (__nv_bfloat16*)n->out;
@@ -135,8 +144,8 @@ int llmcache_dense(const llmcache_dense_args* v, void* stream) {
     return LLMCACHE_ERR_SHAPE;
   int dev = -1;
   Dev d;
-  const int rc = device_of_call(&dev, &d);
-  if (rc != LLMCACHE_OK) return rc;
+  const cudaError_t e = ready(&dev, &d);
+  if (e != cudaSuccess) return done(e);
   if (!pointer_on_device(v->a, dev)) return LLMCACHE_ERR_ARG;
   a.a = (const uint8_t*)v->a; a.w = (const uint8_t*)v->w; a.a_scale = v->a_scale; a.w_scale = v->w_scale; a.bias = v->bias;
   a.residual = (const __nv_bfloat16*)v->residual; a.out = (__nv_bfloat16*)v->out;

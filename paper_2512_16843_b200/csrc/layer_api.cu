@@ -341,7 +341,7 @@ int llmcache_layer_quantise(llmcache_layer_t* L, uint32_t format, void* workspac
   cudaGetDevice(&prev);
   if (prev != D.device && cudaSetDevice(D.device) != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
   const bool eight = format != LLMCACHE_BF16, was_eight = L->format != LLMCACHE_BF16;
-  cudaError_t e = eight ? setup_dense8_tc() : cudaSuccess;
+  cudaError_t e = eight ? setup_eight() : cudaSuccess;
   int rc = LLMCACHE_OK;
   // The new weights' memory before anything of the layer changes: the caller's, the library's that is there already (its size depends on
   // the layer alone), or new.

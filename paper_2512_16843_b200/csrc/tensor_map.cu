@@ -1,4 +1,5 @@
 // Host-side construction of TMA tensor maps.
+#include <mutex>
 #include "llmcache_internal.cuh"
 #include "ptx.cuh"
 #include "attn.cuh"
@@ -12,7 +13,10 @@ static EncodeTiledFn g_encode = nullptr;
 typedef CUresult (*PointerAttributeFn)(void*, CUpointer_attribute, CUdeviceptr);
 static PointerAttributeFn g_pointer = nullptr;
 
+// (objects of several kinds set themselves up with it, on any threads)
 cudaError_t tensor_map_setup() {
+  static std::mutex mu;
+  std::lock_guard<std::mutex> lock(mu);
   if (g_encode) return cudaSuccess;
   void* fn = nullptr;
   cudaDriverEntryPointQueryResult q;
