@@ -1,4 +1,8 @@
 """A layer whose weights are brought to 8 bits a second time: what a refused call leaves behind, and whose memory the weights use."""
+import subprocess
+import sys
+import textwrap
+
 import pytest
 import torch
 
@@ -111,3 +115,60 @@ def test_a_workspace_that_overlaps_the_one_before(shift):
     layer.quantise("e4m3", whole[shift:shift + need])
     assert torch.equal(forward(layer, x), want) and not torch.equal(want, other)
     layer.close()
+
+
+def test_first_calls_on_several_threads():
+    """In a process of its own: products and layers that are quantised, for the first time and all at once."""
+    code = textwrap.dedent("""
+        import threading, torch
+        from paper_2512_16843_b200 import binding as L
+        from paper_2512_16843_b200 import synth
+        torch.cuda.init()
+        g = torch.Generator(device="cuda").manual_seed(1)
+        sizes = [(1000, 1024, 512), (40, 64, 4096), (9, 300, 128), (300, 2000, 784)]
+        data = []
+        for m, n, k in sizes:
+            a, w = (torch.randn((r, k), generator=g, device="cuda").mul(20).to(torch.int8) for r in (m, n))
+            data.append((a, torch.ones(m, device="cuda"), w, torch.ones(n, device="cuda"), torch.zeros((m, (n + 7) // 8 * 8), dtype=torch.bfloat16, device="cuda")[:, :n]))
+        layers = [L.Layer(synth.layer_weights(128, 256, i, "cuda"), heads=2, seq_len=32, max_seqs=2) for i in range(4)]
+        x = synth.randn((2, 32, 128), 9, "cuda", torch.bfloat16)
+        outs = [torch.zeros_like(x) for _ in layers]
+        torch.cuda.synchronize()
+        start, errors = threading.Barrier(8), []
+        def run(f):
+            try:
+                start.wait()
+                f()
+            except Exception as e:
+                errors.append(e)
+        def product(d):
+            def f():
+                stream = torch.cuda.Stream()
+                for _ in range(50):
+                    L.llmcache_dense(*d, stream=stream)
+                stream.synchronize()
+            return f
+        def layer(l, o):
+            def f():
+                stream = torch.cuda.Stream()
+                for _ in range(5):
+                    l.quantise("int8", stream=stream)
+                    l.forward(x, o, stream=stream)
+                stream.synchronize()
+            return f
+        threads = [threading.Thread(target=run, args=(f,)) for f in [product(d) for d in data] + [layer(l, o) for l, o in zip(layers, outs)]]
+        for t in threads: t.start()
+        for t in threads: t.join()
+        assert not errors, errors
+        for a, sa, w, sw, out in data:
+            want = (a.double() @ w.double().t()).to(torch.bfloat16)
+            assert torch.equal(out, want)
+        for l, o in zip(layers, outs):
+            again = torch.zeros_like(x)
+            l.forward(x, again)
+            torch.cuda.synchronize()
+            assert torch.equal(o, again)
+        print("fine")
+    """)
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip().endswith("fine"), r.stdout + r.stderr
