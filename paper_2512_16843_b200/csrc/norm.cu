@@ -111,23 +111,30 @@ struct Shape {
   static constexpr uint32_t THREADS = TPR <= 32 ? 128 : TPR, ROWS = THREADS / TPR;
 };
 
+// Pieces of eight elements that a thread of a row's TPR may have.  At least: fewer would leave as many threads idle as half of them with twice
+// the pieces, and the choice takes those (launch_kind).
+template <int TPR>
+constexpr uint32_t LEAST_CH = TPR == 8 ? 1 : TPR <= 64 ? 2 : 3;
+template <int TPR>
+constexpr uint32_t MOST_CH = TPR <= 32 ? 3 : TPR == 256 ? 8 : 4;
+
 // Rows of 256 threads with four pieces each and more: their next row waits in shared memory, each thread's pieces in its own place, so that
 // registers are left for more blocks, that is more rows on their way through the reductions at a time.
-template <int TPR, int CH>
+template <int TPR, uint32_t CH>
 constexpr bool STAGED = TPR == 256 && CH >= 4;
 // blocks per SM that the registers are to be enough for (0: as many as come of it)
-template <int TPR, int CH>
-constexpr int BLOCKS = !STAGED<TPR, CH> ? (TPR == 256 && CH == 3 ? 2 : 0) : CH <= 6 ? 3 : 2;
+template <int TPR, uint32_t CH>
+constexpr int BLOCKS = !STAGED<TPR, CH> ? (TPR == 256 ? 2 : 0) : CH <= 6 ? 3 : 2;
 
 // TPR threads per row, CH pieces of eight elements each.  A thread's columns are the same in every row, so gains and biases stay in
 // registers where there is room for them (KEEP): read again for every row they keep the first-level cache busy for longer than the row takes
 // (1,536 columns, rms without residual: 94 us per 105 M elements, 73 with KEEP).
-template <int TPR, int CH, int KIND>
+template <int TPR, uint32_t CH, int KIND>
 __global__ void __launch_bounds__(Shape<TPR>::THREADS, (BLOCKS<TPR, CH>))
 k_norm(const NormArgs a) {
   griddep_sync();
   constexpr uint32_t ROWS = Shape<TPR>::ROWS;
-  constexpr bool KEEP = KIND != NORM_NONE && (TPR <= 128 || (TPR == 256 && CH <= 3));
+  constexpr bool KEEP = KIND != NORM_NONE && TPR <= 256 && !STAGED<TPR, CH>;
   __shared__ float slots[TPR > 32 ? 3 * (TPR / 32) : 1];
   float* const slot0 = slots;
   float* const slot1 = slots + (TPR > 32 ? TPR / 32 : 0);
@@ -264,7 +271,7 @@ k_norm(const NormArgs a) {
   if constexpr (STAGED<TPR, CH>) ld16_async_wait();      // (a block without a row: nothing of it is on its way when the block ends)
 }
 
-template <int TPR, int CH, int KIND>
+template <int TPR, uint32_t CH, int KIND>
 cudaError_t launch_shape(const NormArgs& a, int sm_count, cudaStream_t st) {
   constexpr uint32_t ROWS = Shape<TPR>::ROWS, THREADS = Shape<TPR>::THREADS;
   // as many blocks as run at a time: a second, partial wave of them would leave SMs idle
@@ -291,19 +298,11 @@ cudaError_t launch_shape(const NormArgs& a, int sm_count, cudaStream_t st) {
   return launch_k(k_norm<TPR, CH, KIND>, dim3((uint32_t)blocks), dim3(THREADS), smem, st, a);
 }
 
-template <int TPR, int KIND>
+template <int TPR, int KIND, uint32_t CH = LEAST_CH<TPR>>
 cudaError_t launch_width(const NormArgs& a, uint32_t ch, int sm_count, cudaStream_t st) {
-  switch (ch) {
-    case 1: return launch_shape<TPR, 1, KIND>(a, sm_count, st);
-    case 2: return launch_shape<TPR, 2, KIND>(a, sm_count, st);
-    case 3: return launch_shape<TPR, 3, KIND>(a, sm_count, st);
-    case 4: if constexpr (TPR > 32) return launch_shape<TPR, 4, KIND>(a, sm_count, st);
-    case 5: if constexpr (TPR == 256) return launch_shape<TPR, 5, KIND>(a, sm_count, st);
-    case 6: if constexpr (TPR == 256) return launch_shape<TPR, 6, KIND>(a, sm_count, st);
-    case 7: if constexpr (TPR == 256) return launch_shape<TPR, 7, KIND>(a, sm_count, st);
-    case 8: if constexpr (TPR == 256) return launch_shape<TPR, 8, KIND>(a, sm_count, st);
-    default: return cudaErrorInvalidValue;
-  }
+  if (ch == CH) return launch_shape<TPR, CH, KIND>(a, sm_count, st);
+  if constexpr (CH < MOST_CH<TPR>) return launch_width<TPR, KIND, CH + 1>(a, ch, sm_count, st);
+  return cudaErrorInvalidValue;
 }
 
 template <int KIND>
@@ -317,6 +316,7 @@ cudaError_t launch_kind(const NormArgs& a, int sm_count, cudaStream_t st) {
   uint32_t best = widest, least = ~0u;
   for (uint32_t threads = 8; threads <= widest; threads *= 2) {
     const uint32_t ch = (pieces + threads - 1) / threads, idle = threads * ch - pieces;
+    // (MOST_CH; 256 threads take five and more only where 512 are not to be had)
     if (ch <= (threads <= 32 ? 3 : threads < widest || widest == 512 ? 4 : 8) && idle < least) { best = threads; least = idle; }
   }
   const uint32_t ch = (pieces + best - 1) / best;
