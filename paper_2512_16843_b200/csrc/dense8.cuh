@@ -19,6 +19,7 @@ struct NormArgs {
   const uint32_t* count_dev;       // rows = min(n_rows, *count_dev * rows_per_count), or n_rows
   uint32_t rows_per_count;
 };
+cudaError_t setup_norm();
 cudaError_t launch_norm(const NormArgs& a, int sm_count, cudaStream_t st);
 
 // llmcache_dense_args, checked; leading dimensions in elements
@@ -46,6 +47,7 @@ cudaError_t setup_dense8_split();
 uint32_t dense8_clusters(int dev, uint32_t parts);
 cudaError_t launch_dense8_split(const DenseArgs& a, uint32_t parts, cudaStream_t st);
 // up to 32 rows
+cudaError_t setup_dense8_few();
 cudaError_t launch_dense8_few(const DenseArgs& a, int sm_count, cudaStream_t st);
 cudaError_t launch_dense8(const DenseArgs& a, int sm_count, cudaStream_t st);
 

@@ -35,6 +35,8 @@ cudaError_t ready(int* dev, Dev* out) {
     cudaError_t e = cudaGetSymbolAddress((void**)&p, g_dense_status);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&d.sm_count, cudaDevAttrMultiProcessorCount, *dev);
     if (e == cudaSuccess) e = setup_dense8_tc();
+    if (e == cudaSuccess) e = setup_dense8_few();
+    if (e == cudaSuccess) e = setup_norm();
     if (e != cudaSuccess) return e;
     d.status = p;
     d.ready = true;

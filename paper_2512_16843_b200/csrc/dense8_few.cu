@@ -119,6 +119,9 @@ __global__ void __launch_bounds__(512) k_dense8_few(const DenseArgs p) {
 }
 
 template <int NT>
+void (*kernel_for(bool i8))(const DenseArgs) { return i8 ? k_dense8_few<NT, true> : k_dense8_few<NT, false>; }
+
+template <int NT>
 cudaError_t launch_tokens(const DenseArgs& a, int sm_count, cudaStream_t st) {
   const uint32_t pieces = (a.k + 63) / 64, channels = (a.n + FEW_CH - 1) / FEW_CH;
   // three pieces of k or more for a warp, up to 8 warps; 16 only where the channels do not fill the SMs (8,192 x 8,192: 17 us
@@ -126,11 +129,21 @@ cudaError_t launch_tokens(const DenseArgs& a, int sm_count, cudaStream_t st) {
   const uint32_t most = channels * 8ull >= 24ull * (uint32_t)sm_count ? 8 : 16;
   const uint32_t want = pieces < 4 ? pieces : pieces < 16 ? 4 : pieces < 64 ? 8 : 16, warps = want < most ? want : most;
   const size_t smem = (size_t)warps * NT * 8 * FEW_CH * 4;
-  auto kern = a.format == LLMCACHE_I8 ? k_dense8_few<NT, true> : k_dense8_few<NT, false>;
-  return launch_k(kern, dim3(channels), dim3(warps * 32), smem, st, a);
+  return launch_k(kernel_for<NT>(a.format == LLMCACHE_I8), dim3(channels), dim3(warps * 32), smem, st, a);
 }
 
 }  // namespace
+
+// The kernels are loaded with the others' set-up, not with the first call that takes them, which may stand in a capture.
+cudaError_t setup_dense8_few() {
+  cudaFuncAttributes f;
+  for (const bool i8 : {true, false})
+    for (auto k : {kernel_for<1>(i8), kernel_for<2>(i8), kernel_for<4>(i8)}) {
+      const cudaError_t e = cudaFuncGetAttributes(&f, k);
+      if (e != cudaSuccess) return e;
+    }
+  return cudaSuccess;
+}
 
 cudaError_t launch_dense8_few(const DenseArgs& a, int sm_count, cudaStream_t st) {
   if (a.m <= 8) return launch_tokens<1>(a, sm_count, st);

@@ -306,6 +306,14 @@ int llmcache_layer_score_mods(llmcache_layer_t* L, const llmcache_score_mods* mo
 int llmcache_layer_rms(llmcache_layer_t* L, uint32_t on) {
   if (!L || on > 1) return LLMCACHE_ERR_ARG;
   if (on && !norm_serves(L->desc)) return LLMCACHE_ERR_UNSUPPORTED;
+  if (on) {
+    int prev = 0;
+    cudaGetDevice(&prev);
+    if (prev != L->desc.device && cudaSetDevice(L->desc.device) != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
+    const cudaError_t e = setup_eight();
+    if (prev != L->desc.device) cudaSetDevice(prev);
+    if (e != cudaSuccess) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
+  }
   L->rms = on != 0;
   return LLMCACHE_OK;
 }

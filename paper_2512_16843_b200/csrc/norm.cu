@@ -6,7 +6,6 @@
 // Bound by HBM: 2 bytes per element for each of x, residual, total and out that a call has, 1 for q, each moved once.  A
 // row therefore stays in registers between its three reductions (mean, squares, largest magnitude).  131,072 x 1,024 with residual and total to e4m3 takes
 // 144 us (6.5 TB/s), 4,001 x 4,096 to e4m3 9.2 (5.4), 12,288 x 768 to bf16 and int8 9.9 (4.8), 2,988 x 9,272 rms to int8 32 (2.6: see STAGED).
-#include <atomic>
 #include <cuda_fp8.h>
 #include "dense8.cuh"
 #include "ptx.cuh"
@@ -271,42 +270,61 @@ k_norm(const NormArgs a) {
   if constexpr (STAGED<TPR, CH>) ld16_async_wait();      // (a block without a row: nothing of it is on its way when the block ends)
 }
 
+template <int TPR, uint32_t CH>
+constexpr uint32_t stage_bytes(bool residual) { return STAGED<TPR, CH> ? Shape<TPR>::THREADS * CH * 16 * (residual ? 2 : 1) : 0; }
+// blocks per SM that run at a time, without and with a residual, on each device that has been set up
 template <int TPR, uint32_t CH, int KIND>
-cudaError_t launch_shape(const NormArgs& a, int sm_count, cudaStream_t st) {
-  constexpr uint32_t ROWS = Shape<TPR>::ROWS, THREADS = Shape<TPR>::THREADS;
-  // as many blocks as run at a time: a second, partial wave of them would leave SMs idle
+int g_resident[MAX_DEVICES][2];
+
+template <int TPR, uint32_t CH, int KIND>
+cudaError_t launch_shape(const NormArgs& a, int dev, int sm_count, cudaStream_t st) {
+  constexpr uint32_t ROWS = Shape<TPR>::ROWS;
   const bool res = a.residual != nullptr;
-  const uint32_t smem = STAGED<TPR, CH> ? THREADS * CH * 16 * (res ? 2 : 1) : 0;
-  static std::atomic<int> resident[MAX_DEVICES][2];       // (attributes belong to a device)
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return cudaErrorInvalidDevice;
-  int per_sm = resident[dev][res].load(std::memory_order_relaxed);
-  if (!per_sm) {
-    cudaError_t e = cudaSuccess;
-    if (smem) e = cudaFuncSetAttribute(k_norm<TPR, CH, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, THREADS * CH * 32);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k_norm<TPR, CH, KIND>, THREADS, smem);
-    if (e != cudaSuccess) return e;
-    if (per_sm < 1) return cudaErrorInvalidConfiguration;
-    resident[dev][res].store(per_sm, std::memory_order_relaxed);
-  }
-  // With three large arrays or more besides q, reads and writes of fewer rows at a time are easier on the memory (1,024 columns, residual
-  // and total: 124 us per 105 M elements with 12 blocks per SM, 114 with 10; with x and q alone 76 and 80).
+  int per_sm = g_resident<TPR, CH, KIND>[dev][res];
+  if (!per_sm) return cudaErrorInvalidDevice;           // (not set up)
+  // As many blocks as run at a time: a second, partial wave of them would leave SMs idle.  With three large arrays or more besides q, reads and
+  // writes of fewer rows at a time are easier on the memory (1,024 columns, residual and total: 124 us per 105 M elements with 12 blocks per SM, 114
+  // with 10; with x and q alone 76 and 80).
   if (1 + (a.residual != nullptr) + (a.total != nullptr) + (a.out != nullptr) >= 3) per_sm -= per_sm / 6;
   const unsigned long long cap = (unsigned long long)sm_count * per_sm;
   unsigned long long blocks = ((unsigned long long)a.n_rows + ROWS - 1) / ROWS;
   if (blocks > cap) blocks = cap;
-  return launch_k(k_norm<TPR, CH, KIND>, dim3((uint32_t)blocks), dim3(THREADS), smem, st, a);
+  return launch_k(k_norm<TPR, CH, KIND>, dim3((uint32_t)blocks), dim3(Shape<TPR>::THREADS), stage_bytes<TPR, CH>(res), st, a);
 }
 
 template <int TPR, int KIND, uint32_t CH = LEAST_CH<TPR>>
-cudaError_t launch_width(const NormArgs& a, uint32_t ch, int sm_count, cudaStream_t st) {
-  if (ch == CH) return launch_shape<TPR, CH, KIND>(a, sm_count, st);
-  if constexpr (CH < MOST_CH<TPR>) return launch_width<TPR, KIND, CH + 1>(a, ch, sm_count, st);
+cudaError_t launch_width(const NormArgs& a, uint32_t ch, int dev, int sm_count, cudaStream_t st) {
+  if (ch == CH) return launch_shape<TPR, CH, KIND>(a, dev, sm_count, st);
+  if constexpr (CH < MOST_CH<TPR>) return launch_width<TPR, KIND, CH + 1>(a, ch, dev, sm_count, st);
   return cudaErrorInvalidValue;
 }
 
+// the same shapes, set up on the current device
+template <int TPR, int KIND, uint32_t CH = LEAST_CH<TPR>>
+cudaError_t setup_width(int dev) {
+  cudaError_t e = cudaFuncSetAttribute(k_norm<TPR, CH, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, stage_bytes<TPR, CH>(true));
+  for (int res = 0; res < 2 && e == cudaSuccess; ++res) {
+    int per_sm = 0;
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k_norm<TPR, CH, KIND>, Shape<TPR>::THREADS, stage_bytes<TPR, CH>(res != 0));
+    if (e == cudaSuccess && per_sm < 1) e = cudaErrorInvalidConfiguration;
+    if (e == cudaSuccess) g_resident<TPR, CH, KIND>[dev][res] = per_sm;
+  }
+  if constexpr (CH < MOST_CH<TPR>) return e == cudaSuccess ? setup_width<TPR, KIND, CH + 1>(dev) : e;
+  return e;
+}
 template <int KIND>
-cudaError_t launch_kind(const NormArgs& a, int sm_count, cudaStream_t st) {
+cudaError_t setup_kind(int dev) {
+  cudaError_t e = setup_width<8, KIND>(dev);
+  if (e == cudaSuccess) e = setup_width<16, KIND>(dev);
+  if (e == cudaSuccess) e = setup_width<32, KIND>(dev);
+  if (e == cudaSuccess) e = setup_width<64, KIND>(dev);
+  if (e == cudaSuccess) e = setup_width<128, KIND>(dev);
+  if (e == cudaSuccess) e = setup_width<256, KIND>(dev);
+  return e == cudaSuccess ? setup_width<512, KIND>(dev) : e;
+}
+
+template <int KIND>
+cudaError_t launch_kind(const NormArgs& a, int dev, int sm_count, cudaStream_t st) {
   // As few threads without a piece of eight elements as there may be, with up to four pieces per thread (5,000 columns: 256 threads of three
   // pieces 104 us where 512 of two take 149); three per thread of a warp, whose registers hold the gains of no more (1,024 columns: 64
   // threads of two 113 us, 32 of four 121).  Up to eight for 256 threads,
@@ -321,24 +339,35 @@ cudaError_t launch_kind(const NormArgs& a, int sm_count, cudaStream_t st) {
   }
   const uint32_t ch = (pieces + best - 1) / best;
   switch (best) {
-    case 8: return launch_width<8, KIND>(a, ch, sm_count, st);
-    case 16: return launch_width<16, KIND>(a, ch, sm_count, st);
-    case 32: return launch_width<32, KIND>(a, ch, sm_count, st);
-    case 64: return launch_width<64, KIND>(a, ch, sm_count, st);
-    case 128: return launch_width<128, KIND>(a, ch, sm_count, st);
-    case 256: return launch_width<256, KIND>(a, ch, sm_count, st);
-    default: return launch_width<512, KIND>(a, ch, sm_count, st);
+    case 8: return launch_width<8, KIND>(a, ch, dev, sm_count, st);
+    case 16: return launch_width<16, KIND>(a, ch, dev, sm_count, st);
+    case 32: return launch_width<32, KIND>(a, ch, dev, sm_count, st);
+    case 64: return launch_width<64, KIND>(a, ch, dev, sm_count, st);
+    case 128: return launch_width<128, KIND>(a, ch, dev, sm_count, st);
+    case 256: return launch_width<256, KIND>(a, ch, dev, sm_count, st);
+    default: return launch_width<512, KIND>(a, ch, dev, sm_count, st);
   }
 }
 
 }  // namespace
 
+cudaError_t setup_norm() {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev < 0 || dev >= MAX_DEVICES)) e = cudaErrorInvalidDevice;
+  if (e == cudaSuccess) e = setup_kind<NORM_NONE>(dev);
+  if (e == cudaSuccess) e = setup_kind<NORM_LAYER>(dev);
+  return e == cudaSuccess ? setup_kind<NORM_RMS>(dev) : e;
+}
+
 cudaError_t launch_norm(const NormArgs& a, int sm_count, cudaStream_t st) {
   if (a.n_rows == 0) return cudaSuccess;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return cudaErrorInvalidDevice;
   switch (a.kind) {
-    case NORM_NONE: return launch_kind<NORM_NONE>(a, sm_count, st);
-    case NORM_LAYER: return launch_kind<NORM_LAYER>(a, sm_count, st);
-    case NORM_RMS: return launch_kind<NORM_RMS>(a, sm_count, st);
+    case NORM_NONE: return launch_kind<NORM_NONE>(a, dev, sm_count, st);
+    case NORM_LAYER: return launch_kind<NORM_LAYER>(a, dev, sm_count, st);
+    case NORM_RMS: return launch_kind<NORM_RMS>(a, dev, sm_count, st);
     default: return cudaErrorInvalidValue;
   }
 }

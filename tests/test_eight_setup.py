@@ -46,3 +46,16 @@ def test_all_public_entries_pass_through_it():
 def test_driver_entry_points_are_looked_up_behind_a_lock():
     body = dict(functions(code(os.path.join(CSRC, "tensor_map.cu"))))["tensor_map_setup"]
     assert 0 <= body.find("lock_guard") < body.find("g_encode")
+
+
+@pytest.mark.parametrize("name", ["setup_norm", "setup_dense8_few"])
+def test_norm_and_few_rows_are_set_up_with_the_others(name):
+    assert callers(name) == {("dense8_api.cu", "ready")}
+
+
+def test_nothing_is_set_up_by_a_launch():
+    for file in ("norm.cu", "dense8_tc.cu", "dense8_split.cu", "dense8_few.cu"):
+        for f, body in functions(code(os.path.join(CSRC, file))):
+            if "cudaFuncSetAttribute" in body or "cudaOccupancyMax" in body:
+                assert f.startswith("setup_"), (file, f)
+    assert "setup_eight()" in dict(functions(code(os.path.join(CSRC, "layer_api.cu"))))["llmcache_layer_rms"]
