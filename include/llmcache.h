@@ -669,7 +669,14 @@ int llmcache_dense(const llmcache_dense_args* args, void* stream);
 /* LLMCACHE_OK, or LLMCACHE_ERR_TIMEOUT once a bounded device-side wait of llmcache_dense has expired on the current device
  * (sticky).  Synchronises the device. */
 int llmcache_dense_status(void);
-/* As llmcache_bank_debug_knobs, for llmcache_dense on the current device (which it must have run on before). */
+/* As llmcache_bank_debug_knobs, for llmcache_dense on the current device (which it must have run on before).  Bits 8 to 11 of flags, where they are
+ * not zero, name the form of the kernel that llmcache_dense takes there from then on instead of the one with the least estimated time: tiles of
+ * 256 x 256 by pairs of blocks, of 128 x 128, of 128 x 64, clusters of 2, 4 or 8 blocks that share a tile's k, weights through registers.
+ * A call that the form cannot serve (clusters: at least as many blocks of 128 bytes of k as blocks; registers: at most 32 rows) is refused with
+ * LLMCACHE_ERR_UNSUPPORTED.  Layers take no notice. */
+enum { LLMCACHE_DENSE_PAIRS = 1, LLMCACHE_DENSE_128 = 2, LLMCACHE_DENSE_64 = 3, LLMCACHE_DENSE_CLUSTERS_2 = 4, LLMCACHE_DENSE_CLUSTERS_4 = 5,
+       LLMCACHE_DENSE_CLUSTERS_8 = 6, LLMCACHE_DENSE_FEW = 7 };
+#define LLMCACHE_KNOB_DENSE_FORM(form) ((uint32_t)(form) << 8)
 int llmcache_dense_debug_knobs(uint64_t wait_limit_ns, uint32_t flags);
 
 /* Rotation of a head's columns by position: the pairs of columns (i, i + dims / 2) -- or (2 i, 2 i + 1), interleaved --, i < dims / 2,

@@ -49,6 +49,9 @@ EXPORTS = [
     "llmcache_layer_quantise_bytes", "llmcache_layer_quantise", "llmcache_layer_rms", "llmcache_layer_rotation",
 ]
 KNOB_PRODUCER_IDLE = 1
+# forms of the 8-bit product's kernel, for llmcache_dense_debug_knobs (flags = KNOB_DENSE_FORM * form)
+DENSE_PAIRS, DENSE_128, DENSE_64, DENSE_CLUSTERS_2, DENSE_CLUSTERS_4, DENSE_CLUSTERS_8, DENSE_FEW = 1, 2, 3, 4, 5, 6, 7
+KNOB_DENSE_FORM = 256
 FINGERPRINT_STATIC_MAX_FLOATS = 2 * 1024 * 1024
 KERNEL_NAMES = ["pool", "project", "rownorm", "scan", "decide", "touch", "gather", "select", "scatter", "evict",
                 "pool_finish"]

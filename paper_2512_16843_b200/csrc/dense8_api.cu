@@ -12,7 +12,7 @@ inline bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)
 
 __device__ __align__(16) uint32_t g_dense_status[4];
 constexpr int MAX_DEVICES = 64;
-struct Dev { bool ready = false; uint32_t* status = nullptr; int sm_count = 0; };
+struct Dev { bool ready = false; uint32_t* status = nullptr; int sm_count = 0; uint32_t form = 0; };      // form: llmcache_dense_debug_knobs
 Dev g_dev[MAX_DEVICES];
 std::mutex g_mu;
 
@@ -54,6 +54,14 @@ bool take_ld(int64_t ld, uint64_t rows, uint64_t cols, uint32_t step, long long*
 }
 
 constexpr uint32_t MOST_ROWS = 0x7FFFFFFFu;
+
+// whether a form that was asked for (llmcache_dense_debug_knobs) can serve a call; m is not zero
+bool form_serves(const DenseArgs& a, uint32_t form) {
+  if (form == LLMCACHE_DENSE_FEW) return a.m <= 32;
+  if (form < LLMCACHE_DENSE_CLUSTERS_2) return true;
+  const uint64_t parts = 2ull << (form - LLMCACHE_DENSE_CLUSTERS_2);
+  return (a.k + 127) / 128 >= parts && ((uint64_t)a.m + 127) / 128 * (((uint64_t)a.n + 63) / 64) * parts <= 0x7FFFFFFFull;
+}
 
 }  // namespace
 
@@ -154,30 +162,39 @@ int llmcache_dense(const llmcache_dense_args* v, void* stream) {
   a.m = v->m; a.n = v->n; a.k = v->k; a.act = v->act; a.format = v->format;
   a.count_dev = v->count_dev; a.rows_per_count = v->rows_per_count ? v->rows_per_count : 1;
   a.status = d.status;
+  if (d.form) {
+    if (!form_serves(a, d.form)) return LLMCACHE_ERR_UNSUPPORTED;
+    return done(d.form == LLMCACHE_DENSE_FEW ? launch_dense8_few(a, d.sm_count, (cudaStream_t)stream)
+                                             : launch_dense8_tc(a, (int)d.form - LLMCACHE_DENSE_PAIRS, dev, d.sm_count, (cudaStream_t)stream));
+  }
   return done(launch_dense8(a, d.sm_count, (cudaStream_t)stream));
 }
 
-static int dense_status_word(uint32_t** status) {
+int llmcache_dense_status(void) {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
-  std::lock_guard<std::mutex> lock(g_mu);
-  *status = g_dev[dev].ready ? g_dev[dev].status : nullptr;
-  return LLMCACHE_OK;
-}
-
-int llmcache_dense_status(void) {
   uint32_t *status = nullptr, s = 0;
-  const int rc = dense_status_word(&status);
-  if (rc != LLMCACHE_OK || !status) return rc;               // never used on this device: nothing to report
+  {
+    std::lock_guard<std::mutex> lock(g_mu);
+    if (!g_dev[dev].ready) return LLMCACHE_OK;               // never used on this device: nothing to report
+    status = g_dev[dev].status;
+  }
   if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&s, status, 4, cudaMemcpyDeviceToHost) != cudaSuccess) return done(cudaErrorUnknown);
   return s ? LLMCACHE_ERR_TIMEOUT : LLMCACHE_OK;
 }
 
 int llmcache_dense_debug_knobs(uint64_t wait_limit_ns, uint32_t flags) {
+  const uint32_t form = flags >> 8 & 15u;
+  if (form > LLMCACHE_DENSE_FEW) return LLMCACHE_ERR_ARG;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) { cudaGetLastError(); return LLMCACHE_ERR_CUDA; }
   uint32_t* status = nullptr;
-  const int rc = dense_status_word(&status);
-  if (rc != LLMCACHE_OK) return rc;
-  if (!status) return LLMCACHE_ERR_STATE;
+  {
+    std::lock_guard<std::mutex> lock(g_mu);
+    if (!g_dev[dev].ready) return LLMCACHE_ERR_STATE;
+    g_dev[dev].form = form;
+    status = g_dev[dev].status;
+  }
   const uint32_t w[3] = {flags, (uint32_t)(wait_limit_ns & 0xFFFFFFFFull), (uint32_t)(wait_limit_ns >> 32)};
   if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(status + 1, w, sizeof(w), cudaMemcpyHostToDevice) != cudaSuccess) return done(cudaErrorUnknown);
   return LLMCACHE_OK;
