@@ -615,6 +615,7 @@ enum { LLMCACHE_ACT_NONE = 0, LLMCACHE_ACT_GELU_ERF = 1, LLMCACHE_ACT_GELU_TANH 
  *     NONE: y = h      LAYER: y = (h - mean(h)) / sqrt(var(h) + eps) * gain + bias     RMS: y = h / sqrt(mean(h^2) + eps) * gain + bias
  *     total = bf16(h)      out = bf16(y)
  *     scale = max |y| / 127 (LLMCACHE_I8) or / 448 (LLMCACHE_E4M3), q = y / scale rounded to nearest even
+ * (The squares are f32 too: a row with magnitudes above 1.8e19 overflows them, and its normed values are the bias alone.)
  * A row of y below 1e-30 has scale 0 and zeros; a row with an infinity or NaN has a scale of NaN and zeros, so that products of
  * it are NaN.  Any of total, out and q may be left out, not all.  Leading dimensions (`_ld`) count elements from row to row,
  * multiples of 8 and at least cols; they are not looked at where there is one row.  x, residual, total, out, gain and bias are 16-byte aligned, q is
@@ -646,7 +647,8 @@ typedef struct llmcache_norm_args {
  * least n, which may be any number (columns n.. of out stay as they were).  (Rows of a and w that start on 32 bytes are read twice as fast as
  * others, on 128 a little faster still.)  They are not looked at where there is one row.  a, w,
  * w_scale, bias, out and residual are 16-byte aligned.  residual may be out itself (same address, same leading dimension); out overlaps nothing
- * otherwise.  GELU is within 3.8e-5 of the function. */
+ * otherwise.  GELU is within 3.8e-5 of the function; below arguments of -3, where the function itself is smaller than 0.004, that is more than the
+ * rounding to bf16 (2 % of it at -3.5; from -4.3 on the result is 0).  a_scale * sum is formed first and has to stay below 3.4e38. */
 typedef struct llmcache_dense_args {
   uint32_t struct_size;
   uint32_t format;           /* LLMCACHE_I8 | LLMCACHE_E4M3 */

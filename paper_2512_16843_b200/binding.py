@@ -698,7 +698,8 @@ class Layer:
 
     def quantise(self, to="int8", workspace=None, stream=None):
         """The layer's products in 8 bits (to: "int8" or "e4m3") in the calls that follow, from weights that this call brings to
-        that type on the stream; None: back to bf16.  workspace: a tensor of llmcache_layer_quantise_bytes bytes, or None."""
+        that type on the stream; None: back to bf16.  workspace: a tensor of llmcache_layer_quantise_bytes bytes, or None.  A call that
+        is refused leaves the layer as it was."""
         if to is not None and to not in _FORMATS:
             raise LLMCacheError(ERR_ARG, 'quantise: "int8", "e4m3" or None')
         if workspace is not None:
@@ -928,7 +929,7 @@ def llmcache_norm(x, *, kind="rms", gain=None, bias=None, eps=1e-5, residual=Non
                   n_rows_dev=None, stream=None) -> None:
     """h = x + residual -> total; its norm (kind: "rms", "layer", "none") -> out in bf16, q in 8 bits with a scale per row.
     x, residual, total, out: bf16 [rows, cols]; gain, bias: f32 [cols]; q: int8 or float8_e4m3fn [rows, cols], scale: f32
-    [rows].  n_rows_dev: int32 on the device, only that many rows are processed."""
+    [rows].  eps <= 0 stands for 1e-5.  n_rows_dev: int32 on the device, only that many rows are processed."""
     if not isinstance(x, torch.Tensor):
         raise LLMCacheError(ERR_ARG, "llmcache_norm: x is a tensor")
     kind_id = _NORMS.get(kind)

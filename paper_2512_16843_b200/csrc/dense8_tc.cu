@@ -7,8 +7,11 @@
 // tile (cta_group::2): each block loads its 128 rows of a and 128 of w and keeps 128 rows of the accumulator, so a block's copies are
 // 64 bytes per cycle at the tensor cores' full rate where a tile of its own would need 96.  Small ones take 128 x 128 or 128 x 64 per
 // block, or clusters that share their k (dense8_split.cu), by estimated time (below).  One elected lane of a warp issues copies, products and
-// commits: behind a branch on lane 0 the compiler issues each in a loop over lanes, and a step of k took 275 ns whatever the tile, 157 so.
-// 32,768 x 4,096 x 1,024 112 us, 120 with GELU (2,450 and 2,290 T operations per second); 65,536 x 1,024 x 4,096 178, e4m3 with residual 197; 1,001 x 50,257 x 768 44.
+// commits: behind a branch on lane 0 the compiler issues each in a loop over lanes, and a step of k of a block alone took 275 ns whatever its tile.  A step of
+// one tile alone, rows on 128 bytes, takes 157 ns for 128 x 128 (239 with rows on 32 bytes, 360 on 16), 192 for 128 x 64 (192, 270) and 262 to 292
+// for a pair's (the same, 360); with all SMs at work 195 to 225, 200 to 220 and 290 to 370.
+// 32,768 x 4,096 x 1,024 112 us, 120 to 127 with GELU (2,450 and 2,230 T operations per second); 65,536 x 1,024 x 4,096 179, e4m3 with residual 197 to 209;
+// 1,001 x 50,257 x 768 43 to 48.
 //
 // An epilogue warp has 32 rows x 64 columns of its own and a box of 4 KB in shared memory for them: the residual comes into
 // the box by TMA while the tile is still being summed, the result takes its place and leaves by TMA in rows of 128 bytes.  Warps meet
@@ -468,16 +471,19 @@ cudaError_t setup_dense8_tc() {
 
 // What a form of the kernel takes, in us: `fixed` with the first tile's epilogue, a step for each 128 bytes of a tile's k, and for every further tile
 // of a block as many steps again, or the epilogue where that is longer (`tile`, more with a residual).  A block's step is bound by its
-// copies' rows of 128 bytes (0.8 ns each; 1.08 where rows do not start on 128 bytes, 1.5 where not on 32) or by its instructions.  Fitted to 114 products of 34
-// to 32,000 rows, 64 to 20,000 columns and k of 64 to 8,192, each timed in all forms; taking the least of these comes out 0.5 % above the best
-// form of each.  (The largest tile that gives every SM one, which was the rule before: 3,743 x 1,019 x 8,144 53 us where pairs take 34; 2,056 x 671 x 5,008
-// 27 and 20.5 in 128 x 128; 2,500 x 2,304 x 768 13.5 and 11.2.)
+// copies' rows of 128 bytes (0.8 ns each; 1.08 where rows do not start on 128 bytes, 1.5 where not on 32) or by its instructions.  Fitted, with all SMs at
+// work, to products of 34 to 32,000 rows, 64 to 20,000 columns and k of 64 to 8,192, each timed in all forms; over 114 such products
+// (profiles/eight_bit_forms.md) taking the least of these is 0.9 % above the best form of each, 34 % at worst (45 x 3,292 x 1,360: 52 clusters of 2 take
+// 8.4 us, 128 x 64 6.2).  (The largest tile that gives every SM one, which was the rule before: 3,743 x 1,019 x 8,144 53 us where pairs take 34; 2,056 x 671 x
+// 5,008 27 and 20.5 in 128 x 128; 2,500 x 2,304 x 768 13.5 and 11.2.)  The activation is left out (GELU adds 8 % to a
+// pair's tile at k of 1,024).
 struct FormTime { float fixed, instructions, tile, residual; };
 constexpr FormTime T_PAIR{8.4f, 0.272f, 2.9f, 1.6f}, T_128{4.8f, 0.f, 2.2f, 0.8f}, T_64{3.9f, 0.19f, 1.7f, 0.45f};
 constexpr FormTime T_SPLIT[3] = {{4.7f, 0.19f, 0.f, 0.f}, {4.75f, 0.19f, 0.f, 0.f}, {4.5f, 0.19f, 0.f, 0.f}};        // 2, 4, 8 blocks
 float form_time(const DenseArgs& a, const FormTime& f, uint32_t rows_a, uint32_t rows_w, unsigned long long tiles, unsigned long long at_a_time, uint32_t steps) {
   auto row = [](long long ld) { return ld % 32 ? 1.5e-3f : ld % 128 ? 1.08e-3f : 0.8e-3f; };
   const float copies = rows_a * row(a.a_ld) + rows_w * row(a.w_ld), k = steps * (copies > f.instructions ? copies : f.instructions);
+  // (a tile's steps and the epilogue of the one before run side by side, but not at full speed: 0.12 us for each step, fitted with the rest)
   const float further = f.tile + (a.residual ? f.residual : 0.f) + 0.12f * steps;
   return f.fixed + k + (float)((tiles + at_a_time - 1) / at_a_time - 1) * (k > further ? k : further);
 }

@@ -5,7 +5,12 @@
 //
 // Bound by HBM: 2 bytes per element for each of x, residual, total and out that a call has, 1 for q, each moved once.  A
 // row therefore stays in registers between its three reductions (mean, squares, largest magnitude).  131,072 x 1,024 with residual and total to e4m3 takes
-// 144 us (6.5 TB/s), 4,001 x 4,096 to e4m3 9.2 (5.4), 12,288 x 768 to bf16 and int8 9.9 (4.8), 2,988 x 9,272 rms to int8 32 (2.6: see STAGED).
+// 144 us (6.5 TB/s), 98,304 x 768 layer norm to bf16 and int8 69 (5.5), 131,072 x 1,024 rms to bf16 alone 91 (5.9), 4,001 x 4,096 to e4m3 10.0 (4.9),
+// 12,288 x 768 layer norm to bf16 and int8 11.7 (4.0; 9.9 where part of it lies in L2).
+//
+// Where little is moved per element the work per row counts: its reductions are a chain, and the rows that an SM has registers for do not
+// cover it.  105 M elements of 1,024 columns from bf16 to int8 take 52 us without a norm and 76 with rms (48 are the bytes' time), of 2,048
+// 75, of 5,000 90; 2,988 x 9,272 18, 27 with rms and 42 with a residual and layer norm (12.7 and, with the residual, 21.1; see STAGED).
 #include <cuda_fp8.h>
 #include "dense8.cuh"
 #include "ptx.cuh"
@@ -328,7 +333,7 @@ cudaError_t launch_kind(const NormArgs& a, int dev, int sm_count, cudaStream_t s
   // As few threads without a piece of eight elements as there may be, with up to four pieces per thread (5,000 columns: 256 threads of three
   // pieces 104 us where 512 of two take 149); three per thread of a warp, whose registers hold the gains of no more (1,024 columns: 64
   // threads of two 113 us, 32 of four 121).  Up to eight for 256 threads,
-  // with the next row in shared memory: 2,988 x 9,272, rms 31 us, with 512 threads and the next row in registers 41; 4,000 x 12,288 49 and 59; 512 threads
+  // with the next row in shared memory: 2,988 x 9,272, rms and total to e4m3 31 us, with 512 threads and the next row in registers 41; 4,000 x 12,288 49 and 59; 512 threads
   // only where there is an SM for every row (8 rows of 12,680: 4.0 us, 4.2 with 256).
   const uint32_t pieces = a.cols / 8, widest = a.n_rows <= (uint32_t)sm_count ? 512 : 256;
   uint32_t best = widest, least = ~0u;
